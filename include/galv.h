@@ -397,6 +397,89 @@ int galv_skip_estimate(galv_ctx* ctx, const galv_shape* shape, const int32_t* L,
                        const int32_t* time_q, const int32_t* mem_q, const int32_t* trans_q,
                        int64_t* counts, void* stream);
 
+/*
+ * Microscaled tensors: what a plan's layers keep between their forward and backward pass in 8 bits instead of
+ * bytes_per_elem, and products of operands in 4 bits (the paper has no counterpart; the planner prices both with
+ * galv_add_form_cost, these calls carry them out).
+ *
+ * A matrix [rows][cols] is held in blocks of 32 consecutive columns of a row, nb = ceil(cols/32) of them, with one
+ * power of two a block: value = element * 2^(scale byte - 127).  The exponent is the smallest (not below -127) under
+ * which the block's largest magnitude does not pass the largest element, so that nothing saturates and an element is
+ * off by at most half a step; elements are rounded to nearest, ties to even.  A block that holds an infinity or a NaN
+ * gets scale byte 255 and stands for NaN as a whole.  Columns behind a row's end are held as zeros.
+ *   GALV_MX8: elements of 4 exponent and 3 mantissa bits (largest 448); codes [rows][nb*32] bytes;
+ *             scales [rows][nb rounded up to a multiple of 16] bytes, zero behind nb.
+ *   GALV_MX4: elements of 2 exponent bits and 1 mantissa bit (0, .5, 1, 1.5, 2, 3, 4, 6); codes [rows][nb*16] bytes, the
+ *             even column in the low half; scales in tiles of 128 rows x 4 blocks, [ceil(rows/128)][ceil(nb/4)] of them,
+ *             each [row % 32][row / 32 % 4][block % 4] bytes, zero behind rows and nb: the order in which the tensor
+ *             cores take them.
+ * codes and scales are 16-byte aligned.  Matrices of numbers are (pointer, row stride in elements >= the row's length,
+ * type), aligned to their element; 16-byte aligned rows are read and written faster.  fp16 results of a value that was
+ * held as a finite number saturate at 65504.  Limits: 0 <= rows, 1 <= cols, both < 2^31 - 128; no output may overlap an input but
+ * where a call says so.  Like the rest of the library these calls allocate nothing, run on `stream` of the
+ * context's device (whichever device is current) and may be captured in a CUDA graph; two calls that overlap on the GPU
+ * need workspaces of their own.
+ */
+#define GALV_F32 0
+#define GALV_BF16 1
+#define GALV_F16 2
+#define GALV_MX8 8
+#define GALV_MX4 4
+#define GALV_ACT_GELU 0      /* x Phi(x) */
+#define GALV_ACT_GELU_TANH 1 /* x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2 */
+#define GALV_ACT_SILU 2      /* x / (1 + exp(-x)) */
+#define GALV_NORM_LAYER 0    /* (x - mean) / sqrt(var + eps) * weight + bias */
+#define GALV_NORM_RMS 1      /* x / sqrt(mean(x^2) + eps) * weight */
+
+/* Bytes of codes and of scales for a matrix (0 on sizes or a format outside the limits, and for rows = 0). */
+size_t galv_mx_codes_bytes(int64_t rows, int64_t cols, int32_t fmt);
+size_t galv_mx_scales_bytes(int64_t rows, int64_t cols, int32_t fmt);
+/* x -> codes, scales; and back.  Every byte of codes and scales is written. */
+int galv_mx_pack(galv_ctx* ctx, int64_t rows, int64_t cols, const void* x, int64_t x_stride, int32_t dtype, int32_t fmt,
+                 uint8_t* codes, uint8_t* scales, void* stream);
+int galv_mx_unpack(galv_ctx* ctx, int64_t rows, int64_t cols, int32_t fmt, const uint8_t* codes, const uint8_t* scales,
+                   void* x, int64_t x_stride, int32_t dtype, void* stream);
+/* dx = dy * f'(x), the activation function's input x held in GALV_MX8.  dx may be dy (same pointer and stride). */
+int galv_mx_act_backward(galv_ctx* ctx, int64_t rows, int64_t cols, int32_t act, const uint8_t* codes, const uint8_t* scales,
+                         const void* dy, int64_t dy_stride, void* dx, int64_t dx_stride, int32_t dtype, void* stream);
+/*
+ * Gradients of a norm over each row whose input x is held in GALV_MX8: the norm's statistics are those of the held
+ * values, so the gradients are exactly the formula's at that point.  weight [cols] of `dtype`, NULL: ones.
+ * dweight = sum over rows of dy * xhat, dbias = sum over rows of dy (both fp32 [cols]; summed in a fixed order: the same call
+ * gives the same bits).  dweight may be NULL, dbias must be NULL for GALV_NORM_RMS and may be for the other.  eps >= 0;
+ * a row of equal values with eps = 0 gives NaN or infinity as the formula does.  With rows = 0 dweight and dbias are zeros.
+ * dx may be dy (same pointer and stride).  workspace: 256-byte aligned; it holds partial sums.
+ */
+size_t galv_mx_norm_workspace_bytes(const galv_ctx* ctx, int64_t rows, int64_t cols);
+int galv_mx_norm_backward(galv_ctx* ctx, int64_t rows, int64_t cols, int32_t kind, float eps, const uint8_t* codes,
+                          const uint8_t* scales, const void* dy, int64_t dy_stride, const void* weight, void* dx,
+                          int64_t dx_stride, int32_t dtype, float* dweight, float* dbias, void* workspace,
+                          size_t workspace_bytes, void* stream);
+/*
+ * Weight gradient of a linear layer y = x w^T whose input x [tokens][k] is held in GALV_MX8:
+ *   dw[n][k] = base[n][k] + sum_t dy[t][n] x[t][k]
+ * dy [tokens][n] of `dtype` (GALV_BF16 or GALV_F16), dw and base [n][k] contiguous of `dw_dtype` (`dtype` or GALV_F32); base NULL: zero;
+ * dw may be base.  x enters the product in dy's type, which holds its elements exactly unless they leave that type's range
+ * (GALV_F16: saturating at 65504; small ones rounded as subnormals); products are summed in fp32, base is added in fp32, and the sum
+ * rounded once.  The order of the sums is fixed by sizes, strides and alignment.  With tokens = 0, dw is base or zeros.
+ * workspace: 256-byte aligned, the bytes that the query gives for the same sizes, dy pointer and stride (0: may be NULL).
+ */
+size_t galv_mx_weight_grad_workspace_bytes(const galv_ctx* ctx, int64_t tokens, int64_t n, int64_t k, const void* dy,
+                                           int64_t dy_stride);
+int galv_mx_weight_grad(galv_ctx* ctx, int64_t tokens, int64_t n, int64_t k, const void* dy, int64_t dy_stride, int32_t dtype,
+                        const uint8_t* codes, const uint8_t* scales, const void* base, void* dw, int32_t dw_dtype,
+                        void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * Product of two matrices held in GALV_MX4, a [m][k] and b [n][k]:
+ *   y[i][j] = sum_k a[i][k] b[j][k] + bias[j]
+ * summed in fp32 and rounded once to `dtype` (any of the three).  bias [n] of `dtype`, NULL: none.  The order of the sums is fixed
+ * by the sizes.  With m = 0 nothing is written.  workspace as above.
+ */
+size_t galv_mx_matmul_workspace_bytes(const galv_ctx* ctx, int64_t m, int64_t n, int64_t k);
+int galv_mx_matmul(galv_ctx* ctx, int64_t m, int64_t n, int64_t k, const uint8_t* a_codes, const uint8_t* a_scales,
+                   const uint8_t* b_codes, const uint8_t* b_scales, const void* bias, void* y, int64_t y_stride, int32_t dtype,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
 /* Bytes of device arena galv_search_host needs (0 on invalid shape). */
 size_t galv_search_host_arena_bytes(const galv_ctx* ctx, const galv_shape* shape, int with_model);
 

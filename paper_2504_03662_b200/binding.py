@@ -29,6 +29,10 @@ def CLUSTER_SIZE(n: int) -> int:
     return (n & 31) << 16
 TRANS_PER_LAYER = 4
 STATIC_WORKSPACE_BYTES = 1 << 20
+F32, BF16, F16 = 0, 1, 2
+MX8, MX4 = 8, 4
+ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2
+NORM_LAYER, NORM_RMS = 0, 1
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libgalv.so")
 
@@ -38,7 +42,9 @@ EXPORTS = ("galv_create", "galv_destroy", "galv_strerror", "galv_last_error", "g
            "galv_dp_search_static", "galv_select_best", "galv_prune_strategies",
            "galv_compact_tables", "galv_expand_plan", "galv_plan_cost", "galv_graph_create", "galv_graph_launch",
            "galv_graph_destroy", "galv_layer_optima", "galv_stage_partition", "galv_add_switch_cost",
-           "galv_switch_decision", "galv_skip_estimate")
+           "galv_switch_decision", "galv_skip_estimate", "galv_mx_codes_bytes", "galv_mx_scales_bytes", "galv_mx_pack",
+           "galv_mx_unpack", "galv_mx_act_backward", "galv_mx_norm_workspace_bytes", "galv_mx_norm_backward",
+           "galv_mx_weight_grad_workspace_bytes", "galv_mx_weight_grad", "galv_mx_matmul_workspace_bytes", "galv_mx_matmul")
 
 
 class galv_shape(C.Structure):
@@ -98,6 +104,19 @@ def load_library() -> C.CDLL:
     lib.galv_set_profiling.argtypes = [vp, C.c_int]
     lib.galv_last_layer_loop_ms.argtypes = [vp, C.POINTER(C.c_float)]
     lib.galv_layer_loop_ms_stats.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(C.c_float), C.POINTER(C.c_float), C.POINTER(C.c_int)]
+    i32, f32 = C.c_int32, C.c_float
+    for f in (lib.galv_mx_codes_bytes, lib.galv_mx_scales_bytes):
+        f.argtypes, f.restype = [i64, i64, i32], sz
+    lib.galv_mx_pack.argtypes = [vp, i64, i64, vp, i64, i32, i32, vp, vp, vp]
+    lib.galv_mx_unpack.argtypes = [vp, i64, i64, i32, vp, vp, vp, i64, i32, vp]
+    lib.galv_mx_act_backward.argtypes = [vp, i64, i64, i32, vp, vp, vp, i64, vp, i64, i32, vp]
+    lib.galv_mx_norm_workspace_bytes.argtypes, lib.galv_mx_norm_workspace_bytes.restype = [vp, i64, i64], sz
+    lib.galv_mx_norm_backward.argtypes = [vp, i64, i64, i32, f32, vp, vp, vp, i64, vp, vp, i64, i32, vp, vp, vp, sz, vp]
+    lib.galv_mx_weight_grad_workspace_bytes.argtypes = [vp, i64, i64, i64, vp, i64]
+    lib.galv_mx_weight_grad_workspace_bytes.restype = sz
+    lib.galv_mx_weight_grad.argtypes = [vp, i64, i64, i64, vp, i64, i32, vp, vp, vp, vp, i32, vp, sz, vp]
+    lib.galv_mx_matmul_workspace_bytes.argtypes, lib.galv_mx_matmul_workspace_bytes.restype = [vp, i64, i64, i64], sz
+    lib.galv_mx_matmul.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, i32, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -113,6 +132,19 @@ def _ptr(t) -> Optional[int]:
 
 def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
+
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _matrix(t):
+    """(pointer, row stride in elements) of a 2-D tensor whose rows are contiguous."""
+    assert t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "matrices crossing the boundary have contiguous rows"
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _ws(t):
+    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
 
 
 def make_shape(B: int, Lmax: int, S: int, M: int, flags: int = STORE_C_FULL, m_pitch: Optional[int] = None) -> galv_shape:
@@ -259,3 +291,45 @@ class Galv:
         mean, lo, hi, n = C.c_float(), C.c_float(), C.c_float(), C.c_int()
         self._check(self.lib.galv_layer_loop_ms_stats(self.h, C.byref(mean), C.byref(lo), C.byref(hi), C.byref(n)))
         return mean.value, lo.value, hi.value, n.value
+
+    def _mx_stream(self) -> int:
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def galv_mx_pack(self, x, fmt, codes, scales):
+        p, stride = _matrix(x)
+        self._check(self.lib.galv_mx_pack(self.h, x.shape[0], x.shape[1], p, stride, _DTYPES[x.dtype], fmt, _ptr(codes), _ptr(scales),
+                                          self._mx_stream()))
+
+    def galv_mx_unpack(self, fmt, codes, scales, x):
+        p, stride = _matrix(x)
+        self._check(self.lib.galv_mx_unpack(self.h, x.shape[0], x.shape[1], fmt, _ptr(codes), _ptr(scales), p, stride, _DTYPES[x.dtype],
+                                            self._mx_stream()))
+
+    def galv_mx_act_backward(self, act, codes, scales, dy, dx):
+        (p, ps), (q, qs) = _matrix(dy), _matrix(dx)
+        self._check(self.lib.galv_mx_act_backward(self.h, dy.shape[0], dy.shape[1], act, _ptr(codes), _ptr(scales), p, ps, q, qs,
+                                                  _DTYPES[dy.dtype], self._mx_stream()))
+
+    def galv_mx_norm_workspace_bytes(self, rows, cols) -> int:
+        return int(self.lib.galv_mx_norm_workspace_bytes(self.h, rows, cols))
+
+    def galv_mx_norm_backward(self, kind, eps, codes, scales, dy, weight, dx, dweight, dbias, workspace):
+        (p, ps), (q, qs) = _matrix(dy), _matrix(dx)
+        self._check(self.lib.galv_mx_norm_backward(self.h, dy.shape[0], dy.shape[1], kind, eps, _ptr(codes), _ptr(scales), p, ps, _ptr(weight),
+                                                   q, qs, _DTYPES[dy.dtype], _ptr(dweight), _ptr(dbias), *_ws(workspace), self._mx_stream()))
+
+    def galv_mx_weight_grad_workspace_bytes(self, dy, k) -> int:
+        return int(self.lib.galv_mx_weight_grad_workspace_bytes(self.h, dy.shape[0], dy.shape[1], k, *_matrix(dy)))
+
+    def galv_mx_weight_grad(self, dy, codes, scales, base, dw, workspace):
+        p, ps = _matrix(dy)
+        self._check(self.lib.galv_mx_weight_grad(self.h, dy.shape[0], dy.shape[1], dw.shape[1], p, ps, _DTYPES[dy.dtype], _ptr(codes), _ptr(scales),
+                                                 _ptr(base), _ptr(dw), _DTYPES[dw.dtype], *_ws(workspace), self._mx_stream()))
+
+    def galv_mx_matmul_workspace_bytes(self, m, n, k) -> int:
+        return int(self.lib.galv_mx_matmul_workspace_bytes(self.h, m, n, k))
+
+    def galv_mx_matmul(self, k, a_codes, a_scales, b_codes, b_scales, bias, y, workspace):
+        p, ps = _matrix(y)
+        self._check(self.lib.galv_mx_matmul(self.h, y.shape[0], y.shape[1], k, _ptr(a_codes), _ptr(a_scales), _ptr(b_codes), _ptr(b_scales), _ptr(bias),
+                                            p, ps, _DTYPES[y.dtype], *_ws(workspace), self._mx_stream()))

@@ -1,0 +1,175 @@
+// Microscaled blocks: conversions and row access shared by the kernels that pack, restore and use them.
+// The format is described in include/galv.h.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "galv_internal.h"
+
+// Calls run on the context's device, whichever is current.
+struct MxDevice {
+    int old = -1;
+    cudaError_t err;
+    explicit MxDevice(const galv_ctx* ctx)
+    {
+        err = cudaGetDevice(&old);
+        if (err == cudaSuccess && old != ctx->device) err = cudaSetDevice(ctx->device);
+        else old = -1;
+    }
+    ~MxDevice() { if (old >= 0) cudaSetDevice(old); }
+};
+
+constexpr int64_t kMxMost = (int64_t(1) << 31) - 128;      // rows and columns stay below this
+
+inline bool mx_size_ok(int64_t rows, int64_t cols) { return rows >= 0 && cols >= 1 && rows < kMxMost && cols < kMxMost; }
+inline bool mx_dtype_ok(int32_t t) { return t == GALV_F32 || t == GALV_BF16 || t == GALV_F16; }
+inline int mx_size_of(int32_t t) { return t == GALV_F32 ? 4 : 2; }
+inline bool mx_aligned(const void* p, int a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+// a matrix of numbers: present, aligned to its element, rows that do not overlap
+inline bool mx_matrix_ok(const void* p, int64_t stride, int64_t cols, int32_t t) { return p && mx_aligned(p, mx_size_of(t)) && stride >= cols && stride < (int64_t(1) << 40); }
+// its rows can be read in 16-byte pieces
+inline bool mx_rows16(const void* p, int64_t stride, int32_t t) { return mx_aligned(p, 16) && stride * mx_size_of(t) % 16 == 0; }
+inline int64_t mx_blocks(int64_t cols) { return (cols + 31) / 32; }
+inline int64_t mx_pitch8(int64_t cols) { return (mx_blocks(cols) + 15) / 16 * 16; }      // bytes of a row of GALV_MX8 scales
+
+template <int T> struct MxType;
+template <> struct MxType<GALV_F32> { using type = float; };
+template <> struct MxType<GALV_BF16> { using type = __nv_bfloat16; };
+template <> struct MxType<GALV_F16> { using type = __half; };
+
+__device__ __forceinline__ float mx_float(float v) { return v; }
+__device__ __forceinline__ float mx_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float mx_float(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T mx_round(float v);
+template <> __device__ __forceinline__ float mx_round<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 mx_round<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half mx_round<__half>(float v) { return __float2half_rn(v); }
+// what was held as a finite number stays one in fp16 (a NaN passes both comparisons)
+template <typename T> __device__ __forceinline__ float mx_held(float v) { return v; }
+template <> __device__ __forceinline__ float mx_held<__half>(float v) { return v > 65504.f ? 65504.f : v < -65504.f ? -65504.f : v; }
+
+// 8 elements of a row as one piece: 16 bytes of 16-bit numbers, 32 of fp32.
+template <typename T> struct MxPiece { uint4 q[sizeof(T) / 2]; };
+
+// VEC: the row starts on a 16-byte boundary (c0 is a multiple of 8).  Behind `cols`: zeros.
+template <typename T, bool VEC>
+__device__ __forceinline__ void mx_load8(const T* __restrict__ row, long long c0, long long cols, float (&v)[8])
+{
+    if (VEC && c0 + 8 <= cols) {
+        MxPiece<T> p;
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) p.q[i] = __ldg(reinterpret_cast<const uint4*>(row + c0) + i);
+        const T* e = reinterpret_cast<const T*>(&p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = mx_float(e[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c0 + i < cols ? mx_float(row[c0 + i]) : 0.f;
+    }
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void mx_store8(T* __restrict__ row, long long c0, long long cols, const float (&v)[8])
+{
+    if (VEC && c0 + 8 <= cols) {
+        MxPiece<T> p;
+        T* e = reinterpret_cast<T*>(&p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = mx_round<T>(v[i]);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(row + c0)[i] = p.q[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c0 + i < cols) row[c0 + i] = mx_round<T>(v[i]);
+    }
+}
+
+// Scale byte of a block whose largest magnitude has these bits: the smallest exponent under which it does not pass the largest element,
+// 448 = 1.75 * 2^8 or 6 = 1.5 * 2^2.  Whole numbers only, so exact; 255 for an infinity or a NaN.
+template <int FMT>
+__device__ __forceinline__ int mx_scale_byte(uint32_t amax_bits)
+{
+    constexpr int top = FMT == GALV_MX8 ? 8 : 2;
+    constexpr uint32_t mant = FMT == GALV_MX8 ? 0x600000u : 0x400000u;
+    if (amax_bits >= 0x7f800000u) return 255;
+    const int b = (int)(amax_bits >> 23) - top + ((amax_bits & 0x7fffffu) > mant ? 1 : 0);
+    return b < 0 ? 0 : b;
+}
+// 2^(127 - byte); bytes up to 253 occur
+__device__ __forceinline__ float mx_inverse(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
+// 2^(byte - 127), NaN for 255
+__device__ __forceinline__ float mx_scale(int byte) { return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7fc00000u : (uint32_t)byte << 23); }
+
+// Four numbers to four 8-bit elements, to nearest even (the conversion saturates; nothing here passes 448).
+__device__ __forceinline__ uint32_t mx_to8(float a, float b, float c, float d)
+{
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+    return (uint32_t)lo | (uint32_t)hi << 16;
+}
+// Eight numbers to eight 4-bit elements, element 0 lowest.
+__device__ __forceinline__ uint32_t mx_to4(const float (&v)[8])
+{
+    uint32_t r;
+    asm("{\n.reg .b8 a, b, c, d;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n"
+        "mov.b32 %0, {a, b, c, d};\n}" : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return r;
+}
+__device__ __forceinline__ void mx_from8(uint32_t w, float* v)
+{
+    uint32_t lo, hi;
+    asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %2;\ncvt.rn.f16x2.e4m3x2 %0, l;\ncvt.rn.f16x2.e4m3x2 %1, h;\n}" : "=r"(lo), "=r"(hi) : "r"(w));
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+    v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+}
+__device__ __forceinline__ void mx_from4(uint32_t w, float (&v)[8])
+{
+    uint32_t h[4];
+    asm("{\n.reg .b8 a, b, c, d;\nmov.b32 {a, b, c, d}, %4;\n"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\ncvt.rn.f16x2.e2m1x2 %1, b;\ncvt.rn.f16x2.e2m1x2 %2, c;\ncvt.rn.f16x2.e2m1x2 %3, d;\n}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+        v[2 * i] = f.x; v[2 * i + 1] = f.y;
+    }
+}
+
+// Where the scale byte of (row, block) lies.
+template <int FMT>
+__device__ __forceinline__ long long mx_scale_at(long long row, long long b, long long per_row)      // per_row: bytes a row (MX8), tiles a row of tiles (MX4)
+{
+    if (FMT == GALV_MX8) return row * per_row + b;
+    return ((row >> 7) * per_row + (b >> 2)) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (b & 3);
+}
+
+// The 8 held values of piece c (columns 8c .. 8c+7) of a row.
+template <int FMT>
+__device__ __forceinline__ void mx_restore8(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, long long row, long long c, long long nb,
+                                            long long per_row, float (&v)[8])
+{
+    if (FMT == GALV_MX8) {
+        const uint2 w = __ldg(reinterpret_cast<const uint2*>(codes + (row * nb * 32 + c * 8)));
+        mx_from8(w.x, v);
+        mx_from8(w.y, v + 4);
+    } else {
+        mx_from4(__ldg(reinterpret_cast<const uint32_t*>(codes + (row * nb * 16 + c * 4))), v);
+    }
+    const float s = mx_scale(__ldg(scales + mx_scale_at<FMT>(row, c >> 2, per_row)));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= s;
+}
+
+#define MX_DISPATCH_TYPE(dtype, ...)                                                                                  \
+    do {                                                                                                              \
+        if ((dtype) == GALV_F32) { using T = float; __VA_ARGS__; }                                                    \
+        else if ((dtype) == GALV_BF16) { using T = __nv_bfloat16; __VA_ARGS__; }                                      \
+        else { using T = __half; __VA_ARGS__; }                                                                       \
+    } while (0)

@@ -1,0 +1,293 @@
+"""Microscaled tensors: activations kept in 8 bits and used by the backward pass, products of operands in 4 bits.
+
+A plan of the search says, layer by layer, what is kept and how fast the layer multiplies; the operators here carry the
+microscaled choices out.  The functions allocate their results through PyTorch and call the library's kernels on the
+current stream of the tensors' device; formats and formulas are those of include/galv.h.  `linear`, `norm` and
+`activation` are the same as differentiable functions: their inputs are kept in 8 bits for the backward pass.
+
+A context of the library belongs to one host thread, so every thread (the autograd engine's among them) gets its own
+for each device.
+"""
+from __future__ import annotations
+
+import threading
+from dataclasses import dataclass
+from typing import Optional
+
+import torch
+
+from . import binding as gb
+
+ACTS = {"gelu": gb.ACT_GELU, "gelu_tanh": gb.ACT_GELU_TANH, "silu": gb.ACT_SILU}
+NORMS = {"layer": gb.NORM_LAYER, "rms": gb.NORM_RMS}
+_local = threading.local()
+
+
+def context(device: torch.device) -> gb.Galv:
+    """This thread's library context on a CUDA device."""
+    made = _local.__dict__.setdefault("made", {})
+    index = torch.cuda.current_device() if device.index is None else device.index
+    if index not in made:
+        made[index] = gb.Galv(index)
+    return made[index]
+
+
+@dataclass(frozen=True)
+class Packed:
+    """A matrix [rows][cols] in blocks of 32 columns: element codes, one scale byte a block."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    rows: int
+    cols: int
+    fmt: int = gb.MX8
+
+    def __post_init__(self):
+        for t, n in ((self.codes, codes_bytes(self.rows, self.cols, self.fmt)), (self.scales, scales_bytes(self.rows, self.cols, self.fmt))):
+            if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() < n:
+                raise ValueError(f"a [{self.rows}][{self.cols}] matrix in {self.fmt} bits takes {n} contiguous bytes, got {t.dtype} {tuple(t.shape)}")
+
+    @property
+    def nbytes(self) -> int:
+        return self.codes.numel() + self.scales.numel()
+
+
+def codes_bytes(rows: int, cols: int, fmt: int = gb.MX8) -> int:
+    return rows * (-(-cols // 32)) * 4 * fmt
+
+
+def scales_bytes(rows: int, cols: int, fmt: int = gb.MX8) -> int:
+    nb = -(-cols // 32)
+    return rows * (-(-nb // 16) * 16) if fmt == gb.MX8 else -(-rows // 128) * -(-nb // 4) * 512
+
+
+def _on(*tensors: Optional[torch.Tensor]) -> gb.Galv:
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("microscaled operators take CUDA tensors (no CPU path)")
+        if dev is not None and t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device}")
+        dev = t.device
+    return context(dev)
+
+
+def _kind(t: torch.Tensor, what: str, dtypes=(torch.float32, torch.bfloat16, torch.float16)):
+    if t.dtype not in dtypes:
+        raise ValueError(f"{what} is one of {', '.join(str(d).replace('torch.', '') for d in dtypes)}, not {t.dtype}")
+
+
+def _rows(t: torch.Tensor, what: str) -> torch.Tensor:
+    """A 2-D tensor whose rows are contiguous and do not overlap (a copy where they are not)."""
+    if t.dim() != 2:
+        raise ValueError(f"{what} is a matrix, not of shape {tuple(t.shape)}")
+    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        return t.contiguous()
+    return t
+
+
+def _like(t: torch.Tensor, p: Packed, what: str):
+    if tuple(t.shape) != (p.rows, p.cols):
+        raise ValueError(f"{what} of shape {tuple(t.shape)} beside a held matrix [{p.rows}][{p.cols}]")
+
+
+def _eight(p: Packed):
+    if p.fmt != gb.MX8:
+        raise ValueError("the backward pass reads what was kept in 8 bits")
+
+
+def _workspace(nbytes: int, device) -> Optional[torch.Tensor]:
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def pack(x: torch.Tensor, fmt: int = gb.MX8) -> Packed:
+    """Holds a matrix in blocks of 8- or 4-bit elements."""
+    if fmt not in (gb.MX8, gb.MX4):
+        raise ValueError(f"a format is 8 or 4 bits, not {fmt}")
+    _kind(x, "x")
+    x = _rows(x, "x")
+    g = _on(x)
+    rows, cols = x.shape
+    if cols < 1:
+        raise ValueError("rows of at least one column")
+    p = Packed(torch.empty(codes_bytes(rows, cols, fmt), dtype=torch.uint8, device=x.device),
+               torch.empty(scales_bytes(rows, cols, fmt), dtype=torch.uint8, device=x.device), rows, cols, fmt)
+    g.galv_mx_pack(x, fmt, p.codes, p.scales)
+    return p
+
+
+def unpack(p: Packed, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """The numbers a packed matrix stands for."""
+    g = _on(p.codes, p.scales)
+    x = torch.empty(p.rows, p.cols, dtype=dtype, device=p.codes.device)
+    _kind(x, "dtype")
+    g.galv_mx_unpack(p.fmt, p.codes, p.scales, x)
+    return x
+
+
+def act_backward(dy: torch.Tensor, kept: Packed, act: str = "gelu") -> torch.Tensor:
+    """dy * f'(x) for an activation function ("gelu", "gelu_tanh", "silu") whose input x was kept in 8 bits."""
+    if act not in ACTS:
+        raise ValueError(f"an activation function is one of {', '.join(ACTS)}, not {act!r}")
+    _kind(dy, "dy")
+    _eight(kept)
+    dy = _rows(dy, "dy")
+    _like(dy, kept, "dy")
+    g = _on(dy, kept.codes, kept.scales)
+    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
+    g.galv_mx_act_backward(ACTS[act], kept.codes, kept.scales, dy, dx)
+    return dx
+
+
+def norm_backward(dy: torch.Tensor, kept: Packed, weight: Optional[torch.Tensor] = None, kind: str = "layer", eps: float = 1e-5):
+    """(dx, dweight, dbias) of a "layer" or "rms" norm over rows whose input was kept in 8 bits; dweight and dbias in fp32, dbias None for "rms"."""
+    if kind not in NORMS:
+        raise ValueError(f"a norm is one of {', '.join(NORMS)}, not {kind!r}")
+    _kind(dy, "dy")
+    _eight(kept)
+    dy = _rows(dy, "dy")
+    _like(dy, kept, "dy")
+    if weight is not None and (weight.dtype != dy.dtype or tuple(weight.shape) != (kept.cols,)):
+        raise ValueError(f"weight is [{kept.cols}] of {dy.dtype}")
+    g = _on(dy, kept.codes, kept.scales, weight)
+    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
+    dweight = torch.empty(kept.cols, dtype=torch.float32, device=dy.device)
+    dbias = torch.empty(kept.cols, dtype=torch.float32, device=dy.device) if kind == "layer" else None
+    ws = _workspace(g.galv_mx_norm_workspace_bytes(kept.rows, kept.cols), dy.device)
+    g.galv_mx_norm_backward(NORMS[kind], eps, kept.codes, kept.scales, dy, None if weight is None else weight.contiguous(), dx, dweight, dbias, ws)
+    return dx, dweight, dbias
+
+
+def weight_grad(dy: torch.Tensor, kept: Packed, dtype: Optional[torch.dtype] = None, base: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """base + dy^T x for a linear layer whose input x was kept in 8 bits: [columns of dy][columns of x].  `out` may be `base`."""
+    _kind(dy, "dy", (torch.bfloat16, torch.float16))
+    _eight(kept)
+    dy = _rows(dy, "dy")
+    if dy.shape[0] != kept.rows or dy.shape[1] < 1:
+        raise ValueError(f"dy of shape {tuple(dy.shape)} beside {kept.rows} kept rows")
+    shape = (dy.shape[1], kept.cols)
+    dtype = dtype or (out if out is not None else base if base is not None else dy).dtype
+    if dtype not in (dy.dtype, torch.float32):
+        raise ValueError(f"a weight gradient is of {dy.dtype} or float32, not {dtype}")
+    for t, what in ((base, "base"), (out, "out")):
+        if t is not None and (t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError(f"{what} is a contiguous {shape} of {dtype}")
+    g = _on(dy, kept.codes, kept.scales, base, out)
+    dw = torch.empty(shape, dtype=dtype, device=dy.device) if out is None else out
+    ws = _workspace(g.galv_mx_weight_grad_workspace_bytes(dy, kept.cols), dy.device)
+    g.galv_mx_weight_grad(dy, kept.codes, kept.scales, base, dw, ws)
+    return dw
+
+
+def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, bias: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """a b^T + bias for two matrices held in 4 bits."""
+    if a.fmt != gb.MX4 or b.fmt != gb.MX4:
+        raise ValueError("a product takes operands held in 4 bits")
+    if a.cols != b.cols or b.rows < 1:
+        raise ValueError(f"a product of [{a.rows}][{a.cols}] and [{b.rows}][{b.cols}] transposed")
+    if bias is not None and (bias.dtype != dtype or tuple(bias.shape) != (b.rows,)):
+        raise ValueError(f"bias is [{b.rows}] of {dtype}")
+    g = _on(a.codes, a.scales, b.codes, b.scales, bias)
+    y = torch.empty(a.rows, b.rows, dtype=dtype, device=a.codes.device)
+    _kind(y, "dtype")
+    ws = _workspace(g.galv_mx_matmul_workspace_bytes(a.rows, b.rows, a.cols), y.device)
+    g.galv_mx_matmul(a.cols, a.codes, a.scales, b.codes, b.scales, None if bias is None else bias.contiguous(), y, ws)
+    return y
+
+
+# ------------------------------------------------------------------------------------------------- differentiable forms
+
+def _flat(x: torch.Tensor) -> torch.Tensor:
+    return x.reshape(-1, x.shape[-1])
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, four):
+        flat = _flat(x)
+        if four:
+            y = matmul(pack(flat, gb.MX4), pack(weight, gb.MX4), x.dtype, bias)
+        else:
+            y = flat @ weight.t() if bias is None else torch.addmm(bias, flat, weight.t())
+        kept = pack(flat) if ctx.needs_input_grad[1] else None
+        ctx.save_for_backward(weight, *((kept.codes, kept.scales) if kept else ()))
+        ctx.shape, ctx.has_bias = x.shape, bias is not None
+        return y.view(*x.shape[:-1], weight.shape[0])
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        weight, *kept = ctx.saved_tensors
+        flat = _flat(dy)
+        dx = dw = db = None
+        if ctx.needs_input_grad[0]:
+            dx = (flat @ weight).view(ctx.shape)
+        if ctx.needs_input_grad[1]:
+            dw = weight_grad(flat, Packed(*kept, flat.shape[0], weight.shape[1]), weight.dtype)
+        if ctx.has_bias and ctx.needs_input_grad[2]:
+            db = flat.sum(0, dtype=torch.float32).to(dy.dtype)
+        return dx, dw, db, None
+
+
+def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, four: bool = False) -> torch.Tensor:
+    """x weight^T + bias (bf16 or fp16), x kept in 8 bits for the weight's gradient.  `four`: the forward product takes both operands in
+    4 bits; the gradients are those of the product of the unrounded operands (straight through the rounding)."""
+    _kind(x, "x", (torch.bfloat16, torch.float16))
+    if weight.dim() != 2 or weight.dtype != x.dtype or weight.shape[1] != x.shape[-1]:
+        raise ValueError(f"weight of shape {tuple(weight.shape)} and {weight.dtype} beside x of {tuple(x.shape)} and {x.dtype}")
+    return _Linear.apply(x, weight, bias, four)
+
+
+class _Norm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, kind, eps):
+        n = (x.shape[-1],)
+        y = torch.nn.functional.layer_norm(x, n, weight, bias, eps) if kind == "layer" else torch.nn.functional.rms_norm(x, n, weight, eps)
+        kept = pack(_flat(x))
+        ctx.save_for_backward(kept.codes, kept.scales, *(() if weight is None else (weight,)))
+        ctx.kind, ctx.eps, ctx.shape, ctx.bias_type = kind, eps, x.shape, None if bias is None else bias.dtype
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        codes, scales, *weight = ctx.saved_tensors
+        flat = _flat(dy)
+        dx, dw, db = norm_backward(flat, Packed(codes, scales, *flat.shape), weight[0] if weight else None, ctx.kind, ctx.eps)
+        return (dx.view(ctx.shape), dw.to(weight[0].dtype) if weight else None, None if ctx.bias_type is None else db.to(ctx.bias_type), None, None)
+
+
+def norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, kind: str = "layer", eps: float = 1e-5) -> torch.Tensor:
+    """A "layer" or "rms" norm over the last axis, x kept in 8 bits for the backward pass."""
+    if kind not in NORMS:
+        raise ValueError(f"a norm is one of {', '.join(NORMS)}, not {kind!r}")
+    if kind == "rms" and bias is not None:
+        raise ValueError("an rms norm has no bias")
+    _kind(x, "x")
+    return _Norm.apply(x, weight, bias, kind, eps)
+
+
+class _Activation(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, act):
+        kept = pack(_flat(x))
+        ctx.save_for_backward(kept.codes, kept.scales)
+        ctx.act, ctx.shape = act, x.shape
+        f = torch.nn.functional
+        return f.silu(x) if act == "silu" else f.gelu(x, approximate="tanh" if act == "gelu_tanh" else "none")
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        flat = _flat(dy)
+        return act_backward(flat, Packed(*ctx.saved_tensors, *flat.shape), ctx.act).view(ctx.shape), None
+
+
+def activation(x: torch.Tensor, act: str = "gelu") -> torch.Tensor:
+    """gelu, gelu_tanh or silu, x kept in 8 bits for the backward pass."""
+    if act not in ACTS:
+        raise ValueError(f"an activation function is one of {', '.join(ACTS)}, not {act!r}")
+    _kind(x, "x")
+    return _Activation.apply(x, act)
