@@ -173,3 +173,8 @@ __device__ __forceinline__ void mx_restore8(const uint8_t* __restrict__ codes, c
         else if ((dtype) == GALV_BF16) { using T = __nv_bfloat16; __VA_ARGS__; }                                      \
         else { using T = __half; __VA_ARGS__; }                                                                       \
     } while (0)
+
+// Tensor map of a matrix [rows][cols] whose rows are `pitch` bytes apart, read in boxes [box_rows][box_cols]; swizzle: rows of 128 bytes, their
+// 16-byte pieces exchanged by row % 8.
+cudaError_t galv_mx_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows,
+                        uint32_t box_cols, bool swizzle);

@@ -1,0 +1,491 @@
+// Weight gradient of a layer whose input was kept in 8 bits: dw[n][k] = base[n][k] + sum_t dy[t][n] x[t][k].
+//
+// The sum runs over tokens, along which the blocks' powers of two change, so they cannot be taken out of it: the kept values are restored to
+// dy's 16-bit type on their way to the tensor cores, exactly (4 significant bits and a power of two).  A pair of CTAs owns a tile of 256 x 256 of dw
+// (tcgen05.mma over both, M = N = 256): each stages 128 columns of dy and restores 128 columns of x, so every restored value is used 256 times.
+// Per CTA: a producer thread (bulk tensor copies of 64 tokens of dy, codes and scales), eight warps that restore (8 bits in, 16 bits out into
+// the swizzled rows the tensor cores read), one thread that issues the matrix instructions for the pair, eight warps that take
+// sums from the tensor memory while the next are made (two accumulators of 256 columns fill it) and move results out.
+// Both operands lie with tokens along their rows ("MN-major"): dy and the codes are read as they are stored, nothing is transposed.
+
+#include <type_traits>
+
+#include "galv_mx.cuh"
+#include "galv_tc.cuh"
+
+namespace {
+
+constexpr int kStages = 5, kTokens = 64, kTile = 256, kHalf = kTile / 2;
+constexpr int kDyBytes = kTokens * kHalf * 2, kCodeBytes = kTokens * kHalf, kScaleBytes = kTokens * 16, kXBytes = kTokens * kHalf * 2;
+constexpr int kStageBytes = kDyBytes + kXBytes + kCodeBytes + kScaleBytes;
+constexpr int kOutBytes = 8 * 2048;                       // 32 x 16 sums of each warp that moves them out
+constexpr int kSmem = 1024 + kStages * kStageBytes + kOutBytes + 256;
+constexpr int kThreads = 768, kRestoreWarps = 4, kRestoreGroups = 3;      // warps: 4 for copies and matrix instructions, 8 for sums, three groups of 4 that restore
+// Registers of a thread of each: 128 * 24 + 256 * 168 + 384 * 40 = 768 * 80, what the block is launched with.
+constexpr int kRegsIssue = 24, kRegsSum = 168, kRegsRestore = 40;
+// A tensor core's sum is cut at every addition: over 4096 tokens it is 1.6e-6 of the result off, over 1000 half of that (the error grows with the
+// root of the length).  So after this many chunks (1024 tokens) the sum goes to fp32 registers, rounded additions.
+constexpr int kSegment = 16;
+constexpr int kGroup = 8;                                 // tiles along n whose columns of dy stay in L2 while their k runs
+
+struct WgradArgs {
+    long long tokens, n, k;
+    int tiles_n, tiles_k, splits, chunks;
+    const void* base;
+    void* dw;
+    float* partial;                                       // [splits][n][k], or NULL
+    int vec;                                              // four results of a row can be moved at once
+};
+
+__device__ unsigned int g_timeouts;
+
+struct Unit { int tn, tk, split, c0, c1; };
+__device__ __forceinline__ Unit unit_of(const WgradArgs& a, int u)
+{
+    Unit w;
+    const int tile = u / a.splits, per = kGroup * a.tiles_k, first = tile / per * kGroup;
+    const int size = min(kGroup, a.tiles_n - first);
+    w.split = u % a.splits;
+    w.tn = first + tile % per % size;
+    w.tk = tile % per / size;
+    w.c0 = (int)((long long)w.split * a.chunks / a.splits);
+    w.c1 = (int)((long long)(w.split + 1) * a.chunks / a.splits);
+    return w;
+}
+
+// Four 8-bit elements times 2^(byte - 127) as two pairs of 16-bit numbers.  common: the shorter way holds for this byte.
+template <typename T> struct Restore;
+template <> struct Restore<__nv_bfloat16> {
+    // An element's exponent and mantissa moved four bits down lie where a bf16 has its own: the value times 2^-120.  One product with 2^(120 + s)
+    // restores it exactly (below bf16's normal numbers rounded once); from s = 8 on that factor leaves the type and two take its place.
+    __device__ __forceinline__ static bool common(uint32_t byte) { return byte <= 134; }
+    __device__ __forceinline__ static uint32_t factor(uint32_t byte) { return (byte + 120 << 7) * 0x10001u; }
+    __device__ __forceinline__ static uint32_t mul(uint32_t a, uint32_t b)
+    {
+        uint32_t r;
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    __device__ __forceinline__ static void bits(uint32_t w, uint32_t& lo, uint32_t& hi)
+    {
+        const uint32_t top = (w & 0x80808080u) | (w >> 4 & 0x07070707u), low = w << 4 & 0xf0f0f0f0u;
+        lo = __byte_perm(low, top, 0x5140);
+        hi = __byte_perm(low, top, 0x7362);
+    }
+    __device__ __forceinline__ static void four(uint32_t w, uint32_t f, uint32_t& lo, uint32_t& hi)
+    {
+        bits(w, lo, hi);
+        lo = mul(lo, f);
+        hi = mul(hi, f);
+    }
+    __device__ __forceinline__ static void four_any(uint32_t w, uint32_t byte, uint32_t& lo, uint32_t& hi)
+    {
+        if (common(byte)) { four(w, factor(byte), lo, hi); return; }
+        const uint32_t f = byte == 255 ? 0x7fc07fc0u : (byte << 7) * 0x10001u;
+        bits(w, lo, hi);
+        lo = mul(mul(lo, (247u << 7) * 0x10001u), f);
+        hi = mul(mul(hi, (247u << 7) * 0x10001u), f);
+    }
+};
+template <> struct Restore<__half> {
+    // 2^s in fp16 where that and the largest element under it are normal numbers, else through fp32, saturating.
+    __device__ __forceinline__ static bool common(uint32_t byte) { return byte >= 113 && byte <= 134; }
+    __device__ __forceinline__ static uint32_t factor(uint32_t byte) { return (byte - 112 << 10) * 0x10001u; }
+    __device__ __forceinline__ static void four(uint32_t w, uint32_t f, uint32_t& lo, uint32_t& hi)
+    {
+        uint32_t a, b;
+        asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %2;\ncvt.rn.f16x2.e4m3x2 %0, l;\ncvt.rn.f16x2.e4m3x2 %1, h;\n}" : "=r"(a), "=r"(b) : "r"(w));
+        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(lo) : "r"(a), "r"(f));
+        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(b), "r"(f));
+    }
+    __device__ __forceinline__ static uint32_t clip(float a, float b)
+    {
+        const __half2 h = __floats2half2_rn(mx_held<__half>(a), mx_held<__half>(b));
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    __device__ __forceinline__ static void four_any(uint32_t w, uint32_t byte, uint32_t& lo, uint32_t& hi)
+    {
+        float v[4];
+        const float s = mx_scale((int)byte);
+        mx_from8(w, v);
+        lo = clip(v[0] * s, v[1] * s);
+        hi = clip(v[2] * s, v[3] * s);
+    }
+};
+
+template <typename O> struct Four;
+template <> struct Four<float> { using type = float4; };
+template <> struct Four<__nv_bfloat16> { using type = uint2; };
+template <> struct Four<__half> { using type = uint2; };
+
+// 32 x 16 sums from the warp's shared memory (rows of 64 bytes, their 16-byte pieces exchanged by row / 2 % 4) to rows r0.. and columns c0.. of an
+// [n][k] matrix.
+template <typename O>
+__device__ __forceinline__ void move_out(uint32_t from, long long r0, long long c0, long long n, long long k, const O* base, O* out, bool vec)
+{
+    const int lane = threadIdx.x % 32;
+    if (vec) {
+        const long long c = c0 + lane % 4 * 4;
+        if (c >= k) return;                               // k is a multiple of 4 here
+        using Q = typename Four<O>::type;
+        Q q[4];
+        if (base) {                                       // all loads first: out may be base
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (r0 + i * 8 + lane / 4 < n) q[i] = *reinterpret_cast<const Q*>(base + (r0 + i * 8 + lane / 4) * k + c);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = i * 8 + lane / 4;
+            if (r0 + row >= n) continue;
+            float v[4];
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(from + row * 64 + ((lane % 4) ^ (row >> 1 & 3)) * 16));
+            O* e = reinterpret_cast<O*>(&q[i]);
+            if (base) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] += mx_float(e[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = mx_round<O>(v[j]);
+            *reinterpret_cast<Q*>(out + (r0 + row) * k + c) = q[i];
+        }
+    } else {
+        const long long c = c0 + lane % 16;
+        if (c >= k) return;
+        for (int row = lane / 16; row < 32 && r0 + row < n; row += 2) {
+            float v;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(from + row * 64 + ((lane % 16 / 4) ^ (row >> 1 & 3)) * 16 + lane % 4 * 4));
+            const long long at = (r0 + row) * k + c;
+            if (base) v += mx_float(base[at]);
+            out[at] = mx_round<O>(v);
+        }
+    }
+}
+
+template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(N)); }
+template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(N)); }
+
+template <typename T, typename O>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+mx_wgrad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap code_map, const __grid_constant__ CUtensorMap scale_map,
+                const __grid_constant__ WgradArgs a)
+{
+    extern __shared__ unsigned char raw[];
+    const uint32_t base = (tc::smem_at(raw) + 1023) & ~1023u;
+    const uint32_t dy_at = base, x_at = base + kStages * kDyBytes, code_at = x_at + kStages * kXBytes, scale_at = code_at + kStages * kCodeBytes;
+    const uint32_t out_at = scale_at + kStages * kScaleBytes, bars = out_at + kOutBytes;
+    const uint32_t full = bars, conv = bars + 8 * kStages, empty = bars + 16 * kStages, acc_full = bars + 24 * kStages, acc_empty = acc_full + 16, drain = acc_empty + 16,
+                   slot = drain + 8;
+    __shared__ int failed;
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = tc::cluster_rank();
+    const int units = a.tiles_n * a.tiles_k * a.splits, first = blockIdx.x / 2, stride = gridDim.x / 2;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            tc::bar_init(full + 8 * s, 1);
+            tc::bar_init(conv + 8 * s, 2 * kRestoreWarps);
+            tc::bar_init(empty + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            tc::bar_init(acc_full + 8 * b, 1);
+            tc::bar_init(acc_empty + 8 * b, 16);
+        }
+        tc::bar_init(drain, 1);
+        tc::bar_init_done();
+        failed = 0;
+        tc::prefetch_map(&dy_map);
+        tc::prefetch_map(&code_map);
+        tc::prefetch_map(&scale_map);
+    }
+    if (warp == 2) tc::tmem_alloc<2>(slot, 512);
+    tc::fence_before();
+    __syncthreads();
+    tc::cluster_sync();                                   // the pair's barriers exist
+    tc::fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+
+    // every wait is bounded; who gives up says so, the others run into their own bound
+    auto waited = [&](uint32_t bar, uint32_t parity) {
+        if (tc::bar_wait(bar, parity)) return true;
+        *(volatile int*)&failed = 1;
+        return false;
+    };
+
+    if (warp < 4) fewer_registers<kRegsIssue>();
+    if (warp == 0) {
+        if (tc::elect()) {
+            int it = 0;
+            bool ok = true;
+            for (int u = first; u < units && ok; u += stride) {
+                const Unit w = unit_of(a, u);
+                const int n0 = w.tn * kTile + rank * kHalf, k0 = w.tk * kTile + rank * kHalf;
+                for (int c = w.c0; c < w.c1; ++c, ++it) {
+                    const int s = it % kStages;
+                    if (!(ok = waited(empty + 8 * s, (it / kStages & 1) ^ 1))) break;
+                    const uint32_t bar = full + 8 * s;
+                    tc::bar_expect(bar, kDyBytes + kCodeBytes + kScaleBytes);
+                    tc::load_2d(dy_at + s * kDyBytes, &dy_map, n0, c * kTokens, bar);
+                    tc::load_2d(dy_at + s * kDyBytes + kDyBytes / 2, &dy_map, n0 + 64, c * kTokens, bar);
+                    tc::load_2d(code_at + s * kCodeBytes, &code_map, k0, c * kTokens, bar);
+                    tc::load_2d(scale_at + s * kScaleBytes, &scale_map, k0 / 32 & ~15, c * kTokens, bar);
+                }
+            }
+            if (*(volatile int*)&failed)                  // copies still in flight
+                for (int i = it < kStages ? 0 : it - kStages; i < it; ++i) tc::bar_wait(full + 8 * (i % kStages), i / kStages & 1);
+        }
+    } else if (warp == 1) {
+        if (rank == 0 && tc::elect()) {
+            // fp32 sums, A and B of type T with the summed index across the rows, 256 x 256
+            constexpr uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+            constexpr uint32_t what = 1u << 4 | type << 7 | type << 10 | 1u << 15 | 1u << 16 | (uint32_t)(kTile >> 3) << 17 | (uint32_t)(kTile >> 4) << 24;
+            int it = 0, done = 0;
+            bool ok = true;
+            for (int u = first; u < units && ok; u += stride) {
+                const Unit w = unit_of(a, u);
+                for (int c = w.c0; c < w.c1 && ok; ++done) {
+                    const uint32_t buf = done & 1, d = tmem + buf * 256;
+                    const int end = min(c + kSegment, w.c1);
+                    if (!(ok = waited(acc_empty + 8 * buf, (done / 2 & 1) ^ 1))) break;
+                    tc::fence_after();
+                    for (bool add = false; c < end; ++c, ++it, add = true) {
+                        const int s = it % kStages;
+                        if (!(ok = waited(conv + 8 * s, it / kStages & 1))) break;
+                        tc::fence_after();
+#pragma unroll
+                        for (int j = 0; j < kTokens / 16; ++j)
+                            tc::mma_f16<2>(d, tc::operand(dy_at + s * kDyBytes + j * 2048, 8192, 1024), tc::operand(x_at + s * kXBytes + j * 2048, 8192, 1024), what, add || j > 0);
+                        tc::mma_commit<2>(empty + 8 * s);
+                    }
+                    if (ok) tc::mma_commit<2>(acc_full + 8 * buf);
+                }
+            }
+            if (*(volatile int*)&failed) {
+                tc::mma_commit<2>(drain);
+                tc::bar_wait(drain, 0);
+            }
+        }
+    } else if (warp >= 4 && warp < 12) {
+        more_registers<kRegsSum>();
+        const int quad = warp % 4, half = (warp - 4) / 4;  // 32 rows, 128 columns
+        const uint32_t mine = out_at + (warp - 4) * 2048, from = tmem + half * 128 + ((uint32_t)quad * 32 << 16);
+        int done = 0;
+        bool ok = true;
+        for (int u = first; u < units && ok; u += stride) {
+            const Unit w = unit_of(a, u);
+            float sum[128];
+#pragma unroll
+            for (int i = 0; i < 128; ++i) sum[i] = 0.f;
+            for (int c = w.c0; c < w.c1; c += kSegment, ++done) {
+                const uint32_t buf = done & 1;
+                if (!(ok = waited(acc_full + 8 * buf, done / 2 & 1))) break;
+                tc::fence_after();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    uint32_t v[16];
+                    tc::tmem_load16(from + buf * 256 + j * 16, v);
+                    tc::tmem_wait_load();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sum[j * 16 + i] += __uint_as_float(v[i]);
+                }
+                tc::fence_before();                       // this accumulator may be summed into again
+                __syncwarp();
+                if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_empty + 8 * buf, 0));
+            }
+            if (!ok) break;
+            const long long r0 = (long long)w.tn * kTile + rank * kHalf + quad * 32;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                __syncwarp();
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" :: "r"(mine + lane * 64 + (q ^ (lane >> 1 & 3)) * 16), "f"(sum[j * 16 + 4 * q]), "f"(sum[j * 16 + 4 * q + 1]),
+                                 "f"(sum[j * 16 + 4 * q + 2]), "f"(sum[j * 16 + 4 * q + 3]) : "memory");
+                __syncwarp();
+                const long long c0 = (long long)w.tk * kTile + half * 128 + j * 16;
+                if (r0 < a.n && c0 < a.k) {
+                    if (a.partial) move_out<float>(mine, r0, c0, a.n, a.k, nullptr, a.partial + (long long)w.split * a.n * a.k, a.vec);
+                    else move_out<O>(mine, r0, c0, a.n, a.k, (const O*)a.base, (O*)a.dw, a.vec);
+                }
+            }
+        }
+    } else if (warp >= 12) {
+        fewer_registers<kRegsRestore>();
+        // the two groups of warps take chunks in turn; a thread has 16 columns c*16.. of rows t/8, t/8 + 16, + 32, + 48
+        const int t = threadIdx.x % 128, c = t % 8, late = c / 4, group = (warp - 12) / 4;
+        int it = 0;
+        bool ok = true;
+        for (int u = first; u < units && ok; u += stride) {
+            const Unit w = unit_of(a, u);
+            const int block = (w.tk * kTile + rank * kHalf) / 32 % 16 + c / 2;
+            for (int ch = w.c0; ch < w.c1; ++ch, ++it) {
+                if (it % kRestoreGroups != group) continue;
+                const int s = it % kStages;
+                if (!(ok = waited(full + 8 * s, it / kStages & 1))) break;
+                // 64 columns a swizzled row; lanes 4..7 of eight write their second piece first, so that the eight meet all banks
+                const uint32_t to = x_at + s * kXBytes + (c / 4) * 8192 + (t / 8) * 128;
+                const uint32_t even = to + ((c % 4 * 2 + late) ^ (t / 8 & 7)) * 16, odd = to + ((c % 4 * 2 + 1 - late) ^ (t / 8 & 7)) * 16;      // rows 16 apart: the same exchange
+                auto put = [&](int i, const uint32_t (&o)[8]) {
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(even + i * 2048), "r"(late ? o[4] : o[0]), "r"(late ? o[5] : o[1]), "r"(late ? o[6] : o[2]), "r"(late ? o[7] : o[3]) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(odd + i * 2048), "r"(late ? o[0] : o[4]), "r"(late ? o[1] : o[5]), "r"(late ? o[2] : o[6]), "r"(late ? o[3] : o[7]) : "memory");
+                };
+#pragma unroll
+                for (int h = 0; h < 4; h += 2) {
+                    uint32_t q[2][4], byte[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int row = t / 8 + (h + i) * 16;
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[i][0]), "=r"(q[i][1]), "=r"(q[i][2]), "=r"(q[i][3]) : "r"(code_at + s * kCodeBytes + row * 128 + c * 16));
+                        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte[i]) : "r"(scale_at + s * kScaleBytes + row * 16 + block));
+                    }
+                    if (__all_sync(0xffffffffu, Restore<T>::common(byte[0]) && Restore<T>::common(byte[1]))) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t f = Restore<T>::factor(byte[i]);
+                            uint32_t o[8];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) Restore<T>::four(q[i][j], f, o[2 * j], o[2 * j + 1]);
+                            put(h + i, o);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            uint32_t o[8];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) Restore<T>::four_any(q[i][j], byte[i], o[2 * j], o[2 * j + 1]);
+                            put(h + i, o);
+                        }
+                    }
+                }
+                tc::fence_async();
+                __syncwarp();
+                if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(conv + 8 * s, 0));
+            }
+        }
+    }
+    __syncwarp();
+    tc::fence_before();
+    __syncthreads();
+    tc::cluster_sync();                                   // neither CTA's memory is read by the other any more
+    if (threadIdx.x == 0 && failed) atomicAdd(&g_timeouts, 1u);
+    if (warp == 2) tc::tmem_free<2>(tmem, 512);
+}
+
+// dw = base + the splits' sums, in order.
+template <typename O>
+__global__ void __launch_bounds__(256) mx_wgrad_join_kernel(long long count, int splits, const float* __restrict__ partial, const O* base, O* dw)
+{
+    for (long long e = (long long)blockIdx.x * 256 + threadIdx.x; e < count; e += (long long)gridDim.x * 256) {
+        float v = partial[e];
+        for (int s = 1; s < splits; ++s) v += partial[s * count + e];
+        dw[e] = mx_round<O>(base ? mx_float(base[e]) + v : v);
+    }
+}
+
+template <typename O>
+__global__ void __launch_bounds__(256) mx_fill_kernel(long long count, const O* base, O* dw)
+{
+    for (long long e = (long long)blockIdx.x * 256 + threadIdx.x; e < count; e += (long long)gridDim.x * 256) dw[e] = base ? base[e] : mx_round<O>(0.f);
+}
+
+// Rows that bulk copies cannot take (not on 16-byte boundaries) into rows that they can.
+__global__ void __launch_bounds__(256) mx_align_kernel(long long rows, long long cols, const uint16_t* __restrict__ x, long long stride, uint16_t* __restrict__ out, long long pitch)
+{
+    for (long long r = blockIdx.x; r < rows; r += gridDim.x)
+        for (long long c = threadIdx.x; c < cols; c += 256) out[r * pitch + c] = x[r * stride + c];
+}
+
+struct WgradPlan { int tiles_n, tiles_k, splits, chunks, clusters; size_t aligned, partial, total; };
+
+WgradPlan plan_of(const galv_ctx* ctx, int64_t tokens, int64_t n, int64_t k, const void* dy, int64_t dy_stride)
+{
+    WgradPlan p;
+    const int most = ctx->num_sms / 2;
+    p.tiles_n = (int)((n + kTile - 1) / kTile);
+    p.tiles_k = (int)((k + kTile - 1) / kTile);
+    p.chunks = (int)((tokens + kTokens - 1) / kTokens);
+    const int64_t tiles = (int64_t)p.tiles_n * p.tiles_k;
+    p.splits = 1;
+    if (tiles < most && p.chunks >= 8) {
+        p.splits = (int)(most / tiles);
+        if (p.splits > p.chunks / 4) p.splits = p.chunks / 4;
+    }
+    const int64_t units = tiles * p.splits;
+    p.clusters = (int)(units < most ? units : most);
+    auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    p.aligned = mx_rows16(dy, dy_stride, GALV_BF16) && dy_stride * 2 < ((int64_t)1 << 40) ? 0 : up((size_t)tokens * ((n + 7) / 8 * 8) * 2);
+    p.partial = p.splits > 1 ? up((size_t)p.splits * n * k * 4) : 0;
+    p.total = p.aligned + p.partial;
+    return p;
+}
+
+template <typename T, typename O>
+cudaError_t launch(const WgradPlan& p, const CUtensorMap& dy, const CUtensorMap& codes, const CUtensorMap& scales, const WgradArgs& a, cudaStream_t st)
+{
+    cudaError_t e = cudaFuncSetAttribute(mx_wgrad_kernel<T, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+    mx_wgrad_kernel<T, O><<<p.clusters * 2, kThreads, kSmem, st>>>(dy, codes, scales, a);
+    if (a.partial) mx_wgrad_join_kernel<O><<<148 * 8, 256, 0, st>>>(a.n * a.k, a.splits, a.partial, (const O*)a.base, (O*)a.dw);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+extern "C" size_t galv_mx_weight_grad_workspace_bytes(const galv_ctx* ctx, int64_t tokens, int64_t n, int64_t k, const void* dy, int64_t dy_stride)
+{
+    if (!ctx || !mx_size_ok(tokens, n) || !mx_size_ok(tokens, k) || tokens == 0) return 0;
+    return plan_of(ctx, tokens, n, k, dy, dy_stride).total;
+}
+
+extern "C" int galv_mx_weight_grad(galv_ctx* ctx, int64_t tokens, int64_t n, int64_t k, const void* dy, int64_t dy_stride, int32_t dtype, const uint8_t* codes,
+                                   const uint8_t* scales, const void* base, void* dw, int32_t dw_dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx) return GALV_ERR_INVALID_ARG;
+    if (!mx_size_ok(tokens, n) || !mx_size_ok(tokens, k) || (dtype != GALV_BF16 && dtype != GALV_F16) || (dw_dtype != dtype && dw_dtype != GALV_F32))
+        return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_mx_weight_grad: sizes or types outside the limits");
+    if (!mx_matrix_ok(dw, k, k, dw_dtype) || (base && !mx_aligned(base, mx_size_of(dw_dtype))))
+        return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_mx_weight_grad: NULL or misaligned dw or base");
+    if (tokens > 0 && (!mx_matrix_ok(dy, dy_stride, n, dtype) || !codes || !scales || !mx_aligned(codes, 16) || !mx_aligned(scales, 16)))
+        return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_mx_weight_grad: NULL or misaligned pointer, or a row stride below n");
+    const size_t need = galv_mx_weight_grad_workspace_bytes(ctx, tokens, n, k, dy, dy_stride);
+    if (need && (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < need))
+        return galv_set_error(ctx, GALV_ERR_WORKSPACE, "galv_mx_weight_grad: workspace NULL, misaligned or too small");
+    MxDevice dev(ctx);
+    if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaError_t e = cudaSuccess;
+    if (tokens == 0) {
+        if (dw != base) {
+            if (dw_dtype == GALV_F32) mx_fill_kernel<float><<<ctx->num_sms * 8, 256, 0, st>>>(n * k, (const float*)base, (float*)dw);
+            else mx_fill_kernel<__half><<<ctx->num_sms * 8, 256, 0, st>>>(n * k, (const __half*)base, (__half*)dw);
+            e = cudaGetLastError();
+        }
+    } else {
+        const WgradPlan p = plan_of(ctx, tokens, n, k, dy, dy_stride);
+        const void* rows = dy;
+        int64_t stride = dy_stride;
+        if (p.aligned) {
+            stride = (n + 7) / 8 * 8;
+            mx_align_kernel<<<(int)(tokens < ctx->num_sms * 16 ? tokens : ctx->num_sms * 16), 256, 0, st>>>(tokens, n, (const uint16_t*)dy, dy_stride, (uint16_t*)workspace, stride);
+            rows = workspace;
+        }
+        CUtensorMap dm, cm, sm;
+        const CUtensorMapDataType type = dtype == GALV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+        e = galv_mx_map(&dm, type, rows, tokens, n, stride * 2, kTokens, 64, true);
+        if (e == cudaSuccess) e = galv_mx_map(&cm, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, tokens, mx_blocks(k) * 32, mx_blocks(k) * 32, kTokens, kHalf, false);
+        if (e == cudaSuccess) e = galv_mx_map(&sm, CU_TENSOR_MAP_DATA_TYPE_UINT8, scales, tokens, mx_pitch8(k), mx_pitch8(k), kTokens, 16, false);
+        if (e != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, "galv_mx_weight_grad: tensor map");
+        WgradArgs a;
+        a.tokens = tokens; a.n = n; a.k = k;
+        a.tiles_n = p.tiles_n; a.tiles_k = p.tiles_k; a.splits = p.splits; a.chunks = p.chunks;
+        a.base = base; a.dw = dw;
+        a.partial = p.partial ? reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + p.aligned) : nullptr;
+        const int four = p.partial ? 16 : 4 * mx_size_of(dw_dtype);
+        a.vec = k % 4 == 0 && (p.partial || (mx_aligned(dw, four) && mx_aligned(base, four)));
+        if (dtype == GALV_BF16) e = dw_dtype == GALV_F32 ? launch<__nv_bfloat16, float>(p, dm, cm, sm, a, st) : launch<__nv_bfloat16, __nv_bfloat16>(p, dm, cm, sm, a, st);
+        else e = dw_dtype == GALV_F32 ? launch<__half, float>(p, dm, cm, sm, a, st) : launch<__half, __half>(p, dm, cm, sm, a, st);
+    }
+    return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
+}
