@@ -3,7 +3,7 @@
 // The sum runs over tokens, along which the blocks' powers of two change, so they cannot be taken out of it: the kept values are restored to
 // dy's 16-bit type on their way to the tensor cores, exactly (4 significant bits and a power of two).  A pair of CTAs owns a tile of 256 x 256 of dw
 // (tcgen05.mma over both, M = N = 256): each stages 128 columns of dy and restores 128 columns of x, so every restored value is used 256 times.
-// Per CTA: a producer thread (bulk tensor copies of 64 tokens of dy, codes and scales), eight warps that restore (8 bits in, 16 bits out into
+// Per CTA: two threads that start bulk tensor copies (64 tokens of dy; of codes and scales), twelve warps that restore (8 bits in, 16 bits out into
 // the swizzled rows the tensor cores read), one thread that issues the matrix instructions for the pair, eight warps that take
 // sums from the tensor memory while the next are made (two accumulators of 256 columns fill it) and move results out.
 // Both operands lie with tokens along their rows ("MN-major"): dy and the codes are read as they are stored, nothing is transposed.
@@ -15,11 +15,13 @@
 
 namespace {
 
-constexpr int kStages = 5, kTokens = 64, kTile = 256, kHalf = kTile / 2;
+constexpr int kTokens = 64, kTile = 256, kHalf = kTile / 2;
+// Rings of chunks of 64 tokens, each held only while it is needed: dy from its copy to its product, restored x from restoring to the product, codes and
+// scales from their copy to restoring.  One ring of five chunks of all of them left the tensor cores waiting a third of the time.
+constexpr int kDyRing = 5, kXRing = 5, kCodeRing = 5;
 constexpr int kDyBytes = kTokens * kHalf * 2, kCodeBytes = kTokens * kHalf, kScaleBytes = kTokens * 16, kXBytes = kTokens * kHalf * 2;
-constexpr int kStageBytes = kDyBytes + kXBytes + kCodeBytes + kScaleBytes;
 constexpr int kOutBytes = 8 * 2048;                       // 32 x 16 sums of each warp that moves them out
-constexpr int kSmem = 1024 + kStages * kStageBytes + kOutBytes + 256;
+constexpr int kSmem = 1024 + kDyRing * kDyBytes + kXRing * kXBytes + kCodeRing * (kCodeBytes + kScaleBytes) + kOutBytes + 512;
 constexpr int kThreads = 768, kRestoreWarps = 4, kRestoreGroups = 3;      // warps: 4 for copies and matrix instructions, 8 for sums, three groups of 4 that restore
 // Registers of a thread of each: 128 * 24 + 256 * 168 + 384 * 40 = 768 * 80, what the block is launched with.
 constexpr int kRegsIssue = 24, kRegsSum = 168, kRegsRestore = 40;
@@ -172,9 +174,10 @@ mx_wgrad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constan
 {
     extern __shared__ unsigned char raw[];
     const uint32_t base = (tc::smem_at(raw) + 1023) & ~1023u;
-    const uint32_t dy_at = base, x_at = base + kStages * kDyBytes, code_at = x_at + kStages * kXBytes, scale_at = code_at + kStages * kCodeBytes;
-    const uint32_t out_at = scale_at + kStages * kScaleBytes, bars = out_at + kOutBytes;
-    const uint32_t full = bars, conv = bars + 8 * kStages, empty = bars + 16 * kStages, acc_full = bars + 24 * kStages, acc_empty = acc_full + 16, drain = acc_empty + 16,
+    const uint32_t dy_at = base, x_at = dy_at + kDyRing * kDyBytes, code_at = x_at + kXRing * kXBytes, scale_at = code_at + kCodeRing * kCodeBytes;
+    const uint32_t out_at = scale_at + kCodeRing * kScaleBytes, bars = out_at + kOutBytes;
+    const uint32_t dy_full = bars, dy_other = dy_full + 8 * kDyRing, dy_empty = dy_other + 8 * kDyRing, x_full = dy_empty + 8 * kDyRing, x_empty = x_full + 8 * kXRing,
+                   code_full = x_empty + 8 * kXRing, code_empty = code_full + 8 * kCodeRing, acc_full = code_empty + 8 * kCodeRing, acc_empty = acc_full + 16, drain = acc_empty + 16,
                    slot = drain + 8;
     __shared__ int failed;
 
@@ -183,10 +186,18 @@ mx_wgrad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constan
     const int units = a.tiles_n * a.tiles_k * a.splits, first = blockIdx.x / 2, stride = gridDim.x / 2;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
-            tc::bar_init(full + 8 * s, 1);
-            tc::bar_init(conv + 8 * s, 2 * kRestoreWarps);
-            tc::bar_init(empty + 8 * s, 1);
+        for (int s = 0; s < kDyRing; ++s) {
+            tc::bar_init(dy_full + 8 * s, 1);
+            tc::bar_init(dy_other + 8 * s, 1);
+            tc::bar_init(dy_empty + 8 * s, 1);
+        }
+        for (int s = 0; s < kXRing; ++s) {
+            tc::bar_init(x_full + 8 * s, 2 * kRestoreWarps);
+            tc::bar_init(x_empty + 8 * s, 1);
+        }
+        for (int s = 0; s < kCodeRing; ++s) {
+            tc::bar_init(code_full + 8 * s, 1);
+            tc::bar_init(code_empty + 8 * s, kRestoreWarps);
         }
         for (int b = 0; b < 2; ++b) {
             tc::bar_init(acc_full + 8 * b, 1);
@@ -215,29 +226,57 @@ mx_wgrad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constan
     };
 
     if (warp < 4) fewer_registers<kRegsIssue>();
-    if (warp == 0) {
+    if (warp == 0) {                                      // copies of codes and scales
         if (tc::elect()) {
             int it = 0;
             bool ok = true;
             for (int u = first; u < units && ok; u += stride) {
                 const Unit w = unit_of(a, u);
-                const int n0 = w.tn * kTile + rank * kHalf, k0 = w.tk * kTile + rank * kHalf;
+                const int k0 = w.tk * kTile + rank * kHalf;
                 for (int c = w.c0; c < w.c1; ++c, ++it) {
-                    const int s = it % kStages;
-                    if (!(ok = waited(empty + 8 * s, (it / kStages & 1) ^ 1))) break;
-                    const uint32_t bar = full + 8 * s;
-                    tc::bar_expect(bar, kDyBytes + kCodeBytes + kScaleBytes);
-                    tc::load_2d(dy_at + s * kDyBytes, &dy_map, n0, c * kTokens, bar);
-                    tc::load_2d(dy_at + s * kDyBytes + kDyBytes / 2, &dy_map, n0 + 64, c * kTokens, bar);
-                    tc::load_2d(code_at + s * kCodeBytes, &code_map, k0, c * kTokens, bar);
-                    tc::load_2d(scale_at + s * kScaleBytes, &scale_map, k0 / 32 & ~15, c * kTokens, bar);
+                    const int s = it % kCodeRing;
+                    if (!(ok = waited(code_empty + 8 * s, (it / kCodeRing & 1) ^ 1))) break;
+                    tc::bar_expect(code_full + 8 * s, kCodeBytes + kScaleBytes);
+                    tc::load_2d(code_at + s * kCodeBytes, &code_map, k0, c * kTokens, code_full + 8 * s);
+                    tc::load_2d(scale_at + s * kScaleBytes, &scale_map, k0 / 32 & ~15, c * kTokens, code_full + 8 * s);
                 }
             }
             if (*(volatile int*)&failed)                  // copies still in flight
-                for (int i = it < kStages ? 0 : it - kStages; i < it; ++i) tc::bar_wait(full + 8 * (i % kStages), i / kStages & 1);
+                for (int i = it < kCodeRing ? 0 : it - kCodeRing; i < it; ++i) tc::bar_wait(code_full + 8 * (i % kCodeRing), i / kCodeRing & 1);
+        }
+    } else if (warp == 3) {                               // copies of dy
+        if (tc::elect()) {
+            int it = 0;
+            bool ok = true;
+            for (int u = first; u < units && ok; u += stride) {
+                const Unit w = unit_of(a, u);
+                const int n0 = w.tn * kTile + rank * kHalf;
+                for (int c = w.c0; c < w.c1; ++c, ++it) {
+                    const int s = it % kDyRing;
+                    if (!(ok = waited(dy_empty + 8 * s, (it / kDyRing & 1) ^ 1))) break;
+                    tc::bar_expect(dy_full + 8 * s, kDyBytes);
+                    tc::load_2d(dy_at + s * kDyBytes, &dy_map, n0, c * kTokens, dy_full + 8 * s);
+                    tc::load_2d(dy_at + s * kDyBytes + kDyBytes / 2, &dy_map, n0 + 64, c * kTokens, dy_full + 8 * s);
+                }
+            }
+            if (*(volatile int*)&failed)
+                for (int i = it < kDyRing ? 0 : it - kDyRing; i < it; ++i) tc::bar_wait(dy_full + 8 * (i % kDyRing), i / kDyRing & 1);
+        }
+    } else if (warp == 1 && rank == 1) {                  // tells the first CTA that this one's dy is there
+        if (tc::elect()) {
+            int it = 0;
+            bool ok = true;
+            for (int u = first; u < units && ok; u += stride) {
+                const Unit w = unit_of(a, u);
+                for (int c = w.c0; c < w.c1; ++c, ++it) {
+                    const int s = it % kDyRing;
+                    if (!(ok = waited(dy_full + 8 * s, it / kDyRing & 1))) break;
+                    tc::bar_arrive_cluster(tc::in_cta(dy_other + 8 * s, 0));
+                }
+            }
         }
     } else if (warp == 1) {
-        if (rank == 0 && tc::elect()) {
+        if (tc::elect()) {
             // fp32 sums, A and B of type T with the summed index across the rows, 256 x 256
             constexpr uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
             constexpr uint32_t what = 1u << 4 | type << 7 | type << 10 | 1u << 15 | 1u << 16 | (uint32_t)(kTile >> 3) << 17 | (uint32_t)(kTile >> 4) << 24;
@@ -251,13 +290,14 @@ mx_wgrad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constan
                     if (!(ok = waited(acc_empty + 8 * buf, (done / 2 & 1) ^ 1))) break;
                     tc::fence_after();
                     for (bool add = false; c < end; ++c, ++it, add = true) {
-                        const int s = it % kStages;
-                        if (!(ok = waited(conv + 8 * s, it / kStages & 1))) break;
+                        const int s = it % kDyRing, x = it % kXRing;
+                        if (!(ok = waited(dy_full + 8 * s, it / kDyRing & 1) && waited(dy_other + 8 * s, it / kDyRing & 1) && waited(x_full + 8 * x, it / kXRing & 1))) break;
                         tc::fence_after();
 #pragma unroll
                         for (int j = 0; j < kTokens / 16; ++j)
-                            tc::mma_f16<2>(d, tc::operand(dy_at + s * kDyBytes + j * 2048, 8192, 1024), tc::operand(x_at + s * kXBytes + j * 2048, 8192, 1024), what, add || j > 0);
-                        tc::mma_commit<2>(empty + 8 * s);
+                            tc::mma_f16<2>(d, tc::operand(dy_at + s * kDyBytes + j * 2048, 8192, 1024), tc::operand(x_at + x * kXBytes + j * 2048, 8192, 1024), what, add || j > 0);
+                        tc::mma_commit<2>(dy_empty + 8 * s);
+                        tc::mma_commit<2>(x_empty + 8 * x);
                     }
                     if (ok) tc::mma_commit<2>(acc_full + 8 * buf);
                 }
@@ -313,55 +353,60 @@ mx_wgrad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constan
         }
     } else if (warp >= 12) {
         fewer_registers<kRegsRestore>();
-        // the two groups of warps take chunks in turn; a thread has 16 columns c*16.. of rows t/8, t/8 + 16, + 32, + 48
-        const int t = threadIdx.x % 128, c = t % 8, late = c / 4, group = (warp - 12) / 4;
+        // The groups of warps take chunks in turn.  A thread restores four pieces of 16 elements: columns c*16.. and (c+4)*16.. of rows r and r + 8.  Eight
+        // lanes are eight rows: both the codes' and the restored rows' 16-byte pieces are exchanged by row % 8, so the eight meet all banks.
+        const int t = threadIdx.x % 128, c = t % 32 / 8, r = t / 32 * 16 + t % 8, group = (warp - 12) / 4;
         int it = 0;
         bool ok = true;
         for (int u = first; u < units && ok; u += stride) {
             const Unit w = unit_of(a, u);
-            const int block = (w.tk * kTile + rank * kHalf) / 32 % 16 + c / 2;
+            const uint32_t scale_from = scale_at + r * 16 + (w.tk * kTile + rank * kHalf) / 32 % 16 + c / 2;
             for (int ch = w.c0; ch < w.c1; ++ch, ++it) {
                 if (it % kRestoreGroups != group) continue;
-                const int s = it % kStages;
-                if (!(ok = waited(full + 8 * s, it / kStages & 1))) break;
-                // 64 columns a swizzled row; lanes 4..7 of eight write their second piece first, so that the eight meet all banks
-                const uint32_t to = x_at + s * kXBytes + (c / 4) * 8192 + (t / 8) * 128;
-                const uint32_t even = to + ((c % 4 * 2 + late) ^ (t / 8 & 7)) * 16, odd = to + ((c % 4 * 2 + 1 - late) ^ (t / 8 & 7)) * 16;      // rows 16 apart: the same exchange
-                auto put = [&](int i, const uint32_t (&o)[8]) {
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(even + i * 2048), "r"(late ? o[4] : o[0]), "r"(late ? o[5] : o[1]), "r"(late ? o[6] : o[2]), "r"(late ? o[7] : o[3]) : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(odd + i * 2048), "r"(late ? o[0] : o[4]), "r"(late ? o[1] : o[5]), "r"(late ? o[2] : o[6]), "r"(late ? o[3] : o[7]) : "memory");
+                const int s = it % kCodeRing, x = it % kXRing;
+                if (!(ok = waited(code_full + 8 * s, it / kCodeRing & 1) && waited(x_empty + 8 * x, (it / kXRing & 1) ^ 1))) break;
+                uint32_t byte[2][2], from[2], to[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte[i][h]) : "r"(scale_from + s * kScaleBytes + i * 128 + h * 2));
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {             // 64 columns a restored row
+                    from[h] = code_at + s * kCodeBytes + r * 128 + ((c + 4 * h) ^ (r & 7)) * 16;
+                    to[h] = x_at + x * kXBytes + h * 8192 + r * 128 + ((2 * c) ^ (r & 7)) * 16;
+                }
+                const bool common = Restore<T>::common(byte[0][0]) && Restore<T>::common(byte[0][1]) && Restore<T>::common(byte[1][0]) && Restore<T>::common(byte[1][1]);
+                auto piece = [&](int i, int h, auto four) {
+                    uint32_t q[4], o[8];
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]) : "r"(from[h] + i * 1024));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) four(q[j], o[2 * j], o[2 * j + 1]);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(to[h] + i * 1024), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"((to[h] ^ 16) + i * 1024), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
                 };
+                if (__all_sync(0xffffffffu, common)) {
 #pragma unroll
-                for (int h = 0; h < 4; h += 2) {
-                    uint32_t q[2][4], byte[2];
+                    for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int row = t / 8 + (h + i) * 16;
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[i][0]), "=r"(q[i][1]), "=r"(q[i][2]), "=r"(q[i][3]) : "r"(code_at + s * kCodeBytes + row * 128 + c * 16));
-                        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte[i]) : "r"(scale_at + s * kScaleBytes + row * 16 + block));
-                    }
-                    if (__all_sync(0xffffffffu, Restore<T>::common(byte[0]) && Restore<T>::common(byte[1]))) {
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const uint32_t f = Restore<T>::factor(byte[i]);
-                            uint32_t o[8];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) Restore<T>::four(q[i][j], f, o[2 * j], o[2 * j + 1]);
-                            put(h + i, o);
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t f = Restore<T>::factor(byte[i][h]);
+                            piece(i, h, [f](uint32_t v, uint32_t& lo, uint32_t& hi) { Restore<T>::four(v, f, lo, hi); });
                         }
-                    } else {
+                } else {
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            uint32_t o[8];
+                    for (int i = 0; i < 2; ++i)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) Restore<T>::four_any(q[i][j], byte[i], o[2 * j], o[2 * j + 1]);
-                            put(h + i, o);
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t b = byte[i][h];
+                            piece(i, h, [b](uint32_t v, uint32_t& lo, uint32_t& hi) { Restore<T>::four_any(v, b, lo, hi); });
                         }
-                    }
                 }
                 tc::fence_async();
                 __syncwarp();
-                if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(conv + 8 * s, 0));
+                if (lane == 0) {
+                    tc::bar_arrive(code_empty + 8 * s);
+                    tc::bar_arrive_cluster(tc::in_cta(x_full + 8 * x, 0));
+                }
             }
         }
     }
@@ -474,7 +519,7 @@ extern "C" int galv_mx_weight_grad(galv_ctx* ctx, int64_t tokens, int64_t n, int
         CUtensorMap dm, cm, sm;
         const CUtensorMapDataType type = dtype == GALV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
         e = galv_mx_map(&dm, type, rows, tokens, n, stride * 2, kTokens, 64, true);
-        if (e == cudaSuccess) e = galv_mx_map(&cm, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, tokens, mx_blocks(k) * 32, mx_blocks(k) * 32, kTokens, kHalf, false);
+        if (e == cudaSuccess) e = galv_mx_map(&cm, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, tokens, mx_blocks(k) * 32, mx_blocks(k) * 32, kTokens, kHalf, true);
         if (e == cudaSuccess) e = galv_mx_map(&sm, CU_TENSOR_MAP_DATA_TYPE_UINT8, scales, tokens, mx_pitch8(k), mx_pitch8(k), kTokens, 16, false);
         if (e != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, "galv_mx_weight_grad: tensor map");
         WgradArgs a;
