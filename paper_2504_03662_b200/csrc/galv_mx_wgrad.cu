@@ -119,47 +119,77 @@ template <typename O> struct Four;
 template <> struct Four<float> { using type = float4; };
 template <> struct Four<__nv_bfloat16> { using type = uint2; };
 template <> struct Four<__half> { using type = uint2; };
+template <typename O> __device__ __forceinline__ float2 two(uint32_t w);
+template <> __device__ __forceinline__ float2 two<__nv_bfloat16>(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+template <> __device__ __forceinline__ float2 two<__half>(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+template <typename O> __device__ __forceinline__ uint32_t join(float a, float b);
+template <> __device__ __forceinline__ uint32_t join<__nv_bfloat16>(float a, float b) { const __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t*>(&h); }
+template <> __device__ __forceinline__ uint32_t join<__half>(float a, float b) { const __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<const uint32_t*>(&h); }
+template <typename Q, typename O> struct AddFour {
+    static __device__ __forceinline__ void to(float (&v)[4], const Q& q)
+    {
+        const float2 a = two<O>(q.x), b = two<O>(q.y);
+        v[0] += a.x; v[1] += a.y; v[2] += b.x; v[3] += b.y;
+    }
+};
+template <typename O> struct AddFour<float4, O> { static __device__ __forceinline__ void to(float (&v)[4], const float4& q) { v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w; } };
+template <typename Q, typename O> struct RoundFour { static __device__ __forceinline__ Q of(const float (&v)[4]) { return make_uint2(join<O>(v[0], v[1]), join<O>(v[2], v[3])); } };
+template <typename O> struct RoundFour<float4, O> { static __device__ __forceinline__ float4 of(const float (&v)[4]) { return make_float4(v[0], v[1], v[2], v[3]); } };
 
-// 32 x 16 sums from the warp's shared memory (rows of 64 bytes, their 16-byte pieces exchanged by row / 2 % 4) to rows r0.. and columns c0.. of an
-// [n][k] matrix.
+// A warp's 32 x 128 sums in tensor memory, a row a lane, to a matrix with rows k apart: 16 columns at a time go through the warp's shared memory
+// (rows of 64 bytes, their 16-byte pieces exchanged by row / 2 % 4), so that lanes next to one another write next to one another.  base and out point to
+// the thread's first place; `rows` and `cols` of them exist.  All loads of a round come before its first store: out may be base.
 template <typename O>
-__device__ __forceinline__ void move_out(uint32_t from, long long r0, long long c0, long long n, long long k, const O* base, O* out, bool vec)
+__device__ __forceinline__ void move_out(uint32_t tmem, uint32_t mine, const O* base, O* out, long long k, int rows, int cols, bool vec)
 {
     const int lane = threadIdx.x % 32;
-    if (vec) {
-        const long long c = c0 + lane % 4 * 4;
-        if (c >= k) return;                               // k is a multiple of 4 here
-        using Q = typename Four<O>::type;
-        Q q[4];
-        if (base) {                                       // all loads first: out may be base
+    using Q = typename Four<O>::type;
+    // vec: a lane has 4 columns of rows lane / 4 + 8 i, k is a multiple of 4; else one column of rows lane / 16 + 2 i
+    const uint32_t from = vec ? mine + lane / 4 * 64 + ((lane % 4) ^ (lane >> 3 & 3)) * 16 : mine + lane / 16 * 64 + lane % 4 * 4, piece = lane % 16 / 4;
+    rows -= vec ? lane / 4 : lane / 16;
+    cols -= vec ? lane % 4 * 4 : lane % 16;
+#pragma unroll 1
+    for (int j = 0; j < 128; j += 16) {
+        uint32_t s[16];
+        tc::tmem_load16(tmem + j, s);
+        tc::tmem_wait_load();
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(mine + lane * 64 + (q ^ (lane >> 1 & 3)) * 16), "r"(s[4 * q]), "r"(s[4 * q + 1]), "r"(s[4 * q + 2]), "r"(s[4 * q + 3]) : "memory");
+        __syncwarp();
+        const bool in = j < cols;
+        if (vec) {
+            float v[4][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (r0 + i * 8 + lane / 4 < n) q[i] = *reinterpret_cast<const Q*>(base + (r0 + i * 8 + lane / 4) * k + c);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = i * 8 + lane / 4;
-            if (r0 + row >= n) continue;
-            float v[4];
-            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(from + row * 64 + ((lane % 4) ^ (row >> 1 & 3)) * 16));
-            O* e = reinterpret_cast<O*>(&q[i]);
+                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[i][0]), "=f"(v[i][1]), "=f"(v[i][2]), "=f"(v[i][3]) : "r"(from + i * 512));
             if (base) {
+                Q q[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] += mx_float(e[j]);
+                for (int i = 0; i < 4; ++i)
+                    if (in && i * 8 < rows) q[i] = *reinterpret_cast<const Q*>(base + i * 8 * k + j);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) AddFour<Q, O>::to(v[i], q[i]);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] = mx_round<O>(v[j]);
-            *reinterpret_cast<Q*>(out + (r0 + row) * k + c) = q[i];
-        }
-    } else {
-        const long long c = c0 + lane % 16;
-        if (c >= k) return;
-        for (int row = lane / 16; row < 32 && r0 + row < n; row += 2) {
-            float v;
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(from + row * 64 + ((lane % 16 / 4) ^ (row >> 1 & 3)) * 16 + lane % 4 * 4));
-            const long long at = (r0 + row) * k + c;
-            if (base) v += mx_float(base[at]);
-            out[at] = mx_round<O>(v);
+            for (int i = 0; i < 4; ++i)
+                if (in && i * 8 < rows) *reinterpret_cast<Q*>(out + i * 8 * k + j) = RoundFour<Q, O>::of(v[i]);
+        } else {
+#pragma unroll
+            for (int h = 0; h < 32; h += 16) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[i]) : "r"(from + (h + 2 * i) * 64 + (piece ^ (i & 3)) * 16));
+                if (base) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (in && h + 2 * i < rows) v[i] += mx_float(base[(h + 2 * i) * k + j]);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (in && h + 2 * i < rows) out[(h + 2 * i) * k + j] = mx_round<O>(v[i]);
+            }
         }
     }
 }
@@ -315,41 +345,46 @@ mx_wgrad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constan
         bool ok = true;
         for (int u = first; u < units && ok; u += stride) {
             const Unit w = unit_of(a, u);
-            float sum[128];
+            uint32_t buf = done & 1;
+            if (w.c1 - w.c0 > kSegment) {                 // earlier segments are taken up here, the last one is added where it lies
+                float sum[128];
 #pragma unroll
-            for (int i = 0; i < 128; ++i) sum[i] = 0.f;
-            for (int c = w.c0; c < w.c1; c += kSegment, ++done) {
-                const uint32_t buf = done & 1;
-                if (!(ok = waited(acc_full + 8 * buf, done / 2 & 1))) break;
-                tc::fence_after();
+                for (int i = 0; i < 128; ++i) sum[i] = 0.f;
+                for (int c = w.c0; c < w.c1; c += kSegment) {
+                    buf = done & 1;
+                    if (!(ok = waited(acc_full + 8 * buf, done / 2 & 1))) break;
+                    tc::fence_after();
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    uint32_t v[16];
-                    tc::tmem_load16(from + buf * 256 + j * 16, v);
-                    tc::tmem_wait_load();
+                    for (int j = 0; j < 128; j += 16) {
+                        uint32_t v[16];
+                        tc::tmem_load16(from + buf * 256 + j, v);
+                        tc::tmem_wait_load();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) sum[j * 16 + i] += __uint_as_float(v[i]);
+                        for (int i = 0; i < 16; ++i) sum[j + i] += __uint_as_float(v[i]);
+                    }
+                    if (c + kSegment < w.c1) {            // this accumulator may be summed into again
+                        tc::fence_before();
+                        __syncwarp();
+                        if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_empty + 8 * buf, 0));
+                        ++done;
+                    }
                 }
-                tc::fence_before();                       // this accumulator may be summed into again
-                __syncwarp();
-                if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_empty + 8 * buf, 0));
+#pragma unroll
+                for (int j = 0; j < 128; j += 16) tc::tmem_store16(from + buf * 256 + j, sum + j);
+                tc::tmem_wait_store();
+            } else if ((ok = waited(acc_full + 8 * buf, done / 2 & 1))) {
+                tc::fence_after();
             }
             if (!ok) break;
-            const long long r0 = (long long)w.tn * kTile + rank * kHalf + quad * 32;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                __syncwarp();
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" :: "r"(mine + lane * 64 + (q ^ (lane >> 1 & 3)) * 16), "f"(sum[j * 16 + 4 * q]), "f"(sum[j * 16 + 4 * q + 1]),
-                                 "f"(sum[j * 16 + 4 * q + 2]), "f"(sum[j * 16 + 4 * q + 3]) : "memory");
-                __syncwarp();
-                const long long c0 = (long long)w.tk * kTile + half * 128 + j * 16;
-                if (r0 < a.n && c0 < a.k) {
-                    if (a.partial) move_out<float>(mine, r0, c0, a.n, a.k, nullptr, a.partial + (long long)w.split * a.n * a.k, a.vec);
-                    else move_out<O>(mine, r0, c0, a.n, a.k, (const O*)a.base, (O*)a.dw, a.vec);
-                }
-            }
+            const long long r0 = (long long)w.tn * kTile + rank * kHalf + quad * 32, c0 = (long long)w.tk * kTile + half * 128;
+            const int rows = (int)min(32ll, a.n - r0), cols = (int)min(128ll, a.k - c0);
+            const long long at = (r0 + (a.vec ? lane / 4 : lane / 16)) * a.k + c0 + (a.vec ? lane % 4 * 4 : lane % 16);
+            if (a.partial) move_out<float>(from + buf * 256, mine, nullptr, a.partial + (w.split * a.n * a.k + at), a.k, rows, cols, a.vec);
+            else move_out<O>(from + buf * 256, mine, a.base ? (const O*)a.base + at : nullptr, (O*)a.dw + at, a.k, rows, cols, a.vec);
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_empty + 8 * buf, 0));
+            ++done;
         }
     } else if (warp >= 12) {
         fewer_registers<kRegsRestore>();
