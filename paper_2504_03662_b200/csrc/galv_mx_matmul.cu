@@ -1,74 +1,320 @@
-// Product of two tensors held in 4 bits.
+// Product of two matrices held in 4 bits: y[i][j] = sum_k a[i][k] b[j][k] + bias[j].
+//
+// The tensor cores take the elements as they are held and the blocks' powers of two beside them (tcgen05.mma kind::mxf4 with block scales), so
+// nothing is restored.  A pair of CTAs owns a tile of 256 x 256 of y: each stages 128 rows of a and of b, 256 columns (128 bytes a row) at a time, its own
+// rows' scales of a and all 256 rows' scales of b; the scales lie in memory in the order in which they go to tensor memory (galv.h).
+// Tensor memory: two accumulators of 256 columns that share 48 of them, and 24 columns of scales.  The warps that move a tile out begin with
+// the shared columns, after which the next tile's sums may start.
 
 #include "galv_mx.cuh"
+#include "galv_tc.cuh"
 
 namespace {
 
-constexpr int kTile = 64, kDeep = 16, kThreads = 256;
+constexpr int kStages = 5, kTile = 256, kHalf = kTile / 2, kChunkBytes = 128, kChunkBlocks = 8;      // 256 columns a chunk
+constexpr int kRowsBytes = kHalf * kChunkBytes, kScaleA = 1024, kScaleB = 2048;
+constexpr int kStageBytes = 2 * kRowsBytes + kScaleA + kScaleB;
+constexpr int kOutBytes = 8 * 2048;
+constexpr int kSmem = 1024 + kStages * kStageBytes + kOutBytes + 256;
+constexpr int kThreads = 384;
+constexpr int kSecond = 208, kShared = kTile - kSecond, kScalesAt = kSecond + kTile;                 // columns of tensor memory
+constexpr int kGroup = 8;                                 // tiles along m whose rows of a stay in L2 while their n runs
 
-// 64 x 64 outputs a CTA, 4 x 4 a thread, fp32 sums in order of the summed index.
-__device__ __forceinline__ void tile_step(const float (*a)[kTile + 4], const float (*b)[kTile + 4], int ty, int tx, float (&acc)[4][4])
+struct MatmulArgs {
+    long long m, n, stride;
+    int blocks, groups;                                   // of 32 columns; of 4 blocks
+    int tiles_m, tiles_n, splits, chunks;
+    const uint8_t* a_scales;
+    const uint8_t* b_scales;
+    const void* bias;
+    void* y;
+    float* partial;                                       // [splits][m][n], or NULL
+    int vec;                                              // four results of a row can be moved at once
+};
+
+__device__ unsigned int g_timeouts;
+
+struct Unit { int tm, tn, split, c0, c1; };
+__device__ __forceinline__ Unit unit_of(const MatmulArgs& a, int u)
 {
+    Unit w;
+    const int tile = u / a.splits, per = kGroup * a.tiles_n, first = tile / per * kGroup;
+    const int size = min(kGroup, a.tiles_m - first);
+    w.split = u % a.splits;
+    w.tm = first + tile % per % size;
+    w.tn = tile % per / size;
+    w.c0 = (int)((long long)w.split * a.chunks / a.splits);
+    w.c1 = (int)((long long)(w.split + 1) * a.chunks / a.splits);
+    return w;
+}
+
+template <typename O> struct Four;
+template <> struct Four<float> {
+    using type = float4;
+    static __device__ __forceinline__ float4 of(const float (&v)[4]) { return make_float4(v[0], v[1], v[2], v[3]); }
+};
+template <> struct Four<__nv_bfloat16> {
+    using type = uint2;
+    static __device__ __forceinline__ uint32_t two(float a, float b) { const __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t*>(&h); }
+    static __device__ __forceinline__ uint2 of(const float (&v)[4]) { return make_uint2(two(v[0], v[1]), two(v[2], v[3])); }
+};
+template <> struct Four<__half> {
+    using type = uint2;
+    static __device__ __forceinline__ uint32_t two(float a, float b) { const __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<const uint32_t*>(&h); }
+    static __device__ __forceinline__ uint2 of(const float (&v)[4]) { return make_uint2(two(v[0], v[1]), two(v[2], v[3])); }
+};
+
+// 16 columns of a warp's 32 rows of sums to y, through the warp's shared memory (rows of 64 bytes, their 16-byte pieces exchanged by row / 2 % 4).
+// bias and out point to the thread's first place of these columns; `rows` and `cols` of them exist from there.
+template <typename O>
+__device__ __forceinline__ void move_out(uint32_t tmem, uint32_t mine, const O* bias, O* out, long long stride, int rows, int cols, bool vec)
+{
+    const int lane = threadIdx.x % 32;
+    uint32_t s[16];
+    tc::tmem_load16(tmem, s);
+    tc::tmem_wait_load();
+    __syncwarp();
 #pragma unroll
-    for (int k = 0; k < kDeep; ++k) {
-        float u[4], v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { u[i] = a[k][ty * 4 + i]; v[i] = b[k][tx * 4 + i]; }
+    for (int q = 0; q < 4; ++q)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(mine + lane * 64 + (q ^ (lane >> 1 & 3)) * 16), "r"(s[4 * q]), "r"(s[4 * q + 1]), "r"(s[4 * q + 2]), "r"(s[4 * q + 3]) : "memory");
+    __syncwarp();
+    if (vec) {
+        float v[4][4], b[4] = {};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[i][0]), "=f"(v[i][1]), "=f"(v[i][2]), "=f"(v[i][3])
+                         : "r"(mine + lane / 4 * 64 + ((lane % 4) ^ (lane >> 3 & 3)) * 16 + i * 512));
+        if (bias && cols > 0) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(u[i], v[j], acc[i][j]);
+            for (int j = 0; j < 4; ++j) b[j] = mx_float(bias[j]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i][j] += b[j];
+            if (cols > 0 && i * 8 < rows) *reinterpret_cast<typename Four<O>::type*>(out + i * 8 * stride) = Four<O>::of(v[i]);
+        }
+    } else {
+        const float b = bias && cols > 0 ? mx_float(bias[0]) : 0.f;
+#pragma unroll
+        for (int h = 0; h < 32; h += 16) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[i]) : "r"(mine + lane / 16 * 64 + lane % 4 * 4 + (h + 2 * i) * 64 + ((lane % 16 / 4) ^ (i & 3)) * 16));
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (cols > 0 && h + 2 * i < rows) out[(h + 2 * i) * stride] = mx_round<O>(v[i] + b);
+        }
     }
 }
 
-// The elements of 16 columns are multiplied as they are and the sum takes the two blocks' powers of two at once: a held value alone may pass fp32's
-// range (6 * 2^126 is one) where the product does not.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) mx_matmul_simple_kernel(long long m, long long n, long long nb, const uint8_t* __restrict__ ac, const uint8_t* __restrict__ as,
-                                                                    const uint8_t* __restrict__ bc, const uint8_t* __restrict__ bs, const T* __restrict__ bias,
-                                                                    T* __restrict__ y, long long y_stride)
+template <typename O>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+mx_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const __grid_constant__ MatmulArgs a)
 {
-    __shared__ float a[kDeep][kTile + 4], b[kDeep][kTile + 4];
-    __shared__ int sc[2][kTile];
-    const long long m0 = (long long)blockIdx.y * kTile, n0 = (long long)blockIdx.x * kTile, tiles = (nb + 3) / 4;
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    float acc[4][4] = {};
-    for (long long p0 = 0; p0 < nb * 4; p0 += kDeep / 8) {
-        __syncthreads();
-        const int which = threadIdx.x / 128, r = threadIdx.x % 128 / 2, p = threadIdx.x % 2;
-        const long long row = (which ? n0 : m0) + r;
-        float v[8] = {};
-        int byte = 0;
-        if (row < (which ? n : m)) {
-            mx_from4(*reinterpret_cast<const uint32_t*>((which ? bc : ac) + row * nb * 16 + (p0 + p) * 4), v);
-            byte = (which ? bs : as)[mx_scale_at<GALV_MX4>(row, p0 >> 2, tiles)];
+    extern __shared__ unsigned char raw[];
+    const uint32_t base = (tc::smem_at(raw) + 1023) & ~1023u;
+    const uint32_t a_at = base, b_at = a_at + kStages * kRowsBytes, sa_at = b_at + kStages * kRowsBytes, sb_at = sa_at + kStages * kScaleA, out_at = sb_at + kStages * kScaleB,
+                   bars = out_at + kOutBytes;
+    const uint32_t full = bars, other = full + 8 * kStages, empty = other + 8 * kStages, acc_full = empty + 8 * kStages, acc_free = acc_full + 16, drain = acc_free + 8, slot = drain + 8;
+    __shared__ int failed;
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = tc::cluster_rank();
+    const int units = a.tiles_m * a.tiles_n * a.splits, first = blockIdx.x / 2, stride = gridDim.x / 2;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            tc::bar_init(full + 8 * s, 1);
+            tc::bar_init(other + 8 * s, 1);
+            tc::bar_init(empty + 8 * s, 1);
         }
-        if (p == 0) sc[which][r] = byte;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) (which ? b : a)[p * 8 + i][r] = byte == 255 ? __uint_as_float(0x7fc00000u) : v[i];
-        __syncthreads();
-        float part[4][4] = {};
-        tile_step(a, b, ty, tx, part);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] += ldexpf(part[i][j], sc[0][ty * 4 + i] + sc[1][tx * 4 + j] - 254);
+        for (int b = 0; b < 2; ++b) tc::bar_init(acc_full + 8 * b, 1);
+        tc::bar_init(acc_free, 16);
+        tc::bar_init(drain, 1);
+        tc::bar_init_done();
+        failed = 0;
+        tc::prefetch_map(&a_map);
+        tc::prefetch_map(&b_map);
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const long long r = m0 + ty * 4 + i, c = n0 + tx * 4 + j;
-            if (r < m && c < n) y[r * y_stride + c] = mx_round<T>(bias ? acc[i][j] + mx_float(bias[c]) : acc[i][j]);
+    if (warp == 2) tc::tmem_alloc<2>(slot, 512);
+    tc::fence_before();
+    __syncthreads();
+    tc::cluster_sync();                                   // the pair's barriers exist
+    tc::fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+
+    auto waited = [&](uint32_t bar, uint32_t parity) {
+        if (tc::bar_wait(bar, parity)) return true;
+        *(volatile int*)&failed = 1;
+        return false;
+    };
+
+    if (warp == 0) {
+        if (tc::elect()) {
+            int it = 0;
+            bool ok = true;
+            for (int u = first; u < units && ok; u += stride) {
+                const Unit w = unit_of(a, u);
+                const int m0 = w.tm * kTile + rank * kHalf, n0 = w.tn * kTile + rank * kHalf;
+                // tiles of scales: rows of this CTA of a, all rows of the pair of b; those behind the last row do not exist
+                const bool a_in = m0 < a.m, b_in = w.tn * kTile + kHalf < a.n;
+                const uint8_t* sa = a.a_scales + (long long)(m0 / 128) * a.groups * 512;
+                const uint8_t* sb = a.b_scales + (long long)(w.tn * 2) * a.groups * 512;
+                for (int c = w.c0; c < w.c1; ++c, ++it) {
+                    const int s = it % kStages;
+                    const uint32_t bar = full + 8 * s, bytes = min(2, a.groups - 2 * c) * 512;
+                    if (!(ok = waited(empty + 8 * s, (it / kStages & 1) ^ 1))) break;
+                    tc::bar_expect(bar, 2 * kRowsBytes + bytes * (1 + a_in + b_in));
+                    tc::load_2d(a_at + s * kRowsBytes, &a_map, c * kChunkBytes, m0, bar);
+                    tc::load_2d(b_at + s * kRowsBytes, &b_map, c * kChunkBytes, n0, bar);
+                    if (a_in) tc::load_bytes(sa_at + s * kScaleA, sa + (long long)c * 1024, bytes, bar);
+                    tc::load_bytes(sb_at + s * kScaleB, sb + (long long)c * 1024, bytes, bar);
+                    if (b_in) tc::load_bytes(sb_at + s * kScaleB + 1024, sb + ((long long)a.groups * 512 + (long long)c * 1024), bytes, bar);
+                }
+            }
+            if (*(volatile int*)&failed)                  // copies still in flight
+                for (int i = it < kStages ? 0 : it - kStages; i < it; ++i) tc::bar_wait(full + 8 * (i % kStages), i / kStages & 1);
         }
+    } else if (warp == 1 && rank == 1) {                  // tells the first CTA that this one's rows are there
+        if (tc::elect()) {
+            int it = 0;
+            bool ok = true;
+            for (int u = first; u < units && ok; u += stride) {
+                const Unit w = unit_of(a, u);
+                for (int c = w.c0; c < w.c1; ++c, ++it) {
+                    if (!(ok = waited(full + 8 * (it % kStages), it / kStages & 1))) break;
+                    tc::bar_arrive_cluster(tc::in_cta(other + 8 * (it % kStages), 0));
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (tc::elect()) {
+            // e2m1 by e2m1, scales that are powers of two, 256 x 256; bits 4 and 29: which pair of a scale column's four bytes
+            constexpr uint32_t what = 1u << 7 | 1u << 10 | (uint32_t)(kTile >> 3) << 17 | 1u << 23 | (uint32_t)(kTile >> 4) << 24;
+            const uint32_t sa = tmem + kScalesAt, sb = sa + 8;
+            int it = 0, done = 0;
+            bool ok = true;
+            for (int u = first; u < units && ok; u += stride, ++done) {
+                const Unit w = unit_of(a, u);
+                const uint32_t d = tmem + (done & 1) * kSecond;
+                if (done > 0 && !(ok = waited(acc_free, (done - 1) & 1))) break;
+                tc::fence_after();
+                for (int c = w.c0; c < w.c1; ++c, ++it) {
+                    const int s = it % kStages;
+                    if (!(ok = waited(full + 8 * s, it / kStages & 1) && waited(other + 8 * s, it / kStages & 1))) break;
+                    tc::fence_after();
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        tc::copy_scales<2>(sa + g * 4, tc::operand_plain(sa_at + s * kScaleA + g * 512));
+                        tc::copy_scales<2>(sb + g * 8, tc::operand_plain(sb_at + s * kScaleB + g * 512));
+                        tc::copy_scales<2>(sb + g * 8 + 4, tc::operand_plain(sb_at + s * kScaleB + 1024 + g * 512));
+                    }
+                    const int steps = min(4, (a.blocks - c * kChunkBlocks + 1) / 2);      // of 64 columns
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (j < steps) {
+                            const uint32_t pick = (j & 1) * 2;
+                            tc::mma_mx4<2>(d, tc::operand(a_at + s * kRowsBytes + j * 32, 16, 1024), tc::operand(b_at + s * kRowsBytes + j * 32, 16, 1024), what | pick << 4 | pick << 29,
+                                           sa + j / 2 * 4, sb + j / 2 * 8, c > w.c0 || j > 0);
+                        }
+                    tc::mma_commit<2>(empty + 8 * s);
+                }
+                if (ok) tc::mma_commit<2>(acc_full + 8 * (done & 1));
+            }
+            if (*(volatile int*)&failed) {
+                tc::mma_commit<2>(drain);
+                tc::bar_wait(drain, 0);
+            }
+        }
+    } else if (warp >= 4) {
+        const int quad = warp % 4, half = (warp - 4) / 4;  // 32 rows, every other 16 columns
+        const uint32_t mine = out_at + (warp - 4) * 2048, lanes = (uint32_t)quad * 32 << 16;
+        int done = 0;
+        for (int u = first; u < units; u += stride, ++done) {
+            const Unit w = unit_of(a, u);
+            const uint32_t buf = done & 1;
+            if (!waited(acc_full + 8 * buf, done / 2 & 1)) break;
+            tc::fence_after();
+            const int lr = a.vec ? lane / 4 : lane / 16, lc = a.vec ? lane % 4 * 4 : lane % 16;
+            const long long r0 = (long long)w.tm * kTile + rank * kHalf + quad * 32, c0 = (long long)w.tn * kTile;
+            const int rows = (int)max(-64ll, min(32ll, a.m - r0)) - lr, cols = (int)min(256ll, a.n - c0) - lc;
+            const long long at = (r0 + lr) * a.stride + c0 + lc, pat = w.split * a.m * a.n + (r0 + lr) * a.n + c0 + lc;
+#pragma unroll 1
+            for (int i = 0; i < 8; ++i) {
+                // the columns that both accumulators have come first: the last 48 of the one, the first of the other
+                const int col = ((2 * i + half) * 16 + (buf ? 0 : kSecond)) % kTile;
+                const uint32_t from = tmem + buf * kSecond + col + lanes;
+                if (a.partial) move_out<float>(from, mine, nullptr, a.partial + pat + col, a.n, rows, cols - col, a.vec);
+                else move_out<O>(from, mine, a.bias ? (const O*)a.bias + c0 + lc + col : nullptr, (O*)a.y + at + col, a.stride, rows, cols - col, a.vec);
+                if (i == 1) {                             // four pieces of 16: 48 shared columns and 16 more
+                    tc::fence_before();
+                    __syncwarp();
+                    if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_free, 0));
+                }
+            }
+        }
+    }
+    __syncwarp();
+    tc::fence_before();
+    __syncthreads();
+    tc::cluster_sync();                                   // neither CTA's memory is read by the other any more
+    if (threadIdx.x == 0 && failed) atomicAdd(&g_timeouts, 1u);
+    if (warp == 2) tc::tmem_free<2>(tmem, 512);
+}
+
+// y = the splits' sums, in order, and the bias.
+template <typename O>
+__global__ void __launch_bounds__(256) mx_matmul_join_kernel(long long m, long long n, int splits, const float* __restrict__ partial, const O* __restrict__ bias, O* __restrict__ y, long long stride)
+{
+    const long long count = m * n;
+    for (long long e = (long long)blockIdx.x * 256 + threadIdx.x; e < count; e += (long long)gridDim.x * 256) {
+        float v = partial[e];
+        for (int s = 1; s < splits; ++s) v += partial[s * count + e];
+        const long long r = e / n, c = e - r * n;
+        y[r * stride + c] = mx_round<O>(bias ? v + mx_float(bias[c]) : v);
+    }
+}
+
+struct MatmulPlan { int tiles_m, tiles_n, splits, chunks, clusters; size_t partial; };
+
+MatmulPlan plan_of(const galv_ctx* ctx, int64_t m, int64_t n, int64_t k)
+{
+    MatmulPlan p;
+    const int most = ctx->num_sms / 2;
+    p.tiles_m = (int)((m + kTile - 1) / kTile);
+    p.tiles_n = (int)((n + kTile - 1) / kTile);
+    p.chunks = (int)((mx_blocks(k) + kChunkBlocks - 1) / kChunkBlocks);
+    const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+    p.splits = 1;
+    if (tiles < most && p.chunks >= 8) {
+        p.splits = (int)(most / tiles);
+        if (p.splits > p.chunks / 4) p.splits = p.chunks / 4;
+    }
+    const int64_t units = tiles * p.splits;
+    p.clusters = (int)(units < most ? units : most);
+    p.partial = p.splits > 1 ? (((size_t)p.splits * m * n * 4 + 255) & ~(size_t)255) : 0;
+    return p;
+}
+
+template <typename O>
+cudaError_t launch(const MatmulPlan& p, const CUtensorMap& am, const CUtensorMap& bm, const MatmulArgs& a, cudaStream_t st)
+{
+    cudaError_t e = cudaFuncSetAttribute(mx_matmul_kernel<O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+    mx_matmul_kernel<O><<<p.clusters * 2, kThreads, kSmem, st>>>(am, bm, a);
+    if (a.partial) mx_matmul_join_kernel<O><<<148 * 8, 256, 0, st>>>(a.m, a.n, a.splits, a.partial, (const O*)a.bias, (O*)a.y, a.stride);
+    return cudaGetLastError();
 }
 
 }  // namespace
 
 extern "C" size_t galv_mx_matmul_workspace_bytes(const galv_ctx* ctx, int64_t m, int64_t n, int64_t k)
 {
-    if (!ctx || !mx_size_ok(m, k) || !mx_size_ok(n, k)) return 0;
-    return 0;
+    if (!ctx || !mx_size_ok(m, k) || !mx_size_ok(n, k) || m == 0 || n == 0) return 0;
+    return plan_of(ctx, m, n, k).partial;
 }
 
 extern "C" int galv_mx_matmul(galv_ctx* ctx, int64_t m, int64_t n, int64_t k, const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes,
@@ -82,14 +328,23 @@ extern "C" int galv_mx_matmul(galv_ctx* ctx, int64_t m, int64_t n, int64_t k, co
     if (!a_codes || !a_scales || !b_codes || !b_scales || !mx_aligned(a_codes, 16) || !mx_aligned(a_scales, 16) || !mx_aligned(b_codes, 16) ||
         !mx_aligned(b_scales, 16) || !mx_matrix_ok(y, y_stride, n, dtype) || (bias && !mx_aligned(bias, mx_size_of(dtype))))
         return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_mx_matmul: NULL or misaligned pointer, or a row stride below n");
-    const size_t need = galv_mx_matmul_workspace_bytes(ctx, m, n, k);
-    if (need && (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < need))
+    const MatmulPlan p = plan_of(ctx, m, n, k);
+    if (p.partial && (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < p.partial))
         return galv_set_error(ctx, GALV_ERR_WORKSPACE, "galv_mx_matmul: workspace NULL, misaligned or too small");
     MxDevice dev(ctx);
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
-    cudaStream_t st = (cudaStream_t)stream;
-    const dim3 grid((unsigned)((n + kTile - 1) / kTile), (unsigned)((m + kTile - 1) / kTile));
-    MX_DISPATCH_TYPE(dtype, mx_matmul_simple_kernel<T><<<grid, kThreads, 0, st>>>(m, n, mx_blocks(k), a_codes, a_scales, b_codes, b_scales, (const T*)bias, (T*)y, y_stride));
-    const cudaError_t e = cudaGetLastError();
+    CUtensorMap am, bm;
+    const uint64_t pitch = mx_blocks(k) * 16;
+    cudaError_t e = galv_mx_map(&am, CU_TENSOR_MAP_DATA_TYPE_UINT8, a_codes, m, pitch, pitch, kHalf, kChunkBytes, true);
+    if (e == cudaSuccess) e = galv_mx_map(&bm, CU_TENSOR_MAP_DATA_TYPE_UINT8, b_codes, n, pitch, pitch, kHalf, kChunkBytes, true);
+    if (e != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, "galv_mx_matmul: tensor map");
+    MatmulArgs a;
+    a.m = m; a.n = n; a.stride = y_stride;
+    a.blocks = (int)mx_blocks(k); a.groups = (a.blocks + 3) / 4;
+    a.tiles_m = p.tiles_m; a.tiles_n = p.tiles_n; a.splits = p.splits; a.chunks = p.chunks;
+    a.a_scales = a_scales; a.b_scales = b_scales; a.bias = bias; a.y = y;
+    a.partial = p.partial ? reinterpret_cast<float*>(workspace) : nullptr;
+    a.vec = p.partial ? n % 4 == 0 : n % 4 == 0 && y_stride % 4 == 0 && mx_aligned(y, 4 * mx_size_of(dtype));
+    MX_DISPATCH_TYPE(dtype, e = launch<T>(p, am, bm, a, (cudaStream_t)stream));
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
