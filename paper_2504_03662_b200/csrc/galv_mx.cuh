@@ -69,14 +69,55 @@ __device__ __forceinline__ void mx_load8(const T* __restrict__ row, long long c0
     }
 }
 
+// ... of a matrix that the same kernel may write (in place): not by the read-only path.
+template <typename T, bool VEC>
+__device__ __forceinline__ void mx_load8_rw(const T* row, long long c0, long long cols, float (&v)[8])
+{
+    if (VEC && c0 + 8 <= cols) {
+        MxPiece<T> p;
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) p.q[i] = reinterpret_cast<const uint4*>(row + c0)[i];
+        const T* e = reinterpret_cast<const T*>(&p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = mx_float(e[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c0 + i < cols ? mx_float(row[c0 + i]) : 0.f;
+    }
+}
+
+template <typename T> __device__ __forceinline__ MxPiece<T> mx_piece(const float (&v)[8])
+{
+    MxPiece<T> p;
+    T* e = reinterpret_cast<T*>(&p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = mx_round<T>(v[i]);
+    return p;
+}
+template <> __device__ __forceinline__ MxPiece<__nv_bfloat16> mx_piece<__nv_bfloat16>(const float (&v)[8])      // two numbers an instruction
+{
+    MxPiece<__nv_bfloat16> p;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p.q[0].x) : "f"(v[1]), "f"(v[0]));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p.q[0].y) : "f"(v[3]), "f"(v[2]));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p.q[0].z) : "f"(v[5]), "f"(v[4]));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p.q[0].w) : "f"(v[7]), "f"(v[6]));
+    return p;
+}
+template <> __device__ __forceinline__ MxPiece<__half> mx_piece<__half>(const float (&v)[8])
+{
+    MxPiece<__half> p;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(p.q[0].x) : "f"(v[1]), "f"(v[0]));
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(p.q[0].y) : "f"(v[3]), "f"(v[2]));
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(p.q[0].z) : "f"(v[5]), "f"(v[4]));
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(p.q[0].w) : "f"(v[7]), "f"(v[6]));
+    return p;
+}
+
 template <typename T, bool VEC>
 __device__ __forceinline__ void mx_store8(T* __restrict__ row, long long c0, long long cols, const float (&v)[8])
 {
     if (VEC && c0 + 8 <= cols) {
-        MxPiece<T> p;
-        T* e = reinterpret_cast<T*>(&p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = mx_round<T>(v[i]);
+        const MxPiece<T> p = mx_piece<T>(v);
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(row + c0)[i] = p.q[i];
     } else {

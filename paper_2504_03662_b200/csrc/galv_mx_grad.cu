@@ -35,7 +35,7 @@ __global__ void __launch_bounds__(kThreads) mx_act_kernel(long long rows, long l
     for (long long item = first; item < rows * pieces; item += step) {
         float x[8], g[8];
         mx_restore8<GALV_MX8>(codes, scales, row, c, nb, per_row, x);
-        mx_load8<T, VEC>(dy + row * dy_stride, c * 8, cols, g);
+        mx_load8_rw<T, VEC>(dy + row * dy_stride, c * 8, cols, g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) g[i] *= act_slope<ACT>(x[i]);
         mx_store8<T, VEC>(dx + row * dx_stride, c * 8, cols, g);
@@ -43,6 +43,322 @@ __global__ void __launch_bounds__(kThreads) mx_act_kernel(long long rows, long l
         c += dc;
         if (c >= pieces) { c -= pieces; ++row; }
     }
+}
+
+// ---- norms
+//
+// One pass: a row's codes and gradient are read once, its statistics and the two means of the gradient come from registers, and the column sums stay with
+// the thread that has the column, over all rows that its CTA takes (where a thread has two pieces of 8 columns, dweight's in shared memory: with both sums in
+// registers only half as many threads fit, and the pass took twice as long).  The next rows are on their way into shared memory
+// meanwhile, each thread's pieces its own, so that only the rows' sums need a barrier.  Bound by memory (2 + 2 + 33/32 bytes an element of 16
+// bits) with some twenty instructions an element close behind.
+
+constexpr int kBlockThreads = 1024;
+constexpr int kWarpColumns = 1024;                        // up to here a warp has a row to itself, and no barrier
+
+struct NormArgs {
+    long long rows, cols, nb, pitch, dy_stride, dx_stride;
+    float eps;
+    const uint8_t* codes;
+    const uint8_t* scales;
+    const void* dy;
+    const void* weight;
+    void* dx;
+    float* part;                                          // [parts][2][cols]: dweight, dbias
+};
+
+template <typename T> struct Raw8 { uint4 q[sizeof(T) / 2]; };
+template <typename T> __device__ __forceinline__ float raw_at(const Raw8<T>& r, int i);
+template <> __device__ __forceinline__ float raw_at<float>(const Raw8<float>& r, int i) { return __uint_as_float((&r.q[i / 4].x)[i % 4]); }
+template <> __device__ __forceinline__ float raw_at<__nv_bfloat16>(const Raw8<__nv_bfloat16>& r, int i)
+{
+    const uint32_t w = (&r.q[0].x)[i / 2];
+    return __uint_as_float(i % 2 ? w & 0xffff0000u : w << 16);
+}
+template <> __device__ __forceinline__ float raw_at<__half>(const Raw8<__half>& r, int i)
+{
+    const uint32_t w = (&r.q[0].x)[i / 2];
+    const __half2 h = *reinterpret_cast<const __half2*>(&w);
+    return i % 2 ? __high2float(h) : __low2float(h);
+}
+
+template <int N> __device__ __forceinline__ void copy_async(uint32_t to, const void* from, int bytes)      // zeros behind `bytes`
+{
+    if (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to), "l"(from), "r"(bytes) : "memory");
+    else if (N == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" :: "r"(to), "l"(from), "r"(bytes) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" :: "r"(to), "l"(from), "r"(bytes) : "memory");
+}
+
+// Sums of four values over a warp: each exchange halves the values a lane still has, so that lanes 8 g .. 8 g + 7 end with value g's.
+__device__ __forceinline__ float warp_sums(const float4& v)
+{
+    const int lane = threadIdx.x % 32;
+    float a = lane & 16 ? v.z : v.x, b = lane & 16 ? v.w : v.y;
+    a += __shfl_xor_sync(0xffffffffu, lane & 16 ? v.x : v.z, 16);
+    b += __shfl_xor_sync(0xffffffffu, lane & 16 ? v.y : v.w, 16);
+    float c = lane & 8 ? b : a;
+    c += __shfl_xor_sync(0xffffffffu, lane & 8 ? a : b, 8);
+#pragma unroll
+    for (int o = 4; o; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+    return c;
+}
+// Sums of up to four values over the threads that share a row: a warp, or the CTA (one barrier; `red` is another one in turn).
+template <bool WARP, int N>
+__device__ __forceinline__ float4 row_sums(const float4& v, float4* red)
+{
+    float c = warp_sums(v);
+    if (!WARP) {
+        if (threadIdx.x % 8 == 0) reinterpret_cast<float*>(red)[threadIdx.x / 32 * 4 + threadIdx.x % 32 / 8] = c;
+        __syncthreads();
+        c = warp_sums(threadIdx.x % 32 < blockDim.x / 32 ? red[threadIdx.x % 32] : make_float4(0.f, 0.f, 0.f, 0.f));
+    }
+    float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+    r.x = __shfl_sync(0xffffffffu, c, 0);
+    if (N > 1) r.y = __shfl_sync(0xffffffffu, c, 8);
+    if (N > 2) r.z = __shfl_sync(0xffffffffu, c, 16);
+    return r;
+}
+// ... of one.
+template <bool WARP>
+__device__ __forceinline__ float row_sum(float a, float* red)
+{
+#pragma unroll
+    for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+    if (WARP) return a;
+    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = a;
+    __syncthreads();
+    a = threadIdx.x % 32 < blockDim.x / 32 ? red[threadIdx.x % 32] : 0.f;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+    return a;
+}
+
+template <typename T> struct NormStage {
+    static constexpr int count = 2;
+    static constexpr int piece = 8 * (int)sizeof(T) + 8 + 4;               // bytes: dy, codes, the word that has the scale byte
+};
+
+template <typename T, bool LAYER, bool VEC, bool WARP, int PP>
+__global__ void __launch_bounds__(WARP ? 256 : kBlockThreads, WARP && PP < 4 ? 2 : 1) mx_norm_kernel(const NormArgs a)
+{
+    constexpr int NS = NormStage<T>::count, kDy = 8 * (int)sizeof(T);
+    extern __shared__ __align__(16) unsigned char raw[];
+    constexpr bool kShared = !WARP && PP > 1;             // dweight's sums lie in shared memory
+    __shared__ float4 red[2][32];
+    __shared__ float red1[2][32];
+    const int team = WARP ? threadIdx.x / 32 : 0, teams = WARP ? blockDim.x / 32 : 1, lane = WARP ? threadIdx.x % 32 : threadIdx.x, width = WARP ? 32 : blockDim.x;
+    const int pieces = (int)((a.cols + 7) / 8), slots = width * PP;
+    const float inv_n = 1.f / (float)a.cols;
+    // weights [slots][8], then each team's stages of dy [slots][8], codes [slots][8 bytes], scale words [slots], then sums [2][slots][4]
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(raw), mine = base + slots * kDy + team * NS * slots * NormStage<T>::piece;
+    const uint32_t sums = mine + NS * slots * NormStage<T>::piece;
+    for (int c = threadIdx.x; c < slots * 8; c += blockDim.x) reinterpret_cast<T*>(raw)[c] = a.weight && c < a.cols ? ((const T*)a.weight)[c] : mx_round<T>(1.f);
+    __syncthreads();
+
+    float dw[kShared ? 8 : PP * 8] = {}, db[LAYER ? PP * 8 : 1] = {};
+    auto sums_load = [&](int p) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(dw[4 * i]), "=f"(dw[4 * i + 1]), "=f"(dw[4 * i + 2]), "=f"(dw[4 * i + 3]) : "r"(sums + (i * slots + lane + p * width) * 16));
+    };
+    auto sums_store = [&](int p) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" :: "r"(sums + (i * slots + lane + p * width) * 16), "f"(dw[4 * i]), "f"(dw[4 * i + 1]), "f"(dw[4 * i + 2]), "f"(dw[4 * i + 3]) : "memory");
+    };
+    if (kShared) {
+#pragma unroll
+        for (int p = 0; p < PP; ++p) sums_store(p);
+    }
+    const long long first = (long long)blockIdx.x * teams + team, step = (long long)gridDim.x * teams;
+    const uint8_t* codes = a.codes + first * a.nb * 32 + lane * 8;
+    const uint8_t* scales = a.scales + first * a.pitch;
+    const T* dy = (const T*)a.dy + first * a.dy_stride + lane * 8;
+    T* dx = (T*)a.dx + first * a.dx_stride;
+    const int cols = (int)a.cols;
+    long long ahead = first;
+    auto fetch = [&](int stage) {
+        if (ahead < a.rows) {
+            const uint32_t to = mine + stage * slots * NormStage<T>::piece;
+#pragma unroll
+            for (int p = 0; p < PP; ++p) {
+                const int at = lane + p * width;
+                if (at < pieces) {
+                    if (VEC) {
+                        const int left = (cols - at * 8) * (int)sizeof(T);
+                        copy_async<16>(to + at * kDy, dy + p * width * 8, min(16, left));
+                        if (kDy == 32) copy_async<16>(to + at * kDy + 16, left > 16 ? dy + p * width * 8 + 4 : dy, min(16, max(0, left - 16)));
+                    }
+                    copy_async<8>(to + slots * kDy + at * 8, codes + p * width * 8, 8);
+                    copy_async<4>(to + slots * (kDy + 8) + at * 4, scales + (at >> 4) * 4, 4);
+                }
+            }
+            ahead += step;
+            codes += step * a.nb * 32;
+            scales += step * a.pitch;
+            dy += step * a.dy_stride;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int n = 0; n < NS - 1; ++n) fetch(n);
+    int turn = 0, stage = 0;
+    for (long long row = first; row < a.rows; row += step, turn ^= 1, dx += step * a.dx_stride) {
+        fetch((stage + NS - 1) % NS);
+        asm volatile("cp.async.wait_group %0;" :: "n"(NS - 1) : "memory");
+        const uint32_t from = mine + stage * slots * NormStage<T>::piece;
+        stage = (stage + 1) % NS;
+        float x[PP * 8], s[PP];
+        Raw8<T> d[PP];
+        auto weights = [&](int p) {
+            Raw8<T> w;
+#pragma unroll
+            for (int i = 0; i < kDy / 16; ++i)
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.q[i].x), "=r"(w.q[i].y), "=r"(w.q[i].z), "=r"(w.q[i].w) : "r"(base + (lane + p * width) * kDy + i * 16));
+            return w;
+        };
+        // x: the sum (LAYER) or the sum of squares; y: dy * weight; z: dy * weight * x
+        float4 m = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int p = 0; p < PP; ++p) {
+            const int at = lane + p * width;
+            uint2 code = make_uint2(0, 0);
+            uint32_t word = 0;
+#pragma unroll
+            for (int i = 0; i < kDy / 16; ++i) d[p].q[i] = make_uint4(0, 0, 0, 0);
+            if (at < pieces) {
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(code.x), "=r"(code.y) : "r"(from + slots * kDy + at * 8));
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(word) : "r"(from + slots * (kDy + 8) + at * 4));
+                if (VEC) {
+#pragma unroll
+                    for (int i = 0; i < kDy / 16; ++i)
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(d[p].q[i].x), "=r"(d[p].q[i].y), "=r"(d[p].q[i].z), "=r"(d[p].q[i].w) : "r"(from + at * kDy + i * 16));
+                } else {
+                    const T* from_row = (const T*)a.dy + row * a.dy_stride;
+                    T* e = reinterpret_cast<T*>(&d[p]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (at * 8 + i < cols) e[i] = from_row[at * 8 + i];
+                }
+            }
+            mx_from8(code.x, x + 8 * p);
+            mx_from8(code.y, x + 8 * p + 4);
+            s[p] = mx_scale((int)(word >> (at >> 2 & 3) * 8 & 255));
+            const Raw8<T> w = weights(p);
+            float sx = 0.f, sgx = 0.f;                    // before the block's power of two
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float v = x[8 * p + i], gw = raw_at<T>(d[p], i) * raw_at<T>(w, i);
+                sx = LAYER ? sx + v : fmaf(v, v, sx);
+                if (LAYER) m.y += gw;
+                sgx = fmaf(gw, v, sgx);
+            }
+            m.x = LAYER ? fmaf(sx, s[p], m.x) : fmaf(sx * s[p], s[p], m.x);
+            m.z = fmaf(sgx, s[p], m.z);
+        }
+        m = row_sums<WARP, 3>(m, red[turn]);
+        float mean = 0.f, mg = 0.f, sq = m.x, sgx = m.z;
+        if (LAYER) {
+            mean = m.x * inv_n;
+            mg = m.y * inv_n;
+            sgx -= mean * m.y;
+            sq = 0.f;
+        }
+#pragma unroll
+        for (int p = 0; p < PP; ++p) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[8 * p + i] = LAYER ? fmaf(x[8 * p + i], s[p], -mean) : x[8 * p + i] * s[p];
+            if (LAYER) {
+                const int left = cols - (lane + p * width) * 8;
+                if (left < 8) {                           // behind the row's end
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (i >= left) x[8 * p + i] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sq = fmaf(x[8 * p + i], x[8 * p + i], sq);
+            }
+        }
+        if (LAYER) sq = row_sum<WARP>(sq, red1[turn]);
+        const float r = 1.f / sqrtf(sq * inv_n + a.eps), c = -sgx * inv_n * r * r * r, mr = -mg * r;
+#pragma unroll
+        for (int p = 0; p < PP; ++p) {
+            const Raw8<T> w = weights(p);
+            float v[8];
+            if (kShared) sums_load(p);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float y = raw_at<T>(d[p], i), yr = y * r, xv = x[8 * p + i];
+                v[i] = fmaf(yr, raw_at<T>(w, i), LAYER ? fmaf(c, xv, mr) : c * xv);
+                float& sum = dw[kShared ? i : 8 * p + i];
+                sum = fmaf(yr, xv, sum);
+                if (LAYER) db[8 * p + i] += y;
+            }
+            if (kShared) sums_store(p);
+            mx_store8<T, VEC>(dx, (lane + p * width) * 8, cols, v);
+        }
+    }
+    // this CTA's column sums
+    const long long pitch = pieces * 8;
+    float* part = a.part + (long long)blockIdx.x * 2 * pitch;
+    if (WARP) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();
+        float* joined = reinterpret_cast<float*>(raw);    // [2][kWarpColumns] over what is not read any more
+        for (int t = 0; t < teams; ++t) {                 // the warps' in order
+            if (team == t) {
+#pragma unroll
+                for (int p = 0; p < PP; ++p)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int c = (lane + p * 32) * 8 + i;
+                        if (c < pitch) {
+                            joined[c] = t ? joined[c] + dw[8 * p + i] : dw[8 * p + i];
+                            if (LAYER) joined[kWarpColumns + c] = t ? joined[kWarpColumns + c] + db[8 * p + i] : db[8 * p + i];
+                        }
+                    }
+            }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < pitch; c += blockDim.x) {
+            part[c] = joined[c];
+            if (LAYER) part[pitch + c] = joined[kWarpColumns + c];
+        }
+    } else {
+#pragma unroll
+        for (int p = 0; p < PP; ++p) {
+            const int at = lane + p * width;
+            if (at >= pieces) continue;
+            if (kShared) sums_load(p);
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) {
+                const int k = (kShared ? 0 : 8 * p) + i;
+                *reinterpret_cast<float4*>(part + at * 8ll + i) = make_float4(dw[k], dw[k + 1], dw[k + 2], dw[k + 3]);
+                if (LAYER) *reinterpret_cast<float4*>(part + pitch + at * 8ll + i) = make_float4(db[8 * p + i], db[8 * p + i + 1], db[8 * p + i + 2], db[8 * p + i + 3]);
+            }
+        }
+    }
+}
+
+// dweight and dbias: the CTAs' sums in a fixed order, 32 columns a CTA, 32 threads a column that take every 32nd.
+__global__ void __launch_bounds__(1024) mx_norm_join_kernel(long long cols, long long pitch, int parts, const float* __restrict__ part, float* dweight, float* dbias)
+{
+    __shared__ float sum[32][33];
+    const int x = threadIdx.x % 32, k = threadIdx.x / 32, which = blockIdx.y;
+    const long long c = (long long)blockIdx.x * 32 + x;
+    float v = 0.f;
+    if (c < cols) {
+#pragma unroll 4
+        for (int p = k; p < parts; p += 32) v += part[((long long)p * 2 + which) * pitch + c];
+    }
+    sum[k][x] = v;
+    __syncthreads();
+    v = sum[x][k];                                        // now a warp has a column
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    float* out = which ? dbias : dweight;
+    const long long mine = (long long)blockIdx.x * 32 + k;
+    if (x == 0 && mine < cols && out) out[mine] = v;
 }
 
 __device__ __forceinline__ float block_sum(float v, float* red)
@@ -53,115 +369,152 @@ __device__ __forceinline__ float block_sum(float v, float* red)
     if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
     __syncthreads();
     float s = 0.f;
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) s += red[w];
+    for (int w = 0; w < (int)blockDim.x / 32; ++w) s += red[w];
     return s;
 }
 
-// One CTA a row: statistics, the two means of the gradient, dx; mean and 1/sqrt(var + eps) stay for the column sums.
-template <typename T, bool LAYER>
-__global__ void __launch_bounds__(kThreads) mx_norm_rows_kernel(long long rows, long long cols, long long nb, long long pitch, float eps,
-                                                                const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const T* dy,
-                                                                long long dy_stride, const T* __restrict__ weight, T* dx, long long dx_stride, float2* stats)
+// Rows too long for registers: a CTA goes over its row four times (the first reads it, the others find it in the caches).  Mean and 1/sqrt(var + eps) stay for
+// the column sums, which come first where dx may be dy: this kernel runs without dx before them and with it after them.
+template <typename T, bool LAYER, bool VEC>
+__global__ void __launch_bounds__(512) mx_norm_wide_kernel(const NormArgs a, float2* stats, bool last)
 {
-    __shared__ float red[kThreads / 32];
-    const long long pieces = (cols + 7) / 8;
-    const float inv_n = 1.f / (float)cols;
-    for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
-        float mean = 0.f;
+    __shared__ float red[16];
+    const long long pieces = (a.cols + 7) / 8;
+    const float inv_n = 1.f / (float)a.cols;
+    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T* dy = (const T*)a.dy + row * a.dy_stride;
+        T* dx = (T*)a.dx + row * a.dx_stride;
         float x[8], g[8], w[8];
-        if (LAYER) {
-            float s = 0.f;
-            for (long long c = threadIdx.x; c < pieces; c += kThreads) {
-                mx_restore8<GALV_MX8>(codes, scales, row, c, nb, pitch, x);
+        if (!last) {
+            float mean = 0.f, s = 0.f;
+            if (LAYER) {
+                for (long long c = threadIdx.x; c < pieces; c += 512) {
+                    mx_restore8<GALV_MX8>(a.codes, a.scales, row, c, a.nb, a.pitch, x);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s += x[i];
+                    for (int i = 0; i < 8; ++i) s += x[i];
+                }
+                mean = block_sum(s, red) * inv_n;
             }
-            mean = block_sum(s, red) * inv_n;
-        }
-        float s = 0.f;
-        for (long long c = threadIdx.x; c < pieces; c += kThreads) {
-            mx_restore8<GALV_MX8>(codes, scales, row, c, nb, pitch, x);
+            s = 0.f;
+            for (long long c = threadIdx.x; c < pieces; c += 512) {
+                mx_restore8<GALV_MX8>(a.codes, a.scales, row, c, a.nb, a.pitch, x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c * 8 + i < cols) s += (x[i] - mean) * (x[i] - mean);
+                for (int i = 0; i < 8; ++i)
+                    if (c * 8 + i < a.cols) s = fmaf(x[i] - mean, x[i] - mean, s);
+            }
+            const float rstd = 1.f / sqrtf(block_sum(s, red) * inv_n + a.eps);
+            if (threadIdx.x == 0) stats[row] = make_float2(mean, rstd);
+            continue;
         }
-        const float rstd = 1.f / sqrtf(block_sum(s, red) * inv_n + eps);
+        const float mean = stats[row].x, rstd = stats[row].y;
         float sg = 0.f, sgx = 0.f;
-        for (long long c = threadIdx.x; c < pieces; c += kThreads) {
-            mx_restore8<GALV_MX8>(codes, scales, row, c, nb, pitch, x);
-            mx_load8<T, false>(dy + row * dy_stride, c * 8, cols, g);
-            if (weight) mx_load8<T, false>(weight, c * 8, cols, w);
+        for (long long c = threadIdx.x; c < pieces; c += 512) {
+            mx_restore8<GALV_MX8>(a.codes, a.scales, row, c, a.nb, a.pitch, x);
+            mx_load8_rw<T, VEC>(dy, c * 8, a.cols, g);
+            if (a.weight) mx_load8<T, false>((const T*)a.weight, c * 8, a.cols, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float gw = weight ? g[i] * w[i] : g[i];
+                const float gw = a.weight ? g[i] * w[i] : g[i];
                 sg += gw;
-                sgx += gw * ((x[i] - mean) * rstd);
+                sgx = fmaf(gw, x[i] - mean, sgx);
             }
         }
-        const float mg = LAYER ? block_sum(sg, red) * inv_n : 0.f, mgx = block_sum(sgx, red) * inv_n;
-        for (long long c = threadIdx.x; c < pieces; c += kThreads) {
-            mx_restore8<GALV_MX8>(codes, scales, row, c, nb, pitch, x);
-            mx_load8<T, false>(dy + row * dy_stride, c * 8, cols, g);
-            if (weight) mx_load8<T, false>(weight, c * 8, cols, w);
+        const float mg = LAYER ? block_sum(sg, red) * inv_n : 0.f, m = block_sum(sgx, red) * inv_n * rstd * rstd;
+        for (long long c = threadIdx.x; c < pieces; c += 512) {
+            mx_restore8<GALV_MX8>(a.codes, a.scales, row, c, a.nb, a.pitch, x);
+            mx_load8_rw<T, VEC>(dy, c * 8, a.cols, g);
+            if (a.weight) mx_load8<T, false>((const T*)a.weight, c * 8, a.cols, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) g[i] = rstd * ((weight ? g[i] * w[i] : g[i]) - mg - (x[i] - mean) * rstd * mgx);
-            mx_store8<T, false>(dx + row * dx_stride, c * 8, cols, g);
+            for (int i = 0; i < 8; ++i) g[i] = rstd * ((a.weight ? g[i] * w[i] : g[i]) - mg - (x[i] - mean) * m);
+            mx_store8<T, VEC>(dx, c * 8, a.cols, g);
         }
-        if (threadIdx.x == 0) stats[row] = make_float2(mean, rstd);
     }
 }
 
-// One thread a column, rows in order.  Launched before the rows' kernel, which may write dx over dy.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) mx_norm_cols_kernel(long long rows, long long cols, long long nb, long long pitch, const uint8_t* __restrict__ codes,
-                                                                const uint8_t* __restrict__ scales, const T* __restrict__ dy, long long dy_stride,
-                                                                const float2* __restrict__ stats, float* dweight, float* dbias)
+// ... and their column sums: a thread has a piece of 8 columns and every gridDim.y-th row.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(128) mx_norm_columns_kernel(const NormArgs a, const float2* __restrict__ stats)
 {
-    const long long c = (long long)blockIdx.x * kThreads + threadIdx.x;
-    if (c >= cols) return;
-    float dw = 0.f, db = 0.f, x[8];
-    for (long long row = 0; row < rows; ++row) {
+    const long long c = (long long)blockIdx.x * 128 + threadIdx.x;
+    if (c * 8 >= a.cols) return;
+    float dw[8] = {}, db[8] = {}, x[8], g[8];
+    for (long long row = blockIdx.y; row < a.rows; row += gridDim.y) {
         const float2 st = stats[row];
-        const float g = mx_float(dy[row * dy_stride + c]);
-        mx_restore8<GALV_MX8>(codes, scales, row, c >> 3, nb, pitch, x);
-        float xv = 0.f;
+        mx_restore8<GALV_MX8>(a.codes, a.scales, row, c, a.nb, a.pitch, x);
+        mx_load8_rw<T, VEC>((const T*)a.dy + row * a.dy_stride, c * 8, a.cols, g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i == (c & 7)) xv = x[i];
-        dw += g * ((xv - st.x) * st.y);
-        db += g;
+        for (int i = 0; i < 8; ++i) {
+            dw[i] = fmaf(g[i], (x[i] - st.x) * st.y, dw[i]);
+            db[i] += g[i];
+        }
     }
-    if (dweight) dweight[c] = dw;
-    if (dbias) dbias[c] = db;
+    const long long pitch = (a.cols + 7) / 8 * 8;
+    float* part = a.part + (long long)blockIdx.y * 2 * pitch + c * 8;
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+        *reinterpret_cast<float4*>(part + i) = make_float4(dw[i], dw[i + 1], dw[i + 2], dw[i + 3]);
+        *reinterpret_cast<float4*>(part + pitch + i) = make_float4(db[i], db[i + 1], db[i + 2], db[i + 3]);
+    }
 }
 
-template <bool LAYER>
-__global__ void __launch_bounds__(kThreads) mx_norm_stats_kernel(long long rows, long long cols, long long nb, long long pitch, float eps,
-                                                                 const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, float2* stats)
+struct NormPlan { bool warp, wide; int pp, threads, grid, parts, smem; size_t stats, total; };
+
+NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtype)
 {
-    __shared__ float red[kThreads / 32];
-    const long long pieces = (cols + 7) / 8;
-    const float inv_n = 1.f / (float)cols;
-    for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
-        float mean = 0.f, x[8], s = 0.f;
-        if (LAYER) {
-            for (long long c = threadIdx.x; c < pieces; c += kThreads) {
-                mx_restore8<GALV_MX8>(codes, scales, row, c, nb, pitch, x);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s += x[i];
-            }
-            mean = block_sum(s, red) * inv_n;
-        }
-        s = 0.f;
-        for (long long c = threadIdx.x; c < pieces; c += kThreads) {
-            mx_restore8<GALV_MX8>(codes, scales, row, c, nb, pitch, x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c * 8 + i < cols) s += (x[i] - mean) * (x[i] - mean);
-        }
-        const float rstd = 1.f / sqrtf(block_sum(s, red) * inv_n + eps);
-        if (threadIdx.x == 0) stats[row] = make_float2(mean, rstd);
+    NormPlan p;
+    const int64_t pieces = (cols + 7) / 8;
+    const bool four = dtype == GALV_F32;
+    const int stages = four ? NormStage<float>::count : NormStage<__half>::count, piece = four ? NormStage<float>::piece : NormStage<__half>::piece;
+    p.stats = 0;
+    p.wide = false;
+    p.warp = cols <= kWarpColumns;
+    if (p.warp) {
+        p.pp = pieces <= 32 ? 1 : pieces <= 64 ? 2 : 4;
+        p.threads = 256;
+        const int64_t most = ctx->num_sms * (p.pp == 4 ? 1 : 2), need = (rows + 7) / 8;
+        p.parts = p.grid = (int)(need < most ? need : most);
+        p.smem = 32 * p.pp * (piece - 12 + 8 * stages * piece);
+        if (p.smem < 2 * kWarpColumns * 4) p.smem = 2 * kWarpColumns * 4;
+    } else {
+        p.pp = pieces <= kBlockThreads ? 1 : 2;
+        p.threads = (int)(((pieces + p.pp - 1) / p.pp + 31) / 32 * 32);
+        const int64_t smem = (int64_t)p.threads * p.pp * (piece - 12 + stages * piece + (p.pp > 1 ? 32 : 0));
+        p.wide = p.threads > kBlockThreads || smem > ctx->smem_optin - 2048;
+        const int64_t most = ctx->num_sms * (p.threads <= 256 ? 4 : p.threads <= 512 ? 2 : 1);
+        p.parts = p.grid = (int)(rows < most ? rows : most);
+        p.smem = (int)smem;
+    }
+    if (p.wide) {
+        p.threads = 512;
+        p.grid = (int)(rows < ctx->num_sms * 4 ? rows : ctx->num_sms * 4);
+        p.parts = (int)(rows < 8 ? rows : 8);
+        p.stats = ((size_t)rows * sizeof(float2) + 255) & ~(size_t)255;
+    }
+    p.total = p.stats + (((size_t)p.parts * 2 * pieces * 8 * 4 + 255) & ~(size_t)255);
+    return p;
+}
+
+template <typename T, bool LAYER, bool VEC, bool WARP, int PP>
+void norm_start(const NormPlan& p, const NormArgs& a, cudaStream_t st)
+{
+    if (p.smem > 48 * 1024) cudaFuncSetAttribute(mx_norm_kernel<T, LAYER, VEC, WARP, PP>, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
+    mx_norm_kernel<T, LAYER, VEC, WARP, PP><<<p.grid, p.threads, p.smem, st>>>(a);
+}
+
+template <typename T, bool LAYER, bool VEC>
+void norm_launch(const NormPlan& p, const NormArgs& a, float2* stats, bool sums, cudaStream_t st)
+{
+    if (p.wide) {
+        mx_norm_wide_kernel<T, LAYER, VEC><<<p.grid, 512, 0, st>>>(a, stats, false);
+        if (sums) mx_norm_columns_kernel<T, VEC><<<dim3((unsigned)((a.cols + 1023) / 1024), p.parts), 128, 0, st>>>(a, stats);
+        mx_norm_wide_kernel<T, LAYER, VEC><<<p.grid, 512, 0, st>>>(a, stats, true);
+    } else if (p.warp) {
+        if (p.pp == 1) norm_start<T, LAYER, VEC, true, 1>(p, a, st);
+        else if (p.pp == 2) norm_start<T, LAYER, VEC, true, 2>(p, a, st);
+        else norm_start<T, LAYER, VEC, true, 4>(p, a, st);
+    } else {
+        if (p.pp == 1) norm_start<T, LAYER, VEC, false, 1>(p, a, st);
+        else norm_start<T, LAYER, VEC, false, 2>(p, a, st);
     }
 }
 
@@ -198,8 +551,9 @@ extern "C" int galv_mx_act_backward(galv_ctx* ctx, int64_t rows, int64_t cols, i
 
 extern "C" size_t galv_mx_norm_workspace_bytes(const galv_ctx* ctx, int64_t rows, int64_t cols)
 {
-    if (!ctx || !mx_size_ok(rows, cols)) return 0;
-    return ((size_t)rows * sizeof(float2) + 255) & ~(size_t)255;
+    if (!ctx || !mx_size_ok(rows, cols) || rows == 0) return 0;
+    const size_t a = norm_plan(ctx, rows, cols, GALV_F32).total, b = norm_plan(ctx, rows, cols, GALV_F16).total;
+    return a > b ? a : b;
 }
 
 extern "C" int galv_mx_norm_backward(galv_ctx* ctx, int64_t rows, int64_t cols, int32_t kind, float eps, const uint8_t* codes, const uint8_t* scales,
@@ -228,15 +582,17 @@ extern "C" int galv_mx_norm_backward(galv_ctx* ctx, int64_t rows, int64_t cols, 
         return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_mx_norm_backward: dx may be dy with the same stride only");
     if (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < galv_mx_norm_workspace_bytes(ctx, rows, cols))
         return galv_set_error(ctx, GALV_ERR_WORKSPACE, "galv_mx_norm_backward: workspace NULL, misaligned or too small");
-    const long long nb = mx_blocks(cols), pitch = mx_pitch8(cols), most = (long long)ctx->num_sms * 8;
-    const int grid = (int)(rows < most ? rows : most), cgrid = (int)((cols + kThreads - 1) / kThreads);
+    const NormPlan p = norm_plan(ctx, rows, cols, dtype);
+    NormArgs a;
+    a.rows = rows; a.cols = cols; a.nb = mx_blocks(cols); a.pitch = mx_pitch8(cols); a.dy_stride = dy_stride; a.dx_stride = dx_stride;
+    a.eps = eps; a.codes = codes; a.scales = scales; a.dy = dy; a.weight = weight; a.dx = dx;
+    a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + p.stats);
     float2* stats = reinterpret_cast<float2*>(workspace);
-    if (kind == GALV_NORM_LAYER) mx_norm_stats_kernel<true><<<grid, kThreads, 0, st>>>(rows, cols, nb, pitch, eps, codes, scales, stats);
-    else mx_norm_stats_kernel<false><<<grid, kThreads, 0, st>>>(rows, cols, nb, pitch, eps, codes, scales, stats);
+    const bool vec = mx_rows16(dy, dy_stride, dtype) && mx_rows16(dx, dx_stride, dtype), layer = kind == GALV_NORM_LAYER, sums = dweight || dbias;
     MX_DISPATCH_TYPE(dtype,
-        if (dweight || dbias) mx_norm_cols_kernel<T><<<cgrid, kThreads, 0, st>>>(rows, cols, nb, pitch, codes, scales, (const T*)dy, dy_stride, stats, dweight, dbias);
-        if (kind == GALV_NORM_LAYER) mx_norm_rows_kernel<T, true><<<grid, kThreads, 0, st>>>(rows, cols, nb, pitch, eps, codes, scales, (const T*)dy, dy_stride, (const T*)weight, (T*)dx, dx_stride, stats);
-        else mx_norm_rows_kernel<T, false><<<grid, kThreads, 0, st>>>(rows, cols, nb, pitch, eps, codes, scales, (const T*)dy, dy_stride, (const T*)weight, (T*)dx, dx_stride, stats));
+        if (layer) { if (vec) norm_launch<T, true, true>(p, a, stats, sums, st); else norm_launch<T, true, false>(p, a, stats, sums, st); }
+        else { if (vec) norm_launch<T, false, true>(p, a, stats, sums, st); else norm_launch<T, false, false>(p, a, stats, sums, st); });
+    if (sums) mx_norm_join_kernel<<<dim3((unsigned)((cols + 31) / 32), dbias ? 2 : 1), 1024, 0, st>>>(cols, (cols + 7) / 8 * 8, p.parts, a.part, dweight, dbias);
     e = cudaGetLastError();
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
