@@ -63,6 +63,7 @@ struct NormArgs {
     const uint8_t* scales;
     const void* dy;
     const void* weight;
+    bool weight16;                                        // on a 16-byte boundary
     void* dx;
     float* part;                                          // [parts][2][cols]: dweight, dbias
 };
@@ -103,14 +104,14 @@ __device__ __forceinline__ float warp_sums(const float4& v)
     return c;
 }
 // Sums of up to four values over the threads that share a row: a warp, or the CTA (one barrier; `red` is another one in turn).
-template <bool WARP, int N>
+template <int W, int N>
 __device__ __forceinline__ float4 row_sums(const float4& v, float4* red)
 {
     float c = warp_sums(v);
-    if (!WARP) {
+    if (W > 32) {
         if (threadIdx.x % 8 == 0) reinterpret_cast<float*>(red)[threadIdx.x / 32 * 4 + threadIdx.x % 32 / 8] = c;
         __syncthreads();
-        c = warp_sums(threadIdx.x % 32 < blockDim.x / 32 ? red[threadIdx.x % 32] : make_float4(0.f, 0.f, 0.f, 0.f));
+        c = warp_sums(threadIdx.x % 32 < W / 32 ? red[threadIdx.x % 32] : make_float4(0.f, 0.f, 0.f, 0.f));
     }
     float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
     r.x = __shfl_sync(0xffffffffu, c, 0);
@@ -119,15 +120,15 @@ __device__ __forceinline__ float4 row_sums(const float4& v, float4* red)
     return r;
 }
 // ... of one.
-template <bool WARP>
+template <int W>
 __device__ __forceinline__ float row_sum(float a, float* red)
 {
 #pragma unroll
     for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-    if (WARP) return a;
+    if (W == 32) return a;
     if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = a;
     __syncthreads();
-    a = threadIdx.x % 32 < blockDim.x / 32 ? red[threadIdx.x % 32] : 0.f;
+    a = threadIdx.x % 32 < W / 32 ? red[threadIdx.x % 32] : 0.f;
 #pragma unroll
     for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
     return a;
@@ -138,21 +139,38 @@ template <typename T> struct NormStage {
     static constexpr int piece = 8 * (int)sizeof(T) + 8 + 4;               // bytes: dy, codes, the word that has the scale byte
 };
 
-template <typename T, bool LAYER, bool VEC, bool WARP, int PP>
-__global__ void __launch_bounds__(WARP ? 256 : kBlockThreads, WARP && PP < 4 ? 2 : 1) mx_norm_kernel(const NormArgs a)
+// W: threads that share a row (32: a warp, eight rows a CTA; else the CTA); PP: pieces of 8 columns a thread.
+template <typename T, bool LAYER, bool VEC, int W, int PP>
+__global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) : W <= 256 ? 4 : W <= 512 ? 2 : 1) mx_norm_kernel(const __grid_constant__ NormArgs a)
 {
+    constexpr bool WARP = W == 32;
     constexpr int NS = NormStage<T>::count, kDy = 8 * (int)sizeof(T);
     extern __shared__ __align__(16) unsigned char raw[];
     constexpr bool kShared = !WARP && PP > 1;             // dweight's sums lie in shared memory
     __shared__ float4 red[2][32];
     __shared__ float red1[2][32];
-    const int team = WARP ? threadIdx.x / 32 : 0, teams = WARP ? blockDim.x / 32 : 1, lane = WARP ? threadIdx.x % 32 : threadIdx.x, width = WARP ? 32 : blockDim.x;
-    const int pieces = (int)((a.cols + 7) / 8), slots = width * PP;
+    constexpr int teams = WARP ? 8 : 1, width = W, slots = W * PP;
+    const int team = WARP ? threadIdx.x / 32 : 0, lane = WARP ? threadIdx.x % 32 : threadIdx.x;
+    const int pieces = (int)((a.cols + 7) / 8);
     const float inv_n = 1.f / (float)a.cols;
     // weights [slots][8], then each team's stages of dy [slots][8], codes [slots][8 bytes], scale words [slots], then sums [2][slots][4]
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(raw), mine = base + slots * kDy + team * NS * slots * NormStage<T>::piece;
     const uint32_t sums = mine + NS * slots * NormStage<T>::piece;
-    for (int c = threadIdx.x; c < slots * 8; c += blockDim.x) reinterpret_cast<T*>(raw)[c] = a.weight && c < a.cols ? ((const T*)a.weight)[c] : mx_round<T>(1.f);
+    for (int c = threadIdx.x * 8; c < slots * 8; c += (WARP ? 256 : W) * 8) {
+        float w[8];
+        if (a.weight && c < a.cols) {
+            if (a.weight16) mx_load8<T, true>((const T*)a.weight, c, a.cols, w);
+            else mx_load8<T, false>((const T*)a.weight, c, a.cols, w);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = 1.f;
+        }
+        const MxPiece<T> piece = mx_piece<T>(w);
+#pragma unroll
+        for (int i = 0; i < kDy / 16; ++i) *reinterpret_cast<uint4*>(raw + c * (int)sizeof(T) + i * 16) = piece.q[i];
+    }
+    // pieces behind the row's end stay zeros
+    for (int e = lane; e < NS * slots * NormStage<T>::piece / 4; e += W) asm volatile("st.shared.b32 [%0], %1;" :: "r"(mine + e * 4), "r"(0) : "memory");
     __syncthreads();
 
     float dw[kShared ? 8 : PP * 8] = {}, db[LAYER ? PP * 8 : 1] = {};
@@ -222,13 +240,15 @@ __global__ void __launch_bounds__(WARP ? 256 : kBlockThreads, WARP && PP < 4 ? 2
 #pragma unroll
         for (int p = 0; p < PP; ++p) {
             const int at = lane + p * width;
-            uint2 code = make_uint2(0, 0);
-            uint32_t word = 0;
+            uint2 code;
+            uint32_t word;
+            if (!VEC) {
 #pragma unroll
-            for (int i = 0; i < kDy / 16; ++i) d[p].q[i] = make_uint4(0, 0, 0, 0);
-            if (at < pieces) {
-                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(code.x), "=r"(code.y) : "r"(from + slots * kDy + at * 8));
-                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(word) : "r"(from + slots * (kDy + 8) + at * 4));
+                for (int i = 0; i < kDy / 16; ++i) d[p].q[i] = make_uint4(0, 0, 0, 0);
+            }
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(code.x), "=r"(code.y) : "r"(from + slots * kDy + at * 8));
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(word) : "r"(from + slots * (kDy + 8) + at * 4));
+            if (VEC || at < pieces) {
                 if (VEC) {
 #pragma unroll
                     for (int i = 0; i < kDy / 16; ++i)
@@ -256,7 +276,7 @@ __global__ void __launch_bounds__(WARP ? 256 : kBlockThreads, WARP && PP < 4 ? 2
             m.x = LAYER ? fmaf(sx, s[p], m.x) : fmaf(sx * s[p], s[p], m.x);
             m.z = fmaf(sgx, s[p], m.z);
         }
-        m = row_sums<WARP, 3>(m, red[turn]);
+        m = row_sums<W, 3>(m, red[turn]);
         float mean = 0.f, mg = 0.f, sq = m.x, sgx = m.z;
         if (LAYER) {
             mean = m.x * inv_n;
@@ -279,7 +299,7 @@ __global__ void __launch_bounds__(WARP ? 256 : kBlockThreads, WARP && PP < 4 ? 2
                 for (int i = 0; i < 8; ++i) sq = fmaf(x[8 * p + i], x[8 * p + i], sq);
             }
         }
-        if (LAYER) sq = row_sum<WARP>(sq, red1[turn]);
+        if (LAYER) sq = row_sum<W>(sq, red1[turn]);
         const float r = 1.f / sqrtf(sq * inv_n + a.eps), c = -sgx * inv_n * r * r * r, mr = -mg * r;
 #pragma unroll
         for (int p = 0; p < PP; ++p) {
@@ -320,7 +340,7 @@ __global__ void __launch_bounds__(WARP ? 256 : kBlockThreads, WARP && PP < 4 ? 2
             }
             __syncthreads();
         }
-        for (int c = threadIdx.x; c < pitch; c += blockDim.x) {
+        for (int c = threadIdx.x; c < pitch; c += 256) {
             part[c] = joined[c];
             if (LAYER) part[pitch + c] = joined[kWarpColumns + c];
         }
@@ -477,7 +497,9 @@ NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtyp
         if (p.smem < 2 * kWarpColumns * 4) p.smem = 2 * kWarpColumns * 4;
     } else {
         p.pp = pieces <= kBlockThreads ? 1 : 2;
-        p.threads = (int)(((pieces + p.pp - 1) / p.pp + 31) / 32 * 32);
+        const int64_t need = (pieces + p.pp - 1) / p.pp;
+        p.threads = p.pp == 1 ? (need <= 256 ? 256 : need <= 512 ? 512 : 1024) : need <= 768 ? 768 : 1024;
+        if (need > kBlockThreads) p.threads = kBlockThreads + 1;
         const int64_t smem = (int64_t)p.threads * p.pp * (piece - 12 + stages * piece + (p.pp > 1 ? 32 : 0));
         p.wide = p.threads > kBlockThreads || smem > ctx->smem_optin - 2048;
         const int64_t most = ctx->num_sms * (p.threads <= 256 ? 4 : p.threads <= 512 ? 2 : 1);
@@ -494,11 +516,11 @@ NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtyp
     return p;
 }
 
-template <typename T, bool LAYER, bool VEC, bool WARP, int PP>
+template <typename T, bool LAYER, bool VEC, int W, int PP>
 void norm_start(const NormPlan& p, const NormArgs& a, cudaStream_t st)
 {
-    if (p.smem > 48 * 1024) cudaFuncSetAttribute(mx_norm_kernel<T, LAYER, VEC, WARP, PP>, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
-    mx_norm_kernel<T, LAYER, VEC, WARP, PP><<<p.grid, p.threads, p.smem, st>>>(a);
+    if (p.smem > 48 * 1024) cudaFuncSetAttribute(mx_norm_kernel<T, LAYER, VEC, W, PP>, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
+    mx_norm_kernel<T, LAYER, VEC, W, PP><<<p.grid, p.threads, p.smem, st>>>(a);
 }
 
 template <typename T, bool LAYER, bool VEC>
@@ -509,12 +531,16 @@ void norm_launch(const NormPlan& p, const NormArgs& a, float2* stats, bool sums,
         if (sums) mx_norm_columns_kernel<T, VEC><<<dim3((unsigned)((a.cols + 1023) / 1024), p.parts), 128, 0, st>>>(a, stats);
         mx_norm_wide_kernel<T, LAYER, VEC><<<p.grid, 512, 0, st>>>(a, stats, true);
     } else if (p.warp) {
-        if (p.pp == 1) norm_start<T, LAYER, VEC, true, 1>(p, a, st);
-        else if (p.pp == 2) norm_start<T, LAYER, VEC, true, 2>(p, a, st);
-        else norm_start<T, LAYER, VEC, true, 4>(p, a, st);
+        if (p.pp == 1) norm_start<T, LAYER, VEC, 32, 1>(p, a, st);
+        else if (p.pp == 2) norm_start<T, LAYER, VEC, 32, 2>(p, a, st);
+        else norm_start<T, LAYER, VEC, 32, 4>(p, a, st);
+    } else if (p.pp == 1) {
+        if (p.threads == 256) norm_start<T, LAYER, VEC, 256, 1>(p, a, st);
+        else if (p.threads == 512) norm_start<T, LAYER, VEC, 512, 1>(p, a, st);
+        else norm_start<T, LAYER, VEC, 1024, 1>(p, a, st);
     } else {
-        if (p.pp == 1) norm_start<T, LAYER, VEC, false, 1>(p, a, st);
-        else norm_start<T, LAYER, VEC, false, 2>(p, a, st);
+        if (p.threads == 768) norm_start<T, LAYER, VEC, 768, 2>(p, a, st);
+        else norm_start<T, LAYER, VEC, 1024, 2>(p, a, st);
     }
 }
 
@@ -585,7 +611,7 @@ extern "C" int galv_mx_norm_backward(galv_ctx* ctx, int64_t rows, int64_t cols, 
     const NormPlan p = norm_plan(ctx, rows, cols, dtype);
     NormArgs a;
     a.rows = rows; a.cols = cols; a.nb = mx_blocks(cols); a.pitch = mx_pitch8(cols); a.dy_stride = dy_stride; a.dx_stride = dx_stride;
-    a.eps = eps; a.codes = codes; a.scales = scales; a.dy = dy; a.weight = weight; a.dx = dx;
+    a.eps = eps; a.codes = codes; a.scales = scales; a.dy = dy; a.weight = weight; a.weight16 = mx_aligned(weight, 16); a.dx = dx;
     a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + p.stats);
     float2* stats = reinterpret_cast<float2*>(workspace);
     const bool vec = mx_rows16(dy, dy_stride, dtype) && mx_rows16(dx, dx_stride, dtype), layer = kind == GALV_NORM_LAYER, sums = dweight || dbias;
