@@ -45,16 +45,71 @@ template <typename T> __device__ __forceinline__ T mx_round(float v);
 template <> __device__ __forceinline__ float mx_round<float>(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 mx_round<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half mx_round<__half>(float v) { return __float2half_rn(v); }
+template <typename T> __device__ __forceinline__ T mx_zero() { return mx_round<T>(0.f); }
 // what was held as a finite number stays one in fp16 (a NaN passes both comparisons)
 template <typename T> __device__ __forceinline__ float mx_held(float v) { return v; }
 template <> __device__ __forceinline__ float mx_held<__half>(float v) { return v > 65504.f ? 65504.f : v < -65504.f ? -65504.f : v; }
 
+// How a pass over a matrix's pieces of 8 columns is spread: a CTA of 256 threads has `each` pieces a thread, 256 * each of a row, or whole short rows (the
+// width of a row is then a power of two of threads).  One division a CTA.  A thread's pieces are all loaded before the first is used: with two
+// 16-byte loads under way a thread the pass reached 3.7 TB/s, with four 5 and more.
+constexpr int kMxThreads = 256;
+template <typename T> struct MxEach { static constexpr int count = sizeof(T) == 2 ? 4 : 2; };
+struct MxSpread {
+    int log;          // threads along a row: 1 << log
+    int each;
+    unsigned segs;    // CTAs along a row
+    int dr, dc;       // from one of a thread's pieces to the next
+    long long blocks; // CTAs in all
+    MxSpread(long long rows, long long pieces, int each_) : log(0), each(each_)
+    {
+        while (log < 8 && (1ll << log) < pieces) ++log;
+        const int rpc = kMxThreads >> log;
+        const bool along = log == 8;
+        segs = along ? (unsigned)((pieces + each * kMxThreads - 1) / (each * kMxThreads)) : 1;
+        dr = along ? 0 : rpc;
+        dc = along ? kMxThreads : 0;
+        blocks = (along ? rows : (rows + each * rpc - 1) / (each * rpc)) * (long long)segs;
+    }
+    int grid() const { return (int)(blocks < (1ll << 30) ? blocks : (1ll << 30)); }
+};
+struct MxPlace { int row, c; };
+__device__ __forceinline__ MxPlace mx_place(const MxSpread& s, long long block)
+{
+    const int rows = (int)(block / s.segs), seg = (int)(block - (long long)rows * s.segs);
+    MxPlace p;
+    p.row = (int)((s.dr ? (long long)rows * s.each * s.dr : rows) + (threadIdx.x >> s.log));      // may pass the last row by a CTA's rows: galv.h's limit leaves room
+    p.c = seg * s.each * kMxThreads + (threadIdx.x & ((1 << s.log) - 1));
+    return p;
+}
+
 // 8 elements of a row as one piece: 16 bytes of 16-bit numbers, 32 of fp32.
 template <typename T> struct MxPiece { uint4 q[sizeof(T) / 2]; };
 
-// VEC: the row starts on a 16-byte boundary (c0 is a multiple of 8).  Behind `cols`: zeros.
+// As they lie in memory.  VEC: the row starts on a 16-byte boundary (c0 is a multiple of 8).  Behind `cols`: zeros.
 template <typename T, bool VEC>
-__device__ __forceinline__ void mx_load8(const T* __restrict__ row, long long c0, long long cols, float (&v)[8])
+__device__ __forceinline__ MxPiece<T> mx_fetch8(const T* row, int c0, int cols)
+{
+    MxPiece<T> p;
+    if (VEC && c0 + 8 <= cols) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) p.q[i] = reinterpret_cast<const uint4*>(row + c0)[i];
+    } else {
+        T* e = reinterpret_cast<T*>(&p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = c0 + i < cols ? row[c0 + i] : mx_zero<T>();
+    }
+    return p;
+}
+template <typename T> __device__ __forceinline__ void mx_floats(const MxPiece<T>& p, float (&v)[8])
+{
+    const T* e = reinterpret_cast<const T*>(&p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = mx_float(e[i]);
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void mx_load8(const T* __restrict__ row, int c0, int cols, float (&v)[8])
 {
     if (VEC && c0 + 8 <= cols) {
         MxPiece<T> p;
@@ -71,7 +126,7 @@ __device__ __forceinline__ void mx_load8(const T* __restrict__ row, long long c0
 
 // ... of a matrix that the same kernel may write (in place): not by the read-only path.
 template <typename T, bool VEC>
-__device__ __forceinline__ void mx_load8_rw(const T* row, long long c0, long long cols, float (&v)[8])
+__device__ __forceinline__ void mx_load8_rw(const T* row, int c0, int cols, float (&v)[8])
 {
     if (VEC && c0 + 8 <= cols) {
         MxPiece<T> p;
@@ -114,7 +169,7 @@ template <> __device__ __forceinline__ MxPiece<__half> mx_piece<__half>(const fl
 }
 
 template <typename T, bool VEC>
-__device__ __forceinline__ void mx_store8(T* __restrict__ row, long long c0, long long cols, const float (&v)[8])
+__device__ __forceinline__ void mx_store8(T* __restrict__ row, int c0, int cols, const float (&v)[8])
 {
     if (VEC && c0 + 8 <= cols) {
         const MxPiece<T> p = mx_piece<T>(v);
@@ -142,6 +197,21 @@ __device__ __forceinline__ int mx_scale_byte(uint32_t amax_bits)
 __device__ __forceinline__ float mx_inverse(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
 // 2^(byte - 127), NaN for 255
 __device__ __forceinline__ float mx_scale(int byte) { return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7fc00000u : (uint32_t)byte << 23); }
+
+// Bits (fp32) of the largest magnitude among 8 numbers.  Magnitudes order like their bits, infinities and NaN above all numbers.
+__device__ __forceinline__ uint32_t mx_pairs_most(const uint4& q)
+{
+    const uint32_t k = 0x7fff7fffu, m = __vimax3_u16x2(__vmaxu2(q.x & k, q.y & k), q.z & k, q.w & k);
+    return max(m & 0xffffu, m >> 16);
+}
+template <typename T> __device__ __forceinline__ uint32_t mx_most(const MxPiece<T>& p);
+template <> __device__ __forceinline__ uint32_t mx_most<__nv_bfloat16>(const MxPiece<__nv_bfloat16>& p) { return mx_pairs_most(p.q[0]) << 16; }
+template <> __device__ __forceinline__ uint32_t mx_most<__half>(const MxPiece<__half>& p) { return __float_as_uint(__half2float(__ushort_as_half((unsigned short)mx_pairs_most(p.q[0])))); }
+template <> __device__ __forceinline__ uint32_t mx_most<float>(const MxPiece<float>& p)
+{
+    const uint32_t k = 0x7fffffffu;
+    return max(max(max(p.q[0].x & k, p.q[0].y & k), max(p.q[0].z & k, p.q[0].w & k)), max(max(p.q[1].x & k, p.q[1].y & k), max(p.q[1].z & k, p.q[1].w & k)));
+}
 
 // Four numbers to four 8-bit elements, to nearest even (the conversion saturates; nothing here passes 448).
 __device__ __forceinline__ uint32_t mx_to8(float a, float b, float c, float d)
@@ -185,25 +255,19 @@ __device__ __forceinline__ void mx_from4(uint32_t w, float (&v)[8])
 
 // Where the scale byte of (row, block) lies.
 template <int FMT>
-__device__ __forceinline__ long long mx_scale_at(long long row, long long b, long long per_row)      // per_row: bytes a row (MX8), tiles a row of tiles (MX4)
+__device__ __forceinline__ long long mx_scale_at(int row, int b, int per_row)      // per_row: bytes a row (MX8), tiles a row of tiles (MX4)
 {
-    if (FMT == GALV_MX8) return row * per_row + b;
-    return ((row >> 7) * per_row + (b >> 2)) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (b & 3);
+    if (FMT == GALV_MX8) return (long long)row * per_row + b;
+    return ((long long)(row >> 7) * per_row + (b >> 2)) * 512 + ((row & 31) * 16 + ((row >> 5) & 3) * 4 + (b & 3));
 }
 
-// The 8 held values of piece c (columns 8c .. 8c+7) of a row.
-template <int FMT>
-__device__ __forceinline__ void mx_restore8(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, long long row, long long c, long long nb,
-                                            long long per_row, float (&v)[8])
+// The 8 values held in GALV_MX8 of piece c (columns 8c .. 8c+7) of a row.
+__device__ __forceinline__ void mx_restore8(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, long long row, int c, long long nb, long long per_row, float (&v)[8])
 {
-    if (FMT == GALV_MX8) {
-        const uint2 w = __ldg(reinterpret_cast<const uint2*>(codes + (row * nb * 32 + c * 8)));
-        mx_from8(w.x, v);
-        mx_from8(w.y, v + 4);
-    } else {
-        mx_from4(__ldg(reinterpret_cast<const uint32_t*>(codes + (row * nb * 16 + c * 4))), v);
-    }
-    const float s = mx_scale(__ldg(scales + mx_scale_at<FMT>(row, c >> 2, per_row)));
+    const uint2 w = __ldg(reinterpret_cast<const uint2*>(codes + (row * nb * 32 + c * 8ll)));
+    mx_from8(w.x, v);
+    mx_from8(w.y, v + 4);
+    const float s = mx_scale(__ldg(scales + row * per_row + (c >> 2)));
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= s;
 }

@@ -4,44 +4,86 @@
 
 namespace {
 
-constexpr int kThreads = 256;
+__device__ __forceinline__ float exp2_fast(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }      // within 2^-22 of the value
+__device__ __forceinline__ float inverse_fast(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }   // within 1 step
+__device__ __forceinline__ float clamped(float x, float most)      // a NaN stays one
+{
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(most));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(-most));
+    return x;
+}
 
-// f'(x) of the activation functions, 0 or 1 from |x| = 100 on (a NaN passes both comparisons).
+// f'(x) of the activation functions, within 4e-7 (gelu_tanh 1e-6) of the largest slope: the pass has some twenty instructions an element at the memory's
+// rate, and the exact functions take fifty.  From the bounds of x on, the slopes are 0 and 1 to 32 bits.
 template <int ACT>
 __device__ __forceinline__ float act_slope(float x)
 {
-    x = x > 100.f ? 100.f : x < -100.f ? -100.f : x;
     if (ACT == GALV_ACT_GELU) {
-        // Phi(x) + x phi(x)
-        return 0.5f * (1.f + erff(x * 0.70710678118654752f)) + x * expf(-0.5f * x * x) * 0.39894228040143268f;
+        // Phi(x) + x phi(x).  Abramowitz and Stegun 7.1.26: erfc(u) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) exp(-u^2), t = 1 / (1 + p u), to 1.5e-7 for u >= 0;
+        // with u = |x| / sqrt(2) the exponential is phi's.
+        x = clamped(x, 30.f);
+        const float e = exp2_fast(x * x * -0.72134752f);               // exp(-x^2 / 2)
+        const float t = inverse_fast(fmaf(fabsf(x), 0.3275911f * 0.70710678f, 1.f));
+        float q = fmaf(t, 1.061405429f, -1.453152027f);
+        q = fmaf(t, q, 1.421413741f);
+        q = fmaf(t, q, -0.284496736f);
+        q = fmaf(t, q, 0.254829592f);
+        q *= 0.5f * t * e;                                             // Phi(-|x|)
+        return fmaf(x * 0.39894228f, e, x >= 0.f ? 1.f - q : q);
     } else if (ACT == GALV_ACT_GELU_TANH) {
-        const float k = 0.79788456080286536f, x2 = x * x;
-        const float t = tanhf(k * x * (1.f + 0.044715f * x2));
-        return 0.5f * (1.f + t) + 0.5f * x * (1.f - t * t) * k * (1.f + 3.f * 0.044715f * x2);
+        // (1 + tanh z) / 2 = 1 / (1 + exp(-2 z)) = s and its slope 2 z' exp(-2 z) s^2, without a difference of near numbers
+        x = clamped(x, 10.f);
+        const float x2 = x * x;
+        const float e = exp2_fast(x * fmaf(x2, -2.f * 0.79788456f * 0.044715f * 1.44269504f, -2.f * 0.79788456f * 1.44269504f));
+        const float s = inverse_fast(1.f + e);
+        return fmaf(x * fmaf(x2, 6.f * 0.79788456f * 0.044715f, 2.f * 0.79788456f), e * s * s, s);
     } else {
-        const float s = 1.f / (1.f + expf(-x));
-        return s * (1.f + x * (1.f - s));
+        x = clamped(x, 80.f);
+        const float e = exp2_fast(x * -1.44269504f), s = inverse_fast(1.f + e);
+        return fmaf(x * e * s, s, s);
     }
 }
 
 template <typename T, int ACT, bool VEC>
-__global__ void __launch_bounds__(kThreads) mx_act_kernel(long long rows, long long cols, long long nb, long long pieces, long long per_row,
-                                                          const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const T* dy,
-                                                          long long dy_stride, T* dx, long long dx_stride)
+__global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread spread, int rows, int cols, int nb, int pieces, int per_row,
+                                                            const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const T* dy,
+                                                            long long dy_stride, T* dx, long long dx_stride)
 {
-    const long long step = (long long)gridDim.x * kThreads, dr = step / pieces, dc = step % pieces;
-    const long long first = (long long)blockIdx.x * kThreads + threadIdx.x;
-    long long row = first / pieces, c = first % pieces;
-    for (long long item = first; item < rows * pieces; item += step) {
-        float x[8], g[8];
-        mx_restore8<GALV_MX8>(codes, scales, row, c, nb, per_row, x);
-        mx_load8_rw<T, VEC>(dy + row * dy_stride, c * 8, cols, g);
+    for (long long block = blockIdx.x; block < spread.blocks; block += gridDim.x) {
+        const MxPlace at = mx_place(spread, block);
+        constexpr int U = MxEach<T>::count;
+        uint2 code[U];
+        int byte[U];
+        MxPiece<T> raw[U];
+        const T* from = dy + at.row * dy_stride;
+        const uint8_t* held = codes + ((long long)at.row * nb * 32 + at.c * 8ll);
+        const uint8_t* power = scales + ((long long)at.row * per_row + (at.c >> 2));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] *= act_slope<ACT>(x[i]);
-        mx_store8<T, VEC>(dx + row * dx_stride, c * 8, cols, g);
-        row += dr;
-        c += dc;
-        if (c >= pieces) { c -= pieces; ++row; }
+        for (int h = 0; h < U; ++h) {
+            const int row = at.row + h * spread.dr, c = at.c + h * spread.dc;
+            if (row < rows && c < pieces) {
+                code[h] = __ldg(reinterpret_cast<const uint2*>(held));
+                byte[h] = __ldg(power);
+                raw[h] = mx_fetch8<T, VEC>(from, c * 8, cols);
+            }
+            from += spread.dr * dy_stride;
+            held += (long long)spread.dr * nb * 32 + spread.dc * 8;
+            power += (long long)spread.dr * per_row + spread.dc / 4;
+        }
+        T* to = dx + at.row * dx_stride;
+#pragma unroll
+        for (int h = 0; h < U; ++h, to += spread.dr * dx_stride) {
+            const int row = at.row + h * spread.dr, c = at.c + h * spread.dc;
+            if (row >= rows || c >= pieces) continue;
+            float x[8], g[8];
+            mx_from8(code[h].x, x);
+            mx_from8(code[h].y, x + 4);
+            mx_floats(raw[h], g);
+            const float s = mx_scale(byte[h]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[i] *= act_slope<ACT>(x[i] * s);
+            mx_store8<T, VEC>(to, c * 8, cols, g);
+        }
     }
 }
 
@@ -159,8 +201,8 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
     for (int c = threadIdx.x * 8; c < slots * 8; c += (WARP ? 256 : W) * 8) {
         float w[8];
         if (a.weight && c < a.cols) {
-            if (a.weight16) mx_load8<T, true>((const T*)a.weight, c, a.cols, w);
-            else mx_load8<T, false>((const T*)a.weight, c, a.cols, w);
+            if (a.weight16) mx_load8<T, true>((const T*)a.weight, c, (int)a.cols, w);
+            else mx_load8<T, false>((const T*)a.weight, c, (int)a.cols, w);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = 1.f;
@@ -409,7 +451,7 @@ __global__ void __launch_bounds__(512) mx_norm_wide_kernel(const NormArgs a, flo
             float mean = 0.f, s = 0.f;
             if (LAYER) {
                 for (long long c = threadIdx.x; c < pieces; c += 512) {
-                    mx_restore8<GALV_MX8>(a.codes, a.scales, row, c, a.nb, a.pitch, x);
+                    mx_restore8(a.codes, a.scales, row, (int)c, a.nb, a.pitch, x);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) s += x[i];
                 }
@@ -417,7 +459,7 @@ __global__ void __launch_bounds__(512) mx_norm_wide_kernel(const NormArgs a, flo
             }
             s = 0.f;
             for (long long c = threadIdx.x; c < pieces; c += 512) {
-                mx_restore8<GALV_MX8>(a.codes, a.scales, row, c, a.nb, a.pitch, x);
+                mx_restore8(a.codes, a.scales, row, (int)c, a.nb, a.pitch, x);
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     if (c * 8 + i < a.cols) s = fmaf(x[i] - mean, x[i] - mean, s);
@@ -429,9 +471,9 @@ __global__ void __launch_bounds__(512) mx_norm_wide_kernel(const NormArgs a, flo
         const float mean = stats[row].x, rstd = stats[row].y;
         float sg = 0.f, sgx = 0.f;
         for (long long c = threadIdx.x; c < pieces; c += 512) {
-            mx_restore8<GALV_MX8>(a.codes, a.scales, row, c, a.nb, a.pitch, x);
-            mx_load8_rw<T, VEC>(dy, c * 8, a.cols, g);
-            if (a.weight) mx_load8<T, false>((const T*)a.weight, c * 8, a.cols, w);
+            mx_restore8(a.codes, a.scales, row, (int)c, a.nb, a.pitch, x);
+            mx_load8_rw<T, VEC>(dy, (int)c * 8, (int)a.cols, g);
+            if (a.weight) mx_load8<T, false>((const T*)a.weight, (int)c * 8, (int)a.cols, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float gw = a.weight ? g[i] * w[i] : g[i];
@@ -441,12 +483,12 @@ __global__ void __launch_bounds__(512) mx_norm_wide_kernel(const NormArgs a, flo
         }
         const float mg = LAYER ? block_sum(sg, red) * inv_n : 0.f, m = block_sum(sgx, red) * inv_n * rstd * rstd;
         for (long long c = threadIdx.x; c < pieces; c += 512) {
-            mx_restore8<GALV_MX8>(a.codes, a.scales, row, c, a.nb, a.pitch, x);
-            mx_load8_rw<T, VEC>(dy, c * 8, a.cols, g);
-            if (a.weight) mx_load8<T, false>((const T*)a.weight, c * 8, a.cols, w);
+            mx_restore8(a.codes, a.scales, row, (int)c, a.nb, a.pitch, x);
+            mx_load8_rw<T, VEC>(dy, (int)c * 8, (int)a.cols, g);
+            if (a.weight) mx_load8<T, false>((const T*)a.weight, (int)c * 8, (int)a.cols, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) g[i] = rstd * ((a.weight ? g[i] * w[i] : g[i]) - mg - (x[i] - mean) * m);
-            mx_store8<T, VEC>(dx, c * 8, a.cols, g);
+            mx_store8<T, VEC>(dx, (int)c * 8, (int)a.cols, g);
         }
     }
 }
@@ -460,8 +502,8 @@ __global__ void __launch_bounds__(128) mx_norm_columns_kernel(const NormArgs a, 
     float dw[8] = {}, db[8] = {}, x[8], g[8];
     for (long long row = blockIdx.y; row < a.rows; row += gridDim.y) {
         const float2 st = stats[row];
-        mx_restore8<GALV_MX8>(a.codes, a.scales, row, c, a.nb, a.pitch, x);
-        mx_load8_rw<T, VEC>((const T*)a.dy + row * a.dy_stride, c * 8, a.cols, g);
+        mx_restore8(a.codes, a.scales, row, (int)c, a.nb, a.pitch, x);
+        mx_load8_rw<T, VEC>((const T*)a.dy + row * a.dy_stride, (int)c * 8, (int)a.cols, g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             dw[i] = fmaf(g[i], (x[i] - st.x) * st.y, dw[i]);
@@ -559,14 +601,14 @@ extern "C" int galv_mx_act_backward(galv_ctx* ctx, int64_t rows, int64_t cols, i
         return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_mx_act_backward: dx may be dy with the same stride only");
     MxDevice dev(ctx);
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
-    const long long nb = mx_blocks(cols), pieces = (cols + 7) / 8, pitch = mx_pitch8(cols);
+    const int nb = (int)mx_blocks(cols), pitch = (int)mx_pitch8(cols), pieces = (int)((cols + 7) / 8);
     const bool vec = mx_rows16(dy, dy_stride, dtype) && mx_rows16(dx, dx_stride, dtype);
-    const long long blocks = (rows * pieces + kThreads - 1) / kThreads, most = (long long)ctx->num_sms * 32;
-    const int grid = (int)(blocks < most ? blocks : most);
+    const MxSpread spread(rows, pieces, dtype == GALV_F32 ? MxEach<float>::count : MxEach<__half>::count);
+    const int grid = spread.grid();
     cudaStream_t st = (cudaStream_t)stream;
 #define MX_ACT(ACT)                                                                                                                                        \
-    MX_DISPATCH_TYPE(dtype, if (vec) mx_act_kernel<T, ACT, true><<<grid, kThreads, 0, st>>>(rows, cols, nb, pieces, pitch, codes, scales, (const T*)dy, dy_stride, (T*)dx, dx_stride); \
-                     else mx_act_kernel<T, ACT, false><<<grid, kThreads, 0, st>>>(rows, cols, nb, pieces, pitch, codes, scales, (const T*)dy, dy_stride, (T*)dx, dx_stride))
+    MX_DISPATCH_TYPE(dtype, if (vec) mx_act_kernel<T, ACT, true><<<grid, kMxThreads, 0, st>>>(spread, (int)rows, (int)cols, nb, pieces, pitch, codes, scales, (const T*)dy, dy_stride, (T*)dx, dx_stride); \
+                     else mx_act_kernel<T, ACT, false><<<grid, kMxThreads, 0, st>>>(spread, (int)rows, (int)cols, nb, pieces, pitch, codes, scales, (const T*)dy, dy_stride, (T*)dx, dx_stride))
     if (act == GALV_ACT_GELU) MX_ACT(GALV_ACT_GELU);
     else if (act == GALV_ACT_GELU_TANH) MX_ACT(GALV_ACT_GELU_TANH);
     else MX_ACT(GALV_ACT_SILU);

@@ -7,76 +7,92 @@
 
 namespace {
 
-constexpr int kThreads = 256;
-
-// Pieces of 8 columns, row by row; a row has `pieces` of them, up to the last scale byte that has to be written.
-struct PieceWalk {
-    long long row;
-    long long c;
-    __device__ PieceWalk(long long item, long long pieces) : row(item / pieces), c(item % pieces) {}
-    __device__ void step(long long dr, long long dc, long long pieces)
-    {
-        row += dr;
-        c += dc;
-        if (c >= pieces) { c -= pieces; ++row; }
-    }
-};
-
+// Rows up to rows_out and pieces up to `pieces` have a scale byte to write; rows and nb * 4 pieces lie in the matrix.
 template <typename T, int FMT, bool VEC>
-__global__ void __launch_bounds__(kThreads) mx_pack_kernel(long long rows, long long rows_out, long long cols, long long nb, long long pieces, long long per_row,
-                                                           const T* __restrict__ x, long long stride, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales)
+__global__ void __launch_bounds__(kMxThreads) mx_pack_kernel(const MxSpread spread, int rows, int rows_out, int cols, int nb, int pieces, int per_row,
+                                                             const T* __restrict__ x, long long stride, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales)
 {
-    const long long step = (long long)gridDim.x * kThreads, dr = step / pieces, dc = step % pieces;
-    PieceWalk at((long long)blockIdx.x * kThreads + threadIdx.x, pieces);
-    // a row has a multiple of 4 pieces, so the four threads of a block agree; a warp leaves as a whole
-    for (long long item = (long long)blockIdx.x * kThreads + threadIdx.x; item - threadIdx.x % 32 < rows_out * pieces; item += step, at.step(dr, dc, pieces)) {
-        const bool in = at.row < rows && at.c < nb * 4;
-        float v[8];
+    for (long long block = blockIdx.x; block < spread.blocks; block += gridDim.x) {
+        const MxPlace at = mx_place(spread, block);
+        constexpr int U = MxEach<T>::count;
+        MxPiece<T> raw[U];
+        const T* from = x + at.row * stride;
+        uint8_t* to = codes + ((long long)at.row * nb * 4 + at.c) * FMT;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.f;
-        if (in) mx_load8<T, VEC>(x + at.row * stride, at.c * 8, cols, v);
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-        const int byte = mx_scale_byte<FMT>(m);
-        const float inv = byte == 255 ? 0.f : mx_inverse(byte);
-        if (in) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = byte == 255 ? 0.f : v[i] * inv;
-            if (FMT == GALV_MX8) {
-                uint2 w;
-                w.x = mx_to8(v[0], v[1], v[2], v[3]);
-                w.y = mx_to8(v[4], v[5], v[6], v[7]);
-                *reinterpret_cast<uint2*>(codes + (at.row * nb * 32 + at.c * 8)) = w;
+        for (int h = 0; h < U; ++h, from += spread.dr * stride) {
+            const int row = at.row + h * spread.dr, c = at.c + h * spread.dc;
+            if (row < rows && c < nb * 4) {
+                raw[h] = mx_fetch8<T, VEC>(from, c * 8, cols);
             } else {
-                *reinterpret_cast<uint32_t*>(codes + (at.row * nb * 16 + at.c * 4)) = mx_to4(v);
+#pragma unroll
+                for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[h].q[i] = make_uint4(0, 0, 0, 0);
             }
         }
-        if ((at.c & 3) == 0 && at.row < rows_out) scales[mx_scale_at<FMT>(at.row, at.c >> 2, per_row)] = (uint8_t)byte;      // zero outside the matrix
+#pragma unroll
+        for (int h = 0; h < U; ++h, to += ((long long)spread.dr * nb * 4 + spread.dc) * FMT) {
+            const int row = at.row + h * spread.dr, c = at.c + h * spread.dc;
+            uint32_t m = mx_most<T>(raw[h]);
+            m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));            // the four threads of a block lie next to one another
+            m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+            const int byte = mx_scale_byte<FMT>(m);
+            if (row < rows && c < nb * 4) {
+                const float inv = mx_inverse(byte);
+                float v[8];
+                mx_floats(raw[h], v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= inv;
+                if (FMT == GALV_MX8) {
+                    uint2 w;
+                    w.x = mx_to8(v[0], v[1], v[2], v[3]);
+                    w.y = mx_to8(v[4], v[5], v[6], v[7]);
+                    if (byte == 255) w = make_uint2(0, 0);
+                    *reinterpret_cast<uint2*>(to) = w;
+                } else {
+                    *reinterpret_cast<uint32_t*>(to) = byte == 255 ? 0 : mx_to4(v);
+                }
+            }
+            if ((c & 3) == 0 && row < rows_out && c < pieces) scales[mx_scale_at<FMT>(row, c >> 2, per_row)] = (uint8_t)byte;      // zero outside the matrix
+        }
     }
 }
 
 template <typename T, int FMT, bool VEC>
-__global__ void __launch_bounds__(kThreads) mx_unpack_kernel(long long rows, long long cols, long long nb, long long pieces, long long per_row,
-                                                             const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ x, long long stride)
+__global__ void __launch_bounds__(kMxThreads) mx_unpack_kernel(const MxSpread spread, int rows, int cols, int nb, int pieces, int per_row,
+                                                               const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ x, long long stride)
 {
-    const long long step = (long long)gridDim.x * kThreads, dr = step / pieces, dc = step % pieces;
-    PieceWalk at((long long)blockIdx.x * kThreads + threadIdx.x, pieces);
-    for (long long item = (long long)blockIdx.x * kThreads + threadIdx.x; item < rows * pieces; item += step, at.step(dr, dc, pieces)) {
-        float v[8];
-        mx_restore8<FMT>(codes, scales, at.row, at.c, nb, per_row, v);
+    for (long long block = blockIdx.x; block < spread.blocks; block += gridDim.x) {
+        const MxPlace at = mx_place(spread, block);
+        constexpr int U = MxEach<T>::count;
+        uint2 code[U];
+        int byte[U];
+        const uint8_t* held = codes + ((long long)at.row * nb * 4 + at.c) * FMT;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = mx_held<T>(v[i]);
-        mx_store8<T, VEC>(x + at.row * stride, at.c * 8, cols, v);
+        for (int h = 0; h < U; ++h, held += ((long long)spread.dr * nb * 4 + spread.dc) * FMT) {
+            const int row = at.row + h * spread.dr, c = at.c + h * spread.dc;
+            if (row < rows && c < pieces) {
+                if (FMT == GALV_MX8) code[h] = __ldg(reinterpret_cast<const uint2*>(held));
+                else code[h].x = __ldg(reinterpret_cast<const uint32_t*>(held));
+                byte[h] = __ldg(scales + mx_scale_at<FMT>(row, c >> 2, per_row));
+            }
+        }
+        T* to = x + at.row * stride;
+#pragma unroll
+        for (int h = 0; h < U; ++h, to += spread.dr * stride) {
+            const int row = at.row + h * spread.dr, c = at.c + h * spread.dc;
+            if (row >= rows || c >= pieces) continue;
+            float v[8];
+            if (FMT == GALV_MX8) {
+                mx_from8(code[h].x, v);
+                mx_from8(code[h].y, v + 4);
+            } else {
+                mx_from4(code[h].x, v);
+            }
+            const float s = mx_scale(byte[h]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = mx_held<T>(v[i] * s);
+            mx_store8<T, VEC>(to, c * 8, cols, v);
+        }
     }
-}
-
-int pass_grid(const galv_ctx* ctx, long long items)
-{
-    const long long blocks = (items + kThreads - 1) / kThreads, most = (long long)ctx->num_sms * 32;
-    return (int)(blocks < most ? blocks : most);
 }
 
 }  // namespace
@@ -105,16 +121,17 @@ extern "C" int galv_mx_pack(galv_ctx* ctx, int64_t rows, int64_t cols, const voi
         return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_mx_pack: NULL or misaligned pointer, or a row stride below cols");
     MxDevice dev(ctx);
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
-    const long long nb = mx_blocks(cols);
+    const int nb = (int)mx_blocks(cols);
     const bool vec = mx_rows16(x, x_stride, dtype);
     // every scale byte is written, those behind the rows and blocks too
-    const long long rows_out = fmt == GALV_MX8 ? rows : (rows + 127) / 128 * 128;
-    const long long pieces = fmt == GALV_MX8 ? mx_pitch8(cols) * 4 : (nb + 3) / 4 * 16, per_row = fmt == GALV_MX8 ? mx_pitch8(cols) : (nb + 3) / 4;
-    const int grid = pass_grid(ctx, rows_out * pieces);
+    const int rows_out = (int)(fmt == GALV_MX8 ? rows : (rows + 127) / 128 * 128), per_row = fmt == GALV_MX8 ? (int)mx_pitch8(cols) : (nb + 3) / 4;
+    const int pieces = fmt == GALV_MX8 ? per_row * 4 : per_row * 16;
+    const MxSpread spread(rows_out, pieces, dtype == GALV_F32 ? MxEach<float>::count : MxEach<__half>::count);
+    const int grid = spread.grid();
     cudaStream_t st = (cudaStream_t)stream;
 #define MX_PACK(FMT)                                                                                                                                         \
-    MX_DISPATCH_TYPE(dtype, if (vec) mx_pack_kernel<T, FMT, true><<<grid, kThreads, 0, st>>>(rows, rows_out, cols, nb, pieces, per_row, (const T*)x, x_stride, codes, scales); \
-                     else mx_pack_kernel<T, FMT, false><<<grid, kThreads, 0, st>>>(rows, rows_out, cols, nb, pieces, per_row, (const T*)x, x_stride, codes, scales))
+    MX_DISPATCH_TYPE(dtype, if (vec) mx_pack_kernel<T, FMT, true><<<grid, kMxThreads, 0, st>>>(spread, (int)rows, rows_out, (int)cols, nb, pieces, per_row, (const T*)x, x_stride, codes, scales); \
+                     else mx_pack_kernel<T, FMT, false><<<grid, kMxThreads, 0, st>>>(spread, (int)rows, rows_out, (int)cols, nb, pieces, per_row, (const T*)x, x_stride, codes, scales))
     if (fmt == GALV_MX8) MX_PACK(GALV_MX8);
     else MX_PACK(GALV_MX4);
 #undef MX_PACK
@@ -133,13 +150,15 @@ extern "C" int galv_mx_unpack(galv_ctx* ctx, int64_t rows, int64_t cols, int32_t
         return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_mx_unpack: NULL or misaligned pointer, or a row stride below cols");
     MxDevice dev(ctx);
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
-    const long long nb = mx_blocks(cols), pieces = (cols + 7) / 8, per_row = fmt == GALV_MX8 ? mx_pitch8(cols) : (nb + 3) / 4;
+    const int nb = (int)mx_blocks(cols), pieces = (int)((cols + 7) / 8);
+    const int per_row = fmt == GALV_MX8 ? (int)mx_pitch8(cols) : (nb + 3) / 4;
     const bool vec = mx_rows16(x, x_stride, dtype);
-    const int grid = pass_grid(ctx, rows * pieces);
+    const MxSpread spread(rows, pieces, dtype == GALV_F32 ? MxEach<float>::count : MxEach<__half>::count);
+    const int grid = spread.grid();
     cudaStream_t st = (cudaStream_t)stream;
 #define MX_UNPACK(FMT)                                                                                                                         \
-    MX_DISPATCH_TYPE(dtype, if (vec) mx_unpack_kernel<T, FMT, true><<<grid, kThreads, 0, st>>>(rows, cols, nb, pieces, per_row, codes, scales, (T*)x, x_stride); \
-                     else mx_unpack_kernel<T, FMT, false><<<grid, kThreads, 0, st>>>(rows, cols, nb, pieces, per_row, codes, scales, (T*)x, x_stride))
+    MX_DISPATCH_TYPE(dtype, if (vec) mx_unpack_kernel<T, FMT, true><<<grid, kMxThreads, 0, st>>>(spread, (int)rows, (int)cols, nb, pieces, per_row, codes, scales, (T*)x, x_stride); \
+                     else mx_unpack_kernel<T, FMT, false><<<grid, kMxThreads, 0, st>>>(spread, (int)rows, (int)cols, nb, pieces, per_row, codes, scales, (T*)x, x_stride))
     if (fmt == GALV_MX8) MX_UNPACK(GALV_MX8);
     else MX_UNPACK(GALV_MX4);
 #undef MX_UNPACK
