@@ -49,6 +49,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
                                                             const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const T* dy,
                                                             long long dy_stride, T* dx, long long dx_stride)
 {
+    __shared__ __align__(16) T buf[VEC ? 1 : kMxThreads / 32][256];
     for (long long block = blockIdx.x; block < spread.blocks; block += gridDim.x) {
         const MxPlace at = mx_place(spread, block);
         constexpr int U = MxEach<T>::count;
@@ -65,6 +66,11 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
                 code[h] = __ldg(reinterpret_cast<const uint2*>(held));
                 byte[h] = __ldg(power);
                 raw[h] = mx_fetch8<T, VEC>(from, c * 8, cols);
+            } else if (!VEC) {
+                code[h] = make_uint2(0, 0);
+                byte[h] = 0;
+#pragma unroll
+                for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[h].q[i] = make_uint4(0, 0, 0, 0);
             }
             from += spread.dr * dy_stride;
             held += (long long)spread.dr * nb * 32 + spread.dc * 8;
@@ -74,7 +80,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
 #pragma unroll
         for (int h = 0; h < U; ++h, to += spread.dr * dx_stride) {
             const int row = at.row + h * spread.dr, c = at.c + h * spread.dc;
-            if (row >= rows || c >= pieces) continue;
+            if (VEC && (row >= rows || c >= pieces)) continue;
             float x[8], g[8];
             mx_from8(code[h].x, x);
             mx_from8(code[h].y, x + 4);
@@ -82,7 +88,8 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
             const float s = mx_scale(byte[h]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) g[i] *= act_slope<ACT>(x[i] * s);
-            mx_store8<T, VEC>(to, c * 8, cols, g);
+            if (VEC) mx_store8<T, true>(to, c * 8, cols, g);
+            else mx_scatter8<T>(buf[threadIdx.x / 32], MxPlaces<T>(dx, dx_stride, spread, at, h, rows, cols), g);
         }
     }
 }
@@ -189,6 +196,7 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
     constexpr int NS = NormStage<T>::count, kDy = 8 * (int)sizeof(T);
     extern __shared__ __align__(16) unsigned char raw[];
     constexpr bool kShared = !WARP && PP > 1;             // dweight's sums lie in shared memory
+    __shared__ __align__(16) T buf[VEC ? 1 : (WARP ? 8 : W / 32)][256];
     __shared__ float4 red[2][32];
     __shared__ float red1[2][32];
     constexpr int teams = WARP ? 8 : 1, width = W, slots = W * PP;
@@ -284,24 +292,17 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
             const int at = lane + p * width;
             uint2 code;
             uint32_t word;
-            if (!VEC) {
-#pragma unroll
-                for (int i = 0; i < kDy / 16; ++i) d[p].q[i] = make_uint4(0, 0, 0, 0);
-            }
             asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(code.x), "=r"(code.y) : "r"(from + slots * kDy + at * 8));
             asm volatile("ld.shared.b32 %0, [%1];" : "=r"(word) : "r"(from + slots * (kDy + 8) + at * 4));
-            if (VEC || at < pieces) {
-                if (VEC) {
+            if (VEC) {
 #pragma unroll
-                    for (int i = 0; i < kDy / 16; ++i)
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(d[p].q[i].x), "=r"(d[p].q[i].y), "=r"(d[p].q[i].z), "=r"(d[p].q[i].w) : "r"(from + at * kDy + i * 16));
-                } else {
-                    const T* from_row = (const T*)a.dy + row * a.dy_stride;
-                    T* e = reinterpret_cast<T*>(&d[p]);
+                for (int i = 0; i < kDy / 16; ++i)
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(d[p].q[i].x), "=r"(d[p].q[i].y), "=r"(d[p].q[i].z), "=r"(d[p].q[i].w) : "r"(from + at * kDy + i * 16));
+            } else {
+                const T* from_row = (const T*)a.dy + row * a.dy_stride;
+                T* e = reinterpret_cast<T*>(&d[p]);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (at * 8 + i < cols) e[i] = from_row[at * 8 + i];
-                }
+                for (int i = 0; i < 8; ++i) e[i] = at * 8 + i < cols ? from_row[at * 8 + i] : mx_zero<T>();
             }
             mx_from8(code.x, x + 8 * p);
             mx_from8(code.y, x + 8 * p + 4);
@@ -357,7 +358,15 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
                 if (LAYER) db[8 * p + i] += y;
             }
             if (kShared) sums_store(p);
-            mx_store8<T, VEC>(dx, (lane + p * width) * 8, cols, v);
+            if (VEC) {
+                mx_store8<T, true>(dx, (lane + p * width) * 8, cols, v);
+            } else {
+                mx_scatter8<T>(buf[threadIdx.x / 32], [&](int l, int& n) {
+                    const int c = ((lane & ~31) + l + p * width) * 8;
+                    n = min(8, cols - c);
+                    return dx + c;
+                }, v);
+            }
         }
     }
     // this CTA's column sums
@@ -543,7 +552,7 @@ NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtyp
         p.threads = p.pp == 1 ? (need <= 256 ? 256 : need <= 512 ? 512 : 1024) : need <= 768 ? 768 : 1024;
         if (need > kBlockThreads) p.threads = kBlockThreads + 1;
         const int64_t smem = (int64_t)p.threads * p.pp * (piece - 12 + stages * piece + (p.pp > 1 ? 32 : 0));
-        p.wide = p.threads > kBlockThreads || smem > ctx->smem_optin - 2048;
+        p.wide = p.threads > kBlockThreads || smem > ctx->smem_optin - 36 * 1024;
         const int64_t most = ctx->num_sms * (p.threads <= 256 ? 4 : p.threads <= 512 ? 2 : 1);
         p.parts = p.grid = (int)(rows < most ? rows : most);
         p.smem = (int)smem;

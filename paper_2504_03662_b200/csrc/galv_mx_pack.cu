@@ -60,6 +60,7 @@ template <typename T, int FMT, bool VEC>
 __global__ void __launch_bounds__(kMxThreads) mx_unpack_kernel(const MxSpread spread, int rows, int cols, int nb, int pieces, int per_row,
                                                                const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ x, long long stride)
 {
+    __shared__ __align__(16) T buf[VEC ? 1 : kMxThreads / 32][256];
     for (long long block = blockIdx.x; block < spread.blocks; block += gridDim.x) {
         const MxPlace at = mx_place(spread, block);
         constexpr int U = MxEach<T>::count;
@@ -79,7 +80,9 @@ __global__ void __launch_bounds__(kMxThreads) mx_unpack_kernel(const MxSpread sp
 #pragma unroll
         for (int h = 0; h < U; ++h, to += spread.dr * stride) {
             const int row = at.row + h * spread.dr, c = at.c + h * spread.dc;
-            if (row >= rows || c >= pieces) continue;
+            const bool in = row < rows && c < pieces;
+            if (VEC && !in) continue;
+            if (!VEC && !in) { code[h] = make_uint2(0, 0); byte[h] = 0; }
             float v[8];
             if (FMT == GALV_MX8) {
                 mx_from8(code[h].x, v);
@@ -90,7 +93,8 @@ __global__ void __launch_bounds__(kMxThreads) mx_unpack_kernel(const MxSpread sp
             const float s = mx_scale(byte[h]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = mx_held<T>(v[i] * s);
-            mx_store8<T, VEC>(to, c * 8, cols, v);
+            if (VEC) mx_store8<T, true>(to, c * 8, cols, v);
+            else mx_scatter8<T>(buf[threadIdx.x / 32], MxPlaces<T>(x, stride, spread, at, h, rows, cols), v);
         }
     }
 }
