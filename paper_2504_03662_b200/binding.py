@@ -44,7 +44,8 @@ EXPORTS = ("galv_create", "galv_destroy", "galv_strerror", "galv_last_error", "g
            "galv_graph_destroy", "galv_layer_optima", "galv_stage_partition", "galv_add_switch_cost",
            "galv_switch_decision", "galv_skip_estimate", "galv_mx_codes_bytes", "galv_mx_scales_bytes", "galv_mx_pack",
            "galv_mx_unpack", "galv_mx_act_backward", "galv_mx_norm_workspace_bytes", "galv_mx_norm_backward",
-           "galv_mx_weight_grad_workspace_bytes", "galv_mx_weight_grad", "galv_mx_matmul_workspace_bytes", "galv_mx_matmul")
+           "galv_mx_weight_grad_workspace_bytes", "galv_mx_weight_grad", "galv_mx_matmul_workspace_bytes", "galv_mx_matmul",
+           "galv_add_form_cost")
 
 
 class galv_shape(C.Structure):
@@ -90,6 +91,7 @@ def load_library() -> C.CDLL:
     lib.galv_expand_plan.argtypes = [vp, C.c_int32, C.c_int32, vp, vp, vp]
     lib.galv_plan_cost.argtypes = [vp, shp] + [vp] * 8
     lib.galv_add_switch_cost.argtypes = [vp, shp] + [vp] * 7
+    lib.galv_add_form_cost.argtypes = [vp, shp, vp, vp, i64] + [vp] * 8
     lib.galv_switch_decision.argtypes = [vp, C.c_int32, vp, vp, vp, C.c_int32, vp, vp]
     lib.galv_graph_create.argtypes = [vp, shp, vp, vp, i64, vp, vp] + [vp] * 7 + [sz] + [vp] * 6 + [C.POINTER(vp)]
     lib.galv_graph_launch.argtypes = [vp, vp, vp]
@@ -139,8 +141,9 @@ _DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 def _matrix(t):
     """(pointer, row stride in elements) of a 2-D tensor whose rows are contiguous."""
-    assert t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "matrices crossing the boundary have contiguous rows"
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    (rows, cols), (stride, step) = t.shape, t.stride()
+    assert cols <= 1 or step == 1, "matrices crossing the boundary have contiguous rows"
+    return t.data_ptr(), stride if rows > 1 else max(stride, cols)
 
 
 def _ws(t):
@@ -220,6 +223,10 @@ class Galv:
         self._check(self.lib.galv_add_switch_cost(self.h, C.byref(shape), _ptr(L), _ptr(time_q), _ptr(trans_q), _ptr(cur_plan),
                                                   _ptr(horizon), _ptr(time_out), _stream()))
 
+    def galv_add_form_cost(self, shape, L, layers, layer_stride_B, strat, inst, forms, time_s, mem_bytes, time_q, mem_q):
+        self._check(self.lib.galv_add_form_cost(self.h, C.byref(shape), _ptr(L), _ptr(layers), layer_stride_B, _ptr(strat), _ptr(inst),
+                                                _ptr(forms), _ptr(time_s), _ptr(mem_bytes), _ptr(time_q), _ptr(mem_q), _stream()))
+
     def galv_switch_decision(self, B, cur_cost, new_cost, new_status, hysteresis_permille, decision):
         self._check(self.lib.galv_switch_decision(self.h, B, _ptr(cur_cost), _ptr(new_cost), _ptr(new_status),
                                                   int(hysteresis_permille), _ptr(decision), _stream()))
@@ -293,7 +300,7 @@ class Galv:
         return mean.value, lo.value, hi.value, n.value
 
     def _mx_stream(self) -> int:
-        return torch.cuda.current_stream(self.device).cuda_stream
+        return torch._C._cuda_getCurrentRawStream(self.device)
 
     def galv_mx_pack(self, x, fmt, codes, scales):
         p, stride = _matrix(x)

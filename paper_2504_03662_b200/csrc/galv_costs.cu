@@ -24,25 +24,12 @@
 // evaluated once per pair of such classes and written out from a small table.
 
 #include "galv_internal.h"
+#include "galv_quant.cuh"
 
 namespace {
 
 constexpr int kWindow = 8;         // how far back a layer looks for its twin
 constexpr int kThreads = 256;
-
-__device__ __forceinline__ int32_t quant_time(double t_s, double unit_ns) {
-    double q = rint(t_s * 1e9 / unit_ns);
-    if (!(q < 1073741824.0)) q = 1073741824.0;
-    if (q < 0.0) q = 0.0;
-    return (int32_t)q;
-}
-
-__device__ __forceinline__ int32_t quant_mem(double bytes, double bin_bytes) {
-    double q = ceil(bytes / bin_bytes);
-    if (!(q < 1073741824.0)) q = 1073741824.0;
-    if (q < 0.0) q = 0.0;
-    return (int32_t)q;
-}
 
 __device__ __forceinline__ bool pos_finite(double x) { return x > 0.0 && x < INFINITY; }
 __device__ __forceinline__ bool nonneg_finite(double x) { return x >= 0.0 && x < INFINITY; }

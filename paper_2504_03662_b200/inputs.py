@@ -35,6 +35,8 @@ STRATEGY_DESC = np.dtype(
 INST_PARAMS = np.dtype(
     [(n, "<f8") for n in ("b", "act_mult", "flops_rate", "bw_tp", "bw_dp",
                           "bytes_per_elem", "bin_bytes", "time_unit_ns")], align=True)
+FORM_DESC = np.dtype([("keep_bits", "<i4"), ("mul_bits", "<i4"), ("keep_s_per_byte", "<f8"), ("mul_speed", "<f8")], align=True)
+assert FORM_DESC.itemsize == 24
 assert LAYER_DESC.itemsize == 80 and STRATEGY_DESC.itemsize == 32 and INST_PARAMS.itemsize == 64
 
 _GOLDEN = np.uint64(0x9E3779B97F4A7C15)
@@ -85,6 +87,7 @@ class Workload:
     layers: Optional[np.ndarray] = None         # [B or 1][Lmax] LAYER_DESC
     strat: Optional[np.ndarray] = None          # [S] STRATEGY_DESC
     inst: Optional[np.ndarray] = None           # [B] INST_PARAMS
+    forms: Optional[np.ndarray] = None          # [S] FORM_DESC: how strategies keep and multiply (with layers only)
     meta: dict = field(default_factory=dict)
 
     @property
@@ -112,7 +115,17 @@ class Workload:
             layers = pick(layers)
         return Workload(self.name, len(idx), self.Lmax, self.S, self.M, pick(self.L),
                         pick(self.time_q), pick(self.mem_q), pick(self.trans_q),
-                        layers, self.strat, pick(self.inst), dict(self.meta))
+                        layers, self.strat, pick(self.inst), self.forms, dict(self.meta))
+
+    def with_forms(self, forms) -> "Workload":
+        """Every strategy as it is, then every strategy in each of `forms` (rows of FORM_DESC): strategy f * S + s is s in form f."""
+        if not self.has_model:
+            raise ValueError("forms are priced by the cost model: a workload of measured tables has its own times and sizes")
+        rows = np.concatenate([np.array([(0, 0, 0.0, 1.0)], FORM_DESC), np.asarray(forms, FORM_DESC).reshape(-1)])
+        if self.S * len(rows) > 256:
+            raise ValueError(f"{self.S} strategies in {len(rows)} forms: at most 256 in all")
+        return Workload(self.name + "_forms", self.B, self.Lmax, self.S * len(rows), self.M, self.L, layers=self.layers,
+                        strat=np.tile(self.strat, len(rows)), inst=self.inst, forms=np.repeat(rows, self.S), meta=dict(self.meta))
 
 
 # --------------------------------------------------------------------------- random tables

@@ -11,8 +11,7 @@ for each device.
 from __future__ import annotations
 
 import threading
-from dataclasses import dataclass
-from typing import Optional
+from typing import Optional, Union
 
 import torch
 
@@ -20,66 +19,66 @@ from . import binding as gb
 
 ACTS = {"gelu": gb.ACT_GELU, "gelu_tanh": gb.ACT_GELU_TANH, "silu": gb.ACT_SILU}
 NORMS = {"layer": gb.NORM_LAYER, "rms": gb.NORM_RMS}
+_NUMBERS = (torch.float32, torch.bfloat16, torch.float16)
+_SHORT = (torch.bfloat16, torch.float16)
 _local = threading.local()
 
 
-def context(device: torch.device) -> gb.Galv:
+def context(device: Union[int, torch.device]) -> gb.Galv:
     """This thread's library context on a CUDA device."""
-    made = _local.__dict__.setdefault("made", {})
-    index = torch.cuda.current_device() if device.index is None else device.index
-    if index not in made:
+    index = device if isinstance(device, int) else torch.cuda.current_device() if device.index is None else device.index
+    try:
+        return _local.made[index]
+    except (AttributeError, KeyError):
+        made = _local.__dict__.setdefault("made", {})
         made[index] = gb.Galv(index)
-    return made[index]
+        return made[index]
 
 
-@dataclass(frozen=True)
+def codes_bytes(rows: int, cols: int, fmt: int = gb.MX8) -> int:
+    return rows * ((cols + 31) // 32) * 4 * fmt
+
+
+def scales_bytes(rows: int, cols: int, fmt: int = gb.MX8) -> int:
+    nb = (cols + 31) // 32
+    return rows * ((nb + 15) // 16 * 16) if fmt == gb.MX8 else (rows + 127) // 128 * ((nb + 3) // 4) * 512
+
+
 class Packed:
     """A matrix [rows][cols] in blocks of 32 columns: element codes, one scale byte a block."""
-    codes: torch.Tensor
-    scales: torch.Tensor
-    rows: int
-    cols: int
-    fmt: int = gb.MX8
+    __slots__ = ("codes", "scales", "rows", "cols", "fmt")
 
-    def __post_init__(self):
-        for t, n in ((self.codes, codes_bytes(self.rows, self.cols, self.fmt)), (self.scales, scales_bytes(self.rows, self.cols, self.fmt))):
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, fmt: int = gb.MX8):
+        if fmt not in (gb.MX8, gb.MX4):
+            raise ValueError(f"a format is 8 or 4 bits, not {fmt}")
+        for t, n in ((codes, codes_bytes(rows, cols, fmt)), (scales, scales_bytes(rows, cols, fmt))):
             if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() < n:
-                raise ValueError(f"a [{self.rows}][{self.cols}] matrix in {self.fmt} bits takes {n} contiguous bytes, got {t.dtype} {tuple(t.shape)}")
+                raise ValueError(f"a [{rows}][{cols}] matrix in {fmt} bits takes {n} contiguous bytes, got {t.dtype} {tuple(t.shape)}")
+        self.codes, self.scales, self.rows, self.cols, self.fmt = codes, scales, rows, cols, fmt
 
     @property
     def nbytes(self) -> int:
         return self.codes.numel() + self.scales.numel()
 
 
-def codes_bytes(rows: int, cols: int, fmt: int = gb.MX8) -> int:
-    return rows * (-(-cols // 32)) * 4 * fmt
-
-
-def scales_bytes(rows: int, cols: int, fmt: int = gb.MX8) -> int:
-    nb = -(-cols // 32)
-    return rows * (-(-nb // 16) * 16) if fmt == gb.MX8 else -(-rows // 128) * -(-nb // 4) * 512
-
-
-def _on(*tensors: Optional[torch.Tensor]) -> gb.Galv:
-    dev = None
+def _on(*tensors: torch.Tensor) -> gb.Galv:
+    """The context of the device that all tensors lie on."""
+    dev = tensors[0].get_device()
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("microscaled operators take CUDA tensors (no CPU path)")
-        if dev is not None and t.device != dev:
-            raise ValueError(f"tensors on {dev} and {t.device}")
-        dev = t.device
+        if t.get_device() != dev or not t.is_cuda:
+            raise ValueError(f"microscaled operators take CUDA tensors of one device (no CPU path), not {', '.join(str(u.device) for u in tensors)}")
     return context(dev)
 
 
-def _kind(t: torch.Tensor, what: str, dtypes=(torch.float32, torch.bfloat16, torch.float16)):
-    if t.dtype not in dtypes:
-        raise ValueError(f"{what} is one of {', '.join(str(d).replace('torch.', '') for d in dtypes)}, not {t.dtype}")
+def _kind(dtype: torch.dtype, what: str, dtypes=_NUMBERS):
+    if dtype not in dtypes:
+        raise ValueError(f"{what} is one of {', '.join(str(d).replace('torch.', '') for d in dtypes)}, not {dtype}")
 
 
 def _rows(t: torch.Tensor, what: str) -> torch.Tensor:
     """A 2-D tensor whose rows are contiguous and do not overlap (a copy where they are not)."""
+    if t.is_contiguous() and t.dim() == 2:
+        return t
     if t.dim() != 2:
         raise ValueError(f"{what} is a matrix, not of shape {tuple(t.shape)}")
     if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
@@ -87,41 +86,39 @@ def _rows(t: torch.Tensor, what: str) -> torch.Tensor:
     return t
 
 
-def _like(t: torch.Tensor, p: Packed, what: str):
-    if tuple(t.shape) != (p.rows, p.cols):
+def _beside(t: torch.Tensor, p: Packed, what: str):
+    if p.fmt != gb.MX8:
+        raise ValueError("the backward pass reads what was kept in 8 bits")
+    if t.shape[0] != p.rows or t.shape[1] != p.cols:
         raise ValueError(f"{what} of shape {tuple(t.shape)} beside a held matrix [{p.rows}][{p.cols}]")
 
 
-def _eight(p: Packed):
-    if p.fmt != gb.MX8:
-        raise ValueError("the backward pass reads what was kept in 8 bits")
-
-
-def _workspace(nbytes: int, device) -> Optional[torch.Tensor]:
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+def _bytes(n: int, device) -> torch.Tensor:
+    return torch.empty(n, dtype=torch.uint8, device=device)
 
 
 def pack(x: torch.Tensor, fmt: int = gb.MX8) -> Packed:
     """Holds a matrix in blocks of 8- or 4-bit elements."""
-    if fmt not in (gb.MX8, gb.MX4):
+    if fmt != gb.MX8 and fmt != gb.MX4:
         raise ValueError(f"a format is 8 or 4 bits, not {fmt}")
-    _kind(x, "x")
+    _kind(x.dtype, "x")
     x = _rows(x, "x")
     g = _on(x)
     rows, cols = x.shape
     if cols < 1:
         raise ValueError("rows of at least one column")
-    p = Packed(torch.empty(codes_bytes(rows, cols, fmt), dtype=torch.uint8, device=x.device),
-               torch.empty(scales_bytes(rows, cols, fmt), dtype=torch.uint8, device=x.device), rows, cols, fmt)
+    p = Packed.__new__(Packed)
+    p.codes, p.scales = _bytes(codes_bytes(rows, cols, fmt), x.device), _bytes(scales_bytes(rows, cols, fmt), x.device)
+    p.rows, p.cols, p.fmt = rows, cols, fmt
     g.galv_mx_pack(x, fmt, p.codes, p.scales)
     return p
 
 
 def unpack(p: Packed, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """The numbers a packed matrix stands for."""
+    _kind(dtype, "dtype")
     g = _on(p.codes, p.scales)
     x = torch.empty(p.rows, p.cols, dtype=dtype, device=p.codes.device)
-    _kind(x, "dtype")
     g.galv_mx_unpack(p.fmt, p.codes, p.scales, x)
     return x
 
@@ -130,10 +127,9 @@ def act_backward(dy: torch.Tensor, kept: Packed, act: str = "gelu") -> torch.Ten
     """dy * f'(x) for an activation function ("gelu", "gelu_tanh", "silu") whose input x was kept in 8 bits."""
     if act not in ACTS:
         raise ValueError(f"an activation function is one of {', '.join(ACTS)}, not {act!r}")
-    _kind(dy, "dy")
-    _eight(kept)
+    _kind(dy.dtype, "dy")
     dy = _rows(dy, "dy")
-    _like(dy, kept, "dy")
+    _beside(dy, kept, "dy")
     g = _on(dy, kept.codes, kept.scales)
     dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
     g.galv_mx_act_backward(ACTS[act], kept.codes, kept.scales, dy, dx)
@@ -144,40 +140,44 @@ def norm_backward(dy: torch.Tensor, kept: Packed, weight: Optional[torch.Tensor]
     """(dx, dweight, dbias) of a "layer" or "rms" norm over rows whose input was kept in 8 bits; dweight and dbias in fp32, dbias None for "rms"."""
     if kind not in NORMS:
         raise ValueError(f"a norm is one of {', '.join(NORMS)}, not {kind!r}")
-    _kind(dy, "dy")
-    _eight(kept)
+    _kind(dy.dtype, "dy")
     dy = _rows(dy, "dy")
-    _like(dy, kept, "dy")
+    _beside(dy, kept, "dy")
     if weight is not None and (weight.dtype != dy.dtype or tuple(weight.shape) != (kept.cols,)):
         raise ValueError(f"weight is [{kept.cols}] of {dy.dtype}")
-    g = _on(dy, kept.codes, kept.scales, weight)
+    g = _on(dy, kept.codes, kept.scales) if weight is None else _on(dy, kept.codes, kept.scales, weight)
     dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
     dweight = torch.empty(kept.cols, dtype=torch.float32, device=dy.device)
     dbias = torch.empty(kept.cols, dtype=torch.float32, device=dy.device) if kind == "layer" else None
-    ws = _workspace(g.galv_mx_norm_workspace_bytes(kept.rows, kept.cols), dy.device)
-    g.galv_mx_norm_backward(NORMS[kind], eps, kept.codes, kept.scales, dy, None if weight is None else weight.contiguous(), dx, dweight, dbias, ws)
+    n = g.galv_mx_norm_workspace_bytes(kept.rows, kept.cols)
+    g.galv_mx_norm_backward(NORMS[kind], eps, kept.codes, kept.scales, dy, None if weight is None else weight.contiguous(), dx, dweight, dbias,
+                            _bytes(n, dy.device) if n else None)
     return dx, dweight, dbias
 
 
 def weight_grad(dy: torch.Tensor, kept: Packed, dtype: Optional[torch.dtype] = None, base: Optional[torch.Tensor] = None,
                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """base + dy^T x for a linear layer whose input x was kept in 8 bits: [columns of dy][columns of x].  `out` may be `base`."""
-    _kind(dy, "dy", (torch.bfloat16, torch.float16))
-    _eight(kept)
+    _kind(dy.dtype, "dy", _SHORT)
     dy = _rows(dy, "dy")
+    if kept.fmt != gb.MX8:
+        raise ValueError("the backward pass reads what was kept in 8 bits")
     if dy.shape[0] != kept.rows or dy.shape[1] < 1:
         raise ValueError(f"dy of shape {tuple(dy.shape)} beside {kept.rows} kept rows")
     shape = (dy.shape[1], kept.cols)
     dtype = dtype or (out if out is not None else base if base is not None else dy).dtype
-    if dtype not in (dy.dtype, torch.float32):
+    if dtype != dy.dtype and dtype != torch.float32:
         raise ValueError(f"a weight gradient is of {dy.dtype} or float32, not {dtype}")
+    tensors = [dy, kept.codes, kept.scales]
     for t, what in ((base, "base"), (out, "out")):
-        if t is not None and (t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()):
-            raise ValueError(f"{what} is a contiguous {shape} of {dtype}")
-    g = _on(dy, kept.codes, kept.scales, base, out)
+        if t is not None:
+            if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+                raise ValueError(f"{what} is a contiguous {shape} of {dtype}")
+            tensors.append(t)
+    g = _on(*tensors)
     dw = torch.empty(shape, dtype=dtype, device=dy.device) if out is None else out
-    ws = _workspace(g.galv_mx_weight_grad_workspace_bytes(dy, kept.cols), dy.device)
-    g.galv_mx_weight_grad(dy, kept.codes, kept.scales, base, dw, ws)
+    n = g.galv_mx_weight_grad_workspace_bytes(dy, kept.cols)
+    g.galv_mx_weight_grad(dy, kept.codes, kept.scales, base, dw, _bytes(n, dy.device) if n else None)
     return dw
 
 
@@ -187,13 +187,13 @@ def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, bias: Opti
         raise ValueError("a product takes operands held in 4 bits")
     if a.cols != b.cols or b.rows < 1:
         raise ValueError(f"a product of [{a.rows}][{a.cols}] and [{b.rows}][{b.cols}] transposed")
+    _kind(dtype, "dtype")
     if bias is not None and (bias.dtype != dtype or tuple(bias.shape) != (b.rows,)):
         raise ValueError(f"bias is [{b.rows}] of {dtype}")
-    g = _on(a.codes, a.scales, b.codes, b.scales, bias)
+    g = _on(a.codes, a.scales, b.codes, b.scales) if bias is None else _on(a.codes, a.scales, b.codes, b.scales, bias)
     y = torch.empty(a.rows, b.rows, dtype=dtype, device=a.codes.device)
-    _kind(y, "dtype")
-    ws = _workspace(g.galv_mx_matmul_workspace_bytes(a.rows, b.rows, a.cols), y.device)
-    g.galv_mx_matmul(a.cols, a.codes, a.scales, b.codes, b.scales, None if bias is None else bias.contiguous(), y, ws)
+    n = g.galv_mx_matmul_workspace_bytes(a.rows, b.rows, a.cols)
+    g.galv_mx_matmul(a.cols, a.codes, a.scales, b.codes, b.scales, None if bias is None else bias.contiguous(), y, _bytes(n, y.device) if n else None)
     return y
 
 
@@ -234,7 +234,7 @@ class _Linear(torch.autograd.Function):
 def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, four: bool = False) -> torch.Tensor:
     """x weight^T + bias (bf16 or fp16), x kept in 8 bits for the weight's gradient.  `four`: the forward product takes both operands in
     4 bits; the gradients are those of the product of the unrounded operands (straight through the rounding)."""
-    _kind(x, "x", (torch.bfloat16, torch.float16))
+    _kind(x.dtype, "x", _SHORT)
     if weight.dim() != 2 or weight.dtype != x.dtype or weight.shape[1] != x.shape[-1]:
         raise ValueError(f"weight of shape {tuple(weight.shape)} and {weight.dtype} beside x of {tuple(x.shape)} and {x.dtype}")
     return _Linear.apply(x, weight, bias, four)
@@ -265,7 +265,7 @@ def norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[
         raise ValueError(f"a norm is one of {', '.join(NORMS)}, not {kind!r}")
     if kind == "rms" and bias is not None:
         raise ValueError("an rms norm has no bias")
-    _kind(x, "x")
+    _kind(x.dtype, "x")
     return _Norm.apply(x, weight, bias, kind, eps)
 
 
@@ -289,5 +289,5 @@ def activation(x: torch.Tensor, act: str = "gelu") -> torch.Tensor:
     """gelu, gelu_tanh or silu, x kept in 8 bits for the backward pass."""
     if act not in ACTS:
         raise ValueError(f"an activation function is one of {', '.join(ACTS)}, not {act!r}")
-    _kind(x, "x")
+    _kind(x.dtype, "x")
     return _Activation.apply(x, act)

@@ -11,12 +11,50 @@ from typing import Optional
 import numpy as np
 import torch
 
-from . import binding as gb
-from .inputs import Workload
+from . import binding as gb, mx
+from .inputs import FORM_DESC, Workload
 
 
 def _dev_bytes(a: np.ndarray, device) -> torch.Tensor:
     return torch.from_numpy(np.ascontiguousarray(a).view(np.uint8).reshape(-1).copy()).to(device)
+
+
+def _seconds(f, reps: int = 5) -> float:
+    """Shortest time of a call on the current stream, by events, after two calls that are not timed."""
+    best = float("inf")
+    for k in range(reps + 2):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        f()
+        b.record()
+        b.synchronize()
+        if k >= 2:
+            best = min(best, a.elapsed_time(b) * 1e-3)
+    return best
+
+
+def measure_forms(galv: gb.Galv, hidden: int, tokens: int, keep: bool = True, multiply: bool = True) -> np.ndarray:
+    """Forms of strategies (rows of FORM_DESC for Workload.with_forms) with the rates of this device: the hardware profiler's part for the
+    microscaled operators.  A layer's input [tokens][hidden] in bf16 is packed in 8 bits and used for a weight gradient, beside the plain
+    gradient of the 16-bit input; and multiplied in 4 bits (packed in the call), beside the plain product."""
+    dev = torch.device("cuda", galv.device)
+    g = torch.Generator(device=dev).manual_seed(1)
+    x, dy, w = (torch.randn(*s, generator=g, device=dev).to(torch.bfloat16) for s in ((tokens, hidden), (tokens, hidden), (hidden, hidden)))
+    rows = []
+    s_per_byte, speed = 0.0, 1.0
+    with torch.cuda.device(dev):
+        if keep:
+            kept = mx.pack(x)
+            plain = _seconds(lambda: dy.t() @ x)
+            s_per_byte = (_seconds(lambda: mx.pack(x)) + max(0.0, _seconds(lambda: mx.weight_grad(dy, kept)) - plain)) / (x.numel() * 2)
+            rows.append((8, 0, s_per_byte, 1.0))
+        if multiply:
+            w4 = mx.pack(w, gb.MX4)
+            speed = _seconds(lambda: x @ w.t()) / _seconds(lambda: mx.matmul(mx.pack(x, gb.MX4), w4))
+            rows.append((0, 4, 0.0, speed))
+        if keep and multiply:
+            rows.append((8, 4, s_per_byte, speed))
+    return np.array(rows, FORM_DESC)
 
 
 class SearchBuffers:
@@ -45,7 +83,9 @@ class SearchBuffers:
             self.time_q = torch.from_numpy(np.ascontiguousarray(w.time_q, np.int32)).to(dev)
             self.mem_q = torch.from_numpy(np.ascontiguousarray(w.mem_q, np.int32)).to(dev)
             self.trans_q = torch.from_numpy(np.ascontiguousarray(w.trans_q, np.int32)).to(dev)
-        self.time_s = self.mem_bytes = None
+        self.time_s = self.mem_bytes = self.forms = None
+        if w.forms is not None:
+            self.forms = _dev_bytes(w.forms, dev)
         self.C = torch.empty(B, Lm, S, P, **i32) if flags & gb.STORE_C_FULL else None
         self.A = torch.empty(B, Lm, S, P, dtype=torch.uint8, device=dev) if flags & gb.STORE_ARGMIN else None
         self.C_last = torch.empty(B, S, P, **i32)
@@ -58,12 +98,16 @@ class SearchBuffers:
     def eval_costs(self, want_fp64: bool = False):
         w = self.w
         assert w.has_model
+        want_fp64 = want_fp64 or self.forms is not None            # forms are priced from the doubles
         if want_fp64 and self.time_s is None:
             self.time_s = torch.zeros(w.B, w.Lmax, w.S, dtype=torch.float64, device=self.dev)
             self.mem_bytes = torch.zeros(w.B, w.Lmax, w.S, dtype=torch.float64, device=self.dev)
         self.galv.galv_eval_costs(self.shape, self.L, self.layers, self.layer_stride_B, self.strat, self.inst,
                                   self.time_s if want_fp64 else None, self.mem_bytes if want_fp64 else None,
                                   self.time_q, self.mem_q, self.trans_q, self.status)
+        if self.forms is not None:
+            self.galv.galv_add_form_cost(self.shape, self.L, self.layers, self.layer_stride_B, self.strat, self.inst, self.forms,
+                                         self.time_s, self.mem_bytes, self.time_q, self.mem_q)
 
     def dp_search(self):
         self.galv.galv_dp_search(self.shape, self.L, self.time_q, self.mem_q, self.trans_q, self.C, self.A,
@@ -103,6 +147,8 @@ class HostSearch:
     """The host-buffer entry point: pinned host inputs/outputs and a device arena."""
 
     def __init__(self, galv: gb.Galv, w: Workload, flags: int = gb.STORE_C_FULL):
+        if w.forms is not None:
+            raise ValueError("the host entry point prices no forms: use SearchBuffers")
         self.galv, self.w = galv, w
         if w.trans_q is not None and w.trans_q.ndim == 4:          # one transition matrix per layer
             flags |= gb.TRANS_PER_LAYER
