@@ -17,7 +17,7 @@ constexpr int kStageBytes = 2 * kRowsBytes + kScaleA + kScaleB;
 constexpr int kOutBytes = 8 * 2048;
 constexpr int kSmem = 1024 + kStages * kStageBytes + kOutBytes + 256;
 constexpr int kThreads = 384;
-constexpr int kSecond = 208, kShared = kTile - kSecond, kScalesAt = kSecond + kTile;                 // columns of tensor memory
+constexpr int kSecond = 208, kScalesAt = kSecond + kTile;                                            // columns of tensor memory
 constexpr int kGroup = 8;                                 // tiles along m whose rows of a stay in L2 while their n runs
 
 struct MatmulArgs {
@@ -278,7 +278,152 @@ __global__ void __launch_bounds__(256) mx_matmul_join_kernel(long long m, long l
     }
 }
 
-struct MatmulPlan { int tiles_m, tiles_n, splits, chunks, clusters; size_t partial; };
+// ---- few rows of a
+//
+// Up to 64 rows of a: reading b is all there is.  b's rows take the tensor cores' 128 rows and a's the columns (16 to 64 of them), a CTA has 128 rows
+// of b, and the CTAs of a cluster share the summed index, so that about one CTA an SM streams b.  Each sends its sums' slices of a's rows
+// to the CTA of the cluster that has them, which adds them in order: no second kernel, no memory between.  With 8192 x 8192 of b, 7 rows of a take 10.1 us
+// (17.0 in the kernel above and its second one), 64 rows 14.8 (17.2); 128 would take 21.1 (20.0), so they do not come here.
+
+constexpr int kFewThreads = 256;
+template <int N> struct Few {                             // N: rows of a, rounded up
+    static constexpr int stages = 6;
+    static constexpr int rows_b = 128 * kChunkBytes, rows_a = N * kChunkBytes, scales = 1024;
+    static constexpr int stage = rows_b + rows_a + 2 * scales;
+    static constexpr int inbox = N * 128 * 4;
+    static constexpr int smem = 1024 + stages * stage + inbox + 256;
+};
+
+template <typename O, int N>
+__global__ void __launch_bounds__(kFewThreads, 1)
+mx_matmul_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const __grid_constant__ MatmulArgs a)
+{
+    using F = Few<N>;
+    extern __shared__ unsigned char raw[];
+    const uint32_t base = (tc::smem_at(raw) + 1023) & ~1023u;
+    const uint32_t b_at = base, a_at = b_at + F::stages * F::rows_b, sb_at = a_at + F::stages * F::rows_a, sa_at = sb_at + F::stages * F::scales,
+                   inbox = sa_at + F::stages * F::scales, bars = inbox + F::inbox;
+    const uint32_t full = bars, empty = full + 8 * F::stages, acc_full = empty + 8 * F::stages, slot = acc_full + 8;
+    __shared__ int failed;
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, ranks = a.splits;
+    const uint32_t rank = tc::cluster_rank();
+    const int tile = blockIdx.x / ranks, n0 = tile * 128;
+    const int c0 = (int)((long long)rank * a.chunks / ranks), c1 = (int)((long long)(rank + 1) * a.chunks / ranks);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < F::stages; ++s) {
+            tc::bar_init(full + 8 * s, 1);
+            tc::bar_init(empty + 8 * s, 1);
+        }
+        tc::bar_init(acc_full, 1);
+        tc::bar_init_done();
+        failed = 0;
+        tc::prefetch_map(&a_map);
+        tc::prefetch_map(&b_map);
+    }
+    constexpr uint32_t columns = N <= 32 ? 64 : 128, scales_at = N < 32 ? 32 : N;
+    if (warp == 2) tc::tmem_alloc<1>(slot, columns);
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+
+    auto waited = [&](uint32_t bar, uint32_t parity) {
+        if (tc::bar_wait(bar, parity)) return true;
+        *(volatile int*)&failed = 1;
+        return false;
+    };
+
+    if (warp == 0) {
+        if (tc::elect()) {
+            const uint8_t* sb = a.b_scales + (long long)tile * a.groups * 512;
+            int it = 0;
+            for (int c = c0; c < c1; ++c, ++it) {
+                const int s = it % F::stages;
+                const uint32_t bar = full + 8 * s, bytes = min(2, a.groups - 2 * c) * 512;
+                if (!waited(empty + 8 * s, (it / F::stages & 1) ^ 1)) break;
+                tc::bar_expect(bar, F::rows_b + F::rows_a + 2 * bytes);
+                tc::load_2d(b_at + s * F::rows_b, &b_map, c * kChunkBytes, n0, bar);
+                tc::load_2d(a_at + s * F::rows_a, &a_map, c * kChunkBytes, 0, bar);
+                tc::load_bytes(sb_at + s * F::scales, sb + (long long)c * 1024, bytes, bar);
+                tc::load_bytes(sa_at + s * F::scales, a.a_scales + (long long)c * 1024, bytes, bar);
+            }
+            if (*(volatile int*)&failed)                  // copies still in flight
+                for (int i = it < F::stages ? 0 : it - F::stages; i < it; ++i) tc::bar_wait(full + 8 * (i % F::stages), i / F::stages & 1);
+        }
+    } else if (warp == 1) {
+        if (tc::elect()) {
+            constexpr uint32_t what = 1u << 7 | 1u << 10 | (uint32_t)(N >> 3) << 17 | 1u << 23 | (uint32_t)(128 >> 4) << 24;
+            const uint32_t sb = tmem + scales_at, sa = sb + 8;
+            int it = 0;
+            for (int c = c0; c < c1; ++c, ++it) {
+                const int s = it % F::stages;
+                if (!waited(full + 8 * s, it / F::stages & 1)) break;
+                tc::fence_after();
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    tc::copy_scales<1>(sb + g * 4, tc::operand_plain(sb_at + s * F::scales + g * 512));
+                    tc::copy_scales<1>(sa + g * 4, tc::operand_plain(sa_at + s * F::scales + g * 512));
+                }
+                const int steps = min(4, (a.blocks - c * kChunkBlocks + 1) / 2);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < steps) {
+                        const uint32_t pick = (j & 1) * 2;
+                        tc::mma_mx4<1>(tmem, tc::operand(b_at + s * F::rows_b + j * 32, 16, 1024), tc::operand(a_at + s * F::rows_a + j * 32, 16, 1024), what | pick << 4 | pick << 29,
+                                       sb + j / 2 * 4, sa + j / 2 * 4, c > c0 || j > 0);
+                    }
+                tc::mma_commit<1>(empty + 8 * s);
+            }
+            tc::mma_commit<1>(acc_full);                  // also after a wait that ran out: nothing may be in flight when the memory goes
+            tc::bar_wait(acc_full, 0);
+        }
+    }
+    __syncwarp();
+    const int quad = warp - 4, row = quad * 32 + lane, mine = N / ranks;      // a thread has one row of b; this CTA finishes `mine` rows of a
+    bool ok = true;
+    if (warp >= 4) {
+        ok = waited(acc_full, 0);
+        tc::fence_after();
+        if (ok) {
+#pragma unroll 1
+            for (int j = 0; j < N; j += 16) {
+                uint32_t v[16];
+                tc::tmem_load16(tmem + j + ((uint32_t)quad * 32 << 16), v);
+                tc::tmem_wait_load();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int col = j + i, to = col / mine;
+                    const uint32_t at = inbox + (((rank * mine) + col % mine) * 128 + row) * 4;
+                    asm volatile("st.shared::cluster.b32 [%0], %1;" :: "r"(tc::in_cta(at, to)), "r"(v[i]) : "memory");
+                }
+            }
+        }
+    }
+    tc::fence_before();
+    __syncthreads();
+    tc::cluster_sync();                                   // every slice is where it belongs
+    if (warp >= 4 && ok && n0 + row < a.n) {
+        const float b = a.bias ? mx_float(((const O*)a.bias)[n0 + row]) : 0.f;
+        for (int j = 0; j < mine; ++j) {
+            const int col = rank * mine + j;
+            if (col >= a.m) break;
+            float sum = 0.f;
+            for (int r = 0; r < ranks; ++r) {
+                float v;
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(inbox + ((r * mine + j) * 128 + row) * 4));
+                sum = r ? sum + v : v;
+            }
+            ((O*)a.y)[col * a.stride + n0 + row] = mx_round<O>(a.bias ? sum + b : sum);
+        }
+    }
+    if (threadIdx.x == 0 && failed) atomicAdd(&g_timeouts, 1u);
+    if (warp == 2) tc::tmem_free<1>(tmem, columns);
+}
+
+struct MatmulPlan { int few, tiles_m, tiles_n, splits, chunks, clusters; size_t partial; };
 
 MatmulPlan plan_of(const galv_ctx* ctx, int64_t m, int64_t n, int64_t k)
 {
@@ -287,6 +432,16 @@ MatmulPlan plan_of(const galv_ctx* ctx, int64_t m, int64_t n, int64_t k)
     p.tiles_m = (int)((m + kTile - 1) / kTile);
     p.tiles_n = (int)((n + kTile - 1) / kTile);
     p.chunks = (int)((mx_blocks(k) + kChunkBlocks - 1) / kChunkBlocks);
+    p.few = m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 0;
+    if (p.few) {                                          // clusters along the summed index, two chunks a CTA at least
+        p.tiles_m = 1;
+        p.tiles_n = (int)((n + 127) / 128);
+        p.splits = 1;
+        while (p.splits < 8 && (int64_t)p.tiles_n * p.splits * 2 <= ctx->num_sms && p.chunks >= p.splits * 4) p.splits *= 2;
+        p.clusters = p.tiles_n;
+        p.partial = 0;
+        return p;
+    }
     const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
     p.splits = 1;
     if (tiles < most && p.chunks >= 8) {
@@ -299,9 +454,31 @@ MatmulPlan plan_of(const galv_ctx* ctx, int64_t m, int64_t n, int64_t k)
     return p;
 }
 
+template <typename O, int N>
+cudaError_t launch_few(const MatmulPlan& p, const CUtensorMap& am, const CUtensorMap& bm, const MatmulArgs& a, cudaStream_t st)
+{
+    cudaError_t e = cudaFuncSetAttribute(mx_matmul_few_kernel<O, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, Few<N>::smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(p.tiles_n * p.splits));
+    cfg.blockDim = dim3(kFewThreads);
+    cfg.dynamicSmemBytes = Few<N>::smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)p.splits;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, mx_matmul_few_kernel<O, N>, am, bm, a);
+}
+
 template <typename O>
 cudaError_t launch(const MatmulPlan& p, const CUtensorMap& am, const CUtensorMap& bm, const MatmulArgs& a, cudaStream_t st)
 {
+    if (p.few == 16) return launch_few<O, 16>(p, am, bm, a, st);
+    if (p.few == 32) return launch_few<O, 32>(p, am, bm, a, st);
+    if (p.few == 64) return launch_few<O, 64>(p, am, bm, a, st);
     cudaError_t e = cudaFuncSetAttribute(mx_matmul_kernel<O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
     mx_matmul_kernel<O><<<p.clusters * 2, kThreads, kSmem, st>>>(am, bm, a);
@@ -335,7 +512,7 @@ extern "C" int galv_mx_matmul(galv_ctx* ctx, int64_t m, int64_t n, int64_t k, co
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
     CUtensorMap am, bm;
     const uint64_t pitch = mx_blocks(k) * 16;
-    cudaError_t e = galv_mx_map(&am, CU_TENSOR_MAP_DATA_TYPE_UINT8, a_codes, m, pitch, pitch, kHalf, kChunkBytes, true);
+    cudaError_t e = galv_mx_map(&am, CU_TENSOR_MAP_DATA_TYPE_UINT8, a_codes, m, pitch, pitch, p.few ? p.few : kHalf, kChunkBytes, true);
     if (e == cudaSuccess) e = galv_mx_map(&bm, CU_TENSOR_MAP_DATA_TYPE_UINT8, b_codes, n, pitch, pitch, kHalf, kChunkBytes, true);
     if (e != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, "galv_mx_matmul: tensor map");
     MatmulArgs a;
