@@ -18,7 +18,7 @@ constexpr int kOutBytes = 8 * 2048;
 constexpr int kSmem = 1024 + kStages * kStageBytes + kOutBytes + 256;
 constexpr int kThreads = 384;
 constexpr int kSecond = 208, kScalesAt = kSecond + kTile;                                            // columns of tensor memory
-constexpr int kGroup = 8;                                 // tiles along m whose rows of a stay in L2 while their n runs
+constexpr int kGroup = 16;                                // tiles along m whose rows of a stay in L2 while their n runs
 
 struct MatmulArgs {
     long long m, n, stride;
