@@ -141,13 +141,21 @@ _DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 def _matrix(t):
     """(pointer, row stride in elements) of a 2-D tensor whose rows are contiguous."""
-    (rows, cols), (stride, step) = t.shape, t.stride()
-    assert cols <= 1 or step == 1, "matrices crossing the boundary have contiguous rows"
-    return t.data_ptr(), stride if rows > 1 else max(stride, cols)
+    stride, step = t.stride()
+    assert step == 1 or t.shape[1] <= 1, "matrices crossing the boundary have contiguous rows"
+    return t.data_ptr(), max(stride, t.shape[1]) if t.shape[0] <= 1 else stride
 
 
 def _ws(t):
     return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _raw_stream(device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def make_shape(B: int, Lmax: int, S: int, M: int, flags: int = STORE_C_FULL, m_pitch: Optional[int] = None) -> galv_shape:
@@ -299,44 +307,48 @@ class Galv:
         self._check(self.lib.galv_layer_loop_ms_stats(self.h, C.byref(mean), C.byref(lo), C.byref(hi), C.byref(n)))
         return mean.value, lo.value, hi.value, n.value
 
-    def _mx_stream(self) -> int:
-        return torch._C._cuda_getCurrentRawStream(self.device)
+    # Microscaled operators: matrices are 2-D tensors with contiguous rows, codes and scales uint8 tensors; on the current stream of the
+    # context's device.  These calls are short, so the pointers are taken without the checks of _ptr (mx.py has made its own).
 
     def galv_mx_pack(self, x, fmt, codes, scales):
-        p, stride = _matrix(x)
-        self._check(self.lib.galv_mx_pack(self.h, x.shape[0], x.shape[1], p, stride, _DTYPES[x.dtype], fmt, _ptr(codes), _ptr(scales),
-                                          self._mx_stream()))
+        rc = self.lib.galv_mx_pack(self.h, *x.shape, *_matrix(x), _DTYPES[x.dtype], fmt, codes.data_ptr(), scales.data_ptr(), _raw_stream(self.device))
+        if rc:
+            self._check(rc)
 
     def galv_mx_unpack(self, fmt, codes, scales, x):
-        p, stride = _matrix(x)
-        self._check(self.lib.galv_mx_unpack(self.h, x.shape[0], x.shape[1], fmt, _ptr(codes), _ptr(scales), p, stride, _DTYPES[x.dtype],
-                                            self._mx_stream()))
+        rc = self.lib.galv_mx_unpack(self.h, *x.shape, fmt, codes.data_ptr(), scales.data_ptr(), *_matrix(x), _DTYPES[x.dtype], _raw_stream(self.device))
+        if rc:
+            self._check(rc)
 
     def galv_mx_act_backward(self, act, codes, scales, dy, dx):
-        (p, ps), (q, qs) = _matrix(dy), _matrix(dx)
-        self._check(self.lib.galv_mx_act_backward(self.h, dy.shape[0], dy.shape[1], act, _ptr(codes), _ptr(scales), p, ps, q, qs,
-                                                  _DTYPES[dy.dtype], self._mx_stream()))
+        rc = self.lib.galv_mx_act_backward(self.h, *dy.shape, act, codes.data_ptr(), scales.data_ptr(), *_matrix(dy), *_matrix(dx), _DTYPES[dy.dtype],
+                                           _raw_stream(self.device))
+        if rc:
+            self._check(rc)
 
     def galv_mx_norm_workspace_bytes(self, rows, cols) -> int:
-        return int(self.lib.galv_mx_norm_workspace_bytes(self.h, rows, cols))
+        return self.lib.galv_mx_norm_workspace_bytes(self.h, rows, cols)
 
     def galv_mx_norm_backward(self, kind, eps, codes, scales, dy, weight, dx, dweight, dbias, workspace):
-        (p, ps), (q, qs) = _matrix(dy), _matrix(dx)
-        self._check(self.lib.galv_mx_norm_backward(self.h, dy.shape[0], dy.shape[1], kind, eps, _ptr(codes), _ptr(scales), p, ps, _ptr(weight),
-                                                   q, qs, _DTYPES[dy.dtype], _ptr(dweight), _ptr(dbias), *_ws(workspace), self._mx_stream()))
+        rc = self.lib.galv_mx_norm_backward(self.h, *dy.shape, kind, eps, codes.data_ptr(), scales.data_ptr(), *_matrix(dy), _at(weight), *_matrix(dx),
+                                            _DTYPES[dy.dtype], _at(dweight), _at(dbias), *_ws(workspace), _raw_stream(self.device))
+        if rc:
+            self._check(rc)
 
     def galv_mx_weight_grad_workspace_bytes(self, dy, k) -> int:
-        return int(self.lib.galv_mx_weight_grad_workspace_bytes(self.h, dy.shape[0], dy.shape[1], k, *_matrix(dy)))
+        return self.lib.galv_mx_weight_grad_workspace_bytes(self.h, *dy.shape, k, *_matrix(dy))
 
     def galv_mx_weight_grad(self, dy, codes, scales, base, dw, workspace):
-        p, ps = _matrix(dy)
-        self._check(self.lib.galv_mx_weight_grad(self.h, dy.shape[0], dy.shape[1], dw.shape[1], p, ps, _DTYPES[dy.dtype], _ptr(codes), _ptr(scales),
-                                                 _ptr(base), _ptr(dw), _DTYPES[dw.dtype], *_ws(workspace), self._mx_stream()))
+        rc = self.lib.galv_mx_weight_grad(self.h, *dy.shape, dw.shape[1], *_matrix(dy), _DTYPES[dy.dtype], codes.data_ptr(), scales.data_ptr(), _at(base),
+                                          dw.data_ptr(), _DTYPES[dw.dtype], *_ws(workspace), _raw_stream(self.device))
+        if rc:
+            self._check(rc)
 
     def galv_mx_matmul_workspace_bytes(self, m, n, k) -> int:
-        return int(self.lib.galv_mx_matmul_workspace_bytes(self.h, m, n, k))
+        return self.lib.galv_mx_matmul_workspace_bytes(self.h, m, n, k)
 
     def galv_mx_matmul(self, k, a_codes, a_scales, b_codes, b_scales, bias, y, workspace):
-        p, ps = _matrix(y)
-        self._check(self.lib.galv_mx_matmul(self.h, y.shape[0], y.shape[1], k, _ptr(a_codes), _ptr(a_scales), _ptr(b_codes), _ptr(b_scales), _ptr(bias),
-                                            p, ps, _DTYPES[y.dtype], *_ws(workspace), self._mx_stream()))
+        rc = self.lib.galv_mx_matmul(self.h, *y.shape, k, a_codes.data_ptr(), a_scales.data_ptr(), b_codes.data_ptr(), b_scales.data_ptr(), _at(bias),
+                                     *_matrix(y), _DTYPES[y.dtype], *_ws(workspace), _raw_stream(self.device))
+        if rc:
+            self._check(rc)

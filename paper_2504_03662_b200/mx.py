@@ -49,11 +49,13 @@ class Packed:
     __slots__ = ("codes", "scales", "rows", "cols", "fmt")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, fmt: int = gb.MX8):
-        if fmt not in (gb.MX8, gb.MX4):
+        if fmt != gb.MX8 and fmt != gb.MX4:
             raise ValueError(f"a format is 8 or 4 bits, not {fmt}")
-        for t, n in ((codes, codes_bytes(rows, cols, fmt)), (scales, scales_bytes(rows, cols, fmt))):
-            if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() < n:
-                raise ValueError(f"a [{rows}][{cols}] matrix in {fmt} bits takes {n} contiguous bytes, got {t.dtype} {tuple(t.shape)}")
+        if rows < 0 or cols < 1:
+            raise ValueError(f"no matrix of {rows} rows and {cols} columns")
+        nc, ns = codes_bytes(rows, cols, fmt), scales_bytes(rows, cols, fmt)
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.numel() < nc or scales.numel() < ns or not codes.is_contiguous() or not scales.is_contiguous():
+            raise ValueError(f"a [{rows}][{cols}] matrix in {fmt} bits takes {nc} and {ns} contiguous bytes, got {codes.dtype} {tuple(codes.shape)} and {scales.dtype} {tuple(scales.shape)}")
         self.codes, self.scales, self.rows, self.cols, self.fmt = codes, scales, rows, cols, fmt
 
     @property
