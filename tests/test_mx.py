@@ -277,6 +277,35 @@ def test_act_backward(rows, cols, pad, dtype, act):
 
 @gpu
 @pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("dtype,pad", [("bf16", 0), ("f16", 3)])
+def test_act_backward_of_large_matrices(dtype, pad, act):
+    """Sizes at which slopes are looked up, powers of two inside and outside the table; the slope in 64 bits by torch on the device."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rows, cols = 4000, 8200
+    x = torch.randn(rows, cols, generator=g, device="cuda") * torch.exp2(torch.arange(rows, device="cuda").remainder(61).float() - 40)[:, None]
+    kept = mx.pack(x)
+    v = mx.unpack(kept, torch.float32).double()
+    wide = torch.randn(rows, cols + pad, generator=g, device="cuda").to(DT[dtype])
+    dy = wide[:, :cols]
+    if act == "silu":
+        s = torch.sigmoid(v)
+        slope64 = s * (1 + v * (1 - s))
+    elif act == "gelu":
+        slope64 = torch.special.ndtr(v) + v * torch.exp(-v * v / 2) / np.sqrt(2 * np.pi)
+    else:
+        k = np.sqrt(2 / np.pi)
+        c = v.clamp(-50, 50)
+        t = torch.tanh(k * (c + 0.044715 * c ** 3))
+        slope64 = 0.5 * (1 + t) + 0.5 * c * (1 - t * t) * k * (1 + 3 * 0.044715 * c * c)
+    want = dy.double() * slope64
+    f = torch.finfo(DT[dtype])
+    tol = dy.double().abs() * 21 * HALF + torch.maximum(want.abs() * f.eps / 2, torch.tensor(f.smallest_normal * f.eps / 2, device="cuda", dtype=torch.float64))
+    off = (mx.act_backward(dy, kept, act).double() - want).abs()
+    assert (off <= tol).all(), (off - tol).max()
+
+
+@gpu
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
 def test_act_backward_far_out(act):
     x = torch.tensor([[0.0, 1e-30, -1e-30, 5.0, -5.0, 12.0, -12.0, 90.0, -90.0, 1e4, -1e4, 1e18, -1e18, 1e30, -1e30, 3e38, -3e38]]).repeat_interleave(32, 1)
     kept, v = packed(x, 8)
