@@ -105,6 +105,7 @@ int galv_create(galv_ctx** out, int device_ordinal)
     ctx->profiling = 0;
     ctx->prof_count = 0;
     ctx->plan_valid = 0;
+    ctx->mx_timeouts = 0;
     for (auto& ev : ctx->pev) ev = nullptr;
     int cur = -1;
     cudaGetDevice(&cur);

@@ -70,6 +70,7 @@ struct galv_ctx {
     galv_shape plan_shape;     // the resident kernel's plan for the shape of the last search
     RsPlan plans[2];
     int plan_launches, plan_valid;
+    unsigned mx_timeouts;      // waits of microscaled products that had run out when galv_mx_status last looked
     char err[512];
 };
 

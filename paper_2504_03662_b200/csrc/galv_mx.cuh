@@ -73,12 +73,12 @@ struct MxSpread {
     }
     int grid() const { return (int)(blocks < (1ll << 30) ? blocks : (1ll << 30)); }
 };
-struct MxPlace { int row, c; };
+struct MxPlace { unsigned row, c; };                      // either may pass the matrix by what a CTA has: up to 2^31 + 1024 rows, 8 * (2^28 + 1024) columns
 __device__ __forceinline__ MxPlace mx_place(const MxSpread& s, long long block)
 {
-    const int rows = (int)(block / s.segs), seg = (int)(block - (long long)rows * s.segs);
+    const unsigned rows = (unsigned)(block / s.segs), seg = (unsigned)(block - (long long)rows * s.segs);
     MxPlace p;
-    p.row = (int)((s.dr ? (long long)rows * s.each * s.dr : rows) + (threadIdx.x >> s.log));      // may pass the last row by a CTA's rows: galv.h's limit leaves room
+    p.row = (s.dr ? rows * s.each * s.dr : rows) + (threadIdx.x >> s.log);
     p.c = seg * s.each * kMxThreads + (threadIdx.x & ((1 << s.log) - 1));
     return p;
 }
@@ -207,14 +207,14 @@ template <typename T>
 struct MxPlaces {
     T* x;
     long long stride;
-    int row0, c0, log, rows, cols;
-    __device__ __forceinline__ MxPlaces(T* x_, long long stride_, const MxSpread& s, const MxPlace& at, int h, int rows_, int cols_)
-        : x(x_), stride(stride_), row0(at.row - (int)(threadIdx.x >> s.log) + h * s.dr), c0(at.c - (int)(threadIdx.x & ((1 << s.log) - 1)) + h * s.dc), log(s.log), rows(rows_), cols(cols_) {}
+    unsigned row0, c0, log, rows, cols;
+    __device__ __forceinline__ MxPlaces(T* x_, long long stride_, const MxSpread& s, const MxPlace& at, int h, unsigned rows_, unsigned cols_)
+        : x(x_), stride(stride_), row0(at.row - (threadIdx.x >> s.log) + h * s.dr), c0(at.c - (threadIdx.x & ((1 << s.log) - 1)) + h * s.dc), log(s.log), rows(rows_), cols(cols_) {}
     __device__ __forceinline__ T* operator()(int l, int& n) const
     {
-        const int t = (threadIdx.x & ~31) + l, row = row0 + (t >> log), c = (c0 + (t & ((1 << log) - 1))) * 8;
-        n = row < rows ? min(8, cols - c) : 0;
-        return x + (row * stride + c);
+        const unsigned t = (threadIdx.x & ~31) + l, row = row0 + (t >> log), c = (c0 + (t & ((1 << log) - 1))) * 8;
+        n = row < rows && c < cols ? (int)min(8u, cols - c) : 0;
+        return x + ((long long)row * stride + c);
     }
 };
 
@@ -291,7 +291,7 @@ __device__ __forceinline__ void mx_from4(uint32_t w, float (&v)[8])
 
 // Where the scale byte of (row, block) lies.
 template <int FMT>
-__device__ __forceinline__ long long mx_scale_at(int row, int b, int per_row)      // per_row: bytes a row (MX8), tiles a row of tiles (MX4)
+__device__ __forceinline__ long long mx_scale_at(unsigned row, unsigned b, int per_row)      // per_row: bytes a row (MX8), tiles a row of tiles (MX4)
 {
     if (FMT == GALV_MX8) return (long long)row * per_row + b;
     return ((long long)(row >> 7) * per_row + (b >> 2)) * 512 + ((row & 31) * 16 + ((row >> 5) & 3) * 4 + (b & 3));
@@ -314,6 +314,9 @@ __device__ __forceinline__ void mx_restore8(const uint8_t* __restrict__ codes, c
         else if ((dtype) == GALV_BF16) { using T = __nv_bfloat16; __VA_ARGS__; }                                      \
         else { using T = __half; __VA_ARGS__; }                                                                       \
     } while (0)
+
+// CTAs of weight gradients that have given up a wait, copied on the stream.
+cudaError_t galv_mx_wgrad_timeouts(unsigned* count, cudaStream_t st);
 
 // Tensor map of a matrix [rows][cols] whose rows are `pitch` bytes apart, read in boxes [box_rows][box_cols]; swizzle: rows of 128 bytes, their
 // 16-byte pieces exchanged by row % 8.

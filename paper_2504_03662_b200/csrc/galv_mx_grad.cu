@@ -50,7 +50,7 @@ __device__ __forceinline__ float act_slope(float x)
 constexpr int kTableFirst = 127 - 22, kTableScales = 32, kTableBytes = kTableScales * 256 * 4;
 
 template <typename T, int ACT, bool VEC, bool TABLE>
-__global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread spread, int rows, int cols, int nb, int pieces, int per_row,
+__global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread spread, unsigned rows, int cols, int nb, unsigned pieces, int per_row,
                                                             const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const T* dy,
                                                             long long dy_stride, T* dx, long long dx_stride)
 {
@@ -77,11 +77,11 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
         const uint8_t* power = scales + ((long long)at.row * per_row + (at.c >> 2));
 #pragma unroll
         for (int h = 0; h < U; ++h) {
-            const int row = at.row + h * spread.dr, c = at.c + h * spread.dc;
+            const unsigned row = at.row + h * spread.dr, c = at.c + h * spread.dc;
             if (row < rows && c < pieces) {
                 code[h] = __ldg(reinterpret_cast<const uint2*>(held));
                 byte[h] = __ldg(power);
-                raw[h] = mx_fetch8<T, VEC>(from, c * 8, cols);
+                raw[h] = mx_fetch8<T, VEC>(from, (int)c * 8, cols);
             } else if (!VEC) {
                 code[h] = make_uint2(0, 0);
                 byte[h] = 0;
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
         T* to = dx + at.row * dx_stride;
 #pragma unroll
         for (int h = 0; h < U; ++h, to += spread.dr * dx_stride) {
-            const int row = at.row + h * spread.dr, c = at.c + h * spread.dc;
+            const unsigned row = at.row + h * spread.dr, c = at.c + h * spread.dc;
             if (VEC && (row >= rows || c >= pieces)) continue;
             float x[8], g[8];
             mx_floats(raw[h], g);
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
 #pragma unroll
                 for (int i = 0; i < 8; ++i) g[i] *= act_slope<ACT>(x[i] * s);
             }
-            if (VEC) mx_store8<T, true>(to, c * 8, cols, g);
+            if (VEC) mx_store8<T, true>(to, (int)c * 8, cols, g);
             else mx_scatter8<T>(buf[threadIdx.x / 32], MxPlaces<T>(dx, dx_stride, spread, at, h, rows, cols), g);
         }
     }
@@ -641,13 +641,13 @@ extern "C" int galv_mx_act_backward(galv_ctx* ctx, int64_t rows, int64_t cols, i
     const bool vec = mx_rows16(dy, dy_stride, dtype) && mx_rows16(dx, dx_stride, dtype);
     const MxSpread spread(rows, pieces, dtype == GALV_F32 ? MxEach<float>::count : MxEach<__half>::count);
     // A table pays for 16-bit numbers (fp32 is at the memory's rate without) where each CTA has four rounds or more: 4096 x 32768 in bf16 takes 123 us with
-    // it and 153 without for gelu, 119 and 130 for gelu_tanh; 115 without and 118 with for silu, which goes without.
-    const long long resident = (long long)ctx->num_sms * 6;
+    // it and 153 without for gelu, 120 and 130 for gelu_tanh; 115 without and 118 with for silu, which goes without.  Four CTAs fit an SM.
+    const long long resident = (long long)ctx->num_sms * 4;
     const bool table = dtype != GALV_F32 && act != GALV_ACT_SILU && spread.blocks >= 4 * resident;
     const int grid = table ? (int)resident : spread.grid();
     cudaStream_t st = (cudaStream_t)stream;
 #define MX_ACT_START(ACT, VEC, TABLE, SMEM) \
-    mx_act_kernel<T, ACT, VEC, TABLE><<<grid, kMxThreads, SMEM, st>>>(spread, (int)rows, (int)cols, nb, pieces, pitch, codes, scales, (const T*)dy, dy_stride, (T*)dx, dx_stride)
+    mx_act_kernel<T, ACT, VEC, TABLE><<<grid, kMxThreads, SMEM, st>>>(spread, (unsigned)rows, (int)cols, nb, pieces, pitch, codes, scales, (const T*)dy, dy_stride, (T*)dx, dx_stride)
 #define MX_ACT(ACT)                                                                                                          \
     MX_DISPATCH_TYPE(dtype,                                                                                                  \
         constexpr bool can = sizeof(T) == 2 && ACT != GALV_ACT_SILU;                                                                            \

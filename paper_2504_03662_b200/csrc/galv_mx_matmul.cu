@@ -525,3 +525,18 @@ extern "C" int galv_mx_matmul(galv_ctx* ctx, int64_t m, int64_t n, int64_t k, co
     MX_DISPATCH_TYPE(dtype, e = launch<T>(p, am, bm, a, (cudaStream_t)stream));
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
+
+extern "C" int galv_mx_status(galv_ctx* ctx, void* stream)
+{
+    if (!ctx) return GALV_ERR_INVALID_ARG;
+    MxDevice dev(ctx);
+    if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
+    unsigned mine = 0, other = 0;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&mine, g_timeouts, sizeof(mine), 0, cudaMemcpyDeviceToHost, (cudaStream_t)stream);
+    if (e == cudaSuccess) e = galv_mx_wgrad_timeouts(&other, (cudaStream_t)stream);
+    if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
+    if (e != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
+    const bool more = mine + other != ctx->mx_timeouts;
+    ctx->mx_timeouts = mine + other;
+    return more ? galv_set_error(ctx, GALV_ERR_TIMEOUT, "galv_mx_status: a bounded wait of a microscaled product ran out") : GALV_OK;
+}

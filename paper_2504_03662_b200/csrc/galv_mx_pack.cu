@@ -9,7 +9,7 @@ namespace {
 
 // Rows up to rows_out and pieces up to `pieces` have a scale byte to write; rows and nb * 4 pieces lie in the matrix.
 template <typename T, int FMT, bool VEC>
-__global__ void __launch_bounds__(kMxThreads) mx_pack_kernel(const MxSpread spread, int rows, int rows_out, int cols, int nb, int pieces, int per_row,
+__global__ void __launch_bounds__(kMxThreads) mx_pack_kernel(const MxSpread spread, unsigned rows, unsigned rows_out, int cols, unsigned nb, unsigned pieces, int per_row,
                                                              const T* __restrict__ x, long long stride, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales)
 {
     for (long long block = blockIdx.x; block < spread.blocks; block += gridDim.x) {
@@ -20,9 +20,9 @@ __global__ void __launch_bounds__(kMxThreads) mx_pack_kernel(const MxSpread spre
         uint8_t* to = codes + ((long long)at.row * nb * 4 + at.c) * FMT;
 #pragma unroll
         for (int h = 0; h < U; ++h, from += spread.dr * stride) {
-            const int row = at.row + h * spread.dr, c = at.c + h * spread.dc;
+            const unsigned row = at.row + h * spread.dr, c = at.c + h * spread.dc;
             if (row < rows && c < nb * 4) {
-                raw[h] = mx_fetch8<T, VEC>(from, c * 8, cols);
+                raw[h] = mx_fetch8<T, VEC>(from, (int)c * 8, cols);
             } else {
 #pragma unroll
                 for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[h].q[i] = make_uint4(0, 0, 0, 0);
@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_pack_kernel(const MxSpread spre
         }
 #pragma unroll
         for (int h = 0; h < U; ++h, to += ((long long)spread.dr * nb * 4 + spread.dc) * FMT) {
-            const int row = at.row + h * spread.dr, c = at.c + h * spread.dc;
+            const unsigned row = at.row + h * spread.dr, c = at.c + h * spread.dc;
             uint32_t m = mx_most<T>(raw[h]);
             m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));            // the four threads of a block lie next to one another
             m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_pack_kernel(const MxSpread spre
 }
 
 template <typename T, int FMT, bool VEC>
-__global__ void __launch_bounds__(kMxThreads) mx_unpack_kernel(const MxSpread spread, int rows, int cols, int nb, int pieces, int per_row,
+__global__ void __launch_bounds__(kMxThreads) mx_unpack_kernel(const MxSpread spread, unsigned rows, int cols, unsigned nb, unsigned pieces, int per_row,
                                                                const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ x, long long stride)
 {
     __shared__ __align__(16) T buf[VEC ? 1 : kMxThreads / 32][256];
@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_unpack_kernel(const MxSpread sp
         const uint8_t* held = codes + ((long long)at.row * nb * 4 + at.c) * FMT;
 #pragma unroll
         for (int h = 0; h < U; ++h, held += ((long long)spread.dr * nb * 4 + spread.dc) * FMT) {
-            const int row = at.row + h * spread.dr, c = at.c + h * spread.dc;
+            const unsigned row = at.row + h * spread.dr, c = at.c + h * spread.dc;
             if (row < rows && c < pieces) {
                 if (FMT == GALV_MX8) code[h] = __ldg(reinterpret_cast<const uint2*>(held));
                 else code[h].x = __ldg(reinterpret_cast<const uint32_t*>(held));
@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_unpack_kernel(const MxSpread sp
         T* to = x + at.row * stride;
 #pragma unroll
         for (int h = 0; h < U; ++h, to += spread.dr * stride) {
-            const int row = at.row + h * spread.dr, c = at.c + h * spread.dc;
+            const unsigned row = at.row + h * spread.dr, c = at.c + h * spread.dc;
             const bool in = row < rows && c < pieces;
             if (VEC && !in) continue;
             if (!VEC && !in) { code[h] = make_uint2(0, 0); byte[h] = 0; }
@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_unpack_kernel(const MxSpread sp
             const float s = mx_scale(byte[h]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = mx_held<T>(v[i] * s);
-            if (VEC) mx_store8<T, true>(to, c * 8, cols, v);
+            if (VEC) mx_store8<T, true>(to, (int)c * 8, cols, v);
             else mx_scatter8<T>(buf[threadIdx.x / 32], MxPlaces<T>(x, stride, spread, at, h, rows, cols), v);
         }
     }
@@ -128,14 +128,15 @@ extern "C" int galv_mx_pack(galv_ctx* ctx, int64_t rows, int64_t cols, const voi
     const int nb = (int)mx_blocks(cols);
     const bool vec = mx_rows16(x, x_stride, dtype);
     // every scale byte is written, those behind the rows and blocks too
-    const int rows_out = (int)(fmt == GALV_MX8 ? rows : (rows + 127) / 128 * 128), per_row = fmt == GALV_MX8 ? (int)mx_pitch8(cols) : (nb + 3) / 4;
+    const unsigned rows_out = (unsigned)(fmt == GALV_MX8 ? rows : (rows + 127) / 128 * 128);
+    const int per_row = fmt == GALV_MX8 ? (int)mx_pitch8(cols) : (nb + 3) / 4;
     const int pieces = fmt == GALV_MX8 ? per_row * 4 : per_row * 16;
     const MxSpread spread(rows_out, pieces, dtype == GALV_F32 ? MxEach<float>::count : MxEach<__half>::count);
     const int grid = spread.grid();
     cudaStream_t st = (cudaStream_t)stream;
 #define MX_PACK(FMT)                                                                                                                                         \
-    MX_DISPATCH_TYPE(dtype, if (vec) mx_pack_kernel<T, FMT, true><<<grid, kMxThreads, 0, st>>>(spread, (int)rows, rows_out, (int)cols, nb, pieces, per_row, (const T*)x, x_stride, codes, scales); \
-                     else mx_pack_kernel<T, FMT, false><<<grid, kMxThreads, 0, st>>>(spread, (int)rows, rows_out, (int)cols, nb, pieces, per_row, (const T*)x, x_stride, codes, scales))
+    MX_DISPATCH_TYPE(dtype, if (vec) mx_pack_kernel<T, FMT, true><<<grid, kMxThreads, 0, st>>>(spread, (unsigned)rows, rows_out, (int)cols, nb, pieces, per_row, (const T*)x, x_stride, codes, scales); \
+                     else mx_pack_kernel<T, FMT, false><<<grid, kMxThreads, 0, st>>>(spread, (unsigned)rows, rows_out, (int)cols, nb, pieces, per_row, (const T*)x, x_stride, codes, scales))
     if (fmt == GALV_MX8) MX_PACK(GALV_MX8);
     else MX_PACK(GALV_MX4);
 #undef MX_PACK
@@ -161,8 +162,8 @@ extern "C" int galv_mx_unpack(galv_ctx* ctx, int64_t rows, int64_t cols, int32_t
     const int grid = spread.grid();
     cudaStream_t st = (cudaStream_t)stream;
 #define MX_UNPACK(FMT)                                                                                                                         \
-    MX_DISPATCH_TYPE(dtype, if (vec) mx_unpack_kernel<T, FMT, true><<<grid, kMxThreads, 0, st>>>(spread, (int)rows, (int)cols, nb, pieces, per_row, codes, scales, (T*)x, x_stride); \
-                     else mx_unpack_kernel<T, FMT, false><<<grid, kMxThreads, 0, st>>>(spread, (int)rows, (int)cols, nb, pieces, per_row, codes, scales, (T*)x, x_stride))
+    MX_DISPATCH_TYPE(dtype, if (vec) mx_unpack_kernel<T, FMT, true><<<grid, kMxThreads, 0, st>>>(spread, (unsigned)rows, (int)cols, nb, pieces, per_row, codes, scales, (T*)x, x_stride); \
+                     else mx_unpack_kernel<T, FMT, false><<<grid, kMxThreads, 0, st>>>(spread, (unsigned)rows, (int)cols, nb, pieces, per_row, codes, scales, (T*)x, x_stride))
     if (fmt == GALV_MX8) MX_UNPACK(GALV_MX8);
     else MX_UNPACK(GALV_MX4);
 #undef MX_UNPACK

@@ -504,6 +504,9 @@ WgradPlan plan_of(const galv_ctx* ctx, int64_t tokens, int64_t n, int64_t k, con
 template <typename T, typename O>
 cudaError_t launch(const WgradPlan& p, const CUtensorMap& dy, const CUtensorMap& codes, const CUtensorMap& scales, const WgradArgs& a, cudaStream_t st)
 {
+    // the registers that the kernel hands round are those it was built with: any other build would wait for what it never had
+    static const int regs = [] { cudaFuncAttributes f; return cudaFuncGetAttributes(&f, mx_wgrad_kernel<T, O>) == cudaSuccess ? f.numRegs : 0; }();
+    if (regs * kThreads < 128 * kRegsIssue + 256 * kRegsSum + 128 * kRestoreGroups * kRegsRestore) return cudaErrorInvalidDeviceFunction;
     cudaError_t e = cudaFuncSetAttribute(mx_wgrad_kernel<T, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
     mx_wgrad_kernel<T, O><<<p.clusters * 2, kThreads, kSmem, st>>>(dy, codes, scales, a);
@@ -569,3 +572,5 @@ extern "C" int galv_mx_weight_grad(galv_ctx* ctx, int64_t tokens, int64_t n, int
     }
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
+
+cudaError_t galv_mx_wgrad_timeouts(unsigned* count, cudaStream_t st) { return cudaMemcpyFromSymbolAsync(count, g_timeouts, sizeof(*count), 0, cudaMemcpyDeviceToHost, st); }

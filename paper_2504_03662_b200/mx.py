@@ -268,6 +268,9 @@ def norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[
     if kind == "rms" and bias is not None:
         raise ValueError("an rms norm has no bias")
     _kind(x.dtype, "x")
+    for t, what in ((weight, "weight"), (bias, "bias")):
+        if t is not None and (t.dtype != x.dtype or tuple(t.shape) != x.shape[-1:]):
+            raise ValueError(f"{what} is [{x.shape[-1]}] of {x.dtype}")
     return _Norm.apply(x, weight, bias, kind, eps)
 
 

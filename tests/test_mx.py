@@ -161,6 +161,7 @@ def _fake(rows=4, cols=64, fmt=8):
     lambda: mx.linear(torch.zeros(4, 64), torch.zeros(8, 64)),
     lambda: mx.linear(torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(8, 63, dtype=torch.bfloat16)),
     lambda: mx.norm(torch.zeros(4, 64), bias=torch.zeros(64), kind="rms"),
+    lambda: mx.norm(torch.zeros(4, 64), torch.ones(64, dtype=torch.bfloat16)),      # would only show in the backward pass
     lambda: mx.activation(torch.zeros(4, 64), "relu"),
 ])
 def test_refusals(call):
@@ -511,6 +512,8 @@ def test_the_library_refuses():
     assert lib.galv_mx_matmul_workspace_bytes(h, 4, 8, 64) <= 8192 and mm() == gb.OK and mm(m=0, y=None) == gb.OK
     assert mm(n=0) == mm(k=0) == mm(m=-1) == mm(y=None) == mm(stride=7) == mm(dtype=5) == bad
     torch.cuda.synchronize()
+    assert lib.galv_mx_status(None, None) == bad
+    galv.galv_mx_status()                                           # no wait has run out
 
 
 def _everything(x, dy, w4, weight):
@@ -567,6 +570,34 @@ def test_captured_and_replayed():
     graph.replay()
     graph.replay()
     assert all(torch.equal(a, b) for a, b in zip(out, want2))
+
+
+@gpu
+def test_offsets_beyond_32_bits():
+    """2.15e9 elements: the last rows of everything are what they are on their own."""
+    rows, cols, last = 65600, 32800, 80
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(rows, cols, generator=g, device="cuda", dtype=torch.bfloat16)
+    tail = x[-last:].clone()
+    kept, small = mx.pack(x), mx.pack(tail)
+    assert torch.equal(kept.codes[-small.codes.numel():], small.codes) and torch.equal(kept.scales[-small.scales.numel():], small.scales)
+    assert torch.equal(mx.unpack(kept)[-last:], mx.unpack(small))
+    for act in ("gelu", "silu"):
+        got = mx.act_backward(x, kept, act)[-last:].float()
+        assert torch.allclose(got, mx.act_backward(tail, small, act).float(), rtol=2 ** -7, atol=1.3e-5)      # looked up or computed: 21 * 2^-24 of |dy| < 5 and half a step each
+        del got
+    assert torch.equal(mx.norm_backward(x, kept)[0][-last:], mx.norm_backward(tail, small)[0])
+    dy = torch.zeros(rows, 16, device="cuda", dtype=torch.bfloat16)
+    dy[-last:] = torch.randn(last, 16, generator=g, device="cuda").bfloat16()
+    a, b = mx.weight_grad(dy, kept, torch.float32), mx.weight_grad(dy[-last:].contiguous(), small, torch.float32)
+    assert torch.allclose(a, b, rtol=1e-5, atol=1e-4)               # tokens in other chunks, other orders: (80 / 16 + 4) * 2^-23 of sums of magnitudes below 90 at most
+    four, four_tail = mx.pack(x, 4), mx.pack(tail, 4)
+    assert torch.equal(mx.unpack(four)[-last:], mx.unpack(four_tail))
+    del x, kept, four
+    left, right = mx.pack(torch.randn(rows, 64, generator=g, device="cuda", dtype=torch.bfloat16), 4), mx.pack(torch.randn(cols, 64, generator=g, device="cuda", dtype=torch.bfloat16), 4)
+    y = mx.matmul(left, right, torch.float16)
+    want = mx.unpack(left, torch.float32)[-last:].double() @ mx.unpack(right, torch.float32).double().t()
+    assert ((y[-last:].double() - want).abs() <= want.abs() * 2.0 ** -11 + 1e-6).all()
 
 
 # ------------------------------------------------------------------------------------------------- a run of them
