@@ -86,14 +86,41 @@ __device__ __forceinline__ MxPlace mx_place(const MxSpread& s, long long block)
 // 8 elements of a row as one piece: 16 bytes of 16-bit numbers, 32 of fp32.
 template <typename T> struct MxPiece { uint4 q[sizeof(T) / 2]; };
 
-// As they lie in memory.  VEC: the row starts on a 16-byte boundary (c0 is a multiple of 8).  Behind `cols`: zeros.
+// 16 bytes from `at` bytes (a multiple of 2) behind the start of the 32 in a and b.
+__device__ __forceinline__ uint4 mx_shifted(const uint4& a, const uint4& b, uint32_t at)
+{
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (at & 8) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (at & 4) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    const uint32_t bits = (at & 2) * 8;
+    return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+}
+
+// As they lie in memory, zeros behind `cols`.  VEC: the row starts on a 16-byte boundary (c0 is a multiple of 8).  Else a piece inside its row is taken from the
+// aligned 16 bytes around it, which lie in the row too; the first and the last pieces go element by element, and so do short rows (`pieces` false), where a
+// warp would take both ways.
 template <typename T, bool VEC>
-__device__ __forceinline__ MxPiece<T> mx_fetch8(const T* row, int c0, int cols)
+__device__ __forceinline__ MxPiece<T> mx_fetch8(const T* row, int c0, int cols, bool pieces = true)
 {
     MxPiece<T> p;
     if (VEC && c0 + 8 <= cols) {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) p.q[i] = reinterpret_cast<const uint4*>(row + c0)[i];
+    } else if (!VEC && pieces && c0 >= 8 && c0 + 16 <= cols) {
+        const uintptr_t from = reinterpret_cast<uintptr_t>(row + c0);
+        const uint32_t at = from & 15;
+        const uint4* g = reinterpret_cast<const uint4*>(from - at);
+        uint4 w[sizeof(T) / 2 + 1];
+#pragma unroll
+        for (int i = 0; i <= (int)sizeof(T) / 2; ++i) w[i] = g[i];
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) p.q[i] = mx_shifted(w[i], w[i + 1], at);
     } else {
         T* e = reinterpret_cast<T*>(&p);
 #pragma unroll
@@ -168,28 +195,65 @@ template <> __device__ __forceinline__ MxPiece<__half> mx_piece<__half>(const fl
     return p;
 }
 
+// What was held as a finite number stays one in fp16.
+template <typename T> __device__ __forceinline__ MxPiece<T> mx_piece_held(const float (&v)[8]) { return mx_piece<T>(v); }
+template <> __device__ __forceinline__ MxPiece<__half> mx_piece_held<__half>(const float (&v)[8])
+{
+    MxPiece<__half> p;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(p.q[0].x) : "f"(v[1]), "f"(v[0]));
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(p.q[0].y) : "f"(v[3]), "f"(v[2]));
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(p.q[0].z) : "f"(v[5]), "f"(v[4]));
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(p.q[0].w) : "f"(v[7]), "f"(v[6]));
+    return p;
+}
+
 template <typename T, bool VEC>
-__device__ __forceinline__ void mx_store8(T* __restrict__ row, int c0, int cols, const float (&v)[8])
+__device__ __forceinline__ void mx_store8(T* __restrict__ row, int c0, int cols, const MxPiece<T>& p)
 {
     if (VEC && c0 + 8 <= cols) {
-        const MxPiece<T> p = mx_piece<T>(v);
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(row + c0)[i] = p.q[i];
     } else {
+        const T* e = reinterpret_cast<const T*>(&p);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (c0 + i < cols) row[c0 + i] = mx_round<T>(v[i]);
+            if (c0 + i < cols) row[c0 + i] = e[i];
     }
 }
 
-// Rows that do not start on 16-byte boundaries: a warp writes its 32 pieces through shared memory, 32 elements next to one another at a time (each lane
-// its own 8 in turn took 2.3 times as long; reading them in turn is the faster way, the lines stay in the first cache).  place(l, n): lane
-// l's first element, n of which exist.
+// Rows that do not start on 16-byte boundaries: a warp whose 32 pieces lie next to one another in a row writes them through shared memory, so that
+// aligned 16 bytes leave at a time (single elements of lanes in turn took five times as long).  start: lane 0's first element; n of them exist from there.
+template <typename T>
+__device__ __forceinline__ void mx_scatter_run(T* buf, T* start, int n, const MxPiece<T>& p)
+{
+    constexpr int G = 16 / (int)sizeof(T);                // elements of 16 bytes
+    const int lane = threadIdx.x % 32;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(buf + lane * 8)[i] = p.q[i];
+    __syncwarp();
+    n = min(n, 256);
+    const int ahead = (int)(reinterpret_cast<uintptr_t>(start) & 15) / (int)sizeof(T), lead = (G - ahead) % G;      // elements from the boundary before to the start, and to the one behind
+    const uint32_t at = lead * (int)sizeof(T);            // of each 16 bytes, in shared memory
+#pragma unroll
+    for (int k = 0; k < 256 / G; k += 32) {
+        const int first = lead + (k + lane) * G;
+        if (first + G <= n) {
+            const uint4* from = reinterpret_cast<const uint4*>(buf) + (k + lane);
+            *reinterpret_cast<uint4*>(start + first) = mx_shifted(from[0], from[1], at);
+        } else if (first + G <= 256) {                    // the row's end
+#pragma unroll 1
+            for (int i = first; i < n; ++i) start[i] = buf[i];
+        }
+    }
+    const int edge = lane < lead ? lane : 256 - G + lane; // before the first boundary, behind the last
+    if (ahead && lane < G && edge < n) start[edge] = buf[edge];
+}
+// ... of pieces in several rows: 32 elements next to one another at a time.  place(l, n): lane l's first element, n of which exist.
 template <typename T, typename Place>
-__device__ __forceinline__ void mx_scatter8(T* buf, const Place& place, const float (&v)[8])
+__device__ __forceinline__ void mx_scatter8(T* buf, const Place& place, const MxPiece<T>& p)
 {
     const int lane = threadIdx.x % 32, e = lane % 8;
-    const MxPiece<T> p = mx_piece<T>(v);
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(buf + lane * 8)[i] = p.q[i];
@@ -217,6 +281,18 @@ struct MxPlaces {
         return x + ((long long)row * stride + c);
     }
 };
+// A spread pass's piece c of a row (`row`: its start; exists: whether it is one) to rows that do not start on 16-byte boundaries.
+template <typename T>
+__device__ __forceinline__ void mx_store_spread(T* buf, T* row, unsigned c, bool exists, T* x, long long stride, const MxSpread& s, const MxPlace& at, int h, unsigned rows, unsigned cols,
+                                                const MxPiece<T>& p)
+{
+    if (s.log >= 5) {                                     // the warp's pieces lie in one row
+        const unsigned c0 = (c - threadIdx.x % 32) * 8;
+        mx_scatter_run<T>(buf, row + c0, exists && c0 < cols ? (int)min(256u, cols - c0) : 0, p);
+    } else {
+        mx_scatter8<T>(buf, MxPlaces<T>(x, stride, s, at, h, rows, cols), p);
+    }
+}
 
 // Scale byte of a block whose largest magnitude has these bits: the smallest exponent under which it does not pass the largest element,
 // 448 = 1.75 * 2^8 or 6 = 1.5 * 2^2.  Whole numbers only, so exact; 255 for an infinity or a NaN.

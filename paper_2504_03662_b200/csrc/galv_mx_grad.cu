@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
                                                             const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const T* dy,
                                                             long long dy_stride, T* dx, long long dx_stride)
 {
-    __shared__ __align__(16) T buf[VEC ? 1 : kMxThreads / 32][256];
+    __shared__ __align__(16) T buf[VEC ? 1 : kMxThreads / 32][256 + 8];
     extern __shared__ float table[];
     if (TABLE) {
         float x[4];
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
             if (row < rows && c < pieces) {
                 code[h] = __ldg(reinterpret_cast<const uint2*>(held));
                 byte[h] = __ldg(power);
-                raw[h] = mx_fetch8<T, VEC>(from, (int)c * 8, cols);
+                raw[h] = mx_fetch8<T, VEC>(from, (int)c * 8, cols, spread.log >= 5);
             } else if (!VEC) {
                 code[h] = make_uint2(0, 0);
                 byte[h] = 0;
@@ -115,8 +115,8 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
 #pragma unroll
                 for (int i = 0; i < 8; ++i) g[i] *= act_slope<ACT>(x[i] * s);
             }
-            if (VEC) mx_store8<T, true>(to, (int)c * 8, cols, g);
-            else mx_scatter8<T>(buf[threadIdx.x / 32], MxPlaces<T>(dx, dx_stride, spread, at, h, rows, cols), g);
+            if (VEC) mx_store8<T, true>(to, (int)c * 8, cols, mx_piece<T>(g));
+            else mx_store_spread<T>(buf[threadIdx.x / 32], to, c, row < rows, dx, dx_stride, spread, at, h, rows, cols, mx_piece<T>(g));
         }
     }
 }
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
     constexpr int NS = NormStage<T>::count, kDy = 8 * (int)sizeof(T);
     extern __shared__ __align__(16) unsigned char raw[];
     constexpr bool kShared = !WARP && PP > 1;             // dweight's sums lie in shared memory
-    __shared__ __align__(16) T buf[VEC ? 1 : (WARP ? 8 : W / 32)][256];
+    __shared__ __align__(16) T buf[VEC ? 1 : (WARP ? 8 : W / 32)][256 + 8];
     __shared__ float4 red[2][32];
     __shared__ float red1[2][32];
     constexpr int teams = WARP ? 8 : 1, width = W, slots = W * PP;
@@ -326,10 +326,9 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
                 for (int i = 0; i < kDy / 16; ++i)
                     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(d[p].q[i].x), "=r"(d[p].q[i].y), "=r"(d[p].q[i].z), "=r"(d[p].q[i].w) : "r"(from + at * kDy + i * 16));
             } else {
-                const T* from_row = (const T*)a.dy + row * a.dy_stride;
-                T* e = reinterpret_cast<T*>(&d[p]);
+                const MxPiece<T> piece = mx_fetch8<T, false>((const T*)a.dy + row * a.dy_stride, at * 8, cols);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] = at * 8 + i < cols ? from_row[at * 8 + i] : mx_zero<T>();
+                for (int i = 0; i < kDy / 16; ++i) d[p].q[i] = piece.q[i];
             }
             mx_from8(code.x, x + 8 * p);
             mx_from8(code.y, x + 8 * p + 4);
@@ -386,13 +385,10 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
             }
             if (kShared) sums_store(p);
             if (VEC) {
-                mx_store8<T, true>(dx, (lane + p * width) * 8, cols, v);
+                mx_store8<T, true>(dx, (lane + p * width) * 8, cols, mx_piece<T>(v));
             } else {
-                mx_scatter8<T>(buf[threadIdx.x / 32], [&](int l, int& n) {
-                    const int c = ((lane & ~31) + l + p * width) * 8;
-                    n = min(8, cols - c);
-                    return dx + c;
-                }, v);
+                const int c = ((lane & ~31) + p * width) * 8;
+                mx_scatter_run<T>(buf[threadIdx.x / 32], dx + c, cols - c, mx_piece<T>(v));
             }
         }
     }
@@ -524,7 +520,7 @@ __global__ void __launch_bounds__(512) mx_norm_wide_kernel(const NormArgs a, flo
             if (a.weight) mx_load8<T, false>((const T*)a.weight, (int)c * 8, (int)a.cols, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) g[i] = rstd * ((a.weight ? g[i] * w[i] : g[i]) - mg - (x[i] - mean) * m);
-            mx_store8<T, VEC>(dx, (int)c * 8, (int)a.cols, g);
+            mx_store8<T, VEC>(dx, (int)c * 8, (int)a.cols, mx_piece<T>(g));
         }
     }
 }

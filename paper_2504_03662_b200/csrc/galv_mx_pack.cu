@@ -23,7 +23,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_pack_kernel(const MxSpread spre
         for (int h = 0; h < U; ++h, from += spread.dr * stride) {
             const unsigned row = at.row + h * spread.dr, c = at.c + h * spread.dc;
             if (row < rows && c < nb * 4) {
-                raw[h] = mx_fetch8<T, VEC>(from, (int)c * 8, cols);
+                raw[h] = mx_fetch8<T, VEC>(from, (int)c * 8, cols, spread.log >= 5);
             } else {
 #pragma unroll
                 for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[h].q[i] = make_uint4(0, 0, 0, 0);
@@ -57,14 +57,15 @@ __global__ void __launch_bounds__(kMxThreads) mx_pack_kernel(const MxSpread spre
     }
 }
 
+constexpr int kUnpackEach = 4;                            // pieces a thread, of any type: what is read is small
 template <typename T, int FMT, bool VEC>
 __global__ void __launch_bounds__(kMxThreads) mx_unpack_kernel(const MxSpread spread, unsigned rows, int cols, unsigned nb, unsigned pieces, int per_row,
                                                                const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ x, long long stride)
 {
-    __shared__ __align__(16) T buf[VEC ? 1 : kMxThreads / 32][256];
+    __shared__ __align__(16) T buf[VEC ? 1 : kMxThreads / 32][256 + 8];
     for (long long block = blockIdx.x; block < spread.blocks; block += gridDim.x) {
         const MxPlace at = mx_place(spread, block);
-        constexpr int U = MxEach<T>::count;
+        constexpr int U = kUnpackEach;
         uint2 code[U];
         int byte[U];
         const uint8_t* held = codes + ((long long)at.row * nb * 4 + at.c) * FMT;
@@ -93,9 +94,9 @@ __global__ void __launch_bounds__(kMxThreads) mx_unpack_kernel(const MxSpread sp
             }
             const float s = mx_scale(byte[h]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = mx_held<T>(v[i] * s);
-            if (VEC) mx_store8<T, true>(to, (int)c * 8, cols, v);
-            else mx_scatter8<T>(buf[threadIdx.x / 32], MxPlaces<T>(x, stride, spread, at, h, rows, cols), v);
+            for (int i = 0; i < 8; ++i) v[i] *= s;
+            if (VEC) mx_store8<T, true>(to, (int)c * 8, cols, mx_piece_held<T>(v));
+            else mx_store_spread<T>(buf[threadIdx.x / 32], to, c, row < rows, x, stride, spread, at, h, rows, cols, mx_piece_held<T>(v));
         }
     }
 }
@@ -159,7 +160,7 @@ extern "C" int galv_mx_unpack(galv_ctx* ctx, int64_t rows, int64_t cols, int32_t
     const int nb = (int)mx_blocks(cols), pieces = (int)((cols + 7) / 8);
     const int per_row = fmt == GALV_MX8 ? (int)mx_pitch8(cols) : (nb + 3) / 4;
     const bool vec = mx_rows16(x, x_stride, dtype);
-    const MxSpread spread(rows, pieces, dtype == GALV_F32 ? MxEach<float>::count : MxEach<__half>::count);
+    const MxSpread spread(rows, pieces, kUnpackEach);
     const int grid = spread.grid();
     cudaStream_t st = (cudaStream_t)stream;
 #define MX_UNPACK(FMT)                                                                                                                         \

@@ -474,11 +474,12 @@ __global__ void __launch_bounds__(256) mx_fill_kernel(long long count, const O* 
     for (long long e = (long long)blockIdx.x * 256 + threadIdx.x; e < count; e += (long long)gridDim.x * 256) dw[e] = base ? base[e] : mx_round<O>(0.f);
 }
 
-// Rows that bulk copies cannot take (not on 16-byte boundaries) into rows that they can.
-__global__ void __launch_bounds__(256) mx_align_kernel(long long rows, long long cols, const uint16_t* __restrict__ x, long long stride, uint16_t* __restrict__ out, long long pitch)
+// Rows that bulk copies cannot take (not on 16-byte boundaries) into rows that they can, zeros behind their ends.
+__global__ void __launch_bounds__(256) mx_align_kernel(long long rows, int cols, const __half* __restrict__ x, long long stride, __half* __restrict__ out, long long pitch)
 {
     for (long long r = blockIdx.x; r < rows; r += gridDim.x)
-        for (long long c = threadIdx.x; c < cols; c += 256) out[r * pitch + c] = x[r * stride + c];
+        for (int c = threadIdx.x * 8; c < cols; c += 2048)
+            *reinterpret_cast<uint4*>(out + r * pitch + c) = mx_fetch8<__half, false>(x + r * stride, c, cols).q[0];
 }
 
 struct WgradPlan { int tiles_n, tiles_k, splits, chunks, clusters; size_t aligned, partial, total; };
@@ -555,7 +556,7 @@ extern "C" int galv_mx_weight_grad(galv_ctx* ctx, int64_t tokens, int64_t n, int
         int64_t stride = dy_stride;
         if (p.aligned) {
             stride = (n + 7) / 8 * 8;
-            mx_align_kernel<<<(int)(tokens < ctx->num_sms * 16 ? tokens : ctx->num_sms * 16), 256, 0, st>>>(tokens, n, (const uint16_t*)dy, dy_stride, (uint16_t*)workspace, stride);
+            mx_align_kernel<<<(int)(tokens < ctx->num_sms * 16 ? tokens : ctx->num_sms * 16), 256, 0, st>>>(tokens, (int)n, (const __half*)dy, dy_stride, (__half*)workspace, stride);
             rows = workspace;
         }
         CUtensorMap dm, cm, sm;
