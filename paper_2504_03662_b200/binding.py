@@ -151,6 +151,10 @@ def _ws(t):
     return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
 
 
+def _address(t) -> int:
+    return t if t.__class__ is int else t.data_ptr()
+
+
 def _at(t):
     return None if t is None else t.data_ptr()
 
@@ -308,21 +312,22 @@ class Galv:
         self._check(self.lib.galv_layer_loop_ms_stats(self.h, C.byref(mean), C.byref(lo), C.byref(hi), C.byref(n)))
         return mean.value, lo.value, hi.value, n.value
 
-    # Microscaled operators: matrices are 2-D tensors with contiguous rows, codes and scales uint8 tensors; on the current stream of the
-    # context's device.  These calls are short, so the pointers are taken without the checks of _ptr (mx.py has made its own).
+    # Microscaled operators: matrices are 2-D tensors with contiguous rows, codes and scales uint8 tensors or their
+    # addresses; on the current stream of the context's device.  These calls are short, so the pointers are taken without the checks of _ptr (mx.py has
+    # made its own).
 
     def galv_mx_pack(self, x, fmt, codes, scales):
-        rc = self.lib.galv_mx_pack(self.h, *x.shape, *_matrix(x), _DTYPES[x.dtype], fmt, codes.data_ptr(), scales.data_ptr(), _raw_stream(self.device))
+        rc = self.lib.galv_mx_pack(self.h, *x.shape, *_matrix(x), _DTYPES[x.dtype], fmt, _address(codes), _address(scales), _raw_stream(self.device))
         if rc:
             self._check(rc)
 
     def galv_mx_unpack(self, fmt, codes, scales, x):
-        rc = self.lib.galv_mx_unpack(self.h, *x.shape, fmt, codes.data_ptr(), scales.data_ptr(), *_matrix(x), _DTYPES[x.dtype], _raw_stream(self.device))
+        rc = self.lib.galv_mx_unpack(self.h, *x.shape, fmt, _address(codes), _address(scales), *_matrix(x), _DTYPES[x.dtype], _raw_stream(self.device))
         if rc:
             self._check(rc)
 
     def galv_mx_act_backward(self, act, codes, scales, dy, dx):
-        rc = self.lib.galv_mx_act_backward(self.h, *dy.shape, act, codes.data_ptr(), scales.data_ptr(), *_matrix(dy), *_matrix(dx), _DTYPES[dy.dtype],
+        rc = self.lib.galv_mx_act_backward(self.h, *dy.shape, act, _address(codes), _address(scales), *_matrix(dy), *_matrix(dx), _DTYPES[dy.dtype],
                                            _raw_stream(self.device))
         if rc:
             self._check(rc)
@@ -331,7 +336,7 @@ class Galv:
         return self.lib.galv_mx_norm_workspace_bytes(self.h, rows, cols)
 
     def galv_mx_norm_backward(self, kind, eps, codes, scales, dy, weight, dx, dweight, dbias, workspace):
-        rc = self.lib.galv_mx_norm_backward(self.h, *dy.shape, kind, eps, codes.data_ptr(), scales.data_ptr(), *_matrix(dy), _at(weight), *_matrix(dx),
+        rc = self.lib.galv_mx_norm_backward(self.h, *dy.shape, kind, eps, _address(codes), _address(scales), *_matrix(dy), _at(weight), *_matrix(dx),
                                             _DTYPES[dy.dtype], _at(dweight), _at(dbias), *_ws(workspace), _raw_stream(self.device))
         if rc:
             self._check(rc)
@@ -340,7 +345,7 @@ class Galv:
         return self.lib.galv_mx_weight_grad_workspace_bytes(self.h, *dy.shape, k, *_matrix(dy))
 
     def galv_mx_weight_grad(self, dy, codes, scales, base, dw, workspace):
-        rc = self.lib.galv_mx_weight_grad(self.h, *dy.shape, dw.shape[1], *_matrix(dy), _DTYPES[dy.dtype], codes.data_ptr(), scales.data_ptr(), _at(base),
+        rc = self.lib.galv_mx_weight_grad(self.h, *dy.shape, dw.shape[1], *_matrix(dy), _DTYPES[dy.dtype], _address(codes), _address(scales), _at(base),
                                           dw.data_ptr(), _DTYPES[dw.dtype], *_ws(workspace), _raw_stream(self.device))
         if rc:
             self._check(rc)
@@ -349,7 +354,7 @@ class Galv:
         return self.lib.galv_mx_matmul_workspace_bytes(self.h, m, n, k)
 
     def galv_mx_matmul(self, k, a_codes, a_scales, b_codes, b_scales, bias, y, workspace):
-        rc = self.lib.galv_mx_matmul(self.h, *y.shape, k, a_codes.data_ptr(), a_scales.data_ptr(), b_codes.data_ptr(), b_scales.data_ptr(), _at(bias),
+        rc = self.lib.galv_mx_matmul(self.h, *y.shape, k, _address(a_codes), _address(a_scales), _address(b_codes), _address(b_scales), _at(bias),
                                      *_matrix(y), _DTYPES[y.dtype], *_ws(workspace), _raw_stream(self.device))
         if rc:
             self._check(rc)

@@ -45,8 +45,9 @@ def scales_bytes(rows: int, cols: int, fmt: int = gb.MX8) -> int:
 
 
 class Packed:
-    """A matrix [rows][cols] in blocks of 32 columns: element codes, one scale byte a block."""
-    __slots__ = ("codes", "scales", "rows", "cols", "fmt")
+    """A matrix [rows][cols] in blocks of 32 columns: element codes, one scale byte a block.  (What `pack` makes has both in one piece of memory, of
+    which `codes` and `scales` are views made when they are asked for.)"""
+    __slots__ = ("_codes", "_scales", "_both", "_at", "rows", "cols", "fmt", "device")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, fmt: int = gb.MX8):
         if fmt != gb.MX8 and fmt != gb.MX4:
@@ -56,20 +57,51 @@ class Packed:
         nc, ns = codes_bytes(rows, cols, fmt), scales_bytes(rows, cols, fmt)
         if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.numel() < nc or scales.numel() < ns or not codes.is_contiguous() or not scales.is_contiguous():
             raise ValueError(f"a [{rows}][{cols}] matrix in {fmt} bits takes {nc} and {ns} contiguous bytes, got {codes.dtype} {tuple(codes.shape)} and {scales.dtype} {tuple(scales.shape)}")
-        self.codes, self.scales, self.rows, self.cols, self.fmt = codes, scales, rows, cols, fmt
+        if codes.device != scales.device:
+            raise ValueError(f"codes on {codes.device} and scales on {scales.device}")
+        self._codes, self._scales, self._both, self._at = codes, scales, None, (codes.data_ptr(), scales.data_ptr())
+        self.rows, self.cols, self.fmt, self.device = rows, cols, fmt, codes.device
+
+    @classmethod
+    def _empty(cls, rows: int, cols: int, fmt: int, device: torch.device) -> "Packed":
+        nc = (codes_bytes(rows, cols, fmt) + 255) & ~255
+        p = cls.__new__(cls)
+        p._codes = p._scales = None
+        p._both = torch.empty(nc + scales_bytes(rows, cols, fmt), dtype=torch.uint8, device=device)
+        at = p._both.data_ptr()
+        p._at = at, at + nc
+        p.rows, p.cols, p.fmt, p.device = rows, cols, fmt, device
+        return p
+
+    @property
+    def codes(self) -> torch.Tensor:
+        if self._codes is None:
+            self._codes = self._both[:codes_bytes(self.rows, self.cols, self.fmt)]
+        return self._codes
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._scales is None:
+            self._scales = self._both[(codes_bytes(self.rows, self.cols, self.fmt) + 255) & ~255:]
+        return self._scales
 
     @property
     def nbytes(self) -> int:
-        return self.codes.numel() + self.scales.numel()
+        return codes_bytes(self.rows, self.cols, self.fmt) + scales_bytes(self.rows, self.cols, self.fmt)
 
 
-def _on(*tensors: torch.Tensor) -> gb.Galv:
-    """The context of the device that all tensors lie on."""
-    dev = tensors[0].get_device()
-    for t in tensors:
-        if t.get_device() != dev or not t.is_cuda:
-            raise ValueError(f"microscaled operators take CUDA tensors of one device (no CPU path), not {', '.join(str(u.device) for u in tensors)}")
-    return context(dev)
+def _on(device: torch.device, *others: Optional[torch.device]) -> gb.Galv:
+    """The context of the device that everything lies on."""
+    for d in others:
+        if d is not None and d != device:
+            raise ValueError(f"operands on {device} and {d}")
+    if device.type != "cuda":
+        raise ValueError(f"microscaled operators take CUDA tensors (no CPU path), not {device.type}")
+    return context(device.index)
+
+
+def _device(t: Optional[torch.Tensor]) -> Optional[torch.device]:
+    return None if t is None else t.device
 
 
 def _kind(dtype: torch.dtype, what: str, dtypes=_NUMBERS):
@@ -105,23 +137,22 @@ def pack(x: torch.Tensor, fmt: int = gb.MX8) -> Packed:
         raise ValueError(f"a format is 8 or 4 bits, not {fmt}")
     _kind(x.dtype, "x")
     x = _rows(x, "x")
-    g = _on(x)
+    device = x.device
+    g = _on(device)
     rows, cols = x.shape
     if cols < 1:
         raise ValueError("rows of at least one column")
-    p = Packed.__new__(Packed)
-    p.codes, p.scales = _bytes(codes_bytes(rows, cols, fmt), x.device), _bytes(scales_bytes(rows, cols, fmt), x.device)
-    p.rows, p.cols, p.fmt = rows, cols, fmt
-    g.galv_mx_pack(x, fmt, p.codes, p.scales)
+    p = Packed._empty(rows, cols, fmt, device)
+    g.galv_mx_pack(x, fmt, *p._at)
     return p
 
 
 def unpack(p: Packed, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """The numbers a packed matrix stands for."""
     _kind(dtype, "dtype")
-    g = _on(p.codes, p.scales)
-    x = torch.empty(p.rows, p.cols, dtype=dtype, device=p.codes.device)
-    g.galv_mx_unpack(p.fmt, p.codes, p.scales, x)
+    g = _on(p.device)
+    x = torch.empty(p.rows, p.cols, dtype=dtype, device=p.device)
+    g.galv_mx_unpack(p.fmt, *p._at, x)
     return x
 
 
@@ -132,9 +163,10 @@ def act_backward(dy: torch.Tensor, kept: Packed, act: str = "gelu") -> torch.Ten
     _kind(dy.dtype, "dy")
     dy = _rows(dy, "dy")
     _beside(dy, kept, "dy")
-    g = _on(dy, kept.codes, kept.scales)
-    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
-    g.galv_mx_act_backward(ACTS[act], kept.codes, kept.scales, dy, dx)
+    device = dy.device
+    g = _on(device, kept.device)
+    dx = torch.empty(kept.rows, kept.cols, dtype=dy.dtype, device=device)
+    g.galv_mx_act_backward(ACTS[act], *kept._at, dy, dx)
     return dx
 
 
@@ -147,13 +179,13 @@ def norm_backward(dy: torch.Tensor, kept: Packed, weight: Optional[torch.Tensor]
     _beside(dy, kept, "dy")
     if weight is not None and (weight.dtype != dy.dtype or tuple(weight.shape) != (kept.cols,)):
         raise ValueError(f"weight is [{kept.cols}] of {dy.dtype}")
-    g = _on(dy, kept.codes, kept.scales) if weight is None else _on(dy, kept.codes, kept.scales, weight)
-    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
-    dweight = torch.empty(kept.cols, dtype=torch.float32, device=dy.device)
-    dbias = torch.empty(kept.cols, dtype=torch.float32, device=dy.device) if kind == "layer" else None
+    device = dy.device
+    g = _on(device, kept.device, _device(weight))
+    dx = torch.empty(kept.rows, kept.cols, dtype=dy.dtype, device=device)
+    dweight = torch.empty(kept.cols, dtype=torch.float32, device=device)
+    dbias = torch.empty(kept.cols, dtype=torch.float32, device=device) if kind == "layer" else None
     n = g.galv_mx_norm_workspace_bytes(kept.rows, kept.cols)
-    g.galv_mx_norm_backward(NORMS[kind], eps, kept.codes, kept.scales, dy, None if weight is None else weight.contiguous(), dx, dweight, dbias,
-                            _bytes(n, dy.device) if n else None)
+    g.galv_mx_norm_backward(NORMS[kind], eps, *kept._at, dy, None if weight is None else weight.contiguous(), dx, dweight, dbias, _bytes(n, device) if n else None)
     return dx, dweight, dbias
 
 
@@ -170,16 +202,15 @@ def weight_grad(dy: torch.Tensor, kept: Packed, dtype: Optional[torch.dtype] = N
     dtype = dtype or (out if out is not None else base if base is not None else dy).dtype
     if dtype != dy.dtype and dtype != torch.float32:
         raise ValueError(f"a weight gradient is of {dy.dtype} or float32, not {dtype}")
-    tensors = [dy, kept.codes, kept.scales]
     for t, what in ((base, "base"), (out, "out")):
         if t is not None:
             if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
                 raise ValueError(f"{what} is a contiguous {shape} of {dtype}")
-            tensors.append(t)
-    g = _on(*tensors)
-    dw = torch.empty(shape, dtype=dtype, device=dy.device) if out is None else out
+    device = dy.device
+    g = _on(device, kept.device, _device(base), _device(out))
+    dw = torch.empty(shape, dtype=dtype, device=device) if out is None else out
     n = g.galv_mx_weight_grad_workspace_bytes(dy, kept.cols)
-    g.galv_mx_weight_grad(dy, kept.codes, kept.scales, base, dw, _bytes(n, dy.device) if n else None)
+    g.galv_mx_weight_grad(dy, *kept._at, base, dw, _bytes(n, device) if n else None)
     return dw
 
 
@@ -192,10 +223,10 @@ def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, bias: Opti
     _kind(dtype, "dtype")
     if bias is not None and (bias.dtype != dtype or tuple(bias.shape) != (b.rows,)):
         raise ValueError(f"bias is [{b.rows}] of {dtype}")
-    g = _on(a.codes, a.scales, b.codes, b.scales) if bias is None else _on(a.codes, a.scales, b.codes, b.scales, bias)
-    y = torch.empty(a.rows, b.rows, dtype=dtype, device=a.codes.device)
+    g = _on(a.device, b.device, _device(bias))
+    y = torch.empty(a.rows, b.rows, dtype=dtype, device=a.device)
     n = g.galv_mx_matmul_workspace_bytes(a.rows, b.rows, a.cols)
-    g.galv_mx_matmul(a.cols, a.codes, a.scales, b.codes, b.scales, None if bias is None else bias.contiguous(), y, _bytes(n, y.device) if n else None)
+    g.galv_mx_matmul(a.cols, *a._at, *b._at, None if bias is None else bias.contiguous(), y, _bytes(n, a.device) if n else None)
     return y
 
 
