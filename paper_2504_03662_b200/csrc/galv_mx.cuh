@@ -223,6 +223,7 @@ __device__ __forceinline__ void mx_store8(T* __restrict__ row, int c0, int cols,
 
 // Rows that do not start on 16-byte boundaries: a warp whose 32 pieces lie next to one another in a row writes them through shared memory, so that
 // aligned 16 bytes leave at a time (single elements of lanes in turn took five times as long).  start: lane 0's first element; n of them exist from there.
+// buf has room for 256 elements, and 16 bytes behind them can be read.
 template <typename T>
 __device__ __forceinline__ void mx_scatter_run(T* buf, T* start, int n, const MxPiece<T>& p)
 {

@@ -1,6 +1,7 @@
 // Gradients that read a layer's input where it was kept in 8 bits: activation functions and norms.
 
 #include "galv_mx.cuh"
+#include "galv_tc.cuh"
 
 namespace {
 
@@ -142,6 +143,9 @@ struct NormArgs {
     bool weight16;                                        // on a 16-byte boundary
     void* dx;
     float* part;                                          // [parts][2][cols]: dweight, dbias
+    int ranks;                                            // CTAs of the one cluster that finishes dweight and dbias itself, or 0
+    float* dweight;
+    float* dbias;
 };
 
 template <typename T> struct Raw8 { uint4 q[sizeof(T) / 2]; };
@@ -223,7 +227,6 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
     constexpr int NS = NormStage<T>::count, kDy = 8 * (int)sizeof(T);
     extern __shared__ __align__(16) unsigned char raw[];
     constexpr bool kShared = !WARP && PP > 1;             // dweight's sums lie in shared memory
-    __shared__ __align__(16) T buf[VEC ? 1 : (WARP ? 8 : W / 32)][256 + 8];
     __shared__ float4 red[2][32];
     __shared__ float red1[2][32];
     constexpr int teams = WARP ? 8 : 1, width = W, slots = W * PP;
@@ -233,6 +236,8 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
     // weights [slots][8], then each team's stages of dy [slots][8], codes [slots][8 bytes], scale words [slots], then sums [2][slots][4]
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(raw), mine = base + slots * kDy + team * NS * slots * NormStage<T>::piece;
     const uint32_t sums = mine + NS * slots * NormStage<T>::piece;
+    // rows off 16-byte boundaries are not staged: the first stage's place of dy is where a warp's results are put together
+    T* const buf = reinterpret_cast<T*>(raw + (mine - base) + (WARP ? 0 : (threadIdx.x & ~31) * kDy));
     for (int c = threadIdx.x * 8; c < slots * 8; c += (WARP ? 256 : W) * 8) {
         float w[8];
         if (a.weight && c < a.cols) {
@@ -388,37 +393,39 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
                 mx_store8<T, true>(dx, (lane + p * width) * 8, cols, mx_piece<T>(v));
             } else {
                 const int c = ((lane & ~31) + p * width) * 8;
-                mx_scatter_run<T>(buf[threadIdx.x / 32], dx + c, cols - c, mx_piece<T>(v));
+                mx_scatter_run<T>(buf, dx + c, cols - c, mx_piece<T>(v));
             }
         }
     }
     // this CTA's column sums
-    const long long pitch = pieces * 8;
+    const int pitch = pieces * 8;
     float* part = a.part + (long long)blockIdx.x * 2 * pitch;
-    if (WARP) {
+    float* joined = reinterpret_cast<float*>(raw);        // over what is not read any more: [2][apart] (a warp a row: [team][2][apart])
+    const int apart = WARP ? slots * 8 : pitch;
+    if (WARP || a.ranks) {
         asm volatile("cp.async.wait_all;" ::: "memory");
         __syncthreads();
-        float* joined = reinterpret_cast<float*>(raw);    // [2][kWarpColumns] over what is not read any more
-        for (int t = 0; t < teams; ++t) {                 // the warps' in order
-            if (team == t) {
+    }
+    if (WARP) {
 #pragma unroll
-                for (int p = 0; p < PP; ++p)
+        for (int p = 0; p < PP; ++p)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int c = (lane + p * 32) * 8 + i;
-                        if (c < pitch) {
-                            joined[c] = t ? joined[c] + dw[8 * p + i] : dw[8 * p + i];
-                            if (LAYER) joined[kWarpColumns + c] = t ? joined[kWarpColumns + c] + db[8 * p + i] : db[8 * p + i];
-                        }
-                    }
+            for (int i = 0; i < 8; i += 4) {
+                float* to = joined + team * 2 * apart + (lane + p * 32) * 8 + i;
+                const int k = 8 * p + i;
+                *reinterpret_cast<float4*>(to) = make_float4(dw[k], dw[k + 1], dw[k + 2], dw[k + 3]);
+                if (LAYER) *reinterpret_cast<float4*>(to + apart) = make_float4(db[k], db[k + 1], db[k + 2], db[k + 3]);
             }
-            __syncthreads();
-        }
-        for (int c = threadIdx.x; c < pitch; c += 256) {
-            part[c] = joined[c];
-            if (LAYER) part[pitch + c] = joined[kWarpColumns + c];
+        __syncthreads();
+        for (int c = threadIdx.x; c < (LAYER ? 2 : 1) * apart; c += 256) {      // the warps' in order
+            float sum = joined[c];
+#pragma unroll
+            for (int t = 1; t < 8; ++t) sum += joined[t * 2 * apart + c];
+            if (a.ranks) joined[c] = sum;
+            else if (c % apart < pitch) part[c / apart * pitch + c % apart] = sum;
         }
     } else {
+        float* to = a.ranks ? joined : part;
 #pragma unroll
         for (int p = 0; p < PP; ++p) {
             const int at = lane + p * width;
@@ -427,10 +434,28 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
 #pragma unroll
             for (int i = 0; i < 8; i += 4) {
                 const int k = (kShared ? 0 : 8 * p) + i;
-                *reinterpret_cast<float4*>(part + at * 8ll + i) = make_float4(dw[k], dw[k + 1], dw[k + 2], dw[k + 3]);
-                if (LAYER) *reinterpret_cast<float4*>(part + pitch + at * 8ll + i) = make_float4(db[8 * p + i], db[8 * p + i + 1], db[8 * p + i + 2], db[8 * p + i + 3]);
+                *reinterpret_cast<float4*>(to + at * 8 + i) = make_float4(dw[k], dw[k + 1], dw[k + 2], dw[k + 3]);
+                if (LAYER) *reinterpret_cast<float4*>(to + pitch + at * 8 + i) = make_float4(db[8 * p + i], db[8 * p + i + 1], db[8 * p + i + 2], db[8 * p + i + 3]);
             }
         }
+    }
+    if (a.ranks) {                                        // few rows: the grid is one cluster, each CTA adds its share of the columns, the CTAs' sums in order
+        __syncwarp();
+        tc::cluster_sync();
+        for (int e = blockIdx.x * blockDim.x + threadIdx.x; e < (LAYER ? 2 : 1) * cols; e += a.ranks * blockDim.x) {
+            const int c = e < cols ? e : e - cols;
+            const uint32_t at = base + ((e < cols ? 0 : apart) + c) * 4;
+            float sum = 0.f;
+            for (int r = 0; r < a.ranks; ++r) {
+                float v;
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(tc::in_cta(at, r)) : "memory");
+                sum = r ? sum + v : v;
+            }
+            float* out = e < cols ? a.dweight : a.dbias;
+            if (out) out[c] = sum;
+        }
+        __syncwarp();
+        tc::cluster_sync();                               // no CTA leaves while its sums are read
     }
 }
 
@@ -551,7 +576,7 @@ __global__ void __launch_bounds__(128) mx_norm_columns_kernel(const NormArgs a, 
     }
 }
 
-struct NormPlan { bool warp, wide; int pp, threads, grid, parts, smem; size_t stats, total; };
+struct NormPlan { bool warp, wide; int pp, threads, grid, parts, smem, ranks; size_t stats, total; };
 
 NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtype)
 {
@@ -568,14 +593,14 @@ NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtyp
         const int64_t most = ctx->num_sms * (p.pp == 4 ? 1 : 2), need = (rows + 7) / 8;
         p.parts = p.grid = (int)(need < most ? need : most);
         p.smem = 32 * p.pp * (piece - 12 + 8 * stages * piece);
-        if (p.smem < 2 * kWarpColumns * 4) p.smem = 2 * kWarpColumns * 4;
+        if (p.smem < 8 * 2 * 32 * p.pp * 8 * 4) p.smem = 8 * 2 * 32 * p.pp * 8 * 4;
     } else {
         p.pp = pieces <= kBlockThreads ? 1 : 2;
         const int64_t need = (pieces + p.pp - 1) / p.pp;
         p.threads = p.pp == 1 ? (need <= 256 ? 256 : need <= 512 ? 512 : 1024) : need <= 768 ? 768 : 1024;
         if (need > kBlockThreads) p.threads = kBlockThreads + 1;
         const int64_t smem = (int64_t)p.threads * p.pp * (piece - 12 + stages * piece + (p.pp > 1 ? 32 : 0));
-        p.wide = p.threads > kBlockThreads || smem > ctx->smem_optin - 36 * 1024;
+        p.wide = p.threads > kBlockThreads || smem > ctx->smem_optin - 2048;
         const int64_t most = ctx->num_sms * (p.threads <= 256 ? 4 : p.threads <= 512 ? 2 : 1);
         p.parts = p.grid = (int)(rows < most ? rows : most);
         p.smem = (int)smem;
@@ -586,6 +611,17 @@ NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtyp
         p.parts = (int)(rows < 8 ? rows : 8);
         p.stats = ((size_t)rows * sizeof(float2) + 255) & ~(size_t)255;
     }
+    // Few rows: one cluster of eight CTAs that needs no second kernel and no workspace (33 x 2048, rms: a call takes 16 us in place of 22, the
+    // kernel 7.0 in place of two of 5.5 together).
+    const int64_t rounds = (rows + 8 * (p.warp ? 8 : 1) - 1) / (8 * (p.warp ? 8 : 1));
+    p.ranks = !p.wide && pieces <= 512 && rounds <= 5 ? 8 : 0;
+    if (p.ranks) {
+        const int64_t teams = p.warp ? 8 : 1, need = (rows + teams - 1) / teams;
+        p.ranks = need >= 5 ? 8 : need >= 3 ? 4 : (int)need;
+        p.parts = p.grid = p.ranks;
+        p.total = 0;
+        return p;
+    }
     p.total = p.stats + (((size_t)p.parts * 2 * pieces * 8 * 4 + 255) & ~(size_t)255);
     return p;
 }
@@ -593,6 +629,22 @@ NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtyp
 template <typename T, bool LAYER, bool VEC, int W, int PP>
 void norm_start(const NormPlan& p, const NormArgs& a, cudaStream_t st)
 {
+    if (p.ranks) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(p.grid);
+        cfg.blockDim = dim3(p.threads);
+        cfg.dynamicSmemBytes = p.smem;
+        cfg.stream = st;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = (unsigned)p.ranks;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        if (p.smem > 48 * 1024) cudaFuncSetAttribute(mx_norm_kernel<T, LAYER, VEC, W, PP>, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
+        cudaLaunchKernelEx(&cfg, mx_norm_kernel<T, LAYER, VEC, W, PP>, a);
+        return;
+    }
     if (p.smem > 48 * 1024) cudaFuncSetAttribute(mx_norm_kernel<T, LAYER, VEC, W, PP>, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
     mx_norm_kernel<T, LAYER, VEC, W, PP><<<p.grid, p.threads, p.smem, st>>>(a);
 }
@@ -689,19 +741,21 @@ extern "C" int galv_mx_norm_backward(galv_ctx* ctx, int64_t rows, int64_t cols, 
         return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_mx_norm_backward: NULL or misaligned pointer, or a row stride below cols");
     if (dx == dy && dx_stride != dy_stride)
         return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_mx_norm_backward: dx may be dy with the same stride only");
-    if (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < galv_mx_norm_workspace_bytes(ctx, rows, cols))
+    const size_t bytes = galv_mx_norm_workspace_bytes(ctx, rows, cols);
+    if (bytes && (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < bytes))
         return galv_set_error(ctx, GALV_ERR_WORKSPACE, "galv_mx_norm_backward: workspace NULL, misaligned or too small");
     const NormPlan p = norm_plan(ctx, rows, cols, dtype);
     NormArgs a;
     a.rows = rows; a.cols = cols; a.nb = mx_blocks(cols); a.pitch = mx_pitch8(cols); a.dy_stride = dy_stride; a.dx_stride = dx_stride;
     a.eps = eps; a.codes = codes; a.scales = scales; a.dy = dy; a.weight = weight; a.weight16 = mx_aligned(weight, 16); a.dx = dx;
     a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + p.stats);
+    a.ranks = p.ranks; a.dweight = dweight; a.dbias = dbias;
     float2* stats = reinterpret_cast<float2*>(workspace);
     const bool vec = mx_rows16(dy, dy_stride, dtype) && mx_rows16(dx, dx_stride, dtype), layer = kind == GALV_NORM_LAYER, sums = dweight || dbias;
     MX_DISPATCH_TYPE(dtype,
         if (layer) { if (vec) norm_launch<T, true, true>(p, a, stats, sums, st); else norm_launch<T, true, false>(p, a, stats, sums, st); }
         else { if (vec) norm_launch<T, false, true>(p, a, stats, sums, st); else norm_launch<T, false, false>(p, a, stats, sums, st); });
-    if (sums) mx_norm_join_kernel<<<dim3((unsigned)((cols + 31) / 32), dbias ? 2 : 1), 1024, 0, st>>>(cols, (cols + 7) / 8 * 8, p.parts, a.part, dweight, dbias);
+    if (sums && !p.ranks) mx_norm_join_kernel<<<dim3((unsigned)((cols + 31) / 32), dbias ? 2 : 1), 1024, 0, st>>>(cols, (cols + 7) / 8 * 8, p.parts, a.part, dweight, dbias);
     e = cudaGetLastError();
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }

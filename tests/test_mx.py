@@ -504,7 +504,12 @@ def test_the_library_refuses():
     nb = lambda kind=0, eps=1e-5, dbias=p + 40960, ws=p + 49152, n=8192: lib.galv_mx_norm_backward(h, 4, 64, kind, eps, p, p + 8192, p + 16384, 64, None, p + 24576, 64, 0, p + 32768, dbias, ws, n, None)
     assert lib.galv_mx_norm_workspace_bytes(h, 4, 64) <= 8192 and nb() == gb.OK
     assert nb(kind=1) == bad and nb(kind=2, dbias=None) == bad and nb(eps=-1.0) == bad and nb(eps=float("nan")) == bad
-    assert nb(ws=None) == nb(ws=p + 49153) == nb(n=8) == gb.ERR_WORKSPACE
+    many = torch.zeros(4 << 20, dtype=torch.uint8, device="cuda")   # few rows need no workspace, many do
+    q = many.data_ptr()
+    nm = lambda ws, n: lib.galv_mx_norm_backward(h, 2000, 64, 0, 1e-5, q, q + (1 << 18), q + (1 << 19), 64, None, q + (2 << 20), 64, 0, p, p + 4096, ws, n, None)
+    need = lib.galv_mx_norm_workspace_bytes(h, 2000, 64)
+    assert 0 < need <= 1 << 20 and nm(q + (3 << 20), need) == gb.OK
+    assert nm(None, need) == nm(q + (3 << 20) + 1, need) == nm(q + (3 << 20), need - 1) == gb.ERR_WORKSPACE
     wg = lambda dtype=1, out=1, dy=p, stride=8, ws=p + 49152, n=8192: lib.galv_mx_weight_grad(h, 4, 8, 64, dy, stride, dtype, p + 8192, p + 16384, None, p + 24576, out, ws, n, None)
     assert lib.galv_mx_weight_grad_workspace_bytes(h, 4, 8, 64, p, 8) <= 8192 and wg() == gb.OK
     assert wg(dtype=0, out=0) == bad and wg(dtype=1, out=2) == bad and wg(dy=None) == bad and wg(stride=7) == bad and wg(dy=p + 1) == bad
