@@ -135,39 +135,6 @@ template <typename T> __device__ __forceinline__ void mx_floats(const MxPiece<T>
     for (int i = 0; i < 8; ++i) v[i] = mx_float(e[i]);
 }
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void mx_load8(const T* __restrict__ row, int c0, int cols, float (&v)[8])
-{
-    if (VEC && c0 + 8 <= cols) {
-        MxPiece<T> p;
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) p.q[i] = __ldg(reinterpret_cast<const uint4*>(row + c0) + i);
-        const T* e = reinterpret_cast<const T*>(&p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = mx_float(e[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c0 + i < cols ? mx_float(row[c0 + i]) : 0.f;
-    }
-}
-
-// ... of a matrix that the same kernel may write (in place): not by the read-only path.
-template <typename T, bool VEC>
-__device__ __forceinline__ void mx_load8_rw(const T* row, int c0, int cols, float (&v)[8])
-{
-    if (VEC && c0 + 8 <= cols) {
-        MxPiece<T> p;
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) p.q[i] = reinterpret_cast<const uint4*>(row + c0)[i];
-        const T* e = reinterpret_cast<const T*>(&p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = mx_float(e[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c0 + i < cols ? mx_float(row[c0 + i]) : 0.f;
-    }
-}
-
 template <typename T> __device__ __forceinline__ MxPiece<T> mx_piece(const float (&v)[8])
 {
     MxPiece<T> p;

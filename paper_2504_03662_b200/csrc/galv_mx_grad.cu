@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
             if (row < rows && c < pieces) {
                 code[h] = __ldg(reinterpret_cast<const uint2*>(held));
                 byte[h] = __ldg(power);
-                raw[h] = mx_fetch8<T, VEC>(from, (int)c * 8, cols, spread.log >= 5);
+                raw[h] = mx_fetch8<T, VEC>(from, (int)c * 8, cols, spread.log >= 5 && dx != dy);      // in place, a neighbour may write meanwhile
             } else if (!VEC) {
                 code[h] = make_uint2(0, 0);
                 byte[h] = 0;
@@ -144,6 +144,7 @@ struct NormArgs {
     void* dx;
     float* part;                                          // [parts][2][cols]: dweight, dbias
     int ranks;                                            // CTAs of the one cluster that finishes dweight and dbias itself, or 0
+    int share, span;                                      // SPLIT: CTAs of a cluster that share a row, pieces of it that each has (a multiple of 16)
     float* dweight;
     float* dbias;
 };
@@ -214,24 +215,62 @@ __device__ __forceinline__ float row_sum(float a, float* red)
     return a;
 }
 
+// Sums over the threads of a cluster's CTAs: each warp's go to all of them.
+template <int W, int N>
+__device__ __forceinline__ float4 split_sums(const float4& v, float4* red, int share, int rank)
+{
+    float c = warp_sums(v);
+    const int lane = threadIdx.x % 32, q = lane % 8;
+    if (q < share) asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(tc::in_cta(tc::smem_at(red + rank * (W / 32) + threadIdx.x / 32) + lane / 8 * 4, q)), "f"(c) : "memory");
+    __syncwarp();
+    tc::cluster_sync();
+    float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int e = lane; e < share * (W / 32); e += 32) {
+        const float4 o = red[e];
+        r.x += o.x; r.y += o.y; r.z += o.z;
+    }
+    c = warp_sums(r);
+    r.x = __shfl_sync(0xffffffffu, c, 0);
+    if (N > 1) r.y = __shfl_sync(0xffffffffu, c, 8);
+    if (N > 2) r.z = __shfl_sync(0xffffffffu, c, 16);
+    return r;
+}
+template <int W>
+__device__ __forceinline__ float split_sum(float a, float* red, int share, int rank)
+{
+#pragma unroll
+    for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+    const int lane = threadIdx.x % 32;
+    if (lane < share) asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(tc::in_cta(tc::smem_at(red + rank * (W / 32) + threadIdx.x / 32), lane)), "f"(a) : "memory");
+    __syncwarp();
+    tc::cluster_sync();
+    a = 0.f;
+    for (int e = lane; e < share * (W / 32); e += 32) a += red[e];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+    return a;
+}
+
 template <typename T> struct NormStage {
     static constexpr int count = 2;
     static constexpr int piece = 8 * (int)sizeof(T) + 8 + 4;               // bytes: dy, codes, the word that has the scale byte
 };
 
-// W: threads that share a row (32: a warp, eight rows a CTA; else the CTA); PP: pieces of 8 columns a thread.
-template <typename T, bool LAYER, bool VEC, int W, int PP>
+// W: threads that share a row (32: a warp, eight rows a CTA; else the CTA); PP: pieces of 8 columns a thread; SPLIT: the row is shared by a cluster's CTAs.
+template <typename T, bool LAYER, bool VEC, int W, int PP, bool SPLIT>
 __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) : W <= 256 ? 4 : W <= 512 ? 2 : 1) mx_norm_kernel(const __grid_constant__ NormArgs a)
 {
     constexpr bool WARP = W == 32;
     constexpr int NS = NormStage<T>::count, kDy = 8 * (int)sizeof(T);
     extern __shared__ __align__(16) unsigned char raw[];
     constexpr bool kShared = !WARP && PP > 1;             // dweight's sums lie in shared memory
-    __shared__ float4 red[2][32];
-    __shared__ float red1[2][32];
+    __shared__ float4 red[2][SPLIT ? W / 4 : 32];
+    __shared__ float red1[2][SPLIT ? W / 4 : 32];
     constexpr int teams = WARP ? 8 : 1, width = W, slots = W * PP;
     const int team = WARP ? threadIdx.x / 32 : 0, lane = WARP ? threadIdx.x % 32 : threadIdx.x;
-    const int pieces = (int)((a.cols + 7) / 8);
+    const int share = SPLIT ? a.share : 1, rank = SPLIT ? (int)tc::cluster_rank() : 0, lead = SPLIT ? rank * a.span * 8 : 0;      // lead: this CTA's first column
+    const int cols = SPLIT ? max(0, min((int)a.cols - lead, a.span * 8)) : (int)a.cols, pieces = (cols + 7) / 8;
+    const T* weight = (const T*)a.weight + lead;
     const float inv_n = 1.f / (float)a.cols;
     // weights [slots][8], then each team's stages of dy [slots][8], codes [slots][8 bytes], scale words [slots], then sums [2][slots][4]
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(raw), mine = base + slots * kDy + team * NS * slots * NormStage<T>::piece;
@@ -239,21 +278,20 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
     // rows off 16-byte boundaries are not staged: the first stage's place of dy is where a warp's results are put together
     T* const buf = reinterpret_cast<T*>(raw + (mine - base) + (WARP ? 0 : (threadIdx.x & ~31) * kDy));
     for (int c = threadIdx.x * 8; c < slots * 8; c += (WARP ? 256 : W) * 8) {
-        float w[8];
-        if (a.weight && c < a.cols) {
-            if (a.weight16) mx_load8<T, true>((const T*)a.weight, c, (int)a.cols, w);
-            else mx_load8<T, false>((const T*)a.weight, c, (int)a.cols, w);
+        MxPiece<T> piece;
+        if (a.weight && c < cols) {
+            piece = a.weight16 ? mx_fetch8<T, true>(weight, c, cols) : mx_fetch8<T, false>(weight, c, cols);
         } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = 1.f;
+            const float ones[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+            piece = mx_piece<T>(ones);
         }
-        const MxPiece<T> piece = mx_piece<T>(w);
 #pragma unroll
         for (int i = 0; i < kDy / 16; ++i) *reinterpret_cast<uint4*>(raw + c * (int)sizeof(T) + i * 16) = piece.q[i];
     }
     // pieces behind the row's end stay zeros
     for (int e = lane; e < NS * slots * NormStage<T>::piece / 4; e += W) asm volatile("st.shared.b32 [%0], %1;" :: "r"(mine + e * 4), "r"(0) : "memory");
-    __syncthreads();
+    if (SPLIT) tc::cluster_sync();
+    else __syncthreads();
 
     float dw[kShared ? 8 : PP * 8] = {}, db[LAYER ? PP * 8 : 1] = {};
     auto sums_load = [&](int p) {
@@ -270,12 +308,11 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
 #pragma unroll
         for (int p = 0; p < PP; ++p) sums_store(p);
     }
-    const long long first = (long long)blockIdx.x * teams + team, step = (long long)gridDim.x * teams;
-    const uint8_t* codes = a.codes + first * a.nb * 32 + lane * 8;
-    const uint8_t* scales = a.scales + first * a.pitch;
-    const T* dy = (const T*)a.dy + first * a.dy_stride + lane * 8;
-    T* dx = (T*)a.dx + first * a.dx_stride;
-    const int cols = (int)a.cols;
+    const long long first = (long long)(blockIdx.x / share) * teams + team, step = (long long)(gridDim.x / share) * teams;
+    const uint8_t* codes = a.codes + first * a.nb * 32 + lead + lane * 8;
+    const uint8_t* scales = a.scales + first * a.pitch + lead / 32;
+    const T* dy = (const T*)a.dy + first * a.dy_stride + lead + lane * 8;
+    T* dx = (T*)a.dx + first * a.dx_stride + lead;
     long long ahead = first;
     auto fetch = [&](int stage) {
         if (ahead < a.rows) {
@@ -331,7 +368,7 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
                 for (int i = 0; i < kDy / 16; ++i)
                     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(d[p].q[i].x), "=r"(d[p].q[i].y), "=r"(d[p].q[i].z), "=r"(d[p].q[i].w) : "r"(from + at * kDy + i * 16));
             } else {
-                const MxPiece<T> piece = mx_fetch8<T, false>((const T*)a.dy + row * a.dy_stride, at * 8, cols);
+                const MxPiece<T> piece = mx_fetch8<T, false>((const T*)a.dy + row * a.dy_stride + lead, at * 8, cols);
 #pragma unroll
                 for (int i = 0; i < kDy / 16; ++i) d[p].q[i] = piece.q[i];
             }
@@ -350,7 +387,7 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
             m.x = LAYER ? fmaf(sx, s[p], m.x) : fmaf(sx * s[p], s[p], m.x);
             m.z = fmaf(sgx, s[p], m.z);
         }
-        m = row_sums<W, 3>(m, red[turn]);
+        m = SPLIT ? split_sums<W, 3>(m, red[turn], share, rank) : row_sums<W, 3>(m, red[turn]);
         float mean = 0.f, mg = 0.f, sq = m.x, sgx = m.z;
         if (LAYER) {
             mean = m.x * inv_n;
@@ -373,7 +410,7 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
                 for (int i = 0; i < 8; ++i) sq = fmaf(x[8 * p + i], x[8 * p + i], sq);
             }
         }
-        if (LAYER) sq = row_sum<W>(sq, red1[turn]);
+        if (LAYER) sq = SPLIT ? split_sum<W>(sq, red1[turn], share, rank) : row_sum<W>(sq, red1[turn]);
         const float r = 1.f / sqrtf(sq * inv_n + a.eps), c = -sgx * inv_n * r * r * r, mr = -mg * r;
 #pragma unroll
         for (int p = 0; p < PP; ++p) {
@@ -398,8 +435,8 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
         }
     }
     // this CTA's column sums
-    const int pitch = pieces * 8;
-    float* part = a.part + (long long)blockIdx.x * 2 * pitch;
+    const int pitch = SPLIT ? (int)((a.cols + 7) / 8 * 8) : pieces * 8;
+    float* part = a.part + (long long)(blockIdx.x / share) * 2 * pitch + lead;
     float* joined = reinterpret_cast<float*>(raw);        // over what is not read any more: [2][apart] (a warp a row: [team][2][apart])
     const int apart = WARP ? slots * 8 : pitch;
     if (WARP || a.ranks) {
@@ -492,7 +529,7 @@ __device__ __forceinline__ float block_sum(float v, float* red)
     return s;
 }
 
-// Rows too long for registers: a CTA goes over its row four times (the first reads it, the others find it in the caches).  Mean and 1/sqrt(var + eps) stay for
+// Rows too long for a cluster's registers: a CTA goes over its row four times (the first reads it, the others find it in the caches).  Mean and 1/sqrt(var + eps) stay for
 // the column sums, which come first where dx may be dy: this kernel runs without dx before them and with it after them.
 template <typename T, bool LAYER, bool VEC>
 __global__ void __launch_bounds__(512) mx_norm_wide_kernel(const NormArgs a, float2* stats, bool last)
@@ -529,8 +566,8 @@ __global__ void __launch_bounds__(512) mx_norm_wide_kernel(const NormArgs a, flo
         float sg = 0.f, sgx = 0.f;
         for (long long c = threadIdx.x; c < pieces; c += 512) {
             mx_restore8(a.codes, a.scales, row, (int)c, a.nb, a.pitch, x);
-            mx_load8_rw<T, VEC>(dy, (int)c * 8, (int)a.cols, g);
-            if (a.weight) mx_load8<T, false>((const T*)a.weight, (int)c * 8, (int)a.cols, w);
+            mx_floats(mx_fetch8<T, VEC>(dy, (int)c * 8, (int)a.cols, false), g);
+            if (a.weight) mx_floats(mx_fetch8<T, false>((const T*)a.weight, (int)c * 8, (int)a.cols), w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float gw = a.weight ? g[i] * w[i] : g[i];
@@ -541,8 +578,8 @@ __global__ void __launch_bounds__(512) mx_norm_wide_kernel(const NormArgs a, flo
         const float mg = LAYER ? block_sum(sg, red) * inv_n : 0.f, m = block_sum(sgx, red) * inv_n * rstd * rstd;
         for (long long c = threadIdx.x; c < pieces; c += 512) {
             mx_restore8(a.codes, a.scales, row, (int)c, a.nb, a.pitch, x);
-            mx_load8_rw<T, VEC>(dy, (int)c * 8, (int)a.cols, g);
-            if (a.weight) mx_load8<T, false>((const T*)a.weight, (int)c * 8, (int)a.cols, w);
+            mx_floats(mx_fetch8<T, VEC>(dy, (int)c * 8, (int)a.cols, false), g);
+            if (a.weight) mx_floats(mx_fetch8<T, false>((const T*)a.weight, (int)c * 8, (int)a.cols), w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) g[i] = rstd * ((a.weight ? g[i] * w[i] : g[i]) - mg - (x[i] - mean) * m);
             mx_store8<T, VEC>(dx, (int)c * 8, (int)a.cols, mx_piece<T>(g));
@@ -560,7 +597,7 @@ __global__ void __launch_bounds__(128) mx_norm_columns_kernel(const NormArgs a, 
     for (long long row = blockIdx.y; row < a.rows; row += gridDim.y) {
         const float2 st = stats[row];
         mx_restore8(a.codes, a.scales, row, (int)c, a.nb, a.pitch, x);
-        mx_load8_rw<T, VEC>((const T*)a.dy + row * a.dy_stride, (int)c * 8, (int)a.cols, g);
+        mx_floats(mx_fetch8<T, VEC>((const T*)a.dy + row * a.dy_stride, (int)c * 8, (int)a.cols, false), g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             dw[i] = fmaf(g[i], (x[i] - st.x) * st.y, dw[i]);
@@ -576,7 +613,7 @@ __global__ void __launch_bounds__(128) mx_norm_columns_kernel(const NormArgs a, 
     }
 }
 
-struct NormPlan { bool warp, wide; int pp, threads, grid, parts, smem, ranks; size_t stats, total; };
+struct NormPlan { bool warp, wide; int pp, threads, grid, parts, smem, ranks, share, span; size_t stats, total; };
 
 NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtype)
 {
@@ -585,6 +622,8 @@ NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtyp
     const bool four = dtype == GALV_F32;
     const int stages = four ? NormStage<float>::count : NormStage<__half>::count, piece = four ? NormStage<float>::piece : NormStage<__half>::piece;
     p.stats = 0;
+    p.share = 1;
+    p.span = 0;
     p.wide = false;
     p.warp = cols <= kWarpColumns;
     if (p.warp) {
@@ -605,6 +644,23 @@ NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtyp
         p.parts = p.grid = (int)(rows < most ? rows : most);
         p.smem = (int)smem;
     }
+    // A row that one CTA cannot hold is shared by two of a cluster, which exchange its sums over a cluster barrier, up to 16384 columns of fp32 and 32768
+    // of 16 bits, or four, up to 65536: 2048 x 12288 in fp32 takes 114 us for a layer norm, 300 with the kernels for wide rows; 1024 x 32768 in bf16
+    // 102 and 173; 512 x 49152 87 and 128.  What one CTA holds it keeps (2048 x 12288 in bf16: 53 us, shared by two 90), and fp32 shared by four
+    // is no faster than the wide kernels (1024 x 32768: 220 to 275 us and 233).  With four, 32 clusters run at once, not 37.
+    const int64_t most_pieces = four ? 1024 : 2048;       // of a CTA
+    const int clusters = four || pieces <= 2 * most_pieces ? 2 : 4;
+    if (p.wide && pieces <= clusters * most_pieces) {
+        p.wide = false;
+        p.share = clusters;
+        p.pp = four ? 1 : 2;
+        p.span = (int)((pieces + p.share - 1) / p.share + 15) / 16 * 16;
+        p.threads = p.span <= 768 * p.pp ? 768 : 1024;
+        p.smem = p.threads * p.pp * (piece - 12 + stages * piece + (p.pp > 1 ? 32 : 0));
+        const int64_t most = (p.share == 2 ? ctx->num_sms : ctx->num_sms * 7 / 8) / p.share;
+        p.parts = (int)(rows < most ? rows : most);
+        p.grid = p.parts * p.share;
+    }
     if (p.wide) {
         p.threads = 512;
         p.grid = (int)(rows < ctx->num_sms * 4 ? rows : ctx->num_sms * 4);
@@ -614,7 +670,7 @@ NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtyp
     // Few rows: one cluster of eight CTAs that needs no second kernel and no workspace (33 x 2048, rms: a call takes 16 us in place of 22, the
     // kernel 7.0 in place of two of 5.5 together).
     const int64_t rounds = (rows + 8 * (p.warp ? 8 : 1) - 1) / (8 * (p.warp ? 8 : 1));
-    p.ranks = !p.wide && pieces <= 512 && rounds <= 5 ? 8 : 0;
+    p.ranks = !p.wide && p.share == 1 && pieces <= 512 && rounds <= 5 ? 8 : 0;
     if (p.ranks) {
         const int64_t teams = p.warp ? 8 : 1, need = (rows + teams - 1) / teams;
         p.ranks = need >= 5 ? 8 : need >= 3 ? 4 : (int)need;
@@ -626,10 +682,12 @@ NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtyp
     return p;
 }
 
-template <typename T, bool LAYER, bool VEC, int W, int PP>
+template <typename T, bool LAYER, bool VEC, int W, int PP, bool SPLIT = false>
 void norm_start(const NormPlan& p, const NormArgs& a, cudaStream_t st)
 {
-    if (p.ranks) {
+    const auto kernel = mx_norm_kernel<T, LAYER, VEC, W, PP, SPLIT>;
+    if (p.smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
+    if (p.ranks || SPLIT) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(p.grid);
         cfg.blockDim = dim3(p.threads);
@@ -637,16 +695,14 @@ void norm_start(const NormPlan& p, const NormArgs& a, cudaStream_t st)
         cfg.stream = st;
         cudaLaunchAttribute attr;
         attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim.x = (unsigned)p.ranks;
+        attr.val.clusterDim.x = (unsigned)(SPLIT ? p.share : p.ranks);
         attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        if (p.smem > 48 * 1024) cudaFuncSetAttribute(mx_norm_kernel<T, LAYER, VEC, W, PP>, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
-        cudaLaunchKernelEx(&cfg, mx_norm_kernel<T, LAYER, VEC, W, PP>, a);
+        cudaLaunchKernelEx(&cfg, kernel, a);
         return;
     }
-    if (p.smem > 48 * 1024) cudaFuncSetAttribute(mx_norm_kernel<T, LAYER, VEC, W, PP>, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem);
-    mx_norm_kernel<T, LAYER, VEC, W, PP><<<p.grid, p.threads, p.smem, st>>>(a);
+    kernel<<<p.grid, p.threads, p.smem, st>>>(a);
 }
 
 template <typename T, bool LAYER, bool VEC>
@@ -656,6 +712,10 @@ void norm_launch(const NormPlan& p, const NormArgs& a, float2* stats, bool sums,
         mx_norm_wide_kernel<T, LAYER, VEC><<<p.grid, 512, 0, st>>>(a, stats, false);
         if (sums) mx_norm_columns_kernel<T, VEC><<<dim3((unsigned)((a.cols + 1023) / 1024), p.parts), 128, 0, st>>>(a, stats);
         mx_norm_wide_kernel<T, LAYER, VEC><<<p.grid, 512, 0, st>>>(a, stats, true);
+    } else if (p.share > 1) {
+        constexpr int PP = sizeof(T) == 4 ? 1 : 2;
+        if (p.threads == 768) norm_start<T, LAYER, VEC, 768, PP, true>(p, a, st);
+        else norm_start<T, LAYER, VEC, 1024, PP, true>(p, a, st);
     } else if (p.warp) {
         if (p.pp == 1) norm_start<T, LAYER, VEC, 32, 1>(p, a, st);
         else if (p.pp == 2) norm_start<T, LAYER, VEC, 32, 2>(p, a, st);
@@ -749,7 +809,7 @@ extern "C" int galv_mx_norm_backward(galv_ctx* ctx, int64_t rows, int64_t cols, 
     a.rows = rows; a.cols = cols; a.nb = mx_blocks(cols); a.pitch = mx_pitch8(cols); a.dy_stride = dy_stride; a.dx_stride = dx_stride;
     a.eps = eps; a.codes = codes; a.scales = scales; a.dy = dy; a.weight = weight; a.weight16 = mx_aligned(weight, 16); a.dx = dx;
     a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + p.stats);
-    a.ranks = p.ranks; a.dweight = dweight; a.dbias = dbias;
+    a.ranks = p.ranks; a.share = p.share; a.span = p.span; a.dweight = dweight; a.dbias = dbias;
     float2* stats = reinterpret_cast<float2*>(workspace);
     const bool vec = mx_rows16(dy, dy_stride, dtype) && mx_rows16(dx, dx_stride, dtype), layer = kind == GALV_NORM_LAYER, sums = dweight || dbias;
     MX_DISPATCH_TYPE(dtype,

@@ -372,6 +372,15 @@ def test_norm_backward(rows, cols, pad, weighted, dtype, kind):
 
 
 @gpu
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("dtype,rows,cols,pad", [("f32", 300, 12008, 0), ("f32", 77, 16384, 3), ("f32", 2, 16385, 0), ("bf16", 230, 16390, 1), ("f16", 75, 32768, 0), ("f16", 100, 32769, 7),
+                                                 ("bf16", 33, 65536, 0), ("bf16", 2, 65537, 0)])
+def test_norm_backward_of_shared_rows(dtype, rows, cols, pad, kind):
+    """Rows that two or four CTAs share, several a cluster, and both sides of the widths where the way changes."""
+    test_norm_backward(rows, cols, pad, True, dtype, kind)
+
+
+@gpu
 def test_norm_backward_of_odd_rows():
     x = torch.ones(4, 64)
     x[1] = 0
