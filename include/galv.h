@@ -469,7 +469,7 @@ int galv_mx_act_backward(galv_ctx* ctx, int64_t rows, int64_t cols, int32_t act,
  * dweight = sum over rows of dy * xhat, dbias = sum over rows of dy (both fp32 [cols]; summed in a fixed order: the same call
  * gives the same bits).  dweight may be NULL, dbias must be NULL for GALV_NORM_RMS and may be for the other.  eps >= 0;
  * a row of equal values with eps = 0 gives NaN or infinity as the formula does.  With rows = 0 dweight and dbias are zeros.
- * dx may be dy (same pointer and stride).  workspace: 256-byte aligned; it holds partial sums.
+ * dx may be dy (same pointer and stride).  workspace: 256-byte aligned, the bytes that the query gives (0, for few rows: may be NULL).
  */
 size_t galv_mx_norm_workspace_bytes(const galv_ctx* ctx, int64_t rows, int64_t cols);
 int galv_mx_norm_backward(galv_ctx* ctx, int64_t rows, int64_t cols, int32_t kind, float eps, const uint8_t* codes,

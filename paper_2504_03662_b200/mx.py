@@ -5,6 +5,9 @@ microscaled choices out.  The functions allocate their results through PyTorch a
 current stream of the tensors' device; formats and formulas are those of include/galv.h.  `linear`, `norm` and
 `activation` are the same as differentiable functions: their inputs are kept in 8 bits for the backward pass.
 
+Calls and backward passes may be captured in a CUDA graph under PyTorch's rules: after the same call has run once on a
+side stream, and for a backward pass with no eager graph of the same leaves alive.
+
 A context of the library belongs to one host thread, so every thread (the autograd engine's among them) gets its own
 for each device.
 """
@@ -268,7 +271,7 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
     """x weight^T + bias (bf16 or fp16), x kept in 8 bits for the weight's gradient.  `four`: the forward product takes both operands in
     4 bits; the gradients are those of the product of the unrounded operands (straight through the rounding)."""
     _kind(x.dtype, "x", _SHORT)
-    if weight.dim() != 2 or weight.dtype != x.dtype or weight.shape[1] != x.shape[-1]:
+    if weight.dim() != 2 or weight.dtype != x.dtype or weight.shape[0] < 1 or weight.shape[1] != x.shape[-1]:
         raise ValueError(f"weight of shape {tuple(weight.shape)} and {weight.dtype} beside x of {tuple(x.shape)} and {x.dtype}")
     return _Linear.apply(x, weight, bias, four)
 

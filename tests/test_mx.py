@@ -160,6 +160,7 @@ def _fake(rows=4, cols=64, fmt=8):
     lambda: mx.matmul(_fake(fmt=4), _fake(fmt=4), bias=torch.zeros(4)),
     lambda: mx.linear(torch.zeros(4, 64), torch.zeros(8, 64)),
     lambda: mx.linear(torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(8, 63, dtype=torch.bfloat16)),
+    lambda: mx.linear(torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(0, 64, dtype=torch.bfloat16)),      # no such weight gradient
     lambda: mx.norm(torch.zeros(4, 64), bias=torch.zeros(64), kind="rms"),
     lambda: mx.norm(torch.zeros(4, 64), torch.ones(64, dtype=torch.bfloat16)),      # would only show in the backward pass
     lambda: mx.activation(torch.zeros(4, 64), "relu"),
