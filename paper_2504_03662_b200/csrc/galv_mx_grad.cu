@@ -127,8 +127,8 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
 // One pass: a row's codes and gradient are read once, its statistics and the two means of the gradient come from registers, and the column sums stay with
 // the thread that has the column, over all rows that its CTA takes (where a thread has two pieces of 8 columns, dweight's in shared memory: with both sums in
 // registers only half as many threads fit, and the pass took twice as long).  The next rows are on their way into shared memory
-// meanwhile, each thread's pieces its own, so that only the rows' sums need a barrier.  2048 x 12288 in bf16 take 51 us for a layer norm and 43 for an
-// rms norm (2.4 and 3.0 TB/s): 37 instructions an element at 54 % of the issue slots, the rest waits for shuffles and shared memory.
+// meanwhile, each thread's pieces its own, so that only the rows' sums need a barrier.  2048 x 12288 in bf16 take 53 us for a layer norm and 42 for an
+// rms norm (2.4 and 3.0 TB/s): some 37 instructions an element at 54 % of the issue slots, the rest waits for shuffles, shared memory and the row's sums.
 
 constexpr int kBlockThreads = 1024;
 constexpr int kWarpColumns = 1024;                        // up to here a warp has a row to itself, and no barrier
@@ -184,72 +184,57 @@ __device__ __forceinline__ float warp_sums(const float4& v)
     for (int o = 4; o; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
     return c;
 }
-// Sums of up to four values over the threads that share a row: a warp, or the CTA (one barrier; `red` is another one in turn).
-template <int W, int N>
-__device__ __forceinline__ float4 row_sums(const float4& v, float4* red)
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// Sums over the threads that share a row: a warp, a CTA (one barrier; `red` is another one in turn) or a cluster's CTAs (SPLIT: each warp's sums go to all of
+// them).  SQUARES: w is a sum of squares around the mean of the warp's values, whose sum is x; it becomes that around the mean of all (the squares of the
+// distances between the means, times the values behind them, are added), so that mean and deviation take one barrier, not two (2048 x 12288 in fp32,
+// shared by two CTAs: 104 us and 114; no difference within one CTA).  counts: values of each warp, and one over it.
+template <int W, bool SPLIT, bool SQUARES>
+__device__ __forceinline__ float4 row_sums(const float4& v, float4* red, const float2* counts, float inv_n, int share, int rank)
 {
     float c = warp_sums(v);
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, entries = (SPLIT ? share : 1) * (W / 32);
     if (W > 32) {
-        if (threadIdx.x % 8 == 0) reinterpret_cast<float*>(red)[threadIdx.x / 32 * 4 + threadIdx.x % 32 / 8] = c;
-        __syncthreads();
-        c = warp_sums(threadIdx.x % 32 < W / 32 ? red[threadIdx.x % 32] : make_float4(0.f, 0.f, 0.f, 0.f));
+        float* to = reinterpret_cast<float*>(red + (SPLIT ? rank * (W / 32) : 0) + warp) + lane / 8;
+        if (SPLIT) {
+            if (lane % 8 < share) asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(tc::in_cta(tc::smem_at(to), lane % 8)), "f"(c) : "memory");
+            __syncwarp();
+            tc::cluster_sync();
+        } else {
+            if (lane % 8 == 0) *to = c;
+            __syncthreads();
+        }
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int e = lane; e < entries; e += 32) {
+            const float4 o = red[e];
+            sum.x += o.x; sum.y += o.y; sum.z += o.z;
+        }
+        c = warp_sums(sum);
     }
-    float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 r;
     r.x = __shfl_sync(0xffffffffu, c, 0);
-    if (N > 1) r.y = __shfl_sync(0xffffffffu, c, 8);
-    if (N > 2) r.z = __shfl_sync(0xffffffffu, c, 16);
+    r.y = __shfl_sync(0xffffffffu, c, 8);
+    r.z = __shfl_sync(0xffffffffu, c, 16);
+    r.w = 0.f;
+    if (W == 32) {
+        r.w = __shfl_sync(0xffffffffu, c, 24);
+    } else if (SQUARES) {
+        for (int e = lane; e < entries; e += 32) {
+            const float2 n = counts[e];
+            const float apart = red[e].x * n.y - r.x * inv_n;
+            r.w += fmaf(apart * apart, n.x, red[e].w);
+        }
+        r.w = warp_sum(r.w);
+    }
     return r;
-}
-// ... of one.
-template <int W>
-__device__ __forceinline__ float row_sum(float a, float* red)
-{
-#pragma unroll
-    for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-    if (W == 32) return a;
-    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = a;
-    __syncthreads();
-    a = threadIdx.x % 32 < W / 32 ? red[threadIdx.x % 32] : 0.f;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-    return a;
 }
 
-// Sums over the threads of a cluster's CTAs: each warp's go to all of them.
-template <int W, int N>
-__device__ __forceinline__ float4 split_sums(const float4& v, float4* red, int share, int rank)
-{
-    float c = warp_sums(v);
-    const int lane = threadIdx.x % 32, q = lane % 8;
-    if (q < share) asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(tc::in_cta(tc::smem_at(red + rank * (W / 32) + threadIdx.x / 32) + lane / 8 * 4, q)), "f"(c) : "memory");
-    __syncwarp();
-    tc::cluster_sync();
-    float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int e = lane; e < share * (W / 32); e += 32) {
-        const float4 o = red[e];
-        r.x += o.x; r.y += o.y; r.z += o.z;
-    }
-    c = warp_sums(r);
-    r.x = __shfl_sync(0xffffffffu, c, 0);
-    if (N > 1) r.y = __shfl_sync(0xffffffffu, c, 8);
-    if (N > 2) r.z = __shfl_sync(0xffffffffu, c, 16);
-    return r;
-}
-template <int W>
-__device__ __forceinline__ float split_sum(float a, float* red, int share, int rank)
-{
-#pragma unroll
-    for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-    const int lane = threadIdx.x % 32;
-    if (lane < share) asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(tc::in_cta(tc::smem_at(red + rank * (W / 32) + threadIdx.x / 32), lane)), "f"(a) : "memory");
-    __syncwarp();
-    tc::cluster_sync();
-    a = 0.f;
-    for (int e = lane; e < share * (W / 32); e += 32) a += red[e];
-#pragma unroll
-    for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-    return a;
-}
+constexpr int kMostShare = 4;                             // CTAs that share a row
 
 template <typename T> struct NormStage {
     static constexpr int count = 2;
@@ -264,8 +249,9 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
     constexpr int NS = NormStage<T>::count, kDy = 8 * (int)sizeof(T);
     extern __shared__ __align__(16) unsigned char raw[];
     constexpr bool kShared = !WARP && PP > 1;             // dweight's sums lie in shared memory
-    __shared__ float4 red[2][SPLIT ? W / 4 : 32];
-    __shared__ float red1[2][SPLIT ? W / 4 : 32];
+    constexpr int kEntries = W / 32 * (SPLIT ? kMostShare : 1);
+    __shared__ float4 red[2][kEntries];
+    __shared__ float2 counts[kEntries];
     constexpr int teams = WARP ? 8 : 1, width = W, slots = W * PP;
     const int team = WARP ? threadIdx.x / 32 : 0, lane = WARP ? threadIdx.x % 32 : threadIdx.x;
     const int share = SPLIT ? a.share : 1, rank = SPLIT ? (int)tc::cluster_rank() : 0, lead = SPLIT ? rank * a.span * 8 : 0;      // lead: this CTA's first column
@@ -290,8 +276,16 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
     }
     // pieces behind the row's end stay zeros
     for (int e = lane; e < NS * slots * NormStage<T>::piece / 4; e += W) asm volatile("st.shared.b32 [%0], %1;" :: "r"(mine + e * 4), "r"(0) : "memory");
+    if (LAYER && !WARP && threadIdx.x < share * (W / 32)) {
+        const int r = threadIdx.x / (W / 32), w = threadIdx.x % (W / 32), there = SPLIT ? max(0, min((int)a.cols - r * a.span * 8, a.span * 8)) : cols;
+        int n = 0;
+#pragma unroll
+        for (int p = 0; p < PP; ++p) n += max(0, min(256, there - (w * 32 + p * width) * 8));
+        counts[threadIdx.x] = make_float2((float)n, n ? 1.f / (float)n : 0.f);
+    }
     if (SPLIT) tc::cluster_sync();
     else __syncthreads();
+    const float inv_warp = LAYER ? WARP ? inv_n : counts[rank * (W / 32) + threadIdx.x / 32].y : 0.f;
 
     float dw[kShared ? 8 : PP * 8] = {}, db[LAYER ? PP * 8 : 1] = {};
     auto sums_load = [&](int p) {
@@ -387,19 +381,13 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
             m.x = LAYER ? fmaf(sx, s[p], m.x) : fmaf(sx * s[p], s[p], m.x);
             m.z = fmaf(sgx, s[p], m.z);
         }
-        m = SPLIT ? split_sums<W, 3>(m, red[turn], share, rank) : row_sums<W, 3>(m, red[turn]);
-        float mean = 0.f, mg = 0.f, sq = m.x, sgx = m.z;
-        if (LAYER) {
-            mean = m.x * inv_n;
-            mg = m.y * inv_n;
-            sgx -= mean * m.y;
-            sq = 0.f;
-        }
+        float near = 0.f;
+        if (LAYER) {                                      // the values around the warp's mean
+            near = warp_sum(m.x) * inv_warp;
 #pragma unroll
-        for (int p = 0; p < PP; ++p) {
+            for (int p = 0; p < PP; ++p) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[8 * p + i] = LAYER ? fmaf(x[8 * p + i], s[p], -mean) : x[8 * p + i] * s[p];
-            if (LAYER) {
+                for (int i = 0; i < 8; ++i) x[8 * p + i] = fmaf(x[8 * p + i], s[p], -near);
                 const int left = cols - (lane + p * width) * 8;
                 if (left < 8) {                           // behind the row's end
 #pragma unroll
@@ -407,10 +395,18 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
                         if (i >= left) x[8 * p + i] = 0.f;
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sq = fmaf(x[8 * p + i], x[8 * p + i], sq);
+                for (int i = 0; i < 8; ++i) m.w = fmaf(x[8 * p + i], x[8 * p + i], m.w);
             }
         }
-        if (LAYER) sq = SPLIT ? split_sum<W>(sq, red1[turn], share, rank) : row_sum<W>(sq, red1[turn]);
+        m = row_sums<W, SPLIT, LAYER>(m, red[turn], counts, inv_n, share, rank);
+        float sq = m.x, sgx = m.z, mg = 0.f, shift = 0.f;
+        if (LAYER) {
+            const float mean = WARP ? near : m.x * inv_n;
+            mg = m.y * inv_n;
+            sgx -= mean * m.y;
+            sq = m.w;
+            shift = mean - near;
+        }
         const float r = 1.f / sqrtf(sq * inv_n + a.eps), c = -sgx * inv_n * r * r * r, mr = -mg * r;
 #pragma unroll
         for (int p = 0; p < PP; ++p) {
@@ -419,7 +415,7 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
             if (kShared) sums_load(p);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float y = raw_at<T>(d[p], i), yr = y * r, xv = x[8 * p + i];
+                const float y = raw_at<T>(d[p], i), yr = y * r, xv = !LAYER ? x[8 * p + i] * s[p] : WARP ? x[8 * p + i] : x[8 * p + i] - shift;
                 v[i] = fmaf(yr, raw_at<T>(w, i), LAYER ? fmaf(c, xv, mr) : c * xv);
                 float& sum = dw[kShared ? i : 8 * p + i];
                 sum = fmaf(yr, xv, sum);
@@ -639,14 +635,14 @@ NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtyp
         p.threads = p.pp == 1 ? (need <= 256 ? 256 : need <= 512 ? 512 : 1024) : need <= 768 ? 768 : 1024;
         if (need > kBlockThreads) p.threads = kBlockThreads + 1;
         const int64_t smem = (int64_t)p.threads * p.pp * (piece - 12 + stages * piece + (p.pp > 1 ? 32 : 0));
-        p.wide = p.threads > kBlockThreads || smem > ctx->smem_optin - 2048;
+        p.wide = p.threads > kBlockThreads || smem > ctx->smem_optin - 2048 || (four && p.pp > 1);
         const int64_t most = ctx->num_sms * (p.threads <= 256 ? 4 : p.threads <= 512 ? 2 : 1);
         p.parts = p.grid = (int)(rows < most ? rows : most);
         p.smem = (int)smem;
     }
     // A row that one CTA cannot hold is shared by two of a cluster, which exchange its sums over a cluster barrier, up to 16384 columns of fp32 and 32768
-    // of 16 bits, or four, up to 65536: 2048 x 12288 in fp32 takes 114 us for a layer norm, 300 with the kernels for wide rows; 1024 x 32768 in bf16
-    // 102 and 173; 512 x 49152 87 and 128.  What one CTA holds it keeps (2048 x 12288 in bf16: 53 us, shared by two 90), and fp32 shared by four
+    // of 16 bits, or four, up to 65536: 2048 x 12288 in fp32 takes 104 us for a layer norm, 300 with the kernels for wide rows; 1024 x 32768 in bf16
+    // 99 and 173; 512 x 49152 84 and 128.  What one CTA holds it keeps (2048 x 12288 in bf16: 53 us, shared by two 90), and fp32 shared by four
     // is no faster than the wide kernels (1024 x 32768: 220 to 275 us and 233).  With four, 32 clusters run at once, not 37.
     const int64_t most_pieces = four ? 1024 : 2048;       // of a CTA
     const int clusters = four || pieces <= 2 * most_pieces ? 2 : 4;
@@ -724,7 +720,7 @@ void norm_launch(const NormPlan& p, const NormArgs& a, float2* stats, bool sums,
         if (p.threads == 256) norm_start<T, LAYER, VEC, 256, 1>(p, a, st);
         else if (p.threads == 512) norm_start<T, LAYER, VEC, 512, 1>(p, a, st);
         else norm_start<T, LAYER, VEC, 1024, 1>(p, a, st);
-    } else {
+    } else if constexpr (sizeof(T) == 2) {                // (of fp32 a CTA holds no two pieces a thread)
         if (p.threads == 768) norm_start<T, LAYER, VEC, 768, 2>(p, a, st);
         else norm_start<T, LAYER, VEC, 1024, 2>(p, a, st);
     }
