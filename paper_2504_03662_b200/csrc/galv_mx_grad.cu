@@ -127,8 +127,8 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
 // One pass: a row's codes and gradient are read once, its statistics and the two means of the gradient come from registers, and the column sums stay with
 // the thread that has the column, over all rows that its CTA takes (where a thread has two pieces of 8 columns, dweight's in shared memory: with both sums in
 // registers only half as many threads fit, and the pass took twice as long).  The next rows are on their way into shared memory
-// meanwhile, each thread's pieces its own, so that only the rows' sums need a barrier.  2048 x 12288 in bf16 take 53 us for a layer norm and 42 for an
-// rms norm (2.4 and 3.0 TB/s): some 37 instructions an element at 54 % of the issue slots, the rest waits for shuffles, shared memory and the row's sums.
+// meanwhile, each thread's pieces its own, so that only the rows' sums need a barrier.  2048 x 12288 in bf16 take 52.5 us for a layer norm and 41.7 for an
+// rms norm (2.4 and 3.0 TB/s): 39 instructions an element at 60 % of the issue slots, the rest waits for shuffles, shared memory and the row's sums.
 
 constexpr int kBlockThreads = 1024;
 constexpr int kWarpColumns = 1024;                        // up to here a warp has a row to itself, and no barrier
@@ -285,6 +285,7 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
     }
     if (SPLIT) tc::cluster_sync();
     else __syncthreads();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const float inv_warp = LAYER ? WARP ? inv_n : counts[rank * (W / 32) + threadIdx.x / 32].y : 0.f;
 
     float dw[kShared ? 8 : PP * 8] = {}, db[LAYER ? PP * 8 : 1] = {};
@@ -492,13 +493,16 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
     }
 }
 
-// dweight and dbias: the CTAs' sums in a fixed order, 32 columns a CTA, 32 threads a column that take every 32nd.
+// dweight and dbias: the CTAs' sums in a fixed order, 32 columns a CTA, 32 threads a column that take every 32nd.  It is launched while the kernel before it
+// still runs (whose first CTAs allow it), and waits for that one's end: about 1 us less
+// (16384 x 512: 16.1 us, 16.9 one after the other).
 __global__ void __launch_bounds__(1024) mx_norm_join_kernel(long long cols, long long pitch, int parts, const float* __restrict__ part, float* dweight, float* dbias)
 {
     __shared__ float sum[32][33];
     const int x = threadIdx.x % 32, k = threadIdx.x / 32, which = blockIdx.y;
     const long long c = (long long)blockIdx.x * 32 + x;
     float v = 0.f;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (c < cols) {
 #pragma unroll 4
         for (int p = k; p < parts; p += 32) v += part[((long long)p * 2 + which) * pitch + c];
@@ -811,7 +815,18 @@ extern "C" int galv_mx_norm_backward(galv_ctx* ctx, int64_t rows, int64_t cols, 
     MX_DISPATCH_TYPE(dtype,
         if (layer) { if (vec) norm_launch<T, true, true>(p, a, stats, sums, st); else norm_launch<T, true, false>(p, a, stats, sums, st); }
         else { if (vec) norm_launch<T, false, true>(p, a, stats, sums, st); else norm_launch<T, false, false>(p, a, stats, sums, st); });
-    if (sums && !p.ranks) mx_norm_join_kernel<<<dim3((unsigned)((cols + 31) / 32), dbias ? 2 : 1), 1024, 0, st>>>(cols, (cols + 7) / 8 * 8, p.parts, a.part, dweight, dbias);
+    if (sums && !p.ranks) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)((cols + 31) / 32), dbias ? 2 : 1);
+        cfg.blockDim = dim3(1024);
+        cfg.stream = st;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        cudaLaunchKernelEx(&cfg, mx_norm_join_kernel, (long long)cols, (long long)((cols + 7) / 8 * 8), p.parts, (const float*)a.part, dweight, dbias);
+    }
     e = cudaGetLastError();
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
