@@ -478,8 +478,8 @@ __global__ void __launch_bounds__(256) mx_fill_kernel(long long count, const O* 
 __global__ void __launch_bounds__(256) mx_align_kernel(long long rows, int cols, const __half* __restrict__ x, long long stride, __half* __restrict__ out, long long pitch)
 {
     for (long long r = blockIdx.x; r < rows; r += gridDim.x)
-        for (int c = threadIdx.x * 8; c < cols; c += 2048)
-            *reinterpret_cast<uint4*>(out + r * pitch + c) = mx_fetch8<__half, false>(x + r * stride, c, cols).q[0];
+        for (unsigned c = threadIdx.x * 8; c < (unsigned)cols; c += 2048)             // may pass 2^31
+            *reinterpret_cast<uint4*>(out + r * pitch + c) = mx_fetch8<__half, false>(x + r * stride, (int)c, cols).q[0];
 }
 
 struct WgradPlan { int tiles_n, tiles_k, splits, chunks, clusters; size_t aligned, partial, total; };

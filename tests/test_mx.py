@@ -615,6 +615,17 @@ def test_offsets_beyond_32_bits():
     assert ((y[-last:].double() - want).abs() <= want.abs() * 2.0 ** -11 + 1e-6).all()
 
 
+@gpu
+def test_the_widest_weight_gradient():
+    """As many columns of dy as the limit allows, off the 16-byte boundary (realigned before the product): one token, so dw is dy times 3, exactly."""
+    n = 2 ** 31 - 129
+    dy = torch.zeros(n + 1, dtype=torch.bfloat16, device="cuda")[1:].view(1, n)
+    dy[:, ::1000003] = 2.0
+    dy[:, -300:] = torch.arange(300, device="cuda").to(torch.bfloat16)[None] % 64
+    dw = mx.weight_grad(dy, mx.pack(torch.full((1, 1), 3.0, device="cuda")))
+    assert dw.shape == (n, 1) and torch.equal(dw.view(1, n), dy.mul_(3))
+
+
 # ------------------------------------------------------------------------------------------------- a run of them
 
 @gpu
