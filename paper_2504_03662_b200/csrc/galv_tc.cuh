@@ -117,12 +117,10 @@ __device__ __forceinline__ uint64_t operand_plain(uint32_t at)
     return (uint64_t)((at & 0x3ffff) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
 }
 
-template <int G> __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add)
+// 16-bit elements, by a pair of CTAs
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add)
 {
-    if (G == 1)
-        asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" :: "r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
-    else
-        asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" :: "r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" :: "r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
 }
 // 4-bit elements, one power of two for 32 of them: scales at sa, sb in tensor memory
 template <int G> __device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t what, uint32_t sa, uint32_t sb, bool add)
