@@ -329,6 +329,7 @@ mx_matmul_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
     if (warp == 2) tc::tmem_alloc<1>(slot, columns);
     tc::fence_before();
     __syncthreads();
+    tc::cluster_started();                                // waited for before the first store to another CTA
     tc::fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
@@ -385,6 +386,7 @@ mx_matmul_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
         }
     }
     __syncwarp();
+    tc::cluster_wait();                                   // the CTAs that the sums go to run
     const int quad = warp - 4, row = quad * 32 + lane, mine = N / ranks;      // a thread has one row of b; this CTA finishes `mine` rows of a
     bool ok = true;
     if (warp >= 4) {

@@ -26,6 +26,9 @@ __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// The same in two steps, without an order of memory: behind the second, every CTA of the cluster has come to the first, so it runs and its shared memory exists.
+__device__ __forceinline__ void cluster_started() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // the same place in the shared memory of another CTA of the cluster
 __device__ __forceinline__ uint32_t in_cta(uint32_t at, uint32_t rank)
 {
