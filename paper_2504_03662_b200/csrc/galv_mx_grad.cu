@@ -494,9 +494,16 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
 }
 
 // dweight and dbias: the CTAs' sums in a fixed order, 32 columns a CTA, 32 threads a column that take every 32nd.  It is launched while the kernel before it
-// still runs (whose first CTAs allow it), and waits for that one's end: about 1 us less
-// (16384 x 512: 16.1 us, 16.9 one after the other).
-__global__ void __launch_bounds__(1024) mx_norm_join_kernel(long long cols, long long pitch, int parts, const float* __restrict__ part, float* dweight, float* dbias)
+// still runs (once each of that one's CTAs has allowed it or ended), and waits for that one's end: about 1 us less
+// (16384 x 512: 16.1 us, 16.9 one after the other).  The sums are written while this kernel runs, so they are read by plain loads that stay behind the
+// wait: neither the read-only path nor a compiler that may move them is for such data.
+__device__ __forceinline__ float load_behind(const float* p)
+{
+    float v;
+    asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+    return v;
+}
+__global__ void __launch_bounds__(1024) mx_norm_join_kernel(long long cols, long long pitch, int parts, const float* part, float* dweight, float* dbias)
 {
     __shared__ float sum[32][33];
     const int x = threadIdx.x % 32, k = threadIdx.x / 32, which = blockIdx.y;
@@ -505,7 +512,7 @@ __global__ void __launch_bounds__(1024) mx_norm_join_kernel(long long cols, long
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (c < cols) {
 #pragma unroll 4
-        for (int p = k; p < parts; p += 32) v += part[((long long)p * 2 + which) * pitch + c];
+        for (int p = k; p < parts; p += 32) v += load_behind(part + (((long long)p * 2 + which) * pitch + c));
     }
     sum[k][x] = v;
     __syncthreads();
