@@ -95,3 +95,71 @@ def test_joined_column_sums_captured_and_one_after_the_other(rows, cols, kind):
         graph.replay()
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(got, want[first:first + 2]))
+
+
+# ------------------------------------------------------------------------------------------------- weight gradients in segments, tiles and splits
+
+def _rows(g, rows, cols, dtype, pad=0):
+    """Random numbers, rows of other sizes, as a view of a wider matrix where pad > 0."""
+    x = torch.randn(rows, cols + pad, generator=g, device="cuda") * torch.exp2(torch.randint(-2, 3, (rows, 1), generator=g, device="cuda").float())
+    return x.to(dtype)[:, :cols]
+
+
+def _within(got, want, tol, dtype):
+    f = torch.finfo(dtype)
+    rounding = torch.clamp(want.abs() * (f.eps / 2), min=f.smallest_normal * f.eps / 2)
+    off = (got.double() - want).abs()
+    assert not torch.isnan(off).any() and (off <= tol + rounding).all(), f"{(off > tol + rounding).sum()} of {off.numel()} off, first at {(off > tol + rounding).nonzero()[0].tolist()}"
+
+
+@gpu
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("bf16", "f32"), ("f16", "f32")])
+@pytest.mark.parametrize("tokens,n,k,pad", [(2100, 2400, 2048, 0),      # 80 tiles, not split: 33 chunks in three segments, second tiles of some pairs
+                                            (5000, 2050, 2300, 6),      # 81 tiles with ragged ends, five segments, dy on other boundaries
+                                            (1025, 2561, 1793, 0),      # 88 tiles, a second segment of one token, odd rows
+                                            (3000, 1201, 1275, 3),      # 25 tiles, two splits of two segments each
+                                            (9000, 300, 700, 0)])       # 6 tiles, twelve splits of 12 chunks or less
+def test_weight_gradients_of_many_tokens(tokens, n, k, pad, dtype, out):
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    kept = mx.pack(_rows(g, tokens, k, torch.bfloat16))
+    dy = _rows(g, tokens, n, DT[dtype], pad)
+    x64, dy64 = mx.unpack(kept, DT[dtype]).double(), dy.double()
+    want, magnitude = dy64.t() @ x64, dy64.abs().t() @ x64.abs()
+    # a tensor core adds at most 1024 tokens, 16 at a time (a whole step each), registers or splits join them
+    tol = (64 + tokens / 1024 + 16) * 2 * HALF * magnitude
+    got = mx.weight_grad(dy, kept, DT[out])
+    _within(got, want, tol, DT[out])
+    assert torch.equal(got, mx.weight_grad(dy, kept, DT[out]))
+    base = _rows(g, n, k, DT[out])
+    total = base.double() + want
+    joined = mx.weight_grad(dy, kept, base=base)
+    _within(joined, total, tol + HALF * (total.abs() + want.abs()), DT[out])
+    assert mx.weight_grad(dy, kept, base=base, out=base) is base and torch.equal(base, joined)
+
+
+# ------------------------------------------------------------------------------------------------- products of many tiles, and split ones
+
+@gpu
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("m,n,k", [(2600, 2600, 1100),                  # 121 tiles: pairs take a second one while the first moves out; five chunks fill the ring
+                                   (2500, 2305, 4200),                  # 100 tiles of 17 chunks, odd columns
+                                   (65, 20000, 700),                    # 79 tiles in one row of them
+                                   (200, 2048, 8192),                   # 8 tiles, eight splits
+                                   (70, 100, 2048),                     # one tile, two splits
+                                   (513, 1001, 3000)])                  # 12 tiles, three splits, odd columns
+def test_products_of_many_chunks(m, n, k, dtype):
+    g = torch.Generator(device="cuda").manual_seed(m)
+    a, b = mx.pack(_rows(g, m, k, torch.bfloat16), 4), mx.pack(_rows(g, n, k, torch.bfloat16), 4)
+    a64, b64 = mx.unpack(a, torch.float32).double(), mx.unpack(b, torch.float32).double()
+    want, tol = a64 @ b64.t(), (k / 32 + 4) * 2 * HALF * (a64.abs() @ b64.abs().t())
+    got = mx.matmul(a, b, DT[dtype])
+    _within(got, want, tol, DT[dtype])
+    assert torch.equal(got, mx.matmul(a, b, DT[dtype]))
+    bias = _rows(g, 1, n, DT[dtype])[0]
+    total = want + bias.double()
+    _within(mx.matmul(a, b, DT[dtype], bias), total, tol + HALF * total.abs(), DT[dtype])
+    galv = mx.context(torch.device("cuda", 0))                          # into rows of a wider matrix, whose rest stays
+    wide = torch.full((m + 2, n + 5), 5.0, dtype=DT[dtype], device="cuda")
+    ws = torch.full((max(256, galv.galv_mx_matmul_workspace_bytes(m, n, k)),), 0xFF, dtype=torch.uint8, device="cuda")
+    galv.galv_mx_matmul(k, a.codes, a.scales, b.codes, b.scales, None, wide[1:-1, :n], ws)
+    assert torch.equal(wide[1:-1, :n], got) and (wide[0] == 5).all() and (wide[-1] == 5).all() and (wide[:, n:] == 5).all()
