@@ -124,7 +124,7 @@ typedef struct { int32_t tp, dp, zero, ckpt, sp, _pad; double batch_div; } galv_
 typedef struct { double b, act_mult, flops_rate, bw_tp, bw_dp, bytes_per_elem, bin_bytes, time_unit_ns; } galv_inst_params;
 
 /* How a strategy's layers hold and multiply (24 bytes): bits in which a layer's inputs are kept for the backward pass
- * (0: bytes_per_elem; 8: GALV_MX8), bits of the forward products' operands (0: as before; 4: GALV_MX4), seconds that keeping in 8
+ * (0: 16, as the cost model counts them; 8: GALV_MX8), bits of the forward products' operands (0: as before; 4: GALV_MX4), seconds that keeping in 8
  * bits costs for each byte that would have been kept, and how many times faster the products are. */
 typedef struct { int32_t keep_bits, mul_bits; double keep_s_per_byte, mul_speed; } galv_form_desc;
 
@@ -406,12 +406,16 @@ int galv_skip_estimate(galv_ctx* ctx, const galv_shape* shape, const int32_t* L,
  * Forms of strategies (the paper has no counterpart): a strategy may keep its layers' inputs in 8 bits, and multiply in 4, by the
  * calls below this one.  Called after galv_eval_costs on its doubles; for strategies with a form, in IEEE double without fused multiply-add:
  *   keep_bits = 8: kept = the activation bytes of the cost model without the attention scores (with ckpt: the layer's input),
- *                  mem' = mem_bytes - act_mult * (kept - kept * 1.03125 / bytes_per_elem),  time' = time_s + kept * keep_s_per_byte
+ *                  mem' = mem_bytes - act_mult * (kept - kept * 1.03125 / 2),  time' = time_s + kept * keep_s_per_byte
  *   mul_bits = 4:  fwd = c_lin*b*seq*h^2*(1+ckpt)/tp/flops_rate,  time' = time' - (fwd - fwd / mul_speed)
  * and time_q, mem_q are written again from them; other entries, layers l >= L[i] and instances that galv_eval_costs has flagged
  * stay as they are.  The two rates come from the operators as measured on the device (search.py does so).  A form that is none
  * (other bits, a negative or non-finite rate, mul_speed not positive) gets -1 in its strategy's entries, which
  * galv_dp_search flags.  forms [S]; the other arguments are those of galv_eval_costs, time_s and mem_bytes required.
+ * kept is taken for bytes of 16-bit numbers, whatever bytes_per_elem is, as the cost model counts them, and 33/32 bytes hold an element (rows whose
+ * length is no multiple of 512 hold up to 15 scale bytes more).  What a layer's act_rep and act_tp count besides numbers does not shrink: a model with
+ * dropout keeps one-byte masks (two of a full layer's 34 bytes, one of an attention or a feed-forward layer's), for each of which a plan in 8 bits needs
+ * act_mult * seq * b * h * 31/64 bytes more than mem'.
  */
 int galv_add_form_cost(galv_ctx* ctx, const galv_shape* shape, const int32_t* L,
                        const galv_layer_desc* layers, int64_t layer_stride_B,
@@ -420,7 +424,7 @@ int galv_add_form_cost(galv_ctx* ctx, const galv_shape* shape, const int32_t* L,
 
 /*
  * Microscaled tensors: what a plan's layers keep between their forward and backward pass in 8 bits instead of
- * bytes_per_elem, and products of operands in 4 bits (the paper has no counterpart; the planner prices both with
+ * 16, and products of operands in 4 bits (the paper has no counterpart; the planner prices both with
  * galv_add_form_cost, these calls carry them out).
  *
  * A matrix [rows][cols] is held in blocks of 32 consecutive columns of a row, nb = ceil(cols/32) of them, with one

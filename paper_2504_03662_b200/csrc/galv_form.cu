@@ -38,12 +38,13 @@ __global__ void __launch_bounds__(256) form_cost_kernel(int B, int Lmax, int S, 
         const double tp = (double)sd.tp, bq = in.b / sd.batch_div, sbh = ly.seq * bq * ly.h;
         double t = time_s[e], m = mem_bytes[e];
         if (f.keep_bits == 8) {
-            // what the model counts as kept layer inputs (bytes); attention scores and parameters stay as they are
+            // What the model counts as kept layer inputs (bytes); attention scores and parameters stay as they are.  They are bytes of 16-bit numbers whatever
+            // bytes_per_elem says (that is what moves between GPUs), so an element is two of them, and 33/32 in 8 bits.
             double act;
             if (sd.ckpt) act = sd.sp ? 2.0 * sbh / tp : 2.0 * sbh;
             else if (sd.sp) act = sbh * (ly.act_rep + ly.act_tp) / tp;
             else act = sbh * (ly.act_rep + ly.act_tp / tp);
-            m = m - in.act_mult * (act - act * 1.03125 / in.bytes_per_elem);
+            m = m - in.act_mult * (act - act * 1.03125 / 2.0);
             t = t + act * f.keep_s_per_byte;
         }
         if (f.mul_bits == 4) {

@@ -1,0 +1,41 @@
+"""What strategies in 8 and 4 bits cost, against bytes and seconds counted from the tensors that they stand for."""
+import numpy as np
+import pytest
+
+from paper_2504_03662_b200 import inputs
+
+gpu = pytest.mark.gpu
+
+
+def one_layer(ckpt, sp, bytes_per_elem):
+    """One layer of 2048 tokens x 1024 on two tensor-parallel GPUs, which keeps three matrices of that size (one whole, two shared out) and no masks; with
+    checkpointing its input."""
+    layers = np.zeros((1, 1), inputs.LAYER_DESC)
+    for k, v in dict(h=1024.0, seq=1024.0, heads=8.0, c_lin=24.0, p_coef=12.0, act_rep=2.0, act_tp=4.0).items():
+        layers[k] = v
+    strat = np.array([(2, 4, 3, ckpt, sp, 0, 1.0)], inputs.STRATEGY_DESC)
+    inst = np.zeros(1, inputs.INST_PARAMS)
+    for k, v in dict(b=2.0, act_mult=3.0, flops_rate=1e15, bw_tp=4e11, bw_dp=4e11, bytes_per_elem=bytes_per_elem, bin_bytes=64.0, time_unit_ns=1.0).items():
+        inst[k] = v
+    return inputs.Workload("one_layer", 1, 1, 1, 1000, np.ones(1, np.int32), layers=layers, strat=strat, inst=inst)
+
+
+@gpu
+@pytest.mark.parametrize("bytes_per_elem", [1.0, 2.0, 4.0])
+@pytest.mark.parametrize("ckpt,sp", [(0, 0), (0, 1), (1, 0), (1, 1)])
+def test_kept_bytes_are_those_of_the_tensors(ckpt, sp, bytes_per_elem):
+    from paper_2504_03662_b200 import binding as gb, mx
+    from paper_2504_03662_b200.search import SearchBuffers
+    galv = gb.Galv(0)
+    w = one_layer(ckpt, sp, bytes_per_elem).with_forms([(8, 0, 0.0, 1.0)])
+    sb = SearchBuffers(galv, w)
+    sb.eval_costs()
+    tokens, h = 2048, 1024
+    whole, shared = (1, 0) if ckpt else (1, 2)
+    sizes = [(tokens // 2 if sp else tokens, h)] * whole + [(tokens, h // 2)] * shared
+    plain = sum(2 * r * c for r, c in sizes)                        # the cost model's activations are 16-bit numbers
+    held = sum(mx.codes_bytes(r, c) + mx.scales_bytes(r, c) for r, c in sizes)
+    mem = sb.mem_bytes.cpu().numpy()[0, 0]
+    assert mem[0] == mem[1] == 12 * h * h / 2 * 16 / 4 + 3 * plain
+    assert sb.mem_q.cpu().numpy()[0, 0].tolist() == [mem[0] / 64, (mem[0] - 3 * (plain - held)) / 64]
+    galv.close()
