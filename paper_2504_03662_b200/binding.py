@@ -45,7 +45,7 @@ EXPORTS = ("galv_create", "galv_destroy", "galv_strerror", "galv_last_error", "g
            "galv_switch_decision", "galv_skip_estimate", "galv_mx_codes_bytes", "galv_mx_scales_bytes", "galv_mx_pack",
            "galv_mx_unpack", "galv_mx_act_backward", "galv_mx_norm_workspace_bytes", "galv_mx_norm_backward",
            "galv_mx_weight_grad_workspace_bytes", "galv_mx_weight_grad", "galv_mx_matmul_workspace_bytes", "galv_mx_matmul",
-           "galv_add_form_cost", "galv_mx_status")
+           "galv_add_form_cost", "galv_mx_status", "galv_mx_timeouts")
 
 
 class galv_shape(C.Structure):
@@ -120,6 +120,7 @@ def load_library() -> C.CDLL:
     lib.galv_mx_matmul_workspace_bytes.argtypes, lib.galv_mx_matmul_workspace_bytes.restype = [vp, i64, i64, i64], sz
     lib.galv_mx_matmul.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, i32, vp, sz, vp]
     lib.galv_mx_status.argtypes = [vp, vp]
+    lib.galv_mx_timeouts.argtypes, lib.galv_mx_timeouts.restype = [vp], C.POINTER(C.c_uint32)
     _lib = lib
     return lib
 
@@ -360,5 +361,9 @@ class Galv:
             self._check(rc)
 
     def galv_mx_status(self):
-        """Waits for the stream; raises where a bounded wait of a product has run out since the last look."""
+        """Waits for the stream; raises where a bounded wait of a product has run out since the context was made or last looked."""
         self._check(self.lib.galv_mx_status(self.h, _raw_stream(self.device)))
+
+    def galv_mx_timeouts(self) -> int:
+        """Waits that have run out on the device so far; waits for nothing."""
+        return self.lib.galv_mx_timeouts(self.h)[0]

@@ -105,7 +105,6 @@ int galv_create(galv_ctx** out, int device_ordinal)
     ctx->profiling = 0;
     ctx->prof_count = 0;
     ctx->plan_valid = 0;
-    ctx->mx_timeouts = 0;
     for (auto& ev : ctx->pev) ev = nullptr;
     int cur = -1;
     cudaGetDevice(&cur);
@@ -114,6 +113,7 @@ int galv_create(galv_ctx** out, int device_ordinal)
     if (e == cudaSuccess) e = galv_cluster_configure(ctx);
     if (e == cudaSuccess) e = galv_resident_configure(ctx);
     if (e == cudaSuccess) e = galv_solo_configure(ctx);
+    if (e == cudaSuccess) e = galv_mx_configure(ctx);
     for (auto& ev : ctx->pev)
         if (e == cudaSuccess) e = cudaEventCreate(&ev);
     if (cur >= 0 && cur != device_ordinal) cudaSetDevice(cur);

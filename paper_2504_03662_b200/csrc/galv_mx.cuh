@@ -359,9 +359,6 @@ __device__ __forceinline__ void mx_restore8(const uint8_t* __restrict__ codes, c
         else { using T = __half; __VA_ARGS__; }                                                                       \
     } while (0)
 
-// CTAs of weight gradients that have given up a wait, copied on the stream.
-cudaError_t galv_mx_wgrad_timeouts(unsigned* count, cudaStream_t st);
-
 // Tensor map of a matrix [rows][cols] whose rows are `pitch` bytes apart, read in boxes [box_rows][box_cols]; swizzle: rows of 128 bytes, their
 // 16-byte pieces exchanged by row % 8.
 cudaError_t galv_mx_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows,

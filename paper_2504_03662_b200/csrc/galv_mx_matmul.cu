@@ -9,6 +9,8 @@
 // 4096 x 32768 x 8192 into bf16 take 375 us (5.9 PFLOP/s; without copies 323, also without the copies of scales to tensor memory 308, without stores 365).  Five stages: four
 // take 385, six 391.
 
+#include <mutex>
+
 #include "galv_mx.cuh"
 #include "galv_tc.cuh"
 
@@ -33,9 +35,8 @@ struct MatmulArgs {
     void* y;
     float* partial;                                       // [splits][m][n], or NULL
     int vec;                                              // four results of a row can be moved at once
+    unsigned* timeouts;                                   // host memory: CTAs that have given up a wait
 };
-
-__device__ unsigned int g_timeouts;
 
 struct Unit { int tm, tn, split, c0, c1; };
 __device__ __forceinline__ Unit unit_of(const MatmulArgs& a, int u)
@@ -264,7 +265,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constan
     tc::fence_before();
     __syncthreads();
     tc::cluster_sync();                                   // neither CTA's memory is read by the other any more
-    if (threadIdx.x == 0 && failed) atomicAdd(&g_timeouts, 1u);
+    if (threadIdx.x == 0 && failed) atomicAdd_system(a.timeouts, 1u);
     if (warp == 2) tc::tmem_free<2>(tmem, 512);
 }
 
@@ -424,7 +425,7 @@ mx_matmul_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
             ((O*)a.y)[col * a.stride + n0 + row] = mx_round<O>(a.bias ? sum + b : sum);
         }
     }
-    if (threadIdx.x == 0 && failed) atomicAdd(&g_timeouts, 1u);
+    if (threadIdx.x == 0 && failed) atomicAdd_system(a.timeouts, 1u);
     if (warp == 2) tc::tmem_free<1>(tmem, columns);
 }
 
@@ -524,24 +525,49 @@ extern "C" int galv_mx_matmul(galv_ctx* ctx, int64_t m, int64_t n, int64_t k, co
     a.m = m; a.n = n; a.stride = y_stride;
     a.blocks = (int)mx_blocks(k); a.groups = (a.blocks + 3) / 4;
     a.tiles_m = p.tiles_m; a.tiles_n = p.tiles_n; a.splits = p.splits; a.chunks = p.chunks;
-    a.a_scales = a_scales; a.b_scales = b_scales; a.bias = bias; a.y = y;
+    a.a_scales = a_scales; a.b_scales = b_scales; a.bias = bias; a.y = y; a.timeouts = ctx->mx_timeouts_at;
     a.partial = p.partial ? reinterpret_cast<float*>(workspace) : nullptr;
     a.vec = p.partial ? n % 4 == 0 : n % 4 == 0 && y_stride % 4 == 0 && mx_aligned(y, 4 * mx_size_of(dtype));
     MX_DISPATCH_TYPE(dtype, e = launch<T>(p, am, bm, a, (cudaStream_t)stream));
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
 
+// Waits that have run out are counted in host memory, a line of 64 bytes a device, so that they can be read without waiting for anything.  The
+// memory is the process's own and only registered with CUDA: it outlives a device that is reset.
+cudaError_t galv_mx_configure(galv_ctx* ctx)
+{
+    constexpr int most = 64, words = 16;
+    alignas(4096) static unsigned counts[most * words];
+    static std::mutex registering;
+    if (ctx->device < 0 || ctx->device >= most) return cudaErrorInvalidDevice;
+    std::lock_guard<std::mutex> lock(registering);
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;         // another thread may be capturing
+    cudaError_t e = cudaThreadExchangeStreamCaptureMode(&mode);
+    if (e != cudaSuccess) return e;
+    e = cudaHostRegister(counts, sizeof(counts), cudaHostRegisterMapped | cudaHostRegisterPortable);
+    if (e == cudaErrorHostMemoryAlreadyRegistered) {
+        (void)cudaGetLastError();
+        e = cudaSuccess;
+    }
+    ctx->mx_timeouts = counts + ctx->device * words;
+    void* at = nullptr;
+    if (e == cudaSuccess) e = cudaHostGetDevicePointer(&at, ctx->mx_timeouts, 0);
+    ctx->mx_timeouts_at = static_cast<unsigned*>(at);
+    ctx->mx_timeouts_seen = *(volatile unsigned*)ctx->mx_timeouts;
+    const cudaError_t back = cudaThreadExchangeStreamCaptureMode(&mode);
+    return e == cudaSuccess ? back : e;
+}
+
+extern "C" uint32_t* galv_mx_timeouts(const galv_ctx* ctx) { return ctx ? ctx->mx_timeouts : nullptr; }
+
 extern "C" int galv_mx_status(galv_ctx* ctx, void* stream)
 {
     if (!ctx) return GALV_ERR_INVALID_ARG;
     MxDevice dev(ctx);
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
-    unsigned mine = 0, other = 0;
-    cudaError_t e = cudaMemcpyFromSymbolAsync(&mine, g_timeouts, sizeof(mine), 0, cudaMemcpyDeviceToHost, (cudaStream_t)stream);
-    if (e == cudaSuccess) e = galv_mx_wgrad_timeouts(&other, (cudaStream_t)stream);
-    if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
+    const cudaError_t e = cudaStreamSynchronize((cudaStream_t)stream);
     if (e != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
-    const bool more = mine + other != ctx->mx_timeouts;
-    ctx->mx_timeouts = mine + other;
-    return more ? galv_set_error(ctx, GALV_ERR_TIMEOUT, "galv_mx_status: a bounded wait of a microscaled product ran out") : GALV_OK;
+    const unsigned seen = ctx->mx_timeouts_seen;
+    ctx->mx_timeouts_seen = *(volatile unsigned*)ctx->mx_timeouts;
+    return ctx->mx_timeouts_seen != seen ? galv_set_error(ctx, GALV_ERR_TIMEOUT, "galv_mx_status: a bounded wait of a microscaled product ran out") : GALV_OK;
 }

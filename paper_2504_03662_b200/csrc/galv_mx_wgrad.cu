@@ -41,9 +41,8 @@ struct WgradArgs {
     void* dw;
     float* partial;                                       // [splits][n][k], or NULL
     int vec;                                              // four results of a row can be moved at once
+    unsigned* timeouts;                                   // host memory: CTAs that have given up a wait
 };
-
-__device__ unsigned int g_timeouts;
 
 struct Unit { int tn, tk, split, c0, c1; };
 __device__ __forceinline__ Unit unit_of(const WgradArgs& a, int u)
@@ -453,7 +452,7 @@ mx_wgrad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constan
     tc::fence_before();
     __syncthreads();
     tc::cluster_sync();                                   // neither CTA's memory is read by the other any more
-    if (threadIdx.x == 0 && failed) atomicAdd(&g_timeouts, 1u);
+    if (threadIdx.x == 0 && failed) atomicAdd_system(a.timeouts, 1u);
     if (warp == 2) tc::tmem_free<2>(tmem, 512);
 }
 
@@ -569,6 +568,7 @@ extern "C" int galv_mx_weight_grad(galv_ctx* ctx, int64_t tokens, int64_t n, int
         a.tokens = tokens; a.n = n; a.k = k;
         a.tiles_n = p.tiles_n; a.tiles_k = p.tiles_k; a.splits = p.splits; a.chunks = p.chunks;
         a.base = base; a.dw = dw;
+        a.timeouts = ctx->mx_timeouts_at;
         a.partial = p.partial ? reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + p.aligned) : nullptr;
         const int four = p.partial ? 16 : 4 * mx_size_of(dw_dtype);
         a.vec = k % 4 == 0 && (p.partial || (mx_aligned(dw, four) && mx_aligned(base, four)));
@@ -577,5 +577,3 @@ extern "C" int galv_mx_weight_grad(galv_ctx* ctx, int64_t tokens, int64_t n, int
     }
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
-
-cudaError_t galv_mx_wgrad_timeouts(unsigned* count, cudaStream_t st) { return cudaMemcpyFromSymbolAsync(count, g_timeouts, sizeof(*count), 0, cudaMemcpyDeviceToHost, st); }

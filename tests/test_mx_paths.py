@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2504_03662_b200 import binding as gb
 from paper_2504_03662_b200 import mx
 
 from .test_mx import DT, HALF, close, f64, numbers, packed, step
@@ -163,3 +164,49 @@ def test_products_of_many_chunks(m, n, k, dtype):
     ws = torch.full((max(256, galv.galv_mx_matmul_workspace_bytes(m, n, k)),), 0xFF, dtype=torch.uint8, device="cuda")
     galv.galv_mx_matmul(k, a.codes, a.scales, b.codes, b.scales, None, wide[1:-1, :n], ws)
     assert torch.equal(wide[1:-1, :n], got) and (wide[0] == 5).all() and (wide[-1] == 5).all() and (wide[:, n:] == 5).all()
+
+
+# ------------------------------------------------------------------------------------------------- waits that run out
+
+@pytest.fixture
+def counted():
+    """A function that counts `n` more waits as run out on device 0, as the kernels do; all contexts have looked when the test ends."""
+    main = mx.context(torch.device("cuda", 0))
+
+    def more(n):
+        main.lib.galv_mx_timeouts(main.h)[0] += n
+
+    yield more
+    try:
+        main.galv_mx_status()
+    except gb.GalvError:
+        pass
+
+
+def _says_timeout(galv):
+    try:
+        galv.galv_mx_status()
+    except gb.GalvError as e:
+        assert e.code == gb.ERR_TIMEOUT and "wait" in str(e)
+        return True
+    return False
+
+
+@gpu
+def test_each_context_reports_a_wait_that_ran_out_once(counted):
+    old = gb.Galv(0)
+    before = old.galv_mx_timeouts()
+    assert not _says_timeout(old)
+    counted(3)
+    assert old.galv_mx_timeouts() == before + 3
+    fresh = gb.Galv(0)                                              # made behind it: nothing has run out since
+    assert not _says_timeout(fresh)
+    assert _says_timeout(old) and not _says_timeout(old)
+    counted(1)
+    assert _says_timeout(fresh) and _says_timeout(old)
+    assert not _says_timeout(fresh) and not _says_timeout(old)
+    old.close(), fresh.close()
+
+
+def test_the_count_needs_a_context():
+    assert not gb.load_library().galv_mx_timeouts(None)
