@@ -505,7 +505,8 @@ int galv_mx_matmul(galv_ctx* ctx, int64_t m, int64_t n, int64_t k, const uint8_t
                    const uint8_t* b_codes, const uint8_t* b_scales, const void* bias, void* y, int64_t y_stride, int32_t dtype,
                    void* workspace, size_t workspace_bytes, void* stream);
 /* Waits for `stream` and says whether a bounded device-side wait of galv_mx_weight_grad or galv_mx_matmul, of whichever context, has run out on this
- * device since this context was made or last looked (GALV_ERR_TIMEOUT: the results since then are void; GALV_OK otherwise).  Not for stream capture. */
+ * device since this context was made or last looked (GALV_ERR_TIMEOUT: the results since then are void; GALV_OK otherwise).  Not for stream capture.
+ * Both products look too, without waiting, and return GALV_ERR_TIMEOUT in place of a launch; replays of a captured graph do not look. */
 int galv_mx_status(galv_ctx* ctx, void* stream);
 /* Where the device's count of such waits lies: host memory of the library, to be read (volatile) at any time without waiting; NULL without a context. */
 uint32_t* galv_mx_timeouts(const galv_ctx* ctx);

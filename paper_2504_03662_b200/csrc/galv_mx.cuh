@@ -33,6 +33,14 @@ inline bool mx_rows16(const void* p, int64_t stride, int32_t t) { return mx_alig
 inline int64_t mx_blocks(int64_t cols) { return (cols + 31) / 32; }
 inline int64_t mx_pitch8(int64_t cols) { return (mx_blocks(cols) + 15) / 16 * 16; }      // bytes of a row of GALV_MX8 scales
 
+// Whether a wait of a product has run out on the device since the context last looked.
+inline bool mx_ran_out(galv_ctx* ctx)
+{
+    const unsigned seen = ctx->mx_timeouts_seen;
+    ctx->mx_timeouts_seen = *(volatile unsigned*)ctx->mx_timeouts;
+    return ctx->mx_timeouts_seen != seen;
+}
+
 template <int T> struct MxType;
 template <> struct MxType<GALV_F32> { using type = float; };
 template <> struct MxType<GALV_BF16> { using type = __nv_bfloat16; };

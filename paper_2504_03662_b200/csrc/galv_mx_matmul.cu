@@ -514,6 +514,7 @@ extern "C" int galv_mx_matmul(galv_ctx* ctx, int64_t m, int64_t n, int64_t k, co
     const MatmulPlan p = plan_of(ctx, m, n, k);
     if (p.partial && (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < p.partial))
         return galv_set_error(ctx, GALV_ERR_WORKSPACE, "galv_mx_matmul: workspace NULL, misaligned or too small");
+    if (mx_ran_out(ctx)) return galv_set_error(ctx, GALV_ERR_TIMEOUT, "galv_mx_matmul: a bounded wait of an earlier microscaled product ran out");
     MxDevice dev(ctx);
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
     CUtensorMap am, bm;
@@ -567,7 +568,5 @@ extern "C" int galv_mx_status(galv_ctx* ctx, void* stream)
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
     const cudaError_t e = cudaStreamSynchronize((cudaStream_t)stream);
     if (e != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
-    const unsigned seen = ctx->mx_timeouts_seen;
-    ctx->mx_timeouts_seen = *(volatile unsigned*)ctx->mx_timeouts;
-    return ctx->mx_timeouts_seen != seen ? galv_set_error(ctx, GALV_ERR_TIMEOUT, "galv_mx_status: a bounded wait of a microscaled product ran out") : GALV_OK;
+    return mx_ran_out(ctx) ? galv_set_error(ctx, GALV_ERR_TIMEOUT, "galv_mx_status: a bounded wait of a microscaled product ran out") : GALV_OK;
 }

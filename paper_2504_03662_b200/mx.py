@@ -10,6 +10,10 @@ side stream, and for a backward pass with no eager graph of the same leaves aliv
 
 A context of the library belongs to one host thread, so every thread (the autograd engine's among them) gets its own
 for each device.
+
+Waits inside the kernels of `weight_grad` and `matmul` are bounded (two seconds).  Where one has run out, the results since
+then are void: the next call of either on the device raises binding.GalvError with ERR_TIMEOUT, once in each thread, and so does
+`check`, which waits for the current stream first (call it before results are relied on, and behind replays of captured graphs, which look at nothing).
 """
 from __future__ import annotations
 
@@ -36,6 +40,11 @@ def context(device: Union[int, torch.device]) -> gb.Galv:
         made = _local.__dict__.setdefault("made", {})
         made[index] = gb.Galv(index)
         return made[index]
+
+
+def check(device: Union[int, torch.device]):
+    """Waits for the current stream of a CUDA device; raises where a wait of a product has run out there since this thread's context was made or last looked."""
+    context(device).galv_mx_status()
 
 
 def codes_bytes(rows: int, cols: int, fmt: int = gb.MX8) -> int:

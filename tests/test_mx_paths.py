@@ -168,19 +168,27 @@ def test_products_of_many_chunks(m, n, k, dtype):
 
 # ------------------------------------------------------------------------------------------------- waits that run out
 
+def _all_look():
+    """This thread's context and that of the autograd engine's thread look, whatever they find."""
+    x, w = torch.ones(1, 32, device="cuda", dtype=torch.bfloat16), torch.ones(1, 32, device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    for call in (lambda: mx.check(0), lambda: mx.linear(x, w).sum().backward()):
+        try:
+            call()
+        except gb.GalvError as e:
+            assert e.code == gb.ERR_TIMEOUT
+
+
 @pytest.fixture
 def counted():
-    """A function that counts `n` more waits as run out on device 0, as the kernels do; all contexts have looked when the test ends."""
+    """A function that counts `n` more waits as run out on device 0, as the kernels do; every context has looked before the test and behind it."""
     main = mx.context(torch.device("cuda", 0))
 
     def more(n):
         main.lib.galv_mx_timeouts(main.h)[0] += n
 
+    _all_look()
     yield more
-    try:
-        main.galv_mx_status()
-    except gb.GalvError:
-        pass
+    _all_look()
 
 
 def _says_timeout(galv):
@@ -210,3 +218,28 @@ def test_each_context_reports_a_wait_that_ran_out_once(counted):
 
 def test_the_count_needs_a_context():
     assert not gb.load_library().galv_mx_timeouts(None)
+
+
+@gpu
+def test_products_raise_behind_a_wait_that_ran_out(counted):
+    device = torch.device("cuda", 0)
+    x, dy = torch.randn(64, 96, device=device).bfloat16(), torch.randn(64, 32, device=device).bfloat16()
+    kept, four = mx.pack(x), mx.pack(x, 4)
+    want = mx.weight_grad(dy, kept), mx.matmul(four, four)
+    mx.check(device)
+    for call in (lambda: mx.weight_grad(dy, kept), lambda: mx.matmul(four, four), lambda: mx.check(device), lambda: mx.check(0)):
+        counted(1)
+        with pytest.raises(gb.GalvError) as e:
+            call()
+        assert e.value.code == gb.ERR_TIMEOUT
+        call()                                                      # said once
+        assert torch.equal(mx.weight_grad(dy, kept), want[0]) and torch.equal(mx.matmul(four, four), want[1])
+    # a training step: the backward pass runs in a thread of its own, with a context of its own
+    w = torch.randn(32, 96, device=device).bfloat16().requires_grad_()
+    _all_look()
+    mx.linear(x, w).backward(dy)
+    counted(1)
+    y = mx.linear(x, w)
+    with pytest.raises(gb.GalvError):
+        y.backward(dy)
+    mx.linear(x, w).backward(dy)
