@@ -36,7 +36,8 @@ def _seconds(f, reps: int = 5) -> float:
 def measure_forms(galv: gb.Galv, hidden: int, tokens: int, keep: bool = True, multiply: bool = True) -> np.ndarray:
     """Forms of strategies (rows of FORM_DESC for Workload.with_forms) with the rates of this device: the hardware profiler's part for the
     microscaled operators.  A layer's input [tokens][hidden] in bf16 is packed in 8 bits and used for a weight gradient, beside the plain
-    gradient of the 16-bit input; and multiplied in 4 bits (packed in the call), beside the plain product."""
+    gradient of the 16-bit input; and multiplied in 4 bits by a weight [hidden][hidden] (both packed in the call, as mx.linear does it), beside the plain
+    product."""
     dev = torch.device("cuda", galv.device)
     g = torch.Generator(device=dev).manual_seed(1)
     x, dy, w = (torch.randn(*s, generator=g, device=dev).to(torch.bfloat16) for s in ((tokens, hidden), (tokens, hidden), (hidden, hidden)))
@@ -49,8 +50,7 @@ def measure_forms(galv: gb.Galv, hidden: int, tokens: int, keep: bool = True, mu
             s_per_byte = (_seconds(lambda: mx.pack(x)) + max(0.0, _seconds(lambda: mx.weight_grad(dy, kept)) - plain)) / (x.numel() * 2)
             rows.append((8, 0, s_per_byte, 1.0))
         if multiply:
-            w4 = mx.pack(w, gb.MX4)
-            speed = _seconds(lambda: x @ w.t()) / _seconds(lambda: mx.matmul(mx.pack(x, gb.MX4), w4))
+            speed = _seconds(lambda: x @ w.t()) / _seconds(lambda: mx.matmul(mx.pack(x, gb.MX4), mx.pack(w, gb.MX4)))
             rows.append((0, 4, 0.0, speed))
         if keep and multiply:
             rows.append((8, 4, s_per_byte, speed))

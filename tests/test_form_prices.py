@@ -39,3 +39,48 @@ def test_kept_bytes_are_those_of_the_tensors(ckpt, sp, bytes_per_elem):
     assert mem[0] == mem[1] == 12 * h * h / 2 * 16 / 4 + 3 * plain
     assert sb.mem_q.cpu().numpy()[0, 0].tolist() == [mem[0] / 64, (mem[0] - 3 * (plain - held)) / 64]
     galv.close()
+
+
+@pytest.fixture
+def priced_calls(monkeypatch):
+    """Prices for measure_forms: a call that it times costs 1 second and what `cost` says for each microscaled operator in it.  Returns (cost, what each
+    timed call ran, a list that every operator is written to)."""
+    from paper_2504_03662_b200 import mx, search
+    cost, timed, ran = {}, [], []
+
+    def counting(name):
+        f = getattr(mx, name)
+
+        def call(*a, **k):
+            ran.append(f"{name}{a[1]}" if name == "pack" and len(a) > 1 else name)
+            return f(*a, **k)
+        return call
+
+    for name in ("pack", "unpack", "act_backward", "norm_backward", "weight_grad", "matmul"):
+        monkeypatch.setattr(mx, name, counting(name))
+
+    def seconds(f, reps=5):
+        del ran[:]
+        f()
+        timed.append(list(ran))
+        return 1.0 + sum(cost.get(op, 0.0) for op in ran)
+
+    monkeypatch.setattr(search, "_seconds", seconds)
+    return cost, timed, ran
+
+
+@gpu
+def test_the_speed_of_products_is_that_of_the_layer_that_carries_them_out(priced_calls):
+    """What is timed in 4 bits packs and multiplies what mx.linear does."""
+    import torch
+    from paper_2504_03662_b200 import binding as gb, mx
+    from paper_2504_03662_b200.search import measure_forms
+    cost, timed, ran = priced_calls
+    cost.update({"pack4": 4.0, "matmul": 3.0})
+    galv = gb.Galv(0)
+    form = measure_forms(galv, 64, 128, keep=False)
+    del ran[:]
+    mx.linear(torch.ones(128, 64, device="cuda", dtype=torch.bfloat16), torch.ones(64, 64, device="cuda", dtype=torch.bfloat16), four=True)
+    assert sorted(ran) == ["matmul", "pack4", "pack4"] and sorted(timed[-1]) == sorted(ran)
+    assert form["mul_speed"].tolist() == [1.0 / 12.0]
+    galv.close()
