@@ -35,9 +35,10 @@ def _seconds(f, reps: int = 5) -> float:
 
 def measure_forms(galv: gb.Galv, hidden: int, tokens: int, keep: bool = True, multiply: bool = True) -> np.ndarray:
     """Forms of strategies (rows of FORM_DESC for Workload.with_forms) with the rates of this device: the hardware profiler's part for the
-    microscaled operators.  A layer's input [tokens][hidden] in bf16 is packed in 8 bits and used for a weight gradient, beside the plain
-    gradient of the 16-bit input; and multiplied in 4 bits by a weight [hidden][hidden] (both packed in the call, as mx.linear does it), beside the plain
-    product."""
+    microscaled operators.  A layer's input [tokens][hidden] in bf16 is packed in 8 bits and used in the backward pass, beside the plain backward pass of
+    the 16-bit input: the dearest of what may read it counts (the gradient of a weight, of a norm, of an activation function, or restoring it, as
+    queries, keys, values and checkpointed inputs are); and multiplied in 4 bits by a weight [hidden][hidden] (both packed in the call, as mx.linear does it), beside the plain
+    product.  These are rates of one shape: layers of very different widths want their own."""
     dev = torch.device("cuda", galv.device)
     g = torch.Generator(device=dev).manual_seed(1)
     x, dy, w = (torch.randn(*s, generator=g, device=dev).to(torch.bfloat16) for s in ((tokens, hidden), (tokens, hidden), (hidden, hidden)))
@@ -46,8 +47,13 @@ def measure_forms(galv: gb.Galv, hidden: int, tokens: int, keep: bool = True, mu
     with torch.cuda.device(dev):
         if keep:
             kept = mx.pack(x)
-            plain = _seconds(lambda: dy.t() @ x)
-            s_per_byte = (_seconds(lambda: mx.pack(x)) + max(0.0, _seconds(lambda: mx.weight_grad(dy, kept)) - plain)) / (x.numel() * 2)
+            ops, ones = torch.ops.aten, torch.ones(hidden, dtype=x.dtype, device=dev)
+            stats = ops.native_layer_norm(x, [hidden], ones, ones, 1e-5)[1:]
+            uses = [(lambda: mx.weight_grad(dy, kept), lambda: dy.t() @ x),
+                    (lambda: mx.norm_backward(dy, kept, ones), lambda: ops.native_layer_norm_backward(dy, x, [hidden], *stats, ones, ones, [True] * 3)),
+                    (lambda: mx.act_backward(dy, kept), lambda: ops.gelu_backward(dy, x))]
+            more = [_seconds(held) - _seconds(plain) for held, plain in uses] + [_seconds(lambda: mx.unpack(kept))]
+            s_per_byte = (_seconds(lambda: mx.pack(x)) + max(more)) / (x.numel() * 2)
             rows.append((8, 0, s_per_byte, 1.0))
         if multiply:
             speed = _seconds(lambda: x @ w.t()) / _seconds(lambda: mx.matmul(mx.pack(x, gb.MX4), mx.pack(w, gb.MX4)))

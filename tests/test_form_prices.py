@@ -84,3 +84,17 @@ def test_the_speed_of_products_is_that_of_the_layer_that_carries_them_out(priced
     assert sorted(ran) == ["matmul", "pack4", "pack4"] and sorted(timed[-1]) == sorted(ran)
     assert form["mul_speed"].tolist() == [1.0 / 12.0]
     galv.close()
+
+
+@gpu
+@pytest.mark.parametrize("dearest,price", [("weight_grad", 100.0), ("norm_backward", 100.0), ("act_backward", 100.0), ("unpack", 101.0), (None, 1.0)])
+def test_keeping_in_8_bits_costs_packing_and_its_dearest_use(priced_calls, dearest, price):
+    """Each use costs what it takes longer than the plain backward pass; restoring has none beside it (and is the dearest where all are alike)."""
+    from paper_2504_03662_b200 import binding as gb
+    from paper_2504_03662_b200.search import measure_forms
+    cost, timed, ran = priced_calls
+    cost.update({"pack": 6.0, dearest: 100.0})
+    galv = gb.Galv(0)
+    form = measure_forms(galv, 64, 128, multiply=False)
+    assert form["keep_s_per_byte"].tolist() == [(7.0 + price) / (128 * 64 * 2)]
+    galv.close()
