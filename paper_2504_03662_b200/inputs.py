@@ -121,6 +121,8 @@ class Workload:
         """Every strategy as it is, then every strategy in each of `forms` (rows of FORM_DESC): strategy f * S + s is s in form f."""
         if not self.has_model:
             raise ValueError("forms are priced by the cost model: a workload of measured tables has its own times and sizes")
+        if self.forms is not None:
+            raise ValueError("this workload's strategies have forms already: give all of them to the plain workload at once")
         rows = np.concatenate([np.array([(0, 0, 0.0, 1.0)], FORM_DESC), np.asarray(forms, FORM_DESC).reshape(-1)])
         if self.S * len(rows) > 256:
             raise ValueError(f"{self.S} strategies in {len(rows)} forms: at most 256 in all")

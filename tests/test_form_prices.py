@@ -98,3 +98,10 @@ def test_keeping_in_8_bits_costs_packing_and_its_dearest_use(priced_calls, deare
     form = measure_forms(galv, 64, 128, multiply=False)
     assert form["keep_s_per_byte"].tolist() == [(7.0 + price) / (128 * 64 * 2)]
     galv.close()
+
+
+def test_forms_of_forms_are_refused():
+    """A second round would have dropped the first one's forms and kept its strategies."""
+    w = inputs.config1().with_forms([(8, 0, 1e-12, 1.0)])
+    with pytest.raises(ValueError, match="already"):
+        w.with_forms([(0, 4, 0.0, 2.0)])
