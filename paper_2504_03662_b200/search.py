@@ -39,6 +39,8 @@ def measure_forms(galv: gb.Galv, hidden: int, tokens: int, keep: bool = True, mu
     the 16-bit input: the dearest of what may read it counts (the gradient of a weight, of a norm, of an activation function, or restoring it, as
     queries, keys, values and checkpointed inputs are); and multiplied in 4 bits by a weight [hidden][hidden] (both packed in the call, as mx.linear does it), beside the plain
     product.  These are rates of one shape: layers of very different widths want their own."""
+    if hidden < 1 or tokens < 1:
+        raise ValueError(f"rates of a layer of {tokens} tokens x {hidden}: both are at least 1")
     dev = torch.device("cuda", galv.device)
     g = torch.Generator(device=dev).manual_seed(1)
     x, dy, w = (torch.randn(*s, generator=g, device=dev).to(torch.bfloat16) for s in ((tokens, hidden), (tokens, hidden), (hidden, hidden)))

@@ -105,3 +105,12 @@ def test_forms_of_forms_are_refused():
     w = inputs.config1().with_forms([(8, 0, 1e-12, 1.0)])
     with pytest.raises(ValueError, match="already"):
         w.with_forms([(0, 4, 0.0, 2.0)])
+
+
+@pytest.mark.parametrize("hidden,tokens", [(1024, 0), (0, 16), (-1, 16)])
+def test_rates_of_nothing_are_refused(hidden, tokens):
+    """Seconds for each of no bytes: a division by zero in the middle of the measurement before."""
+    from types import SimpleNamespace
+    from paper_2504_03662_b200.search import measure_forms
+    with pytest.raises(ValueError, match="at least 1"):
+        measure_forms(SimpleNamespace(device=0), hidden, tokens)
