@@ -248,6 +248,11 @@ def _flat(x: torch.Tensor) -> torch.Tensor:
     return x.reshape(-1, x.shape[-1])
 
 
+def _last_axis(x: torch.Tensor):
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError(f"x has a last axis of one number or more, not the shape {tuple(x.shape)}")
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, four):
@@ -280,8 +285,11 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
     """x weight^T + bias (bf16 or fp16), x kept in 8 bits for the weight's gradient.  `four`: the forward product takes both operands in
     4 bits; the gradients are those of the product of the unrounded operands (straight through the rounding)."""
     _kind(x.dtype, "x", _SHORT)
+    _last_axis(x)
     if weight.dim() != 2 or weight.dtype != x.dtype or weight.shape[0] < 1 or weight.shape[1] != x.shape[-1]:
         raise ValueError(f"weight of shape {tuple(weight.shape)} and {weight.dtype} beside x of {tuple(x.shape)} and {x.dtype}")
+    if bias is not None and (bias.dtype != x.dtype or bias.dim() > 1):
+        raise ValueError(f"bias is [{weight.shape[0]}] of {x.dtype}, not {tuple(bias.shape)} of {bias.dtype}")
     return _Linear.apply(x, weight, bias, four)
 
 
@@ -310,7 +318,10 @@ def norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[
         raise ValueError(f"a norm is one of {', '.join(NORMS)}, not {kind!r}")
     if kind == "rms" and bias is not None:
         raise ValueError("an rms norm has no bias")
+    if not eps >= 0:
+        raise ValueError(f"eps is 0 or more, not {eps}")
     _kind(x.dtype, "x")
+    _last_axis(x)
     for t, what in ((weight, "weight"), (bias, "bias")):
         if t is not None and (t.dtype != x.dtype or tuple(t.shape) != x.shape[-1:]):
             raise ValueError(f"{what} is [{x.shape[-1]}] of {x.dtype}")
@@ -338,4 +349,5 @@ def activation(x: torch.Tensor, act: str = "gelu") -> torch.Tensor:
     if act not in ACTS:
         raise ValueError(f"an activation function is one of {', '.join(ACTS)}, not {act!r}")
     _kind(x.dtype, "x")
+    _last_axis(x)
     return _Activation.apply(x, act)

@@ -243,3 +243,32 @@ def test_products_raise_behind_a_wait_that_ran_out(counted):
     with pytest.raises(gb.GalvError):
         y.backward(dy)
     mx.linear(x, w).backward(dy)
+
+
+# ------------------------------------------------------------------------------------------------- refusals of the differentiable forms
+
+def _short(*shape):
+    return torch.zeros(shape, dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("call", [
+    lambda: mx.linear(_short(4, 64), _short(8, 64), _short(4, 8)),                 # adds up, but has no gradient of this shape
+    lambda: mx.linear(_short(4, 64), _short(8, 64), _short(1, 8)),
+    lambda: mx.linear(_short(4, 64), _short(8, 64), torch.zeros(8)),
+    lambda: mx.linear(_short(), _short(8, 64)),
+    lambda: mx.linear(_short(4, 0), _short(8, 0)),
+    lambda: mx.norm(torch.zeros(())),
+    lambda: mx.norm(torch.zeros(3, 0)),
+    lambda: mx.activation(torch.zeros(())),
+    lambda: mx.activation(torch.zeros(3, 0)),
+])
+def test_what_the_backward_pass_cannot_take_is_refused_in_front(call):
+    with pytest.raises(ValueError):
+        with torch.no_grad():
+            call()
+
+
+@pytest.mark.parametrize("eps", [-1e-5, float("nan")])
+def test_eps_of_norms_is_looked_at_in_front(eps):
+    with pytest.raises(ValueError, match="eps"):
+        mx.norm(torch.zeros(4, 64), eps=eps)
