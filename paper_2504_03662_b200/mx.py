@@ -122,7 +122,9 @@ def _kind(dtype: torch.dtype, what: str, dtypes=_NUMBERS):
 
 
 def _rows(t: torch.Tensor, what: str) -> torch.Tensor:
-    """A 2-D tensor whose rows are contiguous and do not overlap (a copy where they are not)."""
+    """A 2-D tensor whose rows are contiguous and do not overlap, and that lies in memory as it is (a copy where they are not, or it is a negative view)."""
+    if t.is_neg():
+        t = t.resolve_neg()
     if t.is_contiguous() and t.dim() == 2:
         return t
     if t.dim() != 2:
@@ -130,6 +132,10 @@ def _rows(t: torch.Tensor, what: str) -> torch.Tensor:
     if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
         return t.contiguous()
     return t
+
+
+def _vector(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    return None if t is None else t.resolve_neg().contiguous()
 
 
 def _beside(t: torch.Tensor, p: Packed, what: str):
@@ -197,7 +203,7 @@ def norm_backward(dy: torch.Tensor, kept: Packed, weight: Optional[torch.Tensor]
     dweight = torch.empty(kept.cols, dtype=torch.float32, device=device)
     dbias = torch.empty(kept.cols, dtype=torch.float32, device=device) if kind == "layer" else None
     n = g.galv_mx_norm_workspace_bytes(kept.rows, kept.cols)
-    g.galv_mx_norm_backward(NORMS[kind], eps, *kept._at, dy, None if weight is None else weight.contiguous(), dx, dweight, dbias, _bytes(n, device) if n else None)
+    g.galv_mx_norm_backward(NORMS[kind], eps, *kept._at, dy, _vector(weight), dx, dweight, dbias, _bytes(n, device) if n else None)
     return dx, dweight, dbias
 
 
@@ -216,7 +222,7 @@ def weight_grad(dy: torch.Tensor, kept: Packed, dtype: Optional[torch.dtype] = N
         raise ValueError(f"a weight gradient is of {dy.dtype} or float32, not {dtype}")
     for t, what in ((base, "base"), (out, "out")):
         if t is not None:
-            if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+            if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.is_neg():
                 raise ValueError(f"{what} is a contiguous {shape} of {dtype}")
     device = dy.device
     g = _on(device, kept.device, _device(base), _device(out))
@@ -238,7 +244,7 @@ def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, bias: Opti
     g = _on(a.device, b.device, _device(bias))
     y = torch.empty(a.rows, b.rows, dtype=dtype, device=a.device)
     n = g.galv_mx_matmul_workspace_bytes(a.rows, b.rows, a.cols)
-    g.galv_mx_matmul(a.cols, *a._at, *b._at, None if bias is None else bias.contiguous(), y, _bytes(n, a.device) if n else None)
+    g.galv_mx_matmul(a.cols, *a._at, *b._at, _vector(bias), y, _bytes(n, a.device) if n else None)
     return y
 
 

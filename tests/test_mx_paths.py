@@ -272,3 +272,32 @@ def test_what_the_backward_pass_cannot_take_is_refused_in_front(call):
 def test_eps_of_norms_is_looked_at_in_front(eps):
     with pytest.raises(ValueError, match="eps"):
         mx.norm(torch.zeros(4, 64), eps=eps)
+
+
+# ------------------------------------------------------------------------------------------------- negative views
+
+def _negative(t):
+    """A view that stands for -t, as the imaginary part of a conjugate does; t's own numbers lie in memory."""
+    return torch.complex(torch.zeros_like(t), t).conj().imag
+
+
+def test_a_column_of_a_conjugate_is_taken_as_what_it_stands_for():
+    t = torch.arange(1.0, 6.0).view(5, 1)
+    v = _negative(t)
+    assert v.is_neg() and v.stride(1) == 2                          # one column: the rows are as good as contiguous
+    got = mx._rows(v, "x")
+    assert not got.is_neg() and torch.equal(got, -t)
+    one = _negative(torch.tensor([3.0]))
+    assert one.is_contiguous() and not mx._vector(one).is_neg() and mx._vector(one).item() == -3.0
+    assert mx._vector(None) is None
+    kept = mx.Packed(torch.zeros(32, dtype=torch.uint8), torch.zeros(16, dtype=torch.uint8), 1, 1)
+    out = torch._neg_view(torch.ones(1, 1, dtype=torch.bfloat16))
+    for k in (dict(base=out), dict(out=out)):
+        with pytest.raises(ValueError, match="contiguous"):
+            mx.weight_grad(_short(1, 1), kept, **k)
+
+
+@gpu
+def test_a_negative_column_packed():
+    t = torch.arange(1.0, 6.0, device="cuda").view(5, 1)
+    assert torch.equal(mx.unpack(mx.pack(_negative(t)), torch.float32), -t)
