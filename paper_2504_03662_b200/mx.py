@@ -6,7 +6,8 @@ current stream of the tensors' device; formats and formulas are those of include
 `activation` are the same as differentiable functions: their inputs are kept in 8 bits for the backward pass.
 
 Calls and backward passes may be captured in a CUDA graph under PyTorch's rules: after the same call has run once on a
-side stream, and for a backward pass with no eager graph of the same leaves alive.
+side stream, and for a backward pass with no eager graph of the same leaves alive.  Under autocast the differentiable functions compute in the types of
+their inputs, as they do without.
 
 A context of the library belongs to one host thread, so every thread (the autograd engine's among them) gets its own
 for each device.
@@ -259,8 +260,19 @@ def _last_axis(x: torch.Tensor):
         raise ValueError(f"x has a last axis of one number or more, not the shape {tuple(x.shape)}")
 
 
+def _as_typed(f):
+    """A forward or backward pass in the types of its inputs: under autocast the library's norms would answer in fp32, its products in autocast's type."""
+    def run(*args):
+        if torch.is_autocast_enabled("cuda"):
+            with torch.autocast("cuda", enabled=False):
+                return f(*args)
+        return f(*args)
+    return run
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
+    @_as_typed
     def forward(ctx, x, weight, bias, four):
         flat = _flat(x)
         if four:
@@ -274,6 +286,7 @@ class _Linear(torch.autograd.Function):
 
     @staticmethod
     @torch.autograd.function.once_differentiable
+    @_as_typed
     def backward(ctx, dy):
         weight, *kept = ctx.saved_tensors
         flat = _flat(dy)
@@ -301,6 +314,7 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
 
 class _Norm(torch.autograd.Function):
     @staticmethod
+    @_as_typed
     def forward(ctx, x, weight, bias, kind, eps):
         n = (x.shape[-1],)
         y = torch.nn.functional.layer_norm(x, n, weight, bias, eps) if kind == "layer" else torch.nn.functional.rms_norm(x, n, weight, eps)
@@ -311,6 +325,7 @@ class _Norm(torch.autograd.Function):
 
     @staticmethod
     @torch.autograd.function.once_differentiable
+    @_as_typed
     def backward(ctx, dy):
         codes, scales, *weight = ctx.saved_tensors
         flat = _flat(dy)
@@ -336,6 +351,7 @@ def norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[
 
 class _Activation(torch.autograd.Function):
     @staticmethod
+    @_as_typed
     def forward(ctx, x, act):
         kept = pack(_flat(x))
         ctx.save_for_backward(kept.codes, kept.scales)
@@ -345,6 +361,7 @@ class _Activation(torch.autograd.Function):
 
     @staticmethod
     @torch.autograd.function.once_differentiable
+    @_as_typed
     def backward(ctx, dy):
         flat = _flat(dy)
         return act_backward(flat, Packed(*ctx.saved_tensors, *flat.shape), ctx.act).view(ctx.shape), None

@@ -301,3 +301,30 @@ def test_a_column_of_a_conjugate_is_taken_as_what_it_stands_for():
 def test_a_negative_column_packed():
     t = torch.arange(1.0, 6.0, device="cuda").view(5, 1)
     assert torch.equal(mx.unpack(mx.pack(_negative(t)), torch.float32), -t)
+
+
+# ------------------------------------------------------------------------------------------------- under autocast
+
+@gpu
+@pytest.mark.parametrize("auto", ["bf16", "f16"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("name", ["layer", "rms", "gelu", "linear", "linear4"])
+def test_autocast_changes_nothing(name, dtype, auto):
+    """Results and gradients are those without autocast, bit for bit, backward inside it and behind it."""
+    d = DT[dtype]
+    x, w, dy = numbers(1, 40, 96, d).cuda().requires_grad_(), numbers(2, 64, 96, d).cuda().requires_grad_(), numbers(3, 40, 96 if name in ("layer", "rms", "gelu") else 64, d).cuda()
+    nw, b = numbers(4, 1, 96, d)[0].cuda().requires_grad_(), numbers(5, 1, 64, d)[0].cuda().requires_grad_()
+    calls = {"layer": (lambda: mx.norm(x, nw), (x, nw)), "rms": (lambda: mx.norm(x, nw, kind="rms"), (x, nw)), "gelu": (lambda: mx.activation(x), (x,)),
+             "linear": (lambda: mx.linear(x, w, b), (x, w, b)), "linear4": (lambda: mx.linear(x, w, b, four=True), (x, w, b))}
+    call, leaves = calls[name]
+    y = call()
+    want = [y.detach(), *torch.autograd.grad(y, leaves, dy)]
+    for inside in (True, False):
+        with torch.autocast("cuda", dtype=DT[auto]):
+            y = call()
+            assert y.dtype == d
+            if inside:
+                grads = torch.autograd.grad(y, leaves, dy)
+        if not inside:
+            grads = torch.autograd.grad(y, leaves, dy)
+        assert all(a.dtype == b.dtype and torch.equal(a, b) for a, b in zip([y.detach(), *grads], want))
