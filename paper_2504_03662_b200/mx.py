@@ -273,13 +273,13 @@ def _as_typed(f):
 class _Linear(torch.autograd.Function):
     @staticmethod
     @_as_typed
-    def forward(ctx, x, weight, bias, four):
+    def forward(ctx, x, weight, bias, four, keep):
         flat = _flat(x)
         if four:
             y = matmul(pack(flat, gb.MX4), pack(weight, gb.MX4), x.dtype, bias)
         else:
             y = flat @ weight.t() if bias is None else torch.addmm(bias, flat, weight.t())
-        kept = pack(flat) if ctx.needs_input_grad[1] else None
+        kept = pack(flat) if keep and ctx.needs_input_grad[1] else None
         ctx.save_for_backward(weight, *((kept.codes, kept.scales) if kept else ()))
         ctx.shape, ctx.has_bias = x.shape, bias is not None
         return y.view(*x.shape[:-1], weight.shape[0])
@@ -297,11 +297,11 @@ class _Linear(torch.autograd.Function):
             dw = weight_grad(flat, Packed(*kept, flat.shape[0], weight.shape[1]), weight.dtype)
         if ctx.has_bias and ctx.needs_input_grad[2]:
             db = flat.sum(0, dtype=torch.float32).to(dy.dtype)
-        return dx, dw, db, None
+        return dx, dw, db, None, None
 
 
 def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, four: bool = False) -> torch.Tensor:
-    """x weight^T + bias (bf16 or fp16), x kept in 8 bits for the weight's gradient.  `four`: the forward product takes both operands in
+    """x weight^T + bias (bf16 or fp16), x kept in 8 bits for the weight's gradient (where one will be taken).  `four`: the forward product takes both operands in
     4 bits; the gradients are those of the product of the unrounded operands (straight through the rounding)."""
     _kind(x.dtype, "x", _SHORT)
     _last_axis(x)
@@ -309,18 +309,19 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
         raise ValueError(f"weight of shape {tuple(weight.shape)} and {weight.dtype} beside x of {tuple(x.shape)} and {x.dtype}")
     if bias is not None and (bias.dtype != x.dtype or bias.dim() > 1):
         raise ValueError(f"bias is [{weight.shape[0]}] of {x.dtype}, not {tuple(bias.shape)} of {bias.dtype}")
-    return _Linear.apply(x, weight, bias, four)
+    return _Linear.apply(x, weight, bias, four, torch.is_grad_enabled())
 
 
 class _Norm(torch.autograd.Function):
     @staticmethod
     @_as_typed
-    def forward(ctx, x, weight, bias, kind, eps):
+    def forward(ctx, x, weight, bias, kind, eps, keep):
         n = (x.shape[-1],)
         y = torch.nn.functional.layer_norm(x, n, weight, bias, eps) if kind == "layer" else torch.nn.functional.rms_norm(x, n, weight, eps)
-        kept = pack(_flat(x))
-        ctx.save_for_backward(kept.codes, kept.scales, *(() if weight is None else (weight,)))
-        ctx.kind, ctx.eps, ctx.shape, ctx.bias_type = kind, eps, x.shape, None if bias is None else bias.dtype
+        if keep and any(ctx.needs_input_grad):
+            kept = pack(_flat(x))
+            ctx.save_for_backward(kept.codes, kept.scales, *(() if weight is None else (weight,)))
+            ctx.kind, ctx.eps, ctx.shape, ctx.bias_type = kind, eps, x.shape, None if bias is None else bias.dtype
         return y
 
     @staticmethod
@@ -330,11 +331,11 @@ class _Norm(torch.autograd.Function):
         codes, scales, *weight = ctx.saved_tensors
         flat = _flat(dy)
         dx, dw, db = norm_backward(flat, Packed(codes, scales, *flat.shape), weight[0] if weight else None, ctx.kind, ctx.eps)
-        return (dx.view(ctx.shape), dw.to(weight[0].dtype) if weight else None, None if ctx.bias_type is None else db.to(ctx.bias_type), None, None)
+        return (dx.view(ctx.shape), dw.to(weight[0].dtype) if weight else None, None if ctx.bias_type is None else db.to(ctx.bias_type), None, None, None)
 
 
 def norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, kind: str = "layer", eps: float = 1e-5) -> torch.Tensor:
-    """A "layer" or "rms" norm over the last axis, x kept in 8 bits for the backward pass."""
+    """A "layer" or "rms" norm over the last axis, x kept in 8 bits for the backward pass (where there will be one)."""
     if kind not in NORMS:
         raise ValueError(f"a norm is one of {', '.join(NORMS)}, not {kind!r}")
     if kind == "rms" and bias is not None:
@@ -346,16 +347,18 @@ def norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[
     for t, what in ((weight, "weight"), (bias, "bias")):
         if t is not None and (t.dtype != x.dtype or tuple(t.shape) != x.shape[-1:]):
             raise ValueError(f"{what} is [{x.shape[-1]}] of {x.dtype}")
-    return _Norm.apply(x, weight, bias, kind, eps)
+    _on(x.device, _device(weight), _device(bias))
+    return _Norm.apply(x, weight, bias, kind, eps, torch.is_grad_enabled())
 
 
 class _Activation(torch.autograd.Function):
     @staticmethod
     @_as_typed
-    def forward(ctx, x, act):
-        kept = pack(_flat(x))
-        ctx.save_for_backward(kept.codes, kept.scales)
-        ctx.act, ctx.shape = act, x.shape
+    def forward(ctx, x, act, keep):
+        if keep and ctx.needs_input_grad[0]:
+            kept = pack(_flat(x))
+            ctx.save_for_backward(kept.codes, kept.scales)
+            ctx.act, ctx.shape = act, x.shape
         f = torch.nn.functional
         return f.silu(x) if act == "silu" else f.gelu(x, approximate="tanh" if act == "gelu_tanh" else "none")
 
@@ -364,13 +367,14 @@ class _Activation(torch.autograd.Function):
     @_as_typed
     def backward(ctx, dy):
         flat = _flat(dy)
-        return act_backward(flat, Packed(*ctx.saved_tensors, *flat.shape), ctx.act).view(ctx.shape), None
+        return act_backward(flat, Packed(*ctx.saved_tensors, *flat.shape), ctx.act).view(ctx.shape), None, None
 
 
 def activation(x: torch.Tensor, act: str = "gelu") -> torch.Tensor:
-    """gelu, gelu_tanh or silu, x kept in 8 bits for the backward pass."""
+    """gelu, gelu_tanh or silu, x kept in 8 bits for the backward pass (where there will be one)."""
     if act not in ACTS:
         raise ValueError(f"an activation function is one of {', '.join(ACTS)}, not {act!r}")
     _kind(x.dtype, "x")
     _last_axis(x)
-    return _Activation.apply(x, act)
+    _on(x.device)
+    return _Activation.apply(x, act, torch.is_grad_enabled())

@@ -328,3 +328,41 @@ def test_autocast_changes_nothing(name, dtype, auto):
         if not inside:
             grads = torch.autograd.grad(y, leaves, dy)
         assert all(a.dtype == b.dtype and torch.equal(a, b) for a, b in zip([y.detach(), *grads], want))
+
+
+# ------------------------------------------------------------------------------------------------- nothing is kept where no gradient is taken
+
+@gpu
+@pytest.mark.parametrize("name", ["layer", "rms", "gelu", "linear", "linear4"])
+def test_nothing_is_kept_for_no_backward_pass(name, monkeypatch):
+    d = torch.bfloat16
+    x, w, nw = numbers(1, 40, 96, d).cuda(), numbers(2, 64, 96, d).cuda(), numbers(4, 1, 96, d)[0].cuda()
+    packs, pack = [], mx.pack
+    monkeypatch.setattr(mx, "pack", lambda t, fmt=gb.MX8: packs.append(fmt) or pack(t, fmt))
+    call = {"layer": lambda: mx.norm(x, nw), "rms": lambda: mx.norm(x, nw, kind="rms"), "gelu": lambda: mx.activation(x), "linear": lambda: mx.linear(x, w),
+            "linear4": lambda: mx.linear(x, w, four=True)}[name]
+    four = [gb.MX4] * 2 if name == "linear4" else []
+    plain = call()                                                  # no leaf wants a gradient
+    assert packs == four and not plain.requires_grad
+    for t in (x, w, nw):
+        t.requires_grad_()
+    for mode in (torch.no_grad, torch.inference_mode):
+        del packs[:]
+        with mode():
+            y = call()
+        assert packs == four and torch.equal(y, plain)
+    del packs[:]
+    y = call()
+    assert packs == four + [gb.MX8] and torch.equal(y, plain)
+    leaves = [t for t in (x, w, nw) if torch.autograd.grad(y.float().sum(), t, allow_unused=True, retain_graph=True)[0] is not None]
+    assert len(leaves) == (1 if name == "gelu" else 2)
+    if name.startswith("linear"):                                   # the input's gradient alone reads the weight only
+        del packs[:]
+        w.requires_grad_(False)
+        assert torch.autograd.grad(call().float().sum(), x)[0].shape == x.shape and packs == four
+
+
+@pytest.mark.parametrize("call", [lambda: mx.norm(torch.ones(4, 64)), lambda: mx.activation(torch.ones(4, 64))])
+def test_no_path_on_the_cpu_without_gradients_either(call):
+    with pytest.raises(ValueError, match="CUDA"):
+        call()
