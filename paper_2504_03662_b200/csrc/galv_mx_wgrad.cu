@@ -12,6 +12,7 @@
 // fp16, where restoring is four instructions for four elements in place of nine, 390 to 460.  The loop of matrix instructions alone runs at 1772 TFLOP/s; what
 // is left is restored rows that come late (698 cycles a chunk for 512 of matrix instructions) and the power limit.
 
+#include <atomic>
 #include <type_traits>
 
 #include "galv_mx.cuh"
@@ -509,7 +510,14 @@ template <typename T, typename O>
 cudaError_t launch(const WgradPlan& p, const CUtensorMap& dy, const CUtensorMap& codes, const CUtensorMap& scales, const WgradArgs& a, cudaStream_t st)
 {
     // the registers that the kernel hands round are those it was built with: any other build would wait for what it never had
-    static const int regs = [] { cudaFuncAttributes f; return cudaFuncGetAttributes(&f, mx_wgrad_kernel<T, O>) == cudaSuccess ? f.numRegs : 0; }();
+    static std::atomic<int> known{0};
+    int regs = known.load(std::memory_order_relaxed);
+    if (!regs) {
+        cudaFuncAttributes f;
+        const cudaError_t e = cudaFuncGetAttributes(&f, mx_wgrad_kernel<T, O>);
+        if (e != cudaSuccess) return e;                   // of this call only: the next one asks again
+        known.store(regs = f.numRegs, std::memory_order_relaxed);
+    }
     if (regs * kThreads < 128 * kRegsIssue + 256 * kRegsSum + 128 * kRestoreGroups * kRegsRestore) return cudaErrorInvalidDeviceFunction;
     cudaError_t e = cudaFuncSetAttribute(mx_wgrad_kernel<T, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
