@@ -480,7 +480,7 @@ cudaError_t launch_few(const MatmulPlan& p, const CUtensorMap& am, const CUtenso
 }
 
 template <typename O>
-cudaError_t launch(const MatmulPlan& p, const CUtensorMap& am, const CUtensorMap& bm, const MatmulArgs& a, cudaStream_t st)
+cudaError_t launch(const galv_ctx* ctx, const MatmulPlan& p, const CUtensorMap& am, const CUtensorMap& bm, const MatmulArgs& a, cudaStream_t st)
 {
     if (p.few == 16) return launch_few<O, 16>(p, am, bm, a, st);
     if (p.few == 32) return launch_few<O, 32>(p, am, bm, a, st);
@@ -488,7 +488,7 @@ cudaError_t launch(const MatmulPlan& p, const CUtensorMap& am, const CUtensorMap
     cudaError_t e = cudaFuncSetAttribute(mx_matmul_kernel<O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
     mx_matmul_kernel<O><<<p.clusters * 2, kThreads, kSmem, st>>>(am, bm, a);
-    if (a.partial) mx_matmul_join_kernel<O><<<148 * 8, 256, 0, st>>>(a.m, a.n, a.splits, a.partial, (const O*)a.bias, (O*)a.y, a.stride);
+    if (a.partial) mx_matmul_join_kernel<O><<<ctx->num_sms * 8, 256, 0, st>>>(a.m, a.n, a.splits, a.partial, (const O*)a.bias, (O*)a.y, a.stride);
     return cudaGetLastError();
 }
 
@@ -529,7 +529,7 @@ extern "C" int galv_mx_matmul(galv_ctx* ctx, int64_t m, int64_t n, int64_t k, co
     a.a_scales = a_scales; a.b_scales = b_scales; a.bias = bias; a.y = y; a.timeouts = ctx->mx_timeouts_at;
     a.partial = p.partial ? reinterpret_cast<float*>(workspace) : nullptr;
     a.vec = p.partial ? n % 4 == 0 : n % 4 == 0 && y_stride % 4 == 0 && mx_aligned(y, 4 * mx_size_of(dtype));
-    MX_DISPATCH_TYPE(dtype, e = launch<T>(p, am, bm, a, (cudaStream_t)stream));
+    MX_DISPATCH_TYPE(dtype, e = launch<T>(ctx, p, am, bm, a, (cudaStream_t)stream));
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
 

@@ -507,7 +507,7 @@ WgradPlan plan_of(const galv_ctx* ctx, int64_t tokens, int64_t n, int64_t k, con
 }
 
 template <typename T, typename O>
-cudaError_t launch(const WgradPlan& p, const CUtensorMap& dy, const CUtensorMap& codes, const CUtensorMap& scales, const WgradArgs& a, cudaStream_t st)
+cudaError_t launch(const galv_ctx* ctx, const WgradPlan& p, const CUtensorMap& dy, const CUtensorMap& codes, const CUtensorMap& scales, const WgradArgs& a, cudaStream_t st)
 {
     // the registers that the kernel hands round are those it was built with: any other build would wait for what it never had
     static std::atomic<int> known{0};
@@ -522,7 +522,7 @@ cudaError_t launch(const WgradPlan& p, const CUtensorMap& dy, const CUtensorMap&
     cudaError_t e = cudaFuncSetAttribute(mx_wgrad_kernel<T, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
     mx_wgrad_kernel<T, O><<<p.clusters * 2, kThreads, kSmem, st>>>(dy, codes, scales, a);
-    if (a.partial) mx_wgrad_join_kernel<O><<<148 * 8, 256, 0, st>>>(a.n * a.k, a.splits, a.partial, (const O*)a.base, (O*)a.dw);
+    if (a.partial) mx_wgrad_join_kernel<O><<<ctx->num_sms * 8, 256, 0, st>>>(a.n * a.k, a.splits, a.partial, (const O*)a.base, (O*)a.dw);
     return cudaGetLastError();
 }
 
@@ -581,8 +581,8 @@ extern "C" int galv_mx_weight_grad(galv_ctx* ctx, int64_t tokens, int64_t n, int
         a.partial = p.partial ? reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + p.aligned) : nullptr;
         const int four = p.partial ? 16 : 4 * mx_size_of(dw_dtype);
         a.vec = k % 4 == 0 && (p.partial || (mx_aligned(dw, four) && mx_aligned(base, four)));
-        if (dtype == GALV_BF16) e = dw_dtype == GALV_F32 ? launch<__nv_bfloat16, float>(p, dm, cm, sm, a, st) : launch<__nv_bfloat16, __nv_bfloat16>(p, dm, cm, sm, a, st);
-        else e = dw_dtype == GALV_F32 ? launch<__half, float>(p, dm, cm, sm, a, st) : launch<__half, __half>(p, dm, cm, sm, a, st);
+        if (dtype == GALV_BF16) e = dw_dtype == GALV_F32 ? launch<__nv_bfloat16, float>(ctx, p, dm, cm, sm, a, st) : launch<__nv_bfloat16, __nv_bfloat16>(ctx, p, dm, cm, sm, a, st);
+        else e = dw_dtype == GALV_F32 ? launch<__half, float>(ctx, p, dm, cm, sm, a, st) : launch<__half, __half>(ctx, p, dm, cm, sm, a, st);
     }
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
