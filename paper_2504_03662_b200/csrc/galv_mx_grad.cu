@@ -191,9 +191,11 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 // Sums over the threads that share a row: a warp, a CTA (one barrier; `red` is another one in turn) or a cluster's CTAs (SPLIT: each warp's sums go to all of
-// them).  SQUARES: w is a sum of squares around the mean of the warp's values, whose sum is x; it becomes that around the mean of all (the squares of the
-// distances between the means, times the values behind them, are added), so that mean and deviation take one barrier, not two (2048 x 12288 in fp32,
-// shared by two CTAs: 104 us and 114; no difference within one CTA).  counts: values of each warp, and one over it.
+// them).  SQUARES: x is the mean of the warp's values in every lane, w a sum of squares around it, z one of products with numbers whose sum is y.  x
+// becomes the sum of all values, w and z those around the mean of all (the distances between the means, their squares times the values behind them and
+// themselves times y, are added), so that mean and deviation take one barrier, not two (2048 x 12288 in fp32, shared by two CTAs: 104 us and 114; no
+// difference within one CTA).  A product sum around zero, from which the mean's part came off afterwards, lost three digits where a row's values are nearly
+// equal.  counts: values of each warp, and a 32nd of that (the warp's sum of x is 32 times x, exactly).
 template <int W, bool SPLIT, bool SQUARES>
 __device__ __forceinline__ float4 row_sums(const float4& v, float4* red, const float2* counts, float inv_n, int share, int rank)
 {
@@ -212,24 +214,33 @@ __device__ __forceinline__ float4 row_sums(const float4& v, float4* red, const f
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int e = lane; e < entries; e += 32) {
             const float4 o = red[e];
-            sum.x += o.x; sum.y += o.y; sum.z += o.z;
+            sum.x = SQUARES ? fmaf(o.x, counts[e].y, sum.x) : sum.x + o.x;
+            sum.y += o.y;
+            if (!SQUARES) sum.z += o.z;
         }
         c = warp_sums(sum);
     }
     float4 r;
     r.x = __shfl_sync(0xffffffffu, c, 0);
     r.y = __shfl_sync(0xffffffffu, c, 8);
-    r.z = __shfl_sync(0xffffffffu, c, 16);
     r.w = 0.f;
-    if (W == 32) {
-        r.w = __shfl_sync(0xffffffffu, c, 24);
-    } else if (SQUARES) {
+    if (W > 32 && SQUARES) {
+        float products = 0.f;
         for (int e = lane; e < entries; e += 32) {
-            const float2 n = counts[e];
-            const float apart = red[e].x * n.y - r.x * inv_n;
-            r.w += fmaf(apart * apart, n.x, red[e].w);
+            const float4 o = red[e];
+            const float apart = o.x * (1.f / 32.f) - r.x * inv_n;
+            r.w += fmaf(apart * apart, counts[e].x, o.w);
+            products += fmaf(apart, o.y, o.z);
         }
-        r.w = warp_sum(r.w);
+        float both = lane & 16 ? products : r.w;           // lanes 0 .. 15 end with the squares
+        both += __shfl_xor_sync(0xffffffffu, lane & 16 ? r.w : products, 16);
+#pragma unroll
+        for (int o = 8; o; o >>= 1) both += __shfl_xor_sync(0xffffffffu, both, o);
+        r.w = __shfl_sync(0xffffffffu, both, 0);
+        r.z = __shfl_sync(0xffffffffu, both, 16);
+    } else {
+        r.z = __shfl_sync(0xffffffffu, c, 16);
+        if (W == 32) r.w = __shfl_sync(0xffffffffu, c, 24);
     }
     return r;
 }
@@ -281,12 +292,12 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
         int n = 0;
 #pragma unroll
         for (int p = 0; p < PP; ++p) n += max(0, min(256, there - (w * 32 + p * width) * 8));
-        counts[threadIdx.x] = make_float2((float)n, n ? 1.f / (float)n : 0.f);
+        counts[threadIdx.x] = make_float2((float)n, (float)n * (1.f / 32.f));
     }
     if (SPLIT) tc::cluster_sync();
     else __syncthreads();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const float inv_warp = LAYER ? WARP ? inv_n : counts[rank * (W / 32) + threadIdx.x / 32].y : 0.f;
+    const float mine_n = LAYER && !WARP ? counts[rank * (W / 32) + threadIdx.x / 32].x : 0.f, inv_warp = WARP ? inv_n : mine_n > 0.f ? 1.f / mine_n : 0.f;
 
     float dw[kShared ? 8 : PP * 8] = {}, db[LAYER ? PP * 8 : 1] = {};
     auto sums_load = [&](int p) {
@@ -349,7 +360,8 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
                 asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.q[i].x), "=r"(w.q[i].y), "=r"(w.q[i].z), "=r"(w.q[i].w) : "r"(base + (lane + p * width) * kDy + i * 16));
             return w;
         };
-        // x: the sum (LAYER) or the sum of squares; y: dy * weight; z: dy * weight * x
+        // RMS: x is the sum of squares, z that of dy * weight * x.  LAYER: x is the warp's mean, w and z the sums of squares and of dy * weight * x around it,
+        // y that of dy * weight.
         float4 m = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int p = 0; p < PP; ++p) {
@@ -370,21 +382,26 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
             mx_from8(code.x, x + 8 * p);
             mx_from8(code.y, x + 8 * p + 4);
             s[p] = mx_scale((int)(word >> (at >> 2 & 3) * 8 & 255));
-            const Raw8<T> w = weights(p);
             float sx = 0.f, sgx = 0.f;                    // before the block's power of two
+            if (LAYER) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float v = x[8 * p + i], gw = raw_at<T>(d[p], i) * raw_at<T>(w, i);
-                sx = LAYER ? sx + v : fmaf(v, v, sx);
-                if (LAYER) m.y += gw;
-                sgx = fmaf(gw, v, sgx);
+                for (int i = 0; i < 8; ++i) sx += x[8 * p + i];
+                m.x = fmaf(sx, s[p], m.x);
+            } else {
+                const Raw8<T> w = weights(p);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float v = x[8 * p + i];
+                    sx = fmaf(v, v, sx);
+                    sgx = fmaf(raw_at<T>(d[p], i) * raw_at<T>(w, i), v, sgx);
+                }
+                m.x = fmaf(sx * s[p], s[p], m.x);
+                m.z = fmaf(sgx, s[p], m.z);
             }
-            m.x = LAYER ? fmaf(sx, s[p], m.x) : fmaf(sx * s[p], s[p], m.x);
-            m.z = fmaf(sgx, s[p], m.z);
         }
         float near = 0.f;
         if (LAYER) {                                      // the values around the warp's mean
-            near = warp_sum(m.x) * inv_warp;
+            m.x = near = warp_sum(m.x) * inv_warp;
 #pragma unroll
             for (int p = 0; p < PP; ++p) {
 #pragma unroll
@@ -395,16 +412,22 @@ __global__ void __launch_bounds__(W == 32 ? 256 : W, W == 32 ? (PP < 4 ? 2 : 1) 
                     for (int i = 0; i < 8; ++i)
                         if (i >= left) x[8 * p + i] = 0.f;
                 }
+                const Raw8<T> w = weights(p);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) m.w = fmaf(x[8 * p + i], x[8 * p + i], m.w);
+                for (int i = 0; i < 8; ++i) {
+                    const float v = x[8 * p + i], gw = raw_at<T>(d[p], i) * raw_at<T>(w, i);
+                    m.w = fmaf(v, v, m.w);
+                    m.y += gw;
+                    m.z = fmaf(gw, v, m.z);
+                }
             }
         }
         m = row_sums<W, SPLIT, LAYER>(m, red[turn], counts, inv_n, share, rank);
-        float sq = m.x, sgx = m.z, mg = 0.f, shift = 0.f;
+        const float sgx = m.z;
+        float sq = m.x, mg = 0.f, shift = 0.f;
         if (LAYER) {
             const float mean = WARP ? near : m.x * inv_n;
             mg = m.y * inv_n;
-            sgx -= mean * m.y;
             sq = m.w;
             shift = mean - near;
         }

@@ -366,3 +366,38 @@ def test_nothing_is_kept_for_no_backward_pass(name, monkeypatch):
 def test_no_path_on_the_cpu_without_gradients_either(call):
     with pytest.raises(ValueError, match="CUDA"):
         call()
+
+
+# ------------------------------------------------------------------------------------------------- norms of nearly equal values
+
+@gpu
+@pytest.mark.parametrize("cols", [64, 256, 512, 1024, 2048, 4096, 8192, 16384, 32768])
+def test_layer_norm_gradients_of_nearly_equal_values(cols):
+    """Rows of ones with three values of 15/16, gradients around one: the product sum of gradient and value is a small difference of large sums unless the values are
+    taken around a mean.
+
+    The widths are powers of two, so sums, means and deviations are exact in 32 bits, whichever values they are taken around first.  What is left is counted:
+    96 half steps (chains of fewer than 64 additions and a handful of operations) of what each term is made of.  A product sum is made of |g| |x - near| and
+    |g| |near - mean| for means `near` of parts of the row, whose distances from the row's mean add up to at most those of the values.  The sum of squares, and with it
+    r, is off by 96 half steps.
+    """
+    rng = np.random.default_rng(cols)
+    rows = 6
+    x = np.ones((rows, cols))
+    for row in x:
+        row[rng.integers(0, cols, 3)] = 15 / 16
+    dy = torch.from_numpy(1 + rng.standard_normal((rows, cols))).float()
+    kept, held = packed(torch.from_numpy(x).float(), 8)
+    assert (held == x).all()
+    g = f64(dy)
+    d = x - x.mean(1, keepdims=True)
+    r = 1 / np.sqrt((d * d).mean(1, keepdims=True) + 1e-5)
+    xn = d * r
+    want = r * (g - g.mean(1, keepdims=True) - xn * (g * xn).mean(1, keepdims=True))
+    made = r * ((np.abs(g) * np.abs(d)).mean(1, keepdims=True) + 2 * np.abs(g).max(1, keepdims=True) * np.abs(d).mean(1, keepdims=True))
+    c = 96 * HALF
+    tol = r * (c * (np.abs(g) + np.abs(g).mean(1, keepdims=True)) + np.abs(xn) * (c * made + 3 * c * np.abs((g * xn).mean(1, keepdims=True)))) + c * np.abs(want) + HALF * np.abs(want)
+    dx, dw, db = mx.norm_backward(dy.cuda(), kept)
+    close(dx, want, tol, "dx")
+    close(dw, (g * xn).sum(0), (c + rows * HALF) * np.abs(g * xn).sum(0), "dweight")
+    close(db, g.sum(0), rows * HALF * np.abs(g).sum(0), "dbias")
