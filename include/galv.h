@@ -464,7 +464,8 @@ int galv_mx_pack(galv_ctx* ctx, int64_t rows, int64_t cols, const void* x, int64
                  uint8_t* codes, uint8_t* scales, void* stream);
 int galv_mx_unpack(galv_ctx* ctx, int64_t rows, int64_t cols, int32_t fmt, const uint8_t* codes, const uint8_t* scales,
                    void* x, int64_t x_stride, int32_t dtype, void* stream);
-/* dx = dy * f'(x), the activation function's input x held in GALV_MX8.  dx may be dy (same pointer and stride). */
+/* dx = dy * f'(x), the activation function's input x held in GALV_MX8.  dx may be dy (same pointer and stride).  Slopes are within 4e-7 (GALV_ACT_GELU_TANH
+ * 1e-6) of the formula's, of slopes that reach 1.13: far out, where a slope is near zero, that says little of its own digits. */
 int galv_mx_act_backward(galv_ctx* ctx, int64_t rows, int64_t cols, int32_t act, const uint8_t* codes, const uint8_t* scales,
                          const void* dy, int64_t dy_stride, void* dx, int64_t dx_stride, int32_t dtype, void* stream);
 /*
@@ -472,7 +473,8 @@ int galv_mx_act_backward(galv_ctx* ctx, int64_t rows, int64_t cols, int32_t act,
  * values, so the gradients are exactly the formula's at that point.  weight [cols] of `dtype`, NULL: ones.
  * dweight = sum over rows of dy * xhat, dbias = sum over rows of dy (both fp32 [cols]; summed in a fixed order: the same call
  * gives the same bits).  dweight may be NULL, dbias must be NULL for GALV_NORM_RMS and may be for the other.  eps >= 0;
- * a row of equal values with eps = 0 gives NaN or infinity as the formula does.  With rows = 0 dweight and dbias are zeros.
+ * a row of equal values with eps = 0 gives NaN or infinity as the formula does, and so does a row whose sum of squares leaves fp32, in which statistics
+ * are taken.  With rows = 0 dweight and dbias are zeros.
  * dx may be dy (same pointer and stride).  workspace: 256-byte aligned, the bytes that the query gives (0, for few rows: may be NULL).
  */
 size_t galv_mx_norm_workspace_bytes(const galv_ctx* ctx, int64_t rows, int64_t cols);
@@ -485,8 +487,9 @@ int galv_mx_norm_backward(galv_ctx* ctx, int64_t rows, int64_t cols, int32_t kin
  *   dw[n][k] = base[n][k] + sum_t dy[t][n] x[t][k]
  * dy [tokens][n] of `dtype` (GALV_BF16 or GALV_F16), dw and base [n][k] contiguous of `dw_dtype` (`dtype` or GALV_F32); base NULL: zero;
  * dw may be base.  x enters the product in dy's type, which holds its elements exactly unless they leave that type's range
- * (GALV_F16: saturating at 65504; small ones rounded as subnormals); products are summed in fp32, base is added in fp32, and the sum
- * rounded once.  The order of the sums is fixed by sizes, strides and alignment.  With tokens = 0, dw is base or zeros.
+ * (GALV_F16: saturating at 65504; small ones rounded as subnormals); products are summed in fp32 (by the
+ * tensor cores, which may cut an addition where rounding would halve the error, over 1024 tokens at most, then by rounded additions: 8e-7 of a result's
+ * 2-norm at 1000 tokens), base is added in fp32, and the sum rounded once.  The order of the sums is fixed by sizes, strides and alignment.  With tokens = 0, dw is base or zeros.
  * workspace: 256-byte aligned, the bytes that the query gives for the same sizes, dy pointer and stride (0: may be NULL).
  */
 size_t galv_mx_weight_grad_workspace_bytes(const galv_ctx* ctx, int64_t tokens, int64_t n, int64_t k, const void* dy,
@@ -497,7 +500,7 @@ int galv_mx_weight_grad(galv_ctx* ctx, int64_t tokens, int64_t n, int64_t k, con
 /*
  * Product of two matrices held in GALV_MX4, a [m][k] and b [n][k]:
  *   y[i][j] = sum_k a[i][k] b[j][k] + bias[j]
- * summed in fp32 and rounded once to `dtype` (any of the three).  bias [n] of `dtype`, NULL: none.  The order of the sums is fixed
+ * summed in fp32 (by the tensor cores, over all of k that a split has) and rounded once to `dtype` (any of the three).  bias [n] of `dtype`, NULL: none.  The order of the sums is fixed
  * by the sizes.  With m = 0 nothing is written.  workspace as above.
  */
 size_t galv_mx_matmul_workspace_bytes(const galv_ctx* ctx, int64_t m, int64_t n, int64_t k);

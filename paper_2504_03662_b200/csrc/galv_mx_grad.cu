@@ -127,8 +127,8 @@ __global__ void __launch_bounds__(kMxThreads) mx_act_kernel(const MxSpread sprea
 // One pass: a row's codes and gradient are read once, its statistics and the two means of the gradient come from registers, and the column sums stay with
 // the thread that has the column, over all rows that its CTA takes (where a thread has two pieces of 8 columns, dweight's in shared memory: with both sums in
 // registers only half as many threads fit, and the pass took twice as long).  The next rows are on their way into shared memory
-// meanwhile, each thread's pieces its own, so that only the rows' sums need a barrier.  2048 x 12288 in bf16 take 52.5 us for a layer norm and 41.7 for an
-// rms norm (2.4 and 3.0 TB/s): 39 instructions an element at 60 % of the issue slots, the rest waits for shuffles, shared memory and the row's sums.
+// meanwhile, each thread's pieces its own, so that only the rows' sums need a barrier.  2048 x 12288 in bf16 take 52.0 us for a layer norm and 41.5 for an
+// rms norm (2.4 and 3.1 TB/s): 38 instructions an element at 59 % of the issue slots, the rest waits for shuffles, shared memory and the row's sums.
 
 constexpr int kBlockThreads = 1024;
 constexpr int kWarpColumns = 1024;                        // up to here a warp has a row to itself, and no barrier
@@ -676,7 +676,7 @@ NormPlan norm_plan(const galv_ctx* ctx, int64_t rows, int64_t cols, int32_t dtyp
     }
     // A row that one CTA cannot hold is shared by two of a cluster, which exchange its sums over a cluster barrier, up to 16384 columns of fp32 and 32768
     // of 16 bits, or four, up to 65536: 2048 x 12288 in fp32 takes 104 us for a layer norm, 300 with the kernels for wide rows; 1024 x 32768 in bf16
-    // 99 and 173; 512 x 49152 84 and 128.  What one CTA holds it keeps (2048 x 12288 in bf16: 53 us, shared by two 90), and fp32 shared by four
+    // 100 and 173; 512 x 49152 81 and 128.  What one CTA holds it keeps (2048 x 12288 in bf16: 53 us, shared by two 90), and fp32 shared by four
     // is no faster than the wide kernels (1024 x 32768: 220 to 275 us and 233).  With four, 32 clusters run at once, not 37.
     const int64_t most_pieces = four ? 1024 : 2048;       // of a CTA
     const int clusters = four || pieces <= 2 * most_pieces ? 2 : 4;

@@ -287,7 +287,8 @@ __global__ void __launch_bounds__(256) mx_matmul_join_kernel(long long m, long l
 // Up to 64 rows of a: reading b is all there is.  b's rows take the tensor cores' 128 rows and a's the columns (16 to 64 of them), a CTA has 128 rows
 // of b, and the CTAs of a cluster share the summed index, so that about one CTA an SM streams b.  Each sends its sums' slices of a's rows
 // to the CTA of the cluster that has them, which adds them in order: no second kernel, no memory between.  With 8192 x 8192 of b, 7 rows of a take 10.1 us
-// (17.0 in the kernel above and its second one), 64 rows 14.8 (17.2); 128 would take 21.1 (20.0), so they do not come here.
+// (17.0 in the kernel above and its second one), 64 rows 14.8 (17.2); 128 would take 21.1 (20.0), so they do not come here.  (Calls one behind the other:
+// 8.8 and 13.6 us where b stays in L2, 10.8 and 16.0 where it comes from memory.)
 
 constexpr int kFewThreads = 256;
 template <int N> struct Few {                             // N: rows of a, rounded up

@@ -11,6 +11,8 @@
 // 4096 tokens x 8192 x 8192 in bf16 take 412 to 500 us by the card's power state (1100 to 1335 TFLOP/s; a plain library product of 16-bit inputs 1590), in
 // fp16, where restoring is four instructions for four elements in place of nine, 390 to 460.  The loop of matrix instructions alone runs at 1772 TFLOP/s; what
 // is left is restored rows that come late (698 cycles a chunk for 512 of matrix instructions) and the power limit.
+// Every value is restored once for each 256 columns of dy.  Restoring x to a matrix of its own first (2 bytes an element more) and multiplying that by the
+// library is the faster way for large shapes: 4096 x 8192 x 32768 into bf16 1600 us sustained and 1900 here, 4096 x 8192 x 8192 412 and 483, 2048^3 21.5 and 22.5.
 
 #include <atomic>
 #include <type_traits>
