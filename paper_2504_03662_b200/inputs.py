@@ -87,8 +87,8 @@ class Workload:
     layers: Optional[np.ndarray] = None         # [B or 1][Lmax] LAYER_DESC
     strat: Optional[np.ndarray] = None          # [S] STRATEGY_DESC
     inst: Optional[np.ndarray] = None           # [B] INST_PARAMS
-    forms: Optional[np.ndarray] = None          # [S] FORM_DESC: how strategies keep and multiply (with layers only)
     meta: dict = field(default_factory=dict)
+    forms: Optional[np.ndarray] = None          # [S] FORM_DESC: how strategies keep and multiply (with layers only)
 
     @property
     def has_model(self) -> bool:
@@ -115,7 +115,7 @@ class Workload:
             layers = pick(layers)
         return Workload(self.name, len(idx), self.Lmax, self.S, self.M, pick(self.L),
                         pick(self.time_q), pick(self.mem_q), pick(self.trans_q),
-                        layers, self.strat, pick(self.inst), self.forms, dict(self.meta))
+                        layers, self.strat, pick(self.inst), dict(self.meta), self.forms)
 
     def with_forms(self, forms) -> "Workload":
         """Every strategy as it is, then every strategy in each of `forms` (rows of FORM_DESC): strategy f * S + s is s in form f."""

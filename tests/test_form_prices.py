@@ -114,3 +114,11 @@ def test_rates_of_nothing_are_refused(hidden, tokens):
     from paper_2504_03662_b200.search import measure_forms
     with pytest.raises(ValueError, match="at least 1"):
         measure_forms(SimpleNamespace(device=0), hidden, tokens)
+
+
+def test_workloads_are_made_as_they_were_before_they_had_forms():
+    w = inputs.config1()
+    again = inputs.Workload(w.name, w.B, w.Lmax, w.S, w.M, w.L, None, None, None, w.layers, w.strat, w.inst, {"pp": 1})
+    assert again.meta == {"pp": 1} and again.forms is None
+    f = w.with_forms([(8, 0, 1e-12, 1.0)])
+    assert f.take(slice(0, 2)).forms is f.forms and f.take(slice(0, 2)).meta == f.meta
