@@ -411,11 +411,10 @@ int galv_skip_estimate(galv_ctx* ctx, const galv_shape* shape, const int32_t* L,
  * and time_q, mem_q are written again from them; other entries, layers l >= L[i] and instances that galv_eval_costs has flagged
  * stay as they are.  The two rates come from the operators as measured on the device (search.py does so).  A form that is none
  * (other bits, a negative or non-finite rate, mul_speed not positive) gets -1 in its strategy's entries, which
- * galv_dp_search flags.  forms [S]; the other arguments are those of galv_eval_costs, time_s and mem_bytes required.
+ * galv_dp_search flags.  forms [S]; the other arguments are those of galv_eval_costs (`layers`: see below), time_s and mem_bytes required.
  * kept is taken for bytes of 16-bit numbers, whatever bytes_per_elem is, as the cost model counts them, and 33/32 bytes hold an element (rows whose
- * length is no multiple of 512 hold up to 15 scale bytes more).  What a layer's act_rep and act_tp count besides numbers does not shrink: a model with
- * dropout keeps one-byte masks (two of a full layer's 34 bytes, one of an attention or a feed-forward layer's), for each of which a plan in 8 bits needs
- * act_mult * seq * b * h * 31/64 bytes more than mem'.
+ * length is no multiple of 512 hold up to 15 scale bytes more).  What a layer's act_rep counts besides numbers does not shrink (a model with dropout keeps
+ * one-byte masks: 2 of a full layer's 34 bytes, 1 of an attention or a feed-forward layer's): `layers` here are those of galv_eval_costs with act_rep less it.
  */
 int galv_add_form_cost(galv_ctx* ctx, const galv_shape* shape, const int32_t* L,
                        const galv_layer_desc* layers, int64_t layer_stride_B,

@@ -89,6 +89,7 @@ class Workload:
     inst: Optional[np.ndarray] = None           # [B] INST_PARAMS
     meta: dict = field(default_factory=dict)
     forms: Optional[np.ndarray] = None          # [S] FORM_DESC: how strategies keep and multiply (with layers only)
+    masks: Optional[np.ndarray] = None          # [B or 1][Lmax]: of a layer's act_rep, what does not shrink in 8 bits (with forms only)
 
     @property
     def has_model(self) -> bool:
@@ -110,15 +111,28 @@ class Workload:
         """The sub-batch made of the instances `idx` (a slice or index list)."""
         idx = np.arange(self.B)[idx]
         pick = lambda a: None if a is None else np.ascontiguousarray(a[idx])
-        layers = self.layers
+        layers, masks = self.layers, self.masks
         if layers is not None and layers.shape[0] != 1:
-            layers = pick(layers)
+            layers, masks = pick(layers), pick(masks)
         return Workload(self.name, len(idx), self.Lmax, self.S, self.M, pick(self.L),
                         pick(self.time_q), pick(self.mem_q), pick(self.trans_q),
-                        layers, self.strat, pick(self.inst), dict(self.meta), self.forms)
+                        layers, self.strat, pick(self.inst), dict(self.meta), self.forms, masks)
 
-    def with_forms(self, forms) -> "Workload":
-        """Every strategy as it is, then every strategy in each of `forms` (rows of FORM_DESC): strategy f * S + s is s in form f."""
+    @property
+    def form_layers(self) -> Optional[np.ndarray]:
+        """The layers as forms see them: act_rep without what does not shrink."""
+        if self.masks is None:
+            return self.layers
+        layers = self.layers.copy()
+        layers["act_rep"] -= self.masks
+        return layers
+
+    def with_forms(self, forms, masks=0.0) -> "Workload":
+        """Every strategy as it is, then every strategy in each of `forms` (rows of FORM_DESC): strategy f * S + s is s in form f.
+
+        masks: what of the layers' act_rep are no 16-bit numbers and stays as it is in 8 bits, bytes a token and hidden unit (a number, or one a
+        layer).  A model with dropout keeps one-byte masks: the 10 of a full layer have 2 of them, the 5 of an attention or feed-forward layer 1.
+        """
         if not self.has_model:
             raise ValueError("forms are priced by the cost model: a workload of measured tables has its own times and sizes")
         if self.forms is not None:
@@ -126,8 +140,12 @@ class Workload:
         rows = np.concatenate([np.array([(0, 0, 0.0, 1.0)], FORM_DESC), np.asarray(forms, FORM_DESC).reshape(-1)])
         if self.S * len(rows) > 256:
             raise ValueError(f"{self.S} strategies in {len(rows)} forms: at most 256 in all")
+        masks = np.broadcast_to(np.asarray(masks, np.float64), self.layers.shape)
+        if not ((masks >= 0) & (masks <= self.layers["act_rep"])).all():
+            raise ValueError("masks are a part of act_rep: between 0 and it")
         return Workload(self.name + "_forms", self.B, self.Lmax, self.S * len(rows), self.M, self.L, layers=self.layers,
-                        strat=np.tile(self.strat, len(rows)), inst=self.inst, forms=np.repeat(rows, self.S), meta=dict(self.meta))
+                        strat=np.tile(self.strat, len(rows)), inst=self.inst, meta=dict(self.meta), forms=np.repeat(rows, self.S),
+                        masks=masks.copy() if masks.any() else None)
 
 
 # --------------------------------------------------------------------------- random tables

@@ -94,6 +94,7 @@ class SearchBuffers:
         self.time_s = self.mem_bytes = self.forms = None
         if w.forms is not None:
             self.forms = _dev_bytes(w.forms, dev)
+            self.form_layers = self.layers if w.masks is None else _dev_bytes(w.form_layers, dev)
         self.C = torch.empty(B, Lm, S, P, **i32) if flags & gb.STORE_C_FULL else None
         self.A = torch.empty(B, Lm, S, P, dtype=torch.uint8, device=dev) if flags & gb.STORE_ARGMIN else None
         self.C_last = torch.empty(B, S, P, **i32)
@@ -114,7 +115,7 @@ class SearchBuffers:
                                   self.time_s if want_fp64 else None, self.mem_bytes if want_fp64 else None,
                                   self.time_q, self.mem_q, self.trans_q, self.status)
         if self.forms is not None:
-            self.galv.galv_add_form_cost(self.shape, self.L, self.layers, self.layer_stride_B, self.strat, self.inst, self.forms,
+            self.galv.galv_add_form_cost(self.shape, self.L, self.form_layers, self.layer_stride_B, self.strat, self.inst, self.forms,
                                          self.time_s, self.mem_bytes, self.time_q, self.mem_q)
 
     def dp_search(self):

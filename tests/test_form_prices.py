@@ -122,3 +122,34 @@ def test_workloads_are_made_as_they_were_before_they_had_forms():
     assert again.meta == {"pp": 1} and again.forms is None
     f = w.with_forms([(8, 0, 1e-12, 1.0)])
     assert f.take(slice(0, 2)).forms is f.forms and f.take(slice(0, 2)).meta == f.meta
+
+
+def test_masks_are_a_part_of_the_layers():
+    w = inputs.config3(4)
+    held = w.with_forms([(8, 0, 1e-12, 1.0)], masks=1.0)
+    assert (held.form_layers["act_rep"] == 4.0).all() and (held.layers["act_rep"] == 5.0).all() and (held.take(slice(1, 3)).masks == 1.0).all()
+    each = np.where(np.arange(w.Lmax) % 2 == 0, 1.0, 0.0)
+    assert (w.with_forms([(8, 0, 1e-12, 1.0)], masks=each).form_layers["act_rep"][0] == 5.0 - each).all()
+    assert w.with_forms([(8, 0, 1e-12, 1.0)]).masks is None
+    for bad in (-1.0, 6.0, float("nan")):
+        with pytest.raises(ValueError, match="masks"):
+            w.with_forms([(8, 0, 1e-12, 1.0)], masks=bad)
+
+
+@gpu
+@pytest.mark.parametrize("sp", [0, 1])
+def test_masks_keep_their_bytes(sp):
+    """A layer with two one-byte masks beside its numbers: in 8 bits it holds the packed numbers and the masks."""
+    from paper_2504_03662_b200 import binding as gb
+    from paper_2504_03662_b200.search import SearchBuffers
+    galv = gb.Galv(0)
+    mem = {}
+    for masks in (0.0, 2.0):
+        w = one_layer(0, sp, 2.0)
+        w.layers["act_rep"] += masks
+        sb = SearchBuffers(galv, w.with_forms([(8, 0, 0.0, 1.0)], masks=masks))
+        sb.eval_costs()
+        mem[masks] = sb.mem_q.cpu().numpy()[0, 0] * 64
+    kept_masks = 3 * 2 * 2048 * 1024 // (2 if sp else 1)
+    assert (mem[2.0] - mem[0.0] == kept_masks).all()                # the same for the plain strategy and the one in 8 bits
+    galv.close()
