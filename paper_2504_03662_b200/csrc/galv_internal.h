@@ -71,7 +71,7 @@ struct galv_ctx {
     RsPlan plans[2];
     int plan_launches, plan_valid;
     unsigned* mx_timeouts;     // waits of microscaled products that have run out on this device: host memory that its kernels reach ...
-    unsigned* mx_timeouts_at;  // ... at this address
+    unsigned* mx_timeouts_at;  // ... at this address (NULL: they do not, and no product is launched)
     unsigned mx_timeouts_seen; // ... how many when this context was made or last looked
     char err[512];
 };
@@ -154,7 +154,7 @@ cudaError_t galv_encode_table_3d(CUtensorMap* map, void* base, size_t rows, int 
 // whether it can take the shape, which has no table to write; states: they are kept in its place
 bool galv_solo_plan(const galv_ctx* ctx, const galv_shape* sh, bool states, SoPlan* plan);
 cudaError_t galv_solo_configure(galv_ctx* ctx);
-cudaError_t galv_mx_configure(galv_ctx* ctx);
+void galv_mx_configure(galv_ctx* ctx);
 // whether a batch of some matrices can be worth it, given what the others' plans cost; n: of the resident kernel's launches; pushing: NULL when it cannot run the shape
 bool galv_solo_worth(const galv_ctx* ctx, const galv_shape* sh, bool states, int n, const RsPlan resident[2], const struct ClPlan* pushing, SoPlan* plan);
 cudaError_t galv_solo_launch(const SoPlan& plan, const struct DpArgs& a, cudaStream_t st);

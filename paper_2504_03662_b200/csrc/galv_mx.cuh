@@ -40,6 +40,12 @@ inline bool mx_ran_out(galv_ctx* ctx)
     ctx->mx_timeouts_seen = *(volatile unsigned*)ctx->mx_timeouts;
     return ctx->mx_timeouts_seen != seen;
 }
+// Whether a product may be launched.
+inline int mx_may_run(galv_ctx* ctx, const char* refused, const char* ran_out)
+{
+    if (!ctx->mx_timeouts_at) return galv_set_error(ctx, GALV_ERR_CUDA, refused);
+    return mx_ran_out(ctx) ? galv_set_error(ctx, GALV_ERR_TIMEOUT, ran_out) : GALV_OK;
+}
 
 template <int T> struct MxType;
 template <> struct MxType<GALV_F32> { using type = float; };

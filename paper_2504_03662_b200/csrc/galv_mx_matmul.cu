@@ -515,7 +515,8 @@ extern "C" int galv_mx_matmul(galv_ctx* ctx, int64_t m, int64_t n, int64_t k, co
     const MatmulPlan p = plan_of(ctx, m, n, k);
     if (p.partial && (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < p.partial))
         return galv_set_error(ctx, GALV_ERR_WORKSPACE, "galv_mx_matmul: workspace NULL, misaligned or too small");
-    if (mx_ran_out(ctx)) return galv_set_error(ctx, GALV_ERR_TIMEOUT, "galv_mx_matmul: a bounded wait of an earlier microscaled product ran out");
+    const int may = mx_may_run(ctx, "galv_mx_matmul: the library's host memory could not be registered", "galv_mx_matmul: a bounded wait of an earlier microscaled product ran out");
+    if (may != GALV_OK) return may;
     MxDevice dev(ctx);
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
     CUtensorMap am, bm;
@@ -535,29 +536,27 @@ extern "C" int galv_mx_matmul(galv_ctx* ctx, int64_t m, int64_t n, int64_t k, co
 }
 
 // Waits that have run out are counted in host memory, a line of 64 bytes a device, so that they can be read without waiting for anything.  The
-// memory is the process's own and only registered with CUDA: it outlives a device that is reset.
-cudaError_t galv_mx_configure(galv_ctx* ctx)
+// memory is the process's own and only registered with CUDA: it outlives a device that is reset.  Where it cannot be registered, only the products are refused.
+void galv_mx_configure(galv_ctx* ctx)
 {
     constexpr int most = 64, words = 16;
     alignas(4096) static unsigned counts[most * words];
+    static unsigned none = 0;
     static std::mutex registering;
-    if (ctx->device < 0 || ctx->device >= most) return cudaErrorInvalidDevice;
+    const bool in = ctx->device >= 0 && ctx->device < most;
+    ctx->mx_timeouts = in ? counts + ctx->device * words : &none;
+    ctx->mx_timeouts_at = nullptr;
     std::lock_guard<std::mutex> lock(registering);
     cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;         // another thread may be capturing
-    cudaError_t e = cudaThreadExchangeStreamCaptureMode(&mode);
-    if (e != cudaSuccess) return e;
-    e = cudaHostRegister(counts, sizeof(counts), cudaHostRegisterMapped | cudaHostRegisterPortable);
-    if (e == cudaErrorHostMemoryAlreadyRegistered) {
-        (void)cudaGetLastError();
-        e = cudaSuccess;
+    if (in && cudaThreadExchangeStreamCaptureMode(&mode) == cudaSuccess) {
+        void* at = nullptr;
+        const cudaError_t e = cudaHostRegister(counts, sizeof(counts), cudaHostRegisterMapped | cudaHostRegisterPortable);
+        if ((e == cudaSuccess || e == cudaErrorHostMemoryAlreadyRegistered) && cudaHostGetDevicePointer(&at, ctx->mx_timeouts, 0) == cudaSuccess)
+            ctx->mx_timeouts_at = static_cast<unsigned*>(at);
+        cudaThreadExchangeStreamCaptureMode(&mode);
     }
-    ctx->mx_timeouts = counts + ctx->device * words;
-    void* at = nullptr;
-    if (e == cudaSuccess) e = cudaHostGetDevicePointer(&at, ctx->mx_timeouts, 0);
-    ctx->mx_timeouts_at = static_cast<unsigned*>(at);
+    (void)cudaGetLastError();                             // what went wrong here is not the next call's
     ctx->mx_timeouts_seen = *(volatile unsigned*)ctx->mx_timeouts;
-    const cudaError_t back = cudaThreadExchangeStreamCaptureMode(&mode);
-    return e == cudaSuccess ? back : e;
 }
 
 extern "C" uint32_t* galv_mx_timeouts(const galv_ctx* ctx) { return ctx ? ctx->mx_timeouts : nullptr; }

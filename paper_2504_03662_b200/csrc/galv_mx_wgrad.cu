@@ -549,7 +549,8 @@ extern "C" int galv_mx_weight_grad(galv_ctx* ctx, int64_t tokens, int64_t n, int
     const size_t need = galv_mx_weight_grad_workspace_bytes(ctx, tokens, n, k, dy, dy_stride);
     if (need && (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < need))
         return galv_set_error(ctx, GALV_ERR_WORKSPACE, "galv_mx_weight_grad: workspace NULL, misaligned or too small");
-    if (mx_ran_out(ctx)) return galv_set_error(ctx, GALV_ERR_TIMEOUT, "galv_mx_weight_grad: a bounded wait of an earlier microscaled product ran out");
+    const int may = mx_may_run(ctx, "galv_mx_weight_grad: the library's host memory could not be registered", "galv_mx_weight_grad: a bounded wait of an earlier microscaled product ran out");
+    if (may != GALV_OK) return may;
     MxDevice dev(ctx);
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
     cudaStream_t st = (cudaStream_t)stream;
