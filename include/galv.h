@@ -506,9 +506,69 @@ size_t galv_mx_matmul_workspace_bytes(const galv_ctx* ctx, int64_t m, int64_t n,
 int galv_mx_matmul(galv_ctx* ctx, int64_t m, int64_t n, int64_t k, const uint8_t* a_codes, const uint8_t* a_scales,
                    const uint8_t* b_codes, const uint8_t* b_scales, const void* bias, void* y, int64_t y_stride, int32_t dtype,
                    void* workspace, size_t workspace_bytes, void* stream);
-/* Waits for `stream` and says whether a bounded device-side wait of galv_mx_weight_grad or galv_mx_matmul, of whichever context, has run out on this
+/*
+ * Rows of 8-bit integers: a matrix [rows][cols] with one scale a row, and products of two such matrices (the paper has no counterpart).
+ *   scale[r] = max(largest magnitude of row r, 2^-100) / 127 (fp32, rounded),  code[r][c] = the whole number nearest to x[r][c] / scale[r], ties to even
+ * decided by the exact quotient.  A row that holds an infinity or a NaN gets a NaN for its scale and zeros for its codes: it stands for NaN as a whole.
+ * codes [rows][cols rounded up to a multiple of 16] signed bytes, zero behind a row's end, 16-byte aligned; scales [rows] fp32.  Of tokens a row is a token, of
+ * weights [n][k] an output channel.  Matrices of numbers, limits and streams as above.
+ */
+#define GALV_I8_MOST 131071  /* columns of a product of 8-bit integers: sums of so many stay within 32 bits whatever the codes */
+size_t galv_i8_codes_bytes(int64_t rows, int64_t cols);
+int galv_i8_pack(galv_ctx* ctx, int64_t rows, int64_t cols, const void* x, int64_t x_stride, int32_t dtype, int8_t* codes, float* scales, void* stream);
+/* Results of numbers saturate at the largest number of fp32, fp16 ones at 65504. */
+int galv_i8_unpack(galv_ctx* ctx, int64_t rows, int64_t cols, const int8_t* codes, const float* scales, void* x, int64_t x_stride, int32_t dtype,
+                   void* stream);
+/*
+ * Products of rows by their expert's weights.  The rows of x are sorted by expert: expert e, of `experts` (1 .. 1024), has the rows from
+ * ends[e - 1] (0 for the first) to ends[e] - 1.  ends int32 [experts], device: read by the kernels, so the calls need not wait for it and can be captured.
+ * Ends that fall or leave 0 .. rows count as clamped between the one before and rows.  ends NULL: one expert that has all rows, a plain product.  Rows
+ * from the last end on belong to no expert: their results are zeros, and they enter no sum, whatever they hold.
+ *
+ * galv_i8_matmul:  y[r][j] = (sum_c x_code[r][c] w_code[e][j][c]) * (x_scale[r] * w_scale[e][j]) + bias[e][j]
+ * sums are whole numbers, exact; they are rounded to fp32, the product of the scales is taken in fp32, and the result rounded once more to `dtype` (any of the
+ * three).  w_codes [experts * n rows][k], w_scales [experts * n], bias [experts][n] of `dtype` or NULL.  k <= GALV_I8_MOST.
+ * galv_i8_linear:  the same with x in numbers of `dtype`, put into 8-bit integers in the call.  workspace: 256-byte aligned, the bytes that the query gives.
+ */
+int galv_i8_matmul(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const int8_t* x_codes,
+                   const float* x_scales, const int8_t* w_codes, const float* w_scales, const void* bias, void* y, int64_t y_stride,
+                   int32_t dtype, void* stream);
+size_t galv_i8_linear_workspace_bytes(int64_t rows, int64_t k);
+int galv_i8_linear(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* x, int64_t x_stride,
+                   const int8_t* w_codes, const float* w_scales, const void* bias, void* y, int64_t y_stride, int32_t dtype,
+                   void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * The same in 16 bits, w [experts][n][k] contiguous, everything of `dtype` (GALV_BF16 or GALV_F16):
+ *   galv_expert_matmul       y[r][j]  = sum_c x[r][c] w[e][j][c] + bias[e][j]       (bias [experts][n] or NULL)
+ *   galv_expert_input_grad   dx[r][c] = sum_j dy[r][j] w[e][j][c]
+ *   galv_expert_weight_grad  dw[e][j][c] = base[e][j][c] + sum over e's rows of dy[r][j] x[r][c]
+ *   galv_expert_bias_grad    db[e][j] = sum over e's rows of dy[r][j]
+ * Sums are fp32 (the first three by the tensor cores, which may cut an addition where rounding would halve the error; dw's over 1024 rows at most, then by
+ * rounded additions), biases and base are added in fp32, results rounded once.  dw, base [experts][n][k] contiguous of `dw_dtype`, db [experts][n] of
+ * `db_dtype` (`dtype` or GALV_F32); base NULL: zero; dw may be base.  An expert without rows has base or zeros for its gradient.  The order of
+ * the sums is fixed by sizes, ends, strides and alignment.  Operands whose rows do not start on 16-byte boundaries are moved to ones that do, in the
+ * workspace (256-byte aligned, the bytes that the query gives for the same sizes, pointers and strides; 0: may be NULL).
+ */
+size_t galv_expert_matmul_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* x,
+                                          int64_t x_stride, const void* w);
+int galv_expert_matmul(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* x,
+                       int64_t x_stride, const void* w, const void* bias, void* y, int64_t y_stride, int32_t dtype, void* workspace,
+                       size_t workspace_bytes, void* stream);
+size_t galv_expert_input_grad_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy,
+                                              int64_t dy_stride, const void* w);
+int galv_expert_input_grad(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* dy,
+                           int64_t dy_stride, const void* w, void* dx, int64_t dx_stride, int32_t dtype, void* workspace,
+                           size_t workspace_bytes, void* stream);
+size_t galv_expert_weight_grad_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy,
+                                               int64_t dy_stride, const void* x, int64_t x_stride);
+int galv_expert_weight_grad(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* dy,
+                            int64_t dy_stride, const void* x, int64_t x_stride, int32_t dtype, const void* base, void* dw, int32_t dw_dtype,
+                            void* workspace, size_t workspace_bytes, void* stream);
+int galv_expert_bias_grad(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, const int32_t* ends, const void* dy, int64_t dy_stride,
+                          int32_t dtype, void* db, int32_t db_dtype, void* stream);
+/* Waits for `stream` and says whether a bounded device-side wait of a product (galv_mx_weight_grad, galv_mx_matmul, galv_i8_*, galv_expert_*), of whichever context, has run out on this
  * device since this context was made or last looked (GALV_ERR_TIMEOUT: the results since then are void; GALV_OK otherwise).  Not for stream capture.
- * Both products look too, without waiting, and return GALV_ERR_TIMEOUT in place of a launch; replays of a captured graph do not look. */
+ * The products look too, without waiting, and return GALV_ERR_TIMEOUT in place of a launch; replays of a captured graph do not look. */
 int galv_mx_status(galv_ctx* ctx, void* stream);
 /* Where the device's count of such waits lies: host memory of the library, to be read (volatile) at any time without waiting; NULL without a context. */
 uint32_t* galv_mx_timeouts(const galv_ctx* ctx);

@@ -33,6 +33,7 @@ F32, BF16, F16 = 0, 1, 2
 MX8, MX4 = 8, 4
 ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2
 NORM_LAYER, NORM_RMS = 0, 1
+I8_MOST, EXPERTS_MOST = 131071, 1024
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libgalv.so")
 
@@ -45,7 +46,10 @@ EXPORTS = ("galv_create", "galv_destroy", "galv_strerror", "galv_last_error", "g
            "galv_switch_decision", "galv_skip_estimate", "galv_mx_codes_bytes", "galv_mx_scales_bytes", "galv_mx_pack",
            "galv_mx_unpack", "galv_mx_act_backward", "galv_mx_norm_workspace_bytes", "galv_mx_norm_backward",
            "galv_mx_weight_grad_workspace_bytes", "galv_mx_weight_grad", "galv_mx_matmul_workspace_bytes", "galv_mx_matmul",
-           "galv_add_form_cost", "galv_mx_status", "galv_mx_timeouts")
+           "galv_add_form_cost", "galv_mx_status", "galv_mx_timeouts", "galv_i8_codes_bytes", "galv_i8_pack", "galv_i8_unpack",
+           "galv_i8_matmul", "galv_i8_linear_workspace_bytes", "galv_i8_linear", "galv_expert_matmul_workspace_bytes",
+           "galv_expert_matmul", "galv_expert_input_grad_workspace_bytes", "galv_expert_input_grad",
+           "galv_expert_weight_grad_workspace_bytes", "galv_expert_weight_grad", "galv_expert_bias_grad")
 
 
 class galv_shape(C.Structure):
@@ -121,6 +125,20 @@ def load_library() -> C.CDLL:
     lib.galv_mx_matmul.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, i32, vp, sz, vp]
     lib.galv_mx_status.argtypes = [vp, vp]
     lib.galv_mx_timeouts.argtypes, lib.galv_mx_timeouts.restype = [vp], C.POINTER(C.c_uint32)
+    lib.galv_i8_codes_bytes.argtypes, lib.galv_i8_codes_bytes.restype = [i64, i64], sz
+    lib.galv_i8_pack.argtypes = [vp, i64, i64, vp, i64, i32, vp, vp, vp]
+    lib.galv_i8_unpack.argtypes = [vp, i64, i64, vp, vp, vp, i64, i32, vp]
+    lib.galv_i8_matmul.argtypes = [vp, i64, i32, i64, i64] + [vp] * 7 + [i64, i32, vp]
+    lib.galv_i8_linear_workspace_bytes.argtypes, lib.galv_i8_linear_workspace_bytes.restype = [i64, i64], sz
+    lib.galv_i8_linear.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, vp, vp, vp, i64, i32, vp, sz, vp]
+    for f in (lib.galv_expert_matmul_workspace_bytes, lib.galv_expert_input_grad_workspace_bytes):
+        f.argtypes, f.restype = [vp, i64, i32, i64, i64, vp, i64, vp], sz
+    lib.galv_expert_matmul.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, vp, vp, i64, i32, vp, sz, vp]
+    lib.galv_expert_input_grad.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, vp, i64, i32, vp, sz, vp]
+    lib.galv_expert_weight_grad_workspace_bytes.argtypes = [vp, i64, i32, i64, i64, vp, i64, vp, i64]
+    lib.galv_expert_weight_grad_workspace_bytes.restype = sz
+    lib.galv_expert_weight_grad.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, i64, i32, vp, vp, i32, vp, sz, vp]
+    lib.galv_expert_bias_grad.argtypes = [vp, i64, i32, i64, vp, vp, i64, i32, vp, i32, vp]
     _lib = lib
     return lib
 
@@ -367,3 +385,66 @@ class Galv:
     def galv_mx_timeouts(self) -> int:
         """Waits that have run out on the device so far; waits for nothing."""
         return self.lib.galv_mx_timeouts(self.h)[0]
+
+    # Rows of 8-bit integers (codes int8 [rows][pitch], scales fp32 [rows], tensors or addresses) and experts' products (ends: int32 tensor, or None for one
+    # expert that has all rows; weights [experts][n][k] contiguous).
+
+    def galv_i8_pack(self, x, codes, scales):
+        rc = self.lib.galv_i8_pack(self.h, *x.shape, *_matrix(x), _DTYPES[x.dtype], _address(codes), _address(scales), _raw_stream(self.device))
+        if rc:
+            self._check(rc)
+
+    def galv_i8_unpack(self, codes, scales, x):
+        rc = self.lib.galv_i8_unpack(self.h, *x.shape, _address(codes), _address(scales), *_matrix(x), _DTYPES[x.dtype], _raw_stream(self.device))
+        if rc:
+            self._check(rc)
+
+    def galv_i8_matmul(self, experts, k, ends, x_codes, x_scales, w_codes, w_scales, bias, y):
+        rows, n = y.shape
+        rc = self.lib.galv_i8_matmul(self.h, rows, experts, n, k, _at(ends), _address(x_codes), _address(x_scales), _address(w_codes), _address(w_scales), _at(bias),
+                                     *_matrix(y), _DTYPES[y.dtype], _raw_stream(self.device))
+        if rc:
+            self._check(rc)
+
+    def galv_i8_linear_workspace_bytes(self, rows, k) -> int:
+        return self.lib.galv_i8_linear_workspace_bytes(rows, k)
+
+    def galv_i8_linear(self, experts, ends, x, w_codes, w_scales, bias, y, workspace):
+        rows, n = y.shape
+        rc = self.lib.galv_i8_linear(self.h, rows, experts, n, x.shape[1], _at(ends), *_matrix(x), _address(w_codes), _address(w_scales), _at(bias), *_matrix(y),
+                                     _DTYPES[y.dtype], *_ws(workspace), _raw_stream(self.device))
+        if rc:
+            self._check(rc)
+
+    def galv_expert_matmul_workspace_bytes(self, x, w) -> int:
+        return self.lib.galv_expert_matmul_workspace_bytes(self.h, x.shape[0], *w.shape, *_matrix(x), w.data_ptr())
+
+    def galv_expert_matmul(self, ends, x, w, bias, y, workspace):
+        rc = self.lib.galv_expert_matmul(self.h, x.shape[0], *w.shape, _at(ends), *_matrix(x), w.data_ptr(), _at(bias), *_matrix(y), _DTYPES[y.dtype],
+                                         *_ws(workspace), _raw_stream(self.device))
+        if rc:
+            self._check(rc)
+
+    def galv_expert_input_grad_workspace_bytes(self, dy, w) -> int:
+        return self.lib.galv_expert_input_grad_workspace_bytes(self.h, dy.shape[0], *w.shape, *_matrix(dy), w.data_ptr())
+
+    def galv_expert_input_grad(self, ends, dy, w, dx, workspace):
+        rc = self.lib.galv_expert_input_grad(self.h, dy.shape[0], *w.shape, _at(ends), *_matrix(dy), w.data_ptr(), *_matrix(dx), _DTYPES[dx.dtype],
+                                             *_ws(workspace), _raw_stream(self.device))
+        if rc:
+            self._check(rc)
+
+    def galv_expert_weight_grad_workspace_bytes(self, experts, dy, x) -> int:
+        return self.lib.galv_expert_weight_grad_workspace_bytes(self.h, dy.shape[0], experts, dy.shape[1], x.shape[1], *_matrix(dy), *_matrix(x))
+
+    def galv_expert_weight_grad(self, ends, dy, x, base, dw, workspace):
+        rc = self.lib.galv_expert_weight_grad(self.h, dy.shape[0], *dw.shape, _at(ends), *_matrix(dy), *_matrix(x), _DTYPES[dy.dtype], _at(base), dw.data_ptr(),
+                                              _DTYPES[dw.dtype], *_ws(workspace), _raw_stream(self.device))
+        if rc:
+            self._check(rc)
+
+    def galv_expert_bias_grad(self, ends, dy, db):
+        rc = self.lib.galv_expert_bias_grad(self.h, dy.shape[0], *db.shape, _at(ends), *_matrix(dy), _DTYPES[dy.dtype], db.data_ptr(), _DTYPES[db.dtype],
+                                            _raw_stream(self.device))
+        if rc:
+            self._check(rc)

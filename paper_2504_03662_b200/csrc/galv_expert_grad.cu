@@ -1,0 +1,429 @@
+// Gradients of experts' weights and biases: dw[e][j][c] = base[e][j][c] + sum of dy[r][j] x[r][c], db[e][j] = sum of dy[r][j], over the rows r of expert e.
+//
+// As in the weight gradient of one layer a pair of CTAs owns a tile of 256 x 256 of dw and both operands lie with tokens along their rows, read as they are
+// stored.  An expert's rows end anywhere: its last chunk of 64 holds rows of the next expert (or of none, which may be anything).  Of those the matrix
+// instructions take no steps of 16 rows that are not needed, and what is left of the last step is set to zero in shared memory, in both operands, since
+// zero times what lies there could be NaN.
+// Per CTA: a thread that starts bulk tensor copies, a warp that issues the matrix instructions for the pair (in the second CTA: tells the first that its rows
+// are there) after it has set such rows to zero, eight warps that take sums from the tensor memory while the next are made and move results out.
+
+#include "galv_experts.cuh"
+#include "galv_tc.cuh"
+#include "galv_tile_out.cuh"
+
+namespace {
+
+constexpr int kStages = 6, kTokens = 64, kTile = 256, kHalf = kTile / 2;
+constexpr int kBox = kTokens * 128;                       // 64 rows of 64 columns
+constexpr int kOperand = 2 * kBox, kStageBytes = 2 * kOperand;
+constexpr int kOutBytes = 8 * 2048;
+constexpr int kThreads = 384;
+// A tensor core's sum is cut at every addition, 8e-7 of the result over 1024 rows (the error grows with the root of the length): after this many chunks the
+// sum goes to fp32 registers, rounded additions.
+constexpr int kSegment = 16;
+constexpr int kGroup = 8;                                 // tiles along n whose columns of dy stay in L2 while their k runs
+
+struct GradArgs {
+    long long rows, n, k;
+    int experts, tiles_n, tiles_k;
+    uint32_t what;
+    const int32_t* ends;
+    const void* base;
+    void* dw;
+    int vec;                                              // four results of a row can be moved at once
+    unsigned* timeouts;
+};
+
+struct Unit { int expert, tn, tk, row0, count; };
+__device__ __forceinline__ Unit unit_of(const GradArgs& a, const int* begin, int u)
+{
+    Unit w;
+    const int each = a.tiles_n * a.tiles_k, tile = u % each, per = kGroup * a.tiles_k, first = tile / per * kGroup, size = min(kGroup, a.tiles_n - first);
+    w.expert = u / each;
+    w.tn = first + tile % per % size;
+    w.tk = tile % per / size;
+    w.row0 = begin[w.expert];
+    w.count = begin[w.expert + 1] - w.row0;
+    return w;
+}
+
+// Zeros in the rows of an operand's last step that are not the expert's: `count` rows of the chunk are.
+__device__ __forceinline__ void clear_rows(uint32_t at, int count)
+{
+    const int rows = (-count) & 15, lane = threadIdx.x % 32;      // up to the next step
+    for (int i = lane; i < rows * 32; i += 32) {          // four boxes, 8 pieces of 16 bytes a row
+        const int box = i / (rows * 8), piece = i % (rows * 8);
+        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" :: "r"(at + box * kBox + count * 128 + piece * 16), "r"(0) : "memory");
+    }
+}
+
+// Where an expert has no rows: base, or zeros.
+template <typename O>
+__device__ __forceinline__ void fill(const O* base, O* out, long long k, int rows, int cols)
+{
+    for (int r = 0; r < rows; ++r)
+        for (int c = threadIdx.x % 32; c < cols; c += 32) out[r * k + c] = base ? base[r * k + c] : mx_zero<O>();
+}
+
+template <typename O>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ GradArgs a)
+{
+    extern __shared__ unsigned char raw[];
+    const uint32_t base = (tc::smem_at(raw) + 1023) & ~1023u;
+    const uint32_t out_at = base + kStages * kStageBytes, bars = out_at + kOutBytes;
+    const uint32_t full = bars, other = full + 8 * kStages, empty = other + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16, drain = acc_empty + 16,
+                   slot = drain + 8;
+    int* const begin = reinterpret_cast<int*>(raw + (bars + 256 - tc::smem_at(raw)));
+    __shared__ int failed;
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = tc::cluster_rank();
+    const int units = a.experts * a.tiles_n * a.tiles_k, first = blockIdx.x / 2, stride = gridDim.x / 2;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            tc::bar_init(full + 8 * s, 1);
+            tc::bar_init(other + 8 * s, 1);
+            tc::bar_init(empty + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            tc::bar_init(acc_full + 8 * b, 1);
+            tc::bar_init(acc_empty + 8 * b, 16);
+        }
+        tc::bar_init(drain, 1);
+        tc::bar_init_done();
+        failed = 0;
+        if (a.rows > 0) {                                 // else there are none
+            tc::prefetch_map(&dy_map);
+            tc::prefetch_map(&x_map);
+        }
+    }
+    if (warp == 2) tc::tmem_alloc<2>(slot, 512);
+    if (warp == 3) experts_scan(a.ends, a.experts, a.rows, begin, begin + a.experts + 1);
+    tc::fence_before();
+    __syncthreads();
+    tc::cluster_sync();                                   // the pair's barriers exist
+    tc::fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+
+    auto waited = [&](uint32_t bar, uint32_t parity) {
+        if (tc::bar_wait(bar, parity)) return true;
+        *(volatile int*)&failed = 1;
+        return false;
+    };
+
+    if (warp == 0) {
+        if (tc::elect()) {
+            int it = 0;
+            bool ok = true;
+            for (int u = first; u < units && ok; u += stride) {
+                const Unit w = unit_of(a, begin, u);
+                const int n0 = w.tn * kTile + rank * kHalf, k0 = w.tk * kTile + rank * kHalf;
+                for (int r = 0; r < w.count; r += kTokens, ++it) {
+                    const int s = it % kStages;
+                    const uint32_t bar = full + 8 * s, at = base + s * kStageBytes;
+                    if (!(ok = waited(empty + 8 * s, (it / kStages & 1) ^ 1))) break;
+                    tc::bar_expect(bar, kStageBytes);
+                    tc::load_2d(at, &dy_map, n0, w.row0 + r, bar);
+                    tc::load_2d(at + kBox, &dy_map, n0 + 64, w.row0 + r, bar);
+                    tc::load_2d(at + kOperand, &x_map, k0, w.row0 + r, bar);
+                    tc::load_2d(at + kOperand + kBox, &x_map, k0 + 64, w.row0 + r, bar);
+                }
+            }
+            if (*(volatile int*)&failed)                  // copies still in flight
+                for (int i = it < kStages ? 0 : it - kStages; i < it; ++i) tc::bar_wait(full + 8 * (i % kStages), i / kStages & 1);
+        }
+    } else if (warp == 1 && rank == 1) {                  // tells the first CTA that this one's rows are there
+        int it = 0;
+        bool ok = true;
+        for (int u = first; u < units && ok; u += stride) {
+            const Unit w = unit_of(a, begin, u);
+            for (int r = 0; r < w.count; r += kTokens, ++it) {
+                const int s = it % kStages;
+                if (!(ok = __all_sync(0xffffffffu, waited(full + 8 * s, it / kStages & 1)))) break;
+                if (w.count - r < kTokens) {
+                    clear_rows(base + s * kStageBytes, w.count - r);
+                    tc::fence_async();
+                }
+                __syncwarp();
+                if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(other + 8 * s, 0));
+            }
+        }
+    } else if (warp == 1) {
+        int it = 0, done = 0;
+        bool ok = true;
+        for (int u = first; u < units && ok; u += stride) {
+            const Unit w = unit_of(a, begin, u);
+            for (int r = 0; r < w.count && ok; ++done) {
+                const uint32_t buf = done & 1, d = tmem + buf * kTile;
+                const int end = r + min(kSegment * kTokens, w.count - r);
+                if (!(ok = __all_sync(0xffffffffu, waited(acc_empty + 8 * buf, (done / 2 & 1) ^ 1)))) break;
+                tc::fence_after();
+                for (bool add = false; r < end; r += kTokens, ++it, add = true) {
+                    const int s = it % kStages;
+                    const uint32_t at = base + s * kStageBytes;
+                    if (!(ok = __all_sync(0xffffffffu, waited(full + 8 * s, it / kStages & 1) && waited(other + 8 * s, it / kStages & 1)))) break;
+                    tc::fence_after();
+                    if (w.count - r < kTokens) {
+                        clear_rows(at, w.count - r);
+                        tc::fence_async();
+                        __syncwarp();
+                    }
+                    if (lane == 0) {
+                        const int steps = min(kTokens / 16, (w.count - r + 15) / 16);
+#pragma unroll
+                        for (int j = 0; j < kTokens / 16; ++j)
+                            if (j < steps) tc::mma_f16(d, tc::operand(at + j * 2048, kBox, 1024), tc::operand(at + kOperand + j * 2048, kBox, 1024), a.what, add || j > 0);
+                        tc::mma_commit<2>(empty + 8 * s);
+                    }
+                    __syncwarp();
+                }
+                if (ok && lane == 0) tc::mma_commit<2>(acc_full + 8 * buf);
+            }
+        }
+        if (lane == 0 && *(volatile int*)&failed) {
+            tc::mma_commit<2>(drain);
+            tc::bar_wait(drain, 0);
+        }
+    } else if (warp >= 4) {
+        const int quad = warp % 4, half = (warp - 4) / 4;  // 32 rows, 128 columns
+        const uint32_t mine = out_at + (warp - 4) * 2048, from = tmem + half * 128 + ((uint32_t)quad * 32 << 16);
+        int done = 0;
+        bool ok = true;
+        for (int u = first; u < units && ok; u += stride) {
+            const Unit w = unit_of(a, begin, u);
+            const long long r0 = (long long)w.tn * kTile + rank * kHalf + quad * 32, c0 = (long long)w.tk * kTile + half * 128;
+            const int rows = (int)max(-64ll, min(32ll, a.n - r0)), cols = (int)max(-128ll, min(128ll, a.k - c0));
+            const long long at0 = w.expert * a.n * a.k + r0 * a.k + c0;
+            if (w.count == 0) {
+                fill<O>(a.base ? (const O*)a.base + at0 : nullptr, (O*)a.dw + at0, a.k, rows, cols);
+                continue;
+            }
+            uint32_t buf = done & 1;
+            if (w.count > kSegment * kTokens) {           // earlier segments are taken up here, the last one is added where it lies
+                float sum[128];
+#pragma unroll
+                for (int i = 0; i < 128; ++i) sum[i] = 0.f;
+                for (int left = w.count; left > 0; left -= kSegment * kTokens) {
+                    buf = done & 1;
+                    if (!(ok = waited(acc_full + 8 * buf, done / 2 & 1))) break;
+                    tc::fence_after();
+#pragma unroll
+                    for (int j = 0; j < 128; j += 16) {
+                        uint32_t v[16];
+                        tc::tmem_load16(from + buf * kTile + j, v);
+                        tc::tmem_wait_load();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum[j + i] += __uint_as_float(v[i]);
+                    }
+                    if (left > kSegment * kTokens) {      // this accumulator may be summed into again
+                        tc::fence_before();
+                        __syncwarp();
+                        if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_empty + 8 * buf, 0));
+                        ++done;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 128; j += 16) tc::tmem_store16(from + buf * kTile + j, sum + j);
+                tc::tmem_wait_store();
+            } else if ((ok = waited(acc_full + 8 * buf, done / 2 & 1))) {
+                tc::fence_after();
+            }
+            if (!ok) break;
+            const long long at = at0 + (a.vec ? lane / 4 : lane / 16) * a.k + (a.vec ? lane % 4 * 4 : lane % 16);
+            tile_out::move_out<O>(from + buf * kTile, mine, a.base ? (const O*)a.base + at : nullptr, (O*)a.dw + at, a.k, rows, cols, a.vec);
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_empty + 8 * buf, 0));
+            ++done;
+        }
+    }
+    __syncwarp();
+    tc::fence_before();
+    __syncthreads();
+    tc::cluster_sync();                                   // neither CTA's memory is read by the other any more
+    if (threadIdx.x == 0 && failed) atomicAdd_system(a.timeouts, 1u);
+    if (warp == 2) tc::tmem_free<2>(tmem, 512);
+}
+
+// ---- bias
+//
+// A cluster of 8 CTAs has 128 columns of one expert, a warp every 64th of its rows, a lane 4 columns; the warps' sums are added in their order, then the
+// CTAs'.  Bound by reading dy once.
+
+constexpr int kBiasColumns = 128, kBiasCtas = 8;
+
+template <typename T> __device__ __forceinline__ void add_row(const T* row, int cols, bool vec, float (&sum)[4])
+{
+    if (vec) {
+        if (cols > 0) {
+            const uint2 q = __ldg(reinterpret_cast<const uint2*>(row));
+            const T* e = reinterpret_cast<const T*>(&q);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] += mx_float(e[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < cols) sum[i] += mx_float(row[i]);
+    }
+}
+
+template <typename T, typename O>
+__global__ void __cluster_dims__(kBiasCtas, 1, 1) __launch_bounds__(256)
+expert_bias_grad_kernel(long long rows, int experts, long long n, const int32_t* __restrict__ ends, const T* __restrict__ dy, long long stride, int vec, O* __restrict__ db)
+{
+    extern __shared__ int begin[];
+    __shared__ float part[8][kBiasColumns], sums[kBiasCtas][kBiasColumns];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = tc::cluster_rank();
+    if (warp == 0) experts_scan(ends, experts, rows, begin, begin + experts + 1);
+    tc::cluster_sync();                                   // the first CTA runs, sums can be sent to it
+    const long long blocks = (n + kBiasColumns - 1) / kBiasColumns, all = blocks * experts;
+    for (long long b = blockIdx.x / kBiasCtas; b < all; b += gridDim.x / kBiasCtas) {
+        const int e = (int)(b / blocks);
+        const long long c0 = (b - e * blocks) * kBiasColumns + lane * 4;
+        const int cols = (int)max(0ll, min(4ll, n - c0));
+        const long long end = begin[e + 1];
+        float sum[4] = {};
+#pragma unroll 4
+        for (long long r = begin[e] + (long long)rank * 8 + warp; r < end; r += kBiasCtas * 8) add_row(dy + r * stride + c0, cols, vec, sum);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[warp][lane * 4 + i] = sum[i];
+        __syncthreads();
+        if (threadIdx.x < kBiasColumns) {
+            float v = part[0][threadIdx.x];
+#pragma unroll
+            for (int w = 1; w < 8; ++w) v += part[w][threadIdx.x];
+            asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(tc::in_cta(tc::smem_at(&sums[rank][threadIdx.x]), 0)), "f"(v) : "memory");
+        }
+        tc::cluster_sync();
+        const long long c = (b - e * blocks) * kBiasColumns + threadIdx.x;
+        if (rank == 0 && threadIdx.x < kBiasColumns && c < n) {
+            float v = sums[0][threadIdx.x];
+#pragma unroll
+            for (int r = 1; r < kBiasCtas; ++r) v += sums[r][threadIdx.x];
+            db[e * n + c] = mx_round<O>(v);
+        }
+        tc::cluster_sync();                               // the sums have been read
+    }
+}
+
+size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
+int smem_of(int experts) { return 1024 + kStages * kStageBytes + kOutBytes + 256 + 8 * (experts + 1); }
+
+struct GradPlan { size_t dy, x, total; };
+GradPlan plan_of(int64_t rows, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride)
+{
+    auto moved = [&](const void* p, int64_t stride, int64_t cols) {
+        return mx_rows16(p, stride, GALV_BF16) && stride * 2 < ((int64_t)1 << 40) ? 0 : up((size_t)rows * ((cols + 7) / 8 * 8) * 2);
+    };
+    GradPlan p;
+    p.dy = moved(dy, dy_stride, n);
+    p.x = moved(x, x_stride, k);
+    p.total = p.dy + p.x;
+    return p;
+}
+
+template <typename O>
+cudaError_t launch(const galv_ctx* ctx, const CUtensorMap& dm, const CUtensorMap& xm, const GradArgs& a, cudaStream_t st)
+{
+    const cudaError_t e = cudaFuncSetAttribute(expert_grad_kernel<O>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kExpertsMost));
+    if (e != cudaSuccess) return e;
+    const long long units = (long long)a.experts * a.tiles_n * a.tiles_k;
+    const int pairs = (int)(units < ctx->num_sms / 2 ? units : ctx->num_sms / 2);
+    expert_grad_kernel<O><<<pairs * 2, kThreads, smem_of(a.experts), st>>>(dm, xm, a);
+    return cudaGetLastError();
+}
+
+bool sizes_ok(int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, int32_t dtype, int32_t out_dtype)
+{
+    return mx_size_ok(rows, n) && mx_size_ok(rows, k) && experts >= 1 && experts <= kExpertsMost && (ends || experts == 1) && (dtype == GALV_BF16 || dtype == GALV_F16) &&
+           (out_dtype == dtype || out_dtype == GALV_F32) && ((n + kTile - 1) / kTile) * ((k + kTile - 1) / kTile) * experts < (int64_t)1 << 31;
+}
+
+}  // namespace
+
+extern "C" size_t galv_expert_weight_grad_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* x,
+                                                          int64_t x_stride)
+{
+    if (!ctx || !mx_size_ok(rows, n) || !mx_size_ok(rows, k) || rows == 0 || experts < 1) return 0;
+    return plan_of(rows, n, k, dy, dy_stride, x, x_stride).total;
+}
+
+extern "C" int galv_expert_weight_grad(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* dy, int64_t dy_stride, const void* x,
+                                       int64_t x_stride, int32_t dtype, const void* base, void* dw, int32_t dw_dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx) return GALV_ERR_INVALID_ARG;
+    if (!sizes_ok(rows, experts, n, k, ends, dtype, dw_dtype))
+        return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_expert_weight_grad: sizes, number of experts or types outside the limits");
+    if (!mx_matrix_ok(dw, k, k, dw_dtype) || (base && !mx_aligned(base, mx_size_of(dw_dtype))) || (ends && !mx_aligned(ends, 4)))
+        return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_expert_weight_grad: NULL or misaligned dw, base or ends");
+    if (rows > 0 && (!mx_matrix_ok(dy, dy_stride, n, dtype) || !mx_matrix_ok(x, x_stride, k, dtype)))
+        return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_expert_weight_grad: NULL or misaligned pointer, or a row stride below the row's length");
+    const size_t need = galv_expert_weight_grad_workspace_bytes(ctx, rows, experts, n, k, dy, dy_stride, x, x_stride);
+    if (need && (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < need))
+        return galv_set_error(ctx, GALV_ERR_WORKSPACE, "galv_expert_weight_grad: workspace NULL, misaligned or too small");
+    const int may = mx_may_run(ctx, "galv_expert_weight_grad: the library's host memory could not be registered", "galv_expert_weight_grad: a bounded wait of an earlier product ran out");
+    if (may != GALV_OK) return may;
+    MxDevice dev(ctx);
+    if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
+    cudaStream_t st = (cudaStream_t)stream;
+    GradArgs a;
+    a.rows = rows; a.n = n; a.k = k; a.experts = experts;
+    a.tiles_n = (int)((n + kTile - 1) / kTile); a.tiles_k = (int)((k + kTile - 1) / kTile);
+    const uint32_t t = dtype == GALV_BF16 ? 1u : 0u;      // fp32 sums, both operands of this type with the summed index across their rows, 256 x 256
+    a.what = 1u << 4 | t << 7 | t << 10 | 1u << 15 | 1u << 16 | (uint32_t)(kTile >> 3) << 17 | (uint32_t)(kTile >> 4) << 24;
+    a.ends = ends; a.base = base; a.dw = dw; a.timeouts = ctx->mx_timeouts_at;
+    const int four = 4 * mx_size_of(dw_dtype);
+    a.vec = k % 4 == 0 && mx_aligned(dw, four) && mx_aligned(base, four);
+    CUtensorMap dm = {}, xm = {};
+    if (rows > 0) {
+        const GradPlan p = plan_of(rows, n, k, dy, dy_stride, x, x_stride);
+        if (p.dy) {
+            galv_align_rows(ctx, rows, n, dy, dy_stride, workspace, (n + 7) / 8 * 8, st);
+            dy = workspace;
+            dy_stride = (n + 7) / 8 * 8;
+        }
+        if (p.x) {
+            void* const to = (char*)workspace + p.dy;
+            galv_align_rows(ctx, rows, k, x, x_stride, to, (k + 7) / 8 * 8, st);
+            x = to;
+            x_stride = (k + 7) / 8 * 8;
+        }
+        const CUtensorMapDataType type = dtype == GALV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+        cudaError_t e = galv_mx_map(&dm, type, dy, rows, n, dy_stride * 2, kTokens, 64, true);
+        if (e == cudaSuccess) e = galv_mx_map(&xm, type, x, rows, k, x_stride * 2, kTokens, 64, true);
+        if (e != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, "galv_expert_weight_grad: tensor map");
+    }
+    // without rows no copy is made: the maps are not read
+    cudaError_t e;
+    if (dw_dtype == GALV_F32) e = launch<float>(ctx, dm, xm, a, st);
+    else if (dw_dtype == GALV_BF16) e = launch<__nv_bfloat16>(ctx, dm, xm, a, st);
+    else e = launch<__half>(ctx, dm, xm, a, st);
+    return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
+}
+
+extern "C" int galv_expert_bias_grad(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, const int32_t* ends, const void* dy, int64_t dy_stride, int32_t dtype, void* db, int32_t db_dtype,
+                                     void* stream)
+{
+    if (!ctx) return GALV_ERR_INVALID_ARG;
+    if (!sizes_ok(rows, experts, n, 1, ends, dtype, db_dtype)) return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_expert_bias_grad: sizes, number of experts or types outside the limits");
+    if (!db || !mx_aligned(db, mx_size_of(db_dtype)) || (ends && !mx_aligned(ends, 4)) || (rows > 0 && !mx_matrix_ok(dy, dy_stride, n, dtype)))
+        return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_expert_bias_grad: NULL or misaligned pointer, or a row stride below n");
+    MxDevice dev(ctx);
+    if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
+    const int64_t clusters = (n + kBiasColumns - 1) / kBiasColumns * experts, most = ctx->num_sms;
+    const int grid = (int)(clusters < most ? clusters : most) * kBiasCtas, smem = 8 * (experts + 1);
+    const int vec = n % 4 == 0 && dy_stride % 4 == 0 && mx_aligned(dy, 8);
+    cudaStream_t st = (cudaStream_t)stream;
+    using B = __nv_bfloat16;
+    if (dtype == GALV_BF16 && db_dtype == GALV_F32) expert_bias_grad_kernel<B, float><<<grid, 256, smem, st>>>(rows, experts, n, ends, (const B*)dy, dy_stride, vec, (float*)db);
+    else if (dtype == GALV_BF16) expert_bias_grad_kernel<B, B><<<grid, 256, smem, st>>>(rows, experts, n, ends, (const B*)dy, dy_stride, vec, (B*)db);
+    else if (db_dtype == GALV_F32) expert_bias_grad_kernel<__half, float><<<grid, 256, smem, st>>>(rows, experts, n, ends, (const __half*)dy, dy_stride, vec, (float*)db);
+    else expert_bias_grad_kernel<__half, __half><<<grid, 256, smem, st>>>(rows, experts, n, ends, (const __half*)dy, dy_stride, vec, (__half*)db);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
+}

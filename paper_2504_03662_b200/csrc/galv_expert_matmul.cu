@@ -1,0 +1,433 @@
+// Products of tokens and weights, each token by its expert's: y[r][j] = sum_c x[r][c] w[e][j][c] + bias[e][j] for the rows r of expert e, in 16 bits or in 8-bit
+// integers, and the gradient of x; one expert that has all rows is a plain product.
+//
+// Rows are sorted by expert, where they end is known on the device alone.  So each CTA finds the tiles there are (a scan over the experts), and a grid that
+// fills the card walks through them.  The weights' rows take the tensor cores' 256 rows of a pair of CTAs, the tokens their columns, as many as an expert's last
+// tile has (a multiple of 32): what ragged sizes waste is less than 32 tokens an expert, and a few tokens cost little more than reading the weights.
+// A column of sums depends on its own token alone: a tile's copy of tokens may run into the next expert's, whose sums nobody takes, whatever they are.
+// Per CTA: a thread that starts bulk tensor copies (128 bytes of the summed index a chunk: 128 rows of weights, half of the tile's tokens), one that issues
+// the matrix instructions for the pair, eight warps that move sums from the tensor memory to y while the next are made (two accumulators fill it).
+
+#include <stdio.h>
+
+#include "galv_experts.cuh"
+#include "galv_i8.cuh"
+#include "galv_tc.cuh"
+
+namespace {
+
+enum Kind { kForward, kInputGrad, kWhole };               // 16 bits, summed along the weights' rows; across them; 8-bit integers
+
+constexpr int kStages = 6, kTile = 256, kHalf = kTile / 2, kChunkBytes = 128;
+constexpr int kRowsBytes = kHalf * kChunkBytes, kStageBytes = 2 * kRowsBytes;
+constexpr int kOutBytes = 8 * 2048;
+constexpr int kPart = 16;                                 // tokens of a copy where the tile is not full
+constexpr int kThreads = 384;
+constexpr int kGroup = 16;                                // tiles of tokens that stay in L2 while their tiles of weights run
+
+struct ProductArgs {
+    long long rows, n, stride;                            // tokens, columns of y, from one row of y to the next
+    int experts, tiles_m, chunks, last_steps;             // last_steps: of 32 bytes in the last chunk
+    uint32_t what;                                        // the matrix instruction without its number of tokens
+    const int32_t* ends;
+    const float* x_scales;
+    const float* w_scales;
+    const void* bias;
+    void* y;
+    int vec;                                              // 16 bytes of a row of y can be moved at once
+    unsigned* timeouts;                                   // host memory: CTAs that have given up a wait
+};
+
+// A walk through the tiles: units of 256 weights' rows by up to 256 tokens, those of an expert next to one another.
+struct Walk {
+    const int* begin;
+    const int* before;
+    int tiles_m, expert = 0;
+    int tm, row0, count;                                  // tile of weights' rows; first token and number of tokens
+    __device__ __forceinline__ Walk(const int* begin_, const int* before_, int tiles_m_) : begin(begin_), before(before_), tiles_m(tiles_m_) {}
+    __device__ __forceinline__ void to(int u)             // units in rising order
+    {
+        while (u >= before[expert + 1] * tiles_m) ++expert;
+        const int from = before[expert], all = before[expert + 1] - from, local = u - from * tiles_m;
+        const int per = kGroup * tiles_m, first = local / per * kGroup, size = min(kGroup, all - first), in = local % per;
+        row0 = begin[expert] + (first + in % size) * kTile;
+        tm = in / size;
+        count = min(kTile, begin[expert + 1] - row0);
+    }
+    __device__ __forceinline__ int columns() const { return (count + 31) & ~31; }
+};
+
+// 16 tokens' sums of a warp's 32 channels, a channel a lane, as numbers.
+template <int K>
+__device__ __forceinline__ float number(uint32_t sum, float x_scale, float w_scale, float bias)
+{
+    if (K == kWhole) return fmaf((float)(int)sum, x_scale * w_scale, bias);
+    return __uint_as_float(sum) + bias;
+}
+
+template <int K, typename O>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap part_map,
+                      const __grid_constant__ ProductArgs a)
+{
+    extern __shared__ unsigned char raw[];
+    const uint32_t base = (tc::smem_at(raw) + 1023) & ~1023u;
+    const uint32_t w_at = base, x_at = w_at + kStages * kRowsBytes, out_at = x_at + kStages * kRowsBytes, bars = out_at + kOutBytes;
+    const uint32_t full = bars, other = full + 8 * kStages, empty = other + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16, drain = acc_empty + 16,
+                   slot = drain + 8;
+    int* const begin = reinterpret_cast<int*>(raw + (bars + 256 - tc::smem_at(raw)));
+    int* const before = begin + a.experts + 1;
+    __shared__ int failed;
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = tc::cluster_rank();
+    const int first = blockIdx.x / 2, stride = gridDim.x / 2;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            tc::bar_init(full + 8 * s, 1);
+            tc::bar_init(other + 8 * s, 1);
+            tc::bar_init(empty + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            tc::bar_init(acc_full + 8 * b, 1);
+            tc::bar_init(acc_empty + 8 * b, 16);
+        }
+        tc::bar_init(drain, 1);
+        tc::bar_init_done();
+        failed = 0;
+        tc::prefetch_map(&w_map);
+        tc::prefetch_map(&x_map);
+        tc::prefetch_map(&part_map);
+    }
+    if (warp == 2) tc::tmem_alloc<2>(slot, 512);
+    if (warp == 3) experts_scan(a.ends, a.experts, a.rows, begin, before);
+    tc::fence_before();
+    __syncthreads();
+    tc::cluster_sync();                                   // the pair's barriers exist
+    tc::fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+    const int units = before[a.experts] * a.tiles_m;
+
+    auto waited = [&](uint32_t bar, uint32_t parity) {
+        if (tc::bar_wait(bar, parity)) return true;
+        *(volatile int*)&failed = 1;
+        return false;
+    };
+    Walk w(begin, before, a.tiles_m);
+
+    if (warp == 0) {
+        if (tc::elect()) {
+            constexpr int elements = K == kWhole ? kChunkBytes : kChunkBytes / 2;
+            int it = 0;
+            bool ok = true;
+            for (int u = first; u < units && ok; u += stride) {
+                w.to(u);
+                const int m0 = w.tm * kTile + rank * kHalf, half = w.columns() / 2, r0 = w.row0 + rank * half;
+                for (int c = 0; c < a.chunks; ++c, ++it) {
+                    const int s = it % kStages;
+                    const uint32_t bar = full + 8 * s;
+                    if (!(ok = waited(empty + 8 * s, (it / kStages & 1) ^ 1))) break;
+                    tc::bar_expect(bar, kRowsBytes + half * kChunkBytes);
+                    if (K == kInputGrad) {                // 64 rows of weights, 64 columns a copy
+                        tc::load_3d(w_at + s * kRowsBytes, &w_map, m0, c * elements, w.expert, bar);
+                        tc::load_3d(w_at + s * kRowsBytes + kRowsBytes / 2, &w_map, m0 + 64, c * elements, w.expert, bar);
+                    } else {
+                        tc::load_3d(w_at + s * kRowsBytes, &w_map, c * elements, m0, w.expert, bar);
+                    }
+                    if (half == kHalf) tc::load_2d(x_at + s * kRowsBytes, &x_map, c * elements, r0, bar);
+                    else
+                        for (int i = 0; i < half; i += kPart) tc::load_2d(x_at + s * kRowsBytes + i * kChunkBytes, &part_map, c * elements, r0 + i, bar);
+                }
+            }
+            if (*(volatile int*)&failed)                  // copies still in flight
+                for (int i = it < kStages ? 0 : it - kStages; i < it; ++i) tc::bar_wait(full + 8 * (i % kStages), i / kStages & 1);
+        }
+    } else if (warp == 1 && rank == 1) {                  // tells the first CTA that this one's rows are there
+        if (tc::elect()) {
+            int it = 0;
+            bool ok = true;
+            for (int u = first; u < units && ok; u += stride)
+                for (int c = 0; c < a.chunks; ++c, ++it) {
+                    if (!(ok = waited(full + 8 * (it % kStages), it / kStages & 1))) break;
+                    tc::bar_arrive_cluster(tc::in_cta(other + 8 * (it % kStages), 0));
+                }
+        }
+    } else if (warp == 1) {
+        if (tc::elect()) {
+            int it = 0, done = 0;
+            bool ok = true;
+            for (int u = first; u < units && ok; u += stride, ++done) {
+                w.to(u);
+                const uint32_t buf = done & 1, d = tmem + buf * kTile, what = a.what | (uint32_t)(w.columns() >> 3) << 17;
+                if (!(ok = waited(acc_empty + 8 * buf, (done / 2 & 1) ^ 1))) break;
+                tc::fence_after();
+                for (int c = 0; c < a.chunks; ++c, ++it) {
+                    const int s = it % kStages, steps = c + 1 < a.chunks ? 4 : a.last_steps;
+                    if (!(ok = waited(full + 8 * s, it / kStages & 1) && waited(other + 8 * s, it / kStages & 1))) break;
+                    tc::fence_after();
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (j < steps) {
+                            const uint64_t wo = K == kInputGrad ? tc::operand(w_at + s * kRowsBytes + j * 2048, kRowsBytes / 2, 1024) : tc::operand(w_at + s * kRowsBytes + j * 32, 16, 1024);
+                            const uint64_t xo = tc::operand(x_at + s * kRowsBytes + j * 32, 16, 1024);
+                            if (K == kWhole) tc::mma_i8(d, wo, xo, what, c > 0 || j > 0);
+                            else tc::mma_f16(d, wo, xo, what, c > 0 || j > 0);
+                        }
+                    tc::mma_commit<2>(empty + 8 * s);
+                }
+                if (ok) tc::mma_commit<2>(acc_full + 8 * buf);
+            }
+            if (*(volatile int*)&failed) {
+                tc::mma_commit<2>(drain);
+                tc::bar_wait(drain, 0);
+            }
+        }
+    } else if (warp >= 4) {
+        constexpr int pieces = 32 * (int)sizeof(O) / 16;  // 16-byte pieces of a token's 32 channels
+        const int quad = warp % 4, half = (warp - 4) / 4;  // 32 channels, every other 16 tokens
+        const uint32_t mine = out_at + (warp - 4) * 2048, lanes = (uint32_t)quad * 32 << 16;
+        O* const y = (O*)a.y;
+        int done = 0;
+        for (int u = first; u < units; u += stride, ++done) {
+            w.to(u);
+            const uint32_t buf = done & 1;
+            const long long c0 = (long long)w.tm * kTile + rank * kHalf + quad * 32, ch = c0 + lane, at = w.expert * a.n + ch;
+            const float bias = a.bias && ch < a.n ? mx_float(((const O*)a.bias)[at]) : 0.f, w_scale = K == kWhole && ch < a.n ? a.w_scales[at] : 0.f;
+            if (!waited(acc_full + 8 * buf, done / 2 & 1)) break;
+            tc::fence_after();
+            for (int j = half * 16; j < w.count; j += 32) {
+                const int tokens = min(16, w.count - j);
+                const long long r0 = (long long)w.row0 + j;
+                uint32_t s[16];
+                float x_scale = 0.f;
+                if (K == kWhole && lane < tokens) x_scale = a.x_scales[r0 + lane];
+                tc::tmem_load16(tmem + buf * kTile + j + lanes, s);
+                tc::tmem_wait_load();
+                if (a.vec) {
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const O v = mx_round<O>(number<K>(s[i], K == kWhole ? __shfl_sync(0xffffffffu, x_scale, i) : 0.f, w_scale, bias));
+                        const uint32_t to = mine + (i * 32 + lane) * (int)sizeof(O);
+                        if (sizeof(O) == 2) asm volatile("st.shared.b16 [%0], %1;" :: "r"(to), "h"(*reinterpret_cast<const uint16_t*>(&v)) : "memory");
+                        else asm volatile("st.shared.b32 [%0], %1;" :: "r"(to), "r"(*reinterpret_cast<const uint32_t*>(&v)) : "memory");
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 16 * pieces; i += 32) {
+                        const int p = i + lane, token = p / pieces, piece = p % pieces;
+                        uint4 q;
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(mine + p * 16));
+                        const long long col = c0 + piece * (16 / (int)sizeof(O));
+                        if (token < tokens && col < a.n) *reinterpret_cast<uint4*>(y + (r0 + token) * a.stride + col) = q;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float v = number<K>(s[i], K == kWhole ? __shfl_sync(0xffffffffu, x_scale, i) : 0.f, w_scale, bias);
+                        if (i < tokens && ch < a.n) y[(r0 + i) * a.stride + ch] = mx_round<O>(v);
+                    }
+                }
+            }
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_empty + 8 * buf, 0));
+        }
+        // rows of no expert
+        for (long long r = begin[a.experts] + (long long)blockIdx.x * 8 + warp - 4; r < a.rows; r += gridDim.x * 8ll)
+            for (long long c = lane; c < a.n; c += 32) y[r * a.stride + c] = mx_zero<O>();
+    }
+    __syncwarp();
+    tc::fence_before();
+    __syncthreads();
+    tc::cluster_sync();                                   // neither CTA's memory is read by the other any more
+    if (threadIdx.x == 0 && failed) atomicAdd_system(a.timeouts, 1u);
+    if (warp == 2) tc::tmem_free<2>(tmem, 512);
+}
+
+size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
+int smem_of(int experts) { return 1024 + kStages * kStageBytes + kOutBytes + 256 + 8 * (experts + 1); }
+
+// Where the operands of a product in 16 bits that bulk copies cannot take as they are go in the workspace.
+struct AlignPlan { size_t x, w, total; };
+AlignPlan align_plan(int64_t rows, int64_t x_cols, const void* x, int64_t x_stride, int64_t experts, int64_t n, int64_t k, const void* w)
+{
+    AlignPlan p;
+    p.x = mx_rows16(x, x_stride, GALV_BF16) && x_stride * 2 < ((int64_t)1 << 40) ? 0 : up((size_t)rows * ((x_cols + 7) / 8 * 8) * 2);
+    p.w = mx_rows16(w, k, GALV_BF16) ? 0 : up((size_t)experts * n * ((k + 7) / 8 * 8) * 2);
+    p.total = p.x + p.w;
+    return p;
+}
+
+template <int K, typename O>
+cudaError_t launch(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap& xm, const CUtensorMap& pm, const ProductArgs& a, cudaStream_t st)
+{
+    const int smem = smem_of(a.experts);
+    const cudaError_t e = cudaFuncSetAttribute(expert_product_kernel<K, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kExpertsMost));
+    if (e != cudaSuccess) return e;
+    const long long most = (a.rows / kTile + (a.rows < a.experts ? a.rows : a.experts)) * a.tiles_m;      // units, whatever the ends say
+    const int pairs = (int)(most < ctx->num_sms / 2 ? most : ctx->num_sms / 2);
+    expert_product_kernel<K, O><<<pairs * 2, kThreads, smem, st>>>(wm, xm, pm, a);
+    return cudaGetLastError();
+}
+
+bool units_fit(int64_t rows, int64_t experts, int64_t n) { return (rows / kTile + experts) * ((n + kTile - 1) / kTile) < (int64_t)1 << 31; }
+
+// y = x w^T or x w by expert, both in 16 bits.  across: w [experts][cols of x][n], summed across its rows.
+int product16(galv_ctx* ctx, const char* name, bool across, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* x, int64_t x_stride, const void* w,
+              const void* bias, void* y, int64_t y_stride, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int64_t w_rows = across ? k : n, w_cols = across ? n : k;
+    auto wrong = [&](int code, const char* what) {
+        char text[160];
+        snprintf(text, sizeof(text), "%s: %s", name, what);
+        return galv_set_error(ctx, code, text);
+    };
+    if (!mx_size_ok(rows, n) || !mx_size_ok(rows, k) || experts < 1 || experts > kExpertsMost || (!ends && experts != 1) || (dtype != GALV_BF16 && dtype != GALV_F16) ||
+        !units_fit(rows, experts, n))
+        return wrong(GALV_ERR_INVALID_ARG, "sizes, number of experts or type outside the limits");
+    if (rows == 0) return GALV_OK;
+    if (!mx_matrix_ok(x, x_stride, k, dtype) || !mx_matrix_ok(w, w_cols, w_cols, dtype) || !mx_matrix_ok(y, y_stride, n, dtype) || (bias && !mx_aligned(bias, 2)) ||
+        (ends && !mx_aligned(ends, 4)))
+        return wrong(GALV_ERR_INVALID_ARG, "NULL or misaligned pointer, or a row stride below the row's length");
+    const AlignPlan p = align_plan(rows, k, x, x_stride, experts, w_rows, w_cols, w);
+    if (p.total && (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < p.total)) return wrong(GALV_ERR_WORKSPACE, "workspace NULL, misaligned or too small");
+    const int may = mx_may_run(ctx, "experts' product: the library's host memory could not be registered", "experts' product: a bounded wait of an earlier product ran out");
+    if (may != GALV_OK) return may;
+    MxDevice dev(ctx);
+    if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
+    cudaStream_t st = (cudaStream_t)stream;
+    int64_t w_pitch = w_cols;
+    if (p.x) {
+        galv_align_rows(ctx, rows, k, x, x_stride, workspace, (k + 7) / 8 * 8, st);
+        x = workspace;
+        x_stride = (k + 7) / 8 * 8;
+    }
+    if (p.w) {
+        void* const to = (char*)workspace + p.x;
+        w_pitch = (w_cols + 7) / 8 * 8;
+        galv_align_rows(ctx, (int64_t)experts * w_rows, w_cols, w, w_cols, to, w_pitch, st);
+        w = to;
+    }
+    const CUtensorMapDataType type = dtype == GALV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    CUtensorMap wm, xm, pm;
+    cudaError_t e = galv_map_3d(&wm, type, w, experts, w_rows, w_cols, w_pitch * 2, across ? 64 : kHalf, 64);
+    if (e == cudaSuccess) e = galv_mx_map(&xm, type, x, rows, k, x_stride * 2, kHalf, 64, true);
+    if (e == cudaSuccess) e = galv_mx_map(&pm, type, x, rows, k, x_stride * 2, kPart, 64, true);
+    if (e != cudaSuccess) return wrong(GALV_ERR_CUDA, "tensor map");
+    ProductArgs a;
+    a.rows = rows; a.n = n; a.stride = y_stride; a.experts = experts; a.tiles_m = (int)((n + kTile - 1) / kTile);
+    a.chunks = (int)((k + 63) / 64); a.last_steps = (int)((k - (a.chunks - 1) * 64ll + 15) / 16);
+    const uint32_t t = dtype == GALV_BF16 ? 1u : 0u;      // fp32 sums, both operands of this type, the weights' summed index along or across their rows
+    a.what = 1u << 4 | t << 7 | t << 10 | (across ? 1u << 15 : 0u) | (uint32_t)(kTile >> 4) << 24;
+    a.ends = ends; a.x_scales = a.w_scales = nullptr; a.bias = bias; a.y = y; a.timeouts = ctx->mx_timeouts_at;
+    a.vec = n % 8 == 0 && y_stride % 8 == 0 && mx_aligned(y, 16);
+    if (dtype == GALV_BF16) e = across ? launch<kInputGrad, __nv_bfloat16>(ctx, wm, xm, pm, a, st) : launch<kForward, __nv_bfloat16>(ctx, wm, xm, pm, a, st);
+    else e = across ? launch<kInputGrad, __half>(ctx, wm, xm, pm, a, st) : launch<kForward, __half>(ctx, wm, xm, pm, a, st);
+    return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
+}
+
+bool whole_sizes_ok(int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, int32_t dtype)
+{
+    return mx_size_ok(rows, n) && mx_size_ok(rows, k) && k <= GALV_I8_MOST && experts >= 1 && experts <= kExpertsMost && (ends || experts == 1) && mx_dtype_ok(dtype) &&
+           units_fit(rows, experts, n);
+}
+bool whole_pointers_ok(int64_t n, const int32_t* ends, const int8_t* w_codes, const float* w_scales, const void* bias, const void* y, int64_t y_stride, int32_t dtype)
+{
+    return w_codes && w_scales && mx_aligned(w_codes, 16) && mx_aligned(w_scales, 4) && mx_matrix_ok(y, y_stride, n, dtype) && (!bias || mx_aligned(bias, mx_size_of(dtype))) &&
+           (!ends || mx_aligned(ends, 4));
+}
+
+int whole_launch(galv_ctx* ctx, const char* name, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const int8_t* x_codes, const float* x_scales,
+                 const int8_t* w_codes, const float* w_scales, const void* bias, void* y, int64_t y_stride, int32_t dtype, cudaStream_t st)
+{
+    const int64_t pitch = i8_pitch(k);
+    CUtensorMap wm, xm, pm;
+    cudaError_t e = galv_map_3d(&wm, CU_TENSOR_MAP_DATA_TYPE_UINT8, w_codes, experts, n, pitch, pitch, kHalf, kChunkBytes);
+    if (e == cudaSuccess) e = galv_mx_map(&xm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, pitch, pitch, kHalf, kChunkBytes, true);
+    if (e == cudaSuccess) e = galv_mx_map(&pm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, pitch, pitch, kPart, kChunkBytes, true);
+    if (e != cudaSuccess) {
+        char text[100];
+        snprintf(text, sizeof(text), "%s: tensor map", name);
+        return galv_set_error(ctx, GALV_ERR_CUDA, text);
+    }
+    ProductArgs a;
+    a.rows = rows; a.n = n; a.stride = y_stride; a.experts = experts; a.tiles_m = (int)((n + kTile - 1) / kTile);
+    a.chunks = (int)((pitch + kChunkBytes - 1) / kChunkBytes); a.last_steps = (int)((pitch - (a.chunks - 1) * (int64_t)kChunkBytes + 31) / 32);
+    a.what = 2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(kTile >> 4) << 24;      // 32-bit whole sums of signed 8-bit operands
+    a.ends = ends; a.x_scales = x_scales; a.w_scales = w_scales; a.bias = bias; a.y = y; a.timeouts = ctx->mx_timeouts_at;
+    const int per = 16 / mx_size_of(dtype);
+    a.vec = n % per == 0 && y_stride % per == 0 && mx_aligned(y, 16);
+    MX_DISPATCH_TYPE(dtype, e = (launch<kWhole, T>(ctx, wm, xm, pm, a, st)));
+    return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
+}
+
+int whole_may(galv_ctx* ctx) { return mx_may_run(ctx, "8-bit product: the library's host memory could not be registered", "8-bit product: a bounded wait of an earlier product ran out"); }
+
+}  // namespace
+
+extern "C" size_t galv_expert_matmul_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* x, int64_t x_stride, const void* w)
+{
+    if (!ctx || !mx_size_ok(rows, n) || !mx_size_ok(rows, k) || rows == 0 || experts < 1 || experts > kExpertsMost) return 0;
+    return align_plan(rows, k, x, x_stride, experts, n, k, w).total;
+}
+
+extern "C" int galv_expert_matmul(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* x, int64_t x_stride, const void* w, const void* bias,
+                                  void* y, int64_t y_stride, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx) return GALV_ERR_INVALID_ARG;
+    return product16(ctx, "galv_expert_matmul", false, rows, experts, n, k, ends, x, x_stride, w, bias, y, y_stride, dtype, workspace, workspace_bytes, stream);
+}
+
+extern "C" size_t galv_expert_input_grad_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* w)
+{
+    if (!ctx || !mx_size_ok(rows, n) || !mx_size_ok(rows, k) || rows == 0 || experts < 1 || experts > kExpertsMost) return 0;
+    return align_plan(rows, n, dy, dy_stride, experts, n, k, w).total;
+}
+
+extern "C" int galv_expert_input_grad(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* dy, int64_t dy_stride, const void* w, void* dx,
+                                      int64_t dx_stride, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx) return GALV_ERR_INVALID_ARG;
+    return product16(ctx, "galv_expert_input_grad", true, rows, experts, k, n, ends, dy, dy_stride, w, nullptr, dx, dx_stride, dtype, workspace, workspace_bytes, stream);
+}
+
+extern "C" int galv_i8_matmul(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const int8_t* x_codes, const float* x_scales, const int8_t* w_codes,
+                              const float* w_scales, const void* bias, void* y, int64_t y_stride, int32_t dtype, void* stream)
+{
+    if (!ctx) return GALV_ERR_INVALID_ARG;
+    if (!whole_sizes_ok(rows, experts, n, k, ends, dtype)) return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_i8_matmul: sizes, number of experts or type outside the limits");
+    if (rows == 0) return GALV_OK;
+    if (!x_codes || !x_scales || !mx_aligned(x_codes, 16) || !mx_aligned(x_scales, 4) || !whole_pointers_ok(n, ends, w_codes, w_scales, bias, y, y_stride, dtype))
+        return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_i8_matmul: NULL or misaligned pointer, or a row stride below n");
+    const int may = whole_may(ctx);
+    if (may != GALV_OK) return may;
+    MxDevice dev(ctx);
+    if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
+    return whole_launch(ctx, "galv_i8_matmul", rows, experts, n, k, ends, x_codes, x_scales, w_codes, w_scales, bias, y, y_stride, dtype, (cudaStream_t)stream);
+}
+
+extern "C" size_t galv_i8_linear_workspace_bytes(int64_t rows, int64_t k) { return mx_size_ok(rows, k) ? up((size_t)rows * i8_pitch(k)) + up((size_t)rows * 4) : 0; }
+
+extern "C" int galv_i8_linear(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* x, int64_t x_stride, const int8_t* w_codes,
+                              const float* w_scales, const void* bias, void* y, int64_t y_stride, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx) return GALV_ERR_INVALID_ARG;
+    if (!whole_sizes_ok(rows, experts, n, k, ends, dtype)) return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_i8_linear: sizes, number of experts or type outside the limits");
+    if (rows == 0) return GALV_OK;
+    if (!mx_matrix_ok(x, x_stride, k, dtype) || !whole_pointers_ok(n, ends, w_codes, w_scales, bias, y, y_stride, dtype))
+        return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_i8_linear: NULL or misaligned pointer, or a row stride below the row's length");
+    if (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < galv_i8_linear_workspace_bytes(rows, k))
+        return galv_set_error(ctx, GALV_ERR_WORKSPACE, "galv_i8_linear: workspace NULL, misaligned or too small");
+    const int may = whole_may(ctx);
+    if (may != GALV_OK) return may;
+    MxDevice dev(ctx);
+    if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
+    int8_t* const codes = (int8_t*)workspace;
+    float* const scales = (float*)(codes + up((size_t)rows * i8_pitch(k)));
+    const cudaError_t e = galv_i8_pack_launch(ctx->num_sms, rows, k, x, x_stride, dtype, codes, scales, (cudaStream_t)stream);
+    if (e != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
+    return whole_launch(ctx, "galv_i8_linear", rows, experts, n, k, ends, codes, scales, w_codes, w_scales, bias, y, y_stride, dtype, (cudaStream_t)stream);
+}

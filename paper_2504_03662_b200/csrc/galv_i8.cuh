@@ -1,0 +1,9 @@
+// Rows of 8-bit integers: layout and packing shared by the translation units that hold and multiply them.  The format is described in include/galv.h.
+#pragma once
+
+#include "galv_mx.cuh"
+
+constexpr float kI8Least = 7.888609052210118e-31f;        // 2^-100: a row's largest magnitude counts as this at least, so that its scale's inverse is a number
+inline int64_t i8_pitch(int64_t cols) { return (cols + 15) / 16 * 16; }      // bytes of a row of codes
+
+cudaError_t galv_i8_pack_launch(int num_sms, int64_t rows, int64_t cols, const void* x, int64_t stride, int32_t dtype, int8_t* codes, float* scales, cudaStream_t st);

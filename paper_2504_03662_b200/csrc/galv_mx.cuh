@@ -377,3 +377,6 @@ __device__ __forceinline__ void mx_restore8(const uint8_t* __restrict__ codes, c
 // 16-byte pieces exchanged by row % 8.
 cudaError_t galv_mx_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows,
                         uint32_t box_cols, bool swizzle);
+// ... of several such matrices one behind the other, read in swizzled boxes of one of them each (zeros behind each one's last row).
+cudaError_t galv_map_3d(CUtensorMap* map, CUtensorMapDataType type, const void* base, uint64_t matrices, uint64_t rows, uint64_t cols, uint64_t pitch,
+                        uint32_t box_rows, uint32_t box_cols);

@@ -173,8 +173,9 @@ extern "C" int galv_mx_unpack(galv_ctx* ctx, int64_t rows, int64_t cols, int32_t
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
 
-cudaError_t galv_mx_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows, uint32_t box_cols,
-                        bool swizzle)
+namespace {
+
+cudaError_t encode(CUtensorMap* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box, bool swizzle)
 {
     using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -186,9 +187,25 @@ cudaError_t galv_mx_map(CUtensorMap* map, CUtensorMapDataType type, const void* 
         return reinterpret_cast<Encode>(p);
     }();
     if (!fn) return cudaErrorNotSupported;
-    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {pitch};
-    const cuuint32_t box[2] = {box_cols, box_rows}, one[2] = {1, 1};
-    const CUresult r = fn(map, type, 2, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+    const cuuint32_t one[3] = {1, 1, 1};
+    const CUresult r = fn(map, type, rank, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+}  // namespace
+
+cudaError_t galv_mx_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows, uint32_t box_cols,
+                        bool swizzle)
+{
+    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {pitch};
+    const cuuint32_t box[2] = {box_cols, box_rows};
+    return encode(map, type, 2, base, dims, strides, box, swizzle);
+}
+
+cudaError_t galv_map_3d(CUtensorMap* map, CUtensorMapDataType type, const void* base, uint64_t matrices, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows, uint32_t box_cols)
+{
+    const cuuint64_t dims[3] = {cols, rows, matrices}, strides[2] = {pitch, rows * pitch};
+    const cuuint32_t box[3] = {box_cols, box_rows, 1};
+    return encode(map, type, 3, base, dims, strides, box, true);
 }

@@ -17,10 +17,14 @@
 #include <atomic>
 #include <type_traits>
 
+#include "galv_experts.cuh"
 #include "galv_mx.cuh"
 #include "galv_tc.cuh"
+#include "galv_tile_out.cuh"
 
 namespace {
+
+using tile_out::move_out;
 
 constexpr int kTokens = 64, kTile = 256, kHalf = kTile / 2;
 // Rings of chunks of 64 tokens, each held only while it is needed: dy from its copy to its product, restored x from restoring to the product, codes and
@@ -120,85 +124,6 @@ template <> struct Restore<__half> {
         hi = clip(v[2] * s, v[3] * s);
     }
 };
-
-template <typename O> struct Four;
-template <> struct Four<float> { using type = float4; };
-template <> struct Four<__nv_bfloat16> { using type = uint2; };
-template <> struct Four<__half> { using type = uint2; };
-template <typename O> __device__ __forceinline__ float2 two(uint32_t w);
-template <> __device__ __forceinline__ float2 two<__nv_bfloat16>(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
-template <> __device__ __forceinline__ float2 two<__half>(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
-template <typename O> __device__ __forceinline__ uint32_t join(float a, float b);
-template <> __device__ __forceinline__ uint32_t join<__nv_bfloat16>(float a, float b) { const __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t*>(&h); }
-template <> __device__ __forceinline__ uint32_t join<__half>(float a, float b) { const __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<const uint32_t*>(&h); }
-template <typename Q, typename O> struct AddFour {
-    static __device__ __forceinline__ void to(float (&v)[4], const Q& q)
-    {
-        const float2 a = two<O>(q.x), b = two<O>(q.y);
-        v[0] += a.x; v[1] += a.y; v[2] += b.x; v[3] += b.y;
-    }
-};
-template <typename O> struct AddFour<float4, O> { static __device__ __forceinline__ void to(float (&v)[4], const float4& q) { v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w; } };
-template <typename Q, typename O> struct RoundFour { static __device__ __forceinline__ Q of(const float (&v)[4]) { return make_uint2(join<O>(v[0], v[1]), join<O>(v[2], v[3])); } };
-template <typename O> struct RoundFour<float4, O> { static __device__ __forceinline__ float4 of(const float (&v)[4]) { return make_float4(v[0], v[1], v[2], v[3]); } };
-
-// A warp's 32 x 128 sums in tensor memory, a row a lane, to a matrix with rows k apart: 16 columns at a time go through the warp's shared memory
-// (rows of 64 bytes, their 16-byte pieces exchanged by row / 2 % 4), so that lanes next to one another write next to one another.  base and out point to
-// the thread's first place; `rows` and `cols` of them exist.  All loads of a round come before its first store: out may be base.
-template <typename O>
-__device__ __forceinline__ void move_out(uint32_t tmem, uint32_t mine, const O* base, O* out, long long k, int rows, int cols, bool vec)
-{
-    const int lane = threadIdx.x % 32;
-    using Q = typename Four<O>::type;
-    // vec: a lane has 4 columns of rows lane / 4 + 8 i, k is a multiple of 4; else one column of rows lane / 16 + 2 i
-    const uint32_t from = vec ? mine + lane / 4 * 64 + ((lane % 4) ^ (lane >> 3 & 3)) * 16 : mine + lane / 16 * 64 + lane % 4 * 4, piece = lane % 16 / 4;
-    rows -= vec ? lane / 4 : lane / 16;
-    cols -= vec ? lane % 4 * 4 : lane % 16;
-#pragma unroll 1
-    for (int j = 0; j < 128; j += 16) {
-        uint32_t s[16];
-        tc::tmem_load16(tmem + j, s);
-        tc::tmem_wait_load();
-        __syncwarp();
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(mine + lane * 64 + (q ^ (lane >> 1 & 3)) * 16), "r"(s[4 * q]), "r"(s[4 * q + 1]), "r"(s[4 * q + 2]), "r"(s[4 * q + 3]) : "memory");
-        __syncwarp();
-        const bool in = j < cols;
-        if (vec) {
-            float v[4][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[i][0]), "=f"(v[i][1]), "=f"(v[i][2]), "=f"(v[i][3]) : "r"(from + i * 512));
-            if (base) {
-                Q q[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (in && i * 8 < rows) q[i] = *reinterpret_cast<const Q*>(base + i * 8 * k + j);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) AddFour<Q, O>::to(v[i], q[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (in && i * 8 < rows) *reinterpret_cast<Q*>(out + i * 8 * k + j) = RoundFour<Q, O>::of(v[i]);
-        } else {
-#pragma unroll
-            for (int h = 0; h < 32; h += 16) {
-                float v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[i]) : "r"(from + (h + 2 * i) * 64 + (piece ^ (i & 3)) * 16));
-                if (base) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (in && h + 2 * i < rows) v[i] += mx_float(base[(h + 2 * i) * k + j]);
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (in && h + 2 * i < rows) out[(h + 2 * i) * k + j] = mx_round<O>(v[i]);
-            }
-        }
-    }
-}
 
 template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(N)); }
 template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(N)); }
@@ -530,6 +455,11 @@ cudaError_t launch(const galv_ctx* ctx, const WgradPlan& p, const CUtensorMap& d
 
 }  // namespace
 
+void galv_align_rows(const galv_ctx* ctx, int64_t rows, int64_t cols, const void* x, int64_t stride, void* out, int64_t pitch, cudaStream_t st)
+{
+    mx_align_kernel<<<(int)(rows < ctx->num_sms * 16 ? rows : ctx->num_sms * 16), 256, 0, st>>>(rows, (int)cols, (const __half*)x, stride, (__half*)out, pitch);
+}
+
 extern "C" size_t galv_mx_weight_grad_workspace_bytes(const galv_ctx* ctx, int64_t tokens, int64_t n, int64_t k, const void* dy, int64_t dy_stride)
 {
     if (!ctx || !mx_size_ok(tokens, n) || !mx_size_ok(tokens, k) || tokens == 0) return 0;
@@ -567,7 +497,7 @@ extern "C" int galv_mx_weight_grad(galv_ctx* ctx, int64_t tokens, int64_t n, int
         int64_t stride = dy_stride;
         if (p.aligned) {
             stride = (n + 7) / 8 * 8;
-            mx_align_kernel<<<(int)(tokens < ctx->num_sms * 16 ? tokens : ctx->num_sms * 16), 256, 0, st>>>(tokens, (int)n, (const __half*)dy, dy_stride, (__half*)workspace, stride);
+            galv_align_rows(ctx, tokens, n, dy, dy_stride, workspace, stride, st);
             rows = workspace;
         }
         CUtensorMap dm, cm, sm;

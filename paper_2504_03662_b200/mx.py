@@ -273,10 +273,13 @@ def _as_typed(f):
 class _Linear(torch.autograd.Function):
     @staticmethod
     @_as_typed
-    def forward(ctx, x, weight, bias, four, keep):
+    def forward(ctx, x, weight, bias, four, keep, eight):
         flat = _flat(x)
         if four:
             y = matmul(pack(flat, gb.MX4), pack(weight, gb.MX4), x.dtype, bias)
+        elif eight:
+            from . import i8                              # which takes its checks from this module
+            y = i8.linear(flat, i8.pack(weight), bias)
         else:
             y = flat @ weight.t() if bias is None else torch.addmm(bias, flat, weight.t())
         kept = pack(flat) if keep and ctx.needs_input_grad[1] else None
@@ -297,19 +300,27 @@ class _Linear(torch.autograd.Function):
             dw = weight_grad(flat, Packed(*kept, flat.shape[0], weight.shape[1]), weight.dtype)
         if ctx.has_bias and ctx.needs_input_grad[2]:
             db = flat.sum(0, dtype=torch.float32).to(dy.dtype)
-        return dx, dw, db, None, None
+        return dx, dw, db, None, None, None
 
 
-def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, four: bool = False) -> torch.Tensor:
+def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, four: bool = False, eight: bool = False) -> torch.Tensor:
     """x weight^T + bias (bf16 or fp16), x kept in 8 bits for the weight's gradient (where one will be taken).  `four`: the forward product takes both operands in
-    4 bits; the gradients are those of the product of the unrounded operands (straight through the rounding)."""
+    4 bits; `eight`: in 8-bit integers with a scale for each token and each output (module i8); the gradients are those of the product of the unrounded operands (straight
+    through the rounding)."""
     _kind(x.dtype, "x", _SHORT)
     _last_axis(x)
     if weight.dim() != 2 or weight.dtype != x.dtype or weight.shape[0] < 1 or weight.shape[1] != x.shape[-1]:
         raise ValueError(f"weight of shape {tuple(weight.shape)} and {weight.dtype} beside x of {tuple(x.shape)} and {x.dtype}")
     if bias is not None and (bias.dtype != x.dtype or bias.dim() > 1):
         raise ValueError(f"bias is [{weight.shape[0]}] of {x.dtype}, not {tuple(bias.shape)} of {bias.dtype}")
-    return _Linear.apply(x, weight, bias, four, torch.is_grad_enabled())
+    if eight:
+        if four:
+            raise ValueError("a forward product is in 4 bits or in 8-bit integers, not both")
+        if x.shape[-1] > gb.I8_MOST:
+            raise ValueError(f"products of 8-bit integers sum up to {gb.I8_MOST} columns, not {x.shape[-1]}")
+        if bias is not None and tuple(bias.shape) != weight.shape[:1]:
+            raise ValueError(f"bias is [{weight.shape[0]}] of {x.dtype}, not {tuple(bias.shape)} of {bias.dtype}")
+    return _Linear.apply(x, weight, bias, four, torch.is_grad_enabled(), eight)
 
 
 class _Norm(torch.autograd.Function):
