@@ -566,6 +566,13 @@ int galv_expert_weight_grad(galv_ctx* ctx, int64_t rows, int32_t experts, int64_
                             void* workspace, size_t workspace_bytes, void* stream);
 int galv_expert_bias_grad(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, const int32_t* ends, const void* dy, int64_t dy_stride,
                           int32_t dtype, void* db, int32_t db_dtype, void* stream);
+/* The last three in one call, each where its result is asked for (dx, dw [experts][n][k], db [experts][n], all of `dtype`; NULL: not; x and w may be NULL where
+ * no result needs them).  workspace: the bytes that the query gives with the x and w that are needed, else NULL. */
+size_t galv_expert_backward_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy,
+                                            int64_t dy_stride, const void* x, int64_t x_stride, const void* w);
+int galv_expert_backward(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* dy,
+                         int64_t dy_stride, const void* x, int64_t x_stride, const void* w, int32_t dtype, void* dx, int64_t dx_stride,
+                         void* dw, void* db, void* workspace, size_t workspace_bytes, void* stream);
 /* Waits for `stream` and says whether a bounded device-side wait of a product (galv_mx_weight_grad, galv_mx_matmul, galv_i8_*, galv_expert_*), of whichever context, has run out on this
  * device since this context was made or last looked (GALV_ERR_TIMEOUT: the results since then are void; GALV_OK otherwise).  Not for stream capture.
  * The products look too, without waiting, and return GALV_ERR_TIMEOUT in place of a launch; replays of a captured graph do not look. */

@@ -49,7 +49,8 @@ EXPORTS = ("galv_create", "galv_destroy", "galv_strerror", "galv_last_error", "g
            "galv_add_form_cost", "galv_mx_status", "galv_mx_timeouts", "galv_i8_codes_bytes", "galv_i8_pack", "galv_i8_unpack",
            "galv_i8_matmul", "galv_i8_linear_workspace_bytes", "galv_i8_linear", "galv_expert_matmul_workspace_bytes",
            "galv_expert_matmul", "galv_expert_input_grad_workspace_bytes", "galv_expert_input_grad",
-           "galv_expert_weight_grad_workspace_bytes", "galv_expert_weight_grad", "galv_expert_bias_grad")
+           "galv_expert_weight_grad_workspace_bytes", "galv_expert_weight_grad", "galv_expert_bias_grad",
+           "galv_expert_backward_workspace_bytes", "galv_expert_backward")
 
 
 class galv_shape(C.Structure):
@@ -139,6 +140,9 @@ def load_library() -> C.CDLL:
     lib.galv_expert_weight_grad_workspace_bytes.restype = sz
     lib.galv_expert_weight_grad.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, i64, i32, vp, vp, i32, vp, sz, vp]
     lib.galv_expert_bias_grad.argtypes = [vp, i64, i32, i64, vp, vp, i64, i32, vp, i32, vp]
+    lib.galv_expert_backward_workspace_bytes.argtypes = [vp, i64, i32, i64, i64, vp, i64, vp, i64, vp]
+    lib.galv_expert_backward_workspace_bytes.restype = sz
+    lib.galv_expert_backward.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, i64, vp, i32, vp, i64, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -446,5 +450,15 @@ class Galv:
     def galv_expert_bias_grad(self, ends, dy, db):
         rc = self.lib.galv_expert_bias_grad(self.h, dy.shape[0], *db.shape, _at(ends), *_matrix(dy), _DTYPES[dy.dtype], db.data_ptr(), _DTYPES[db.dtype],
                                             _raw_stream(self.device))
+        if rc:
+            self._check(rc)
+
+    def galv_expert_backward(self, shape, ends, dy, x, w, dx, dw, db, room):
+        """shape: (experts, n, k); x, w, dx, dw, db or None; room(bytes): a workspace of so many."""
+        rows, dm, xm = dy.shape[0], _matrix(dy), (None, 0) if x is None else _matrix(x)
+        size = self.lib.galv_expert_backward_workspace_bytes(self.h, rows, *shape, *dm, *xm, _at(w))
+        ws = room(size) if size else None
+        rc = self.lib.galv_expert_backward(self.h, rows, *shape, _at(ends), *dm, *xm, _at(w), _DTYPES[dy.dtype], *((None, 0) if dx is None else _matrix(dx)), _at(dw), _at(db),
+                                           *_ws(ws), _raw_stream(self.device))
         if rc:
             self._check(rc)

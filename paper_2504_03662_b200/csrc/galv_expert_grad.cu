@@ -4,8 +4,8 @@
 // stored.  An expert's rows end anywhere: its last chunk of 64 holds rows of the next expert (or of none, which may be anything).  Of those the matrix
 // instructions take no steps of 16 rows that are not needed, and what is left of the last step is set to zero in shared memory, in both operands, since
 // zero times what lies there could be NaN.
-// Per CTA: a thread that starts bulk tensor copies, a warp that issues the matrix instructions for the pair (in the second CTA: tells the first that its rows
-// are there) after it has set such rows to zero, eight warps that take sums from the tensor memory while the next are made and move results out.
+// Per CTA: a thread that starts bulk tensor copies, a warp that sets such rows to zero and tells the first CTA of the pair that a chunk is there, a thread (of the first)
+// that issues the matrix instructions for the pair, eight warps that take sums from the tensor memory while the next are made and move results out.
 
 #include "galv_experts.cuh"
 #include "galv_tc.cuh"
@@ -13,10 +13,10 @@
 
 namespace {
 
-constexpr int kStages = 6, kTokens = 64, kTile = 256, kHalf = kTile / 2;
+constexpr int kStages = 5, kTokens = 64, kTile = 256, kHalf = kTile / 2;
 constexpr int kBox = kTokens * 128;                       // 64 rows of 64 columns
 constexpr int kOperand = 2 * kBox, kStageBytes = 2 * kOperand;
-constexpr int kOutBytes = 8 * 2048;
+constexpr int kOutBytes = 8 * 4096;                       // 32 rows of 128 bytes of each warp that moves results out
 constexpr int kThreads = 384;
 // A tensor core's sum is cut at every addition, 8e-7 of the result over 1024 rows (the error grows with the root of the length): after this many chunks the
 // sum goes to fp32 registers, rounded additions.
@@ -30,7 +30,7 @@ struct GradArgs {
     const int32_t* ends;
     const void* base;
     void* dw;
-    int vec;                                              // four results of a row can be moved at once
+    int boxes;                                            // base and dw are moved by bulk copies
     unsigned* timeouts;
 };
 
@@ -65,15 +65,41 @@ __device__ __forceinline__ void fill(const O* base, O* out, long long k, int row
         for (int c = threadIdx.x % 32; c < cols; c += 32) out[r * k + c] = base ? base[r * k + c] : mx_zero<O>();
 }
 
+// 16 bytes of results: sums, and what base has there
+__device__ __forceinline__ uint4 four_words(const uint32_t* v, const uint4* base, float)
+{
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
+    if (base) {
+        f[0] += __uint_as_float(base->x); f[1] += __uint_as_float(base->y); f[2] += __uint_as_float(base->z); f[3] += __uint_as_float(base->w);
+    }
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
+template <typename O>
+__device__ __forceinline__ uint4 four_words(const uint32_t* v, const uint4* base, O)
+{
+    MxPiece<O> p;
+    float f[8], b[8];
+    if (base) {
+        p.q[0] = *base;
+        mx_floats(p, b);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = base ? b[i] + __uint_as_float(v[i]) : __uint_as_float(v[i]);
+    return mx_piece<O>(f).q[0];
+}
+
 template <typename O>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ GradArgs a)
+expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap base_map,
+                   const __grid_constant__ CUtensorMap dw_map, const __grid_constant__ GradArgs a)
 {
     extern __shared__ unsigned char raw[];
     const uint32_t base = (tc::smem_at(raw) + 1023) & ~1023u;
     const uint32_t out_at = base + kStages * kStageBytes, bars = out_at + kOutBytes;
-    const uint32_t full = bars, other = full + 8 * kStages, empty = other + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16, drain = acc_empty + 16,
-                   slot = drain + 8;
+    const uint32_t full = bars, ready = full + 8 * kStages, empty = ready + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16, drain = acc_empty + 16,
+                   base_full = drain + 8, slot = base_full + 64;
     int* const begin = reinterpret_cast<int*>(raw + (bars + 256 - tc::smem_at(raw)));
     __shared__ int failed;
 
@@ -84,7 +110,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
             tc::bar_init(full + 8 * s, 1);
-            tc::bar_init(other + 8 * s, 1);
+            tc::bar_init(ready + 8 * s, 2);
             tc::bar_init(empty + 8 * s, 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -92,6 +118,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
             tc::bar_init(acc_empty + 8 * b, 16);
         }
         tc::bar_init(drain, 1);
+        for (int b = 0; b < 8; ++b) tc::bar_init(base_full + 8 * b, 1);
         tc::bar_init_done();
         failed = 0;
         if (a.rows > 0) {                                 // else there are none
@@ -100,7 +127,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
         }
     }
     if (warp == 2) tc::tmem_alloc<2>(slot, 512);
-    if (warp == 3) experts_scan(a.ends, a.experts, a.rows, begin, begin + a.experts + 1);
+    if (warp == 0) experts_scan(a.ends, a.experts, a.rows, begin, begin + a.experts + 1);
     tc::fence_before();
     __syncthreads();
     tc::cluster_sync();                                   // the pair's barriers exist
@@ -135,7 +162,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
             if (*(volatile int*)&failed)                  // copies still in flight
                 for (int i = it < kStages ? 0 : it - kStages; i < it; ++i) tc::bar_wait(full + 8 * (i % kStages), i / kStages & 1);
         }
-    } else if (warp == 1 && rank == 1) {                  // tells the first CTA that this one's rows are there
+    } else if (warp == 3) {                               // tells the first CTA that this one's rows are there, with zeros for what is not the expert's
         int it = 0;
         bool ok = true;
         for (int u = first; u < units && ok; u += stride) {
@@ -148,72 +175,72 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
                     tc::fence_async();
                 }
                 __syncwarp();
-                if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(other + 8 * s, 0));
+                if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(ready + 8 * s, 0));
             }
         }
-    } else if (warp == 1) {
-        int it = 0, done = 0;
-        bool ok = true;
-        for (int u = first; u < units && ok; u += stride) {
-            const Unit w = unit_of(a, begin, u);
-            for (int r = 0; r < w.count && ok; ++done) {
-                const uint32_t buf = done & 1, d = tmem + buf * kTile;
-                const int end = r + min(kSegment * kTokens, w.count - r);
-                if (!(ok = __all_sync(0xffffffffu, waited(acc_empty + 8 * buf, (done / 2 & 1) ^ 1)))) break;
-                tc::fence_after();
-                for (bool add = false; r < end; r += kTokens, ++it, add = true) {
-                    const int s = it % kStages;
-                    const uint32_t at = base + s * kStageBytes;
-                    if (!(ok = __all_sync(0xffffffffu, waited(full + 8 * s, it / kStages & 1) && waited(other + 8 * s, it / kStages & 1)))) break;
+    } else if (warp == 1 && rank == 0) {
+        if (tc::elect()) {
+            int it = 0, done = 0;
+            bool ok = true;
+            for (int u = first; u < units && ok; u += stride) {
+                const Unit w = unit_of(a, begin, u);
+                for (int r = 0; r < w.count && ok; ++done) {
+                    const uint32_t buf = done & 1, d = tmem + buf * kTile;
+                    const int end = r + min(kSegment * kTokens, w.count - r);
+                    if (!(ok = waited(acc_empty + 8 * buf, (done / 2 & 1) ^ 1))) break;
                     tc::fence_after();
-                    if (w.count - r < kTokens) {
-                        clear_rows(at, w.count - r);
-                        tc::fence_async();
-                        __syncwarp();
-                    }
-                    if (lane == 0) {
-                        const int steps = min(kTokens / 16, (w.count - r + 15) / 16);
+                    for (bool add = false; r < end; r += kTokens, ++it, add = true) {
+                        const int s = it % kStages, steps = min(kTokens / 16, (w.count - r + 15) / 16);
+                        const uint32_t at = base + s * kStageBytes;
+                        if (!(ok = waited(ready + 8 * s, it / kStages & 1))) break;
+                        tc::fence_after();
 #pragma unroll
                         for (int j = 0; j < kTokens / 16; ++j)
-                            if (j < steps) tc::mma_f16(d, tc::operand(at + j * 2048, kBox, 1024), tc::operand(at + kOperand + j * 2048, kBox, 1024), a.what, add || j > 0);
+                            if (j < steps) tc::mma_f16<2>(d, tc::operand(at + j * 2048, kBox, 1024), tc::operand(at + kOperand + j * 2048, kBox, 1024), a.what, add || j > 0);
                         tc::mma_commit<2>(empty + 8 * s);
                     }
-                    __syncwarp();
+                    if (ok) tc::mma_commit<2>(acc_full + 8 * buf);
                 }
-                if (ok && lane == 0) tc::mma_commit<2>(acc_full + 8 * buf);
+            }
+            if (*(volatile int*)&failed) {
+                tc::mma_commit<2>(drain);
+                tc::bar_wait(drain, 0);
             }
         }
-        if (lane == 0 && *(volatile int*)&failed) {
-            tc::mma_commit<2>(drain);
-            tc::bar_wait(drain, 0);
-        }
     } else if (warp >= 4) {
+        constexpr int piece = 128 / (int)sizeof(O);        // columns of a copy
         const int quad = warp % 4, half = (warp - 4) / 4;  // 32 rows, 128 columns
-        const uint32_t mine = out_at + (warp - 4) * 2048, from = tmem + half * 128 + ((uint32_t)quad * 32 << 16);
+        const uint32_t mine = out_at + (warp - 4) * 4096, from = tmem + half * 128 + ((uint32_t)quad * 32 << 16), base_bar = base_full + 8 * (warp - 4);
         int done = 0;
-        bool ok = true;
+        uint32_t phase = 0;
+        bool ok = true, fetched = false;
         for (int u = first; u < units && ok; u += stride) {
             const Unit w = unit_of(a, begin, u);
             const long long r0 = (long long)w.tn * kTile + rank * kHalf + quad * 32, c0 = (long long)w.tk * kTile + half * 128;
             const int rows = (int)max(-64ll, min(32ll, a.n - r0)), cols = (int)max(-128ll, min(128ll, a.k - c0));
-            const long long at0 = w.expert * a.n * a.k + r0 * a.k + c0;
-            if (w.count == 0) {
-                fill<O>(a.base ? (const O*)a.base + at0 : nullptr, (O*)a.dw + at0, a.k, rows, cols);
-                continue;
-            }
-            uint32_t buf = done & 1;
+            const bool some = rows > 0 && cols > 0;
+            auto fetch = [&](int c) {                      // base's piece, once the copy before has read this memory
+                fetched = true;
+                if (lane == 0) {
+                    tc::stores_read();
+                    tc::bar_expect(base_bar, 4096);
+                    tc::load_3d(mine, &base_map, (int)c0 + c, (int)r0, w.expert, base_bar);
+                }
+            };
+            if (a.boxes && a.base && some) fetch(0);
+            uint32_t acc = done & 1;
             if (w.count > kSegment * kTokens) {           // earlier segments are taken up here, the last one is added where it lies
                 float sum[128];
 #pragma unroll
                 for (int i = 0; i < 128; ++i) sum[i] = 0.f;
                 for (int left = w.count; left > 0; left -= kSegment * kTokens) {
-                    buf = done & 1;
-                    if (!(ok = waited(acc_full + 8 * buf, done / 2 & 1))) break;
+                    acc = done & 1;
+                    if (!(ok = waited(acc_full + 8 * acc, done / 2 & 1))) break;
                     tc::fence_after();
 #pragma unroll
                     for (int j = 0; j < 128; j += 16) {
                         uint32_t v[16];
-                        tc::tmem_load16(from + buf * kTile + j, v);
+                        tc::tmem_load16(from + acc * kTile + j, v);
                         tc::tmem_wait_load();
 #pragma unroll
                         for (int i = 0; i < 16; ++i) sum[j + i] += __uint_as_float(v[i]);
@@ -221,24 +248,68 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
                     if (left > kSegment * kTokens) {      // this accumulator may be summed into again
                         tc::fence_before();
                         __syncwarp();
-                        if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_empty + 8 * buf, 0));
+                        if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_empty + 8 * acc, 0));
                         ++done;
                     }
                 }
 #pragma unroll
-                for (int j = 0; j < 128; j += 16) tc::tmem_store16(from + buf * kTile + j, sum + j);
+                for (int j = 0; j < 128; j += 16) tc::tmem_store16(from + acc * kTile + j, sum + j);
                 tc::tmem_wait_store();
-            } else if ((ok = waited(acc_full + 8 * buf, done / 2 & 1))) {
+            } else if (w.count > 0 && (ok = waited(acc_full + 8 * acc, done / 2 & 1))) {
                 tc::fence_after();
             }
+            if (a.boxes) {
+                if (some)
+#pragma unroll 1
+                    for (int c = 0; c < cols; c += piece) {
+                        uint32_t v[piece];
+                        if (a.base && c > 0) fetch(c);
+                        if (w.count > 0) {
+#pragma unroll
+                            for (int i = 0; i < piece; i += 32) tc::tmem_load32(from + acc * kTile + c + i, v + i);
+                            tc::tmem_wait_load();
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < piece; ++i) v[i] = 0;
+                        }
+                        if (a.base) {
+                            ok = waited(base_bar, phase) && ok;
+                            phase ^= 1;
+                            fetched = false;
+                        } else {
+                            if (lane == 0) tc::stores_read();
+                            __syncwarp();
+                        }
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {      // a lane has a row; its 16-byte pieces are exchanged by row % 8
+                            const uint32_t at = mine + lane * 128 + ((q ^ (lane & 7)) * 16);
+                            uint4 b;
+                            if (a.base) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(at));
+                            const uint4 o = four_words(v + q * (16 / (int)sizeof(O)), a.base ? &b : nullptr, O());
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(at), "r"(o.x), "r"(o.y), "r"(o.z), "r"(o.w) : "memory");
+                        }
+                        tc::fence_async();
+                        __syncwarp();
+                        if (lane == 0) {
+                            tc::store_3d(&dw_map, (int)c0 + c, (int)r0, w.expert, mine);
+                            tc::stores_end();
+                        }
+                    }
+            } else if (ok) {
+                const long long at0 = w.expert * a.n * a.k + r0 * a.k + c0, at = at0 + lane / 16 * a.k + lane % 16;
+                if (w.count > 0) tile_out::move_out<O>(from + acc * kTile, mine, a.base ? (const O*)a.base + at : nullptr, (O*)a.dw + at, a.k, rows, cols, false);
+                else fill<O>(a.base ? (const O*)a.base + at0 : nullptr, (O*)a.dw + at0, a.k, rows, cols);
+            }
             if (!ok) break;
-            const long long at = at0 + (a.vec ? lane / 4 : lane / 16) * a.k + (a.vec ? lane % 4 * 4 : lane % 16);
-            tile_out::move_out<O>(from + buf * kTile, mine, a.base ? (const O*)a.base + at : nullptr, (O*)a.dw + at, a.k, rows, cols, a.vec);
-            tc::fence_before();
-            __syncwarp();
-            if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_empty + 8 * buf, 0));
-            ++done;
+            if (w.count > 0) {
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_empty + 8 * acc, 0));
+                ++done;
+            }
         }
+        if (fetched) tc::bar_wait(base_bar, phase);       // after a wait that ran out: a copy still in flight
+        if (lane == 0) tc::stores_read();
     }
     __syncwarp();
     tc::fence_before();
@@ -328,13 +399,20 @@ GradPlan plan_of(int64_t rows, int64_t n, int64_t k, const void* dy, int64_t dy_
 }
 
 template <typename O>
-cudaError_t launch(const galv_ctx* ctx, const CUtensorMap& dm, const CUtensorMap& xm, const GradArgs& a, cudaStream_t st)
+cudaError_t launch(const galv_ctx* ctx, const CUtensorMap& dm, const CUtensorMap& xm, CUtensorMapDataType type, GradArgs& a, cudaStream_t st)
 {
+    CUtensorMap bm = {}, wm = {};
+    a.boxes = mx_rows16(a.dw, a.k, sizeof(O) == 4 ? GALV_F32 : GALV_BF16) && mx_aligned(a.base, 16);
+    if (a.boxes) {
+        cudaError_t e = galv_map_3d(&wm, type, a.dw, a.experts, a.n, a.k, a.k * sizeof(O), 32, 128 / sizeof(O));
+        if (e == cudaSuccess && a.base) e = galv_map_3d(&bm, type, a.base, a.experts, a.n, a.k, a.k * sizeof(O), 32, 128 / sizeof(O));
+        if (e != cudaSuccess) return e;
+    }
     const cudaError_t e = cudaFuncSetAttribute(expert_grad_kernel<O>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kExpertsMost));
     if (e != cudaSuccess) return e;
     const long long units = (long long)a.experts * a.tiles_n * a.tiles_k;
     const int pairs = (int)(units < ctx->num_sms / 2 ? units : ctx->num_sms / 2);
-    expert_grad_kernel<O><<<pairs * 2, kThreads, smem_of(a.experts), st>>>(dm, xm, a);
+    expert_grad_kernel<O><<<pairs * 2, kThreads, smem_of(a.experts), st>>>(dm, xm, bm, wm, a);
     return cudaGetLastError();
 }
 
@@ -377,8 +455,6 @@ extern "C" int galv_expert_weight_grad(galv_ctx* ctx, int64_t rows, int32_t expe
     const uint32_t t = dtype == GALV_BF16 ? 1u : 0u;      // fp32 sums, both operands of this type with the summed index across their rows, 256 x 256
     a.what = 1u << 4 | t << 7 | t << 10 | 1u << 15 | 1u << 16 | (uint32_t)(kTile >> 3) << 17 | (uint32_t)(kTile >> 4) << 24;
     a.ends = ends; a.base = base; a.dw = dw; a.timeouts = ctx->mx_timeouts_at;
-    const int four = 4 * mx_size_of(dw_dtype);
-    a.vec = k % 4 == 0 && mx_aligned(dw, four) && mx_aligned(base, four);
     CUtensorMap dm = {}, xm = {};
     if (rows > 0) {
         const GradPlan p = plan_of(rows, n, k, dy, dy_stride, x, x_stride);
@@ -400,9 +476,9 @@ extern "C" int galv_expert_weight_grad(galv_ctx* ctx, int64_t rows, int32_t expe
     }
     // without rows no copy is made: the maps are not read
     cudaError_t e;
-    if (dw_dtype == GALV_F32) e = launch<float>(ctx, dm, xm, a, st);
-    else if (dw_dtype == GALV_BF16) e = launch<__nv_bfloat16>(ctx, dm, xm, a, st);
-    else e = launch<__half>(ctx, dm, xm, a, st);
+    if (dw_dtype == GALV_F32) e = launch<float>(ctx, dm, xm, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, a, st);
+    else if (dw_dtype == GALV_BF16) e = launch<__nv_bfloat16>(ctx, dm, xm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a, st);
+    else e = launch<__half>(ctx, dm, xm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, a, st);
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
 
@@ -426,4 +502,60 @@ extern "C" int galv_expert_bias_grad(galv_ctx* ctx, int64_t rows, int32_t expert
     else expert_bias_grad_kernel<__half, __half><<<grid, 256, smem, st>>>(rows, experts, n, ends, (const __half*)dy, dy_stride, vec, (__half*)db);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
+}
+
+namespace {
+
+// What the three gradients need one after the other: dy in rows that bulk copies can take, read by all, and behind it what any of them needs for itself.
+struct BackwardPlan { size_t dy, total; int64_t stride; };
+BackwardPlan backward_plan(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const void* w)
+{
+    BackwardPlan p;
+    p.dy = plan_of(rows, n, k, dy, dy_stride, x, x_stride).dy;
+    p.stride = p.dy ? (n + 7) / 8 * 8 : dy_stride;
+    const void* const at = p.dy ? nullptr : dy;           // moved rows lie on 256 bytes
+    const size_t a = w ? galv_expert_input_grad_workspace_bytes(ctx, rows, experts, n, k, at, p.stride, w) : 0;
+    const size_t b = x ? galv_expert_weight_grad_workspace_bytes(ctx, rows, experts, n, k, at, p.stride, x, x_stride) : 0;
+    p.total = p.dy + (a > b ? a : b);
+    return p;
+}
+
+}  // namespace
+
+extern "C" size_t galv_expert_backward_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
+                                                       const void* w)
+{
+    if (!ctx || !mx_size_ok(rows, n) || !mx_size_ok(rows, k) || rows == 0 || experts < 1 || experts > kExpertsMost) return 0;
+    return backward_plan(ctx, rows, experts, n, k, dy, dy_stride, x, x_stride, w).total;
+}
+
+extern "C" int galv_expert_backward(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
+                                    const void* w, int32_t dtype, void* dx, int64_t dx_stride, void* dw, void* db, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx) return GALV_ERR_INVALID_ARG;
+    if (!sizes_ok(rows, experts, n, k, ends, dtype, dtype)) return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_expert_backward: sizes, number of experts or type outside the limits");
+    if (rows > 0 && (!mx_matrix_ok(dy, dy_stride, n, dtype) || (dw && !x) || (dx && !w)))
+        return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_expert_backward: NULL or misaligned pointer, or a row stride below the row's length");
+    char* ws = (char*)workspace;
+    if (rows > 0) {
+        const BackwardPlan p = backward_plan(ctx, rows, experts, n, k, dy, dy_stride, dw ? x : nullptr, x_stride, dx ? w : nullptr);
+        if (p.total && (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < p.total))
+            return galv_set_error(ctx, GALV_ERR_WORKSPACE, "galv_expert_backward: workspace NULL, misaligned or too small");
+        if (p.dy) {
+            MxDevice dev(ctx);
+            if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
+            galv_align_rows(ctx, rows, n, dy, dy_stride, workspace, p.stride, (cudaStream_t)stream);
+            const cudaError_t e = cudaGetLastError();
+            if (e != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
+            dy = workspace;
+            dy_stride = p.stride;
+            ws += p.dy;
+            workspace_bytes -= p.dy;
+        }
+    }
+    int rc = GALV_OK;
+    if (dx) rc = galv_expert_input_grad(ctx, rows, experts, n, k, ends, dy, dy_stride, w, dx, dx_stride, dtype, ws, workspace_bytes, stream);
+    if (rc == GALV_OK && dw) rc = galv_expert_weight_grad(ctx, rows, experts, n, k, ends, dy, dy_stride, x, x_stride, dtype, nullptr, dw, dtype, ws, workspace_bytes, stream);
+    if (rc == GALV_OK && db) rc = galv_expert_bias_grad(ctx, rows, experts, n, ends, dy, dy_stride, dtype, db, dtype, stream);
+    return rc;
 }

@@ -28,7 +28,7 @@ constexpr int kGroup = 16;                                // tiles of tokens tha
 struct ProductArgs {
     long long rows, n, stride;                            // tokens, columns of y, from one row of y to the next
     int experts, tiles_m, chunks, last_steps;             // last_steps: of 32 bytes in the last chunk
-    uint32_t what;                                        // the matrix instruction without its number of tokens
+    uint32_t what;                                        // the matrix instruction without its sizes (the second kernel's: without its number of tokens)
     const int32_t* ends;
     const float* x_scales;
     const float* w_scales;
@@ -122,6 +122,7 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
             constexpr int elements = K == kWhole ? kChunkBytes : kChunkBytes / 2;
             int it = 0;
             bool ok = true;
+            if (K == kWhole) tc::before_is_over();        // the tokens may be put into 8-bit integers by the kernel in front
             for (int u = first; u < units && ok; u += stride) {
                 w.to(u);
                 const int m0 = w.tm * kTile + rank * kHalf, half = w.columns() / 2, r0 = w.row0 + rank * half;
@@ -172,8 +173,8 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
                         if (j < steps) {
                             const uint64_t wo = K == kInputGrad ? tc::operand(w_at + s * kRowsBytes + j * 2048, kRowsBytes / 2, 1024) : tc::operand(w_at + s * kRowsBytes + j * 32, 16, 1024);
                             const uint64_t xo = tc::operand(x_at + s * kRowsBytes + j * 32, 16, 1024);
-                            if (K == kWhole) tc::mma_i8(d, wo, xo, what, c > 0 || j > 0);
-                            else tc::mma_f16(d, wo, xo, what, c > 0 || j > 0);
+                            if (K == kWhole) tc::mma_i8<2>(d, wo, xo, what, c > 0 || j > 0);
+                            else tc::mma_f16<2>(d, wo, xo, what, c > 0 || j > 0);
                         }
                     tc::mma_commit<2>(empty + 8 * s);
                 }
@@ -190,6 +191,7 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
         const uint32_t mine = out_at + (warp - 4) * 2048, lanes = (uint32_t)quad * 32 << 16;
         O* const y = (O*)a.y;
         int done = 0;
+        if (K == kWhole) tc::before_is_over();
         for (int u = first; u < units; u += stride, ++done) {
             w.to(u);
             const uint32_t buf = done & 1;
@@ -247,6 +249,168 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
     if (warp == 2) tc::tmem_free<2>(tmem, 512);
 }
 
+// ---- few rows
+//
+// Up to 64 rows in all: reading the weights of the experts that have some is all there is.  A CTA has 128 of an expert's weights' rows, so that two fit an SM
+// and one starts while the other runs; the CTAs of a cluster share the summed index, so that about two an SM stream.  Each sends its sums' slices of the tokens
+// to the CTA of the cluster that has them, which adds them in order: no second kernel, no memory between.  Which expert a cluster has is found on the device (the
+// s-th of those that have rows); clusters are launched for as many experts as there could be, those that are too many end at once.  The weights' first copies
+// start before the kernel in front, which puts the tokens into 8-bit integers, is over.
+
+constexpr int kFewThreads = 256, kFewRows = 64;
+template <int N> struct Few {                             // N: rows, rounded up
+    static constexpr int stages = N == 16 ? 5 : N == 32 ? 4 : 3;
+    static constexpr int rows_w = 128 * kChunkBytes, rows_x = N * kChunkBytes, stage = rows_w + rows_x;
+    static constexpr int inbox = N * 128 * 4;
+    static constexpr int smem = 1024 + stages * stage + inbox + 256;
+};
+
+template <int K, typename O, int N>
+__global__ void __launch_bounds__(kFewThreads, 2)
+expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap part_map, const __grid_constant__ ProductArgs a, int tiles, int ranks)
+{
+    using F = Few<N>;
+    extern __shared__ unsigned char raw[];
+    const uint32_t base = (tc::smem_at(raw) + 1023) & ~1023u;
+    const uint32_t w_at = base, x_at = w_at + F::stages * F::rows_w, inbox = x_at + F::stages * F::rows_x, bars = inbox + F::inbox;
+    const uint32_t full = bars, empty = full + 8 * F::stages, acc_full = empty + 8 * F::stages, slot = acc_full + 8;
+    __shared__ int failed, mine[4];                       // expert (or -1), its first row, how many; where rows of no expert begin
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = tc::cluster_rank();
+    const int unit = blockIdx.x / ranks, tile = unit % tiles, nth = unit / tiles;
+    const long long n0 = tile * 128ll;
+    const int c0 = (int)((long long)rank * a.chunks / ranks), c1 = (int)((long long)(rank + 1) * a.chunks / ranks);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < F::stages; ++s) {
+            tc::bar_init(full + 8 * s, 1);
+            tc::bar_init(empty + 8 * s, 1);
+        }
+        tc::bar_init(acc_full, 1);
+        tc::bar_init_done();
+        failed = 0;
+        tc::prefetch_map(&w_map);
+        tc::prefetch_map(&part_map);
+    }
+    constexpr uint32_t columns = N <= 32 ? 32 : 64;
+    if (warp == 2) tc::tmem_alloc<1>(slot, columns);
+    if (warp == 3) experts_nth(a.ends, a.experts, a.rows, nth, mine);
+    tc::fence_before();
+    __syncthreads();
+    const int expert = mine[0], row0 = mine[1], count = mine[2];
+    if (expert < 0 && nth > 0) {                          // there are not so many: the whole cluster ends
+        tc::before_is_over();
+        if (warp == 2) {
+            uint32_t tmem;
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+            tc::tmem_free<1>(tmem, columns);
+        }
+        return;
+    }
+    tc::cluster_started();                                // waited for before the first store to another CTA
+    tc::fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+
+    auto waited = [&](uint32_t bar, uint32_t parity) {
+        if (tc::bar_wait(bar, parity)) return true;
+        *(volatile int*)&failed = 1;
+        return false;
+    };
+
+    const int boxes = (count + kPart - 1) / kPart;        // of the tokens; none where nobody has rows
+    if (warp == 0) {
+        if (tc::elect()) {
+            constexpr int elements = K == kWhole ? kChunkBytes : kChunkBytes / 2;
+            const int m0 = (int)n0, chunks = boxes ? c1 - c0 : 0, ahead = min(F::stages, chunks);
+            for (int it = 0; it < ahead; ++it) {
+                tc::bar_expect(full + 8 * it, F::rows_w + boxes * kPart * kChunkBytes);
+                tc::load_3d(w_at + it * F::rows_w, &w_map, (c0 + it) * elements, m0, expert, full + 8 * it);
+            }
+            tc::before_is_over();
+            int it = 0;
+            for (; it < chunks; ++it) {
+                const int s = it % F::stages;
+                const uint32_t bar = full + 8 * s;
+                if (it >= ahead) {
+                    if (!waited(empty + 8 * s, (it / F::stages & 1) ^ 1)) break;
+                    tc::bar_expect(bar, F::rows_w + boxes * kPart * kChunkBytes);
+                    tc::load_3d(w_at + s * F::rows_w, &w_map, (c0 + it) * elements, m0, expert, bar);
+                }
+                for (int i = 0; i < boxes; ++i) tc::load_2d(x_at + s * F::rows_x + i * kPart * kChunkBytes, &part_map, (c0 + it) * elements, row0 + i * kPart, bar);
+            }
+            if (*(volatile int*)&failed)                  // copies still in flight
+                for (int i = it < F::stages ? 0 : it - F::stages; i < it; ++i) tc::bar_wait(full + 8 * (i % F::stages), i / F::stages & 1);
+        }
+    } else if (warp == 1) {
+        if (tc::elect()) {
+            const uint32_t what = a.what | (uint32_t)(boxes * kPart >> 3) << 17 | (uint32_t)(128 >> 4) << 24;
+            const int chunks = boxes ? c1 - c0 : 0;
+            for (int it = 0; it < chunks; ++it) {
+                const int s = it % F::stages, steps = c0 + it + 1 < a.chunks ? 4 : a.last_steps;
+                if (!waited(full + 8 * s, it / F::stages & 1)) break;
+                tc::fence_after();
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < steps) {
+                        const uint64_t wo = tc::operand(w_at + s * F::rows_w + j * 32, 16, 1024), xo = tc::operand(x_at + s * F::rows_x + j * 32, 16, 1024);
+                        if (K == kWhole) tc::mma_i8<1>(tmem, wo, xo, what, it > 0 || j > 0);
+                        else tc::mma_f16<1>(tmem, wo, xo, what, it > 0 || j > 0);
+                    }
+                tc::mma_commit<1>(empty + 8 * s);
+            }
+            tc::mma_commit<1>(acc_full);                  // also after a wait that ran out: nothing may be in flight when the memory goes
+            tc::bar_wait(acc_full, 0);
+        }
+    }
+    __syncwarp();
+    tc::before_is_over();
+    tc::cluster_wait();                                   // the CTAs that the sums go to run
+    const int quad = warp - 4, row = quad * 32 + lane, each = N / ranks;      // a thread has one row of weights; this CTA finishes `each` tokens
+    const long long ch = n0 + row, at = expert * a.n + ch;
+    bool ok = true;
+    if (warp >= 4) {
+        ok = waited(acc_full, 0);
+        tc::fence_after();
+        if (ok) {
+#pragma unroll 1
+            for (int j = 0; j < boxes * kPart; j += 16) {
+                uint32_t v[16];
+                tc::tmem_load16(tmem + j + ((uint32_t)quad * 32 << 16), v);
+                tc::tmem_wait_load();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int col = j + i, to = col / each;
+                    asm volatile("st.shared::cluster.b32 [%0], %1;" :: "r"(tc::in_cta(inbox + (((rank * each) + col % each) * 128 + row) * 4, to)), "r"(v[i]) : "memory");
+                }
+            }
+        }
+    }
+    tc::fence_before();
+    __syncthreads();
+    tc::cluster_sync();                                   // every slice is where it belongs
+    if (warp >= 4 && ok && ch < a.n) {
+        const float b = a.bias && expert >= 0 ? mx_float(((const O*)a.bias)[at]) : 0.f, w_scale = K == kWhole && expert >= 0 ? a.w_scales[at] : 0.f;
+        O* const y = (O*)a.y + ch;
+        for (int j = 0; j < each; ++j) {
+            const int col = rank * each + j;
+            if (col >= count) break;
+            uint32_t sum = 0;
+            for (int r = 0; r < ranks; ++r) {
+                uint32_t v;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(inbox + ((r * each + j) * 128 + row) * 4));
+                sum = r == 0 ? v : K == kWhole ? sum + v : __float_as_uint(__uint_as_float(sum) + __uint_as_float(v));
+            }
+            y[(row0 + col) * a.stride] = mx_round<O>(number<K>(sum, K == kWhole ? a.x_scales[row0 + col] : 0.f, w_scale, b));
+        }
+        if (nth == 0)                                     // rows of no expert
+            for (long long r = mine[3] + (int)rank; r < a.rows; r += ranks) y[r * a.stride] = mx_zero<O>();
+    }
+    if (threadIdx.x == 0 && failed) atomicAdd_system(a.timeouts, 1u);
+    if (warp == 2) tc::tmem_free<1>(tmem, columns);
+}
+
 size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 int smem_of(int experts) { return 1024 + kStages * kStageBytes + kOutBytes + 256 + 8 * (experts + 1); }
 
@@ -261,16 +425,61 @@ AlignPlan align_plan(int64_t rows, int64_t x_cols, const void* x, int64_t x_stri
     return p;
 }
 
-template <int K, typename O>
-cudaError_t launch(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap& xm, const CUtensorMap& pm, const ProductArgs& a, cudaStream_t st)
+// in_front: a kernel that these may start beside has just been launched
+void configure(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* attr, unsigned grid, unsigned threads, int smem, unsigned cluster, bool in_front, cudaStream_t st)
 {
+    cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    if (cluster) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        attr[cfg.numAttrs].val.clusterDim.x = cluster;
+        attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+        ++cfg.numAttrs;
+    }
+    if (in_front) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+        ++cfg.numAttrs;
+    }
+}
+
+template <int K, typename O, int N>
+cudaError_t launch_few(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap& pm, const ProductArgs& a, bool in_front, cudaStream_t st)
+{
+    cudaError_t e = cudaFuncSetAttribute(expert_few_kernel<K, O, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, Few<N>::smem);
+    if (e != cudaSuccess) return e;
+    const int tiles = (int)((a.n + 127) / 128);
+    const long long units = tiles * (long long)(a.rows < a.experts ? a.rows : a.experts);
+    int ranks = 1;                                        // two CTAs an SM at most, two chunks a CTA at least
+    while (ranks < 8 && units * ranks <= ctx->num_sms && a.chunks >= ranks * 4) ranks *= 2;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    configure(cfg, attr, (unsigned)(units * ranks), kFewThreads, Few<N>::smem, (unsigned)ranks, in_front, st);
+    return cudaLaunchKernelEx(&cfg, expert_few_kernel<K, O, N>, wm, pm, a, tiles, ranks);
+}
+
+template <int K, typename O>
+cudaError_t launch(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap& xm, const CUtensorMap& pm, ProductArgs& a, bool in_front, cudaStream_t st)
+{
+    if constexpr (K != kInputGrad) {
+        if (a.rows <= 16) return launch_few<K, O, 16>(ctx, wm, pm, a, in_front, st);
+        if (a.rows <= 32) return launch_few<K, O, 32>(ctx, wm, pm, a, in_front, st);
+        if (a.rows <= kFewRows) return launch_few<K, O, 64>(ctx, wm, pm, a, in_front, st);
+    }
     const int smem = smem_of(a.experts);
     const cudaError_t e = cudaFuncSetAttribute(expert_product_kernel<K, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kExpertsMost));
     if (e != cudaSuccess) return e;
+    a.what |= (uint32_t)(kTile >> 4) << 24;
     const long long most = (a.rows / kTile + (a.rows < a.experts ? a.rows : a.experts)) * a.tiles_m;      // units, whatever the ends say
     const int pairs = (int)(most < ctx->num_sms / 2 ? most : ctx->num_sms / 2);
-    expert_product_kernel<K, O><<<pairs * 2, kThreads, smem, st>>>(wm, xm, pm, a);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[1];
+    configure(cfg, attr, (unsigned)pairs * 2, kThreads, smem, 0, in_front, st);
+    return cudaLaunchKernelEx(&cfg, expert_product_kernel<K, O>, wm, xm, pm, a);
 }
 
 bool units_fit(int64_t rows, int64_t experts, int64_t n) { return (rows / kTile + experts) * ((n + kTile - 1) / kTile) < (int64_t)1 << 31; }
@@ -321,11 +530,11 @@ int product16(galv_ctx* ctx, const char* name, bool across, int64_t rows, int32_
     a.rows = rows; a.n = n; a.stride = y_stride; a.experts = experts; a.tiles_m = (int)((n + kTile - 1) / kTile);
     a.chunks = (int)((k + 63) / 64); a.last_steps = (int)((k - (a.chunks - 1) * 64ll + 15) / 16);
     const uint32_t t = dtype == GALV_BF16 ? 1u : 0u;      // fp32 sums, both operands of this type, the weights' summed index along or across their rows
-    a.what = 1u << 4 | t << 7 | t << 10 | (across ? 1u << 15 : 0u) | (uint32_t)(kTile >> 4) << 24;
+    a.what = 1u << 4 | t << 7 | t << 10 | (across ? 1u << 15 : 0u);
     a.ends = ends; a.x_scales = a.w_scales = nullptr; a.bias = bias; a.y = y; a.timeouts = ctx->mx_timeouts_at;
     a.vec = n % 8 == 0 && y_stride % 8 == 0 && mx_aligned(y, 16);
-    if (dtype == GALV_BF16) e = across ? launch<kInputGrad, __nv_bfloat16>(ctx, wm, xm, pm, a, st) : launch<kForward, __nv_bfloat16>(ctx, wm, xm, pm, a, st);
-    else e = across ? launch<kInputGrad, __half>(ctx, wm, xm, pm, a, st) : launch<kForward, __half>(ctx, wm, xm, pm, a, st);
+    if (dtype == GALV_BF16) e = across ? launch<kInputGrad, __nv_bfloat16>(ctx, wm, xm, pm, a, false, st) : launch<kForward, __nv_bfloat16>(ctx, wm, xm, pm, a, false, st);
+    else e = across ? launch<kInputGrad, __half>(ctx, wm, xm, pm, a, false, st) : launch<kForward, __half>(ctx, wm, xm, pm, a, false, st);
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
 
@@ -341,7 +550,7 @@ bool whole_pointers_ok(int64_t n, const int32_t* ends, const int8_t* w_codes, co
 }
 
 int whole_launch(galv_ctx* ctx, const char* name, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const int8_t* x_codes, const float* x_scales,
-                 const int8_t* w_codes, const float* w_scales, const void* bias, void* y, int64_t y_stride, int32_t dtype, cudaStream_t st)
+                 const int8_t* w_codes, const float* w_scales, const void* bias, void* y, int64_t y_stride, int32_t dtype, bool in_front, cudaStream_t st)
 {
     const int64_t pitch = i8_pitch(k);
     CUtensorMap wm, xm, pm;
@@ -356,11 +565,11 @@ int whole_launch(galv_ctx* ctx, const char* name, int64_t rows, int32_t experts,
     ProductArgs a;
     a.rows = rows; a.n = n; a.stride = y_stride; a.experts = experts; a.tiles_m = (int)((n + kTile - 1) / kTile);
     a.chunks = (int)((pitch + kChunkBytes - 1) / kChunkBytes); a.last_steps = (int)((pitch - (a.chunks - 1) * (int64_t)kChunkBytes + 31) / 32);
-    a.what = 2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(kTile >> 4) << 24;      // 32-bit whole sums of signed 8-bit operands
+    a.what = 2u << 4 | 1u << 7 | 1u << 10;      // 32-bit whole sums of signed 8-bit operands
     a.ends = ends; a.x_scales = x_scales; a.w_scales = w_scales; a.bias = bias; a.y = y; a.timeouts = ctx->mx_timeouts_at;
     const int per = 16 / mx_size_of(dtype);
     a.vec = n % per == 0 && y_stride % per == 0 && mx_aligned(y, 16);
-    MX_DISPATCH_TYPE(dtype, e = (launch<kWhole, T>(ctx, wm, xm, pm, a, st)));
+    MX_DISPATCH_TYPE(dtype, e = (launch<kWhole, T>(ctx, wm, xm, pm, a, in_front, st)));
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
 
@@ -406,7 +615,7 @@ extern "C" int galv_i8_matmul(galv_ctx* ctx, int64_t rows, int32_t experts, int6
     if (may != GALV_OK) return may;
     MxDevice dev(ctx);
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
-    return whole_launch(ctx, "galv_i8_matmul", rows, experts, n, k, ends, x_codes, x_scales, w_codes, w_scales, bias, y, y_stride, dtype, (cudaStream_t)stream);
+    return whole_launch(ctx, "galv_i8_matmul", rows, experts, n, k, ends, x_codes, x_scales, w_codes, w_scales, bias, y, y_stride, dtype, false, (cudaStream_t)stream);
 }
 
 extern "C" size_t galv_i8_linear_workspace_bytes(int64_t rows, int64_t k) { return mx_size_ok(rows, k) ? up((size_t)rows * i8_pitch(k)) + up((size_t)rows * 4) : 0; }
@@ -429,5 +638,5 @@ extern "C" int galv_i8_linear(galv_ctx* ctx, int64_t rows, int32_t experts, int6
     float* const scales = (float*)(codes + up((size_t)rows * i8_pitch(k)));
     const cudaError_t e = galv_i8_pack_launch(ctx->num_sms, rows, k, x, x_stride, dtype, codes, scales, (cudaStream_t)stream);
     if (e != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
-    return whole_launch(ctx, "galv_i8_linear", rows, experts, n, k, ends, codes, scales, w_codes, w_scales, bias, y, y_stride, dtype, (cudaStream_t)stream);
+    return whole_launch(ctx, "galv_i8_linear", rows, experts, n, k, ends, codes, scales, w_codes, w_scales, bias, y, y_stride, dtype, true, (cudaStream_t)stream);
 }

@@ -6,6 +6,7 @@
 // Bound by memory, what is read and written once, 3 bytes an element from 16 bits.
 
 #include "galv_i8.cuh"
+#include "galv_tc.cuh"
 
 namespace {
 
@@ -48,6 +49,7 @@ __global__ void __launch_bounds__(256) i8_pack_kernel(long long rows, int cols, 
     __shared__ uint32_t found[2][8];
     const int t = threadIdx.x % threads, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     int turn = 0;
+    tc::next_may_start();                                 // the product that reads the codes waits for this kernel's end itself
     for (long long row0 = (long long)blockIdx.x * (8 / WARPS); row0 < rows; row0 += (long long)gridDim.x * (8 / WARPS), turn ^= 1) {
         const long long row = row0 + warp / WARPS;
         const bool in = row < rows;

@@ -256,7 +256,7 @@ mx_wgrad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constan
                         tc::fence_after();
 #pragma unroll
                         for (int j = 0; j < kTokens / 16; ++j)
-                            tc::mma_f16(d, tc::operand(dy_at + s * kDyBytes + j * 2048, 8192, 1024), tc::operand(x_at + x * kXBytes + j * 2048, 8192, 1024), what, add || j > 0);
+                            tc::mma_f16<2>(d, tc::operand(dy_at + s * kDyBytes + j * 2048, 8192, 1024), tc::operand(x_at + x * kXBytes + j * 2048, 8192, 1024), what, add || j > 0);
                         tc::mma_commit<2>(dy_empty + 8 * s);
                         tc::mma_commit<2>(x_empty + 8 * x);
                     }

@@ -29,7 +29,7 @@ def _count(experts: int):
 
 def _whole(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
     """As it lies in memory, without gaps."""
-    return None if t is None else t.detach().resolve_neg().contiguous()
+    return t if t is None or (t.is_contiguous() and not t.is_neg()) else t.detach().resolve_neg().contiguous()
 
 
 def _weight(weight: torch.Tensor, dtype: torch.dtype):
@@ -58,7 +58,7 @@ def _products(x: torch.Tensor, weight: i8.Packed, ends: torch.Tensor, bias, dtyp
         g.galv_i8_matmul(experts, cols, ends, x.codes, x.scales, weight.codes, weight.scales, bias, y)
     else:
         y = torch.empty(x.shape[0], n, dtype=dtype, device=x.device)
-        g.galv_i8_linear(experts, ends, x, weight.codes, weight.scales, bias, y, _bytes(g.galv_i8_linear_workspace_bytes(*x.shape), x.device))
+        g.galv_i8_linear(experts, ends, x, weight.codes, weight.scales, bias, y, _bytes(i8._room(*x.shape), x.device))
     return y
 
 
@@ -79,12 +79,12 @@ def matmul(x: Union[torch.Tensor, i8.Packed], weight: Union[torch.Tensor, i8.Pac
         raise ValueError(f"y is of x's type {x.dtype}, not {dtype}")
     if isinstance(weight, i8.Packed):
         _kind(x.dtype, "x")
-        return _products(_rows(x.detach(), "x"), weight, ends, bias, x.dtype)
+        return _products(_rows(x, "x"), weight, ends, bias, x.dtype)
     _kind(x.dtype, "x", _SHORT)
     _weight(weight, x.dtype)
     experts, n, k = weight.shape
     _ends(ends, experts)
-    x = _rows(x.detach(), "x")
+    x = _rows(x, "x")
     if x.shape[1] != k:
         raise ValueError(f"x of shape {tuple(x.shape)} beside weights of {k} columns")
     i8._bias(bias, (experts, n), x.dtype)
@@ -102,7 +102,7 @@ def input_grad(dy: torch.Tensor, weight: torch.Tensor, ends: torch.Tensor) -> to
     _weight(weight, dy.dtype)
     experts, n, k = weight.shape
     _ends(ends, experts)
-    dy = _rows(dy.detach(), "dy")
+    dy = _rows(dy, "dy")
     if dy.shape[1] != n:
         raise ValueError(f"dy of shape {tuple(dy.shape)} beside weights of {n} rows")
     g = _on(dy.device, weight.device, ends.device)
@@ -122,7 +122,7 @@ def weight_grad(dy: torch.Tensor, x: torch.Tensor, ends: torch.Tensor, dtype: Op
     experts = ends.shape[0]
     _ends(ends, experts)
     _count(experts)
-    dy, x = _rows(dy.detach(), "dy"), _rows(x.detach(), "x")
+    dy, x = _rows(dy, "dy"), _rows(x, "x")
     if x.dtype != dy.dtype or x.shape[0] != dy.shape[0] or x.shape[1] < 1 or dy.shape[1] < 1:
         raise ValueError(f"dy of shape {tuple(dy.shape)} and {dy.dtype} beside x of {tuple(x.shape)} and {x.dtype}")
     shape = (experts, dy.shape[1], x.shape[1])
@@ -147,7 +147,7 @@ def bias_grad(dy: torch.Tensor, ends: torch.Tensor, dtype: Optional[torch.dtype]
         raise ValueError(f"ends is [experts] of int32, not {tuple(ends.shape)} of {ends.dtype}")
     _ends(ends, ends.shape[0])
     _count(ends.shape[0])
-    dy = _rows(dy.detach(), "dy")
+    dy = _rows(dy, "dy")
     dtype = dtype or dy.dtype
     if dy.shape[1] < 1 or (dtype != dy.dtype and dtype != torch.float32):
         raise ValueError(f"sums of dy of shape {tuple(dy.shape)} in {dy.dtype} or float32, not {dtype}")
@@ -162,7 +162,9 @@ class _Linear(torch.autograd.Function):
     @_as_typed
     def forward(ctx, x, weight, ends, bias):
         y = matmul(x, weight, ends, bias)
-        ctx.save_for_backward(x if ctx.needs_input_grad[1] else None, weight if ctx.needs_input_grad[0] else None, ends)
+        need = ctx.needs_input_grad
+        ctx.save_for_backward(x if need[1] else None, weight if need[0] else None, ends)
+        ctx.shape = weight.shape
         return y
 
     @staticmethod
@@ -170,9 +172,14 @@ class _Linear(torch.autograd.Function):
     @_as_typed
     def backward(ctx, dy):
         x, weight, ends = ctx.saved_tensors
-        dx = input_grad(dy, weight, ends) if ctx.needs_input_grad[0] else None
-        dw = weight_grad(dy, x, ends) if ctx.needs_input_grad[1] else None
-        db = bias_grad(dy, ends) if ctx.needs_input_grad[3] else None
+        need_x, need_w, _, need_b = ctx.needs_input_grad
+        experts, n, k = ctx.shape
+        dy, dtype, device = _rows(dy, "dy"), dy.dtype, dy.device
+        dx = torch.empty(dy.shape[0], k, dtype=dtype, device=device) if need_x else None
+        dw = torch.empty(ctx.shape, dtype=dtype, device=device) if need_w else None
+        db = torch.empty(experts, n, dtype=dtype, device=device) if need_b else None
+        _on(device).galv_expert_backward(ctx.shape, _whole(ends), dy, _rows(x, "x") if need_w else None, _whole(weight) if need_x else None, dx, dw, db,
+                                         lambda size: _bytes(size, device))
         return dx, dw, None, db
 
 

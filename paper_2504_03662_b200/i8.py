@@ -61,6 +61,11 @@ def unpack(p: Packed, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     return x
 
 
+def _room(rows: int, cols: int) -> int:
+    """Bytes of workspace in which a product puts its input into 8-bit integers: codes, then scales, each in whole pieces of 256."""
+    return (rows * pitch(cols) + 255 & ~255) + (rows * 4 + 255 & ~255)
+
+
 def _beside(cols: int, b: Packed):
     if cols != b.cols or b.rows < 1:
         raise ValueError(f"a product of {cols} columns and [{b.rows}][{b.cols}] transposed")
@@ -86,13 +91,16 @@ def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, bias: Opti
 
 def linear(x: torch.Tensor, weight: Packed, bias: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x weight^T + bias over the last axis of x, put into 8-bit integers in the call, with weights held so; in x's type.  Without gradients."""
-    _kind(x.dtype, "x")
-    if x.dim() < 1 or x.shape[-1] < 1:
-        raise ValueError(f"x has a last axis of one number or more, not the shape {tuple(x.shape)}")
-    _beside(x.shape[-1], weight)
-    _bias(bias, (weight.rows,), x.dtype)
-    g = _on(x.device, weight.device, _device(bias))
-    flat = _rows(x.detach().reshape(-1, x.shape[-1]), "x")
-    y = torch.empty(flat.shape[0], weight.rows, dtype=x.dtype, device=x.device)
-    g.galv_i8_linear(1, None, flat, weight.codes, weight.scales, _vector(bias), y, _bytes(g.galv_i8_linear_workspace_bytes(*flat.shape), x.device))
-    return y.view(*x.shape[:-1], weight.rows)
+    dtype, shape = x.dtype, x.shape
+    _kind(dtype, "x")
+    if len(shape) < 1 or shape[-1] < 1:
+        raise ValueError(f"x has a last axis of one number or more, not the shape {tuple(shape)}")
+    _beside(shape[-1], weight)
+    _bias(bias, (weight.rows,), dtype)
+    device = x.device
+    g = _on(device, weight.device, _device(bias))
+    flat = _rows(x if len(shape) == 2 else x.reshape(-1, shape[-1]), "x")
+    rows, cols = flat.shape
+    y = torch.empty(rows, weight.rows, dtype=dtype, device=device)
+    g.galv_i8_linear(1, None, flat, weight.codes, weight.scales, _vector(bias), y, _bytes(_room(rows, cols), device))
+    return y if len(shape) == 2 else y.view(*shape[:-1], weight.rows)
