@@ -214,6 +214,11 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
         int done = 0;
         uint32_t phase = 0;
         bool ok = true, fetched = false;
+        auto release = [&](uint32_t acc) {                 // it may be summed into again
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_empty + 8 * acc, 0));
+        };
         for (int u = first; u < units && ok; u += stride) {
             const Unit w = unit_of(a, begin, u);
             const long long r0 = (long long)w.tn * kTile + rank * kHalf + quad * 32, c0 = (long long)w.tk * kTile + half * 128;
@@ -246,9 +251,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
                         for (int i = 0; i < 16; ++i) sum[j + i] += __uint_as_float(v[i]);
                     }
                     if (left > kSegment * kTokens) {      // this accumulator may be summed into again
-                        tc::fence_before();
-                        __syncwarp();
-                        if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_empty + 8 * acc, 0));
+                        release(acc);
                         ++done;
                     }
                 }
@@ -268,6 +271,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
 #pragma unroll
                             for (int i = 0; i < piece; i += 32) tc::tmem_load32(from + acc * kTile + c + i, v + i);
                             tc::tmem_wait_load();
+                            if (c + piece >= cols) release(acc);
                         } else {
 #pragma unroll
                             for (int i = 0; i < piece; ++i) v[i] = 0;
@@ -302,9 +306,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
             }
             if (!ok) break;
             if (w.count > 0) {
-                tc::fence_before();
-                __syncwarp();
-                if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(acc_empty + 8 * acc, 0));
+                if (!a.boxes || !some) release(acc);
                 ++done;
             }
         }
