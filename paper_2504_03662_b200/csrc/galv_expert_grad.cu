@@ -127,7 +127,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
         }
     }
     if (warp == 2) tc::tmem_alloc<2>(slot, 512);
-    if (warp == 0) experts_scan(a.ends, a.experts, a.rows, begin, begin + a.experts + 1);
+    if (warp == 0) experts_begin(a.ends, a.experts, a.rows, begin);
     tc::fence_before();
     __syncthreads();
     tc::cluster_sync();                                   // the pair's barriers exist
@@ -352,7 +352,7 @@ expert_bias_grad_kernel(long long rows, int experts, long long n, const int32_t*
     __shared__ float part[8][kBiasColumns], sums[kBiasCtas][kBiasColumns];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = tc::cluster_rank();
-    if (warp == 0) experts_scan(ends, experts, rows, begin, begin + experts + 1);
+    if (warp == 0) experts_begin(ends, experts, rows, begin);
     tc::cluster_sync();                                   // the first CTA runs, sums can be sent to it
     const long long blocks = (n + kBiasColumns - 1) / kBiasColumns, all = blocks * experts;
     for (long long b = blockIdx.x / kBiasCtas; b < all; b += gridDim.x / kBiasCtas) {
@@ -385,7 +385,7 @@ expert_bias_grad_kernel(long long rows, int experts, long long n, const int32_t*
 }
 
 size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
-int smem_of(int experts) { return 1024 + kStages * kStageBytes + kOutBytes + 256 + 8 * (experts + 1); }
+int smem_of(int experts) { return 1024 + kStages * kStageBytes + kOutBytes + 256 + 4 * (experts + 1); }
 
 struct GradPlan { size_t dy, x, total; };
 GradPlan plan_of(int64_t rows, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride)
@@ -494,7 +494,7 @@ extern "C" int galv_expert_bias_grad(galv_ctx* ctx, int64_t rows, int32_t expert
     MxDevice dev(ctx);
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
     const int64_t clusters = (n + kBiasColumns - 1) / kBiasColumns * experts, most = ctx->num_sms;
-    const int grid = (int)(clusters < most ? clusters : most) * kBiasCtas, smem = 8 * (experts + 1);
+    const int grid = (int)(clusters < most ? clusters : most) * kBiasCtas, smem = 4 * (experts + 1);
     const int vec = n % 4 == 0 && dy_stride % 4 == 0 && mx_aligned(dy, 8);
     cudaStream_t st = (cudaStream_t)stream;
     using B = __nv_bfloat16;

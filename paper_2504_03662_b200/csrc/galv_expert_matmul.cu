@@ -5,8 +5,8 @@
 // fills the card walks through them.  The weights' rows take the tensor cores' 256 rows of a pair of CTAs, the tokens their columns, as many as an expert's last
 // tile has (a multiple of 32): what ragged sizes waste is less than 32 tokens an expert, and a few tokens cost little more than reading the weights.
 // A column of sums depends on its own token alone: a tile's copy of tokens may run into the next expert's, whose sums nobody takes, whatever they are.
-// Per CTA: a thread that starts bulk tensor copies (128 bytes of the summed index a chunk: 128 rows of weights, half of the tile's tokens), one that issues
-// the matrix instructions for the pair, eight warps that move sums from the tensor memory to y while the next are made (two accumulators fill it).
+// Per CTA: a thread that starts bulk tensor copies (128 bytes of the summed index a chunk: 128 rows of weights, half of the tile's tokens; both CTAs' tell the
+// first one's barrier), one (in the first) that issues the matrix instructions for the pair, eight warps that move sums from the tensor memory to y while the next are made (two accumulators fill it).
 
 #include <stdio.h>
 
@@ -21,8 +21,11 @@ enum Kind { kForward, kInputGrad, kWhole };               // 16 bits, summed alo
 constexpr int kStages = 6, kTile = 256, kHalf = kTile / 2, kChunkBytes = 128;
 constexpr int kRowsBytes = kHalf * kChunkBytes, kStageBytes = 2 * kRowsBytes;
 constexpr int kOutBytes = 8 * 2048;
-constexpr int kPart = 16;                                 // tokens of a copy where the tile is not full
+constexpr int kBox = 64, kPart = 16;                      // tokens of a copy, and of one where fewer are left
 constexpr int kThreads = 384;
+// What a chunk costs besides its tokens, in tokens.  Measured at 256, 160, 128 and 64 tokens of every tile (2048 x 8192): 411, 320, 285 and 258 ns in 16 bits, 437, 337, 305 and 282
+// in 8-bit integers; of the input gradient, whose weights come in twice as many copies, 450, 360, 330 and 326.
+constexpr float kFixed[3] = {260.f, 440.f, 260.f};
 constexpr int kGroup = 16;                                // tiles of tokens that stay in L2 while their tiles of weights run
 
 struct ProductArgs {
@@ -42,17 +45,23 @@ struct ProductArgs {
 struct Walk {
     const int* begin;
     const int* before;
-    int tiles_m, expert = 0;
+    int tiles_m, expert = -1, from = 0, all = 0, each = 0;      // the expert's first tile of tokens, how many it has and of how many rows
     int tm, row0, count;                                  // tile of weights' rows; first token and number of tokens
     __device__ __forceinline__ Walk(const int* begin_, const int* before_, int tiles_m_) : begin(begin_), before(before_), tiles_m(tiles_m_) {}
     __device__ __forceinline__ void to(int u)             // units in rising order
     {
-        while (u >= before[expert + 1] * tiles_m) ++expert;
-        const int from = before[expert], all = before[expert + 1] - from, local = u - from * tiles_m;
-        const int per = kGroup * tiles_m, first = local / per * kGroup, size = min(kGroup, all - first), in = local % per;
-        row0 = begin[expert] + (first + in % size) * kTile;
+        if (u >= (from + all) * tiles_m) {
+            do {
+                ++expert;
+                from += all;
+                all = before[expert + 1] - from;
+            } while (u >= (from + all) * tiles_m);
+            each = experts_tile(begin[expert + 1] - begin[expert], all);
+        }
+        const int local = u - from * tiles_m, per = kGroup * tiles_m, first = local / per * kGroup, size = min(kGroup, all - first), in = local % per;
+        row0 = begin[expert] + (first + in % size) * each;
         tm = in / size;
-        count = min(kTile, begin[expert + 1] - row0);
+        count = min(each, begin[expert + 1] - row0);
     }
     __device__ __forceinline__ int columns() const { return (count + 31) & ~31; }
 };
@@ -73,11 +82,12 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
     extern __shared__ unsigned char raw[];
     const uint32_t base = (tc::smem_at(raw) + 1023) & ~1023u;
     const uint32_t w_at = base, x_at = w_at + kStages * kRowsBytes, out_at = x_at + kStages * kRowsBytes, bars = out_at + kOutBytes;
-    const uint32_t full = bars, other = full + 8 * kStages, empty = other + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16, drain = acc_empty + 16,
+    const uint32_t full = bars, empty = full + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16, drain = acc_empty + 16,
                    slot = drain + 8;
     int* const begin = reinterpret_cast<int*>(raw + (bars + 256 - tc::smem_at(raw)));
     int* const before = begin + a.experts + 1;
     __shared__ int failed;
+    __shared__ float prices[8];
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = tc::cluster_rank();
@@ -86,7 +96,6 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
             tc::bar_init(full + 8 * s, 1);
-            tc::bar_init(other + 8 * s, 1);
             tc::bar_init(empty + 8 * s, 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -101,7 +110,19 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
         tc::prefetch_map(&part_map);
     }
     if (warp == 2) tc::tmem_alloc<2>(slot, 512);
-    if (warp == 3) experts_scan(a.ends, a.experts, a.rows, begin, before);
+    if (warp == 3) experts_begin(a.ends, a.experts, a.rows, begin);
+    __syncthreads();
+    if (warp >= 4) {                                      // a size of tiles each: 256, 224 .. 32 rows
+        const float price = experts_price(begin, a.experts, kTile - (warp - 4) * 32, a.tiles_m, stride, kFixed[K]);
+        if (lane == 0) prices[warp - 4] = price;
+    }
+    __syncthreads();
+    if (warp == 3) {                                      // the cheapest, of equals the largest
+        int best = 0;
+        for (int i = 1; i < 8; ++i)
+            if (prices[i] < prices[best]) best = i;
+        experts_before(begin, a.experts, kTile - best * 32, before);
+    }
     tc::fence_before();
     __syncthreads();
     tc::cluster_sync();                                   // the pair's barriers exist
@@ -111,7 +132,7 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
     const int units = before[a.experts] * a.tiles_m;
 
     auto waited = [&](uint32_t bar, uint32_t parity) {
-        if (tc::bar_wait(bar, parity)) return true;
+        if (tc::bar_wait_own(bar, parity)) return true;
         *(volatile int*)&failed = 1;
         return false;
     };
@@ -128,34 +149,23 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
                 const int m0 = w.tm * kTile + rank * kHalf, half = w.columns() / 2, r0 = w.row0 + rank * half;
                 for (int c = 0; c < a.chunks; ++c, ++it) {
                     const int s = it % kStages;
-                    const uint32_t bar = full + 8 * s;
+                    const uint32_t bar = tc::in_cta(full + 8 * s, 0), ws = w_at + s * kRowsBytes, xs = x_at + s * kRowsBytes;
                     if (!(ok = waited(empty + 8 * s, (it / kStages & 1) ^ 1))) break;
-                    tc::bar_expect(bar, kRowsBytes + half * kChunkBytes);
+                    if (rank == 0) tc::bar_expect(full + 8 * s, 2 * (kRowsBytes + half * kChunkBytes));      // of both CTAs
                     if (K == kInputGrad) {                // 64 rows of weights, 64 columns a copy
-                        tc::load_3d(w_at + s * kRowsBytes, &w_map, m0, c * elements, w.expert, bar);
-                        tc::load_3d(w_at + s * kRowsBytes + kRowsBytes / 2, &w_map, m0 + 64, c * elements, w.expert, bar);
+                        tc::load_3d_pair(ws, &w_map, m0, c * elements, w.expert, bar);
+                        tc::load_3d_pair(ws + kRowsBytes / 2, &w_map, m0 + 64, c * elements, w.expert, bar);
                     } else {
-                        tc::load_3d(w_at + s * kRowsBytes, &w_map, c * elements, m0, w.expert, bar);
+                        tc::load_3d_pair(ws, &w_map, c * elements, m0, w.expert, bar);
                     }
-                    if (half == kHalf) tc::load_2d(x_at + s * kRowsBytes, &x_map, c * elements, r0, bar);
-                    else
-                        for (int i = 0; i < half; i += kPart) tc::load_2d(x_at + s * kRowsBytes + i * kChunkBytes, &part_map, c * elements, r0 + i, bar);
+                    int i = 0;
+                    for (; i + kBox <= half; i += kBox) tc::load_2d_pair(xs + i * kChunkBytes, &x_map, c * elements, r0 + i, bar);
+                    for (; i < half; i += kPart) tc::load_2d_pair(xs + i * kChunkBytes, &part_map, c * elements, r0 + i, bar);
                 }
             }
-            if (*(volatile int*)&failed)                  // copies still in flight
-                for (int i = it < kStages ? 0 : it - kStages; i < it; ++i) tc::bar_wait(full + 8 * (i % kStages), i / kStages & 1);
+            if (*(volatile int*)&failed) tc::settle();
         }
-    } else if (warp == 1 && rank == 1) {                  // tells the first CTA that this one's rows are there
-        if (tc::elect()) {
-            int it = 0;
-            bool ok = true;
-            for (int u = first; u < units && ok; u += stride)
-                for (int c = 0; c < a.chunks; ++c, ++it) {
-                    if (!(ok = waited(full + 8 * (it % kStages), it / kStages & 1))) break;
-                    tc::bar_arrive_cluster(tc::in_cta(other + 8 * (it % kStages), 0));
-                }
-        }
-    } else if (warp == 1) {
+    } else if (warp == 1 && rank == 0) {
         if (tc::elect()) {
             int it = 0, done = 0;
             bool ok = true;
@@ -166,7 +176,7 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
                 tc::fence_after();
                 for (int c = 0; c < a.chunks; ++c, ++it) {
                     const int s = it % kStages, steps = c + 1 < a.chunks ? 4 : a.last_steps;
-                    if (!(ok = waited(full + 8 * s, it / kStages & 1) && waited(other + 8 * s, it / kStages & 1))) break;
+                    if (!(ok = waited(full + 8 * s, it / kStages & 1))) break;
                     tc::fence_after();
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
@@ -314,7 +324,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_consta
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
 
     auto waited = [&](uint32_t bar, uint32_t parity) {
-        if (tc::bar_wait(bar, parity)) return true;
+        if (tc::bar_wait_own(bar, parity)) return true;
         *(volatile int*)&failed = 1;
         return false;
     };
@@ -474,7 +484,7 @@ cudaError_t launch(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap
     const cudaError_t e = cudaFuncSetAttribute(expert_product_kernel<K, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kExpertsMost));
     if (e != cudaSuccess) return e;
     a.what |= (uint32_t)(kTile >> 4) << 24;
-    const long long most = (a.rows / kTile + (a.rows < a.experts ? a.rows : a.experts)) * a.tiles_m;      // units, whatever the ends say
+    const long long most = (a.rows / 32 + (a.rows < a.experts ? a.rows : a.experts)) * a.tiles_m;      // units, whatever the ends say and their size is
     const int pairs = (int)(most < ctx->num_sms / 2 ? most : ctx->num_sms / 2);
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];
@@ -482,7 +492,7 @@ cudaError_t launch(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap
     return cudaLaunchKernelEx(&cfg, expert_product_kernel<K, O>, wm, xm, pm, a);
 }
 
-bool units_fit(int64_t rows, int64_t experts, int64_t n) { return (rows / kTile + experts) * ((n + kTile - 1) / kTile) < (int64_t)1 << 31; }
+bool units_fit(int64_t rows, int64_t experts, int64_t n) { return (rows / 32 + experts) * ((n + kTile - 1) / kTile) < (int64_t)1 << 31; }
 
 // y = x w^T or x w by expert, both in 16 bits.  across: w [experts][cols of x][n], summed across its rows.
 int product16(galv_ctx* ctx, const char* name, bool across, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* x, int64_t x_stride, const void* w,
@@ -523,7 +533,7 @@ int product16(galv_ctx* ctx, const char* name, bool across, int64_t rows, int32_
     const CUtensorMapDataType type = dtype == GALV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     CUtensorMap wm, xm, pm;
     cudaError_t e = galv_map_3d(&wm, type, w, experts, w_rows, w_cols, w_pitch * 2, across ? 64 : kHalf, 64);
-    if (e == cudaSuccess) e = galv_mx_map(&xm, type, x, rows, k, x_stride * 2, kHalf, 64, true);
+    if (e == cudaSuccess) e = galv_mx_map(&xm, type, x, rows, k, x_stride * 2, kBox, 64, true);
     if (e == cudaSuccess) e = galv_mx_map(&pm, type, x, rows, k, x_stride * 2, kPart, 64, true);
     if (e != cudaSuccess) return wrong(GALV_ERR_CUDA, "tensor map");
     ProductArgs a;
@@ -555,7 +565,7 @@ int whole_launch(galv_ctx* ctx, const char* name, int64_t rows, int32_t experts,
     const int64_t pitch = i8_pitch(k);
     CUtensorMap wm, xm, pm;
     cudaError_t e = galv_map_3d(&wm, CU_TENSOR_MAP_DATA_TYPE_UINT8, w_codes, experts, n, pitch, pitch, kHalf, kChunkBytes);
-    if (e == cudaSuccess) e = galv_mx_map(&xm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, pitch, pitch, kHalf, kChunkBytes, true);
+    if (e == cudaSuccess) e = galv_mx_map(&xm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, pitch, pitch, kBox, kChunkBytes, true);
     if (e == cudaSuccess) e = galv_mx_map(&pm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, pitch, pitch, kPart, kChunkBytes, true);
     if (e != cudaSuccess) {
         char text[100];

@@ -3,14 +3,14 @@
 
 #include "galv_mx.cuh"
 
-constexpr int kExpertsMost = 1024, kTileRows = 256;
+constexpr int kExpertsMost = 1024;
 
-// In shared memory, by one warp: begin[e] is expert e's first row and before[e] how many tiles of kTileRows rows the experts before e have; [experts]: the
-// end and the count of all.  Ends count as they would if each were clamped between the one before it and the rows there are.  ends NULL: one expert has all rows.
-__device__ __forceinline__ void experts_scan(const int32_t* __restrict__ ends, int experts, long long rows, int* begin, int* before)
+// In shared memory, by one warp: begin[e] is expert e's first row, begin[experts] the end of all.  Ends count as they would if each were clamped between the
+// one before it and the rows there are.  ends NULL: one expert has all rows.
+__device__ __forceinline__ void experts_begin(const int32_t* __restrict__ ends, int experts, long long rows, int* begin)
 {
     const int lane = threadIdx.x % 32;
-    int last = 0, tiles = 0;
+    int last = 0;
     for (int b = 0; b < experts; b += 32) {
         const int e = b + lane;
         int end = e >= experts ? 0 : ends ? (int)min(max((long long)__ldg(ends + e), 0ll), rows) : (int)rows;
@@ -22,24 +22,51 @@ __device__ __forceinline__ void experts_scan(const int32_t* __restrict__ ends, i
         end = max(end, last);
         int first = __shfl_up_sync(0xffffffffu, end, 1);
         if (lane == 0) first = last;
-        const int mine = (int)(((unsigned)(end - first) + kTileRows - 1) / kTileRows);
+        if (e < experts) begin[e] = first;
+        last = __shfl_sync(0xffffffffu, end, 31);
+    }
+    if (lane == 0) begin[experts] = last;
+}
+
+// Rows of an expert's tiles where none has more than `most` (a multiple of 32): as many as it needs, of one size, a multiple of 32 again.
+__device__ __forceinline__ int experts_tiles(int rows, int most) { return (int)(((unsigned)rows + most - 1) / most); }
+__device__ __forceinline__ int experts_tile(int rows, int tiles) { return tiles ? (int)((((unsigned)rows + tiles - 1) / tiles + 31) & ~31u) : 0; }
+
+// What the tiles of at most `most` rows would take, by one warp: the rounds of `pairs` of CTAs that they make, each by `across` tiles of weights' rows, times their mean cost.
+// A tile of r rows takes fixed + r for each chunk of the summed index.
+__device__ __forceinline__ float experts_price(const int* begin, int experts, int most, int across, int pairs, float fixed)
+{
+    float tiles = 0.f, cost = 0.f;
+    for (int e = threadIdx.x % 32; e < experts; e += 32) {
+        const int rows = begin[e + 1] - begin[e], mine = experts_tiles(rows, most);
+        tiles += mine;
+        cost += mine * (fixed + experts_tile(rows, mine));
+    }
+#pragma unroll
+    for (int o = 16; o; o /= 2) {
+        tiles += __shfl_xor_sync(0xffffffffu, tiles, o);
+        cost += __shfl_xor_sync(0xffffffffu, cost, o);
+    }
+    return tiles > 0.f ? ceilf(tiles * across / pairs) * (cost / tiles) : 0.f;
+}
+
+// before[e]: how many tiles the experts before e have, before[experts] all, by one warp.
+__device__ __forceinline__ void experts_before(const int* begin, int experts, int most, int* before)
+{
+    const int lane = threadIdx.x % 32;
+    int tiles = 0;
+    for (int b = 0; b < experts; b += 32) {
+        const int e = b + lane, mine = e < experts ? experts_tiles(begin[e + 1] - begin[e], most) : 0;
         int sum = mine;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
             const int other = __shfl_up_sync(0xffffffffu, sum, o);
             if (lane >= o) sum += other;
         }
-        if (e < experts) {
-            begin[e] = first;
-            before[e] = tiles + sum - mine;
-        }
-        last = __shfl_sync(0xffffffffu, end, 31);
+        if (e < experts) before[e] = tiles + sum - mine;
         tiles += __shfl_sync(0xffffffffu, sum, 31);
     }
-    if (lane == 0) {
-        begin[experts] = last;
-        before[experts] = tiles;
-    }
+    if (lane == 0) before[experts] = tiles;
 }
 
 // The nth (from 0) of the experts that have rows, to shared memory by one warp: which it is, its first row and how many; -1, 0, 0 where there are fewer.  And

@@ -10,8 +10,6 @@
 
 namespace {
 
-constexpr int kMost = 8;                                  // pieces of 8 columns that a thread keeps
-
 // The numbers nearest to v / s in the low bytes of t, ties to even; inv is 1 / s rounded, half is s / 2.  With |v / s| < 127.5 the sum v * inv + 1.5 * 2^23 is
 // rounded to a whole number q off by one at most, and only where the remainder r = v - q s has left [-half, half].  r is a multiple of a quarter of s's last
 // place and not above it by more than its rounding can tell (at q = 1 and v just below half the rounded |r| may be half itself: q goes to 0 then, which is right).
@@ -41,9 +39,10 @@ __device__ __forceinline__ uint2 codes_of(const float (&v)[8], float s, float in
     return w;
 }
 
-// WARPS of a CTA of 8 have a row.
-template <typename T, bool VEC, int WARPS>
-__global__ void __launch_bounds__(256) i8_pack_kernel(long long rows, int cols, int pieces, const T* __restrict__ x, long long stride, int8_t* __restrict__ codes, float* __restrict__ scales)
+// WARPS of a CTA of 8 have a row, of which a thread keeps P pieces of 8 columns in registers.
+template <typename T, bool VEC, int WARPS, int P>
+__global__ void __launch_bounds__(256, P > 4 ? 2 : sizeof(T) == 2 ? 5 : 4)
+i8_pack_kernel(long long rows, int cols, int pieces, const T* __restrict__ x, long long stride, int8_t* __restrict__ codes, float* __restrict__ scales)
 {
     constexpr int threads = WARPS * 32;
     __shared__ uint32_t found[2][8];
@@ -54,27 +53,27 @@ __global__ void __launch_bounds__(256) i8_pack_kernel(long long rows, int cols, 
         const long long row = row0 + warp / WARPS;
         const bool in = row < rows;
         const T* from = x + row * stride;
-        MxPiece<T> raw[kMost];
+        MxPiece<T> raw[P];
         uint32_t m = 0;
         if (in) {
 #pragma unroll
-            for (int h = 0; h < kMost; ++h) {
+            for (int h = 0; h < P; ++h) {
                 const unsigned c = t + h * threads;       // pieces of a row reach 2^28, and some more in the last step
                 if (c < (unsigned)pieces) raw[h] = mx_fetch8<T, VEC>(from, (int)(c * 8), cols);
             }
 #pragma unroll
-            for (int h = 0; h < kMost; ++h)
+            for (int h = 0; h < P; ++h)
                 if (t + h * threads < (unsigned)pieces) m = max(m, mx_most<T>(raw[h]));
-            for (unsigned c = t + kMost * threads; c < (unsigned)pieces; c += threads) m = max(m, mx_most<T>(mx_fetch8<T, VEC>(from, (int)(c * 8), cols)));
+            for (unsigned c = t + P * threads; c < (unsigned)pieces; c += threads) m = max(m, mx_most<T>(mx_fetch8<T, VEC>(from, (int)(c * 8), cols)));
         }
         m = __reduce_max_sync(0xffffffffu, m);
-        if (WARPS > 1) {
+        if (WARPS > 1) {                                  // the row's warps meet at a barrier of theirs
             if (lane == 0) found[turn][warp] = m;
-            __syncthreads();
+            asm volatile("bar.sync %0, %1;" :: "r"(1 + warp / WARPS), "n"(threads) : "memory");
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) m = max(m, found[turn][w]);
+            for (int w = 0; w < WARPS; ++w) m = max(m, found[turn][warp / WARPS * WARPS + w]);
         }
-        if (!in) continue;                                // only where a row is a warp's own
+        if (!in) continue;
         const bool bad = m >= 0x7f800000u;
         const float s = __fdiv_rn(fmaxf(__uint_as_float(bad ? 0u : m), kI8Least), 127.f), inv = __fdiv_rn(1.f, s), half = s * 0.5f;
         int8_t* to = codes + row * ((long long)pieces * 8);
@@ -84,9 +83,9 @@ __global__ void __launch_bounds__(256) i8_pack_kernel(long long rows, int cols, 
             *reinterpret_cast<uint2*>(to + c * 8ll) = bad ? make_uint2(0, 0) : codes_of(v, s, inv, half);
         };
 #pragma unroll
-        for (int h = 0; h < kMost; ++h)
+        for (int h = 0; h < P; ++h)
             if (t + h * threads < (unsigned)pieces) put(t + h * threads, raw[h]);
-        for (unsigned c = t + kMost * threads; c < (unsigned)pieces; c += threads) put(c, mx_fetch8<T, VEC>(from, (int)(c * 8), cols));
+        for (unsigned c = t + P * threads; c < (unsigned)pieces; c += threads) put(c, mx_fetch8<T, VEC>(from, (int)(c * 8), cols));
         if (t == 0) scales[row] = bad ? __uint_as_float(0x7fc00000u) : s;
     }
 }
@@ -131,13 +130,22 @@ __global__ void __launch_bounds__(kMxThreads) i8_unpack_kernel(const MxSpread sp
     }
 }
 
+template <typename T, bool VEC, int WARPS, int P>
+void launch_pack(int num_sms, int64_t rows, int64_t cols, const T* x, int64_t stride, int8_t* codes, float* scales, cudaStream_t st)
+{
+    const int64_t ctas = (rows + 8 / WARPS - 1) / (8 / WARPS), most = (int64_t)num_sms * 32;
+    i8_pack_kernel<T, VEC, WARPS, P><<<(int)(ctas < most ? ctas : most), 256, 0, st>>>(rows, (int)cols, (int)(i8_pitch(cols) / 8), x, stride, codes, scales);
+}
+
+// As many warps a row as keep all of it with 4 pieces a thread (8 of the longest rows), and all 8 where there are few rows.
 template <typename T, bool VEC>
 void pack_by_size(int num_sms, int64_t rows, int64_t cols, const T* x, int64_t stride, int8_t* codes, float* scales, cudaStream_t st)
 {
-    const int pieces = (int)(i8_pitch(cols) / 8);
-    const int64_t most = (int64_t)num_sms * 16;
-    if (pieces <= 32 * kMost) i8_pack_kernel<T, VEC, 1><<<(int)((rows + 7) / 8 < most ? (rows + 7) / 8 : most), 256, 0, st>>>(rows, (int)cols, pieces, x, stride, codes, scales);
-    else i8_pack_kernel<T, VEC, 8><<<(int)(rows < most ? rows : most), 256, 0, st>>>(rows, (int)cols, pieces, x, stride, codes, scales);
+    if (cols > 8192) launch_pack<T, VEC, 8, 8>(num_sms, rows, cols, x, stride, codes, scales, st);
+    else if (cols > 4096 || (cols > 256 && rows <= 2 * num_sms)) launch_pack<T, VEC, 8, 4>(num_sms, rows, cols, x, stride, codes, scales, st);
+    else if (cols > 2048) launch_pack<T, VEC, 4, 4>(num_sms, rows, cols, x, stride, codes, scales, st);
+    else if (cols > 1024) launch_pack<T, VEC, 2, 4>(num_sms, rows, cols, x, stride, codes, scales, st);
+    else launch_pack<T, VEC, 1, 4>(num_sms, rows, cols, x, stride, codes, scales, st);
 }
 
 }  // namespace

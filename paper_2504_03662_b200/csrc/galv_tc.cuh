@@ -52,7 +52,7 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.release.cta.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
 }
-// Waits for the phase of `parity` to end; false after about two seconds.
+// Waits for the phase of `parity` to end; false after about two seconds.  What other CTAs of the cluster wrote before they arrived can be read.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
@@ -65,6 +65,25 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity)
     } while (clock64() - start < 4000000000ll);
     return false;
 }
+// ... what this CTA's threads and bulk copies wrote, and what the tensor cores did.
+__device__ __forceinline__ bool bar_wait_own(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if (done) return true;
+    const long long start = clock64();
+    do {
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        if (done) return true;
+    } while (clock64() - start < 4000000000ll);
+    return false;
+}
+// Behind a wait that ran out, where copies may be in flight that nobody here can wait for: they land within microseconds.
+__device__ __forceinline__ void settle()
+{
+    const long long start = clock64();
+    while (clock64() - start < 20000000ll) {}
+}
 
 // ---- bulk copies into shared memory
 __device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar)
@@ -75,6 +94,17 @@ __device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap* map, in
 __device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar)
 {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+// ... that tell a barrier of the pair's first CTA (address from in_cta), in whichever of the two this runs
+__device__ __forceinline__ void load_2d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void load_3d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void load_bytes(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
