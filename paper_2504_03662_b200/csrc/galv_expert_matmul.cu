@@ -18,8 +18,11 @@ namespace {
 
 enum Kind { kForward, kInputGrad, kWhole };               // 16 bits, summed along the weights' rows; across them; 8-bit integers
 
-constexpr int kStages = 6, kTile = 256, kHalf = kTile / 2, kChunkBytes = 128;
-constexpr int kRowsBytes = kHalf * kChunkBytes, kStageBytes = 2 * kRowsBytes;
+constexpr int kTile = 256, kHalf = kTile / 2, kChunkBytes = 128;
+constexpr int kRowsBytes = kHalf * kChunkBytes;
+// The ring of chunks: 6 of full tiles, up to 10 of smaller ones, whose matrix instructions are over sooner and whose copies are to be as far ahead (8-bit integers, tiles of 64
+// tokens, a chunk: 282 ns with 6).
+constexpr int kRing = 12 * kRowsBytes, kStagesMost = 10;
 constexpr int kOutBytes = 8 * 2048;
 constexpr int kBox = 64, kPart = 16;                      // tokens of a copy, and of one where fewer are left
 constexpr int kThreads = 384;
@@ -81,20 +84,21 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
 {
     extern __shared__ unsigned char raw[];
     const uint32_t base = (tc::smem_at(raw) + 1023) & ~1023u;
-    const uint32_t w_at = base, x_at = w_at + kStages * kRowsBytes, out_at = x_at + kStages * kRowsBytes, bars = out_at + kOutBytes;
-    const uint32_t full = bars, empty = full + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16, drain = acc_empty + 16,
+    const uint32_t out_at = base + kRing, bars = out_at + kOutBytes;
+    const uint32_t full = bars, empty = full + 8 * kStagesMost, acc_full = empty + 8 * kStagesMost, acc_empty = acc_full + 16, drain = acc_empty + 16,
                    slot = drain + 8;
     int* const begin = reinterpret_cast<int*>(raw + (bars + 256 - tc::smem_at(raw)));
     int* const before = begin + a.experts + 1;
     __shared__ int failed;
     __shared__ float prices[8];
+    __shared__ int most;                                  // tokens of a tile
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = tc::cluster_rank();
     const int first = blockIdx.x / 2, stride = gridDim.x / 2;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
+        for (int s = 0; s < kStagesMost; ++s) {
             tc::bar_init(full + 8 * s, 1);
             tc::bar_init(empty + 8 * s, 1);
         }
@@ -122,6 +126,7 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
         for (int i = 1; i < 8; ++i)
             if (prices[i] < prices[best]) best = i;
         experts_before(begin, a.experts, kTile - best * 32, before);
+        if (lane == 0) most = kTile - best * 32;
     }
     tc::fence_before();
     __syncthreads();
@@ -129,7 +134,7 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
     tc::fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
-    const int units = before[a.experts] * a.tiles_m;
+    const int units = before[a.experts] * a.tiles_m, stage = kRowsBytes + most / 2 * kChunkBytes, stages = min(kStagesMost, kRing / stage);
 
     auto waited = [&](uint32_t bar, uint32_t parity) {
         if (tc::bar_wait_own(bar, parity)) return true;
@@ -141,52 +146,66 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
     if (warp == 0) {
         if (tc::elect()) {
             constexpr int elements = K == kWhole ? kChunkBytes : kChunkBytes / 2;
-            int it = 0;
-            bool ok = true;
-            if (K == kWhole) tc::before_is_over();        // the tokens may be put into 8-bit integers by the kernel in front
+            int s = 0;
+            uint32_t turn = 1;
+            bool ok = true, over = K != kWhole;
             for (int u = first; u < units && ok; u += stride) {
                 w.to(u);
                 const int m0 = w.tm * kTile + rank * kHalf, half = w.columns() / 2, r0 = w.row0 + rank * half;
-                for (int c = 0; c < a.chunks; ++c, ++it) {
-                    const int s = it % kStages;
-                    const uint32_t bar = tc::in_cta(full + 8 * s, 0), ws = w_at + s * kRowsBytes, xs = x_at + s * kRowsBytes;
-                    if (!(ok = waited(empty + 8 * s, (it / kStages & 1) ^ 1))) break;
+                auto weights = [&](int s, int c) {
+                    const uint32_t bar = tc::in_cta(full + 8 * s, 0), to = base + s * stage;
                     if (rank == 0) tc::bar_expect(full + 8 * s, 2 * (kRowsBytes + half * kChunkBytes));      // of both CTAs
                     if (K == kInputGrad) {                // 64 rows of weights, 64 columns a copy
-                        tc::load_3d_pair(ws, &w_map, m0, c * elements, w.expert, bar);
-                        tc::load_3d_pair(ws + kRowsBytes / 2, &w_map, m0 + 64, c * elements, w.expert, bar);
+                        tc::load_3d_pair(to, &w_map, m0, c * elements, w.expert, bar);
+                        tc::load_3d_pair(to + kRowsBytes / 2, &w_map, m0 + 64, c * elements, w.expert, bar);
                     } else {
-                        tc::load_3d_pair(ws, &w_map, c * elements, m0, w.expert, bar);
+                        tc::load_3d_pair(to, &w_map, c * elements, m0, w.expert, bar);
                     }
+                };
+                int ahead = 0;
+                if (!over) {                              // the kernel in front may still be putting the tokens into 8-bit integers: the weights do not wait for it
+                    for (ahead = 0; ahead < min(stages, a.chunks); ++ahead) weights(ahead, ahead);
+                    tc::before_is_over();
+                    over = true;
+                }
+                for (int c = 0; c < a.chunks; ++c) {
+                    if (c >= ahead) {
+                        if (!(ok = waited(empty + 8 * s, turn))) break;
+                        weights(s, c);
+                    }
+                    const uint32_t bar = tc::in_cta(full + 8 * s, 0), to = base + s * stage + kRowsBytes;
                     int i = 0;
-                    for (; i + kBox <= half; i += kBox) tc::load_2d_pair(xs + i * kChunkBytes, &x_map, c * elements, r0 + i, bar);
-                    for (; i < half; i += kPart) tc::load_2d_pair(xs + i * kChunkBytes, &part_map, c * elements, r0 + i, bar);
+                    for (; i + kBox <= half; i += kBox) tc::load_2d_pair(to + i * kChunkBytes, &x_map, c * elements, r0 + i, bar);
+                    for (; i < half; i += kPart) tc::load_2d_pair(to + i * kChunkBytes, &part_map, c * elements, r0 + i, bar);
+                    if (++s == stages) s = 0, turn ^= 1;
                 }
             }
             if (*(volatile int*)&failed) tc::settle();
         }
     } else if (warp == 1 && rank == 0) {
         if (tc::elect()) {
-            int it = 0, done = 0;
+            int s = 0, done = 0;
+            uint32_t turn = 0;
             bool ok = true;
             for (int u = first; u < units && ok; u += stride, ++done) {
                 w.to(u);
                 const uint32_t buf = done & 1, d = tmem + buf * kTile, what = a.what | (uint32_t)(w.columns() >> 3) << 17;
                 if (!(ok = waited(acc_empty + 8 * buf, (done / 2 & 1) ^ 1))) break;
                 tc::fence_after();
-                for (int c = 0; c < a.chunks; ++c, ++it) {
-                    const int s = it % kStages, steps = c + 1 < a.chunks ? 4 : a.last_steps;
-                    if (!(ok = waited(full + 8 * s, it / kStages & 1))) break;
+                for (int c = 0; c < a.chunks; ++c) {
+                    const int steps = c + 1 < a.chunks ? 4 : a.last_steps;
+                    const uint32_t ws = base + s * stage, xs = ws + kRowsBytes;
+                    if (!(ok = waited(full + 8 * s, turn))) break;
                     tc::fence_after();
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         if (j < steps) {
-                            const uint64_t wo = K == kInputGrad ? tc::operand(w_at + s * kRowsBytes + j * 2048, kRowsBytes / 2, 1024) : tc::operand(w_at + s * kRowsBytes + j * 32, 16, 1024);
-                            const uint64_t xo = tc::operand(x_at + s * kRowsBytes + j * 32, 16, 1024);
+                            const uint64_t wo = K == kInputGrad ? tc::operand(ws + j * 2048, kRowsBytes / 2, 1024) : tc::operand(ws + j * 32, 16, 1024), xo = tc::operand(xs + j * 32, 16, 1024);
                             if (K == kWhole) tc::mma_i8<2>(d, wo, xo, what, c > 0 || j > 0);
                             else tc::mma_f16<2>(d, wo, xo, what, c > 0 || j > 0);
                         }
                     tc::mma_commit<2>(empty + 8 * s);
+                    if (++s == stages) s = 0, turn ^= 1;
                 }
                 if (ok) tc::mma_commit<2>(acc_full + 8 * buf);
             }
@@ -267,23 +286,17 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
 // s-th of those that have rows); clusters are launched for as many experts as there could be, those that are too many end at once.  The weights' first copies
 // start before the kernel in front, which puts the tokens into 8-bit integers, is over.
 
-constexpr int kFewThreads = 256, kFewRows = 64;
-template <int N> struct Few {                             // N: rows, rounded up
-    static constexpr int stages = N == 16 ? 5 : N == 32 ? 4 : 3;
-    static constexpr int rows_w = 128 * kChunkBytes, rows_x = N * kChunkBytes, stage = rows_w + rows_x;
-    static constexpr int inbox = N * 128 * 4;
-    static constexpr int smem = 1024 + stages * stage + inbox + 256;
-};
+constexpr int kFewThreads = 256, kFewRows = 64, kFewStages = 6;
+constexpr int kFewRing = 6 * (128 + kPart) * kChunkBytes;      // shared memory of chunks and of what other CTAs send: 6 chunks for up to 16 tokens, 4 for 64; 5 and 3 in a cluster
+constexpr int kFewSmem = 1024 + kFewRing + 256;
 
-template <int K, typename O, int N>
+template <int K, typename O>
 __global__ void __launch_bounds__(kFewThreads, 2)
 expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap part_map, const __grid_constant__ ProductArgs a, int tiles, int ranks)
 {
-    using F = Few<N>;
     extern __shared__ unsigned char raw[];
     const uint32_t base = (tc::smem_at(raw) + 1023) & ~1023u;
-    const uint32_t w_at = base, x_at = w_at + F::stages * F::rows_w, inbox = x_at + F::stages * F::rows_x, bars = inbox + F::inbox;
-    const uint32_t full = bars, empty = full + 8 * F::stages, acc_full = empty + 8 * F::stages, slot = acc_full + 8;
+    const uint32_t bars = base + kFewRing, full = bars, empty = full + 8 * kFewStages, acc_full = empty + 8 * kFewStages, slot = acc_full + 8;
     __shared__ int failed, mine[4];                       // expert (or -1), its first row, how many; where rows of no expert begin
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -293,7 +306,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_consta
     const int c0 = (int)((long long)rank * a.chunks / ranks), c1 = (int)((long long)(rank + 1) * a.chunks / ranks);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < F::stages; ++s) {
+        for (int s = 0; s < kFewStages; ++s) {
             tc::bar_init(full + 8 * s, 1);
             tc::bar_init(empty + 8 * s, 1);
         }
@@ -303,7 +316,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_consta
         tc::prefetch_map(&w_map);
         tc::prefetch_map(&part_map);
     }
-    constexpr uint32_t columns = N <= 32 ? 32 : 64;
+    constexpr uint32_t columns = kFewRows;
     if (warp == 2) tc::tmem_alloc<1>(slot, columns);
     if (warp == 3) experts_nth(a.ends, a.experts, a.rows, nth, mine);
     tc::fence_before();
@@ -329,100 +342,111 @@ expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_consta
         return false;
     };
 
-    const int boxes = (count + kPart - 1) / kPart;        // of the tokens; none where nobody has rows
+    const int boxes = (count + kPart - 1) / kPart, tokens = boxes * kPart;      // copies of tokens; none where nobody has rows
+    const int stage = (128 + tokens) * kChunkBytes, sent = ranks > 1 ? tokens * 512 : 0, stages = min(kFewStages, (kFewRing - sent) / stage), chunks = boxes ? c1 - c0 : 0;
+    const uint32_t inbox = base + kFewRing - sent;
     if (warp == 0) {
         if (tc::elect()) {
             constexpr int elements = K == kWhole ? kChunkBytes : kChunkBytes / 2;
-            const int m0 = (int)n0, chunks = boxes ? c1 - c0 : 0, ahead = min(F::stages, chunks);
-            for (int it = 0; it < ahead; ++it) {
-                tc::bar_expect(full + 8 * it, F::rows_w + boxes * kPart * kChunkBytes);
-                tc::load_3d(w_at + it * F::rows_w, &w_map, (c0 + it) * elements, m0, expert, full + 8 * it);
-            }
+            const int ahead = min(stages, chunks);
+            auto weights = [&](int s, int it) {
+                tc::bar_expect(full + 8 * s, stage);
+                tc::load_3d(base + s * stage, &w_map, (c0 + it) * elements, (int)n0, expert, full + 8 * s);
+            };
+            for (int it = 0; it < ahead; ++it) weights(it, it);
             tc::before_is_over();
-            int it = 0;
+            int it = 0, s = 0;
+            uint32_t turn = 1;
             for (; it < chunks; ++it) {
-                const int s = it % F::stages;
-                const uint32_t bar = full + 8 * s;
                 if (it >= ahead) {
-                    if (!waited(empty + 8 * s, (it / F::stages & 1) ^ 1)) break;
-                    tc::bar_expect(bar, F::rows_w + boxes * kPart * kChunkBytes);
-                    tc::load_3d(w_at + s * F::rows_w, &w_map, (c0 + it) * elements, m0, expert, bar);
+                    if (!waited(empty + 8 * s, turn)) break;
+                    weights(s, it);
                 }
-                for (int i = 0; i < boxes; ++i) tc::load_2d(x_at + s * F::rows_x + i * kPart * kChunkBytes, &part_map, (c0 + it) * elements, row0 + i * kPart, bar);
+                for (int i = 0; i < boxes; ++i)
+                    tc::load_2d(base + s * stage + (128 + i * kPart) * kChunkBytes, &part_map, (c0 + it) * elements, row0 + i * kPart, full + 8 * s);
+                if (++s == stages) s = 0, turn ^= 1;
             }
-            if (*(volatile int*)&failed)                  // copies still in flight
-                for (int i = it < F::stages ? 0 : it - F::stages; i < it; ++i) tc::bar_wait(full + 8 * (i % F::stages), i / F::stages & 1);
+            if (*(volatile int*)&failed) tc::settle();
         }
     } else if (warp == 1) {
         if (tc::elect()) {
-            const uint32_t what = a.what | (uint32_t)(boxes * kPart >> 3) << 17 | (uint32_t)(128 >> 4) << 24;
-            const int chunks = boxes ? c1 - c0 : 0;
+            const uint32_t what = a.what | (uint32_t)(tokens >> 3) << 17 | (uint32_t)(128 >> 4) << 24;
+            int s = 0;
+            uint32_t turn = 0;
             for (int it = 0; it < chunks; ++it) {
-                const int s = it % F::stages, steps = c0 + it + 1 < a.chunks ? 4 : a.last_steps;
-                if (!waited(full + 8 * s, it / F::stages & 1)) break;
+                const int steps = c0 + it + 1 < a.chunks ? 4 : a.last_steps;
+                const uint32_t ws = base + s * stage, xs = ws + kRowsBytes;
+                if (!waited(full + 8 * s, turn)) break;
                 tc::fence_after();
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (j < steps) {
-                        const uint64_t wo = tc::operand(w_at + s * F::rows_w + j * 32, 16, 1024), xo = tc::operand(x_at + s * F::rows_x + j * 32, 16, 1024);
+                        const uint64_t wo = tc::operand(ws + j * 32, 16, 1024), xo = tc::operand(xs + j * 32, 16, 1024);
                         if (K == kWhole) tc::mma_i8<1>(tmem, wo, xo, what, it > 0 || j > 0);
                         else tc::mma_f16<1>(tmem, wo, xo, what, it > 0 || j > 0);
                     }
                 tc::mma_commit<1>(empty + 8 * s);
+                if (++s == stages) s = 0, turn ^= 1;
             }
             tc::mma_commit<1>(acc_full);                  // also after a wait that ran out: nothing may be in flight when the memory goes
-            tc::bar_wait(acc_full, 0);
+            tc::bar_wait_own(acc_full, 0);
         }
     }
     __syncwarp();
     tc::before_is_over();
     tc::cluster_wait();                                   // the CTAs that the sums go to run
-    const int quad = warp - 4, row = quad * 32 + lane, each = N / ranks;      // a thread has one row of weights; this CTA finishes `each` tokens
+    const int quad = warp - 4, row = quad * 32 + lane, each = tokens / ranks;      // a thread has one row of weights; this CTA finishes `each` tokens
     const long long ch = n0 + row, at = expert * a.n + ch;
+    const bool has = warp >= 4 && expert >= 0 && ch < a.n;
+    const float bias = a.bias && has ? mx_float(((const O*)a.bias)[at]) : 0.f, w_scale = K == kWhole && has ? a.w_scales[at] : 0.f;
+    O* const y = (O*)a.y + ch;
+    auto put = [&](int token, uint32_t sum) {
+        y[(long long)(row0 + token) * a.stride] = mx_round<O>(number<K>(sum, K == kWhole ? a.x_scales[row0 + token] : 0.f, w_scale, bias));
+    };
     bool ok = true;
     if (warp >= 4) {
         ok = waited(acc_full, 0);
         tc::fence_after();
         if (ok) {
 #pragma unroll 1
-            for (int j = 0; j < boxes * kPart; j += 16) {
+            for (int j = 0; j < tokens; j += 16) {
                 uint32_t v[16];
                 tc::tmem_load16(tmem + j + ((uint32_t)quad * 32 << 16), v);
                 tc::tmem_wait_load();
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int col = j + i, to = col / each;
-                    asm volatile("st.shared::cluster.b32 [%0], %1;" :: "r"(tc::in_cta(inbox + (((rank * each) + col % each) * 128 + row) * 4, to)), "r"(v[i]) : "memory");
+                    const int col = j + i;
+                    if (ranks > 1) asm volatile("st.shared::cluster.b32 [%0], %1;" :: "r"(tc::in_cta(inbox + ((rank * each + col % each) * 128 + row) * 4, col / each)), "r"(v[i]) : "memory");
+                    else if (has && col < count) put(col, v[i]);
                 }
             }
         }
     }
     tc::fence_before();
     __syncthreads();
-    tc::cluster_sync();                                   // every slice is where it belongs
-    if (warp >= 4 && ok && ch < a.n) {
-        const float b = a.bias && expert >= 0 ? mx_float(((const O*)a.bias)[at]) : 0.f, w_scale = K == kWhole && expert >= 0 ? a.w_scales[at] : 0.f;
-        O* const y = (O*)a.y + ch;
-        for (int j = 0; j < each; ++j) {
-            const int col = rank * each + j;
-            if (col >= count) break;
-            uint32_t sum = 0;
-            for (int r = 0; r < ranks; ++r) {
-                uint32_t v;
-                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(inbox + ((r * each + j) * 128 + row) * 4));
-                sum = r == 0 ? v : K == kWhole ? sum + v : __float_as_uint(__uint_as_float(sum) + __uint_as_float(v));
+    if (ranks > 1) {
+        tc::cluster_sync();                               // every slice is where it belongs
+        if (has && ok)
+            for (int j = 0; j < each; ++j) {
+                const int col = rank * each + j;
+                if (col >= count) break;
+                uint32_t sum = 0;
+                for (int r = 0; r < ranks; ++r) {
+                    uint32_t v;
+                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(inbox + ((r * each + j) * 128 + row) * 4));
+                    sum = r == 0 ? v : K == kWhole ? sum + v : __float_as_uint(__uint_as_float(sum) + __uint_as_float(v));
+                }
+                put(col, sum);
             }
-            y[(row0 + col) * a.stride] = mx_round<O>(number<K>(sum, K == kWhole ? a.x_scales[row0 + col] : 0.f, w_scale, b));
-        }
-        if (nth == 0)                                     // rows of no expert
-            for (long long r = mine[3] + (int)rank; r < a.rows; r += ranks) y[r * a.stride] = mx_zero<O>();
     }
+    if (nth == 0 && warp >= 4 && ch < a.n)                // rows of no expert
+        for (long long r = mine[3] + (int)rank; r < a.rows; r += ranks) y[r * a.stride] = mx_zero<O>();
     if (threadIdx.x == 0 && failed) atomicAdd_system(a.timeouts, 1u);
     if (warp == 2) tc::tmem_free<1>(tmem, columns);
 }
 
 size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
-int smem_of(int experts) { return 1024 + kStages * kStageBytes + kOutBytes + 256 + 8 * (experts + 1); }
+int smem_of(int experts) { return 1024 + kRing + kOutBytes + 256 + 8 * (experts + 1); }
 
 // Where the operands of a product in 16 bits that bulk copies cannot take as they are go in the workspace.
 struct AlignPlan { size_t x, w, total; };
@@ -457,10 +481,10 @@ void configure(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* attr, unsigned grid
     }
 }
 
-template <int K, typename O, int N>
+template <int K, typename O>
 cudaError_t launch_few(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap& pm, const ProductArgs& a, bool in_front, cudaStream_t st)
 {
-    cudaError_t e = cudaFuncSetAttribute(expert_few_kernel<K, O, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, Few<N>::smem);
+    cudaError_t e = cudaFuncSetAttribute(expert_few_kernel<K, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
     if (e != cudaSuccess) return e;
     const int tiles = (int)((a.n + 127) / 128);
     const long long units = tiles * (long long)(a.rows < a.experts ? a.rows : a.experts);
@@ -468,17 +492,15 @@ cudaError_t launch_few(const galv_ctx* ctx, const CUtensorMap& wm, const CUtenso
     while (ranks < 8 && units * ranks <= ctx->num_sms && a.chunks >= ranks * 4) ranks *= 2;
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
-    configure(cfg, attr, (unsigned)(units * ranks), kFewThreads, Few<N>::smem, (unsigned)ranks, in_front, st);
-    return cudaLaunchKernelEx(&cfg, expert_few_kernel<K, O, N>, wm, pm, a, tiles, ranks);
+    configure(cfg, attr, (unsigned)(units * ranks), kFewThreads, kFewSmem, (unsigned)ranks, in_front, st);
+    return cudaLaunchKernelEx(&cfg, expert_few_kernel<K, O>, wm, pm, a, tiles, ranks);
 }
 
 template <int K, typename O>
 cudaError_t launch(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap& xm, const CUtensorMap& pm, ProductArgs& a, bool in_front, cudaStream_t st)
 {
     if constexpr (K != kInputGrad) {
-        if (a.rows <= 16) return launch_few<K, O, 16>(ctx, wm, pm, a, in_front, st);
-        if (a.rows <= 32) return launch_few<K, O, 32>(ctx, wm, pm, a, in_front, st);
-        if (a.rows <= kFewRows) return launch_few<K, O, 64>(ctx, wm, pm, a, in_front, st);
+        if (a.rows <= kFewRows) return launch_few<K, O>(ctx, wm, pm, a, in_front, st);
     }
     const int smem = smem_of(a.experts);
     const cudaError_t e = cudaFuncSetAttribute(expert_product_kernel<K, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kExpertsMost));
