@@ -538,7 +538,7 @@ int galv_i8_linear(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int6
                    const int8_t* w_codes, const float* w_scales, const void* bias, void* y, int64_t y_stride, int32_t dtype,
                    void* workspace, size_t workspace_bytes, void* stream);
 /*
- * The same in 16 bits, w [experts][n][k] contiguous, everything of `dtype` (GALV_BF16 or GALV_F16):
+ * The same in 16 bits, w [experts][n] rows of k, w_stride apart (n * w_stride from one expert to the next), everything of `dtype` (GALV_BF16 or GALV_F16):
  *   galv_expert_matmul       y[r][j]  = sum_c x[r][c] w[e][j][c] + bias[e][j]       (bias [experts][n] or NULL)
  *   galv_expert_input_grad   dx[r][c] = sum_j dy[r][j] w[e][j][c]
  *   galv_expert_weight_grad  dw[e][j][c] = base[e][j][c] + sum over e's rows of dy[r][j] x[r][c]
@@ -547,17 +547,18 @@ int galv_i8_linear(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int6
  * rounded additions), biases and base are added in fp32, results rounded once.  dw, base [experts][n][k] contiguous of `dw_dtype`, db [experts][n] of
  * `db_dtype` (`dtype` or GALV_F32); base NULL: zero; dw may be base.  An expert without rows has base or zeros for its gradient.  The order of
  * the sums is fixed by sizes, ends, strides and alignment.  Operands whose rows do not start on 16-byte boundaries are moved to ones that do, in the
- * workspace (256-byte aligned, the bytes that the query gives for the same sizes, pointers and strides; 0: may be NULL).
+ * workspace (256-byte aligned, the bytes that the query gives for the same sizes, pointers and strides; 0: may be NULL).  After galv_expert_matmul it holds
+ * x, if that was moved, [rows] rows ceil(k / 8) * 8 apart, and from the next multiple of 256 bytes on w, if that was moved, its rows as far apart.
  */
 size_t galv_expert_matmul_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* x,
-                                          int64_t x_stride, const void* w);
+                                          int64_t x_stride, const void* w, int64_t w_stride);
 int galv_expert_matmul(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* x,
-                       int64_t x_stride, const void* w, const void* bias, void* y, int64_t y_stride, int32_t dtype, void* workspace,
+                       int64_t x_stride, const void* w, int64_t w_stride, const void* bias, void* y, int64_t y_stride, int32_t dtype, void* workspace,
                        size_t workspace_bytes, void* stream);
 size_t galv_expert_input_grad_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy,
-                                              int64_t dy_stride, const void* w);
+                                              int64_t dy_stride, const void* w, int64_t w_stride);
 int galv_expert_input_grad(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* dy,
-                           int64_t dy_stride, const void* w, void* dx, int64_t dx_stride, int32_t dtype, void* workspace,
+                           int64_t dy_stride, const void* w, int64_t w_stride, void* dx, int64_t dx_stride, int32_t dtype, void* workspace,
                            size_t workspace_bytes, void* stream);
 size_t galv_expert_weight_grad_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy,
                                                int64_t dy_stride, const void* x, int64_t x_stride);
@@ -569,9 +570,9 @@ int galv_expert_bias_grad(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t 
 /* The last three in one call, each where its result is asked for (dx, dw [experts][n][k], db [experts][n], all of `dtype`; NULL: not; x and w may be NULL where
  * no result needs them).  workspace: the bytes that the query gives with the x and w that are needed, else NULL. */
 size_t galv_expert_backward_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy,
-                                            int64_t dy_stride, const void* x, int64_t x_stride, const void* w);
+                                            int64_t dy_stride, const void* x, int64_t x_stride, const void* w, int64_t w_stride);
 int galv_expert_backward(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* dy,
-                         int64_t dy_stride, const void* x, int64_t x_stride, const void* w, int32_t dtype, void* dx, int64_t dx_stride,
+                         int64_t dy_stride, const void* x, int64_t x_stride, const void* w, int64_t w_stride, int32_t dtype, void* dx, int64_t dx_stride,
                          void* dw, void* db, void* workspace, size_t workspace_bytes, void* stream);
 /* Waits for `stream` and says whether a bounded device-side wait of a product (galv_mx_weight_grad, galv_mx_matmul, galv_i8_*, galv_expert_*), of whichever context, has run out on this
  * device since this context was made or last looked (GALV_ERR_TIMEOUT: the results since then are void; GALV_OK otherwise).  Not for stream capture.

@@ -133,16 +133,16 @@ def load_library() -> C.CDLL:
     lib.galv_i8_linear_workspace_bytes.argtypes, lib.galv_i8_linear_workspace_bytes.restype = [i64, i64], sz
     lib.galv_i8_linear.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, vp, vp, vp, i64, i32, vp, sz, vp]
     for f in (lib.galv_expert_matmul_workspace_bytes, lib.galv_expert_input_grad_workspace_bytes):
-        f.argtypes, f.restype = [vp, i64, i32, i64, i64, vp, i64, vp], sz
-    lib.galv_expert_matmul.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, vp, vp, i64, i32, vp, sz, vp]
-    lib.galv_expert_input_grad.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, vp, i64, i32, vp, sz, vp]
+        f.argtypes, f.restype = [vp, i64, i32, i64, i64, vp, i64, vp, i64], sz
+    lib.galv_expert_matmul.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, i64, vp, vp, i64, i32, vp, sz, vp]
+    lib.galv_expert_input_grad.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, i64, vp, i64, i32, vp, sz, vp]
     lib.galv_expert_weight_grad_workspace_bytes.argtypes = [vp, i64, i32, i64, i64, vp, i64, vp, i64]
     lib.galv_expert_weight_grad_workspace_bytes.restype = sz
     lib.galv_expert_weight_grad.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, i64, i32, vp, vp, i32, vp, sz, vp]
     lib.galv_expert_bias_grad.argtypes = [vp, i64, i32, i64, vp, vp, i64, i32, vp, i32, vp]
-    lib.galv_expert_backward_workspace_bytes.argtypes = [vp, i64, i32, i64, i64, vp, i64, vp, i64, vp]
+    lib.galv_expert_backward_workspace_bytes.argtypes = [vp, i64, i32, i64, i64, vp, i64, vp, i64, vp, i64]
     lib.galv_expert_backward_workspace_bytes.restype = sz
-    lib.galv_expert_backward.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, i64, vp, i32, vp, i64, vp, vp, vp, sz, vp]
+    lib.galv_expert_backward.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -168,6 +168,18 @@ def _matrix(t):
     stride, step = t.stride()
     assert step == 1 or t.shape[1] <= 1, "matrices crossing the boundary have contiguous rows"
     return t.data_ptr(), max(stride, t.shape[1]) if t.shape[0] <= 1 else stride
+
+
+def _matrices(t):
+    """The same of a 3-D tensor of matrices one behind the other."""
+    if t is None:
+        return None, 0
+    count, rows, cols = t.shape
+    first, stride, step = t.stride()
+    if rows <= 1:
+        stride = first if count > 1 else cols
+    assert (step == 1 or cols <= 1) and stride >= cols and (first == rows * stride or count <= 1), "matrices crossing the boundary have contiguous rows, one distance apart"
+    return t.data_ptr(), stride
 
 
 def _ws(t):
@@ -421,19 +433,19 @@ class Galv:
             self._check(rc)
 
     def galv_expert_matmul_workspace_bytes(self, x, w) -> int:
-        return self.lib.galv_expert_matmul_workspace_bytes(self.h, x.shape[0], *w.shape, *_matrix(x), w.data_ptr())
+        return self.lib.galv_expert_matmul_workspace_bytes(self.h, x.shape[0], *w.shape, *_matrix(x), *_matrices(w))
 
     def galv_expert_matmul(self, ends, x, w, bias, y, workspace):
-        rc = self.lib.galv_expert_matmul(self.h, x.shape[0], *w.shape, _at(ends), *_matrix(x), w.data_ptr(), _at(bias), *_matrix(y), _DTYPES[y.dtype],
+        rc = self.lib.galv_expert_matmul(self.h, x.shape[0], *w.shape, _at(ends), *_matrix(x), *_matrices(w), _at(bias), *_matrix(y), _DTYPES[y.dtype],
                                          *_ws(workspace), _raw_stream(self.device))
         if rc:
             self._check(rc)
 
     def galv_expert_input_grad_workspace_bytes(self, dy, w) -> int:
-        return self.lib.galv_expert_input_grad_workspace_bytes(self.h, dy.shape[0], *w.shape, *_matrix(dy), w.data_ptr())
+        return self.lib.galv_expert_input_grad_workspace_bytes(self.h, dy.shape[0], *w.shape, *_matrix(dy), *_matrices(w))
 
     def galv_expert_input_grad(self, ends, dy, w, dx, workspace):
-        rc = self.lib.galv_expert_input_grad(self.h, dy.shape[0], *w.shape, _at(ends), *_matrix(dy), w.data_ptr(), *_matrix(dx), _DTYPES[dx.dtype],
+        rc = self.lib.galv_expert_input_grad(self.h, dy.shape[0], *w.shape, _at(ends), *_matrix(dy), *_matrices(w), *_matrix(dx), _DTYPES[dx.dtype],
                                              *_ws(workspace), _raw_stream(self.device))
         if rc:
             self._check(rc)
@@ -455,10 +467,10 @@ class Galv:
 
     def galv_expert_backward(self, shape, ends, dy, x, w, dx, dw, db, room):
         """shape: (experts, n, k); x, w, dx, dw, db or None; room(bytes): a workspace of so many."""
-        rows, dm, xm = dy.shape[0], _matrix(dy), (None, 0) if x is None else _matrix(x)
-        size = self.lib.galv_expert_backward_workspace_bytes(self.h, rows, *shape, *dm, *xm, _at(w))
+        rows, dm, xm, wm = dy.shape[0], _matrix(dy), (None, 0) if x is None else _matrix(x), _matrices(w)
+        size = self.lib.galv_expert_backward_workspace_bytes(self.h, rows, *shape, *dm, *xm, *wm)
         ws = room(size) if size else None
-        rc = self.lib.galv_expert_backward(self.h, rows, *shape, _at(ends), *dm, *xm, _at(w), _DTYPES[dy.dtype], *((None, 0) if dx is None else _matrix(dx)), _at(dw), _at(db),
+        rc = self.lib.galv_expert_backward(self.h, rows, *shape, _at(ends), *dm, *xm, *wm, _DTYPES[dy.dtype], *((None, 0) if dx is None else _matrix(dx)), _at(dw), _at(db),
                                            *_ws(ws), _raw_stream(self.device))
         if rc:
             self._check(rc)

@@ -510,13 +510,14 @@ namespace {
 
 // What the three gradients need one after the other: dy in rows that bulk copies can take, read by all, and behind it what any of them needs for itself.
 struct BackwardPlan { size_t dy, total; int64_t stride; };
-BackwardPlan backward_plan(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const void* w)
+BackwardPlan backward_plan(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const void* w,
+                           int64_t w_stride)
 {
     BackwardPlan p;
     p.dy = plan_of(rows, n, k, dy, dy_stride, x, x_stride).dy;
     p.stride = p.dy ? (n + 7) / 8 * 8 : dy_stride;
     const void* const at = p.dy ? nullptr : dy;           // moved rows lie on 256 bytes
-    const size_t a = w ? galv_expert_input_grad_workspace_bytes(ctx, rows, experts, n, k, at, p.stride, w) : 0;
+    const size_t a = w ? galv_expert_input_grad_workspace_bytes(ctx, rows, experts, n, k, at, p.stride, w, w_stride) : 0;
     const size_t b = x ? galv_expert_weight_grad_workspace_bytes(ctx, rows, experts, n, k, at, p.stride, x, x_stride) : 0;
     p.total = p.dy + (a > b ? a : b);
     return p;
@@ -525,14 +526,14 @@ BackwardPlan backward_plan(const galv_ctx* ctx, int64_t rows, int32_t experts, i
 }  // namespace
 
 extern "C" size_t galv_expert_backward_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
-                                                       const void* w)
+                                                       const void* w, int64_t w_stride)
 {
     if (!ctx || !mx_size_ok(rows, n) || !mx_size_ok(rows, k) || rows == 0 || experts < 1 || experts > kExpertsMost) return 0;
-    return backward_plan(ctx, rows, experts, n, k, dy, dy_stride, x, x_stride, w).total;
+    return backward_plan(ctx, rows, experts, n, k, dy, dy_stride, x, x_stride, w, w_stride).total;
 }
 
 extern "C" int galv_expert_backward(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
-                                    const void* w, int32_t dtype, void* dx, int64_t dx_stride, void* dw, void* db, void* workspace, size_t workspace_bytes, void* stream)
+                                    const void* w, int64_t w_stride, int32_t dtype, void* dx, int64_t dx_stride, void* dw, void* db, void* workspace, size_t workspace_bytes, void* stream)
 {
     if (!ctx) return GALV_ERR_INVALID_ARG;
     if (!sizes_ok(rows, experts, n, k, ends, dtype, dtype)) return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_expert_backward: sizes, number of experts or type outside the limits");
@@ -540,7 +541,7 @@ extern "C" int galv_expert_backward(galv_ctx* ctx, int64_t rows, int32_t experts
         return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_expert_backward: NULL or misaligned pointer, or a row stride below the row's length");
     char* ws = (char*)workspace;
     if (rows > 0) {
-        const BackwardPlan p = backward_plan(ctx, rows, experts, n, k, dy, dy_stride, dw ? x : nullptr, x_stride, dx ? w : nullptr);
+        const BackwardPlan p = backward_plan(ctx, rows, experts, n, k, dy, dy_stride, dw ? x : nullptr, x_stride, dx ? w : nullptr, w_stride);
         if (p.total && (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < p.total))
             return galv_set_error(ctx, GALV_ERR_WORKSPACE, "galv_expert_backward: workspace NULL, misaligned or too small");
         if (p.dy) {
@@ -556,7 +557,7 @@ extern "C" int galv_expert_backward(galv_ctx* ctx, int64_t rows, int32_t experts
         }
     }
     int rc = GALV_OK;
-    if (dx) rc = galv_expert_input_grad(ctx, rows, experts, n, k, ends, dy, dy_stride, w, dx, dx_stride, dtype, ws, workspace_bytes, stream);
+    if (dx) rc = galv_expert_input_grad(ctx, rows, experts, n, k, ends, dy, dy_stride, w, w_stride, dx, dx_stride, dtype, ws, workspace_bytes, stream);
     if (rc == GALV_OK && dw) rc = galv_expert_weight_grad(ctx, rows, experts, n, k, ends, dy, dy_stride, x, x_stride, dtype, nullptr, dw, dtype, ws, workspace_bytes, stream);
     if (rc == GALV_OK && db) rc = galv_expert_bias_grad(ctx, rows, experts, n, ends, dy, dy_stride, dtype, db, dtype, stream);
     return rc;

@@ -450,11 +450,11 @@ int smem_of(int experts) { return 1024 + kRing + kOutBytes + 256 + 8 * (experts 
 
 // Where the operands of a product in 16 bits that bulk copies cannot take as they are go in the workspace.
 struct AlignPlan { size_t x, w, total; };
-AlignPlan align_plan(int64_t rows, int64_t x_cols, const void* x, int64_t x_stride, int64_t experts, int64_t n, int64_t k, const void* w)
+AlignPlan align_plan(int64_t rows, int64_t x_cols, const void* x, int64_t x_stride, int64_t experts, int64_t n, int64_t k, const void* w, int64_t w_stride)
 {
     AlignPlan p;
     p.x = mx_rows16(x, x_stride, GALV_BF16) && x_stride * 2 < ((int64_t)1 << 40) ? 0 : up((size_t)rows * ((x_cols + 7) / 8 * 8) * 2);
-    p.w = mx_rows16(w, k, GALV_BF16) ? 0 : up((size_t)experts * n * ((k + 7) / 8 * 8) * 2);
+    p.w = mx_rows16(w, w_stride, GALV_BF16) && n * w_stride * 2 < ((int64_t)1 << 40) ? 0 : up((size_t)experts * n * ((k + 7) / 8 * 8) * 2);
     p.total = p.x + p.w;
     return p;
 }
@@ -518,7 +518,7 @@ bool units_fit(int64_t rows, int64_t experts, int64_t n) { return (rows / 32 + e
 
 // y = x w^T or x w by expert, both in 16 bits.  across: w [experts][cols of x][n], summed across its rows.
 int product16(galv_ctx* ctx, const char* name, bool across, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* x, int64_t x_stride, const void* w,
-              const void* bias, void* y, int64_t y_stride, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream)
+              int64_t w_stride, const void* bias, void* y, int64_t y_stride, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream)
 {
     const int64_t w_rows = across ? k : n, w_cols = across ? n : k;
     auto wrong = [&](int code, const char* what) {
@@ -530,17 +530,17 @@ int product16(galv_ctx* ctx, const char* name, bool across, int64_t rows, int32_
         !units_fit(rows, experts, n))
         return wrong(GALV_ERR_INVALID_ARG, "sizes, number of experts or type outside the limits");
     if (rows == 0) return GALV_OK;
-    if (!mx_matrix_ok(x, x_stride, k, dtype) || !mx_matrix_ok(w, w_cols, w_cols, dtype) || !mx_matrix_ok(y, y_stride, n, dtype) || (bias && !mx_aligned(bias, 2)) ||
+    if (!mx_matrix_ok(x, x_stride, k, dtype) || !mx_matrix_ok(w, w_stride, w_cols, dtype) || !mx_matrix_ok(y, y_stride, n, dtype) || (bias && !mx_aligned(bias, 2)) ||
         (ends && !mx_aligned(ends, 4)))
         return wrong(GALV_ERR_INVALID_ARG, "NULL or misaligned pointer, or a row stride below the row's length");
-    const AlignPlan p = align_plan(rows, k, x, x_stride, experts, w_rows, w_cols, w);
+    const AlignPlan p = align_plan(rows, k, x, x_stride, experts, w_rows, w_cols, w, w_stride);
     if (p.total && (!workspace || !mx_aligned(workspace, 256) || workspace_bytes < p.total)) return wrong(GALV_ERR_WORKSPACE, "workspace NULL, misaligned or too small");
     const int may = mx_may_run(ctx, "experts' product: the library's host memory could not be registered", "experts' product: a bounded wait of an earlier product ran out");
     if (may != GALV_OK) return may;
     MxDevice dev(ctx);
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
     cudaStream_t st = (cudaStream_t)stream;
-    int64_t w_pitch = w_cols;
+    int64_t w_pitch = w_stride;
     if (p.x) {
         galv_align_rows(ctx, rows, k, x, x_stride, workspace, (k + 7) / 8 * 8, st);
         x = workspace;
@@ -549,7 +549,7 @@ int product16(galv_ctx* ctx, const char* name, bool across, int64_t rows, int32_
     if (p.w) {
         void* const to = (char*)workspace + p.x;
         w_pitch = (w_cols + 7) / 8 * 8;
-        galv_align_rows(ctx, (int64_t)experts * w_rows, w_cols, w, w_cols, to, w_pitch, st);
+        galv_align_rows(ctx, (int64_t)experts * w_rows, w_cols, w, w_stride, to, w_pitch, st);
         w = to;
     }
     const CUtensorMapDataType type = dtype == GALV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
@@ -609,30 +609,32 @@ int whole_may(galv_ctx* ctx) { return mx_may_run(ctx, "8-bit product: the librar
 
 }  // namespace
 
-extern "C" size_t galv_expert_matmul_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* x, int64_t x_stride, const void* w)
+extern "C" size_t galv_expert_matmul_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* x, int64_t x_stride, const void* w,
+                                                     int64_t w_stride)
 {
     if (!ctx || !mx_size_ok(rows, n) || !mx_size_ok(rows, k) || rows == 0 || experts < 1 || experts > kExpertsMost) return 0;
-    return align_plan(rows, k, x, x_stride, experts, n, k, w).total;
+    return align_plan(rows, k, x, x_stride, experts, n, k, w, w_stride).total;
 }
 
-extern "C" int galv_expert_matmul(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* x, int64_t x_stride, const void* w, const void* bias,
-                                  void* y, int64_t y_stride, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream)
+extern "C" int galv_expert_matmul(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* x, int64_t x_stride, const void* w, int64_t w_stride,
+                                  const void* bias, void* y, int64_t y_stride, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream)
 {
     if (!ctx) return GALV_ERR_INVALID_ARG;
-    return product16(ctx, "galv_expert_matmul", false, rows, experts, n, k, ends, x, x_stride, w, bias, y, y_stride, dtype, workspace, workspace_bytes, stream);
+    return product16(ctx, "galv_expert_matmul", false, rows, experts, n, k, ends, x, x_stride, w, w_stride, bias, y, y_stride, dtype, workspace, workspace_bytes, stream);
 }
 
-extern "C" size_t galv_expert_input_grad_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* w)
+extern "C" size_t galv_expert_input_grad_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* w,
+                                                         int64_t w_stride)
 {
     if (!ctx || !mx_size_ok(rows, n) || !mx_size_ok(rows, k) || rows == 0 || experts < 1 || experts > kExpertsMost) return 0;
-    return align_plan(rows, n, dy, dy_stride, experts, n, k, w).total;
+    return align_plan(rows, n, dy, dy_stride, experts, n, k, w, w_stride).total;
 }
 
-extern "C" int galv_expert_input_grad(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* dy, int64_t dy_stride, const void* w, void* dx,
-                                      int64_t dx_stride, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream)
+extern "C" int galv_expert_input_grad(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* dy, int64_t dy_stride, const void* w, int64_t w_stride,
+                                      void* dx, int64_t dx_stride, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream)
 {
     if (!ctx) return GALV_ERR_INVALID_ARG;
-    return product16(ctx, "galv_expert_input_grad", true, rows, experts, k, n, ends, dy, dy_stride, w, nullptr, dx, dx_stride, dtype, workspace, workspace_bytes, stream);
+    return product16(ctx, "galv_expert_input_grad", true, rows, experts, k, n, ends, dy, dy_stride, w, w_stride, nullptr, dx, dx_stride, dtype, workspace, workspace_bytes, stream);
 }
 
 extern "C" int galv_i8_matmul(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const int8_t* x_codes, const float* x_scales, const int8_t* w_codes,

@@ -32,6 +32,17 @@ def _whole(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
     return t if t is None or (t.is_contiguous() and not t.is_neg()) else t.detach().resolve_neg().contiguous()
 
 
+def _apart(weight: torch.Tensor) -> torch.Tensor:
+    """Weights whose rows are contiguous and one distance apart (a copy where they are not): rows kept on 16-byte boundaries are used as they lie."""
+    if weight.is_contiguous() and not weight.is_neg():
+        return weight
+    experts, n, k = weight.shape
+    first, stride, step = weight.stride()
+    if weight.is_neg() or step != 1 or stride < k or first != n * stride or n == 1:
+        return _whole(weight)
+    return weight
+
+
 def _weight(weight: torch.Tensor, dtype: torch.dtype):
     if weight.dim() != 3 or weight.dtype != dtype or weight.shape[1] < 1 or weight.shape[2] < 1:
         raise ValueError(f"weight is [experts][columns of y][columns of x] of {dtype}, not {tuple(weight.shape)} of {weight.dtype}")
@@ -80,20 +91,42 @@ def matmul(x: Union[torch.Tensor, i8.Packed], weight: Union[torch.Tensor, i8.Pac
     if isinstance(weight, i8.Packed):
         _kind(x.dtype, "x")
         return _products(_rows(x, "x"), weight, ends, bias, x.dtype)
-    _kind(x.dtype, "x", _SHORT)
-    _weight(weight, x.dtype)
-    experts, n, k = weight.shape
+    return _forward(x, weight, ends, bias)[0]
+
+
+def _forward(x: torch.Tensor, weight: torch.Tensor, ends: torch.Tensor, bias: Optional[torch.Tensor]):
+    """y, and what was multiplied: x and weight as they lie, and the workspace in which the library has moved either to 16-byte boundaries."""
+    dtype, device, shape = x.dtype, x.device, weight.shape
+    _kind(dtype, "x", _SHORT)
+    _weight(weight, dtype)
+    experts, n, k = shape
     _ends(ends, experts)
     x = _rows(x, "x")
-    if x.shape[1] != k:
+    rows, cols = x.shape
+    if cols != k:
         raise ValueError(f"x of shape {tuple(x.shape)} beside weights of {k} columns")
-    i8._bias(bias, (experts, n), x.dtype)
-    g = _on(x.device, weight.device, ends.device, _device(bias))
-    y = torch.empty(x.shape[0], n, dtype=x.dtype, device=x.device)
-    weight = _whole(weight)
+    i8._bias(bias, (experts, n), dtype)
+    g = _on(device, weight.device, ends.device, _device(bias))
+    y = torch.empty(rows, n, dtype=dtype, device=device)
+    weight = _apart(weight)
     size = g.galv_expert_matmul_workspace_bytes(x, weight)
-    g.galv_expert_matmul(_whole(ends), x, weight, _whole(bias), y, _bytes(size, x.device) if size else None)
-    return y
+    ws = _bytes(size, device) if size else None
+    g.galv_expert_matmul(_whole(ends), x, weight, _whole(bias), y, ws)
+    return y, x, weight, ws
+
+
+def _moved(x: torch.Tensor, weight: torch.Tensor, ws: Optional[torch.Tensor]):
+    """Of a forward product: x and weight on 16-byte boundaries, where they were moved to such in its workspace, else as they are."""
+    if ws is None:
+        return x, weight
+    (rows, k), (experts, n, _) = x.shape, weight.shape
+    pitch, at, both = (k + 7) // 8 * 8, 0, ws.view(x.dtype)
+    start, stride = gb._matrix(x)
+    if start % 16 or stride % 8 or stride >= 1 << 39:
+        x, at = both.as_strided((rows, k), (pitch, 1)), (rows * pitch * 2 + 255 & ~255) // 2
+    if at < both.numel():
+        weight = both.as_strided((experts, n, k), (n * pitch, pitch, 1), at)
+    return x, weight
 
 
 def input_grad(dy: torch.Tensor, weight: torch.Tensor, ends: torch.Tensor) -> torch.Tensor:
@@ -107,7 +140,7 @@ def input_grad(dy: torch.Tensor, weight: torch.Tensor, ends: torch.Tensor) -> to
         raise ValueError(f"dy of shape {tuple(dy.shape)} beside weights of {n} rows")
     g = _on(dy.device, weight.device, ends.device)
     dx = torch.empty(dy.shape[0], k, dtype=dy.dtype, device=dy.device)
-    weight = _whole(weight)
+    weight = _apart(weight)
     size = g.galv_expert_input_grad_workspace_bytes(dy, weight)
     g.galv_expert_input_grad(_whole(ends), dy, weight, dx, _bytes(size, dy.device) if size else None)
     return dx
@@ -161,8 +194,10 @@ class _Linear(torch.autograd.Function):
     @staticmethod
     @_as_typed
     def forward(ctx, x, weight, ends, bias):
-        y = matmul(x, weight, ends, bias)
+        y, lies, held, ws = _forward(x, weight, ends, bias)
         need = ctx.needs_input_grad
+        if ws is not None:
+            x, weight = _moved(lies, held, ws)            # the backward pass need not move them again
         ctx.save_for_backward(x if need[1] else None, weight if need[0] else None, ends)
         ctx.shape = weight.shape
         return y
@@ -178,11 +213,12 @@ class _Linear(torch.autograd.Function):
         dx = torch.empty(dy.shape[0], k, dtype=dtype, device=device) if need_x else None
         dw = torch.empty(ctx.shape, dtype=dtype, device=device) if need_w else None
         db = torch.empty(experts, n, dtype=dtype, device=device) if need_b else None
-        _on(device).galv_expert_backward(ctx.shape, _whole(ends), dy, _rows(x, "x") if need_w else None, _whole(weight) if need_x else None, dx, dw, db,
+        _on(device).galv_expert_backward(ctx.shape, _whole(ends), dy, _rows(x, "x") if need_w else None, _apart(weight) if need_x else None, dx, dw, db,
                                          lambda size: _bytes(size, device))
         return dx, dw, None, db
 
 
 def linear(x: torch.Tensor, weight: torch.Tensor, ends: torch.Tensor, bias: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """x weight[e]^T + bias[e] for each row of x and its expert e, in 16 bits, with gradients for x, weight and bias (where they are taken)."""
+    """x weight[e]^T + bias[e] for each row of x and its expert e, in 16 bits, with gradients for x, weight and bias (where they are taken).  Of operands whose rows do not start
+    on 16-byte boundaries the copies that the forward product takes are kept for the backward pass."""
     return _Linear.apply(x, weight, ends, bias)

@@ -76,11 +76,12 @@ def clean(t, behind):
 
 def test_calls_without_a_context_are_refused():
     lib = gb.load_library()
-    assert lib.galv_expert_matmul(None, 1, 1, 1, 1, None, None, 1, None, None, None, 1, 1, None, 0, None) == gb.ERR_INVALID_ARG
-    assert lib.galv_expert_input_grad(None, 1, 1, 1, 1, None, None, 1, None, None, 1, 1, None, 0, None) == gb.ERR_INVALID_ARG
+    assert lib.galv_expert_matmul(None, 1, 1, 1, 1, None, None, 1, None, 1, None, None, 1, 1, None, 0, None) == gb.ERR_INVALID_ARG
+    assert lib.galv_expert_input_grad(None, 1, 1, 1, 1, None, None, 1, None, 1, None, 1, 1, None, 0, None) == gb.ERR_INVALID_ARG
     assert lib.galv_expert_weight_grad(None, 1, 1, 1, 1, None, None, 1, None, 1, 1, None, None, 1, None, 0, None) == gb.ERR_INVALID_ARG
     assert lib.galv_expert_bias_grad(None, 1, 1, 1, None, None, 1, 1, None, 1, None) == gb.ERR_INVALID_ARG
-    assert lib.galv_expert_matmul_workspace_bytes(None, 1, 1, 1, 1, None, 1, None) == lib.galv_expert_weight_grad_workspace_bytes(None, 1, 1, 1, 1, None, 1, None, 1) == 0
+    assert lib.galv_expert_backward(None, 1, 1, 1, 1, None, None, 1, None, 1, None, 1, 1, None, 1, None, None, None, 0, None) == gb.ERR_INVALID_ARG
+    assert lib.galv_expert_matmul_workspace_bytes(None, 1, 1, 1, 1, None, 1, None, 1) == lib.galv_expert_weight_grad_workspace_bytes(None, 1, 1, 1, 1, None, 1, None, 1) == 0
 
 
 B = torch.bfloat16
@@ -271,6 +272,8 @@ def test_strides_and_views(dtype):
         assert all(torch.equal(a, b) for a, b in zip(got, want))
     one = dy[:1].expand(len(x), n)
     assert torch.equal(experts.bias_grad(one, ends), experts.bias_grad(one.contiguous(), ends)) and torch.equal(experts.weight_grad(one, x, ends), experts.weight_grad(one.contiguous(), x, ends))
+    padded = torch.full((3, n, k + 8), float("nan"), dtype=w.dtype, device="cuda")[:, :, :k].copy_(w)      # rows further apart than they are long
+    assert torch.equal(experts.matmul(x, padded, ends, bias), want[0]) and torch.equal(experts.input_grad(dy, padded, ends), want[1])
     strided = torch.zeros(6, dtype=torch.int32, device="cuda")
     strided[::2] = ends
     assert torch.equal(experts.matmul(x, w, strided[::2], bias), want[0])
@@ -303,9 +306,10 @@ def test_gradients_are_those_of_the_function(dtype):
 
 
 @gpu
-def test_linear_takes_only_the_gradients_that_are_asked_for():
+@pytest.mark.parametrize("n,k,pad", [(24, 40, 0), (33, 41, 0), (33, 41, 7), (24, 40, 3), (24, 45, 3), (1, 1, 0)])
+def test_linear_takes_only_the_gradients_that_are_asked_for(n, k, pad):
     counts = [10, 0, 30]
-    x, w, dy, b = inputs(counts, 2, 24, 40, "bf16")
+    x, w, dy, b = inputs(counts, 2, n, k, "bf16", pad)
     x = x.nan_to_num(0.0)
     ends = ends_of(counts)
     want = experts.matmul(x, w, ends, b), experts.input_grad(dy, w, ends), experts.weight_grad(dy, x, ends), experts.bias_grad(dy, ends)
