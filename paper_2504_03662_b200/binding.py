@@ -402,8 +402,8 @@ class Galv:
         """Waits that have run out on the device so far; waits for nothing."""
         return self.lib.galv_mx_timeouts(self.h)[0]
 
-    # Rows of 8-bit integers (codes int8 [rows][pitch], scales fp32 [rows], tensors or addresses) and experts' products (ends: int32 tensor, or None for one
-    # expert that has all rows; weights [experts][n][k] contiguous).
+    # Rows of 8-bit integers (codes int8 [rows][pitch], scales fp32 [rows]) and experts' products (ends: int32 tensor, or None for one expert that has all
+    # rows; weights [experts][n][k], rows one distance apart).  Products and gradients take matrices as (address, row stride) of _matrix and _matrices, a type as its number.
 
     def galv_i8_pack(self, x, codes, scales):
         rc = self.lib.galv_i8_pack(self.h, *x.shape, *_matrix(x), _DTYPES[x.dtype], _address(codes), _address(scales), _raw_stream(self.device))
@@ -415,29 +415,26 @@ class Galv:
         if rc:
             self._check(rc)
 
-    def galv_i8_matmul(self, experts, k, ends, x_codes, x_scales, w_codes, w_scales, bias, y):
-        rows, n = y.shape
-        rc = self.lib.galv_i8_matmul(self.h, rows, experts, n, k, _at(ends), _address(x_codes), _address(x_scales), _address(w_codes), _address(w_scales), _at(bias),
-                                     *_matrix(y), _DTYPES[y.dtype], _raw_stream(self.device))
+    def galv_i8_matmul(self, rows, experts, n, k, ends, x_codes, x_scales, w_codes, w_scales, bias, y, dtype):
+        rc = self.lib.galv_i8_matmul(self.h, rows, experts, n, k, _at(ends), x_codes.data_ptr(), x_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), _at(bias),
+                                     *y, dtype, _raw_stream(self.device))
         if rc:
             self._check(rc)
 
     def galv_i8_linear_workspace_bytes(self, rows, k) -> int:
         return self.lib.galv_i8_linear_workspace_bytes(rows, k)
 
-    def galv_i8_linear(self, experts, ends, x, w_codes, w_scales, bias, y, workspace):
-        rows, n = y.shape
-        rc = self.lib.galv_i8_linear(self.h, rows, experts, n, x.shape[1], _at(ends), *_matrix(x), _address(w_codes), _address(w_scales), _at(bias), *_matrix(y),
-                                     _DTYPES[y.dtype], *_ws(workspace), _raw_stream(self.device))
+    def galv_i8_linear(self, rows, experts, n, k, ends, x, w_codes, w_scales, bias, y, dtype, workspace):
+        rc = self.lib.galv_i8_linear(self.h, rows, experts, n, k, _at(ends), *x, w_codes.data_ptr(), w_scales.data_ptr(), _at(bias), *y, dtype,
+                                     *_ws(workspace), _raw_stream(self.device))
         if rc:
             self._check(rc)
 
-    def galv_expert_matmul_workspace_bytes(self, x, w) -> int:
-        return self.lib.galv_expert_matmul_workspace_bytes(self.h, x.shape[0], *w.shape, *_matrix(x), *_matrices(w))
+    def galv_expert_matmul_workspace_bytes(self, rows, experts, n, k, x, w) -> int:
+        return self.lib.galv_expert_matmul_workspace_bytes(self.h, rows, experts, n, k, *x, *w)
 
-    def galv_expert_matmul(self, ends, x, w, bias, y, workspace):
-        rc = self.lib.galv_expert_matmul(self.h, x.shape[0], *w.shape, _at(ends), *_matrix(x), *_matrices(w), _at(bias), *_matrix(y), _DTYPES[y.dtype],
-                                         *_ws(workspace), _raw_stream(self.device))
+    def galv_expert_matmul(self, rows, experts, n, k, ends, x, w, bias, y, dtype, workspace):
+        rc = self.lib.galv_expert_matmul(self.h, rows, experts, n, k, _at(ends), *x, *w, _at(bias), *y, dtype, *_ws(workspace), _raw_stream(self.device))
         if rc:
             self._check(rc)
 

@@ -58,18 +58,18 @@ def _products(x: torch.Tensor, weight: i8.Packed, ends: torch.Tensor, bias, dtyp
     _count(experts)
     if weight.rows % experts:
         raise ValueError(f"weights of {experts} experts in {weight.rows} rows")
-    n = weight.rows // experts
-    cols = x.cols if isinstance(x, i8.Packed) else x.shape[1]
+    n, held = weight.rows // experts, isinstance(x, i8.Packed)
+    rows, cols = (x.rows, x.cols) if held else x.shape
     i8._beside(cols, weight)
     i8._bias(bias, (experts, n), dtype)
-    g = _on(x.device, weight.device, ends.device, _device(bias))
-    ends, bias = _whole(ends), _whole(bias)
-    if isinstance(x, i8.Packed):
-        y = torch.empty(x.rows, n, dtype=dtype, device=x.device)
-        g.galv_i8_matmul(experts, cols, ends, x.codes, x.scales, weight.codes, weight.scales, bias, y)
+    device = x.device
+    g = _on(device, weight.device, ends.device, _device(bias))
+    y = torch.empty(rows, n, dtype=dtype, device=device)
+    out, number = (y.data_ptr(), n), gb._DTYPES[dtype]
+    if held:
+        g.galv_i8_matmul(rows, experts, n, cols, _whole(ends), x.codes, x.scales, weight.codes, weight.scales, _whole(bias), out, number)
     else:
-        y = torch.empty(x.shape[0], n, dtype=dtype, device=x.device)
-        g.galv_i8_linear(experts, ends, x, weight.codes, weight.scales, bias, y, _bytes(i8._room(*x.shape), x.device))
+        g.galv_i8_linear(rows, experts, n, cols, _whole(ends), gb._matrix(x), weight.codes, weight.scales, _whole(bias), out, number, _bytes(i8._room(rows, cols), device))
     return y
 
 
@@ -109,9 +109,12 @@ def _forward(x: torch.Tensor, weight: torch.Tensor, ends: torch.Tensor, bias: Op
     g = _on(device, weight.device, ends.device, _device(bias))
     y = torch.empty(rows, n, dtype=dtype, device=device)
     weight = _apart(weight)
-    size = g.galv_expert_matmul_workspace_bytes(x, weight)
-    ws = _bytes(size, device) if size else None
-    g.galv_expert_matmul(_whole(ends), x, weight, _whole(bias), y, ws)
+    xm, wm = gb._matrix(x), gb._matrices(weight)
+    ws = None
+    if (xm[0] | wm[0]) % 16 or (xm[1] | wm[1]) % 8 or n * wm[1] >= 1 << 39 or xm[1] >= 1 << 39:      # else nothing has to be moved
+        size = g.galv_expert_matmul_workspace_bytes(rows, experts, n, k, xm, wm)
+        ws = _bytes(size, device) if size else None
+    g.galv_expert_matmul(rows, experts, n, k, _whole(ends), xm, wm, _whole(bias), (y.data_ptr(), n), gb._DTYPES[dtype], ws)
     return y, x, weight, ws
 
 

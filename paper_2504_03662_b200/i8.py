@@ -85,7 +85,7 @@ def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, bias: Opti
     _bias(bias, (b.rows,), dtype)
     g = _on(a.device, b.device, _device(bias))
     y = torch.empty(a.rows, b.rows, dtype=dtype, device=a.device)
-    g.galv_i8_matmul(1, a.cols, None, a.codes, a.scales, b.codes, b.scales, _vector(bias), y)
+    g.galv_i8_matmul(a.rows, 1, b.rows, a.cols, None, a.codes, a.scales, b.codes, b.scales, _vector(bias), (y.data_ptr(), b.rows), gb._DTYPES[dtype])
     return y
 
 
@@ -97,10 +97,10 @@ def linear(x: torch.Tensor, weight: Packed, bias: Optional[torch.Tensor] = None)
         raise ValueError(f"x has a last axis of one number or more, not the shape {tuple(shape)}")
     _beside(shape[-1], weight)
     _bias(bias, (weight.rows,), dtype)
-    device = x.device
+    device, n = x.device, weight.rows
     g = _on(device, weight.device, _device(bias))
     flat = _rows(x if len(shape) == 2 else x.reshape(-1, shape[-1]), "x")
     rows, cols = flat.shape
-    y = torch.empty(rows, weight.rows, dtype=dtype, device=device)
-    g.galv_i8_linear(1, None, flat, weight.codes, weight.scales, _vector(bias), y, _bytes(_room(rows, cols), device))
-    return y if len(shape) == 2 else y.view(*shape[:-1], weight.rows)
+    y = torch.empty(rows, n, dtype=dtype, device=device)
+    g.galv_i8_linear(rows, 1, n, cols, None, gb._matrix(flat), weight.codes, weight.scales, _vector(bias), (y.data_ptr(), n), gb._DTYPES[dtype], _bytes(_room(rows, cols), device))
+    return y if len(shape) == 2 else y.view(*shape[:-1], n)
