@@ -484,7 +484,7 @@ void configure(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* attr, unsigned grid
 template <int K, typename O>
 cudaError_t launch_few(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap& pm, const ProductArgs& a, bool in_front, cudaStream_t st)
 {
-    cudaError_t e = cudaFuncSetAttribute(expert_few_kernel<K, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
+    const cudaError_t e = cudaFuncSetAttribute(expert_few_kernel<K, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
     if (e != cudaSuccess) return e;
     const int tiles = (int)((a.n + 127) / 128);
     const long long units = tiles * (long long)(a.rows < a.experts ? a.rows : a.experts);
@@ -553,9 +553,9 @@ int product16(galv_ctx* ctx, const char* name, bool across, int64_t rows, int32_
         w = to;
     }
     const CUtensorMapDataType type = dtype == GALV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    CUtensorMap wm, xm, pm;
+    CUtensorMap wm, xm = {}, pm;                          // xm is not read where there are few rows
     cudaError_t e = galv_map_3d(&wm, type, w, experts, w_rows, w_cols, w_pitch * 2, across ? 64 : kHalf, 64);
-    if (e == cudaSuccess) e = galv_mx_map(&xm, type, x, rows, k, x_stride * 2, kBox, 64, true);
+    if (e == cudaSuccess && (across || rows > kFewRows)) e = galv_mx_map(&xm, type, x, rows, k, x_stride * 2, kBox, 64, true);
     if (e == cudaSuccess) e = galv_mx_map(&pm, type, x, rows, k, x_stride * 2, kPart, 64, true);
     if (e != cudaSuccess) return wrong(GALV_ERR_CUDA, "tensor map");
     ProductArgs a;
@@ -585,9 +585,9 @@ int whole_launch(galv_ctx* ctx, const char* name, int64_t rows, int32_t experts,
                  const int8_t* w_codes, const float* w_scales, const void* bias, void* y, int64_t y_stride, int32_t dtype, bool in_front, cudaStream_t st)
 {
     const int64_t pitch = i8_pitch(k);
-    CUtensorMap wm, xm, pm;
+    CUtensorMap wm, xm = {}, pm;
     cudaError_t e = galv_map_3d(&wm, CU_TENSOR_MAP_DATA_TYPE_UINT8, w_codes, experts, n, pitch, pitch, kHalf, kChunkBytes);
-    if (e == cudaSuccess) e = galv_mx_map(&xm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, pitch, pitch, kBox, kChunkBytes, true);
+    if (e == cudaSuccess && rows > kFewRows) e = galv_mx_map(&xm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, pitch, pitch, kBox, kChunkBytes, true);
     if (e == cudaSuccess) e = galv_mx_map(&pm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, pitch, pitch, kPart, kChunkBytes, true);
     if (e != cudaSuccess) {
         char text[100];

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from paper_2504_03662_b200 import binding as gb
-from paper_2504_03662_b200 import i8, mx
+from paper_2504_03662_b200 import experts, i8, mx
 
 from .test_mx import DT, HALF, close, f64, numbers, step
 
@@ -223,6 +223,27 @@ def test_linear_is_pack_and_product(shape, n, dtype):
     wide[:, :shape[-1]] = flat
     assert torch.equal(i8.linear(wide[:, :shape[-1]], w, bias), got.reshape(-1, n))
     assert torch.equal(i8.linear(flat.t().contiguous().t(), w, bias), got.reshape(-1, n))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("m,n,k", [(1, 8192, 8192), (2, 130, 16384), (16, 1000, 8192), (17, 300, 4100), (33, 129, 2050), (48, 2000, 2048), (64, 130, 4096), (64, 5000, 777), (7, 40, 131071), (64, 9000, 8192)])
+def test_few_rows(m, n, k, dtype):
+    """Up to 64 rows, in clusters of one to eight CTAs: packed in the call as by themselves, a row that is no number among them."""
+    x = numbers(m + n, m, k + 1, DT[dtype])
+    x[:, 1 + (7919 * m) % k] *= 40
+    x[m // 2, k // 3:] = 0
+    x[m - 1, k] = float("nan") if m > 1 else 3
+    x = x.cuda()
+    w = held(*_held_numbers(n, n, k)[1:])
+    for rows in (x[:, 1:], x[:, 1:].contiguous()):
+        got = i8.linear(rows, w)
+        want = i8.matmul(i8.pack(rows), w, DT[dtype])
+        assert torch.equal(got.nan_to_num(7.0, 8.0, 9.0), want.nan_to_num(7.0, 8.0, 9.0))
+        assert torch.isnan(got[m - 1]).all() == (m > 1) and not torch.isnan(got[:m - 1]).any()
+    ends = torch.tensor([0, m // 3, m // 3, m - m // 4], dtype=torch.int32, device="cuda")
+    if n % 4 == 0:                                                                  # the same weights as four experts', rows behind the last end
+        assert torch.equal(experts.matmul(rows, w, ends).nan_to_num(7.0, 8.0, 9.0), experts.matmul(i8.pack(rows), w, ends, dtype=DT[dtype]).nan_to_num(7.0, 8.0, 9.0))
 
 
 @gpu
