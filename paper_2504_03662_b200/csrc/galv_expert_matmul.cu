@@ -20,15 +20,13 @@ enum Kind { kForward, kInputGrad, kWhole };               // 16 bits, summed alo
 
 constexpr int kTile = 256, kHalf = kTile / 2, kChunkBytes = 128;
 constexpr int kRowsBytes = kHalf * kChunkBytes;
-// The ring of chunks: 6 of full tiles, up to 10 of smaller ones, whose matrix instructions are over sooner and whose copies are to be as far ahead (8-bit integers, tiles of 64
-// tokens, a chunk: 282 ns with 6).
+// The ring of chunks: 6 of full tiles, up to 10 of smaller ones, whose matrix instructions are over sooner and whose copies are to be as far ahead.
 constexpr int kRing = 12 * kRowsBytes, kStagesMost = 10;
 constexpr int kOutBytes = 8 * 2048;
 constexpr int kBox = 64, kPart = 16;                      // tokens of a copy, and of one where fewer are left
 constexpr int kThreads = 384;
-// What a chunk costs besides its tokens, in tokens.  Measured at 256, 160, 128 and 64 tokens of every tile (2048 x 8192): 411, 320, 285 and 258 ns in 16 bits, 437, 337, 305 and 282
-// in 8-bit integers; of the input gradient, whose weights come in twice as many copies, 450, 360, 330 and 326.
-constexpr float kFixed[3] = {260.f, 440.f, 260.f};
+// What a chunk costs besides its tokens, in tokens.  Measured at 256, 160, 128 and 64 tokens of every tile (2048 x 8192): 396, 285, 257 and 213 ns in 16 bits, 425, 306, 272 and 237 in 8-bit integers.
+constexpr float kFixed = 160.f;
 constexpr int kGroup = 16;                                // tiles of tokens that stay in L2 while their tiles of weights run
 
 struct ProductArgs {
@@ -117,7 +115,7 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
     if (warp == 3) experts_begin(a.ends, a.experts, a.rows, begin);
     __syncthreads();
     if (warp >= 4) {                                      // a size of tiles each: 256, 224 .. 32 rows
-        const float price = experts_price(begin, a.experts, kTile - (warp - 4) * 32, a.tiles_m, stride, kFixed[K]);
+        const float price = experts_price(begin, a.experts, kTile - (warp - 4) * 32, a.tiles_m, stride, kFixed);
         if (lane == 0) prices[warp - 4] = price;
     }
     __syncthreads();
@@ -141,6 +139,8 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
         *(volatile int*)&failed = 1;
         return false;
     };
+    // One lane of a warp waits: eight warps of 32 asking all the time slow the issuing thread's own questions (tiles of 64 tokens: 263 ns a chunk for 213).
+    auto warp_waited = [&](uint32_t bar, uint32_t parity) { return __shfl_sync(0xffffffffu, (int)(lane == 0 && waited(bar, parity)), 0) != 0; };
     Walk w(begin, before, a.tiles_m);
 
     if (warp == 0) {
@@ -226,7 +226,7 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
             const uint32_t buf = done & 1;
             const long long c0 = (long long)w.tm * kTile + rank * kHalf + quad * 32, ch = c0 + lane, at = w.expert * a.n + ch;
             const float bias = a.bias && ch < a.n ? mx_float(((const O*)a.bias)[at]) : 0.f, w_scale = K == kWhole && ch < a.n ? a.w_scales[at] : 0.f;
-            if (!waited(acc_full + 8 * buf, done / 2 & 1)) break;
+            if (!warp_waited(acc_full + 8 * buf, done / 2 & 1)) break;
             tc::fence_after();
             for (int j = half * 16; j < w.count; j += 32) {
                 const int tokens = min(16, w.count - j);
@@ -405,7 +405,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_consta
     };
     bool ok = true;
     if (warp >= 4) {
-        ok = waited(acc_full, 0);
+        ok = __shfl_sync(0xffffffffu, (int)(lane == 0 && waited(acc_full, 0)), 0) != 0;
         tc::fence_after();
         if (ok) {
 #pragma unroll 1

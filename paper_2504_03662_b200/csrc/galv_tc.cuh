@@ -68,12 +68,13 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity)
 // ... what this CTA's threads and bulk copies wrote, and what the tensor cores did.
 __device__ __forceinline__ bool bar_wait_own(uint32_t bar, uint32_t parity)
 {
+    constexpr uint32_t sleep = 1000000;                   // nanoseconds at most that a try may take, asleep
     uint32_t done;
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity), "r"(sleep) : "memory");
     if (done) return true;
     const long long start = clock64();
     do {
-        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity), "r"(sleep) : "memory");
         if (done) return true;
     } while (clock64() - start < 4000000000ll);
     return false;
