@@ -462,12 +462,11 @@ class Galv:
         if rc:
             self._check(rc)
 
-    def galv_expert_backward(self, shape, ends, dy, x, w, dx, dw, db, room):
-        """shape: (experts, n, k); x, w, dx, dw, db or None; room(bytes): a workspace of so many."""
-        rows, dm, xm, wm = dy.shape[0], _matrix(dy), (None, 0) if x is None else _matrix(x), _matrices(w)
-        size = self.lib.galv_expert_backward_workspace_bytes(self.h, rows, *shape, *dm, *xm, *wm)
-        ws = room(size) if size else None
-        rc = self.lib.galv_expert_backward(self.h, rows, *shape, _at(ends), *dm, *xm, *wm, _DTYPES[dy.dtype], *((None, 0) if dx is None else _matrix(dx)), _at(dw), _at(db),
-                                           *_ws(ws), _raw_stream(self.device))
+    def galv_expert_backward_workspace_bytes(self, rows, experts, n, k, dy, x, w) -> int:
+        return self.lib.galv_expert_backward_workspace_bytes(self.h, rows, experts, n, k, *dy, *x, *w)
+
+    def galv_expert_backward(self, rows, experts, n, k, ends, dy, x, w, dtype, dx, dw, db, workspace):
+        """x, w and dx as (None, 0), dw and db None where they are not asked for."""
+        rc = self.lib.galv_expert_backward(self.h, rows, experts, n, k, _at(ends), *dy, *x, *w, dtype, *dx, _at(dw), _at(db), *_ws(workspace), _raw_stream(self.device))
         if rc:
             self._check(rc)

@@ -108,14 +108,22 @@ def _forward(x: torch.Tensor, weight: torch.Tensor, ends: torch.Tensor, bias: Op
     i8._bias(bias, (experts, n), dtype)
     g = _on(device, weight.device, ends.device, _device(bias))
     y = torch.empty(rows, n, dtype=dtype, device=device)
-    weight = _apart(weight)
+    weight, ends = _apart(weight), _whole(ends)
     xm, wm = gb._matrix(x), gb._matrices(weight)
     ws = None
-    if (xm[0] | wm[0]) % 16 or (xm[1] | wm[1]) % 8 or n * wm[1] >= 1 << 39 or xm[1] >= 1 << 39:      # else nothing has to be moved
+    if not _lie(n, xm, wm):
         size = g.galv_expert_matmul_workspace_bytes(rows, experts, n, k, xm, wm)
         ws = _bytes(size, device) if size else None
-    g.galv_expert_matmul(rows, experts, n, k, _whole(ends), xm, wm, _whole(bias), (y.data_ptr(), n), gb._DTYPES[dtype], ws)
-    return y, x, weight, ws
+    g.galv_expert_matmul(rows, experts, n, k, ends, xm, wm, _whole(bias), (y.data_ptr(), n), gb._DTYPES[dtype], ws)
+    return y, x, weight, ends, ws
+
+
+def _lie(n: int, *matrices) -> bool:
+    """Whether rows start on 16-byte boundaries, nearer to one another than the library's limit: then it moves nothing."""
+    for start, stride in matrices:
+        if start and (start % 16 or stride % 8 or n * stride >= 1 << 39):
+            return False
+    return True
 
 
 def _moved(x: torch.Tensor, weight: torch.Tensor, ws: Optional[torch.Tensor]):
@@ -197,11 +205,11 @@ class _Linear(torch.autograd.Function):
     @staticmethod
     @_as_typed
     def forward(ctx, x, weight, ends, bias):
-        y, lies, held, ws = _forward(x, weight, ends, bias)
-        need = ctx.needs_input_grad
+        y, x, weight, ends, ws = _forward(x, weight, ends, bias)
+        need_x, need_w, _, _ = ctx.needs_input_grad
         if ws is not None:
-            x, weight = _moved(lies, held, ws)            # the backward pass need not move them again
-        ctx.save_for_backward(x if need[1] else None, weight if need[0] else None, ends)
+            x, weight = _moved(x, weight, ws)             # the backward pass need not move them again
+        ctx.save_for_backward(x if need_w else None, weight if need_x else None, ends)
         ctx.shape = weight.shape
         return y
 
@@ -209,15 +217,21 @@ class _Linear(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     @_as_typed
     def backward(ctx, dy):
-        x, weight, ends = ctx.saved_tensors
+        x, weight, ends = ctx.saved_tensors               # as they lie, from the forward pass
         need_x, need_w, _, need_b = ctx.needs_input_grad
         experts, n, k = ctx.shape
-        dy, dtype, device = _rows(dy, "dy"), dy.dtype, dy.device
-        dx = torch.empty(dy.shape[0], k, dtype=dtype, device=device) if need_x else None
-        dw = torch.empty(ctx.shape, dtype=dtype, device=device) if need_w else None
+        dy = _rows(dy, "dy")
+        rows, dtype, device = dy.shape[0], dy.dtype, dy.device
+        dx = torch.empty(rows, k, dtype=dtype, device=device) if need_x else None
+        dw = torch.empty(experts, n, k, dtype=dtype, device=device) if need_w else None
         db = torch.empty(experts, n, dtype=dtype, device=device) if need_b else None
-        _on(device).galv_expert_backward(ctx.shape, _whole(ends), dy, _rows(x, "x") if need_w else None, _apart(weight) if need_x else None, dx, dw, db,
-                                         lambda size: _bytes(size, device))
+        g = _on(device)
+        dm, xm, wm = gb._matrix(dy), gb._matrix(x) if need_w else (None, 0), gb._matrices(weight)
+        ws = None
+        if not _lie(n, dm, xm, wm):
+            size = g.galv_expert_backward_workspace_bytes(rows, experts, n, k, dm, xm, wm)
+            ws = _bytes(size, device) if size else None
+        g.galv_expert_backward(rows, experts, n, k, ends, dm, xm, wm, gb._DTYPES[dtype], (dx.data_ptr(), k) if need_x else (None, 0), dw, db, ws)
         return dx, dw, None, db
 
 
