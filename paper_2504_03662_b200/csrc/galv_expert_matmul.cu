@@ -586,9 +586,9 @@ int whole_launch(galv_ctx* ctx, const char* name, int64_t rows, int32_t experts,
 {
     const int64_t pitch = i8_pitch(k);
     CUtensorMap wm, xm = {}, pm;
-    cudaError_t e = galv_map_3d(&wm, CU_TENSOR_MAP_DATA_TYPE_UINT8, w_codes, experts, n, pitch, pitch, kHalf, kChunkBytes);
-    if (e == cudaSuccess && rows > kFewRows) e = galv_mx_map(&xm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, pitch, pitch, kBox, kChunkBytes, true);
-    if (e == cudaSuccess) e = galv_mx_map(&pm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, pitch, pitch, kPart, kChunkBytes, true);
+    cudaError_t e = galv_map_3d(&wm, CU_TENSOR_MAP_DATA_TYPE_UINT8, w_codes, experts, n, k, pitch, kHalf, kChunkBytes);
+    if (e == cudaSuccess && rows > kFewRows) e = galv_mx_map(&xm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, k, pitch, kBox, kChunkBytes, true);
+    if (e == cudaSuccess) e = galv_mx_map(&pm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, k, pitch, kPart, kChunkBytes, true);
     if (e != cudaSuccess) {
         char text[100];
         snprintf(text, sizeof(text), "%s: tensor map", name);
@@ -596,7 +596,7 @@ int whole_launch(galv_ctx* ctx, const char* name, int64_t rows, int32_t experts,
     }
     ProductArgs a;
     a.rows = rows; a.n = n; a.stride = y_stride; a.experts = experts; a.tiles_m = (int)((n + kTile - 1) / kTile);
-    a.chunks = (int)((pitch + kChunkBytes - 1) / kChunkBytes); a.last_steps = (int)((pitch - (a.chunks - 1) * (int64_t)kChunkBytes + 31) / 32);
+    a.chunks = (int)((k + kChunkBytes - 1) / kChunkBytes); a.last_steps = (int)((k - (a.chunks - 1) * (int64_t)kChunkBytes + 31) / 32);
     a.what = 2u << 4 | 1u << 7 | 1u << 10;      // 32-bit whole sums of signed 8-bit operands
     a.ends = ends; a.x_scales = x_scales; a.w_scales = w_scales; a.bias = bias; a.y = y; a.timeouts = ctx->mx_timeouts_at;
     const int per = 16 / mx_size_of(dtype);

@@ -139,7 +139,7 @@ CASES = [([1], 0, 1, 1), ([1], 0, 16, 2048), ([2, 0, 1], 1, 100, 64), ([0, 0, 5,
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("counts,behind,n,k", CASES)
 def test_forward_and_gradients(counts, behind, n, k, dtype):
-    for pad in (0, 3):
+    for pad in (0, 3, 8):
         x, w, dy, bias = inputs(counts, behind, n, k, dtype, pad)
         ends, spans = ends_of(counts), clamped(np.cumsum(counts), x.shape[0])
         f = formulas(clean(x, behind), f64(w), spans, clean(dy, behind), f64(bias))
@@ -240,6 +240,98 @@ def test_nobody_has_rows(rows):
     assert not experts.input_grad(dy, w, ends).any() and not experts.weight_grad(dy, x, ends).any() and not experts.bias_grad(dy, ends).any()
     base = numbers(1, 120, 40, torch.float32).view(5, 24, 40).cuda()
     assert torch.equal(experts.weight_grad(dy, x, ends, base=base), base)
+
+
+@gpu
+def test_one_expert_without_ends():
+    """The library's calls take no ends where one expert has all rows: plain products and gradients."""
+    rows, n, k = 300, 136, 72
+    x, w, dy, bias = inputs([rows], 0, n, k, "bf16")
+    ends = ends_of([rows])
+    want = experts.matmul(x, w, ends, bias), experts.input_grad(dy, w, ends), experts.weight_grad(dy, x, ends), experts.bias_grad(dy, ends)
+    y, dx, dw, db = (torch.full_like(t, float("nan")) for t in want)
+    g = mx.context(0)
+    g.galv_expert_matmul(rows, 1, n, k, None, (x.data_ptr(), k), (w.data_ptr(), k), bias, (y.data_ptr(), n), gb.BF16, None)
+    g.galv_expert_backward(rows, 1, n, k, None, (dy.data_ptr(), n), (x.data_ptr(), k), (w.data_ptr(), k), gb.BF16, (dx.data_ptr(), k), dw, db, None)
+    assert all(torch.equal(a, b) for a, b in zip((y, dx, dw, db), want))
+    with pytest.raises(gb.GalvError):
+        g.galv_expert_matmul(rows, 2, n // 2, k, None, (x.data_ptr(), k), (w.data_ptr(), k), None, (y.data_ptr(), n // 2), gb.BF16, None)
+
+
+@gpu
+def test_refusals_of_the_library():
+    """Nothing is launched for pointers, strides, sizes and workspaces that cannot be."""
+    g = mx.context(0)
+    x, w = torch.zeros(8, 64, dtype=B, device="cuda"), torch.zeros(2, 16, 64, dtype=B, device="cuda")
+    ends, y, ws = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(8, 16, dtype=B, device="cuda"), torch.zeros(4096, dtype=torch.uint8, device="cuda")
+    xp, wp, yp = x.data_ptr(), w.data_ptr(), y.data_ptr()
+    calls = [((8, 2, 16, 64, ends, (xp, 64), (wp, 64), None, (yp, 15), gb.BF16, None), gb.ERR_INVALID_ARG),       # rows of y overlap
+             ((8, 2, 16, 64, ends, (xp, 63), (wp, 64), None, (yp, 16), gb.BF16, None), gb.ERR_INVALID_ARG),
+             ((8, 2, 16, 64, ends, (xp, 64), (wp, 63), None, (yp, 16), gb.BF16, None), gb.ERR_INVALID_ARG),
+             ((8, 2, 16, 64, ends, (xp + 1, 64), (wp, 64), None, (yp, 16), gb.BF16, None), gb.ERR_INVALID_ARG),
+             ((8, 2, 16, 64, ends, (None, 64), (wp, 64), None, (yp, 16), gb.BF16, None), gb.ERR_INVALID_ARG),
+             ((8, 2, 16, 64, ends, (xp, 64), (wp, 64), None, (yp, 16), gb.F32, None), gb.ERR_INVALID_ARG),
+             ((8, 1025, 16, 64, ends, (xp, 64), (wp, 64), None, (yp, 16), gb.BF16, None), gb.ERR_INVALID_ARG),
+             ((8, 0, 16, 64, ends, (xp, 64), (wp, 64), None, (yp, 16), gb.BF16, None), gb.ERR_INVALID_ARG),
+             ((8, 2, 0, 64, ends, (xp, 64), (wp, 64), None, (yp, 16), gb.BF16, None), gb.ERR_INVALID_ARG),
+             ((-1, 2, 16, 64, ends, (xp, 64), (wp, 64), None, (yp, 16), gb.BF16, None), gb.ERR_INVALID_ARG),
+             ((2 ** 31, 2, 16, 64, ends, (xp, 64), (wp, 64), None, (yp, 16), gb.BF16, None), gb.ERR_INVALID_ARG),
+             ((4, 2, 16, 63, ends, (xp, 65), (wp, 63), None, (yp, 16), gb.BF16, None), gb.ERR_WORKSPACE),          # rows to be moved
+             ((4, 2, 16, 63, ends, (xp, 65), (wp, 63), None, (yp, 16), gb.BF16, ws[:256]), gb.ERR_WORKSPACE),
+             ((4, 2, 16, 63, ends, (xp, 65), (wp, 63), None, (yp, 16), gb.BF16, ws[1:]), gb.ERR_WORKSPACE)]
+    for args, code in calls:
+        with pytest.raises(gb.GalvError) as e:
+            g.galv_expert_matmul(*args)
+        assert e.value.code == code
+    q = i8.pack(x)
+    s = q.scales
+    for args in ((8, 2, 16, 131072, ends, q.codes, s, q.codes, s, None, (yp, 16), gb.BF16), (8, 2, 16, 64, None, q.codes, s, q.codes, s, None, (yp, 16), gb.BF16),
+                 (8, 2, 16, 64, ends, q.codes[:, 1:], s, q.codes, s, None, (yp, 16), gb.BF16), (8, 2, 16, 64, ends, q.codes, s, q.codes, s, None, (yp, 16), 8)):
+        with pytest.raises(gb.GalvError) as e:
+            g.galv_i8_matmul(*args)
+        assert e.value.code == gb.ERR_INVALID_ARG
+    with pytest.raises(gb.GalvError) as e:
+        g.galv_i8_linear(8, 2, 16, 64, ends, (xp, 64), q.codes, s, None, (yp, 16), gb.BF16, None)
+    assert e.value.code == gb.ERR_WORKSPACE
+    assert not y.any()
+
+
+@gpu
+def test_offsets_past_32_bits():
+    """Results, inputs, weights and gradients of more than 2^31 elements: rows and experts on both sides of it."""
+    n, k = 32768, 64
+    rows = 2 ** 31 // n + 300
+    counts = [rows - 270, 0, 250]
+    g = torch.Generator(device="cuda").manual_seed(1)
+    make = lambda *s: torch.randn(*s, generator=g, device="cuda", dtype=torch.float16)
+    x, w, ends = make(rows, k), make(3, n, k), ends_of(counts)
+    y = experts.matmul(x, w, ends)
+    for a, b, e in ((0, 40, 0), (rows - 310, rows - 270, 0), (rows - 270, rows - 20, 2)):
+        want = x[a:b].double() @ w[e].double().t()
+        size = x[a:b].double().abs() @ w[e].double().abs().t()
+        assert ((y[a:b].double() - want).abs() <= cut(k) * size + want.abs() * 2 ** -11 + 2.0 ** -25).all()
+    assert not y[rows - 20:].any()
+    dx = experts.input_grad(y, w, ends)                                              # y in the place of a gradient
+    a, b = rows - 270, rows - 250
+    want, size = y[a:b].double() @ w[2].double(), y[a:b].double().abs() @ w[2].double().abs()
+    ok = (dx[a:b].double() - want).abs() <= cut(n) * size + want.abs() * 2 ** -11 + 2.0 ** -25
+    assert (ok | (want.abs() > 65000)).all() and not dx[rows - 20:].any()
+    db = experts.bias_grad(y, ends, torch.float32)
+    want, size = y[a:rows - 20].double().sum(0), y[a:rows - 20].double().abs().sum(0)
+    assert ((db[2].double() - want).abs() <= 24 * HALF * size).all()
+    del y, dx
+    E, n, k = 33, 8192, 8192                                                         # 2.2e9 weights
+    counts = [5] * E
+    x, dy, w, ends = make(5 * E, k), make(5 * E, n), make(E, n, k), ends_of(counts)
+    y, dx, dw = experts.matmul(x, w, ends), experts.input_grad(dy, w, ends), experts.weight_grad(dy, x, ends)
+    for e in (0, E - 1):
+        at = slice(5 * e, 5 * e + 5)
+        for got, u, v in ((y[at], x[at], w[e].t()), (dx[at], dy[at], w[e]), (dw[e], dy[at].t(), x[at])):
+            want, size = u.double() @ v.double(), u.double().abs() @ v.double().abs()
+            assert ((got.double() - want).abs() <= cut(u.shape[1]) * size + want.abs() * 2 ** -11 + 2.0 ** -25).all()
+    p = i8.pack(w.view(-1, k))
+    few = i8.Packed(p.codes[(E - 1) * n:], p.scales[(E - 1) * n:], n, k)
+    assert torch.equal(experts.matmul(x, p, ends)[-5:], i8.linear(x[-5:], few))
 
 
 @gpu
