@@ -39,6 +39,7 @@ struct ProductArgs {
     const void* bias;
     void* y;
     int vec;                                              // 16 bytes of a row of y can be moved at once
+    int in_front;                                         // the kernel before this one in the stream puts the tokens into 8-bit integers: all before it is over
     unsigned* timeouts;                                   // host memory: CTAs that have given up a wait
 };
 
@@ -112,6 +113,9 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
         tc::prefetch_map(&part_map);
     }
     if (warp == 2) tc::tmem_alloc<2>(slot, 512);
+    const bool in_front = K == kWhole && a.in_front;
+    if (!in_front) tc::before_is_over();
+    tc::next_may_start();
     if (warp == 3) experts_begin(a.ends, a.experts, a.rows, begin);
     __syncthreads();
     if (warp >= 4) {                                      // a size of tiles each: 256, 224 .. 32 rows
@@ -148,7 +152,7 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
             constexpr int elements = K == kWhole ? kChunkBytes : kChunkBytes / 2;
             int s = 0;
             uint32_t turn = 1;
-            bool ok = true, over = K != kWhole;
+            bool ok = true, over = !in_front;
             for (int u = first; u < units && ok; u += stride) {
                 w.to(u);
                 const int m0 = w.tm * kTile + rank * kHalf, half = w.columns() / 2, r0 = w.row0 + rank * half;
@@ -220,7 +224,7 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
         const uint32_t mine = out_at + (warp - 4) * 2048, lanes = (uint32_t)quad * 32 << 16;
         O* const y = (O*)a.y;
         int done = 0;
-        if (K == kWhole) tc::before_is_over();
+        if (in_front) tc::before_is_over();
         for (int u = first; u < units; u += stride, ++done) {
             w.to(u);
             const uint32_t buf = done & 1;
@@ -318,6 +322,8 @@ expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_consta
     }
     constexpr uint32_t columns = kFewRows;
     if (warp == 2) tc::tmem_alloc<1>(slot, columns);
+    if (K != kWhole || !a.in_front) tc::before_is_over();
+    tc::next_may_start();
     if (warp == 3) experts_nth(a.ends, a.experts, a.rows, nth, mine);
     tc::fence_before();
     __syncthreads();
@@ -459,30 +465,8 @@ AlignPlan align_plan(int64_t rows, int64_t x_cols, const void* x, int64_t x_stri
     return p;
 }
 
-// in_front: a kernel that these may start beside has just been launched
-void configure(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* attr, unsigned grid, unsigned threads, int smem, unsigned cluster, bool in_front, cudaStream_t st)
-{
-    cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = attr;
-    if (cluster) {
-        attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
-        attr[cfg.numAttrs].val.clusterDim.x = cluster;
-        attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
-        ++cfg.numAttrs;
-    }
-    if (in_front) {
-        attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
-        ++cfg.numAttrs;
-    }
-}
-
 template <int K, typename O>
-cudaError_t launch_few(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap& pm, const ProductArgs& a, bool in_front, cudaStream_t st)
+cudaError_t launch_few(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap& pm, const ProductArgs& a, cudaStream_t st)
 {
     const cudaError_t e = cudaFuncSetAttribute(expert_few_kernel<K, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
     if (e != cudaSuccess) return e;
@@ -490,17 +474,15 @@ cudaError_t launch_few(const galv_ctx* ctx, const CUtensorMap& wm, const CUtenso
     const long long units = tiles * (long long)(a.rows < a.experts ? a.rows : a.experts);
     int ranks = 1;                                        // two CTAs an SM at most, two chunks a CTA at least
     while (ranks < 8 && units * ranks <= ctx->num_sms && a.chunks >= ranks * 4) ranks *= 2;
-    cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute attr[2];
-    configure(cfg, attr, (unsigned)(units * ranks), kFewThreads, kFewSmem, (unsigned)ranks, in_front, st);
-    return cudaLaunchKernelEx(&cfg, expert_few_kernel<K, O>, wm, pm, a, tiles, ranks);
+    tc::Launch l((unsigned)(units * ranks), kFewThreads, kFewSmem, (unsigned)ranks, true, st);
+    return cudaLaunchKernelEx(&l.cfg, expert_few_kernel<K, O>, wm, pm, a, tiles, ranks);
 }
 
 template <int K, typename O>
-cudaError_t launch(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap& xm, const CUtensorMap& pm, ProductArgs& a, bool in_front, cudaStream_t st)
+cudaError_t launch(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap& xm, const CUtensorMap& pm, ProductArgs& a, cudaStream_t st)
 {
     if constexpr (K != kInputGrad) {
-        if (a.rows <= kFewRows) return launch_few<K, O>(ctx, wm, pm, a, in_front, st);
+        if (a.rows <= kFewRows) return launch_few<K, O>(ctx, wm, pm, a, st);
     }
     const int smem = smem_of(a.experts);
     const cudaError_t e = cudaFuncSetAttribute(expert_product_kernel<K, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kExpertsMost));
@@ -508,10 +490,10 @@ cudaError_t launch(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap
     a.what |= (uint32_t)(kTile >> 4) << 24;
     const long long most = (a.rows / 32 + (a.rows < a.experts ? a.rows : a.experts)) * a.tiles_m;      // units, whatever the ends say and their size is
     const int pairs = (int)(most < ctx->num_sms / 2 ? most : ctx->num_sms / 2);
-    cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute attr[1];
-    configure(cfg, attr, (unsigned)pairs * 2, kThreads, smem, 0, in_front, st);
-    return cudaLaunchKernelEx(&cfg, expert_product_kernel<K, O>, wm, xm, pm, a);
+    // Beside the kernel before it where that puts its tokens into 8-bit integers, or where one round of tiles is all there is: starting early is 2 us of 18 there.  Of many rounds it
+    // gained nothing (a training step of 16 experts: 433 and 439 us).
+    tc::Launch l((unsigned)pairs * 2, kThreads, smem, 0, a.in_front || most <= ctx->num_sms / 2, st);
+    return cudaLaunchKernelEx(&l.cfg, expert_product_kernel<K, O>, wm, xm, pm, a);
 }
 
 bool units_fit(int64_t rows, int64_t experts, int64_t n) { return (rows / 32 + experts) * ((n + kTile - 1) / kTile) < (int64_t)1 << 31; }
@@ -560,13 +542,14 @@ int product16(galv_ctx* ctx, const char* name, bool across, int64_t rows, int32_
     if (e != cudaSuccess) return wrong(GALV_ERR_CUDA, "tensor map");
     ProductArgs a;
     a.rows = rows; a.n = n; a.stride = y_stride; a.experts = experts; a.tiles_m = (int)((n + kTile - 1) / kTile);
+    a.in_front = 0;
     a.chunks = (int)((k + 63) / 64); a.last_steps = (int)((k - (a.chunks - 1) * 64ll + 15) / 16);
     const uint32_t t = dtype == GALV_BF16 ? 1u : 0u;      // fp32 sums, both operands of this type, the weights' summed index along or across their rows
     a.what = 1u << 4 | t << 7 | t << 10 | (across ? 1u << 15 : 0u);
     a.ends = ends; a.x_scales = a.w_scales = nullptr; a.bias = bias; a.y = y; a.timeouts = ctx->mx_timeouts_at;
     a.vec = n % 8 == 0 && y_stride % 8 == 0 && mx_aligned(y, 16);
-    if (dtype == GALV_BF16) e = across ? launch<kInputGrad, __nv_bfloat16>(ctx, wm, xm, pm, a, false, st) : launch<kForward, __nv_bfloat16>(ctx, wm, xm, pm, a, false, st);
-    else e = across ? launch<kInputGrad, __half>(ctx, wm, xm, pm, a, false, st) : launch<kForward, __half>(ctx, wm, xm, pm, a, false, st);
+    if (dtype == GALV_BF16) e = across ? launch<kInputGrad, __nv_bfloat16>(ctx, wm, xm, pm, a, st) : launch<kForward, __nv_bfloat16>(ctx, wm, xm, pm, a, st);
+    else e = across ? launch<kInputGrad, __half>(ctx, wm, xm, pm, a, st) : launch<kForward, __half>(ctx, wm, xm, pm, a, st);
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
 
@@ -596,12 +579,13 @@ int whole_launch(galv_ctx* ctx, const char* name, int64_t rows, int32_t experts,
     }
     ProductArgs a;
     a.rows = rows; a.n = n; a.stride = y_stride; a.experts = experts; a.tiles_m = (int)((n + kTile - 1) / kTile);
+    a.in_front = in_front;
     a.chunks = (int)((k + kChunkBytes - 1) / kChunkBytes); a.last_steps = (int)((k - (a.chunks - 1) * (int64_t)kChunkBytes + 31) / 32);
     a.what = 2u << 4 | 1u << 7 | 1u << 10;      // 32-bit whole sums of signed 8-bit operands
     a.ends = ends; a.x_scales = x_scales; a.w_scales = w_scales; a.bias = bias; a.y = y; a.timeouts = ctx->mx_timeouts_at;
     const int per = 16 / mx_size_of(dtype);
     a.vec = n % per == 0 && y_stride % per == 0 && mx_aligned(y, 16);
-    MX_DISPATCH_TYPE(dtype, e = (launch<kWhole, T>(ctx, wm, xm, pm, a, in_front, st)));
+    MX_DISPATCH_TYPE(dtype, e = (launch<kWhole, T>(ctx, wm, xm, pm, a, st)));
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
 

@@ -48,7 +48,8 @@ i8_pack_kernel(long long rows, int cols, int pieces, const T* __restrict__ x, lo
     __shared__ uint32_t found[2][8];
     const int t = threadIdx.x % threads, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     int turn = 0;
-    tc::next_may_start();                                 // the product that reads the codes waits for this kernel's end itself
+    tc::before_is_over();
+    tc::next_may_start();                                 // behind the wait: the product that reads the codes takes it that all before this kernel is over
     for (long long row0 = (long long)blockIdx.x * (8 / WARPS); row0 < rows; row0 += (long long)gridDim.x * (8 / WARPS), turn ^= 1) {
         const long long row = row0 + warp / WARPS;
         const bool in = row < rows;
@@ -134,7 +135,8 @@ template <typename T, bool VEC, int WARPS, int P>
 void launch_pack(int num_sms, int64_t rows, int64_t cols, const T* x, int64_t stride, int8_t* codes, float* scales, cudaStream_t st)
 {
     const int64_t ctas = (rows + 8 / WARPS - 1) / (8 / WARPS), most = (int64_t)num_sms * 32;
-    i8_pack_kernel<T, VEC, WARPS, P><<<(int)(ctas < most ? ctas : most), 256, 0, st>>>(rows, (int)cols, (int)(i8_pitch(cols) / 8), x, stride, codes, scales);
+    tc::Launch l((unsigned)(ctas < most ? ctas : most), 256, 0, 0, true, st);
+    cudaLaunchKernelEx(&l.cfg, i8_pack_kernel<T, VEC, WARPS, P>, (long long)rows, (int)cols, (int)(i8_pitch(cols) / 8), x, (long long)stride, codes, scales);
 }
 
 // As many warps a row as keep all of it with 4 pieces a thread (8 of the longest rows), and all 8 where there are few rows.

@@ -455,6 +455,60 @@ def test_captured_with_other_ends():
 
 
 @gpu
+def test_one_behind_the_other_eager_and_captured():
+    """Kernels may begin before the one in front of them is over: each result is the next call's input or weights, fills and copies and other streams' work lie between, and a second
+    replay finds what the first has left."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    make = lambda *s: torch.randn(*s, generator=g, device="cuda", dtype=B) / 8
+    rows, d = 40, 512
+    x0, w = make(rows, d), make(4, d, d)
+    ends = ends_of([10, 0, 25, 5])
+    side = torch.cuda.Stream()
+
+    def chain(x):
+        h = experts.matmul(x, w, ends)                                              # few rows
+        p = i8.pack(h)
+        h = i8.matmul(p, i8.pack(w[0])) + experts.matmul(h, i8.pack(w.view(-1, d)), ends)
+        fork = torch.cuda.Event()
+        fork.record()
+        side.wait_event(fork)
+        with torch.cuda.stream(side):
+            other = experts.matmul(h, w, ends)
+            done = torch.cuda.Event()
+            done.record()
+        torch.cuda.current_stream().wait_event(done)
+        z = torch.zeros(3 * rows, d, dtype=B, device="cuda")
+        z[:rows].copy_(other)
+        z[rows:2 * rows] = h
+        y = experts.matmul(z, w, ends_of_many)                                      # more than 64
+        v = (y[:64].t() @ y[:64]).contiguous()                                      # weights that the next call reads at once
+        q = i8.pack(v / 8)
+        return i8.linear(y, q), i8.linear(y[:5], q), experts.weight_grad(y, z, ends_of_many)
+
+    ends_of_many = ends_of([30, 50, 0, 37])
+    want = chain(x0)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        assert all(torch.equal(a, b) for a, b in zip(chain(x0), want))
+    x1 = make(rows, d)
+    want1 = chain(x1)
+    static = x0.clone()
+    warm = torch.cuda.Stream()
+    warm.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(warm):
+        chain(static)
+    torch.cuda.current_stream().wait_stream(warm)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = chain(static)
+    for x, right in ((x1, want1), (x0, want), (x0, want), (x1, want1)):
+        static.copy_(x)
+        graph.replay()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(got, right))
+
+
+@gpu
 def test_two_streams_at_once():
     counts = [300, 20, 700]
     sets = [inputs(counts, 0, 264, 328, "f16", seed=s) for s in (0, 50)]
