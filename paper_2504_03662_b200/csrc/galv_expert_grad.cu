@@ -4,8 +4,8 @@
 // stored.  An expert's rows end anywhere: its last chunk of 64 holds rows of the next expert (or of none, which may be anything).  Of those the matrix
 // instructions take no steps of 16 rows that are not needed, and what is left of the last step is set to zero in shared memory, in both operands, since
 // zero times what lies there could be NaN.
-// Per CTA: a thread that starts bulk tensor copies, a warp that sets such rows to zero and tells the first CTA of the pair that a chunk is there, a thread (of the first)
-// that issues the matrix instructions for the pair, eight warps that take sums from the tensor memory while the next are made and move results out.
+// Per CTA: a thread that starts bulk tensor copies (both CTAs' tell the first one's barrier, those of a chunk with such rows their own), a warp that sets such rows to zero and then tells the
+// first one's barrier, a thread (of the first) that issues the matrix instructions for the pair, eight warps that take sums from the tensor memory while the next are made and move results out.
 
 #include "galv_experts.cuh"
 #include "galv_tc.cuh"
@@ -98,7 +98,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
     extern __shared__ unsigned char raw[];
     const uint32_t base = (tc::smem_at(raw) + 1023) & ~1023u;
     const uint32_t out_at = base + kStages * kStageBytes, bars = out_at + kOutBytes;
-    const uint32_t full = bars, ready = full + 8 * kStages, empty = ready + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16, drain = acc_empty + 16,
+    const uint32_t full = bars, own = full + 8 * kStages, empty = own + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16, drain = acc_empty + 16,
                    base_full = drain + 8, slot = base_full + 64;
     int* const begin = reinterpret_cast<int*>(raw + (bars + 256 - tc::smem_at(raw)));
     __shared__ int failed;
@@ -109,8 +109,8 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            tc::bar_init(full + 8 * s, 1);
-            tc::bar_init(ready + 8 * s, 2);
+            tc::bar_init(full + 8 * s, 2);                // the producer twice, or what both CTAs' warps say that set rows to zero
+            tc::bar_init(own + 8 * s, 1);
             tc::bar_init(empty + 8 * s, 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -150,33 +150,46 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
                 const int n0 = w.tn * kTile + rank * kHalf, k0 = w.tk * kTile + rank * kHalf;
                 for (int r = 0; r < w.count; r += kTokens, ++it) {
                     const int s = it % kStages;
-                    const uint32_t bar = full + 8 * s, at = base + s * kStageBytes;
                     if (!(ok = waited(empty + 8 * s, (it / kStages & 1) ^ 1))) break;
-                    tc::bar_expect(bar, kStageBytes);
-                    tc::load_2d(at, &dy_map, n0, w.row0 + r, bar);
-                    tc::load_2d(at + kBox, &dy_map, n0 + 64, w.row0 + r, bar);
-                    tc::load_2d(at + kOperand, &x_map, k0, w.row0 + r, bar);
-                    tc::load_2d(at + kOperand + kBox, &x_map, k0 + 64, w.row0 + r, bar);
+                    const bool ragged = w.count - r < kTokens && w.count % 16 != 0;
+                    const uint32_t at = base + s * kStageBytes;
+                    const int row = w.row0 + r;
+                    if (ragged) {                         // zeros come in between: each CTA's own barrier
+                        const uint32_t bar = own + 8 * s;
+                        tc::bar_expect(bar, kStageBytes);
+                        tc::load_2d(at, &dy_map, n0, row, bar);
+                        tc::load_2d(at + kBox, &dy_map, n0 + 64, row, bar);
+                        tc::load_2d(at + kOperand, &x_map, k0, row, bar);
+                        tc::load_2d(at + kOperand + kBox, &x_map, k0 + 64, row, bar);
+                    } else {
+                        const uint32_t bar = tc::in_cta(full + 8 * s, 0);
+                        if (rank == 0) {                  // both CTAs' copies
+                            tc::bar_expect(full + 8 * s, 2 * kStageBytes);
+                            tc::bar_arrive(full + 8 * s);
+                        }
+                        tc::load_2d_pair(at, &dy_map, n0, row, bar);
+                        tc::load_2d_pair(at + kBox, &dy_map, n0 + 64, row, bar);
+                        tc::load_2d_pair(at + kOperand, &x_map, k0, row, bar);
+                        tc::load_2d_pair(at + kOperand + kBox, &x_map, k0 + 64, row, bar);
+                    }
                 }
             }
-            if (*(volatile int*)&failed)                  // copies still in flight
-                for (int i = it < kStages ? 0 : it - kStages; i < it; ++i) tc::bar_wait(full + 8 * (i % kStages), i / kStages & 1);
+            if (*(volatile int*)&failed) tc::settle();
         }
-    } else if (warp == 3) {                               // tells the first CTA that this one's rows are there, with zeros for what is not the expert's
+    } else if (warp == 3) {                               // sets to zero what is not the expert's in the last step of its last chunk, and says so
         int it = 0;
-        bool ok = true;
-        for (int u = first; u < units && ok; u += stride) {
+        uint32_t turns = 0;                               // of each stage's barrier: bit s
+        for (int u = first; u < units; u += stride) {
             const Unit w = unit_of(a, begin, u);
-            for (int r = 0; r < w.count; r += kTokens, ++it) {
-                const int s = it % kStages;
-                if (!(ok = __all_sync(0xffffffffu, waited(full + 8 * s, it / kStages & 1)))) break;
-                if (w.count - r < kTokens) {
-                    clear_rows(base + s * kStageBytes, w.count - r);
-                    tc::fence_async();
-                }
-                __syncwarp();
-                if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(ready + 8 * s, 0));
-            }
+            const int chunks = (w.count + kTokens - 1) / kTokens, s = (it + chunks - 1) % kStages;
+            it += chunks;
+            if (w.count % 16 == 0) continue;
+            if (!__all_sync(0xffffffffu, waited(own + 8 * s, turns >> s & 1))) break;
+            turns ^= 1u << s;
+            clear_rows(base + s * kStageBytes, w.count - (chunks - 1) * kTokens);
+            tc::fence_async();
+            __syncwarp();
+            if (lane == 0) tc::bar_arrive_cluster(tc::in_cta(full + 8 * s, 0));
         }
     } else if (warp == 1 && rank == 0) {
         if (tc::elect()) {
@@ -192,7 +205,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
                     for (bool add = false; r < end; r += kTokens, ++it, add = true) {
                         const int s = it % kStages, steps = min(kTokens / 16, (w.count - r + 15) / 16);
                         const uint32_t at = base + s * kStageBytes;
-                        if (!(ok = waited(ready + 8 * s, it / kStages & 1))) break;
+                        if (!(ok = waited(full + 8 * s, it / kStages & 1))) break;
                         tc::fence_after();
 #pragma unroll
                         for (int j = 0; j < kTokens / 16; ++j)
