@@ -543,7 +543,7 @@ int galv_i8_linear(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int6
  *   galv_expert_input_grad   dx[r][c] = sum_j dy[r][j] w[e][j][c]
  *   galv_expert_weight_grad  dw[e][j][c] = base[e][j][c] + sum over e's rows of dy[r][j] x[r][c]
  *   galv_expert_bias_grad    db[e][j] = sum over e's rows of dy[r][j]
- * Sums are fp32 (the first three by the tensor cores, which may cut an addition where rounding would halve the error; dw's over 1024 rows at most, then by
+ * Sums are fp32 (the first three by the tensor cores, which may cut an addition where rounding would halve the error; dw's over 768 rows at most, then by
  * rounded additions), biases and base are added in fp32, results rounded once.  dw, base [experts][n][k] contiguous of `dw_dtype`, db [experts][n] of
  * `db_dtype` (`dtype` or GALV_F32); base NULL: zero; dw may be base.  An expert without rows has base or zeros for its gradient.  The order of
  * the sums is fixed by sizes, ends, strides and alignment.  Operands whose rows do not start on 16-byte boundaries are moved to ones that do, in the

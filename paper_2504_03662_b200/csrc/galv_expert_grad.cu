@@ -7,6 +7,11 @@
 // Per CTA: a thread that starts bulk tensor copies (both CTAs' tell the first one's barrier, those of a chunk with such rows their own), a warp that sets such rows to zero and then tells the
 // first one's barrier, a thread (of the first) that issues the matrix instructions for the pair, eight warps that take sums from the tensor memory while the next are made and move results out.
 
+//
+// Bound by the loop of copies and matrix instructions: 16 experts of 8192 rows in all, 4096 x 2048 into bf16, take 124 us (1.1 PFLOP/s; the matrix instructions alone 79, with copies 99: shared
+// memory and L2 have both at a time); 8 experts of 16384 rows, 2048 x 8192 onto an fp32 base, 472 us (1.16 PFLOP/s, 3.0 TB/s); 24 experts of 300 rows, 1365 x 2048 into fp16, 38.6 us, which is what
+// the card writes (3.5 TB/s; zeros of this size go at 3.7).
+
 #include "galv_experts.cuh"
 #include "galv_tc.cuh"
 #include "galv_tile_out.cuh"
@@ -18,9 +23,9 @@ constexpr int kBox = kTokens * 128;                       // 64 rows of 64 colum
 constexpr int kOperand = 2 * kBox, kStageBytes = 2 * kOperand;
 constexpr int kOutBytes = 8 * 4096;                       // 32 rows of 128 bytes of each warp that moves results out
 constexpr int kThreads = 384;
-// A tensor core's sum is cut at every addition, 8e-7 of the result over 1024 rows (the error grows with the root of the length): after this many chunks the
-// sum goes to fp32 registers, rounded additions.
-constexpr int kSegment = 16;
+// A tensor core's sum is cut at every addition: 4.8e-7 of the result over 512 rows, 1.0e-6 over 1024 (the cuts go one way, so the error grows with the length).  So after this many chunks
+// the sum goes to fp32 registers, rounded additions.  (Onto an fp32 base, 2048 rows an expert, 8192 x 2048: 460 us with 16 chunks, 472 with 12, 491 with 8.)
+constexpr int kSegment = 12;
 constexpr int kGroup = 8;                                 // tiles along n whose columns of dy stay in L2 while their k runs
 
 struct GradArgs {

@@ -3,7 +3,8 @@
 // A row's scale needs all of the row before its first code: up to 16384 columns stay in the registers of the threads that read them, what lies
 // behind is read twice (from L2).  A code is the whole number nearest to the exact quotient x / s: x * (1 / s) is off by some units of its last place, so
 // the remainder x - q s, which an fp32 multiply-add has exactly, decides next to a half.
-// Bound by memory, what is read and written once, 3 bytes an element from 16 bits.
+// Bound by memory and issue slots, what is read and written once, 3 bytes an element from 16 bits: 4096 x 8192 in bf16 is packed in 22 us (4.5 TB/s; 15 instructions an element), 8192 x 4096 in fp32 in
+// 29 (5.7 TB/s).  With 8 pieces a thread in place of 4 (two CTAs an SM for five) the first took 41.
 
 #include "galv_i8.cuh"
 #include "galv_tc.cuh"
