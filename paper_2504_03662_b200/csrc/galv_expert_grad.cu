@@ -30,7 +30,7 @@ constexpr int kGroup = 8;                                 // tiles along n whose
 
 struct GradArgs {
     long long rows, n, k;
-    int experts, tiles_n, tiles_k;
+    int experts, splits, tiles_n, tiles_k;                // splits: of each expert's rows, with a result of their own each
     uint32_t what;
     const int32_t* ends;
     const void* base;
@@ -39,16 +39,18 @@ struct GradArgs {
     unsigned* timeouts;
 };
 
-struct Unit { int expert, tn, tk, row0, count; };
+struct Unit { int part, tn, tk, row0, count; };           // part: expert * splits + split
 __device__ __forceinline__ Unit unit_of(const GradArgs& a, const int* begin, int u)
 {
     Unit w;
     const int each = a.tiles_n * a.tiles_k, tile = u % each, per = kGroup * a.tiles_k, first = tile / per * kGroup, size = min(kGroup, a.tiles_n - first);
-    w.expert = u / each;
+    w.part = u / each;
     w.tn = first + tile % per % size;
     w.tk = tile % per / size;
-    w.row0 = begin[w.expert];
-    w.count = begin[w.expert + 1] - w.row0;
+    const int expert = w.part / a.splits, rows = begin[expert + 1] - begin[expert];
+    const int len = a.splits == 1 ? rows : (int)((((unsigned)rows + a.splits - 1) / a.splits + kTokens - 1) / kTokens * kTokens), skip = (int)min((long long)(w.part % a.splits) * len, (long long)rows);
+    w.row0 = begin[expert] + skip;
+    w.count = min(len, rows - skip);
     return w;
 }
 
@@ -110,7 +112,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = tc::cluster_rank();
-    const int units = a.experts * a.tiles_n * a.tiles_k, first = blockIdx.x / 2, stride = gridDim.x / 2;
+    const int units = a.experts * a.splits * a.tiles_n * a.tiles_k, first = blockIdx.x / 2, stride = gridDim.x / 2;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
@@ -247,7 +249,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
                 if (lane == 0) {
                     tc::stores_read();
                     tc::bar_expect(base_bar, 4096);
-                    tc::load_3d(mine, &base_map, (int)c0 + c, (int)r0, w.expert, base_bar);
+                    tc::load_3d(mine, &base_map, (int)c0 + c, (int)r0, w.part, base_bar);
                 }
             };
             if (a.boxes && a.base && some) fetch(0);
@@ -313,12 +315,12 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
                         tc::fence_async();
                         __syncwarp();
                         if (lane == 0) {
-                            tc::store_3d(&dw_map, (int)c0 + c, (int)r0, w.expert, mine);
+                            tc::store_3d(&dw_map, (int)c0 + c, (int)r0, w.part, mine);
                             tc::stores_end();
                         }
                     }
             } else if (ok) {
-                const long long at0 = w.expert * a.n * a.k + r0 * a.k + c0, at = at0 + lane / 16 * a.k + lane % 16;
+                const long long at0 = w.part * a.n * a.k + r0 * a.k + c0, at = at0 + lane / 16 * a.k + lane % 16;
                 if (w.count > 0) tile_out::move_out<O>(from + acc * kTile, mine, a.base ? (const O*)a.base + at : nullptr, (O*)a.dw + at, a.k, rows, cols, false);
                 else fill<O>(a.base ? (const O*)a.base + at0 : nullptr, (O*)a.dw + at0, a.k, rows, cols);
             }
@@ -337,6 +339,18 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
     tc::cluster_sync();                                   // neither CTA's memory is read by the other any more
     if (threadIdx.x == 0 && failed) atomicAdd_system(a.timeouts, 1u);
     if (warp == 2) tc::tmem_free<2>(tmem, 512);
+}
+
+// dw = base + the splits' sums, in order.
+template <typename O>
+__global__ void __launch_bounds__(256) expert_grad_join_kernel(long long each, long long count, int splits, const float* __restrict__ partial, const O* base, O* dw)
+{
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < count; i += (long long)gridDim.x * 256) {
+        const float* const p = partial + (i / each * splits * each + i % each);
+        float v = p[0];
+        for (int s = 1; s < splits; ++s) v += p[s * each];
+        dw[i] = mx_round<O>(base ? mx_float(base[i]) + v : v);
+    }
 }
 
 // ---- bias
@@ -405,8 +419,8 @@ expert_bias_grad_kernel(long long rows, int experts, long long n, const int32_t*
 size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 int smem_of(int experts) { return 1024 + kStages * kStageBytes + kOutBytes + 256 + 4 * (experts + 1); }
 
-struct GradPlan { size_t dy, x, total; };
-GradPlan plan_of(int64_t rows, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride)
+struct GradPlan { size_t dy, x, partial, total; int splits; };
+GradPlan plan_of(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride)
 {
     auto moved = [&](const void* p, int64_t stride, int64_t cols) {
         return mx_rows16(p, stride, GALV_BF16) && stride * 2 < ((int64_t)1 << 40) ? 0 : up((size_t)rows * ((cols + 7) / 8 * 8) * 2);
@@ -414,7 +428,17 @@ GradPlan plan_of(int64_t rows, int64_t n, int64_t k, const void* dy, int64_t dy_
     GradPlan p;
     p.dy = moved(dy, dy_stride, n);
     p.x = moved(x, x_stride, k);
-    p.total = p.dy + p.x;
+    // Fewer tiles than half of the pairs and long experts: each expert's rows are split, 256 a split or more (one expert of 16384 rows, 100 x 100: 158 us as one tile, 43 split in 16 and
+    // joined; at 1700 rows an expert the second kernel costs what the splits give).
+    const int64_t units = ((n + kTile - 1) / kTile) * ((k + kTile - 1) / kTile) * experts, pairs = ctx->num_sms / 2;
+    p.splits = 1;
+    if (units * 2 <= pairs && rows >= experts * (int64_t)2048) {
+        const int64_t most = pairs / units, worth = rows / (experts * (int64_t)256);
+        p.splits = (int)(most < worth ? most : worth);
+        if (p.splits > 16) p.splits = 16;
+    }
+    p.partial = p.splits > 1 ? up((size_t)p.splits * experts * n * k * 4) : 0;
+    p.total = p.dy + p.x + p.partial;
     return p;
 }
 
@@ -424,13 +448,13 @@ cudaError_t launch(const galv_ctx* ctx, const CUtensorMap& dm, const CUtensorMap
     CUtensorMap bm = {}, wm = {};
     a.boxes = mx_rows16(a.dw, a.k, sizeof(O) == 4 ? GALV_F32 : GALV_BF16) && mx_aligned(a.base, 16);
     if (a.boxes) {
-        cudaError_t e = galv_map_3d(&wm, type, a.dw, a.experts, a.n, a.k, a.k * sizeof(O), 32, 128 / sizeof(O));
+        cudaError_t e = galv_map_3d(&wm, type, a.dw, (int64_t)a.experts * a.splits, a.n, a.k, a.k * sizeof(O), 32, 128 / sizeof(O));
         if (e == cudaSuccess && a.base) e = galv_map_3d(&bm, type, a.base, a.experts, a.n, a.k, a.k * sizeof(O), 32, 128 / sizeof(O));
         if (e != cudaSuccess) return e;
     }
     const cudaError_t e = cudaFuncSetAttribute(expert_grad_kernel<O>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kExpertsMost));
     if (e != cudaSuccess) return e;
-    const long long units = (long long)a.experts * a.tiles_n * a.tiles_k;
+    const long long units = (long long)a.experts * a.splits * a.tiles_n * a.tiles_k;
     const int pairs = (int)(units < ctx->num_sms / 2 ? units : ctx->num_sms / 2);
     expert_grad_kernel<O><<<pairs * 2, kThreads, smem_of(a.experts), st>>>(dm, xm, bm, wm, a);
     return cudaGetLastError();
@@ -447,8 +471,8 @@ bool sizes_ok(int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t
 extern "C" size_t galv_expert_weight_grad_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* x,
                                                           int64_t x_stride)
 {
-    if (!ctx || !mx_size_ok(rows, n) || !mx_size_ok(rows, k) || rows == 0 || experts < 1) return 0;
-    return plan_of(rows, n, k, dy, dy_stride, x, x_stride).total;
+    if (!ctx || !mx_size_ok(rows, n) || !mx_size_ok(rows, k) || rows == 0 || experts < 1 || experts > kExpertsMost) return 0;
+    return plan_of(ctx, rows, experts, n, k, dy, dy_stride, x, x_stride).total;
 }
 
 extern "C" int galv_expert_weight_grad(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* dy, int64_t dy_stride, const void* x,
@@ -470,14 +494,17 @@ extern "C" int galv_expert_weight_grad(galv_ctx* ctx, int64_t rows, int32_t expe
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
     cudaStream_t st = (cudaStream_t)stream;
     GradArgs a;
-    a.rows = rows; a.n = n; a.k = k; a.experts = experts;
+    a.rows = rows; a.n = n; a.k = k; a.experts = experts; a.splits = 1;
     a.tiles_n = (int)((n + kTile - 1) / kTile); a.tiles_k = (int)((k + kTile - 1) / kTile);
     const uint32_t t = dtype == GALV_BF16 ? 1u : 0u;      // fp32 sums, both operands of this type with the summed index across their rows, 256 x 256
     a.what = 1u << 4 | t << 7 | t << 10 | 1u << 15 | 1u << 16 | (uint32_t)(kTile >> 3) << 17 | (uint32_t)(kTile >> 4) << 24;
     a.ends = ends; a.base = base; a.dw = dw; a.timeouts = ctx->mx_timeouts_at;
     CUtensorMap dm = {}, xm = {};
+    float* partial = nullptr;
     if (rows > 0) {
-        const GradPlan p = plan_of(rows, n, k, dy, dy_stride, x, x_stride);
+        const GradPlan p = plan_of(ctx, rows, experts, n, k, dy, dy_stride, x, x_stride);
+        a.splits = p.splits;
+        if (p.partial) partial = (float*)((char*)workspace + p.dy + p.x);
         if (p.dy) {
             galv_align_rows(ctx, rows, n, dy, dy_stride, workspace, (n + 7) / 8 * 8, st);
             dy = workspace;
@@ -496,7 +523,16 @@ extern "C" int galv_expert_weight_grad(galv_ctx* ctx, int64_t rows, int32_t expe
     }
     // without rows no copy is made: the maps are not read
     cudaError_t e;
-    if (dw_dtype == GALV_F32) e = launch<float>(ctx, dm, xm, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, a, st);
+    if (partial) {
+        a.base = nullptr;
+        a.dw = partial;
+        e = launch<float>(ctx, dm, xm, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, a, st);
+        if (e == cudaSuccess) {
+            const int64_t count = experts * n * k, ctas = (count + 255) / 256, most = (int64_t)ctx->num_sms * 8;
+            MX_DISPATCH_TYPE(dw_dtype, expert_grad_join_kernel<T><<<(int)(ctas < most ? ctas : most), 256, 0, st>>>(n * k, count, a.splits, partial, (const T*)base, (T*)dw));
+            e = cudaGetLastError();
+        }
+    } else if (dw_dtype == GALV_F32) e = launch<float>(ctx, dm, xm, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, a, st);
     else if (dw_dtype == GALV_BF16) e = launch<__nv_bfloat16>(ctx, dm, xm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a, st);
     else e = launch<__half>(ctx, dm, xm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, a, st);
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
@@ -532,7 +568,7 @@ BackwardPlan backward_plan(const galv_ctx* ctx, int64_t rows, int32_t experts, i
                            int64_t w_stride)
 {
     BackwardPlan p;
-    p.dy = plan_of(rows, n, k, dy, dy_stride, x, x_stride).dy;
+    p.dy = plan_of(ctx, rows, experts, n, k, dy, dy_stride, x, x_stride).dy;
     p.stride = p.dy ? (n + 7) / 8 * 8 : dy_stride;
     const void* const at = p.dy ? nullptr : dy;           // moved rows lie on 256 bytes
     const size_t a = w ? galv_expert_input_grad_workspace_bytes(ctx, rows, experts, n, k, at, p.stride, w, w_stride) : 0;

@@ -289,10 +289,10 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
 
 // ---- few rows
 //
-// Up to 64 rows in all: reading the weights of the experts that have some is all there is.  A CTA has 128 of an expert's weights' rows, so that two fit an SM
-// and one starts while the other runs; the CTAs of a cluster share the summed index, so that about two an SM stream.  Each sends its sums' slices of the tokens
-// to the CTA of the cluster that has them, which adds them in order: no second kernel, no memory between.  Which expert a cluster has is found on the device (the
-// s-th of those that have rows); clusters are launched for as many experts as there could be, those that are too many end at once.  The weights' first copies
+// Up to 64 rows in all: reading the weights of the experts that have some is all there is.  (And more rows of so few results that tiles of 256 would leave most SMs without one: the rows go
+// in tiles of 64 then.)  A CTA has 128 of an expert's weights' rows, so that two fit an SM and one starts while the other runs; the CTAs of a cluster share the summed index, so that about two an SM stream.  Each sends its sums' slices of the tokens
+// to the CTA of the cluster that has them, which adds them in order: no second kernel, no memory between.  Which tile of rows a cluster has is found on the device; clusters
+// are launched for as many as there could be, those that are too many end at once.  The weights' first copies
 // start before the kernel in front, which puts the tokens into 8-bit integers, is over.  1 x 8192 x 8192 in 8-bit integers takes 15.4 us beside packing (67 MB: 4.4 TB/s, of which 4 us are the start
 // and the way out; in the kernel above 21.6), 64 rows over 64 experts of 4096 x 2048 50 us (280 MB, 5.6 TB/s).
 
@@ -330,7 +330,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_consta
     if (warp == 2) tc::tmem_alloc<1>(slot, columns);
     if (K != kWhole || !a.in_front) tc::before_is_over();
     tc::next_may_start();
-    if (warp == 3) experts_nth(a.ends, a.experts, a.rows, nth, mine);
+    if (warp == 3) experts_nth(a.ends, a.experts, a.rows, kFewRows, nth, mine);
     tc::fence_before();
     __syncthreads();
     const int expert = mine[0], row0 = mine[1], count = mine[2];
@@ -363,7 +363,12 @@ expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_consta
             const int ahead = min(stages, chunks);
             auto weights = [&](int s, int it) {
                 tc::bar_expect(full + 8 * s, stage);
-                tc::load_3d(base + s * stage, &w_map, (c0 + it) * elements, (int)n0, expert, full + 8 * s);
+                if (K == kInputGrad) {
+                    tc::load_3d(base + s * stage, &w_map, (int)n0, (c0 + it) * elements, expert, full + 8 * s);
+                    tc::load_3d(base + s * stage + kRowsBytes / 2, &w_map, (int)n0 + 64, (c0 + it) * elements, expert, full + 8 * s);
+                } else {
+                    tc::load_3d(base + s * stage, &w_map, (c0 + it) * elements, (int)n0, expert, full + 8 * s);
+                }
             };
             for (int it = 0; it < ahead; ++it) weights(it, it);
             tc::before_is_over();
@@ -393,7 +398,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_consta
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (j < steps) {
-                        const uint64_t wo = tc::operand(ws + j * 32, 16, 1024), xo = tc::operand(xs + j * 32, 16, 1024);
+                        const uint64_t wo = K == kInputGrad ? tc::operand(ws + j * 2048, kRowsBytes / 2, 1024) : tc::operand(ws + j * 32, 16, 1024), xo = tc::operand(xs + j * 32, 16, 1024);
                         if (K == kWhole) tc::mma_i8<1>(tmem, wo, xo, what, it > 0 || j > 0);
                         else tc::mma_f16<1>(tmem, wo, xo, what, it > 0 || j > 0);
                     }
@@ -471,13 +476,19 @@ AlignPlan align_plan(int64_t rows, int64_t x_cols, const void* x, int64_t x_stri
     return p;
 }
 
+// Tiles of 64 rows there can be, whatever the ends say, times tiles of 128 weights' rows.
+int64_t few_units(const ProductArgs& a) { return (a.rows / kFewRows + (a.rows < a.experts ? a.rows : a.experts)) * ((a.n + 127) / 128); }
+
+// Few rows; or a long sum for few results: clusters of 8 with four chunks a CTA or more, all at once on the card (100 rows x 32768 x 16 in 8-bit integers with packing: 60 us in the kernel above, 26 here).
+bool is_few(const galv_ctx* ctx, const ProductArgs& a) { return a.rows <= kFewRows || (a.chunks >= 32 && few_units(a) * 8 <= 2 * ctx->num_sms); }
+
 template <int K, typename O>
 cudaError_t launch_few(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap& pm, const ProductArgs& a, cudaStream_t st)
 {
     const cudaError_t e = cudaFuncSetAttribute(expert_few_kernel<K, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
     if (e != cudaSuccess) return e;
     const int tiles = (int)((a.n + 127) / 128);
-    const long long units = tiles * (long long)(a.rows < a.experts ? a.rows : a.experts);
+    const int64_t units = a.rows <= kFewRows ? tiles * (int64_t)(a.rows < a.experts ? a.rows : a.experts) : few_units(a);
     int ranks = 1;                                        // two CTAs an SM at most, two chunks a CTA at least
     while (ranks < 8 && units * ranks <= ctx->num_sms && a.chunks >= ranks * 4) ranks *= 2;
     tc::Launch l((unsigned)(units * ranks), kFewThreads, kFewSmem, (unsigned)ranks, true, st);
@@ -487,9 +498,7 @@ cudaError_t launch_few(const galv_ctx* ctx, const CUtensorMap& wm, const CUtenso
 template <int K, typename O>
 cudaError_t launch(const galv_ctx* ctx, const CUtensorMap& wm, const CUtensorMap& xm, const CUtensorMap& pm, ProductArgs& a, cudaStream_t st)
 {
-    if constexpr (K != kInputGrad) {
-        if (a.rows <= kFewRows) return launch_few<K, O>(ctx, wm, pm, a, st);
-    }
+    if (is_few(ctx, a)) return launch_few<K, O>(ctx, wm, pm, a, st);
     const int smem = smem_of(a.experts);
     const cudaError_t e = cudaFuncSetAttribute(expert_product_kernel<K, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kExpertsMost));
     if (e != cudaSuccess) return e;
@@ -543,7 +552,7 @@ int product16(galv_ctx* ctx, const char* name, bool across, int64_t rows, int32_
     const CUtensorMapDataType type = dtype == GALV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     CUtensorMap wm, xm = {}, pm;                          // xm is not read where there are few rows
     cudaError_t e = galv_map_3d(&wm, type, w, experts, w_rows, w_cols, w_pitch * 2, across ? 64 : kHalf, 64);
-    if (e == cudaSuccess && (across || rows > kFewRows)) e = galv_mx_map(&xm, type, x, rows, k, x_stride * 2, kBox, 64, true);
+    if (e == cudaSuccess && rows > kFewRows) e = galv_mx_map(&xm, type, x, rows, k, x_stride * 2, kBox, 64, true);
     if (e == cudaSuccess) e = galv_mx_map(&pm, type, x, rows, k, x_stride * 2, kPart, 64, true);
     if (e != cudaSuccess) return wrong(GALV_ERR_CUDA, "tensor map");
     ProductArgs a;

@@ -69,9 +69,9 @@ __device__ __forceinline__ void experts_before(const int* begin, int experts, in
     if (lane == 0) before[experts] = tiles;
 }
 
-// The nth (from 0) of the experts that have rows, to shared memory by one warp: which it is, its first row and how many; -1, 0, 0 where there are fewer.  And
-// where the rows that belong to none begin.
-__device__ __forceinline__ void experts_nth(const int32_t* __restrict__ ends, int experts, long long rows, int nth, int* found)
+// The nth (from 0) of the tiles of `most` rows that the experts have, to shared memory by one warp: whose it is, its first row and how many; -1, 0, 0 where there are fewer.
+// And where the rows that belong to none begin.
+__device__ __forceinline__ void experts_nth(const int32_t* __restrict__ ends, int experts, long long rows, int most, int nth, int* found)
 {
     const int lane = threadIdx.x % 32;
     if (lane < 3) found[lane] = lane == 0 ? -1 : 0;
@@ -88,13 +88,20 @@ __device__ __forceinline__ void experts_nth(const int32_t* __restrict__ ends, in
         end = max(end, last);
         int first = __shfl_up_sync(0xffffffffu, end, 1);
         if (lane == 0) first = last;
-        const unsigned some = __ballot_sync(0xffffffffu, end > first);
-        if (end > first && before + __popc(some & ((1u << lane) - 1)) == nth) {
-            found[0] = e;
-            found[1] = first;
-            found[2] = end - first;
+        const int mine = experts_tiles(end - first, most);
+        int sum = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int other = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += other;
         }
-        before += __popc(some);
+        const int tile = nth - (before + sum - mine);
+        if (tile >= 0 && tile < mine) {
+            found[0] = e;
+            found[1] = first + tile * most;
+            found[2] = min(most, end - found[1]);
+        }
+        before += __shfl_sync(0xffffffffu, sum, 31);
         last = __shfl_sync(0xffffffffu, end, 31);
     }
     if (lane == 0) found[3] = last;

@@ -1,6 +1,6 @@
 // Rows of 8-bit integers with one scale each: packing and restoring a matrix.
 //
-// A row's scale needs all of the row before its first code: up to 16384 columns stay in the registers of the threads that read them, what lies
+// A row's scale needs all of the row before its first code: up to 32768 columns stay in the registers of the threads that read them, what lies
 // behind is read twice (from L2).  A code is the whole number nearest to the exact quotient x / s: x * (1 / s) is off by some units of its last place, so
 // the remainder x - q s, which an fp32 multiply-add has exactly, decides next to a half.
 // Bound by memory and issue slots, what is read and written once, 3 bytes an element from 16 bits: 4096 x 8192 in bf16 is packed in 22 us (4.5 TB/s; 15 instructions an element), 8192 x 4096 in fp32 in
@@ -40,18 +40,20 @@ __device__ __forceinline__ uint2 codes_of(const float (&v)[8], float s, float in
     return w;
 }
 
-// WARPS of a CTA of 8 have a row, of which a thread keeps P pieces of 8 columns in registers.
-template <typename T, bool VEC, int WARPS, int P>
-__global__ void __launch_bounds__(256, P > 4 ? 2 : sizeof(T) == 2 ? 5 : 4)
+// WARPS of a CTA's (8, or all of 16 or 32) have a row, of which a thread keeps 4 pieces of 8 columns in registers.
+constexpr int kPieces = 4;
+template <int WARPS> constexpr int kWarps = WARPS < 8 ? 8 : WARPS;
+template <typename T, bool VEC, int WARPS>
+__global__ void __launch_bounds__(kWarps<WARPS> * 32, (sizeof(T) == 2 ? 40 : 32) / kWarps<WARPS>)
 i8_pack_kernel(long long rows, int cols, int pieces, const T* __restrict__ x, long long stride, int8_t* __restrict__ codes, float* __restrict__ scales)
 {
-    constexpr int threads = WARPS * 32;
-    __shared__ uint32_t found[2][8];
+    constexpr int threads = WARPS * 32, rows_each = kWarps<WARPS> / WARPS, P = kPieces;
+    __shared__ uint32_t found[2][kWarps<WARPS>];
     const int t = threadIdx.x % threads, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     int turn = 0;
     tc::before_is_over();
     tc::next_may_start();                                 // behind the wait: the product that reads the codes takes it that all before this kernel is over
-    for (long long row0 = (long long)blockIdx.x * (8 / WARPS); row0 < rows; row0 += (long long)gridDim.x * (8 / WARPS), turn ^= 1) {
+    for (long long row0 = (long long)blockIdx.x * rows_each; row0 < rows; row0 += (long long)gridDim.x * rows_each, turn ^= 1) {
         const long long row = row0 + warp / WARPS;
         const bool in = row < rows;
         const T* from = x + row * stride;
@@ -132,23 +134,25 @@ __global__ void __launch_bounds__(kMxThreads) i8_unpack_kernel(const MxSpread sp
     }
 }
 
-template <typename T, bool VEC, int WARPS, int P>
+template <typename T, bool VEC, int WARPS>
 void launch_pack(int num_sms, int64_t rows, int64_t cols, const T* x, int64_t stride, int8_t* codes, float* scales, cudaStream_t st)
 {
-    const int64_t ctas = (rows + 8 / WARPS - 1) / (8 / WARPS), most = (int64_t)num_sms * 32;
-    tc::Launch l((unsigned)(ctas < most ? ctas : most), 256, 0, 0, true, st);
-    cudaLaunchKernelEx(&l.cfg, i8_pack_kernel<T, VEC, WARPS, P>, (long long)rows, (int)cols, (int)(i8_pitch(cols) / 8), x, (long long)stride, codes, scales);
+    constexpr int each = kWarps<WARPS> / WARPS;
+    const int64_t ctas = (rows + each - 1) / each, most = (int64_t)num_sms * 32;
+    tc::Launch l((unsigned)(ctas < most ? ctas : most), kWarps<WARPS> * 32, 0, 0, true, st);
+    cudaLaunchKernelEx(&l.cfg, i8_pack_kernel<T, VEC, WARPS>, (long long)rows, (int)cols, (int)(i8_pitch(cols) / 8), x, (long long)stride, codes, scales);
 }
 
-// As many warps a row as keep all of it with 4 pieces a thread (8 of the longest rows), and all 8 where there are few rows.
+// As many warps a row as keep all of it in registers (up to 32768 columns), and 8 where there are few rows.
 template <typename T, bool VEC>
 void pack_by_size(int num_sms, int64_t rows, int64_t cols, const T* x, int64_t stride, int8_t* codes, float* scales, cudaStream_t st)
 {
-    if (cols > 8192) launch_pack<T, VEC, 8, 8>(num_sms, rows, cols, x, stride, codes, scales, st);
-    else if (cols > 4096 || (cols > 256 && rows <= 2 * num_sms)) launch_pack<T, VEC, 8, 4>(num_sms, rows, cols, x, stride, codes, scales, st);
-    else if (cols > 2048) launch_pack<T, VEC, 4, 4>(num_sms, rows, cols, x, stride, codes, scales, st);
-    else if (cols > 1024) launch_pack<T, VEC, 2, 4>(num_sms, rows, cols, x, stride, codes, scales, st);
-    else launch_pack<T, VEC, 1, 4>(num_sms, rows, cols, x, stride, codes, scales, st);
+    if (cols > 16384) launch_pack<T, VEC, 32>(num_sms, rows, cols, x, stride, codes, scales, st);
+    else if (cols > 8192) launch_pack<T, VEC, 16>(num_sms, rows, cols, x, stride, codes, scales, st);
+    else if (cols > 4096 || (cols > 256 && rows <= 2 * num_sms)) launch_pack<T, VEC, 8>(num_sms, rows, cols, x, stride, codes, scales, st);
+    else if (cols > 2048) launch_pack<T, VEC, 4>(num_sms, rows, cols, x, stride, codes, scales, st);
+    else if (cols > 1024) launch_pack<T, VEC, 2>(num_sms, rows, cols, x, stride, codes, scales, st);
+    else launch_pack<T, VEC, 1>(num_sms, rows, cols, x, stride, codes, scales, st);
 }
 
 }  // namespace

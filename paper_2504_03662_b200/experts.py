@@ -228,7 +228,7 @@ class _Linear(torch.autograd.Function):
         g = _on(device)
         dm, xm, wm = gb._matrix(dy), gb._matrix(x) if need_w else (None, 0), gb._matrices(weight)
         ws = None
-        if not _lie(n, dm, xm, wm):
+        if not _lie(n, dm, xm, wm) or (need_w and rows >= 2048 * experts and experts * -(-n // 256) * -(-k // 256) < 64):      # few tiles: the library may split rows
             size = g.galv_expert_backward_workspace_bytes(rows, experts, n, k, dm, xm, wm)
             ws = _bytes(size, device) if size else None
         g.galv_expert_backward(rows, experts, n, k, ends, dm, xm, wm, gb._DTYPES[dtype], (dx.data_ptr(), k) if need_x else (None, 0), dw, db, ws)

@@ -132,7 +132,7 @@ def test_refusals(call):
 # ------------------------------------------------------------------------------------------------- forward and gradients
 
 CASES = [([1], 0, 1, 1), ([1], 0, 16, 2048), ([2, 0, 1], 1, 100, 64), ([0, 0, 5, 0], 0, 33, 70), ([31, 32, 33], 2, 257, 129), ([256], 0, 256, 256), ([300, 0, 257, 1], 70, 300, 200),
-         ([1100, 40], 0, 130, 96), ([3] * 40, 5, 65, 130), ([0] * 7, 9, 40, 24), ([17, 200, 600, 2, 0, 64], 3, 513, 320), ([2500], 100, 24, 40)]
+         ([1100, 40], 0, 130, 96), ([3] * 40, 5, 65, 130), ([0] * 7, 9, 40, 24), ([17, 200, 600, 2, 0, 64], 3, 513, 320), ([2500], 100, 24, 40), ([1100, 0, 6000], 5, 300, 77), ([9000], 0, 70, 264), ([100, 6300, 5], 33, 128, 130)]
 
 
 @gpu
@@ -150,6 +150,11 @@ def test_forward_and_gradients(counts, behind, n, k, dtype):
         for out in (dt, torch.float32):
             tol = (cut(min(most, 768)) + most / 768 * HALF) * f["adw"] + step(out, f["dw"])
             close(experts.weight_grad(dy, x, ends, out), f["dw"], tol, "dw")
+            base = numbers(5, len(counts) * n, k, out).reshape(len(counts), n, k).cuda()
+            total = f["dw"] + f64(base)
+            onto = experts.weight_grad(dy, x, ends, base=base)
+            close(onto, total, tol + step(out, total) + HALF * np.abs(total), "dw onto base")
+            assert experts.weight_grad(dy, x, ends, base=base, out=base) is base and torch.equal(base, onto)
             tol = (most / 64 + 16) * HALF * f["adb"] + step(out, f["db"])
             close(experts.bias_grad(dy, ends, out), f["db"], tol, "db")
 
@@ -175,6 +180,25 @@ def test_products_in_8_bit_integers(counts, behind, n, k, dtype):
     got = experts.matmul(p, w, ends, bias, dt)
     close(got, want, 3 * HALF * size + 2 * HALF * np.abs(want) + step(dt, want))
     assert torch.equal(experts.matmul(x, w, ends, bias), got)
+
+
+@gpu
+@pytest.mark.parametrize("counts,behind,n,k", [([300], 0, 20, 8192), ([70, 0, 130], 9, 136, 4099), ([64, 64, 1], 0, 33, 2048), ([100], 3, 4096, 20), ([65], 0, 9000, 24)])
+def test_long_sums_for_few_results(counts, behind, n, k):
+    """More than 64 rows, whose tiles of 64 clusters take: forward along the weights' rows, the input gradient across them, and the same rows in 8-bit integers."""
+    x, w, dy, bias = inputs(counts, behind, n, k, "bf16")
+    ends, spans = ends_of(counts), clamped(np.cumsum(counts), x.shape[0])
+    f = formulas(clean(x, behind), f64(w), spans, clean(dy, behind), f64(bias))
+    close(experts.matmul(x, w, ends, bias), f["y"], cut(k) * f["ay"] + HALF * np.abs(f["y"]) + step(B, f["y"]), "y")
+    close(experts.input_grad(dy, w, ends), f["dx"], cut(n) * f["adx"] + step(B, f["dx"]), "dx")
+    p, q = i8.pack(x), i8.pack(w.view(-1, k))
+    got = experts.matmul(p, q, ends, dtype=torch.float32)
+    a, b = p.codes[:, :k].double(), q.codes[:, :k].double().view(len(counts), n, k)
+    want = torch.zeros_like(got, dtype=torch.float64)
+    for e, (s, t) in enumerate(spans):
+        want[s:t] = (a[s:t] @ b[e].t()) * p.scales[s:t, None].double() * q.scales.view(-1, n)[e].double()
+    assert ((got.double() - want).abs() <= 4 * HALF * want.abs()).all()
+    assert torch.equal(experts.matmul(x.float(), q, ends), got)
 
 
 @gpu

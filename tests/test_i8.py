@@ -102,7 +102,7 @@ def test_refusals(call):
 
 @gpu
 @pytest.mark.parametrize("dtype", list(DT))
-@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 16), (1, 8192), (3, 17), (9, 2048), (7, 2049), (300, 1000), (2, 16384), (3, 16385), (2, 40011), (1000, 7), (2500, 33)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 16), (1, 8192), (3, 17), (9, 2048), (7, 2049), (300, 1000), (2, 16384), (3, 16385), (400, 9000), (310, 20000), (2, 32769), (2, 40011), (1000, 7), (2500, 33)])
 def test_pack_and_unpack(rows, cols, dtype):
     for pad in (0, 8, 5):
         x = numbers(rows * 7 + cols + pad, rows, cols, DT[dtype], pad)
