@@ -293,8 +293,8 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
 // in tiles of 64 then.)  A CTA has 128 of an expert's weights' rows, so that two fit an SM and one starts while the other runs; the CTAs of a cluster share the summed index, so that about two an SM stream.  Each sends its sums' slices of the tokens
 // to the CTA of the cluster that has them, which adds them in order: no second kernel, no memory between.  Which tile of rows a cluster has is found on the device; clusters
 // are launched for as many as there could be, those that are too many end at once.  The weights' first copies
-// start before the kernel in front, which puts the tokens into 8-bit integers, is over.  1 x 8192 x 8192 in 8-bit integers takes 15.4 us beside packing (67 MB: 4.4 TB/s, of which 4 us are the start
-// and the way out; in the kernel above 21.6), 64 rows over 64 experts of 4096 x 2048 50 us (280 MB, 5.6 TB/s).
+// start before the kernel in front, which puts the tokens into 8-bit integers, is over.  1 x 8192 x 8192 in 8-bit integers takes 15.8 us with packing in front (67 MB: 6.4 TB/s for 10.4 us; the rest
+// is the start and, for 2 us, joining; in the kernel above 21.6 alone), 48 x 2048 x 8192 10, 64 rows over 64 experts of 4096 x 2048 52 (280 MB, 5.4 TB/s).
 
 constexpr int kFewThreads = 256, kFewRows = 64, kFewStages = 6;
 constexpr int kFewRing = 6 * (128 + kPart) * kChunkBytes;      // shared memory of chunks and of what other CTAs send: 6 chunks for up to 16 tokens, 4 for 64; 5 and 3 in a cluster
@@ -307,6 +307,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_consta
     extern __shared__ unsigned char raw[];
     const uint32_t base = (tc::smem_at(raw) + 1023) & ~1023u;
     const uint32_t bars = base + kFewRing, full = bars, empty = full + 8 * kFewStages, acc_full = empty + 8 * kFewStages, slot = acc_full + 8;
+    __shared__ float x_scales[kFewRows];
     __shared__ int failed, mine[4];                       // expert (or -1), its first row, how many; where rows of no expert begin
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -417,24 +418,37 @@ expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_consta
     const bool has = warp >= 4 && expert >= 0 && ch < a.n;
     const float bias = a.bias && has ? mx_float(((const O*)a.bias)[at]) : 0.f, w_scale = K == kWhole && has ? a.w_scales[at] : 0.f;
     O* const y = (O*)a.y + ch;
-    auto put = [&](int token, uint32_t sum) {
-        y[(long long)(row0 + token) * a.stride] = mx_round<O>(number<K>(sum, K == kWhole ? a.x_scales[row0 + token] : 0.f, w_scale, bias));
-    };
+    auto put = [&](int token, uint32_t sum) { y[(long long)(row0 + token) * a.stride] = mx_round<O>(number<K>(sum, K == kWhole ? x_scales[token] : 0.f, w_scale, bias)); };
+    if (K == kWhole && warp >= 4) {                       // the tokens' scales, on their way while the sums are
+        if (row < count) x_scales[row] = a.x_scales[row0 + row];
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+    }
     bool ok = true;
     if (warp >= 4) {
         ok = __shfl_sync(0xffffffffu, (int)(lane == 0 && waited(acc_full, 0)), 0) != 0;
         tc::fence_after();
         if (ok) {
+            // sums of token `to * each + j` to the `to`-th CTA: its [ranks][each] rows of 128 sums
+            int to = 0, j = 0;
+            uint32_t there = tc::in_cta(inbox + (rank * each * 128 + row) * 4, 0);
 #pragma unroll 1
-            for (int j = 0; j < tokens; j += 16) {
+            for (int col = 0; col < tokens; col += 16) {
                 uint32_t v[16];
-                tc::tmem_load16(tmem + j + ((uint32_t)quad * 32 << 16), v);
+                tc::tmem_load16(tmem + col + ((uint32_t)quad * 32 << 16), v);
                 tc::tmem_wait_load();
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int col = j + i;
-                    if (ranks > 1) asm volatile("st.shared::cluster.b32 [%0], %1;" :: "r"(tc::in_cta(inbox + ((rank * each + col % each) * 128 + row) * 4, col / each)), "r"(v[i]) : "memory");
-                    else if (has && col < count) put(col, v[i]);
+                    if (ranks > 1) {
+                        asm volatile("st.shared::cluster.b32 [%0], %1;" :: "r"(there), "r"(v[i]) : "memory");
+                        there += 512;
+                        if (++j == each) {
+                            j = 0;
+                            ++to;
+                            there = tc::in_cta(inbox + (rank * each * 128 + row) * 4, to < ranks ? to : 0);
+                        }
+                    } else if (has && col + i < count) {
+                        put(col + i, v[i]);
+                    }
                 }
             }
         }
@@ -447,12 +461,13 @@ expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_consta
             for (int j = 0; j < each; ++j) {
                 const int col = rank * each + j;
                 if (col >= count) break;
-                uint32_t sum = 0;
-                for (int r = 0; r < ranks; ++r) {
-                    uint32_t v;
-                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(inbox + ((r * each + j) * 128 + row) * 4));
-                    sum = r == 0 ? v : K == kWhole ? sum + v : __float_as_uint(__uint_as_float(sum) + __uint_as_float(v));
-                }
+                uint32_t v[8], sum = 0;
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r < ranks) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v[r]) : "r"(inbox + ((r * each + j) * 128 + row) * 4));
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r < ranks) sum = r == 0 ? v[r] : K == kWhole ? sum + v[r] : __float_as_uint(__uint_as_float(sum) + __uint_as_float(v[r]));
                 put(col, sum);
             }
     }
