@@ -75,7 +75,7 @@ def _products(x: torch.Tensor, weight: i8.Packed, ends: torch.Tensor, bias, dtyp
 
 def matmul(x: Union[torch.Tensor, i8.Packed], weight: Union[torch.Tensor, i8.Packed], ends: torch.Tensor, bias: Optional[torch.Tensor] = None,
            dtype: Optional[torch.dtype] = None) -> torch.Tensor:
-    """x weight[e]^T + bias[e] for each row of x and its expert e.
+    """x weight[e]^T + bias[e] for each row of x and its expert e.  Without gradients (`linear` has them).
 
     weight [experts][columns of y][columns of x] and x [rows][columns] in 16 bits; or weights held in 8-bit integers with the experts' rows one behind the
     other, and x in numbers, which are put into 8-bit integers in the call, or held so too.  bias [experts][columns of y] of y's type: x's, or `dtype` where x is held.

@@ -264,6 +264,10 @@ def test_nobody_has_rows(rows):
     assert not experts.input_grad(dy, w, ends).any() and not experts.weight_grad(dy, x, ends).any() and not experts.bias_grad(dy, ends).any()
     base = numbers(1, 120, 40, torch.float32).view(5, 24, 40).cuda()
     assert torch.equal(experts.weight_grad(dy, x, ends, base=base), base)
+    leaves = [t.clone().requires_grad_() for t in (x, w, torch.ones(5, 24, dtype=B, device="cuda"))]
+    y = experts.linear(leaves[0], leaves[1], ends, leaves[2])
+    grads = torch.autograd.grad(y, leaves, dy)
+    assert not y.any() and all(g.shape == t.shape and not g.any() for g, t in zip(grads, leaves))
 
 
 @gpu
