@@ -547,7 +547,7 @@ int galv_i8_linear(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int6
  * rounded additions), biases and base are added in fp32, results rounded once.  dw, base [experts][n][k] contiguous of `dw_dtype`, db [experts][n] of
  * `db_dtype` (`dtype` or GALV_F32); base NULL: zero; dw may be base.  An expert without rows has base or zeros for its gradient.  The order of
  * the sums is fixed by sizes, ends, strides and alignment.  Operands whose rows do not start on 16-byte boundaries are moved to ones that do, in the
- * workspace (256-byte aligned, the bytes that the query gives for the same sizes, pointers and strides; 0: may be NULL).  After galv_expert_matmul it holds
+ * workspace, where weight gradients of few tiles and long experts keep the sums of parts of their rows too (256-byte aligned, the bytes that the query gives for the same sizes, pointers and strides; 0: may be NULL).  After galv_expert_matmul it holds
  * x, if that was moved, [rows] rows ceil(k / 8) * 8 apart, and from the next multiple of 256 bytes on w, if that was moved, its rows as far apart.
  */
 size_t galv_expert_matmul_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* x,

@@ -11,6 +11,7 @@ from paper_2504_03662_b200 import binding as gb
 from paper_2504_03662_b200 import experts, i8, mx
 
 from .test_mx import HALF, close, f64, numbers, step
+from .test_mx_paths import counted  # noqa: F401  (sets the count of waits that have run out from the host, and back)
 
 gpu = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
@@ -322,6 +323,22 @@ def test_refusals_of_the_library():
         g.galv_i8_linear(8, 2, 16, 64, ends, (xp, 64), q.codes, s, None, (yp, 16), gb.BF16, None)
     assert e.value.code == gb.ERR_WORKSPACE
     assert not y.any()
+
+
+@gpu
+def test_products_raise_behind_a_wait_that_ran_out(counted):                        # noqa: F811
+    """The count is the library's own: an earlier product's void result is said by the next call of any of them, once."""
+    x, w, dy, _ = inputs([30, 70], 0, 40, 64, "bf16")
+    ends, p, q = ends_of([30, 70]), i8.pack(x), i8.pack(w.view(-1, 64))
+    calls = [lambda: experts.matmul(x, w, ends), lambda: experts.input_grad(dy, w, ends), lambda: experts.weight_grad(dy, x, ends), lambda: experts.matmul(p, q, ends),
+             lambda: experts.matmul(x, q, ends), lambda: i8.matmul(p, q), lambda: i8.linear(x, q)]
+    want = [c() for c in calls]
+    for c, right in zip(calls, want):
+        counted(1)
+        with pytest.raises(gb.GalvError) as e:
+            c()
+        assert e.value.code == gb.ERR_TIMEOUT
+        assert torch.equal(c(), right)
 
 
 @gpu
