@@ -256,6 +256,32 @@ def test_weight_gradients_onto_earlier_ones(dtype, out):
 
 
 @gpu
+@pytest.mark.parametrize("n, k", [(1, 1), (3, 5), (33, 7), (40, 31), (35, 33), (7, 127), (130, 129), (257, 134), (65, 300), (290, 385)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_weight_gradients_whose_rows_start_anywhere(n, k, out):
+    """Results at every distance from a 16-byte boundary, with a base at another one: whole numbers, whose sums stay below 256 and are exact, and nothing beside them is written."""
+    counts, E, to = [5, 0, 20, 1], 4, DT[out]
+    rng = np.random.default_rng(n * 1000 + k)
+    x, dy = (torch.tensor(rng.integers(-2, 3, (sum(counts), c)), dtype=torch.bfloat16).cuda() for c in (k, n))
+    base = torch.tensor(rng.integers(-100, 101, (E, n, k)), dtype=to).cuda()
+    ends, size = ends_of(counts), E * n * k
+    dw = torch.tensor(formulas(f64(x), np.zeros((E, n, k)), clamped(np.cumsum(counts), len(x)), f64(dy))["dw"], dtype=to).cuda()
+    for at in range(0, 16 // to.itemsize, 1 if k == 129 else 3):
+        for beside in (None, 0, 1):
+            around = torch.full((size + 64,), 77., dtype=to, device="cuda")
+            result = around[at:at + size].view(E, n, k)
+            if beside is None:
+                first = None
+            elif beside == 0:
+                first = result.copy_(base)
+            else:
+                first = torch.zeros(size + 64, dtype=to, device="cuda")[at + beside:at + beside + size].view(E, n, k).copy_(base)
+            experts.weight_grad(dy, x, ends, to, base=first, out=result)
+            assert torch.equal(result, dw if first is None else dw + base), (at, beside)
+            assert (around[:at] == 77).all() and (around[at + size:] == 77).all()
+
+
+@gpu
 @pytest.mark.parametrize("rows", [0, 3])
 def test_nobody_has_rows(rows):
     x, dy, w = torch.full((rows, 40), float("nan"), dtype=B, device="cuda"), torch.full((rows, 24), float("nan"), dtype=B, device="cuda"), torch.ones(5, 24, 40, dtype=B, device="cuda")
