@@ -64,15 +64,6 @@ __device__ __forceinline__ void clear_rows(uint32_t at, int count)
     }
 }
 
-// Where an expert has no rows: base, or zeros, from boundaries of 32 elements on.
-template <typename O>
-__device__ __forceinline__ void fill(const O* base, O* out, long long k, int rows, int cols)
-{
-    for (int r = 0; r < rows; ++r)
-        for (int c = threadIdx.x % 32 - (int)(reinterpret_cast<uintptr_t>(out + r * k) / sizeof(O) & 31); c < cols; c += 32)
-            if (c >= 0) out[r * k + c] = base ? base[r * k + c] : mx_zero<O>();
-}
-
 // 16 bytes of results: sums, and what base has there
 __device__ __forceinline__ uint4 four_words(const uint32_t* v, const uint4* base, float)
 {
@@ -323,13 +314,11 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
             } else if (ok) {
                 const long long at = w.part * a.n * a.k + r0 * a.k + c0;
                 const O* const b = a.base ? (const O*)a.base + at : nullptr;
-                if (w.count == 0) {
-                    fill<O>(b, (O*)a.dw + at, a.k, rows, cols);
-                } else if (sizeof(O) == 4 || !b) {
-                    tile_out::move_out_odd<O>(from + acc * kTile, mine, b, (O*)a.dw + at, a.k, rows, cols);
+                if (sizeof(O) == 4 || !b) {
+                    tile_out::move_out_odd<O>(from + acc * kTile, mine, b, (O*)a.dw + at, a.k, rows, cols, w.count > 0);
                 } else {                                  // base is added before the rounding, a column a lane
                     const long long own = lane / 16 * a.k + lane % 16;
-                    tile_out::move_out<O>(from + acc * kTile, mine, b + own, (O*)a.dw + at + own, a.k, rows, cols, false);
+                    tile_out::move_out<O>(from + acc * kTile, mine, b + own, (O*)a.dw + at + own, a.k, rows, cols, false, w.count > 0);
                 }
             }
             if (!ok) break;

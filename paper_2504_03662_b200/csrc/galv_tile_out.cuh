@@ -29,9 +29,9 @@ template <typename O> struct RoundFour<float4, O> { static __device__ __forceinl
 
 // A warp's 32 x 128 sums in tensor memory, a row a lane, to a matrix with rows k apart: 16 columns at a time go through the warp's shared memory
 // (rows of 64 bytes, their 16-byte pieces exchanged by row / 2 % 4), so that lanes next to one another write next to one another.  base and out point to
-// the thread's first place; `rows` and `cols` of them exist.  All loads of a round come before its first store: out may be base.
+// the thread's first place; `rows` and `cols` of them exist.  Without `sums` they count as zeros and tensor memory is not read.  All loads of a round come before its first store: out may be base.
 template <typename O>
-__device__ __forceinline__ void move_out(uint32_t tmem, uint32_t mine, const O* base, O* out, long long k, int rows, int cols, bool vec)
+__device__ __forceinline__ void move_out(uint32_t tmem, uint32_t mine, const O* base, O* out, long long k, int rows, int cols, bool vec, bool sums = true)
 {
     const int lane = threadIdx.x % 32;
     using Q = typename Four<O>::type;
@@ -42,8 +42,13 @@ __device__ __forceinline__ void move_out(uint32_t tmem, uint32_t mine, const O* 
 #pragma unroll 1
     for (int j = 0; j < 128; j += 16) {
         uint32_t s[16];
-        tc::tmem_load16(tmem + j, s);
-        tc::tmem_wait_load();
+        if (sums) {
+            tc::tmem_load16(tmem + j, s);
+            tc::tmem_wait_load();
+        } else {
+#pragma unroll
+            for (int q = 0; q < 16; ++q) s[q] = 0;
+        }
         __syncwarp();
 #pragma unroll
         for (int q = 0; q < 4; ++q)
@@ -90,7 +95,7 @@ __device__ __forceinline__ void move_out(uint32_t tmem, uint32_t mine, const O* 
 // instructions and by lines a store: a column a lane, two rows a store, took 54 us for 7 gradients of 2731 x 1365 in fp16 where this takes 41, and 3513 for 64 of 2048 x 4090 onto fp32
 // where this takes 1490 (1040 and 690 without base; where all of it stays in L2, 33 to 67 MB, up to 7 us more).  base only beside fp32: 16-bit results are rounded on their way in.
 template <typename O>
-__device__ __forceinline__ void move_out_odd(uint32_t tmem, uint32_t mine, const O* base, O* out, long long k, int rows, int cols)
+__device__ __forceinline__ void move_out_odd(uint32_t tmem, uint32_t mine, const O* base, O* out, long long k, int rows, int cols, bool sums)
 {
     constexpr int size = sizeof(O), each = 64 / size;     // columns a round
     const int lane = threadIdx.x % 32, bytes = cols * size;
@@ -128,17 +133,19 @@ __device__ __forceinline__ void move_out_odd(uint32_t tmem, uint32_t mine, const
     for (int j = 0; j <= 128 * size && j < bytes + 63; j += 64) {
         const uint32_t turn = j & 64;
         if (j < 128 * size) {
-            uint32_t s[each], w[16];
-            if constexpr (size == 2) {
+            uint32_t w[16];
+            if (!sums) {
+#pragma unroll
+                for (int q = 0; q < 16; ++q) w[q] = 0;
+            } else if constexpr (size == 2) {
+                uint32_t s[each];
                 tc::tmem_load32(tmem + j / size, s);
                 tc::tmem_wait_load();
 #pragma unroll
                 for (int q = 0; q < 16; ++q) w[q] = join<O>(__uint_as_float(s[2 * q]), __uint_as_float(s[2 * q + 1]));
             } else {
-                tc::tmem_load16(tmem + j / size, s);
+                tc::tmem_load16(tmem + j / size, w);
                 tc::tmem_wait_load();
-#pragma unroll
-                for (int q = 0; q < 16; ++q) w[q] = s[q];
             }
             __syncwarp();
 #pragma unroll
