@@ -420,7 +420,7 @@ struct GradPlan { size_t dy, x, partial, total; int splits; };
 GradPlan plan_of(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride)
 {
     auto moved = [&](const void* p, int64_t stride, int64_t cols) {
-        return mx_rows16(p, stride, GALV_BF16) && stride * 2 < ((int64_t)1 << 40) ? 0 : up((size_t)rows * ((cols + 7) / 8 * 8) * 2);
+        return mx_rows16(p, stride, GALV_BF16) && stride * 2 < ((int64_t)1 << 40) ? 0 : up((size_t)rows * galv_aligned_pitch(cols) * 2);
     };
     GradPlan p;
     p.dy = moved(dy, dy_stride, n);
@@ -503,15 +503,15 @@ extern "C" int galv_expert_weight_grad(galv_ctx* ctx, int64_t rows, int32_t expe
         a.splits = p.splits;
         if (p.partial) partial = (float*)((char*)workspace + p.dy + p.x);
         if (p.dy) {
-            galv_align_rows(ctx, rows, n, dy, dy_stride, workspace, (n + 7) / 8 * 8, st);
+            galv_align_rows(ctx, rows, n, dy, dy_stride, workspace, galv_aligned_pitch(n), st);
             dy = workspace;
-            dy_stride = (n + 7) / 8 * 8;
+            dy_stride = galv_aligned_pitch(n);
         }
         if (p.x) {
             void* const to = (char*)workspace + p.dy;
-            galv_align_rows(ctx, rows, k, x, x_stride, to, (k + 7) / 8 * 8, st);
+            galv_align_rows(ctx, rows, k, x, x_stride, to, galv_aligned_pitch(k), st);
             x = to;
-            x_stride = (k + 7) / 8 * 8;
+            x_stride = galv_aligned_pitch(k);
         }
         const CUtensorMapDataType type = dtype == GALV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
         cudaError_t e = galv_mx_map(&dm, type, dy, rows, n, dy_stride * 2, kTokens, 64, true);
@@ -566,7 +566,7 @@ BackwardPlan backward_plan(const galv_ctx* ctx, int64_t rows, int32_t experts, i
 {
     BackwardPlan p;
     p.dy = plan_of(ctx, rows, experts, n, k, dy, dy_stride, x, x_stride).dy;
-    p.stride = p.dy ? (n + 7) / 8 * 8 : dy_stride;
+    p.stride = p.dy ? galv_aligned_pitch(n) : dy_stride;
     const void* const at = p.dy ? nullptr : dy;           // moved rows lie on 256 bytes
     const size_t a = w ? galv_expert_input_grad_workspace_bytes(ctx, rows, experts, n, k, at, p.stride, w, w_stride) : 0;
     const size_t b = x ? galv_expert_weight_grad_workspace_bytes(ctx, rows, experts, n, k, at, p.stride, x, x_stride) : 0;

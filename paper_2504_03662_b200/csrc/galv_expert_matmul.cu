@@ -485,8 +485,8 @@ struct AlignPlan { size_t x, w, total; };
 AlignPlan align_plan(int64_t rows, int64_t x_cols, const void* x, int64_t x_stride, int64_t experts, int64_t n, int64_t k, const void* w, int64_t w_stride)
 {
     AlignPlan p;
-    p.x = mx_rows16(x, x_stride, GALV_BF16) && x_stride * 2 < ((int64_t)1 << 40) ? 0 : up((size_t)rows * ((x_cols + 7) / 8 * 8) * 2);
-    p.w = mx_rows16(w, w_stride, GALV_BF16) && n * w_stride * 2 < ((int64_t)1 << 40) ? 0 : up((size_t)experts * n * ((k + 7) / 8 * 8) * 2);
+    p.x = mx_rows16(x, x_stride, GALV_BF16) && x_stride * 2 < ((int64_t)1 << 40) ? 0 : up((size_t)rows * galv_aligned_pitch(x_cols) * 2);
+    p.w = mx_rows16(w, w_stride, GALV_BF16) && n * w_stride * 2 < ((int64_t)1 << 40) ? 0 : up((size_t)experts * n * galv_aligned_pitch(k) * 2);
     p.total = p.x + p.w;
     return p;
 }
@@ -554,13 +554,13 @@ int product16(galv_ctx* ctx, const char* name, bool across, int64_t rows, int32_
     cudaStream_t st = (cudaStream_t)stream;
     int64_t w_pitch = w_stride;
     if (p.x) {
-        galv_align_rows(ctx, rows, k, x, x_stride, workspace, (k + 7) / 8 * 8, st);
+        galv_align_rows(ctx, rows, k, x, x_stride, workspace, galv_aligned_pitch(k), st);
         x = workspace;
-        x_stride = (k + 7) / 8 * 8;
+        x_stride = galv_aligned_pitch(k);
     }
     if (p.w) {
         void* const to = (char*)workspace + p.x;
-        w_pitch = (w_cols + 7) / 8 * 8;
+        w_pitch = galv_aligned_pitch(w_cols);
         galv_align_rows(ctx, (int64_t)experts * w_rows, w_cols, w, w_stride, to, w_pitch, st);
         w = to;
     }

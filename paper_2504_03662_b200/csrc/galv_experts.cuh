@@ -108,4 +108,7 @@ __device__ __forceinline__ void experts_nth(const int32_t* __restrict__ ends, in
 }
 
 // Matrices whose rows bulk copies cannot take (not on 16-byte boundaries) into rows that they can, zeros behind their ends (galv_mx_wgrad.cu).
+// They are placed on whole lines, short ones on whole sectors: bulk copies of rows that start in the middle of a sector took up to a third longer (8192 rows x 4096 x 1000, input gradient: 87 us,
+// 70 in whole sectors, 62 in whole lines).
+inline int64_t galv_aligned_pitch(int64_t cols) { return cols >= 512 ? (cols + 63) / 64 * 64 : (cols + 15) / 16 * 16; }
 void galv_align_rows(const galv_ctx* ctx, int64_t rows, int64_t cols, const void* x, int64_t stride, void* out, int64_t pitch, cudaStream_t st);
