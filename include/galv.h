@@ -510,7 +510,7 @@ int galv_mx_matmul(galv_ctx* ctx, int64_t m, int64_t n, int64_t k, const uint8_t
  * Rows of 8-bit integers: a matrix [rows][cols] with one scale a row, and products of two such matrices (the paper has no counterpart).
  *   scale[r] = max(largest magnitude of row r, 2^-100) / 127 (fp32, rounded),  code[r][c] = the whole number nearest to x[r][c] / scale[r], ties to even
  * decided by the exact quotient.  A row that holds an infinity or a NaN gets a NaN for its scale and zeros for its codes: it stands for NaN as a whole.
- * codes [rows][cols rounded up to a multiple of 32] signed bytes, zero behind a row's end, 16-byte aligned; scales [rows] fp32.  Of tokens a row is a token, of
+ * codes [rows][cols rounded up to a multiple of 16] signed bytes, zero behind a row's end, 16-byte aligned; scales [rows] fp32.  Of tokens a row is a token, of
  * weights [n][k] an output channel.  Matrices of numbers, limits and streams as above.
  */
 #define GALV_I8_MOST 131071  /* columns of a product of 8-bit integers: sums of so many stay within 32 bits whatever the codes */

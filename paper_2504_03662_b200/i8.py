@@ -16,7 +16,7 @@ from .mx import _bytes, _device, _kind, _on, _rows, _vector
 
 def pitch(cols: int) -> int:
     """Bytes of a row of codes."""
-    return (cols + 31) // 32 * 32
+    return (cols + 15) // 16 * 16
 
 
 class Packed:
