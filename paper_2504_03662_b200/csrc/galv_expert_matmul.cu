@@ -594,14 +594,13 @@ bool whole_pointers_ok(int64_t n, const int32_t* ends, const int8_t* w_codes, co
            (!ends || mx_aligned(ends, 4));
 }
 
-int whole_launch(galv_ctx* ctx, const char* name, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const int8_t* x_codes, const float* x_scales,
-                 const int8_t* w_codes, const float* w_scales, const void* bias, void* y, int64_t y_stride, int32_t dtype, bool in_front, cudaStream_t st)
+int whole_launch(galv_ctx* ctx, const char* name, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const int8_t* x_codes, int64_t x_pitch,
+                 const float* x_scales, const int8_t* w_codes, const float* w_scales, const void* bias, void* y, int64_t y_stride, int32_t dtype, bool in_front, cudaStream_t st)
 {
-    const int64_t pitch = i8_pitch(k);
     CUtensorMap wm, xm = {}, pm;
-    cudaError_t e = galv_map_3d(&wm, CU_TENSOR_MAP_DATA_TYPE_UINT8, w_codes, experts, n, k, pitch, kHalf, kChunkBytes);
-    if (e == cudaSuccess && rows > kFewRows) e = galv_mx_map(&xm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, k, pitch, kBox, kChunkBytes, true);
-    if (e == cudaSuccess) e = galv_mx_map(&pm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, k, pitch, kPart, kChunkBytes, true);
+    cudaError_t e = galv_map_3d(&wm, CU_TENSOR_MAP_DATA_TYPE_UINT8, w_codes, experts, n, k, i8_pitch(k), kHalf, kChunkBytes);
+    if (e == cudaSuccess && rows > kFewRows) e = galv_mx_map(&xm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, k, x_pitch, kBox, kChunkBytes, true);
+    if (e == cudaSuccess) e = galv_mx_map(&pm, CU_TENSOR_MAP_DATA_TYPE_UINT8, x_codes, rows, k, x_pitch, kPart, kChunkBytes, true);
     if (e != cudaSuccess) {
         char text[100];
         snprintf(text, sizeof(text), "%s: tensor map", name);
@@ -663,10 +662,10 @@ extern "C" int galv_i8_matmul(galv_ctx* ctx, int64_t rows, int32_t experts, int6
     if (may != GALV_OK) return may;
     MxDevice dev(ctx);
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
-    return whole_launch(ctx, "galv_i8_matmul", rows, experts, n, k, ends, x_codes, x_scales, w_codes, w_scales, bias, y, y_stride, dtype, false, (cudaStream_t)stream);
+    return whole_launch(ctx, "galv_i8_matmul", rows, experts, n, k, ends, x_codes, i8_pitch(k), x_scales, w_codes, w_scales, bias, y, y_stride, dtype, false, (cudaStream_t)stream);
 }
 
-extern "C" size_t galv_i8_linear_workspace_bytes(int64_t rows, int64_t k) { return mx_size_ok(rows, k) ? up((size_t)rows * i8_pitch(k)) + up((size_t)rows * 4) : 0; }
+extern "C" size_t galv_i8_linear_workspace_bytes(int64_t rows, int64_t k) { return mx_size_ok(rows, k) ? up((size_t)rows * i8_pitch_within(k)) + up((size_t)rows * 4) : 0; }
 
 extern "C" int galv_i8_linear(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* x, int64_t x_stride, const int8_t* w_codes,
                               const float* w_scales, const void* bias, void* y, int64_t y_stride, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream)
@@ -683,8 +682,8 @@ extern "C" int galv_i8_linear(galv_ctx* ctx, int64_t rows, int32_t experts, int6
     MxDevice dev(ctx);
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
     int8_t* const codes = (int8_t*)workspace;
-    float* const scales = (float*)(codes + up((size_t)rows * i8_pitch(k)));
-    const cudaError_t e = galv_i8_pack_launch(ctx->num_sms, rows, k, x, x_stride, dtype, codes, scales, (cudaStream_t)stream);
+    float* const scales = (float*)(codes + up((size_t)rows * i8_pitch_within(k)));
+    const cudaError_t e = galv_i8_pack_launch(ctx->num_sms, rows, k, x, x_stride, dtype, codes, i8_pitch_within(k), scales, (cudaStream_t)stream);
     if (e != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
-    return whole_launch(ctx, "galv_i8_linear", rows, experts, n, k, ends, codes, scales, w_codes, w_scales, bias, y, y_stride, dtype, true, (cudaStream_t)stream);
+    return whole_launch(ctx, "galv_i8_linear", rows, experts, n, k, ends, codes, i8_pitch_within(k), scales, w_codes, w_scales, bias, y, y_stride, dtype, true, (cudaStream_t)stream);
 }

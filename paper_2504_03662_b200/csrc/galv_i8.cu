@@ -135,32 +135,32 @@ __global__ void __launch_bounds__(kMxThreads) i8_unpack_kernel(const MxSpread sp
 }
 
 template <typename T, bool VEC, int WARPS>
-void launch_pack(int num_sms, int64_t rows, int64_t cols, const T* x, int64_t stride, int8_t* codes, float* scales, cudaStream_t st)
+void launch_pack(int num_sms, int64_t rows, int64_t cols, const T* x, int64_t stride, int8_t* codes, int64_t pitch, float* scales, cudaStream_t st)
 {
     constexpr int each = kWarps<WARPS> / WARPS;
     const int64_t ctas = (rows + each - 1) / each, most = (int64_t)num_sms * 32;
     tc::Launch l((unsigned)(ctas < most ? ctas : most), kWarps<WARPS> * 32, 0, 0, true, st);
-    cudaLaunchKernelEx(&l.cfg, i8_pack_kernel<T, VEC, WARPS>, (long long)rows, (int)cols, (int)(i8_pitch(cols) / 8), x, (long long)stride, codes, scales);
+    cudaLaunchKernelEx(&l.cfg, i8_pack_kernel<T, VEC, WARPS>, (long long)rows, (int)cols, (int)(pitch / 8), x, (long long)stride, codes, scales);
 }
 
 // As many warps a row as keep all of it in registers (up to 32768 columns), and 8 where there are few rows.
 template <typename T, bool VEC>
-void pack_by_size(int num_sms, int64_t rows, int64_t cols, const T* x, int64_t stride, int8_t* codes, float* scales, cudaStream_t st)
+void pack_by_size(int num_sms, int64_t rows, int64_t cols, const T* x, int64_t stride, int8_t* codes, int64_t pitch, float* scales, cudaStream_t st)
 {
-    if (cols > 16384) launch_pack<T, VEC, 32>(num_sms, rows, cols, x, stride, codes, scales, st);
-    else if (cols > 8192) launch_pack<T, VEC, 16>(num_sms, rows, cols, x, stride, codes, scales, st);
-    else if (cols > 4096 || (cols > 256 && rows <= 2 * num_sms)) launch_pack<T, VEC, 8>(num_sms, rows, cols, x, stride, codes, scales, st);
-    else if (cols > 2048) launch_pack<T, VEC, 4>(num_sms, rows, cols, x, stride, codes, scales, st);
-    else if (cols > 1024) launch_pack<T, VEC, 2>(num_sms, rows, cols, x, stride, codes, scales, st);
-    else launch_pack<T, VEC, 1>(num_sms, rows, cols, x, stride, codes, scales, st);
+    if (cols > 16384) launch_pack<T, VEC, 32>(num_sms, rows, cols, x, stride, codes, pitch, scales, st);
+    else if (cols > 8192) launch_pack<T, VEC, 16>(num_sms, rows, cols, x, stride, codes, pitch, scales, st);
+    else if (cols > 4096 || (cols > 256 && rows <= 2 * num_sms)) launch_pack<T, VEC, 8>(num_sms, rows, cols, x, stride, codes, pitch, scales, st);
+    else if (cols > 2048) launch_pack<T, VEC, 4>(num_sms, rows, cols, x, stride, codes, pitch, scales, st);
+    else if (cols > 1024) launch_pack<T, VEC, 2>(num_sms, rows, cols, x, stride, codes, pitch, scales, st);
+    else launch_pack<T, VEC, 1>(num_sms, rows, cols, x, stride, codes, pitch, scales, st);
 }
 
 }  // namespace
 
-cudaError_t galv_i8_pack_launch(int num_sms, int64_t rows, int64_t cols, const void* x, int64_t stride, int32_t dtype, int8_t* codes, float* scales, cudaStream_t st)
+cudaError_t galv_i8_pack_launch(int num_sms, int64_t rows, int64_t cols, const void* x, int64_t stride, int32_t dtype, int8_t* codes, int64_t pitch, float* scales, cudaStream_t st)
 {
-    MX_DISPATCH_TYPE(dtype, if (mx_rows16(x, stride, dtype)) pack_by_size<T, true>(num_sms, rows, cols, (const T*)x, stride, codes, scales, st);
-                     else pack_by_size<T, false>(num_sms, rows, cols, (const T*)x, stride, codes, scales, st));
+    MX_DISPATCH_TYPE(dtype, if (mx_rows16(x, stride, dtype)) pack_by_size<T, true>(num_sms, rows, cols, (const T*)x, stride, codes, pitch, scales, st);
+                     else pack_by_size<T, false>(num_sms, rows, cols, (const T*)x, stride, codes, pitch, scales, st));
     return cudaGetLastError();
 }
 
@@ -175,7 +175,7 @@ extern "C" int galv_i8_pack(galv_ctx* ctx, int64_t rows, int64_t cols, const voi
         return galv_set_error(ctx, GALV_ERR_INVALID_ARG, "galv_i8_pack: NULL or misaligned pointer, or a row stride below cols");
     MxDevice dev(ctx);
     if (dev.err != cudaSuccess) return galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(dev.err));
-    const cudaError_t e = galv_i8_pack_launch(ctx->num_sms, rows, cols, x, x_stride, dtype, codes, scales, (cudaStream_t)stream);
+    const cudaError_t e = galv_i8_pack_launch(ctx->num_sms, rows, cols, x, x_stride, dtype, codes, i8_pitch(cols), scales, (cudaStream_t)stream);
     return e == cudaSuccess ? GALV_OK : galv_set_error(ctx, GALV_ERR_CUDA, cudaGetErrorString(e));
 }
 

@@ -62,8 +62,8 @@ def unpack(p: Packed, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
 
 
 def _room(rows: int, cols: int) -> int:
-    """Bytes of workspace in which a product puts its input into 8-bit integers: codes, then scales, each in whole pieces of 256."""
-    return (rows * pitch(cols) + 255 & ~255) + (rows * 4 + 255 & ~255)
+    """Bytes of workspace in which a product puts its input into 8-bit integers: codes in rows of whole pieces of 32, then scales, each in whole pieces of 256."""
+    return (rows * ((cols + 31) // 32 * 32) + 255 & ~255) + (rows * 4 + 255 & ~255)
 
 
 def _beside(cols: int, b: Packed):
