@@ -546,10 +546,14 @@ int galv_i8_linear(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int6
  * Sums are fp32 (the first three by the tensor cores, which may cut an addition where rounding would halve the error; dw's over 768 rows at most, then by
  * rounded additions), biases and base are added in fp32, results rounded once.  dw, base [experts][n][k] contiguous of `dw_dtype`, db [experts][n] of
  * `db_dtype` (`dtype` or GALV_F32); base NULL: zero; dw may be base.  An expert without rows has base or zeros for its gradient.  The order of
- * the sums is fixed by sizes, ends, strides and alignment.  Operands whose rows do not start on 16-byte boundaries are moved to ones that do, in the
- * workspace, where weight gradients of few tiles and long experts keep the sums of parts of their rows too (256-byte aligned, the bytes that the query gives for the same sizes, pointers and strides; 0: may be NULL).  After galv_expert_matmul it holds
- * x, if that was moved, [rows] rows ceil(k / 8) * 8 apart, and from the next multiple of 256 bytes on w, if that was moved, its rows as far apart.
+ * the sums is fixed by sizes, ends, strides and alignment.  An operand is moved to 16-byte boundaries, in the workspace, where its rows do not all start on such (its pointer
+ * or 2 * stride is no multiple of 16) or lie too far apart for bulk copies (x, dy: 2 * stride >= 2^40; w: 2 * n * w_stride >= 2^40).  Weight gradients of few tiles and long experts keep the
+ * sums of parts of their rows there too.  workspace: 256-byte aligned, the bytes that the query gives for the same sizes, pointers and strides; 0: may be NULL.
+ * After galv_expert_matmul it holds x, if that was moved, its rows galv_expert_pitch(k) elements apart with zeros behind their ends, and from the next multiple of 256 bytes
+ * on w, if that was moved, its experts * n rows as far apart: operands of galv_expert_backward that need not be moved again.
  */
+/* Elements from one row of cols 16-bit numbers to the next where the library has moved it (0: cols outside the limits). */
+int64_t galv_expert_pitch(int64_t cols);
 size_t galv_expert_matmul_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* x,
                                           int64_t x_stride, const void* w, int64_t w_stride);
 int galv_expert_matmul(galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const int32_t* ends, const void* x,

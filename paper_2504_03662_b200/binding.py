@@ -50,7 +50,7 @@ EXPORTS = ("galv_create", "galv_destroy", "galv_strerror", "galv_last_error", "g
            "galv_i8_matmul", "galv_i8_linear_workspace_bytes", "galv_i8_linear", "galv_expert_matmul_workspace_bytes",
            "galv_expert_matmul", "galv_expert_input_grad_workspace_bytes", "galv_expert_input_grad",
            "galv_expert_weight_grad_workspace_bytes", "galv_expert_weight_grad", "galv_expert_bias_grad",
-           "galv_expert_backward_workspace_bytes", "galv_expert_backward")
+           "galv_expert_backward_workspace_bytes", "galv_expert_backward", "galv_expert_pitch")
 
 
 class galv_shape(C.Structure):
@@ -132,6 +132,7 @@ def load_library() -> C.CDLL:
     lib.galv_i8_matmul.argtypes = [vp, i64, i32, i64, i64] + [vp] * 7 + [i64, i32, vp]
     lib.galv_i8_linear_workspace_bytes.argtypes, lib.galv_i8_linear_workspace_bytes.restype = [i64, i64], sz
     lib.galv_i8_linear.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, vp, vp, vp, i64, i32, vp, sz, vp]
+    lib.galv_expert_pitch.argtypes, lib.galv_expert_pitch.restype = [i64], i64
     for f in (lib.galv_expert_matmul_workspace_bytes, lib.galv_expert_input_grad_workspace_bytes):
         f.argtypes, f.restype = [vp, i64, i32, i64, i64, vp, i64, vp, i64], sz
     lib.galv_expert_matmul.argtypes = [vp, i64, i32, i64, i64, vp, vp, i64, vp, i64, vp, vp, i64, i32, vp, sz, vp]
@@ -429,6 +430,9 @@ class Galv:
                                      *_ws(workspace), _raw_stream(self.device))
         if rc:
             self._check(rc)
+
+    def galv_expert_pitch(self, cols) -> int:
+        return self.lib.galv_expert_pitch(cols)
 
     def galv_expert_matmul_workspace_bytes(self, rows, experts, n, k, x, w) -> int:
         return self.lib.galv_expert_matmul_workspace_bytes(self.h, rows, experts, n, k, *x, *w)

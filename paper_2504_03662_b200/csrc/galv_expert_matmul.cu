@@ -622,6 +622,8 @@ int whole_may(galv_ctx* ctx) { return mx_may_run(ctx, "8-bit product: the librar
 
 }  // namespace
 
+extern "C" int64_t galv_expert_pitch(int64_t cols) { return mx_size_ok(0, cols) ? galv_aligned_pitch(cols) : 0; }
+
 extern "C" size_t galv_expert_matmul_workspace_bytes(const galv_ctx* ctx, int64_t rows, int32_t experts, int64_t n, int64_t k, const void* x, int64_t x_stride, const void* w,
                                                      int64_t w_stride)
 {

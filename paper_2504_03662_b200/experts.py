@@ -131,8 +131,7 @@ def _moved(x: torch.Tensor, weight: torch.Tensor, ws: Optional[torch.Tensor]):
     if ws is None:
         return x, weight
     (rows, k), (experts, n, _) = x.shape, weight.shape
-    each = 64 if k >= 512 else 16                         # as the library places them
-    pitch, at, both = (k + each - 1) // each * each, 0, ws.view(x.dtype)
+    pitch, at, both = gb.load_library().galv_expert_pitch(k), 0, ws.view(x.dtype)
     start, stride = gb._matrix(x)
     if start % 16 or stride % 8 or stride >= 1 << 39:
         x, at = both.as_strided((rows, k), (pitch, 1)), (rows * pitch * 2 + 255 & ~255) // 2

@@ -85,6 +85,14 @@ def test_calls_without_a_context_are_refused():
     assert lib.galv_expert_matmul_workspace_bytes(None, 1, 1, 1, 1, None, 1, None, 1) == lib.galv_expert_weight_grad_workspace_bytes(None, 1, 1, 1, 1, None, 1, None, 1) == 0
 
 
+def test_distance_of_moved_rows():
+    lib = gb.load_library()
+    for cols in [*range(1, 1400), 2 ** 20 + 1, 2 ** 31 - 129]:
+        pitch = lib.galv_expert_pitch(cols)
+        assert pitch % 8 == 0 and cols <= pitch < cols + 64
+    assert lib.galv_expert_pitch(0) == lib.galv_expert_pitch(-5) == lib.galv_expert_pitch(2 ** 31 - 128) == 0
+
+
 B = torch.bfloat16
 X, W, E3 = torch.zeros(6, 64, dtype=B), torch.zeros(3, 8, 64, dtype=B), torch.zeros(3, dtype=torch.int32)
 W8 = i8.Packed(torch.zeros(24, 64, dtype=torch.int8), torch.zeros(24), 24, 64)
@@ -440,6 +448,46 @@ def test_strides_and_views(dtype):
     strided = torch.zeros(6, dtype=torch.int32, device="cuda")
     strided[::2] = ends
     assert torch.equal(experts.matmul(x, w, strided[::2], bias), want[0])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("k", [7, 100, 511, 513, 1365])
+@pytest.mark.parametrize("odd", ["both", "x", "w"])
+def test_what_the_forward_product_has_moved_lies_where_the_header_says(k, odd, dtype):
+    """Of operands off 16-byte boundaries: read back by the header's rule, and handed on to the three gradients in one call."""
+    g, counts, n = mx.context(0), [60, 0, 17], 40
+    rows, E, number = sum(counts), len(counts), gb._DTYPES[DT[dtype]]
+    x, w, dy, _ = inputs(counts, 0, n, k, dtype)
+    ends, wide = ends_of(counts), (k + 7) // 8 * 8
+    apart = lambda t: torch.zeros(*t.shape[:-1], wide, dtype=t.dtype, device="cuda")[..., :k].copy_(t)      # rows that bulk copies take as they are
+    xv, wv = x if odd != "w" else apart(x), w if odd != "x" else apart(w)
+    xm, wm = gb._matrix(xv), gb._matrices(wv)
+    ws = torch.full((g.galv_expert_matmul_workspace_bytes(rows, E, n, k, xm, wm),), 255, dtype=torch.uint8, device="cuda")
+    y = torch.empty(rows, n, dtype=x.dtype, device="cuda")
+    g.galv_expert_matmul(rows, E, n, k, ends, xm, wm, None, (y.data_ptr(), n), number, ws)
+    pitch, at = g.galv_expert_pitch(k), 0
+    assert pitch >= k and pitch % 8 == 0
+    back = []
+    for t, view, moved in ((x, xv, odd != "w"), (w, wv, odd != "x")):
+        count = t.numel() // k
+        if moved:
+            held = ws[at:at + count * pitch * 2].view(x.dtype).view(*t.shape[:-1], pitch)
+            assert torch.equal(held[..., :k], t) and not held[..., k:].any()
+            at += (count * pitch * 2 + 255) & ~255
+            back.append(held[..., :k])
+        else:
+            back.append(view)
+    assert at == ws.numel()
+    operands = gb._matrix(dy), gb._matrix(back[0]), gb._matrices(back[1])
+    size = g.galv_expert_backward_workspace_bytes(rows, E, n, k, *operands)
+    assert size == 0                                                                 # nothing is moved again
+    dx, dw, db = torch.empty(rows, k, dtype=x.dtype, device="cuda"), torch.empty(E, n, k, dtype=x.dtype, device="cuda"), torch.empty(E, n, dtype=x.dtype, device="cuda")
+    g.galv_expert_backward(rows, E, n, k, ends, *operands, number, (dx.data_ptr(), k), dw, db, None)
+    assert torch.equal(y, experts.matmul(x, w, ends)) and torch.equal(dx, experts.input_grad(dy, w, ends))
+    assert torch.equal(dw, experts.weight_grad(dy, x, ends)) and torch.equal(db, experts.bias_grad(dy, ends))
+    kept = experts._moved(xv, wv, ws)                                                # what the differentiable function keeps
+    assert torch.equal(kept[0], x) and torch.equal(kept[1], w) and [t.data_ptr() for t in kept] == [t.data_ptr() for t in back]
 
 
 # ------------------------------------------------------------------------------------------------- as a differentiable function
