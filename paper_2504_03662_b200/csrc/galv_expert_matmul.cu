@@ -144,7 +144,7 @@ expert_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_co
     const int units = before[a.experts] * a.tiles_m, stage = kRowsBytes + most / 2 * kChunkBytes, stages = min(kStagesMost, kRing / stage);
 
     auto waited = [&](uint32_t bar, uint32_t parity) {
-        if (tc::bar_wait_own(bar, parity)) return true;
+        if (tc::bar_wait_asleep<true>(bar, parity)) return true;
         *(volatile int*)&failed = 1;
         return false;
     };
@@ -350,7 +350,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_consta
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
 
     auto waited = [&](uint32_t bar, uint32_t parity) {
-        if (tc::bar_wait_own(bar, parity)) return true;
+        if (tc::bar_wait_asleep<false>(bar, parity)) return true;
         *(volatile int*)&failed = 1;
         return false;
     };
@@ -407,7 +407,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_consta
                 if (++s == stages) s = 0, turn ^= 1;
             }
             tc::mma_commit<1>(acc_full);                  // also after a wait that ran out: nothing may be in flight when the memory goes
-            tc::bar_wait_own(acc_full, 0);
+            tc::bar_wait_asleep<false>(acc_full, 0);
         }
     }
     __syncwarp();

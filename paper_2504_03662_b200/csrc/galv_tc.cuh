@@ -65,17 +65,24 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity)
     } while (clock64() - start < 4000000000ll);
     return false;
 }
-// ... what this CTA's threads and bulk copies wrote, and what the tensor cores did.
-__device__ __forceinline__ bool bar_wait_own(uint32_t bar, uint32_t parity)
+// The same asleep between tries.  OTHERS false: only what this CTA's threads and bulk copies wrote can be read, and what the tensor cores did; not for barriers that
+// another CTA arrives at, or that its copies tell.
+template <bool OTHERS> __device__ __forceinline__ bool bar_try_asleep(uint32_t bar, uint32_t parity)
 {
-    constexpr uint32_t sleep = 1000000;                   // nanoseconds at most that a try may take, asleep
+    constexpr uint32_t sleep = 1000000;                   // nanoseconds at most that a try may take
     uint32_t done;
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity), "r"(sleep) : "memory");
-    if (done) return true;
+    if (OTHERS)
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity), "r"(sleep) : "memory");
+    else
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity), "r"(sleep) : "memory");
+    return done != 0;
+}
+template <bool OTHERS> __device__ __forceinline__ bool bar_wait_asleep(uint32_t bar, uint32_t parity)
+{
+    if (bar_try_asleep<OTHERS>(bar, parity)) return true;
     const long long start = clock64();
     do {
-        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity), "r"(sleep) : "memory");
-        if (done) return true;
+        if (bar_try_asleep<OTHERS>(bar, parity)) return true;
     } while (clock64() - start < 4000000000ll);
     return false;
 }

@@ -574,6 +574,27 @@ def test_captured_with_other_ends():
 
 
 @gpu
+@pytest.mark.parametrize("n", [1280, 1152, 1040])
+def test_tiles_whose_sums_are_short(n):
+    """One chunk a tile and ten tiles a pair of CTAs: each accumulator is summed into again as soon as both have moved it out.  n leaves the second of a pair all of the last tile's
+    columns or none, and the first all or 16.  Whole numbers, with which nothing rounds."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    counts, rows = [20011, 0, 17, 19001], 39100
+    ends = ends_of(counts)
+    spans = clamped(ends, rows)
+    draw = lambda most, *s: torch.randint(-most, most + 1, s, generator=g, device="cuda")
+    plain = lambda u, v: torch.cat([u[a:b].float() @ v[e].float() for e, (a, b) in enumerate(spans)] + [torch.zeros(rows - spans[-1][1], v.shape[2], device="cuda")])
+    x, w = draw(1, rows, 64).to(B), draw(1, 4, n, 64).to(B)
+    qx, qw = draw(127, rows, 64).to(torch.int8), draw(127, 4, n, 64).to(torch.int8)
+    px, pw = i8.Packed(qx, torch.ones(rows, device="cuda"), rows, 64), i8.Packed(qw, torch.ones(4 * n, device="cuda"), 4 * n, 64)
+    dy, wt = draw(1, rows, 64).to(B), draw(1, 4, 64, n).to(B)
+    want = plain(x, w.transpose(1, 2)), plain(qx, qw.transpose(1, 2)), plain(dy, wt)
+    for _ in range(10):
+        got = experts.matmul(x, w, ends), experts.matmul(px, pw, ends, dtype=torch.float32), experts.input_grad(dy, wt, ends)
+        assert all(torch.equal(a.float(), b) for a, b in zip(got, want))
+
+
+@gpu
 def test_one_behind_the_other_eager_and_captured():
     """Kernels may begin before the one in front of them is over: each result is the next call's input or weights, fills and copies and other streams' work lie between, and a second
     replay finds what the first has left."""
