@@ -139,6 +139,8 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
         *(volatile int*)&failed = 1;
         return false;
     };
+    // Every lane waits and may read what is written; all go the same way, also where the limit ends between two lanes' tries: what follows takes whole warps.
+    auto warp_waited = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, waited(bar, parity)) != 0; };
 
     if (warp == 0) {
         if (tc::elect()) {
@@ -183,7 +185,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
             const int chunks = (w.count + kTokens - 1) / kTokens, s = (it + chunks - 1) % kStages;
             it += chunks;
             if (w.count % 16 == 0) continue;
-            if (!__all_sync(0xffffffffu, waited(own + 8 * s, turns >> s & 1))) break;
+            if (!warp_waited(own + 8 * s, turns >> s & 1)) break;
             turns ^= 1u << s;
             clear_rows(base + s * kStageBytes, w.count - (chunks - 1) * kTokens);
             tc::fence_async();
@@ -233,9 +235,8 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
         };
         for (int u = first; u < units && ok; u += stride) {
             const Unit w = unit_of(a, begin, u);
-            const long long r0 = (long long)w.tn * kTile + rank * kHalf + quad * 32, c0 = (long long)w.tk * kTile + half * 128;
-            const int rows = (int)max(-64ll, min(32ll, a.n - r0)), cols = (int)max(-128ll, min(128ll, a.k - c0));
-            const bool some = rows > 0 && cols > 0;
+            const unsigned r0 = (unsigned)w.tn * kTile + rank * kHalf + quad * 32, c0 = (unsigned)w.tk * kTile + half * 128;      // may pass 2^31
+            const bool some = r0 < a.n && c0 < a.k;
             auto fetch = [&](int c) {                      // base's piece, once the copy before has read this memory
                 fetched = true;
                 if (lane == 0) {
@@ -252,7 +253,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
                 for (int i = 0; i < 128; ++i) sum[i] = 0.f;
                 for (int left = w.count; left > 0; left -= kSegment * kTokens) {
                     acc = done & 1;
-                    if (!(ok = waited(acc_full + 8 * acc, done / 2 & 1))) break;
+                    if (!(ok = warp_waited(acc_full + 8 * acc, done / 2 & 1))) break;
                     tc::fence_after();
 #pragma unroll
                     for (int j = 0; j < 128; j += 16) {
@@ -267,12 +268,15 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
                         ++done;
                     }
                 }
+                if (!ok) break;
 #pragma unroll
                 for (int j = 0; j < 128; j += 16) tc::tmem_store16(from + acc * kTile + j, sum + j);
                 tc::tmem_wait_store();
-            } else if (w.count > 0 && (ok = waited(acc_full + 8 * acc, done / 2 & 1))) {
+            } else if (w.count > 0) {
+                if (!(ok = warp_waited(acc_full + 8 * acc, done / 2 & 1))) break;
                 tc::fence_after();
             }
+            const int rows = (int)max(-64ll, min(32ll, a.n - r0)), cols = (int)max(-128ll, min(128ll, a.k - c0));
             if (a.boxes) {
                 if (some)
 #pragma unroll 1
@@ -289,7 +293,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
                             for (int i = 0; i < piece; ++i) v[i] = 0;
                         }
                         if (a.base) {
-                            ok = waited(base_bar, phase) && ok;
+                            if (!(ok = warp_waited(base_bar, phase))) break;
                             phase ^= 1;
                             fetched = false;
                         } else {
@@ -311,7 +315,7 @@ expert_grad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_cons
                             tc::stores_end();
                         }
                     }
-            } else if (ok) {
+            } else {
                 const long long at = w.part * a.n * a.k + r0 * a.k + c0;
                 const O* const b = a.base ? (const O*)a.base + at : nullptr;
                 if (sizeof(O) == 4 || !b) {
