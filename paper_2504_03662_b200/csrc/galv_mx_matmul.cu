@@ -155,6 +155,8 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constan
         *(volatile int*)&failed = 1;
         return false;
     };
+    // All lanes of a warp go the same way, also where the limit ends between two lanes' tries: what follows takes whole warps.
+    auto warp_waited = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, waited(bar, parity)) != 0; };
 
     if (warp == 0) {
         if (tc::elect()) {
@@ -240,7 +242,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constan
         for (int u = first; u < units; u += stride, ++done) {
             const Unit w = unit_of(a, u);
             const uint32_t buf = done & 1;
-            if (!waited(acc_full + 8 * buf, done / 2 & 1)) break;
+            if (!warp_waited(acc_full + 8 * buf, done / 2 & 1)) break;
             tc::fence_after();
             const int lr = a.vec ? lane / 4 : lane / 16, lc = a.vec ? lane % 4 * 4 : lane % 16;
             const long long r0 = (long long)w.tm * kTile + rank * kHalf + quad * 32, c0 = (long long)w.tn * kTile;
@@ -341,6 +343,8 @@ mx_matmul_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
         *(volatile int*)&failed = 1;
         return false;
     };
+    // All lanes of a warp go the same way, also where the limit ends between two lanes' tries: what follows takes whole warps.
+    auto warp_waited = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, waited(bar, parity)) != 0; };
 
     if (warp == 0) {
         if (tc::elect()) {
@@ -392,7 +396,7 @@ mx_matmul_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_con
     const int quad = warp - 4, row = quad * 32 + lane, mine = N / ranks;      // a thread has one row of b; this CTA finishes `mine` rows of a
     bool ok = true;
     if (warp >= 4) {
-        ok = waited(acc_full, 0);
+        ok = warp_waited(acc_full, 0);
         tc::fence_after();
         if (ok) {
 #pragma unroll 1

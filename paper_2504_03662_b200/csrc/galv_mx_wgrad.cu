@@ -185,6 +185,8 @@ mx_wgrad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constan
         *(volatile int*)&failed = 1;
         return false;
     };
+    // All lanes of a warp go the same way, also where the limit ends between two lanes' tries: what follows takes whole warps.
+    auto warp_waited = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, waited(bar, parity)) != 0; };
 
     if (warp < 4) fewer_registers<kRegsIssue>();
     if (warp == 0) {                                      // copies of codes and scales
@@ -283,7 +285,7 @@ mx_wgrad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constan
                 for (int i = 0; i < 128; ++i) sum[i] = 0.f;
                 for (int c = w.c0; c < w.c1; c += kSegment) {
                     buf = done & 1;
-                    if (!(ok = waited(acc_full + 8 * buf, done / 2 & 1))) break;
+                    if (!(ok = warp_waited(acc_full + 8 * buf, done / 2 & 1))) break;
                     tc::fence_after();
 #pragma unroll
                     for (int j = 0; j < 128; j += 16) {
@@ -300,13 +302,14 @@ mx_wgrad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constan
                         ++done;
                     }
                 }
+                if (!ok) break;
 #pragma unroll
                 for (int j = 0; j < 128; j += 16) tc::tmem_store16(from + buf * 256 + j, sum + j);
                 tc::tmem_wait_store();
-            } else if ((ok = waited(acc_full + 8 * buf, done / 2 & 1))) {
+            } else {
+                if (!(ok = warp_waited(acc_full + 8 * buf, done / 2 & 1))) break;
                 tc::fence_after();
             }
-            if (!ok) break;
             const long long r0 = (long long)w.tn * kTile + rank * kHalf + quad * 32, c0 = (long long)w.tk * kTile + half * 128;
             const int rows = (int)min(32ll, a.n - r0), cols = (int)min(128ll, a.k - c0);
             const long long at = (r0 + (a.vec ? lane / 4 : lane / 16)) * a.k + c0 + (a.vec ? lane % 4 * 4 : lane % 16);
@@ -330,7 +333,7 @@ mx_wgrad_kernel(const __grid_constant__ CUtensorMap dy_map, const __grid_constan
             for (int ch = w.c0; ch < w.c1; ++ch, ++it) {
                 if (it % kRestoreGroups != group) continue;
                 const int s = it % kCodeRing, x = it % kXRing;
-                if (!(ok = waited(code_full + 8 * s, it / kCodeRing & 1) && waited(x_empty + 8 * x, (it / kXRing & 1) ^ 1))) break;
+                if (!(ok = warp_waited(code_full + 8 * s, it / kCodeRing & 1) && warp_waited(x_empty + 8 * x, (it / kXRing & 1) ^ 1))) break;
                 uint32_t byte[2][2], from[2], to[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i)

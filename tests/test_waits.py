@@ -27,7 +27,7 @@ def without(text, opening):
     return text
 
 
-@pytest.mark.parametrize("name", ["galv_expert_matmul.cu", "galv_expert_grad.cu"])
+@pytest.mark.parametrize("name", ["galv_expert_matmul.cu", "galv_expert_grad.cu", "galv_mx_matmul.cu", "galv_mx_wgrad.cu"])
 def test_warps_decide_as_one_where_they_go_on_together(name):
     with open(os.path.join(CSRC, name)) as f:
         text = re.sub(r"//[^\n]*", "", f.read())
