@@ -119,7 +119,7 @@ def _forward(x: torch.Tensor, weight: torch.Tensor, ends: torch.Tensor, bias: Op
 
 
 def _lie(n: int, *matrices) -> bool:
-    """Whether rows start on 16-byte boundaries, nearer to one another than the library's limit: then it moves nothing."""
+    """Whether rows start on 16-byte boundaries, nearer to one another than the header's limit: then the library moves nothing."""
     for start, stride in matrices:
         if start and (start % 16 or stride % 8 or n * stride >= 1 << 39):
             return False
@@ -228,7 +228,7 @@ class _Linear(torch.autograd.Function):
         g = _on(device)
         dm, xm, wm = gb._matrix(dy), gb._matrix(x) if need_w else (None, 0), gb._matrices(weight)
         ws = None
-        if not _lie(n, dm, xm, wm) or (need_w and rows >= 2048 * experts and experts * -(-n // 256) * -(-k // 256) < 64):      # few tiles: the library may split rows
+        if need_w or not _lie(n, dm, xm, wm):             # weight gradients may keep sums of parts of their rows there: the library says so
             size = g.galv_expert_backward_workspace_bytes(rows, experts, n, k, dm, xm, wm)
             ws = _bytes(size, device) if size else None
         g.galv_expert_backward(rows, experts, n, k, ends, dm, xm, wm, gb._DTYPES[dtype], (dx.data_ptr(), k) if need_x else (None, 0), dw, db, ws)

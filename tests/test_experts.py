@@ -93,6 +93,33 @@ def test_distance_of_moved_rows():
     assert lib.galv_expert_pitch(0) == lib.galv_expert_pitch(-5) == lib.galv_expert_pitch(2 ** 31 - 128) == 0
 
 
+@pytest.mark.parametrize("need", [(1, 1, 1), (0, 1, 0), (1, 0, 1)])
+@pytest.mark.parametrize("rows,n,k", [(6, 8, 64), (4096, 256, 256), (5, 3, 7)])
+def test_gradients_get_the_workspace_that_the_library_asks_for(rows, n, k, need, monkeypatch):
+    """A library that wants one for every weight gradient, and for whatever is off 16-byte boundaries: how it splits rows is its own affair."""
+    given = []
+
+    class Library:
+        def galv_expert_matmul_workspace_bytes(self, *a):
+            return 0
+
+        def galv_expert_matmul(self, *a):
+            pass
+
+        def galv_expert_backward_workspace_bytes(self, rows, experts, n, k, dy, x, w):
+            return 512 if x[0] or dy[1] % 8 or w[1] % 8 else 0
+
+        def galv_expert_backward(self, *a):
+            given.append(a)
+
+    monkeypatch.setattr(experts, "_on", lambda *a: Library())
+    leaves = [torch.zeros(s, dtype=torch.bfloat16).requires_grad_(bool(r)) for s, r in zip(((rows, k), (2, n, k), (2, n)), need)]
+    experts.linear(leaves[0], leaves[1], torch.zeros(2, dtype=torch.int32), leaves[2]).sum().backward()
+    (*_, dx, dw, db, ws), = given
+    assert [dx[0] is not None, dw is not None, db is not None] == [bool(r) for r in need]
+    assert (ws is not None and ws.numel() == 512) if need[1] or n % 8 or k % 8 else ws is None
+
+
 B = torch.bfloat16
 X, W, E3 = torch.zeros(6, 64, dtype=B), torch.zeros(3, 8, 64, dtype=B), torch.zeros(3, dtype=torch.int32)
 W8 = i8.Packed(torch.zeros(24, 64, dtype=torch.int8), torch.zeros(24), 24, 64)
@@ -488,6 +515,26 @@ def test_what_the_forward_product_has_moved_lies_where_the_header_says(k, odd, d
     assert torch.equal(dw, experts.weight_grad(dy, x, ends)) and torch.equal(db, experts.bias_grad(dy, ends))
     kept = experts._moved(xv, wv, ws)                                                # what the differentiable function keeps
     assert torch.equal(kept[0], x) and torch.equal(kept[1], w) and [t.data_ptr() for t in kept] == [t.data_ptr() for t in back]
+
+
+@gpu
+def test_what_lies_right_is_not_moved():
+    """The rule that saves asking the library, against what it says: operands of all starts, distances and sizes."""
+    g, lie = mx.context(0), experts._lie
+    for n, k in ((1, 1), (8, 8), (40, 7), (33, 64), (1365, 2731), (4096, 4096)):
+        for at in (0, 2, 8, 16, 256):
+            for pad in (0, 1, 4, 8, 24, 1 << 39):
+                for rows, e in ((100, 1), (100, 5), (50000, 1), (50000, 5)):      # more are split in parts
+                    x, w, dy = (4096 + at, k + pad), (8192 + at // 2 * 2, k + pad), (1 << 20, n + pad)
+                    sizes = rows, e, n, k
+                    if lie(n, x, w):
+                        assert g.galv_expert_matmul_workspace_bytes(*sizes, x, w) == 0
+                    else:                                                            # the rows' limit is taken for the matrices' too
+                        assert g.galv_expert_matmul_workspace_bytes(*sizes, x, w) > 0 or n * (k + pad) >= 1 << 39
+                    if lie(n, dy, w):
+                        assert g.galv_expert_backward_workspace_bytes(*sizes, dy, (None, 0), w) == 0
+                    if lie(n, dy, x):
+                        assert g.galv_expert_backward_workspace_bytes(*sizes, dy, x, (None, 0)) == g.galv_expert_backward_workspace_bytes(*sizes, (1 << 20, 4096), (1 << 21, 4096), (None, 0))
 
 
 # ------------------------------------------------------------------------------------------------- as a differentiable function
