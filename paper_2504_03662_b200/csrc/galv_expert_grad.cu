@@ -6,11 +6,10 @@
 // zero times what lies there could be NaN.
 // Per CTA: a thread that starts bulk tensor copies (both CTAs' tell the first one's barrier, those of a chunk with such rows their own), a warp that sets such rows to zero and then tells the
 // first one's barrier, a thread (of the first) that issues the matrix instructions for the pair, eight warps that take sums from the tensor memory while the next are made and move results out.
-
 //
-// Bound by the loop of copies and matrix instructions: 16 experts of 8192 rows in all, 4096 x 2048 into bf16, take 124 us (1.1 PFLOP/s; the matrix instructions alone 79, with copies 99: shared
-// memory and L2 have both at a time); 8 experts of 16384 rows, 2048 x 8192 onto an fp32 base, 472 us (1.16 PFLOP/s, 3.0 TB/s); 24 experts of 300 rows, 1365 x 2048 into fp16, 38.6 us, which is what
-// the card writes (3.5 TB/s; zeros of this size go at 3.7).
+// Bound by the loop of copies and matrix instructions: 8192 rows over 16 experts, 4096 x 2048 into bf16, take 126 us (1.1 PFLOP/s; the matrix instructions alone 79, with copies 99: shared
+// memory and L2 have both at a time); 16384 rows over 8 experts, 2048 x 8192 onto an fp32 base, 468 us (1.17 PFLOP/s, 3.0 TB/s); 300 rows over 24 experts, 1365 x 2048 into fp16, 38.3 to 39.8 us,
+// which is what the card writes (3.5 TB/s; zeros of this size go at 3.7).
 
 #include "galv_experts.cuh"
 #include "galv_tc.cuh"

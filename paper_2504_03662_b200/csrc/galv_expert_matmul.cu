@@ -9,9 +9,9 @@
 // first one's barrier), one (in the first) that issues the matrix instructions for the pair, eight warps that move
 // sums from the tensor memory to y while the next are made (two accumulators fill it).
 //
-// Bound by the tensor cores at the clock that the card's power allows: 8 experts of 16384 rows, 8192 x 2048 in bf16, take 366 us (1.5 PFLOP/s, tensor pipe active 93 % of the cycles), 429 in a loop of
-// seconds (a library product of that size 416); 4096 x 8192 x 32768 in 8-bit integers 622 us (3.5 POP/s, 98 %), 745 in such a loop (763).  The input gradient of 16 experts, 8192 rows, 4096 x 2048: 106 to 116 us
-// (79 %: five rounds of tiles where four and a half would do).
+// Bound by the tensor cores at the clock that the card's power allows: 16384 rows over 8 experts, 8192 x 2048 in bf16, take 366 to 380 us (1.45 to 1.5 PFLOP/s, tensor pipe active 93 % of the cycles),
+// 429 in a loop of seconds (a library product of that size 416); 4096 x 8192 x 32768 in 8-bit integers 622 us (3.5 POP/s, 98 %), 745 in such a loop (763).  The input gradient of 8192 rows over 16 experts,
+// 4096 x 2048: 106 to 119 us (78 %: five rounds of tiles where four and a half would do).
 
 #include <stdio.h>
 

@@ -237,5 +237,6 @@ class _Linear(torch.autograd.Function):
 
 def linear(x: torch.Tensor, weight: torch.Tensor, ends: torch.Tensor, bias: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x weight[e]^T + bias[e] for each row of x and its expert e, in 16 bits, with gradients for x, weight and bias (where they are taken).  Of operands whose rows do not start
-    on 16-byte boundaries the copies that the forward product takes are kept for the backward pass."""
+    on 16-byte boundaries the copies that the forward product takes are kept for the backward pass: 2 bytes for each element and what fills its rows up, of the weights as much as they take
+    themselves, unless they are kept with rows further apart (weight.stride(1) and its start multiples of 8 elements)."""
     return _Linear.apply(x, weight, ends, bias)

@@ -12,8 +12,8 @@ their inputs, as they do without.
 A context of the library belongs to one host thread, so every thread (the autograd engine's among them) gets its own
 for each device.
 
-Waits inside the kernels of `weight_grad` and `matmul` are bounded (two seconds).  Where one has run out, the results since
-then are void: the next call of either on the device raises binding.GalvError with ERR_TIMEOUT, once in each thread, and so does
+Waits inside the kernels of products are bounded (two seconds): those of `weight_grad` and `matmul` here and of all that modules i8 and experts have but `pack`, `unpack`
+and `bias_grad`.  Where one has run out, the results since then are void: the next call of any of them on the device raises binding.GalvError with ERR_TIMEOUT, once in each thread, and so does
 `check`, which waits for the current stream first (call it before results are relied on, and behind replays of captured graphs, which look at nothing).
 """
 from __future__ import annotations
